@@ -429,6 +429,111 @@ int dipaco_module_sync_static(float *theta, float *momentum, int64_t numel, int3
                               int32_t path_dtype, int32_t chunk_paths, int32_t device,
                               void *cuda_stream);
 
+/*
+ * Operators of the inner phase.  Between two synchronisations every path is trained on its own shard
+ * (Algorithm 1, the inner-optimisation loop).  With the copies of hundreds of paths resident little
+ * device memory is left for activations, so the operators below keep activations in 8 bits: a block
+ * of a path runs its norm, its products and its activation on them, forward and backward, and hands
+ * gradients to an inner optimiser.  They need no context: every buffer is an argument.
+ *
+ * Conventions.  All pointers are device pointers; the calls are asynchronous on cuda_stream, allocate
+ * nothing and can be captured in a CUDA graph.  Arguments are checked before anything is launched
+ * (DIPACO_EINVAL, or DIPACO_ELIMIT for extents beyond 2^31).  A dense matrix is row-major with a row
+ * stride in elements, at any element alignment; 16-byte aligned rows are fastest.  dtype and
+ * param_dtype are DIPACO_F32 or DIPACO_BF16.  Outputs must not overlap inputs.  Extents of zero are
+ * allowed.  Every sum is fp32 and taken in an order that depends on the shapes alone: results are
+ * bitwise reproducible.
+ *
+ * Packed matrices.  8-bit codes (e4m3: 4 exponent and 3 mantissa bits, largest value 448, no infinity)
+ * with one scale for each block of 128 x 128 values, itself an 8-bit power of two (e8m0: byte b is
+ * 2^(b-127), 255 is NaN): value = code * scale.  Packing takes the least scale that brings the largest
+ * finite magnitude of the block to at most 448 (at least 2^-126; a block of zeros has scale 1) and
+ * rounds to the nearest code, ties to even; an infinity or NaN becomes a NaN code and does not
+ * influence the scale.  Blocks are square so that the scale is constant over 128 contracted values
+ * along either side: the same bytes serve a product, its input gradient and its weight gradient.
+ *   codes   rows x cols bytes, row stride `stride` bytes; 16-byte aligned, stride a multiple of 16
+ *   scales  [ceil(rows/128)][ceil(cols/128)] bytes, row-major
+ */
+typedef struct dipaco_packed {
+    void *codes;
+    void *scales;
+    int64_t rows, cols, stride;
+} dipaco_packed;
+
+/* Dense to packed, and back (a code times its scale, rounded once to dtype). */
+int dipaco_pack(const void *x, int64_t x_stride, int32_t dtype, const dipaco_packed *out, int32_t device,
+                void *cuda_stream);
+int dipaco_unpack(const dipaco_packed *x, void *y, int64_t y_stride, int32_t dtype, int32_t device,
+                  void *cuda_stream);
+
+/*
+ * Layer norm of every row:  mean = sum x / C,  var = sum (x - mean)^2 / C,
+ * rstd = 1 / sqrt(var + eps),  y = (x - mean) * rstd * gamma + beta.
+ *   gamma, beta  [cols] of param_dtype; NULL = ones, zeros
+ *   y            NULL = statistics only
+ *   mean, rstd   [rows] fp32, kept for the backward pass; NULL where not wanted
+ */
+int dipaco_layer_norm(const void *x, int64_t x_stride, const void *gamma, const void *beta, void *y,
+                      int64_t y_stride, float *mean, float *rstd, int64_t rows, int64_t cols, float eps,
+                      int32_t dtype, int32_t param_dtype, int32_t device, void *cuda_stream);
+
+/*
+ * The same with the result packed straight from its fp32 value (it feeds a product) and, unless
+ * x_packed is NULL, the input packed as the checkpoint that dipaco_layer_norm_backward reads.  The
+ * extents are those of y; mean and rstd are required and come from the exact input.
+ */
+int dipaco_layer_norm_pack(const void *x, int64_t x_stride, const void *gamma, const void *beta,
+                           const dipaco_packed *y, const dipaco_packed *x_packed, float *mean, float *rstd,
+                           float eps, int32_t dtype, int32_t param_dtype, int32_t device, void *cuda_stream);
+
+/*
+ * Gradient of the layer norm.  With h = (x - mean) * rstd and g = dy * gamma:
+ *   dx = rstd * (g - mean(g) - h * mean(g h)),  dgamma = sum over rows of dy h,  dbeta = sum of dy.
+ *   x, x_packed    exactly one of them: the input, or its 8-bit checkpoint
+ *   gamma          NULL = ones
+ *   dx             of dtype (that of dy and of a dense x); dgamma, dbeta [cols] fp32, overwritten
+ *                  (zero for no rows); each may be NULL, not all three
+ *   workspace      16-byte aligned, at least the bytes that dipaco_layer_norm_workspace reports (a
+ *                  host-only query; may be zero); not needed without dgamma and dbeta
+ */
+int dipaco_layer_norm_workspace(int64_t rows, int64_t cols, int64_t *bytes);
+int dipaco_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                               const dipaco_packed *x_packed, const float *mean, const float *rstd,
+                               const void *gamma, void *dx, int64_t dx_stride, float *dgamma, float *dbeta,
+                               int64_t rows, int64_t cols, int32_t dtype, int32_t param_dtype, void *workspace,
+                               int64_t workspace_bytes, int32_t device, void *cuda_stream);
+
+/*
+ * GELU in its tanh form, gelu(x) = x * s with s = 1 / (1 + exp(-2u)), u = sqrt(2/pi) (x + 0.044715 x^3),
+ * packed from its fp32 value, and, unless x_packed is NULL, its input packed as a checkpoint.
+ * The backward call reads that checkpoint and packs dy * gelu'(x) for the two products that follow,
+ * gelu'(x) = s + x s (1 - s) 2u'.  An infinite input gives NaN, like its product 0 * infinity.
+ */
+int dipaco_gelu_pack(const void *x, int64_t x_stride, int32_t dtype, const dipaco_packed *y,
+                     const dipaco_packed *x_packed, int32_t device, void *cuda_stream);
+int dipaco_gelu_pack_backward(const void *dy, int64_t dy_stride, int32_t dtype, const dipaco_packed *x_packed,
+                              const dipaco_packed *dx, int32_t device, void *cuda_stream);
+
+/*
+ * Product of two packed matrices on the tensor cores, C = op(A) op(B) with fp32 sums, rounded once to
+ * dtype.  op transposes its argument where the flag is nonzero.  For a layer y = x W^T with x
+ * [tokens, in] and W [out, in]:
+ *   forward          y  = x  W^T    transpose_b
+ *   input gradient   dx = dy W      neither
+ *   weight gradient  dW = dy^T x    transpose_a
+ * accumulate adds the product to C (gradients over several batches).
+ *   workspace   16-byte aligned, at least the bytes that dipaco_packed_matmul_workspace reports for
+ *               the product's extents C [m, n], contraction k (a host-only query; may be zero)
+ * Every wait inside the kernel is bounded (4 s).  A wait that runs out ends the kernel in an orderly
+ * way with undefined results; dipaco_packed_matmul_status synchronises the stream, returns
+ * DIPACO_ETIMEOUT once if that has happened on the device since the last query, DIPACO_OK otherwise.
+ */
+int dipaco_packed_matmul_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t transpose_a, int32_t transpose_b,
+                         void *c, int64_t c_stride, int32_t dtype, int32_t accumulate, void *workspace,
+                         int64_t workspace_bytes, int32_t device, void *cuda_stream);
+int dipaco_packed_matmul_status(int32_t device, void *cuda_stream);
+
 const char *dipaco_strerror(int status);
 
 #ifdef __cplusplus

@@ -51,9 +51,19 @@ EXPORTS = [
     "dipaco_set_level_sync", "dipaco_set_shard", "dipaco_set_optimizer", "dipaco_set_adam",
     "dipaco_set_input_kind", "dipaco_plan_shard", "dipaco_create_shard",
     "dipaco_selftest_wait_expiry", "dipaco_set_work_items", "dipaco_set_host_threads",
+    "dipaco_pack", "dipaco_unpack", "dipaco_layer_norm", "dipaco_layer_norm_pack",
+    "dipaco_layer_norm_workspace", "dipaco_layer_norm_backward", "dipaco_gelu_pack",
+    "dipaco_gelu_pack_backward", "dipaco_packed_matmul_workspace", "dipaco_packed_matmul",
+    "dipaco_packed_matmul_status",
 ]
 
 _lib = None
+
+
+class PackedStruct(ctypes.Structure):
+    """``dipaco_packed``: 8-bit codes with one scale per block of 128 x 128 (device pointers)."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("stride", ctypes.c_int64)]
 
 
 class DipacoError(RuntimeError):
@@ -107,6 +117,19 @@ def load() -> ctypes.CDLL:
     lib.dipaco_plan_traffic.argtypes = [vp, vp, vp, vp]
     lib.dipaco_plan_split.argtypes = [vp, vp, i32, i64, i32, vp, vp, vp, vp, vp]
     lib.dipaco_module_sync_static.argtypes = [vp, vp, i64, i32, vp, vp, vp, f32, f32, i32, i32, i32, vp]
+    pk = ctypes.POINTER(PackedStruct)
+    lib.dipaco_pack.argtypes = [vp, i64, i32, pk, i32, vp]
+    lib.dipaco_unpack.argtypes = [pk, vp, i64, i32, i32, vp]
+    lib.dipaco_layer_norm.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, f32, i32, i32, i32, vp]
+    lib.dipaco_layer_norm_pack.argtypes = [vp, i64, vp, vp, pk, pk, vp, vp, f32, i32, i32, i32, vp]
+    lib.dipaco_layer_norm_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    lib.dipaco_layer_norm_backward.argtypes = [vp, i64, vp, i64, pk, vp, vp, vp, vp, i64, vp, vp, i64, i64, i32,
+                                               i32, vp, i64, i32, vp]
+    lib.dipaco_gelu_pack.argtypes = [vp, i64, i32, pk, pk, i32, vp]
+    lib.dipaco_gelu_pack_backward.argtypes = [vp, i64, i32, pk, pk, i32, vp]
+    lib.dipaco_packed_matmul_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
+    lib.dipaco_packed_matmul.argtypes = [pk, pk, i32, i32, vp, i64, i32, i32, vp, i64, i32, vp]
+    lib.dipaco_packed_matmul_status.argtypes = [i32, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("dipaco_strerror", "dipaco_launch_count"):
@@ -366,6 +389,68 @@ def dipaco_module_sync_static(theta_ptr, momentum_ptr, numel, copy_ptrs, path_we
                                             float(outer_lr), float(outer_momentum), int(path_dtype),
                                             int(chunk_paths), int(device), _stream_handle(stream)),
            "dipaco_module_sync_static")
+
+
+# Operators of the inner phase: pointers are integers (None = NULL), packed matrices PackedStruct.
+
+def dipaco_pack(x_ptr, x_stride, dtype, out, device, stream) -> None:
+    _check(load().dipaco_pack(x_ptr, x_stride, dtype, out, device, stream), "dipaco_pack")
+
+
+def dipaco_unpack(x, y_ptr, y_stride, dtype, device, stream) -> None:
+    _check(load().dipaco_unpack(x, y_ptr, y_stride, dtype, device, stream), "dipaco_unpack")
+
+
+def dipaco_layer_norm(x_ptr, x_stride, gamma_ptr, beta_ptr, y_ptr, y_stride, mean_ptr, rstd_ptr, rows, cols, eps,
+                      dtype, param_dtype, device, stream) -> None:
+    _check(load().dipaco_layer_norm(x_ptr, x_stride, gamma_ptr, beta_ptr, y_ptr, y_stride, mean_ptr, rstd_ptr, rows,
+                                    cols, eps, dtype, param_dtype, device, stream), "dipaco_layer_norm")
+
+
+def dipaco_layer_norm_pack(x_ptr, x_stride, gamma_ptr, beta_ptr, y, x_packed, mean_ptr, rstd_ptr, eps, dtype,
+                           param_dtype, device, stream) -> None:
+    _check(load().dipaco_layer_norm_pack(x_ptr, x_stride, gamma_ptr, beta_ptr, y, x_packed, mean_ptr, rstd_ptr, eps,
+                                         dtype, param_dtype, device, stream), "dipaco_layer_norm_pack")
+
+
+def dipaco_layer_norm_workspace(rows, cols) -> int:
+    n = ctypes.c_int64()
+    _check(load().dipaco_layer_norm_workspace(rows, cols, n), "dipaco_layer_norm_workspace")
+    return n.value
+
+
+def dipaco_layer_norm_backward(dy_ptr, dy_stride, x_ptr, x_stride, x_packed, mean_ptr, rstd_ptr, gamma_ptr, dx_ptr,
+                               dx_stride, dgamma_ptr, dbeta_ptr, rows, cols, dtype, param_dtype, workspace_ptr,
+                               workspace_bytes, device, stream) -> None:
+    _check(load().dipaco_layer_norm_backward(dy_ptr, dy_stride, x_ptr, x_stride, x_packed, mean_ptr, rstd_ptr,
+                                             gamma_ptr, dx_ptr, dx_stride, dgamma_ptr, dbeta_ptr, rows, cols, dtype,
+                                             param_dtype, workspace_ptr, workspace_bytes, device, stream),
+           "dipaco_layer_norm_backward")
+
+
+def dipaco_gelu_pack(x_ptr, x_stride, dtype, y, x_packed, device, stream) -> None:
+    _check(load().dipaco_gelu_pack(x_ptr, x_stride, dtype, y, x_packed, device, stream), "dipaco_gelu_pack")
+
+
+def dipaco_gelu_pack_backward(dy_ptr, dy_stride, dtype, x_packed, dx, device, stream) -> None:
+    _check(load().dipaco_gelu_pack_backward(dy_ptr, dy_stride, dtype, x_packed, dx, device, stream),
+           "dipaco_gelu_pack_backward")
+
+
+def dipaco_packed_matmul_workspace(m, n, k) -> int:
+    size = ctypes.c_int64()
+    _check(load().dipaco_packed_matmul_workspace(m, n, k, size), "dipaco_packed_matmul_workspace")
+    return size.value
+
+
+def dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype, accumulate, workspace_ptr,
+                         workspace_bytes, device, stream) -> None:
+    _check(load().dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype, accumulate,
+                                       workspace_ptr, workspace_bytes, device, stream), "dipaco_packed_matmul")
+
+
+def dipaco_packed_matmul_status(device, stream) -> int:
+    return int(load().dipaco_packed_matmul_status(device, stream))
 
 
 # ------------------------------------------------------------------ convenience owner

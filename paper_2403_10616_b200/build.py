@@ -8,15 +8,15 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdipaco.so")
-SOURCES = ["dipaco.cu", "static_sync.cu"]
-DEPENDS = ["dipaco.cu", "static_sync.cu", "kernels.cuh", "plan.hpp", "host_mode.inl",
+SOURCES = ["dipaco.cu", "static_sync.cu", "layer_norm.cu", "packed.cu", "packed_matmul.cu"]
+DEPENDS = SOURCES + ["kernels.cuh", "plan.hpp", "host_mode.inl", "inner_common.cuh",
            os.path.join("..", "..", "include", "dipaco.h")]
 
 
 def nvcc_command(out, verbose=False):
     cmd = ["nvcc", "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
-           "-Xcompiler", "-fPIC,-O2,-Wall,-pthread", "-shared", "-cudart", "static",
+           "--threads", "0", "-Xcompiler", "-fPIC,-O2,-Wall,-pthread", "-shared", "-cudart", "static",
            "-o", out]
     if verbose:
         cmd += ["-Xptxas", "-v"]

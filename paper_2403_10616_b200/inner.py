@@ -1,0 +1,220 @@
+"""Operators of a path's inner phase on torch CUDA tensors (declared in ``include/dipaco.h``).
+
+Layer norm with its gradient, matrices packed in 8 bits (activation checkpoints and the operands of
+the products), the GELU that writes and reads such checkpoints, and the product of packed matrices
+on the tensor cores.  Each function allocates its results (and workspace) with torch, launches on the
+current stream of the tensors' device, and raises ``ValueError`` for shapes and dtypes that do not
+fit together or ``binding.DipacoError`` with the library's status.  There is no CPU path.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple, Union
+
+import torch
+
+from . import binding as B
+
+BLOCK = 128  # one scale per BLOCK x BLOCK values
+_CODES = {torch.float32: B.DIPACO_F32, torch.bfloat16: B.DIPACO_BF16}
+
+
+class Packed:
+    """A matrix in 8 bits: ``codes`` [rows, cols] float8_e4m3fn, row stride a multiple of 16, and
+    ``scales`` [ceil(rows/128), ceil(cols/128)] float8_e8m0fnu, contiguous; value = code * scale."""
+
+    __slots__ = ("codes", "scales", "struct")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        rows, cols = codes.shape
+        if codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu:
+            raise ValueError("codes must be float8_e4m3fn and scales float8_e8m0fnu")
+        if scales.shape != (-(-rows // BLOCK), -(-cols // BLOCK)) or not scales.is_contiguous():
+            raise ValueError("scales must be contiguous with one entry per block of 128 x 128")
+        if cols > 1 and codes.stride(1) != 1:
+            raise ValueError("codes must be row-major")
+        stride = codes.stride(0) if rows > 1 else -(-max(cols, 1) // 16) * 16
+        if not codes.is_cuda or scales.device != codes.device:
+            raise ValueError("codes and scales must be on one CUDA device")
+        self.codes, self.scales = codes, scales
+        self.struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device) -> "Packed":
+        stride = -(-cols // 16) * 16
+        codes = torch.empty((rows, stride), dtype=torch.float8_e4m3fn, device=device)
+        scales = torch.empty((-(-rows // BLOCK), -(-cols // BLOCK)), dtype=torch.float8_e8m0fnu, device=device)
+        return cls(codes if stride == cols else codes[:, :cols], scales)
+
+    @property
+    def shape(self) -> Tuple[int, int]:
+        return self.struct.rows, self.struct.cols
+
+    @property
+    def device(self) -> torch.device:
+        return self.codes.device
+
+
+def _stream(device: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _dense(name: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
+    """(rows, cols, row stride, dtype code) of a row-major matrix on a CUDA device."""
+    code = _CODES.get(x.dtype)
+    if code is None or x.dim() != 2 or not x.is_cuda:
+        raise ValueError("%s must be a float32 or bfloat16 matrix on a CUDA device" % name)
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        raise ValueError("%s must be row-major" % name)
+    return rows, cols, x.stride(0), code
+
+
+def _params(cols: int, device, gamma, beta) -> Tuple[Optional[int], Optional[int], int]:
+    """Pointers of gamma and beta and their common dtype code."""
+    code = None
+    for t in (gamma, beta):
+        if t is None:
+            continue
+        if t.shape != (cols,) or t.dtype not in _CODES or t.device != device or (cols > 1 and t.stride(0) != 1):
+            raise ValueError("gamma and beta must be contiguous float32 or bfloat16 vectors of the row's length")
+        if code not in (None, _CODES[t.dtype]):
+            raise ValueError("gamma and beta must have one dtype")
+        code = _CODES[t.dtype]
+    return (None if gamma is None else gamma.data_ptr(), None if beta is None else beta.data_ptr(),
+            B.DIPACO_F32 if code is None else code)
+
+
+def pack(x: torch.Tensor) -> Packed:
+    """The packed form of a dense matrix."""
+    rows, cols, stride, code = _dense("x", x)
+    out = Packed.empty(rows, cols, x.device)
+    B.dipaco_pack(x.data_ptr(), stride, code, out.struct, x.device.index, _stream(x.device))
+    return out
+
+
+def unpack(x: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The values that a packed matrix stands for."""
+    if dtype not in _CODES:
+        raise ValueError("dtype must be float32 or bfloat16")
+    y = torch.empty(x.shape, dtype=dtype, device=x.device)
+    B.dipaco_unpack(x.struct, y.data_ptr(), y.stride(0), _CODES[dtype], x.device.index, _stream(x.device))
+    return y
+
+
+def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, stats: bool = False):
+    """The norm of every row of x, in x's dtype; with ``stats`` (y, mean, rstd) for the backward pass."""
+    rows, cols, stride, code = _dense("x", x)
+    dev = x.device
+    g, b, pcode = _params(cols, dev, gamma, beta)
+    y = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    if not stats:
+        B.dipaco_layer_norm(x.data_ptr(), stride, g, b, y.data_ptr(), cols, None, None, rows, cols, eps, code, pcode,
+                            dev.index, _stream(dev))
+        return y
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    B.dipaco_layer_norm(x.data_ptr(), stride, g, b, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), rows, cols,
+                        eps, code, pcode, dev.index, _stream(dev))
+    return y, mean, rstd
+
+
+def layer_norm_pack(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                    eps: float = 1e-5, keep: bool = True):
+    """(y, x, mean, rstd): the norm of every row of x, packed, and x itself packed as the checkpoint
+    that ``layer_norm_backward`` reads (None without ``keep``)."""
+    rows, cols, stride, code = _dense("x", x)
+    dev = x.device
+    g, b, pcode = _params(cols, dev, gamma, beta)
+    y = Packed.empty(rows, cols, dev)
+    kept = Packed.empty(rows, cols, dev) if keep else None
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    B.dipaco_layer_norm_pack(x.data_ptr(), stride, g, b, y.struct, kept.struct if keep else None, mean.data_ptr(),
+                             rstd.data_ptr(), eps, code, pcode, dev.index, _stream(dev))
+    return y, kept, mean, rstd
+
+
+def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], mean: torch.Tensor, rstd: torch.Tensor,
+                        gamma: Optional[torch.Tensor] = None):
+    """(dx, dgamma, dbeta) from the norm's input or its packed checkpoint; dgamma and dbeta are fp32."""
+    rows, cols, stride, code = _dense("dy", dy)
+    dev = dy.device
+    g, _, pcode = _params(cols, dev, gamma, None)
+    if tuple(x.shape) != (rows, cols) or x.device != dev:
+        raise ValueError("x and dy must have one shape and device")
+    for t in (mean, rstd):
+        if t.shape != (rows,) or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous():
+            raise ValueError("mean and rstd must be contiguous float32 vectors with one entry per row")
+    x_ptr, x_stride, packed = None, 0, None
+    if isinstance(x, Packed):
+        packed = x.struct
+    else:
+        _, _, x_stride, x_code = _dense("x", x)
+        if x_code != code:
+            raise ValueError("x and dy must have one dtype")
+        x_ptr = x.data_ptr()
+    dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
+    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dev).unbind(0)
+    need = B.dipaco_layer_norm_workspace(rows, cols)
+    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    B.dipaco_layer_norm_backward(dy.data_ptr(), stride, x_ptr, x_stride, packed, mean.data_ptr(), rstd.data_ptr(), g,
+                                 dx.data_ptr(), cols, dgamma.data_ptr(), dbeta.data_ptr(), rows, cols, code, pcode,
+                                 work.data_ptr() if need else None, need, dev.index, _stream(dev))
+    return dx, dgamma, dbeta
+
+
+def gelu_pack(x: torch.Tensor, keep: bool = True):
+    """(y, x): the GELU of x, packed, and x itself packed as the checkpoint that
+    ``gelu_pack_backward`` reads (None without ``keep``)."""
+    rows, cols, stride, code = _dense("x", x)
+    y = Packed.empty(rows, cols, x.device)
+    kept = Packed.empty(rows, cols, x.device) if keep else None
+    B.dipaco_gelu_pack(x.data_ptr(), stride, code, y.struct, kept.struct if keep else None, x.device.index,
+                       _stream(x.device))
+    return y, kept
+
+
+def gelu_pack_backward(dy: torch.Tensor, x: Packed) -> Packed:
+    """dy * gelu'(x), packed, from the GELU's packed input."""
+    rows, cols, stride, code = _dense("dy", dy)
+    if x.shape != (rows, cols) or x.device != dy.device:
+        raise ValueError("x and dy must have one shape and device")
+    dx = Packed.empty(rows, cols, dy.device)
+    B.dipaco_gelu_pack_backward(dy.data_ptr(), stride, code, x.struct, dx.struct, dy.device.index,
+                                _stream(dy.device))
+    return dx
+
+
+def packed_matmul(a: Packed, b: Packed, transpose_a: bool = False, transpose_b: bool = False,
+                  out_dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                  accumulate: bool = False) -> torch.Tensor:
+    """op(a) op(b) with fp32 sums, op transposing where asked.  ``out`` is written (its dtype is the
+    result's), or added to with ``accumulate``."""
+    m, k = a.shape
+    k2, n = b.shape
+    if transpose_a:
+        m, k = k, m
+    if transpose_b:
+        k2, n = n, k2
+    dev = a.device
+    if k != k2 or b.device != dev:
+        raise ValueError("the operands' contracted extents (%d and %d) and devices must agree" % (k, k2))
+    if out is None:
+        if accumulate or out_dtype not in _CODES:
+            raise ValueError("accumulate needs out, and out_dtype is float32 or bfloat16")
+        out, stride, code = torch.empty((m, n), dtype=out_dtype, device=dev), n, _CODES[out_dtype]
+    else:
+        rows, cols, stride, code = _dense("out", out)
+        if (rows, cols) != (m, n) or out.device != dev:
+            raise ValueError("out must be [%d, %d] on the operands' device" % (m, n))
+    need = B.dipaco_packed_matmul_workspace(m, n, k)
+    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    B.dipaco_packed_matmul(a.struct, b.struct, transpose_a, transpose_b, out.data_ptr(), stride, code, accumulate,
+                           work.data_ptr() if need else None, need, dev.index, _stream(dev))
+    return out
+
+
+def packed_matmul_status(device=None) -> int:
+    """Waits for the current stream and reports DIPACO_OK, or DIPACO_ETIMEOUT once after a bounded
+    wait inside a product ran out."""
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    return B.dipaco_packed_matmul_status(dev.index or 0, torch.cuda.current_stream(dev).cuda_stream)
