@@ -6,10 +6,16 @@
 // contracted values; here all of them are equal over a block, so the scale operands in tensor memory
 // are constant words and a block may be contracted along either side: the operand's major-ness in the
 // instruction descriptor is all that differs between the forward product and the two gradients.
+//
+//   pair_kernel    persistent; two SMs share a tile of 256 rows and up to 256 columns (cta_group::2):
+//                  each loads half of A and half of B and keeps half of the sums
+//   skinny_kernel  products with at most 64 rows or columns: 128 of the long side per block, the
+//                  contraction shared by the blocks of a cluster
 #include "inner_common.cuh"
 
 #include <cuda.h>
 
+#include <algorithm>
 #include <cmath>
 
 using namespace dipaco;
@@ -20,50 +26,144 @@ static __device__ int g_product_error;  // set by a bounded wait that ran out
 
 // ------------------------------------------------------------------------------------------ PTX
 
-__device__ __forceinline__ bool elect_one()
+// An address of this block's shared memory as seen from, or for, block `rank` of the cluster.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t address, unsigned rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ unsigned cluster_rank()
+{
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Orders what this thread wrote to shared memory before what the waiting block does.
+__device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// Where only reads of tensor memory have to be over (fence_before_sync orders those).
+__device__ __forceinline__ void arrive_remote(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, unsigned parity)
 {
     unsigned ok;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(ptx::smem_addr(bar)), "r"(parity)
+        : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint64_t *bar)
+// Bounded, and ordered after what other blocks of the cluster did before they arrived.
+__device__ __forceinline__ bool wait_cluster(uint64_t *bar, unsigned parity, int code)
 {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-            dst),
-        "l"(map), "r"(x), "r"(y), "r"(ptx::smem_addr(bar))
-        : "memory");
+    if (try_wait_cluster(bar, parity)) return true;
+    const unsigned long long t0 = ptx::global_timer_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 256; ++i)
+            if (try_wait_cluster(bar, parity)) return true;
+        if (ptx::global_timer_ns() - t0 > BULK_WAIT_LIMIT_NS) {
+            atomicCAS(&g_product_error, 0, code);
+            return false;
+        }
+    }
 }
-__device__ __forceinline__ void tmem_alloc(uint32_t *result, int columns)
+// GROUP: blocks that share a product (cta_group).  With 2 the barrier may be the other block's.
+template <int GROUP>
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_addr(result)),
-                 "r"(columns)
+    if constexpr (GROUP == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+            "[%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x),
+                 "r"(y), "r"(src)
                  : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
 }
-__device__ __forceinline__ void tmem_free(uint32_t address, int columns)
+template <int GROUP> __device__ __forceinline__ void tmem_alloc(uint32_t *result, int columns)
 {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
+    if constexpr (GROUP == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_addr(result)),
+                     "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_addr(result)),
+                     "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+}
+template <int GROUP> __device__ __forceinline__ void tmem_free(uint32_t address, int columns)
+{
+    if constexpr (GROUP == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
 }
 // 32 lanes x 16 bytes of shared memory to four columns of each 32-lane quarter of tensor memory
-__device__ __forceinline__ void tmem_copy_scales(uint32_t address, uint64_t desc)
+template <int GROUP> __device__ __forceinline__ void tmem_copy_scales(uint32_t address, uint64_t desc)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(address), "l"(desc) : "memory");
+    if constexpr (GROUP == 1)
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(address), "l"(desc) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(address), "l"(desc) : "memory");
 }
+template <int GROUP>
 __device__ __forceinline__ void mma_block_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a,
                                                  uint32_t scale_b, bool add)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"((unsigned)add)
-        : "memory");
+    if constexpr (GROUP == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+                d),
+            "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"((unsigned)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+                d),
+            "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"((unsigned)add)
+            : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint64_t *bar)
+// Arrives on the barrier, of both blocks of a pair, once the products issued so far are done.
+template <int GROUP> __device__ __forceinline__ void mma_commit(uint64_t *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                     ptx::smem_addr(bar))
-                 : "memory");
+    if constexpr (GROUP == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                         ptx::smem_addr(bar))
+                     : "memory");
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                ptx::smem_addr(bar)),
+            "h"((unsigned short)3)
+            : "memory");
 }
 __device__ __forceinline__ void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -97,49 +197,533 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t address)
     return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)(128u >> 4) << 16 | (uint64_t)(128u >> 4) << 32 | 1ull << 46;
 }
 
-// ------------------------------------------------------------------------------------------ kernel
+// ------------------------------------------------------------------------------------------ common
 
-constexpr int TILE = 128;                     // of C and of the contraction: one block
-constexpr int TILE_BYTES = TILE * TILE;       // of codes
-constexpr int SCALE_BYTES = 512;              // 32 lanes x 16 bytes
-constexpr int STAGES = 3;                     // two resident blocks per SM
-constexpr int STAGE_BYTES = 2 * TILE_BYTES + 2 * SCALE_BYTES;
-constexpr int PRODUCT_SMEM = STAGES * STAGE_BYTES + 1024;
-constexpr int PRODUCT_THREADS = 192;          // four epilogue warps, load warp, issuing warp
-constexpr int TMEM_COLUMNS = 256;             // 128 of sums, 8 of scales per stage
+constexpr int STEP = 128;                 // contracted values per step: one block
 constexpr int CONTRACTED_PER_MMA = 32;
+constexpr int SCALE_BYTES = 512;          // of shared memory for four columns: 32 lanes x 16 bytes
 // The tensor cores truncate when they add to an fp32 sum, which drifts by about 1.2e-8 of the sum for
-// every 32 contracted values (measured: 2.4e-5 over 65501).  Sums are therefore taken out of tensor
-// memory every CHUNK steps, 2048 values, and added up in registers.
+// every 32 contracted values (2.4e-5 over 65501).  Sums that are returned in fp32 are therefore taken
+// out of tensor memory every CHUNK steps, 2048 values, and added up in registers: under 1e-6.  A result
+// in bf16 has 2e-3 of rounding of its own and keeps one sum.
 constexpr int CHUNK = 16;
 
 struct ProductArgs {
     const uint8_t *a_scales, *b_scales;
     int a_scale_cols, b_scale_cols;
     int transpose_a, transpose_b;  // A is stored [K, M]; B is stored [N, K]
-    int m, n, k;
+    int m, n, steps;
     void *c;
-    long long c_stride;
+    long long c_row, c_col;  // strides of C in elements
     int c_bf16, accumulate;
+    // pair_kernel
+    int tile_n, tiles_m, tiles_n;
+    int whole_tiles;  // tiles that one pair computes from end to end; the steps of the others are dealt out evenly
+    int store_by_tma;
+    float *partial;
 };
 
-__global__ void __launch_bounds__(PRODUCT_THREADS)
-    product_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, ProductArgs p)
+// Bits: A and B e4m3 (0), A and B major-ness, N/8, e8m0 scales, M/16.
+__device__ __forceinline__ uint32_t instruction_desc(const ProductArgs &p, int m, int n)
+{
+    return (uint32_t)(p.transpose_a ? 1 : 0) << 15 | (uint32_t)(p.transpose_b ? 0 : 1) << 16 | (uint32_t)(n >> 3) << 17 |
+           1u << 23 | (uint32_t)(m >> 4) << 24;
+}
+
+__device__ __forceinline__ void store_c(const ProductArgs &p, long long row, long long col, float v)
+{
+    const long long at = row * p.c_row + col * p.c_col;
+    if (p.c_bf16) {
+        __nv_bfloat16 *c = static_cast<__nv_bfloat16 *>(p.c) + at;
+        if (p.accumulate) v += __bfloat162float(*c);
+        *c = __float2bfloat16_rn(v);
+    } else {
+        float *c = static_cast<float *>(p.c) + at;
+        if (p.accumulate) v += *c;
+        *c = v;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ pairs of SMs
+
+// Each block of the pair holds 128 rows of A and half the tile's columns of B per stage.  Tensor memory:
+// two sets of sums, 12 columns of scales per stage at the end.  With 256 columns the sets overlap: the
+// first set's last columns are the second's first.  They are read out first, and the products of the
+// next tile start as soon as that is done; with fewer columns the sets are apart and the next tile's
+// products only wait for the tile before the last to be read out.
+constexpr int PAIR_STAGES = 5;
+constexpr int PAIR_OPERAND_BYTES = 128 * STEP;
+constexpr int PAIR_STAGE_BYTES = 2 * PAIR_OPERAND_BYTES;
+constexpr int PAIR_WORDS_BYTES = 3 * SCALE_BYTES;  // scale words of a step
+constexpr int PAIR_WORDS_STEPS = 8;  // scale words are written for eight steps at a time: a signal between the blocks
+                                     // for each step held the tensor cores up (16384x2048x8192: 427 us against 285)
+constexpr int PAIR_EPILOGUE_WARPS = 8;
+constexpr int PAIR_STAGING_BYTES = 4096;  // per epilogue warp: 32 rows x 32 columns in fp32, or twice in bf16
+// shared memory: operands and staging on 1024-byte boundaries (the swizzle goes by address), then scale words
+constexpr int PAIR_STAGING_AT = PAIR_STAGES * PAIR_STAGE_BYTES;
+constexpr int PAIR_WORDS_AT = PAIR_STAGING_AT + PAIR_EPILOGUE_WARPS * PAIR_STAGING_BYTES;
+constexpr int PAIR_SMEM = PAIR_WORDS_AT + 2 * PAIR_WORDS_STEPS * PAIR_WORDS_BYTES + 1024;
+constexpr int PAIR_THREADS = (PAIR_EPILOGUE_WARPS + 3) * 32;  // + loads, products, scale words
+constexpr int PAIR_SCALE_COLUMNS = 12;
+constexpr int PAIR_SCALES_AT = 512 - PAIR_STAGES * PAIR_SCALE_COLUMNS;
+constexpr int PAIR_MAX_N = 256;
+constexpr int PAIR_ROWS = 256;
+constexpr int RASTER = 8;  // row tiles that share column tiles while those are in L2
+
+// A piece of work: steps [first, last) of a tile.
+struct PairItem {
+    int tile_m, tile_n, first, last;
+    int slot;  // where a partial sum goes; -1: the tile is finished here
+};
+
+// The pieces of one pair: its whole tiles, then its share of the steps of the remaining tiles.
+struct PairWalk {
+    int tile, pairs, whole;
+    long long next, end;
+    bool first_share = true;
+
+    __device__ PairWalk(const ProductArgs &p, int pair, int pairs_) : tile(pair), pairs(pairs_), whole(p.whole_tiles)
+    {
+        const long long units = (long long)(p.tiles_m * p.tiles_n - whole) * p.steps;
+        next = units * pair / pairs;
+        end = units * (pair + 1) / pairs;
+    }
+    __device__ bool take(const ProductArgs &p, int pair, PairItem &item)
+    {
+        int index;
+        if (tile < whole) {
+            index = tile;
+            tile += pairs;
+            item.first = 0;
+            item.last = p.steps;
+            item.slot = -1;
+        } else {
+            if (next >= end) return false;
+            index = whole + (int)(next / p.steps);
+            item.first = (int)(next % p.steps);
+            item.last = (int)min((long long)p.steps, item.first + (end - next));
+            item.slot = item.first == 0 && item.last == p.steps ? -1 : 2 * pair + (first_share ? 0 : 1);
+            next += item.last - item.first;
+            first_share = false;
+        }
+        place(p, index, item.tile_m, item.tile_n);
+        return true;
+    }
+    static __host__ __device__ void place(const ProductArgs &p, int index, int &tile_m, int &tile_n)
+    {
+        const int group = index / (RASTER * p.tiles_n), rest = index % (RASTER * p.tiles_n);
+        const int rows = p.tiles_m - group * RASTER < RASTER ? p.tiles_m - group * RASTER : RASTER;
+        tile_m = group * RASTER + rest % rows;
+        tile_n = rest / rows;
+    }
+};
+
+// Partial sums: [slot][block of the pair][column][128 rows].
+__device__ __forceinline__ long long partial_offset(const ProductArgs &p, int slot, unsigned rank)
+{
+    return ((long long)slot * 2 + rank) * p.tile_n * 128;
+}
+
+// Where an epilogue warp puts 32 columns of its 32 rows.
+__device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUtensorMap &c_map, const PairItem &item,
+                                               unsigned rank, int quarter, int lane, int c0, const float *v,
+                                               uint8_t *staging, int &buffer)
+{
+    if (item.slot >= 0) {
+        float *out = p.partial + partial_offset(p, item.slot, rank) + (long long)c0 * 128 + quarter * 32 + lane;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) out[i * 128] = v[i];
+        return;
+    }
+    const int row0 = item.tile_m * PAIR_ROWS + (int)rank * 128 + quarter * 32;
+    const int col0 = item.tile_n * p.tile_n + c0;
+    if (p.store_by_tma) {
+        // rows of 64 or 128 bytes in the copy engine's swizzle of the same width: no bank conflicts
+        uint8_t *at = staging + (p.c_bf16 ? buffer * 2048 : 0);
+        if (p.c_bf16)
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        else
+            ptx::bulk_wait_read_all();
+        __syncwarp();
+        if (p.c_bf16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<uint4 *>(at + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) =
+                    Unit<__nv_bfloat16>::narrow(v + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                *reinterpret_cast<float4 *>(at + lane * 128 + ((i ^ (lane & 7)) * 16)) =
+                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+        ptx::fence_proxy_async();
+        __syncwarp();
+        // columns and rows outside C are not written
+        if (lane == 0) {
+            if (row0 < p.m && col0 < p.n) tma_store_2d(&c_map, ptx::smem_addr(at), col0, row0);
+            ptx::bulk_commit();
+        }
+        __syncwarp();
+        buffer ^= 1;
+        return;
+    }
+    // any alignment, and sums with what is there: rows through shared memory, a lane per column
+    float *at = reinterpret_cast<float *>(staging);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) at[lane * 32 + ((i + lane) & 31)] = v[i];
+    __syncwarp();
+    const int rows = min(32, p.m - row0);
+    if (col0 + lane < p.n)
+        for (int r = 0; r < rows; ++r) store_c(p, row0 + r, col0 + lane, at[r * 32 + ((lane + r) & 31)]);
+}
+
+template <bool CHUNKED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
+    pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                const __grid_constant__ CUtensorMap c_map, const __grid_constant__ ProductArgs p)
 {
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[STAGES], empty[STAGES], done, drained;
+    __shared__ uint64_t full[PAIR_STAGES], empty[PAIR_STAGES], sums_full[2], sums_read[2], words_full[2], words_empty[2],
+        ended;
     __shared__ uint32_t tmem_base;
     const uint32_t base = (ptx::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t *aligned = raw + (base - ptx::smem_addr(raw));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tiles_n = (p.n + TILE - 1) / TILE;
-    const int tile_m = blockIdx.x / tiles_n, tile_n = blockIdx.x % tiles_n;
-    const int steps = (p.k + TILE - 1) / TILE;
+    const unsigned rank = cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-    if (warp == 5) tmem_alloc(&tmem_base, TMEM_COLUMNS);
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) {
+    if (warp == 0) tmem_alloc<2>(&tmem_base, 512);
+    if (threadIdx.x == 32) {
+        for (int s = 0; s < PAIR_STAGES; ++s) {
             ptx::mbar_init(&full[s], 1);
+            ptx::mbar_init(&empty[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(&sums_full[s], 1);
+            ptx::mbar_init(&sums_read[s], 2 * PAIR_EPILOGUE_WARPS);
+            ptx::mbar_init(&words_full[s], 2);  // of either block
+            ptx::mbar_init(&words_empty[s], 1);
+        }
+        ptx::mbar_init(&ended, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    fence_before_sync();
+    cluster_sync();
+    fence_after_sync();
+    const uint32_t tmem = tmem_base;
+    const int second_set = PAIR_SCALES_AT - p.tile_n;  // column of the second set of sums
+    const bool apart = second_set >= p.tile_n;
+    const int half_n = p.tile_n / 2;
+
+    if (warp == PAIR_EPILOGUE_WARPS) {
+        // ---- loads: this block's halves of A and B
+        const unsigned b_bytes = p.transpose_b ? half_n * STEP : PAIR_OPERAND_BYTES;
+        PairWalk walk(p, pair, pairs);
+        PairItem item;
+        int stage = 0;
+        unsigned phase = 0;
+        bool ok = true;
+        while (ok && walk.take(p, pair, item)) {
+            const int m0 = item.tile_m * PAIR_ROWS + (int)rank * 128, nb = item.tile_n * p.tile_n + (int)rank * half_n;
+            for (int i = item.first; i < item.last; ++i) {
+                ok = bounded_wait(&empty[stage], phase ^ 1, &g_product_error, 1);
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t to = base + stage * PAIR_STAGE_BYTES;
+                    const uint32_t bar = cluster_addr(ptx::smem_addr(&full[stage]), 0);
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * (PAIR_OPERAND_BYTES + b_bytes));
+                    if (p.transpose_a)
+                        tma_load_2d<2>(to, &a_map, m0, i * STEP, bar);
+                    else
+                        tma_load_2d<2>(to, &a_map, i * STEP, m0, bar);
+                    if (p.transpose_b)
+                        tma_load_2d<2>(to + PAIR_OPERAND_BYTES, &b_map, i * STEP, nb, bar);
+                    else
+                        tma_load_2d<2>(to + PAIR_OPERAND_BYTES, &b_map, nb, i * STEP, bar);
+                }
+                __syncwarp();
+                if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
+            }
+        }
+        // the barriers of the last stages are arrived on from the first block: both stay until then
+        for (int s = 0; ok && s < PAIR_STAGES; ++s) {
+            ok = bounded_wait(&empty[stage], phase ^ 1, &g_product_error, 2);
+            if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
+        }
+        if (!ok)  // a wait ran out: let the copies in flight land before the block ends
+            for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    } else if (warp == PAIR_EPILOGUE_WARPS + 2) {
+        // ---- scale words of this block's tensor memory
+        const int a_blocks = (p.m + 127) / 128, b_blocks = (p.n + 127) / 128;
+        PairWalk walk(p, pair, pairs);
+        PairItem item;
+        int set = 0;
+        unsigned phase = 0;
+        bool ok = true;
+        while (ok && walk.take(p, pair, item)) {
+            const int block_a = item.tile_m * 2 + (int)rank;
+            const int n0 = item.tile_n * p.tile_n, block_b = n0 >> 7;
+            unsigned held = 0;  // scale bytes of 32 steps, one step per lane: of A's block and of up to three of B
+            for (int i0 = item.first; i0 < item.last; i0 += PAIR_WORDS_STEPS) {
+                const int at = (i0 - item.first) & 31;
+                if (at == 0 && i0 + lane < item.last) {
+                    const long long kb = i0 + lane;
+                    held = 127u;
+                    if (block_a < a_blocks)
+                        held = p.a_scales[p.transpose_a ? kb * p.a_scale_cols + block_a
+                                                        : (long long)block_a * p.a_scale_cols + kb];
+#pragma unroll
+                    for (int b = 0; b < 3; ++b) {
+                        unsigned byte = 127u;
+                        if (block_b + b < b_blocks)
+                            byte = p.b_scales[p.transpose_b ? (long long)(block_b + b) * p.b_scale_cols + kb
+                                                            : kb * p.b_scale_cols + block_b + b];
+                        held |= byte << (8 * b + 8);
+                    }
+                }
+                ok = bounded_wait(&words_empty[set], phase ^ 1, &g_product_error, 7);
+                if (!ok) break;
+                uint4 *words = reinterpret_cast<uint4 *>(aligned + PAIR_WORDS_AT + set * PAIR_WORDS_STEPS * PAIR_WORDS_BYTES) + lane;
+                for (int i = 0; i < PAIR_WORDS_STEPS && i0 + i < item.last; ++i) {
+                    const unsigned bytes = __shfl_sync(0xffffffffu, held, at + i);
+                    const unsigned wa = (bytes & 255u) * 0x01010101u;
+                    unsigned wb[8];  // of the eight groups of 32 columns
+#pragma unroll
+                    for (int g = 0; g < 8; ++g)
+                        wb[g] = (bytes >> (8 * (((n0 + 32 * g) >> 7) - block_b) + 8) & 255u) * 0x01010101u;
+                    words[0] = make_uint4(wa, wa, wa, wa);
+                    words[32] = make_uint4(wb[0], wb[1], wb[2], wb[3]);
+                    words[64] = make_uint4(wb[4], wb[5], wb[6], wb[7]);
+                    words += PAIR_WORDS_BYTES / 16;
+                }
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) arrive_cluster(cluster_addr(ptx::smem_addr(&words_full[set]), 0));
+                __syncwarp();
+                if (++set == 2) { set = 0; phase ^= 1; }
+            }
+        }
+        for (int s = 0; ok && s < 2; ++s) {  // as for the stages
+            ok = bounded_wait(&words_empty[set], phase ^ 1, &g_product_error, 8);
+            if (++set == 2) { set = 0; phase ^= 1; }
+        }
+    } else if (warp == PAIR_EPILOGUE_WARPS + 1) {
+        // ---- products: one thread of the first block issues them for both
+        if (rank == 0) {
+            const uint32_t idesc = instruction_desc(p, PAIR_ROWS, p.tile_n);
+            // 32 contracted values further on: 32 bytes along a row, or 32 rows of 128 bytes
+            const uint32_t step_a = (p.transpose_a ? CONTRACTED_PER_MMA * 128 : CONTRACTED_PER_MMA) >> 4;
+            const uint32_t step_b = (p.transpose_b ? CONTRACTED_PER_MMA : CONTRACTED_PER_MMA * 128) >> 4;
+            PairWalk walk(p, pair, pairs);
+            PairItem item;
+            int stage = 0, sets = 0;  // sets of sums begun
+            int words_set = 0;
+            unsigned phase = 0, words_phase = 0;
+            bool ok = true;
+            while (ok && walk.take(p, pair, item)) {
+                for (int i = item.first; i < item.last; ++i) {
+                    const int in_words = (i - item.first) % PAIR_WORDS_STEPS;
+                    const bool words_end = in_words == PAIR_WORDS_STEPS - 1 || i + 1 == item.last;
+                    if (in_words == 0) ok = wait_cluster(&words_full[words_set], words_phase, 9);
+                    if (!ok) break;
+                    const int in_set = CHUNKED ? (i - item.first) % CHUNK : i - item.first;
+                    if (in_set == 0) {
+                        // the set before this one (its shared columns), or the one before that, has been read
+                        const int before = sets - (apart ? 2 : 1);
+                        if (before >= 0) ok = bounded_wait(&sums_read[before & 1], (before >> 1) & 1, &g_product_error, 5);
+                        if (!ok) break;
+                    }
+                    ok = bounded_wait(&full[stage], phase, &g_product_error, 3);
+                    if (!ok) break;
+                    fence_after_sync();
+                    if (lane == 0) {
+                        const uint32_t at = base + stage * PAIR_STAGE_BYTES;
+                        const uint32_t scale_a = tmem + PAIR_SCALES_AT + stage * PAIR_SCALE_COLUMNS, scale_b = scale_a + 4;
+                        const uint32_t words = base + PAIR_WORDS_AT + (words_set * PAIR_WORDS_STEPS + in_words) * PAIR_WORDS_BYTES;
+                        tmem_copy_scales<2>(scale_a, scales_desc(words));
+                        tmem_copy_scales<2>(scale_b, scales_desc(words + SCALE_BYTES));
+                        if (p.tile_n > 128) tmem_copy_scales<2>(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
+                        const uint64_t da = operand_desc(at), db = operand_desc(at + PAIR_OPERAND_BYTES);
+                        const uint32_t sums = tmem + ((sets & 1) ? second_set : 0);
+#pragma unroll
+                        for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
+                            mma_block_scaled<2>(sums, da + j * step_a, db + j * step_b, idesc, scale_a, scale_b,
+                                                in_set + j > 0);
+                        mma_commit<2>(&empty[stage]);
+                        if (words_end) mma_commit<2>(&words_empty[words_set]);
+                        if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) mma_commit<2>(&sums_full[sets & 1]);
+                    }
+                    __syncwarp();
+                    if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) ++sets;
+                    if (words_end && ++words_set == 2) { words_set = 0; words_phase ^= 1; }
+                    if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+            if (!ok) {  // products in flight end before the tensor memory is freed
+                if (lane == 0) mma_commit<2>(&ended);
+                bounded_wait(&ended, 0, &g_product_error, 6);
+            }
+        }
+    } else {
+        // ---- epilogue: a warp reads its quarter of the rows and every other group of 32 columns
+        const int quarter = warp & 3, odd = warp >> 2;
+        uint8_t *staging = aligned + PAIR_STAGING_AT + warp * PAIR_STAGING_BYTES;
+        const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&sums_read[0]), 0),
+                                       cluster_addr(ptx::smem_addr(&sums_read[1]), 0)};
+        const int groups = p.tile_n / 32;
+        PairWalk walk(p, pair, pairs);
+        PairItem item;
+        int sets = 0, buffer = 0;
+        bool ok = true;
+        float total[CHUNKED ? 128 : 1];
+        while (ok && walk.take(p, pair, item)) {
+            const int parts = CHUNKED ? (item.last - item.first + CHUNK - 1) / CHUNK : 1;
+            if constexpr (CHUNKED) {
+#pragma unroll
+                for (int i = 0; i < 128; ++i) total[i] = 0.0f;
+            }
+            for (int part = 0; part < parts; ++part, ++sets) {
+                ok = bounded_wait(&sums_full[sets & 1], (sets >> 1) & 1, &g_product_error, 4);
+                if (!ok) break;
+                fence_after_sync();
+                const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? second_set : 0);
+                const bool down = !(sets & 1);  // the columns shared with the other set come first
+                const uint32_t read_bar = down ? read_bars[0] : read_bars[1];
+#pragma unroll
+                for (int t = 0; t < PAIR_MAX_N / 64; ++t) {
+                    if constexpr (CHUNKED) {
+                        // the total's registers need fixed indexes: both orders are written out
+#pragma unroll
+                        for (int order = 0; order < 2; ++order) {
+                            const int u = order ? PAIR_MAX_N / 64 - 1 - t : t, g = 2 * u + odd;
+                            if (down == (order == 1) && g < groups) {
+                                uint32_t r[32];
+                                tmem_load32(from + g * 32, r);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) total[u * 32 + i] += __uint_as_float(r[i]);
+                            }
+                        }
+                    } else {
+                        const int g = 2 * (down ? PAIR_MAX_N / 64 - 1 - t : t) + odd;
+                        if (g < groups) {
+                            uint32_t r[32];
+                            tmem_load32(from + g * 32, r);
+                            if (!apart && t == 0) {
+                                fence_before_sync();
+                                if (lane == 0) arrive_remote(read_bar);
+                                __syncwarp();
+                            }
+                            float v[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+                            finish_columns(p, c_map, item, rank, quarter, lane, g * 32, v, staging, buffer);
+                        }
+                    }
+                    if (CHUNKED && !apart && t == 0) {
+                        fence_before_sync();
+                        if (lane == 0) arrive_remote(read_bar);
+                        __syncwarp();
+                    }
+                }
+                if (apart) {
+                    fence_before_sync();
+                    if (lane == 0) arrive_remote(read_bar);
+                    __syncwarp();
+                }
+            }
+            if constexpr (CHUNKED) {
+                if (ok) {
+#pragma unroll
+                    for (int u = 0; u < PAIR_MAX_N / 64; ++u)
+                        if (2 * u + odd < groups)
+                            finish_columns(p, c_map, item, rank, quarter, lane, (2 * u + odd) * 32, total + u * 32,
+                                           staging, buffer);
+                }
+            }
+        }
+        ptx::bulk_wait_all();
+    }
+    __syncwarp();
+    fence_before_sync();
+    cluster_sync();
+    fence_after_sync();
+    if (warp == 0) tmem_free<2>(tmem, 512);
+}
+
+// Tiles whose steps were dealt out: their partial sums in the order of the steps.  A block joins 32
+// columns of one block's 128 rows.
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs p, int pairs)
+{
+    __shared__ float shared[128][33];
+    const int groups = p.tile_n / 32;
+    const int group = blockIdx.x % groups;
+    const unsigned rank = blockIdx.x / groups % 2;
+    const int tile = blockIdx.x / (2 * groups);  // among those dealt out
+    const long long units = (long long)(p.tiles_m * p.tiles_n - p.whole_tiles) * p.steps;
+    const long long from = (long long)tile * p.steps, to = from + p.steps;
+    // pair q has the steps from units q / pairs on
+    int first = (int)(from * pairs / units);
+    while (first > 0 && units * first / pairs > from) --first;
+    while (units * (first + 1) / pairs <= from) ++first;
+    if (units * first / pairs <= from && units * (first + 1) / pairs >= to) return;  // finished by one pair
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+    const int row = threadIdx.x & 127, side = threadIdx.x >> 7;
+    for (int q = first; q < pairs && units * q / pairs < to; ++q) {
+        const long long begin = units * q / pairs;
+        if (begin == units * (q + 1) / pairs) continue;
+        const int slot = 2 * q + (begin / p.steps == tile ? 0 : 1);
+        const float *in = p.partial + partial_offset(p, slot, rank) + (long long)(group * 32 + side * 16) * 128 + row;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += in[i * 128];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) shared[row][side * 16 + i] = v[i];
+    __syncthreads();
+    int tile_m, tile_n;
+    PairWalk::place(p, p.whole_tiles + tile, tile_m, tile_n);
+    const long long row0 = (long long)tile_m * PAIR_ROWS + rank * 128;
+    const long long col = (long long)tile_n * p.tile_n + group * 32 + (threadIdx.x & 31);
+    if (col < p.n)
+        for (int r = threadIdx.x >> 5; r < 128 && row0 + r < p.m; r += 8)
+            store_c(p, row0 + r, col, shared[r][threadIdx.x & 31]);
+}
+
+// ------------------------------------------------------------------------------------------ few rows or columns
+
+// 128 of the long side ("rows") against all of the short side ("columns", 16, 32 or 64 of them).  The
+// blocks of a cluster share the contraction; block 0 adds the sums up in their order.
+constexpr int SKINNY_STAGES = 4;
+constexpr int SKINNY_MAX_N = 64;
+constexpr int SKINNY_COLUMN_BYTES = 128 * STEP;  // of a stage, where the short side is across rows of codes
+constexpr int SKINNY_THREADS = 192;              // four epilogue warps, load warp, issuing warp
+constexpr int SKINNY_MAX_CLUSTER = 8;
+constexpr int SKINNY_MAX_COLLECTED = 112 * 1024; // other blocks' sums in block 0: leaves room for two blocks per SM
+constexpr int SKINNY_TMEM = 128;                 // 64 of sums, 8 of scales per stage
+
+__host__ __device__ constexpr int skinny_stage_bytes(int column_bytes) { return 128 * STEP + column_bytes + 2 * SCALE_BYTES; }
+
+__global__ void __launch_bounds__(SKINNY_THREADS)
+    skinny_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                  const __grid_constant__ ProductArgs p, int shares, int column_bytes)
+{
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[SKINNY_STAGES], empty[SKINNY_STAGES], done, drained;
+    __shared__ uint32_t tmem_base;
+    const uint32_t base = (ptx::smem_addr(raw) + 1023u) & ~1023u;
+    uint8_t *aligned = raw + (base - ptx::smem_addr(raw));
+    const int stage_bytes = skinny_stage_bytes(column_bytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tile = blockIdx.x / shares, share = blockIdx.x % shares;
+    const int first = (int)((long long)p.steps * share / shares), last = (int)((long long)p.steps * (share + 1) / shares);
+    const int steps = last - first;
+
+    if (warp == 5) tmem_alloc<1>(&tmem_base, SKINNY_TMEM);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < SKINNY_STAGES; ++s) {
+            ptx::mbar_init(&full[s], 2);
             ptx::mbar_init(&empty[s], 1);
         }
         ptx::mbar_init(&done, 1);
@@ -149,122 +733,117 @@ __global__ void __launch_bounds__(PRODUCT_THREADS)
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
-    const uint32_t sums = tmem_base, scale_columns = tmem_base + TILE;
+    const uint32_t tmem = tmem_base;
+    float sum[SKINNY_MAX_N];
+    bool ok = true;
 
     if (warp == 4) {
         int issued = 0;
-        bool ok = true;
-        unsigned held_a = 0, held_b = 0;  // scale bytes of 32 steps, one per lane
+        unsigned held_a = 127, held_b = 127;  // scale bytes of 32 steps, one per lane
         for (int i = 0; i < steps; ++i) {
-            if (i % 32 == 0 && i + lane < steps) {
-                const int kb = i + lane;
-                held_a = p.a_scales[p.transpose_a ? (long long)kb * p.a_scale_cols + tile_m
-                                                  : (long long)tile_m * p.a_scale_cols + kb];
-                held_b = p.b_scales[p.transpose_b ? (long long)tile_n * p.b_scale_cols + kb
-                                                  : (long long)kb * p.b_scale_cols + tile_n];
-            }
-            const int s = i % STAGES;
-            ok = bounded_wait(&empty[s], ((i / STAGES) & 1) ^ 1, &g_product_error, 1);
+            const int s = i % SKINNY_STAGES;
+            ok = bounded_wait(&empty[s], ((i / SKINNY_STAGES) & 1) ^ 1, &g_product_error, 1);
             if (!ok) break;
+            const int k0 = (first + i) * STEP;
+            if (lane == 0) {
+                ptx::mbar_arrive_expect_tx(&full[s], 128 * STEP + column_bytes);
+                const uint32_t at = base + s * stage_bytes, bar = ptx::smem_addr(&full[s]);
+                tma_load_2d<1>(at, &a_map, p.transpose_a ? tile * 128 : k0, p.transpose_a ? k0 : tile * 128, bar);
+                tma_load_2d<1>(at + 128 * STEP, &b_map, p.transpose_b ? k0 : 0, p.transpose_b ? 0 : k0, bar);
+            }
+            ++issued;
+            if (i % 32 == 0 && i + lane < steps) {
+                const long long kb = first + i + lane;
+                held_a = p.a_scales[p.transpose_a ? kb * p.a_scale_cols + tile : (long long)tile * p.a_scale_cols + kb];
+                held_b = p.b_scales[p.transpose_b ? kb : kb * p.b_scale_cols];
+            }
             const unsigned wa = __shfl_sync(0xffffffffu, held_a, i % 32) * 0x01010101u;
             const unsigned wb = __shfl_sync(0xffffffffu, held_b, i % 32) * 0x01010101u;
-            uint8_t *stage = aligned + s * STAGE_BYTES;
-            uint4 *words = reinterpret_cast<uint4 *>(stage + 2 * TILE_BYTES);
+            uint4 *words = reinterpret_cast<uint4 *>(aligned + s * stage_bytes + 128 * STEP + column_bytes);
             words[lane] = make_uint4(wa, wa, wa, wa);
             words[32 + lane] = make_uint4(wb, wb, wb, wb);
             ptx::fence_proxy_async();
             __syncwarp();
-            if (lane == 0) {
-                ptx::mbar_arrive_expect_tx(&full[s], 2 * TILE_BYTES);
-                const uint32_t at = base + s * STAGE_BYTES;
-                if (p.transpose_a)
-                    tma_load_2d(at, &a_map, tile_m * TILE, i * TILE, &full[s]);
-                else
-                    tma_load_2d(at, &a_map, i * TILE, tile_m * TILE, &full[s]);
-                if (p.transpose_b)
-                    tma_load_2d(at + TILE_BYTES, &b_map, i * TILE, tile_n * TILE, &full[s]);
-                else
-                    tma_load_2d(at + TILE_BYTES, &b_map, tile_n * TILE, i * TILE, &full[s]);
-            }
-            ++issued;
+            if (lane == 0) ptx::mbar_arrive(&full[s]);
         }
         if (!ok)  // copies in flight end before the block does
-            for (int i = max(0, issued - STAGES); i < issued; ++i)
-                bounded_wait(&full[i % STAGES], (i / STAGES) & 1, &g_product_error, 2);
+            for (int i = max(0, issued - SKINNY_STAGES); i < issued; ++i)
+                bounded_wait(&full[i % SKINNY_STAGES], (i / SKINNY_STAGES) & 1, &g_product_error, 2);
     } else if (warp == 5) {
-        // bits: A and B e4m3 (0), A and B major-ness, N/8, e8m0 scales, M/16
-        const uint32_t idesc = (uint32_t)(p.transpose_a ? 1 : 0) << 15 | (uint32_t)(p.transpose_b ? 0 : 1) << 16 |
-                               (TILE >> 3) << 17 | 1u << 23 | (TILE >> 4) << 24;
-        // 32 contracted values further on: 32 bytes along a row, or 32 rows of 128 bytes
+        const uint32_t idesc = instruction_desc(p, 128, p.tile_n);
         const uint32_t step_a = (p.transpose_a ? CONTRACTED_PER_MMA * 128 : CONTRACTED_PER_MMA) >> 4;
         const uint32_t step_b = (p.transpose_b ? CONTRACTED_PER_MMA : CONTRACTED_PER_MMA * 128) >> 4;
-        bool ok = true;
         for (int i = 0; i < steps; ++i) {
-            const int s = i % STAGES;
-            ok = bounded_wait(&full[s], (i / STAGES) & 1, &g_product_error, 3);
+            const int s = i % SKINNY_STAGES;
+            ok = bounded_wait(&full[s], (i / SKINNY_STAGES) & 1, &g_product_error, 3);
+            if (ok && i > 0 && i % CHUNK == 0) ok = bounded_wait(&drained, (i / CHUNK - 1) & 1, &g_product_error, 5);
             if (!ok) break;
-            if (i > 0 && i % CHUNK == 0) {
-                ok = bounded_wait(&drained, (i / CHUNK - 1) & 1, &g_product_error, 5);
-                if (!ok) break;
-            }
             fence_after_sync();
-            if (elect_one()) {
-                const uint32_t at = base + s * STAGE_BYTES;
-                const uint32_t scale_a = scale_columns + s * 8, scale_b = scale_a + 4;
-                tmem_copy_scales(scale_a, scales_desc(at + 2 * TILE_BYTES));
-                tmem_copy_scales(scale_b, scales_desc(at + 2 * TILE_BYTES + SCALE_BYTES));
-                const uint64_t da = operand_desc(at), db = operand_desc(at + TILE_BYTES);
+            if (lane == 0) {
+                const uint32_t at = base + s * stage_bytes, words = at + 128 * STEP + column_bytes;
+                const uint32_t scale_a = tmem + SKINNY_MAX_N + s * 8, scale_b = scale_a + 4;
+                tmem_copy_scales<1>(scale_a, scales_desc(words));
+                tmem_copy_scales<1>(scale_b, scales_desc(words + SCALE_BYTES));
+                const uint64_t da = operand_desc(at), db = operand_desc(at + 128 * STEP);
 #pragma unroll
-                for (int j = 0; j < TILE / CONTRACTED_PER_MMA; ++j)
-                    mma_block_scaled(sums, da + j * step_a, db + j * step_b, idesc, scale_a, scale_b, i % CHUNK + j > 0);
-                mma_commit(&empty[s]);
-                if (i + 1 == steps || i % CHUNK == CHUNK - 1) mma_commit(&done);
+                for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
+                    mma_block_scaled<1>(tmem, da + j * step_a, db + j * step_b, idesc, scale_a, scale_b, i % CHUNK + j > 0);
+                mma_commit<1>(&empty[s]);
+                if (i + 1 == steps || i % CHUNK == CHUNK - 1) mma_commit<1>(&done);
             }
             __syncwarp();
         }
     } else {
-        float sum[TILE];
 #pragma unroll
-        for (int i = 0; i < TILE; ++i) sum[i] = 0.0f;
-        bool ok = true;
+        for (int i = 0; i < SKINNY_MAX_N; ++i) sum[i] = 0.0f;
         for (int chunk = 0; chunk * CHUNK < steps; ++chunk) {
             ok = bounded_wait(&done, chunk & 1, &g_product_error, 4);
             if (!ok) break;
             fence_after_sync();
 #pragma unroll
-            for (int c0 = 0; c0 < TILE; c0 += 32) {
-                uint32_t r[32];
-                tmem_load32(sums + ((uint32_t)(warp * 32) << 16) + c0, r);
+            for (int c0 = 0; c0 < SKINNY_MAX_N; c0 += 32) {
+                if (c0 < p.tile_n) {  // of 16 columns the other 16 are read and dropped
+                    uint32_t r[32];
+                    tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) sum[c0 + i] += __uint_as_float(r[i]);
+                    for (int i = 0; i < 32; ++i) sum[c0 + i] += __uint_as_float(r[i]);
+                }
             }
             fence_before_sync();
             ptx::mbar_arrive(&drained);
-        }
-        const long long row = (long long)tile_m * TILE + warp * 32 + lane;
-        if (ok && row < p.m) {
-#pragma unroll
-            for (int i = 0; i < TILE; ++i) {
-                const int col = tile_n * TILE + i;
-                if (col < p.n) {
-                    float v = sum[i];
-                    if (p.c_bf16) {
-                        __nv_bfloat16 *c = static_cast<__nv_bfloat16 *>(p.c) + row * p.c_stride + col;
-                        if (p.accumulate) v += __bfloat162float(*c);
-                        *c = __float2bfloat16_rn(v);
-                    } else {
-                        float *c = static_cast<float *>(p.c) + row * p.c_stride + col;
-                        if (p.accumulate) v += *c;
-                        *c = v;
-                    }
-                }
-            }
         }
     }
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
-    if (warp == 5) tmem_free(tmem_base, TMEM_COLUMNS);
+    if (warp == 5) tmem_free<1>(tmem, SKINNY_TMEM);
+
+    // the stages are free: block 0 collects the other blocks' sums there, [share][column][128 rows]
+    float *sums_of = reinterpret_cast<float *>(aligned);
+    const int columns = min(p.tile_n, p.n);
+    if (shares > 1) {
+        cluster_sync();  // every block's stages are idle
+        if (warp < 4 && share > 0) {
+            const uint32_t to = cluster_addr(base, 0) + ((share - 1) * p.tile_n * 128 + warp * 32 + lane) * 4;
+#pragma unroll
+            for (int i = 0; i < SKINNY_MAX_N; ++i)
+                if (i < columns)
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + i * 512), "f"(sum[i]) : "memory");
+        }
+        cluster_sync();
+        if (share > 0) return;
+    }
+    if (warp < 4) {
+        const long long row = (long long)tile * 128 + warp * 32 + lane;
+#pragma unroll
+        for (int i = 0; i < SKINNY_MAX_N; ++i) {
+            if (i < columns && row < p.m) {
+                float v = sum[i];
+                for (int q = 1; q < shares; ++q) v += sums_of[((q - 1) * p.tile_n + i) * 128 + warp * 32 + lane];
+                store_c(p, row, i, v);
+            }
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -288,17 +867,130 @@ EncodeTiled encode_tiled()
     return fn;
 }
 
-// Boxes of 128 x 128 codes in the 128-byte swizzle; codes outside the matrix read as zero.
-bool operand_map(CUtensorMap *map, const dipaco_packed *x)
+// Boxes of `rows` x 128 codes in the 128-byte swizzle; codes outside the matrix read as zero.
+bool operand_map(CUtensorMap *map, const dipaco_packed *x, int rows)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)x->cols, (cuuint64_t)x->rows};
     const cuuint64_t strides[1] = {(cuuint64_t)x->stride};
-    const cuuint32_t box[2] = {TILE, TILE}, steps[2] = {1, 1};
+    const cuuint32_t box[2] = {128, (cuuint32_t)rows}, steps[2] = {1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, x->codes, dims, strides, box, steps,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Boxes of 32 x 32 results, rows of 64 or 128 bytes in the swizzle of that width.
+bool result_map(CUtensorMap *map, void *c, int64_t m, int64_t n, int64_t stride, int dtype)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const bool bf16 = dtype == DIPACO_BF16;
+    const cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m};
+    const cuuint64_t strides[1] = {(cuuint64_t)(stride * dense_size(dtype))};
+    const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, c, dims, strides,
+                  box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int PAIRS = 74;  // pairs of the 148 SMs
+
+// How a product is cut up.  Times are in clocks of one SM; the constants are measured.
+struct PairPlan {
+    int tile_n = 256, tiles_m = 0, tiles_n = 0, pairs = 0, whole_tiles = 0;
+    int64_t workspace = 0;
+};
+
+PairPlan plan_pairs(int64_t m, int64_t n, int64_t steps)
+{
+    PairPlan best;
+    double best_time = 0.0;
+    for (int tile_n = 256; tile_n >= 64; tile_n -= 32) {
+        PairPlan plan;
+        plan.tile_n = tile_n;
+        plan.tiles_m = (int)ceil_div(m, PAIR_ROWS);
+        plan.tiles_n = (int)ceil_div(n, tile_n);
+        const int64_t tiles = (int64_t)plan.tiles_m * plan.tiles_n;
+        plan.pairs = (int)std::min<int64_t>(PAIRS, tiles);
+        // a step is bound by the products (2 clocks per column) or by its operands' way from L2
+        const double step = std::max(2.0 * tile_n, 64.0 * 4 + tile_n * 1.0);
+        const double gap = tile_n > PAIR_SCALES_AT / 2 ? 500.0 : 0.0;  // sets of sums that overlap
+        const double whole = (double)ceil_div(tiles, plan.pairs) * (steps * step + gap);
+        double time = whole;
+        plan.whole_tiles = (int)tiles;
+        // the last, unfilled round and one full round before it dealt out step by step, with a second
+        // launch that joins the partial sums
+        const int64_t kept = std::max<int64_t>(0, (tiles / PAIRS - 1) * PAIRS), dealt = tiles - kept;
+        if (dealt % PAIRS != 0 && dealt * steps >= 4 * PAIRS) {
+            const double join = 8000.0 + 2.0 * tile_n * 256 * 4 / 40.0;
+            const double shared = (double)(kept / PAIRS) * (steps * step + gap) + (double)dealt * steps / PAIRS * step + 2 * gap + join;
+            if (shared < time) {
+                time = shared;
+                plan.pairs = PAIRS;
+                plan.whole_tiles = (int)kept;
+                plan.workspace = (int64_t)2 * PAIRS * PAIR_ROWS * tile_n * (int64_t)sizeof(float);
+            }
+        }
+        if (best_time == 0.0 || time < best_time) {
+            best_time = time;
+            best = plan;
+        }
+    }
+    return best;
+}
+
+bool is_skinny(int64_t m, int64_t n) { return std::min(m, n) <= SKINNY_MAX_N; }
+
+int launch_skinny(const dipaco_packed *a, const dipaco_packed *b, ProductArgs p, int64_t k, cudaStream_t stream)
+{
+    if (p.m < p.n) {  // C^T = op(B)^T op(A)^T: the long side gives the rows
+        std::swap(a, b);
+        std::swap(p.a_scales, p.b_scales);
+        std::swap(p.a_scale_cols, p.b_scale_cols);
+        std::swap(p.m, p.n);
+        std::swap(p.c_row, p.c_col);
+        const int ta = p.transpose_a;
+        p.transpose_a = !p.transpose_b;
+        p.transpose_b = !ta;
+    }
+    p.tile_n = p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
+    const int column_bytes = p.transpose_b ? p.tile_n * STEP : SKINNY_COLUMN_BYTES;
+    const int64_t tiles = ceil_div(p.m, 128);
+    // enough blocks for two on every SM, at least two steps each
+    const int sums_bytes = p.tile_n * 128 * (int)sizeof(float);
+    const int shares = (int)std::min<int64_t>(
+        {SKINNY_MAX_CLUSTER, ceil_div(p.steps, 2), ceil_div(296, tiles), 1 + SKINNY_MAX_COLLECTED / sums_bytes});
+    const int collected = (shares - 1) * sums_bytes;
+    const int smem = std::max(SKINNY_STAGES * skinny_stage_bytes(column_bytes), collected) + 1024;
+    if (tiles * shares > INT32_MAX) return DIPACO_ELIMIT;
+    CUtensorMap a_map, b_map;
+    if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, p.transpose_b ? p.tile_n : 128)) return DIPACO_ECUDA;
+    if (cudaFuncSetAttribute(skinny_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+        return launch_status();
+    cudaLaunchAttribute cluster = {};
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = shares;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3((unsigned)(tiles * shares));
+    config.blockDim = dim3(SKINNY_THREADS);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = &cluster;
+    config.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&config, skinny_kernel, a_map, b_map, p, shares, column_bytes);
+    return err == cudaSuccess ? DIPACO_OK : launch_status();
+}
+
+template <bool CHUNKED>
+int launch_pairs(const CUtensorMap &a_map, const CUtensorMap &b_map, const CUtensorMap &c_map, const ProductArgs &p,
+                 int pairs, cudaStream_t stream)
+{
+    if (cudaFuncSetAttribute(pair_kernel<CHUNKED>, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM) != cudaSuccess)
+        return launch_status();
+    pair_kernel<CHUNKED><<<2 * pairs, PAIR_THREADS, PAIR_SMEM, stream>>>(a_map, b_map, c_map, p);
+    return launch_status();
 }
 
 } // namespace
@@ -310,7 +1002,7 @@ int dipaco_packed_matmul_workspace(int64_t m, int64_t n, int64_t k, int64_t *byt
     if (!bytes || k < 0) return DIPACO_EINVAL;
     if (const int rc = check_extents(m, n)) return rc;
     if (k > MAX_EXTENT) return DIPACO_ELIMIT;
-    *bytes = 0;
+    *bytes = m == 0 || n == 0 || k == 0 || is_skinny(m, n) ? 0 : plan_pairs(m, n, ceil_div(k, STEP)).workspace;
     return DIPACO_OK;
 }
 
@@ -337,17 +1029,40 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
         const size_t pitch = m == 1 ? n * size : c_stride * size;
         return cudaMemset2DAsync(c, pitch, 0, n * size, m, stream) == cudaSuccess ? DIPACO_OK : launch_status();
     }
-    const int64_t tiles = ceil_div(m, TILE) * ceil_div(n, TILE);
-    if (tiles > INT32_MAX) return DIPACO_ELIMIT;
-    CUtensorMap a_map, b_map;
-    if (!operand_map(&a_map, a) || !operand_map(&b_map, b)) return DIPACO_ECUDA;
-    ProductArgs p = {static_cast<const uint8_t *>(a->scales), static_cast<const uint8_t *>(b->scales),
-                     (int)ceil_div(a->cols, PACK_BLOCK), (int)ceil_div(b->cols, PACK_BLOCK),
-                     transpose_a != 0, transpose_b != 0, (int)m, (int)n, (int)k, c, c_stride,
-                     dtype == DIPACO_BF16, accumulate != 0};
-    if (cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PRODUCT_SMEM) != cudaSuccess)
-        return launch_status();
-    product_kernel<<<(unsigned)tiles, PRODUCT_THREADS, PRODUCT_SMEM, stream>>>(a_map, b_map, p);
+    ProductArgs p = {};
+    p.a_scales = static_cast<const uint8_t *>(a->scales);
+    p.b_scales = static_cast<const uint8_t *>(b->scales);
+    p.a_scale_cols = (int)ceil_div(a->cols, PACK_BLOCK);
+    p.b_scale_cols = (int)ceil_div(b->cols, PACK_BLOCK);
+    p.transpose_a = transpose_a != 0;
+    p.transpose_b = transpose_b != 0;
+    p.m = (int)m;
+    p.n = (int)n;
+    p.steps = (int)ceil_div(k, STEP);
+    p.c = c;
+    p.c_row = c_stride;
+    p.c_col = 1;
+    p.c_bf16 = dtype == DIPACO_BF16;
+    p.accumulate = accumulate != 0;
+    if (is_skinny(m, n)) return launch_skinny(a, b, p, k, stream);
+
+    if (ceil_div(m, PAIR_ROWS) * ceil_div(n, 64) > INT32_MAX) return DIPACO_ELIMIT;
+    const PairPlan plan = plan_pairs(m, n, p.steps);
+    p.tile_n = plan.tile_n;
+    p.tiles_m = plan.tiles_m;
+    p.tiles_n = plan.tiles_n;
+    p.whole_tiles = plan.whole_tiles;
+    p.partial = static_cast<float *>(workspace);
+    CUtensorMap a_map, b_map, c_map = {};
+    if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, transpose_b ? plan.tile_n / 2 : 128)) return DIPACO_ECUDA;
+    p.store_by_tma = !accumulate && rows_aligned16(c, c_stride, m, dense_size(dtype));
+    if (p.store_by_tma && !result_map(&c_map, c, m, n, c_stride, dtype)) return DIPACO_ECUDA;
+    if (const int rc = p.c_bf16 ? launch_pairs<false>(a_map, b_map, c_map, p, plan.pairs, stream)
+                                : launch_pairs<true>(a_map, b_map, c_map, p, plan.pairs, stream))
+        return rc;
+    const int64_t dealt = (int64_t)plan.tiles_m * plan.tiles_n - plan.whole_tiles;
+    if (dealt > 0)
+        join_kernel<<<(unsigned)(dealt * 2 * (plan.tile_n / 32)), 256, 0, stream>>>(p, plan.pairs);
     return launch_status();
 }
 

@@ -447,6 +447,57 @@ def test_product_of_packed_matrices(m, n, k, form):
         assert bool((hold[:, :3] == 3.0).all()) and bool((hold[:, 3 + n:] == 3.0).all())
 
 
+def random_packed_on_device(seed, rows, cols, std=1.0):
+    """(Packed, float64 values on the device) of normal values whose blocks differ in size."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    size = torch.empty(-(-rows // 128), -(-cols // 128), device=DEV).normal_(0.0, 1.0, generator=g).exp()
+    x = torch.empty(rows, cols, device=DEV).normal_(0.0, std, generator=g) * ref.spread(size, rows, cols)
+    p = inner.pack(x)
+    return p, p.codes.double() * ref.spread(p.scales.double(), rows, cols)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", sorted(FORMS))
+@pytest.mark.parametrize("m,n,k", [(2000, 1792, 900), (4100, 2048, 512), (600, 1000, 9000), (3000, 5000, 700),
+                                   (300, 70, 20000), (70, 9000, 1500), (65, 4096, 4096), (20000, 900, 128),
+                                   (10000, 2300, 3584), (64, 5000, 4100), (8000, 20, 2500)])
+def test_product_of_larger_packed_matrices(m, n, k, form):
+    """Several tiles per block, ragged last tiles, contractions shared between blocks."""
+    ta, tb = FORMS[form]
+    a, av = random_packed_on_device(m + n, *((k, m) if ta else (m, k)))
+    b, bv = random_packed_on_device(n + k, *((n, k) if tb else (k, n)), std=0.02)
+    av, bv = (av.t() if ta else av), (bv.t() if tb else bv)
+    want = av @ bv
+    for dtype in (F32, BF16):
+        got = inner.packed_matmul(a, b, ta, tb, dtype)
+        assert inner.packed_matmul_status() == B.DIPACO_OK
+        tol = product_tolerance(av, bv, k)
+        err, tol = (got.double() - want).abs(), tol + half(dtype, want.abs() + tol)
+        assert bool((err <= tol).all()), (dtype, float((err / tol).max()))
+        assert torch.equal(got, inner.packed_matmul(a, b, ta, tb, dtype))
+        out = torch.full((m, n + 3), 1.0, dtype=dtype, device=DEV)[:, 1:n + 1]
+        inner.packed_matmul(a, b, ta, tb, out=out, accumulate=True)
+        total = want + 1.0
+        err = (out.double() - total).abs()
+        tol = product_tolerance(av, bv, k) + U * total.abs()
+        assert bool((err <= tol + half(dtype, total.abs() + tol)).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(300, 400), (40, 50)])
+def test_long_sums_in_fp32_do_not_drift(m, n):
+    """2048 values at a time on the tensor cores, 64 additions each off by at most 2^-24 of the sum on
+    average over truncation, the parts added in fp32: the norm of the error stays under
+    (64 + parts) * 2^-24 of the result's."""
+    k = 40000
+    a, av = random_packed_on_device(1, k, m)
+    b, bv = random_packed_on_device(2, k, n)
+    want = av.t() @ bv
+    got = inner.packed_matmul(a, b, transpose_a=True, out_dtype=F32)
+    assert float((got.double() - want).norm() / want.norm()) <= (64 + k / 2048) * U
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("form", sorted(FORMS))
 def test_products_are_exact_for_small_whole_numbers(form):
