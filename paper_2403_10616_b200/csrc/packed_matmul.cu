@@ -26,6 +26,14 @@ static __device__ int g_product_error;  // set by a bounded wait that ran out
 
 // ------------------------------------------------------------------------------------------ PTX
 
+// True on one thread of the warp.  Asynchronous copies and products are issued under it: the compiler
+// then keeps their operands in uniform registers, which it does not under a test of the lane.
+__device__ __forceinline__ bool elect_one()
+{
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
 // An address of this block's shared memory as seen from, or for, block `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t address, unsigned rank)
 {
@@ -202,6 +210,10 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t address)
 constexpr int STEP = 128;                 // contracted values per step: one block
 constexpr int CONTRACTED_PER_MMA = 32;
 constexpr int SCALE_BYTES = 512;          // of shared memory for four columns: 32 lanes x 16 bytes
+// A scale word holds the bytes of QUAD steps, and the instruction descriptor says which byte counts: the
+// words are copied to tensor memory once for four steps.  Copies take the tensor cores' time: one for
+// each step cost 20 % (8192^3: 555 us, 445 without any copy).
+constexpr int QUAD = 4;
 // The tensor cores truncate when they add to an fp32 sum, which drifts by about 1.2e-8 of the sum for
 // every 32 contracted values (2.4e-5 over 65501).  Sums that are returned in fp32 are therefore taken
 // out of tensor memory every CHUNK steps, 2048 values, and added up in registers: under 1e-6.  A result
@@ -223,12 +235,16 @@ struct ProductArgs {
     float *partial;
 };
 
-// Bits: A and B e4m3 (0), A and B major-ness, N/8, e8m0 scales, M/16.
+// Bits: A and B e4m3 (0), A and B major-ness, N/8, e8m0 scales, M/16; scale_byte_desc adds the scale words'
+// byte for B and A.
 __device__ __forceinline__ uint32_t instruction_desc(const ProductArgs &p, int m, int n)
 {
     return (uint32_t)(p.transpose_a ? 1 : 0) << 15 | (uint32_t)(p.transpose_b ? 0 : 1) << 16 | (uint32_t)(n >> 3) << 17 |
            1u << 23 | (uint32_t)(m >> 4) << 24;
 }
+
+__device__ __forceinline__ uint32_t scale_byte_desc(int byte) { return (uint32_t)byte << 4 | (uint32_t)byte << 29; }
+__device__ __forceinline__ uint32_t byte_at(uint32_t word, int shift) { return word >> shift & 255u; }
 
 __device__ __forceinline__ void store_c(const ProductArgs &p, long long row, long long col, float v)
 {
@@ -247,25 +263,31 @@ __device__ __forceinline__ void store_c(const ProductArgs &p, long long row, lon
 // ------------------------------------------------------------------------------------------ pairs of SMs
 
 // Each block of the pair holds 128 rows of A and half the tile's columns of B per stage.  Tensor memory:
-// two sets of sums, 12 columns of scales per stage at the end.  With 256 columns the sets overlap: the
+// two sets of sums, and scales of five quads of steps at the end.  With 256 columns the sets overlap: the
 // first set's last columns are the second's first.  They are read out first, and the products of the
 // next tile start as soon as that is done; with fewer columns the sets are apart and the next tile's
 // products only wait for the tile before the last to be read out.
 constexpr int PAIR_STAGES = 5;
 constexpr int PAIR_OPERAND_BYTES = 128 * STEP;
 constexpr int PAIR_STAGE_BYTES = 2 * PAIR_OPERAND_BYTES;
-constexpr int PAIR_WORDS_BYTES = 3 * SCALE_BYTES;  // scale words of a step
-constexpr int PAIR_WORDS_STEPS = 8;  // scale words are written for eight steps at a time: a signal between the blocks
-                                     // for each step held the tensor cores up (16384x2048x8192: 427 us against 285)
+constexpr int PAIR_WORDS_BYTES = 3 * SCALE_BYTES;  // scale words of a quad: of A, and of B twice four columns
+// Scale words are written for 16 steps at a time: a signal between the blocks for each step held the
+// tensor cores up (16384x2048x8192: 427 us against 285 with one for eight).
+constexpr int PAIR_WORDS_STEPS = 16;
+constexpr int PAIR_WORDS_SET = PAIR_WORDS_STEPS / QUAD * PAIR_WORDS_BYTES;
 constexpr int PAIR_EPILOGUE_WARPS = 8;
 constexpr int PAIR_STAGING_BYTES = 4096;  // per epilogue warp: 32 rows x 32 columns in fp32, or twice in bf16
 // shared memory: operands and staging on 1024-byte boundaries (the swizzle goes by address), then scale words
 constexpr int PAIR_STAGING_AT = PAIR_STAGES * PAIR_STAGE_BYTES;
 constexpr int PAIR_WORDS_AT = PAIR_STAGING_AT + PAIR_EPILOGUE_WARPS * PAIR_STAGING_BYTES;
-constexpr int PAIR_SMEM = PAIR_WORDS_AT + 2 * PAIR_WORDS_STEPS * PAIR_WORDS_BYTES + 1024;
+constexpr int PAIR_SMEM = PAIR_WORDS_AT + 2 * PAIR_WORDS_SET + 1024;
 constexpr int PAIR_THREADS = (PAIR_EPILOGUE_WARPS + 3) * 32;  // + loads, products, scale words
+// Scale columns are written again five quads later.  The step that begins quad q has been loaded into
+// the stage of the step five before it, which is thus done, and that step is no earlier than the last of
+// quad q - 5.
 constexpr int PAIR_SCALE_COLUMNS = 12;
-constexpr int PAIR_SCALES_AT = 512 - PAIR_STAGES * PAIR_SCALE_COLUMNS;
+constexpr int PAIR_SCALE_SLOTS = PAIR_STAGES;
+constexpr int PAIR_SCALES_AT = 512 - PAIR_SCALE_SLOTS * PAIR_SCALE_COLUMNS;
 constexpr int PAIR_MAX_N = 256;
 constexpr int PAIR_ROWS = 256;
 constexpr int RASTER = 8;  // row tiles that share column tiles while those are in L2
@@ -429,7 +451,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             for (int i = item.first; i < item.last; ++i) {
                 ok = bounded_wait(&empty[stage], phase ^ 1, &g_product_error, 1);
                 if (!ok) break;
-                if (lane == 0) {
+                if (elect_one()) {
                     const uint32_t to = base + stage * PAIR_STAGE_BYTES;
                     const uint32_t bar = cluster_addr(ptx::smem_addr(&full[stage]), 0);
                     if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * (PAIR_OPERAND_BYTES + b_bytes));
@@ -484,14 +506,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                 }
                 ok = bounded_wait(&words_empty[set], phase ^ 1, &g_product_error, 7);
                 if (!ok) break;
-                uint4 *words = reinterpret_cast<uint4 *>(aligned + PAIR_WORDS_AT + set * PAIR_WORDS_STEPS * PAIR_WORDS_BYTES) + lane;
-                for (int i = 0; i < PAIR_WORDS_STEPS && i0 + i < item.last; ++i) {
-                    const unsigned bytes = __shfl_sync(0xffffffffu, held, at + i);
-                    const unsigned wa = (bytes & 255u) * 0x01010101u;
+                uint4 *words = reinterpret_cast<uint4 *>(aligned + PAIR_WORDS_AT + set * PAIR_WORDS_SET) + lane;
+                for (int i = 0; i < PAIR_WORDS_STEPS && i0 + i < item.last; i += QUAD) {
+                    // the quad's bytes of A's block and of the three of B (after the last step: not used)
+                    unsigned wa = 0u, w0 = 0u, w1 = 0u, w2 = 0u;
+#pragma unroll
+                    for (int j = 0; j < QUAD; ++j) {
+                        const unsigned bytes = __shfl_sync(0xffffffffu, held, at + i + j);
+                        wa |= byte_at(bytes, 0) << 8 * j;
+                        w0 |= byte_at(bytes, 8) << 8 * j;
+                        w1 |= byte_at(bytes, 16) << 8 * j;
+                        w2 |= byte_at(bytes, 24) << 8 * j;
+                    }
                     unsigned wb[8];  // of the eight groups of 32 columns
 #pragma unroll
-                    for (int g = 0; g < 8; ++g)
-                        wb[g] = (bytes >> (8 * (((n0 + 32 * g) >> 7) - block_b) + 8) & 255u) * 0x01010101u;
+                    for (int g = 0; g < 8; ++g) {
+                        const int b = ((n0 + 32 * g) >> 7) - block_b;
+                        wb[g] = b == 0 ? w0 : b == 1 ? w1 : w2;
+                    }
                     words[0] = make_uint4(wa, wa, wa, wa);
                     words[32] = make_uint4(wb[0], wb[1], wb[2], wb[3]);
                     words[64] = make_uint4(wb[4], wb[5], wb[6], wb[7]);
@@ -499,7 +531,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                 }
                 ptx::fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) arrive_cluster(cluster_addr(ptx::smem_addr(&words_full[set]), 0));
+                if (elect_one()) arrive_cluster(cluster_addr(ptx::smem_addr(&words_full[set]), 0));
                 __syncwarp();
                 if (++set == 2) { set = 0; phase ^= 1; }
             }
@@ -518,7 +550,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             PairWalk walk(p, pair, pairs);
             PairItem item;
             int stage = 0, sets = 0;  // sets of sums begun
-            int words_set = 0;
+            int words_set = 0, slot = 0;
             unsigned phase = 0, words_phase = 0;
             bool ok = true;
             while (ok && walk.take(p, pair, item)) {
@@ -537,18 +569,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     ok = bounded_wait(&full[stage], phase, &g_product_error, 3);
                     if (!ok) break;
                     fence_after_sync();
-                    if (lane == 0) {
+                    if (elect_one()) {
                         const uint32_t at = base + stage * PAIR_STAGE_BYTES;
-                        const uint32_t scale_a = tmem + PAIR_SCALES_AT + stage * PAIR_SCALE_COLUMNS, scale_b = scale_a + 4;
-                        const uint32_t words = base + PAIR_WORDS_AT + (words_set * PAIR_WORDS_STEPS + in_words) * PAIR_WORDS_BYTES;
-                        tmem_copy_scales<2>(scale_a, scales_desc(words));
-                        tmem_copy_scales<2>(scale_b, scales_desc(words + SCALE_BYTES));
-                        if (p.tile_n > 128) tmem_copy_scales<2>(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
+                        const uint32_t scale_a = tmem + PAIR_SCALES_AT + slot * PAIR_SCALE_COLUMNS, scale_b = scale_a + 4;
+                        if (in_words % QUAD == 0) {
+                            const uint32_t words =
+                                base + PAIR_WORDS_AT + words_set * PAIR_WORDS_SET + in_words / QUAD * PAIR_WORDS_BYTES;
+                            tmem_copy_scales<2>(scale_a, scales_desc(words));
+                            tmem_copy_scales<2>(scale_b, scales_desc(words + SCALE_BYTES));
+                            if (p.tile_n > 128) tmem_copy_scales<2>(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
+                        }
+                        const uint32_t desc = idesc | scale_byte_desc(in_words % QUAD);
                         const uint64_t da = operand_desc(at), db = operand_desc(at + PAIR_OPERAND_BYTES);
                         const uint32_t sums = tmem + ((sets & 1) ? second_set : 0);
 #pragma unroll
                         for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
-                            mma_block_scaled<2>(sums, da + j * step_a, db + j * step_b, idesc, scale_a, scale_b,
+                            mma_block_scaled<2>(sums, da + j * step_a, db + j * step_b, desc, scale_a, scale_b,
                                                 in_set + j > 0);
                         mma_commit<2>(&empty[stage]);
                         if (words_end) mma_commit<2>(&words_empty[words_set]);
@@ -557,11 +593,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     __syncwarp();
                     if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) ++sets;
                     if (words_end && ++words_set == 2) { words_set = 0; words_phase ^= 1; }
+                    if ((words_end || in_words % QUAD == QUAD - 1) && ++slot == PAIR_SCALE_SLOTS) slot = 0;
                     if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
                 }
             }
             if (!ok) {  // products in flight end before the tensor memory is freed
-                if (lane == 0) mma_commit<2>(&ended);
+                if (elect_one()) mma_commit<2>(&ended);
                 bounded_wait(&ended, 0, &g_product_error, 6);
             }
         }
@@ -701,7 +738,7 @@ constexpr int SKINNY_COLUMN_BYTES = 128 * STEP;  // of a stage, where the short 
 constexpr int SKINNY_THREADS = 192;              // four epilogue warps, load warp, issuing warp
 constexpr int SKINNY_MAX_CLUSTER = 8;
 constexpr int SKINNY_MAX_COLLECTED = 112 * 1024; // other blocks' sums in block 0: leaves room for two blocks per SM
-constexpr int SKINNY_TMEM = 128;                 // 64 of sums, 8 of scales per stage
+constexpr int SKINNY_TMEM = 128;                 // 64 of sums, 8 of scales for each of four quads
 
 __host__ __device__ constexpr int skinny_stage_bytes(int column_bytes) { return 128 * STEP + column_bytes + 2 * SCALE_BYTES; }
 
@@ -745,7 +782,7 @@ __global__ void __launch_bounds__(SKINNY_THREADS)
             ok = bounded_wait(&empty[s], ((i / SKINNY_STAGES) & 1) ^ 1, &g_product_error, 1);
             if (!ok) break;
             const int k0 = (first + i) * STEP;
-            if (lane == 0) {
+            if (elect_one()) {
                 ptx::mbar_arrive_expect_tx(&full[s], 128 * STEP + column_bytes);
                 const uint32_t at = base + s * stage_bytes, bar = ptx::smem_addr(&full[s]);
                 tma_load_2d<1>(at, &a_map, p.transpose_a ? tile * 128 : k0, p.transpose_a ? k0 : tile * 128, bar);
@@ -757,14 +794,20 @@ __global__ void __launch_bounds__(SKINNY_THREADS)
                 held_a = p.a_scales[p.transpose_a ? kb * p.a_scale_cols + tile : (long long)tile * p.a_scale_cols + kb];
                 held_b = p.b_scales[p.transpose_b ? kb : kb * p.b_scale_cols];
             }
-            const unsigned wa = __shfl_sync(0xffffffffu, held_a, i % 32) * 0x01010101u;
-            const unsigned wb = __shfl_sync(0xffffffffu, held_b, i % 32) * 0x01010101u;
-            uint4 *words = reinterpret_cast<uint4 *>(aligned + s * stage_bytes + 128 * STEP + column_bytes);
-            words[lane] = make_uint4(wa, wa, wa, wa);
-            words[32 + lane] = make_uint4(wb, wb, wb, wb);
-            ptx::fence_proxy_async();
+            if (i % QUAD == 0) {
+                unsigned wa = 0u, wb = 0u;  // after the last step: not used
+#pragma unroll
+                for (int j = 0; j < QUAD; ++j) {
+                    wa |= __shfl_sync(0xffffffffu, held_a, i % 32 + j) << 8 * j;
+                    wb |= __shfl_sync(0xffffffffu, held_b, i % 32 + j) << 8 * j;
+                }
+                uint4 *words = reinterpret_cast<uint4 *>(aligned + s * stage_bytes + 128 * STEP + column_bytes);
+                words[lane] = make_uint4(wa, wa, wa, wa);
+                words[32 + lane] = make_uint4(wb, wb, wb, wb);
+                ptx::fence_proxy_async();
+            }
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&full[s]);
+            if (elect_one()) ptx::mbar_arrive(&full[s]);
         }
         if (!ok)  // copies in flight end before the block does
             for (int i = max(0, issued - SKINNY_STAGES); i < issued; ++i)
@@ -779,15 +822,19 @@ __global__ void __launch_bounds__(SKINNY_THREADS)
             if (ok && i > 0 && i % CHUNK == 0) ok = bounded_wait(&drained, (i / CHUNK - 1) & 1, &g_product_error, 5);
             if (!ok) break;
             fence_after_sync();
-            if (lane == 0) {
+            if (elect_one()) {
                 const uint32_t at = base + s * stage_bytes, words = at + 128 * STEP + column_bytes;
-                const uint32_t scale_a = tmem + SKINNY_MAX_N + s * 8, scale_b = scale_a + 4;
-                tmem_copy_scales<1>(scale_a, scales_desc(words));
-                tmem_copy_scales<1>(scale_b, scales_desc(words + SCALE_BYTES));
+                // four slots: the step that begins a quad is loaded where the step four before it was
+                const uint32_t scale_a = tmem + SKINNY_MAX_N + i / QUAD % SKINNY_STAGES * 8, scale_b = scale_a + 4;
+                if (i % QUAD == 0) {
+                    tmem_copy_scales<1>(scale_a, scales_desc(words));
+                    tmem_copy_scales<1>(scale_b, scales_desc(words + SCALE_BYTES));
+                }
+                const uint32_t desc = idesc | scale_byte_desc(i % QUAD);
                 const uint64_t da = operand_desc(at), db = operand_desc(at + 128 * STEP);
 #pragma unroll
                 for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
-                    mma_block_scaled<1>(tmem, da + j * step_a, db + j * step_b, idesc, scale_a, scale_b, i % CHUNK + j > 0);
+                    mma_block_scaled<1>(tmem, da + j * step_a, db + j * step_b, desc, scale_a, scale_b, i % CHUNK + j > 0);
                 mma_commit<1>(&empty[s]);
                 if (i + 1 == steps || i % CHUNK == CHUNK - 1) mma_commit<1>(&done);
             }
