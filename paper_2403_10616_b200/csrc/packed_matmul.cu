@@ -230,7 +230,9 @@ struct ProductArgs {
     int c_bf16, accumulate;
     // pair_kernel
     int tile_n, tiles_m, tiles_n;
-    int whole_tiles;  // tiles that one pair computes from end to end; the steps of the others are dealt out evenly
+    int pairs;
+    int whole_tiles;  // tiles that one pair computes from end to end
+    int head, helpers;  // of the others a pair does the first `head` steps, and `helpers` pairs share the rest
     int store_by_tma;
     float *partial;
 };
@@ -267,27 +269,29 @@ __device__ __forceinline__ void store_c(const ProductArgs &p, long long row, lon
 // first set's last columns are the second's first.  They are read out first, and the products of the
 // next tile start as soon as that is done; with fewer columns the sets are apart and the next tile's
 // products only wait for the tile before the last to be read out.
-constexpr int PAIR_STAGES = 5;
+constexpr int PAIR_STAGES = 6;
 constexpr int PAIR_OPERAND_BYTES = 128 * STEP;
 constexpr int PAIR_STAGE_BYTES = 2 * PAIR_OPERAND_BYTES;
 constexpr int PAIR_WORDS_BYTES = 3 * SCALE_BYTES;  // scale words of a quad: of A, and of B twice four columns
-// Scale words are written for 16 steps at a time: a signal between the blocks for each step held the
-// tensor cores up (16384x2048x8192: 427 us against 285 with one for eight).
-constexpr int PAIR_WORDS_STEPS = 16;
+// Scale words are written for eight steps at a time: a signal between the blocks for each step held the
+// tensor cores up (16384x2048x8192: 427 us against 285).
+constexpr int PAIR_WORDS_STEPS = 8;
 constexpr int PAIR_WORDS_SET = PAIR_WORDS_STEPS / QUAD * PAIR_WORDS_BYTES;
 constexpr int PAIR_EPILOGUE_WARPS = 8;
-constexpr int PAIR_STAGING_BYTES = 4096;  // per epilogue warp: 32 rows x 32 columns in fp32, or twice in bf16
+constexpr int PAIR_STAGING_BYTES = 2048;  // per epilogue warp: 32 rows of 64 bytes
 // shared memory: operands and staging on 1024-byte boundaries (the swizzle goes by address), then scale words
 constexpr int PAIR_STAGING_AT = PAIR_STAGES * PAIR_STAGE_BYTES;
 constexpr int PAIR_WORDS_AT = PAIR_STAGING_AT + PAIR_EPILOGUE_WARPS * PAIR_STAGING_BYTES;
 constexpr int PAIR_SMEM = PAIR_WORDS_AT + 2 * PAIR_WORDS_SET + 1024;
 constexpr int PAIR_THREADS = (PAIR_EPILOGUE_WARPS + 3) * 32;  // + loads, products, scale words
-// Scale columns are written again five quads later.  The step that begins quad q has been loaded into
-// the stage of the step five before it, which is thus done, and that step is no earlier than the last of
-// quad q - 5.
+// Scale columns are written again five quads later, when the last step of the quad that had them is done:
+// the step that begins the new quad has been loaded where the step PAIR_STAGES before it was, which is
+// thus done, and only quads of single steps (short contractions) are closer together than that.
 constexpr int PAIR_SCALE_COLUMNS = 12;
-constexpr int PAIR_SCALE_SLOTS = PAIR_STAGES;
+constexpr int PAIR_SCALE_SLOTS = 5;
 constexpr int PAIR_SCALES_AT = 512 - PAIR_SCALE_SLOTS * PAIR_SCALE_COLUMNS;
+// With 256 columns the sets of sums share 60, the first two groups of 32 that are read out.
+static_assert(PAIR_SCALE_SLOTS < PAIR_STAGES && 2 * 256 - PAIR_SCALES_AT <= 64 && 2 * 224 <= PAIR_SCALES_AT, "tensor memory");
 constexpr int PAIR_MAX_N = 256;
 constexpr int PAIR_ROWS = 256;
 constexpr int RASTER = 8;  // row tiles that share column tiles while those are in L2
@@ -298,38 +302,55 @@ struct PairItem {
     int slot;  // where a partial sum goes; -1: the tile is finished here
 };
 
-// The pieces of one pair: its whole tiles, then its share of the steps of the remaining tiles.
+// The pieces of one pair.  Whole tiles come first, one for each pair and round.  The tiles of a last,
+// unfilled round have a pair each for their first `head` steps, and the other pairs share the steps that
+// are left evenly: all pairs are done at about the same time, and most of them are at the same place of
+// the contraction at the same time, so that they share what they load in L2.
 struct PairWalk {
-    int tile, pairs, whole;
-    long long next, end;
+    int tile;
+    long long next, end;  // a helper's share of the last steps, counted through the tiles
     bool first_share = true;
 
-    __device__ PairWalk(const ProductArgs &p, int pair, int pairs_) : tile(pair), pairs(pairs_), whole(p.whole_tiles)
+    __device__ PairWalk(const ProductArgs &p, int pair) : tile(pair)
     {
-        const long long units = (long long)(p.tiles_m * p.tiles_n - whole) * p.steps;
-        next = units * pair / pairs;
-        end = units * (pair + 1) / pairs;
+        next = end = 0;
+        if (p.helpers > 0 && pair >= p.pairs - p.helpers) share(p, pair - (p.pairs - p.helpers), next, end);
+    }
+    // Of helper h: units [begin, end) of the (steps - head) of every dealt tile.
+    static __device__ void share(const ProductArgs &p, int h, long long &begin, long long &end)
+    {
+        const long long units = (long long)(p.tiles_m * p.tiles_n - p.whole_tiles) * (p.steps - p.head);
+        begin = units * h / p.helpers;
+        end = units * (h + 1) / p.helpers;
     }
     __device__ bool take(const ProductArgs &p, int pair, PairItem &item)
     {
+        const int tiles = p.tiles_m * p.tiles_n;
         int index;
-        if (tile < whole) {
+        if (tile < tiles) {
             index = tile;
-            tile += pairs;
+            tile += p.pairs;
             item.first = 0;
-            item.last = p.steps;
-            item.slot = -1;
+            item.last = index < p.whole_tiles ? p.steps : p.head;
+            item.slot = index < p.whole_tiles ? -1 : index - p.whole_tiles;
         } else {
             if (next >= end) return false;
-            index = whole + (int)(next / p.steps);
-            item.first = (int)(next % p.steps);
+            const int tail = p.steps - p.head, dealt = (int)(next / tail);
+            index = p.whole_tiles + dealt;
+            item.first = p.head + (int)(next % tail);
             item.last = (int)min((long long)p.steps, item.first + (end - next));
-            item.slot = item.first == 0 && item.last == p.steps ? -1 : 2 * pair + (first_share ? 0 : 1);
+            item.slot = helper_slot(p, pair - (p.pairs - p.helpers), !first_share, item.first == p.head && item.last == p.steps, dealt);
             next += item.last - item.first;
             first_share = false;
         }
         place(p, index, item.tile_m, item.tile_n);
         return true;
+    }
+    // Partial sums: of the heads, of tails done by one helper, and two per helper for what it shares with others.
+    static __device__ int helper_slot(const ProductArgs &p, int h, bool later, bool whole_tail, int dealt)
+    {
+        const int tiles = p.tiles_m * p.tiles_n - p.whole_tiles;
+        return whole_tail ? tiles + dealt : 2 * tiles + 2 * h + (later ? 1 : 0);
     }
     static __host__ __device__ void place(const ProductArgs &p, int index, int &tile_m, int &tile_n)
     {
@@ -349,7 +370,7 @@ __device__ __forceinline__ long long partial_offset(const ProductArgs &p, int sl
 // Where an epilogue warp puts 32 columns of its 32 rows.
 __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUtensorMap &c_map, const PairItem &item,
                                                unsigned rank, int quarter, int lane, int c0, const float *v,
-                                               uint8_t *staging, int &buffer)
+                                               uint8_t *staging)
 {
     if (item.slot >= 0) {
         float *out = p.partial + partial_offset(p, item.slot, rank) + (long long)c0 * 128 + quarter * 32 + lane;
@@ -360,44 +381,48 @@ __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUten
     const int row0 = item.tile_m * PAIR_ROWS + (int)rank * 128 + quarter * 32;
     const int col0 = item.tile_n * p.tile_n + c0;
     if (p.store_by_tma) {
-        // rows of 64 or 128 bytes in the copy engine's swizzle of the same width: no bank conflicts
-        uint8_t *at = staging + (p.c_bf16 ? buffer * 2048 : 0);
-        if (p.c_bf16)
-            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-        else
+        // rows of 64 bytes in the copy engine's swizzle of that width: no bank conflicts
+        const int parts = p.c_bf16 ? 1 : 2;
+        for (int part = 0; part < parts; ++part) {
             ptx::bulk_wait_read_all();
-        __syncwarp();
-        if (p.c_bf16) {
+            __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<uint4 *>(at + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) =
-                    Unit<__nv_bfloat16>::narrow(v + 8 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<float4 *>(at + lane * 128 + ((i ^ (lane & 7)) * 16)) =
-                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 4; ++i) {
+                uint4 unit;
+                if (p.c_bf16)
+                    unit = Unit<__nv_bfloat16>::narrow(v + 8 * i);
+                else if (part == 0)
+                    unit = Unit<float>::narrow(v + 4 * i);
+                else
+                    unit = Unit<float>::narrow(v + 16 + 4 * i);
+                *reinterpret_cast<uint4 *>(staging + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) = unit;
+            }
+            ptx::fence_proxy_async();
+            __syncwarp();
+            // columns and rows outside C are not written
+            const int col = col0 + part * 16;
+            if (elect_one()) {
+                if (row0 < p.m && col < p.n) tma_store_2d(&c_map, ptx::smem_addr(staging), col, row0);
+                ptx::bulk_commit();
+            }
+            __syncwarp();
         }
-        ptx::fence_proxy_async();
-        __syncwarp();
-        // columns and rows outside C are not written
-        if (lane == 0) {
-            if (row0 < p.m && col0 < p.n) tma_store_2d(&c_map, ptx::smem_addr(at), col0, row0);
-            ptx::bulk_commit();
-        }
-        __syncwarp();
-        buffer ^= 1;
         return;
     }
     // any alignment, and sums with what is there: rows through shared memory, a lane per column
     float *at = reinterpret_cast<float *>(staging);
-    __syncwarp();
+    for (int part = 0; part < 2; ++part) {  // 16 rows at a time
+        __syncwarp();
+        if (lane >> 4 == part) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) at[lane * 32 + ((i + lane) & 31)] = v[i];
-    __syncwarp();
-    const int rows = min(32, p.m - row0);
-    if (col0 + lane < p.n)
-        for (int r = 0; r < rows; ++r) store_c(p, row0 + r, col0 + lane, at[r * 32 + ((lane + r) & 31)]);
+            for (int i = 0; i < 32; ++i) at[(lane & 15) * 32 + ((i + lane) & 31)] = v[i];
+        }
+        __syncwarp();
+        const int rows = min(16, p.m - row0 - part * 16);
+        if (col0 + lane < p.n)
+            for (int r = 0; r < rows; ++r)
+                store_c(p, row0 + part * 16 + r, col0 + lane, at[r * 32 + ((lane + part * 16 + r) & 31)]);
+    }
 }
 
 template <bool CHUNKED>
@@ -413,7 +438,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
     uint8_t *aligned = raw + (base - ptx::smem_addr(raw));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = cluster_rank();
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int pair = blockIdx.x >> 1;
 
     if (warp == 0) tmem_alloc<2>(&tmem_base, 512);
     if (threadIdx.x == 32) {
@@ -441,7 +466,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
     if (warp == PAIR_EPILOGUE_WARPS) {
         // ---- loads: this block's halves of A and B
         const unsigned b_bytes = p.transpose_b ? half_n * STEP : PAIR_OPERAND_BYTES;
-        PairWalk walk(p, pair, pairs);
+        PairWalk walk(p, pair);
         PairItem item;
         int stage = 0;
         unsigned phase = 0;
@@ -478,7 +503,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
     } else if (warp == PAIR_EPILOGUE_WARPS + 2) {
         // ---- scale words of this block's tensor memory
         const int a_blocks = (p.m + 127) / 128, b_blocks = (p.n + 127) / 128;
-        PairWalk walk(p, pair, pairs);
+        PairWalk walk(p, pair);
         PairItem item;
         int set = 0;
         unsigned phase = 0;
@@ -547,10 +572,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             // 32 contracted values further on: 32 bytes along a row, or 32 rows of 128 bytes
             const uint32_t step_a = (p.transpose_a ? CONTRACTED_PER_MMA * 128 : CONTRACTED_PER_MMA) >> 4;
             const uint32_t step_b = (p.transpose_b ? CONTRACTED_PER_MMA : CONTRACTED_PER_MMA * 128) >> 4;
-            PairWalk walk(p, pair, pairs);
+            PairWalk walk(p, pair);
             PairItem item;
             int stage = 0, sets = 0;  // sets of sums begun
             int words_set = 0, slot = 0;
+            int issued = 0;  // steps
+            int ends[PAIR_SCALE_SLOTS] = {};  // where the last quads ended, the latest first
             unsigned phase = 0, words_phase = 0;
             bool ok = true;
             while (ok && walk.take(p, pair, item)) {
@@ -566,8 +593,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                         if (before >= 0) ok = bounded_wait(&sums_read[before & 1], (before >> 1) & 1, &g_product_error, 5);
                         if (!ok) break;
                     }
+                    if (in_words % QUAD == 0) {
+                        const int last = ends[PAIR_SCALE_SLOTS - 1] - 1;
+                        if (last >= 0 && last > issued - PAIR_STAGES)
+                            ok = bounded_wait(&empty[last % PAIR_STAGES], last / PAIR_STAGES & 1, &g_product_error, 6);
+                        if (!ok) break;
+                    }
                     ok = bounded_wait(&full[stage], phase, &g_product_error, 3);
                     if (!ok) break;
+                    ++issued;
                     fence_after_sync();
                     if (elect_one()) {
                         const uint32_t at = base + stage * PAIR_STAGE_BYTES;
@@ -593,13 +627,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     __syncwarp();
                     if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) ++sets;
                     if (words_end && ++words_set == 2) { words_set = 0; words_phase ^= 1; }
-                    if ((words_end || in_words % QUAD == QUAD - 1) && ++slot == PAIR_SCALE_SLOTS) slot = 0;
+                    if (words_end || in_words % QUAD == QUAD - 1) {
+                        if (++slot == PAIR_SCALE_SLOTS) slot = 0;
+#pragma unroll
+                        for (int q = PAIR_SCALE_SLOTS - 1; q > 0; --q) ends[q] = ends[q - 1];
+                        ends[0] = issued;
+                    }
                     if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
                 }
             }
             if (!ok) {  // products in flight end before the tensor memory is freed
                 if (elect_one()) mma_commit<2>(&ended);
-                bounded_wait(&ended, 0, &g_product_error, 6);
+                bounded_wait(&ended, 0, &g_product_error, 10);
             }
         }
     } else {
@@ -609,9 +648,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
         const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&sums_read[0]), 0),
                                        cluster_addr(ptx::smem_addr(&sums_read[1]), 0)};
         const int groups = p.tile_n / 32;
-        PairWalk walk(p, pair, pairs);
+        PairWalk walk(p, pair);
         PairItem item;
-        int sets = 0, buffer = 0;
+        int sets = 0;
         bool ok = true;
         float total[CHUNKED ? 128 : 1];
         while (ok && walk.take(p, pair, item)) {
@@ -654,7 +693,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                             float v[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-                            finish_columns(p, c_map, item, rank, quarter, lane, g * 32, v, staging, buffer);
+                            finish_columns(p, c_map, item, rank, quarter, lane, g * 32, v, staging);
                         }
                     }
                     if (CHUNKED && !apart && t == 0) {
@@ -675,7 +714,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     for (int u = 0; u < PAIR_MAX_N / 64; ++u)
                         if (2 * u + odd < groups)
                             finish_columns(p, c_map, item, rank, quarter, lane, (2 * u + odd) * 32, total + u * 32,
-                                           staging, buffer);
+                                           staging);
                 }
             }
         }
@@ -690,29 +729,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
 
 // Tiles whose steps were dealt out: their partial sums in the order of the steps.  A block joins 32
 // columns of one block's 128 rows.
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs p, int pairs)
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs p)
 {
     __shared__ float shared[128][33];
     const int groups = p.tile_n / 32;
     const int group = blockIdx.x % groups;
     const unsigned rank = blockIdx.x / groups % 2;
     const int tile = blockIdx.x / (2 * groups);  // among those dealt out
-    const long long units = (long long)(p.tiles_m * p.tiles_n - p.whole_tiles) * p.steps;
-    const long long from = (long long)tile * p.steps, to = from + p.steps;
-    // pair q has the steps from units q / pairs on
-    int first = (int)(from * pairs / units);
-    while (first > 0 && units * first / pairs > from) --first;
-    while (units * (first + 1) / pairs <= from) ++first;
-    if (units * first / pairs <= from && units * (first + 1) / pairs >= to) return;  // finished by one pair
-    float v[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
     const int row = threadIdx.x & 127, side = threadIdx.x >> 7;
-    for (int q = first; q < pairs && units * q / pairs < to; ++q) {
-        const long long begin = units * q / pairs;
-        if (begin == units * (q + 1) / pairs) continue;
-        const int slot = 2 * q + (begin / p.steps == tile ? 0 : 1);
-        const float *in = p.partial + partial_offset(p, slot, rank) + (long long)(group * 32 + side * 16) * 128 + row;
+    const long long at = (long long)(group * 32 + side * 16) * 128 + row;
+    float v[16];
+    const float *in = p.partial + partial_offset(p, tile, rank) + at;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = in[i * 128];
+    const int tail = p.steps - p.head;
+    const long long from = (long long)tile * tail, to = from + tail;
+    const long long units = (long long)(p.tiles_m * p.tiles_n - p.whole_tiles) * tail;
+    int h = (int)(from * p.helpers / units);  // the helper that has unit `from`, or the one before it
+    for (; h < p.helpers; ++h) {
+        long long begin, end;
+        PairWalk::share(p, h, begin, end);
+        if (begin >= to) break;
+        if (end <= from || begin == end) continue;
+        const int slot = PairWalk::helper_slot(p, h, begin / tail != tile, begin <= from && end >= to, tile);
+        in = p.partial + partial_offset(p, slot, rank) + at;
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] += in[i * 128];
     }
@@ -927,7 +967,7 @@ bool operand_map(CUtensorMap *map, const dipaco_packed *x, int rows)
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Boxes of 32 x 32 results, rows of 64 or 128 bytes in the swizzle of that width.
+// Boxes of 32 rows of 64 bytes of results, in the swizzle of that width.
 bool result_map(CUtensorMap *map, void *c, int64_t m, int64_t n, int64_t stride, int dtype)
 {
     const EncodeTiled encode = encode_tiled();
@@ -935,9 +975,9 @@ bool result_map(CUtensorMap *map, void *c, int64_t m, int64_t n, int64_t stride,
     const bool bf16 = dtype == DIPACO_BF16;
     const cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m};
     const cuuint64_t strides[1] = {(cuuint64_t)(stride * dense_size(dtype))};
-    const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+    const cuuint32_t box[2] = {bf16 ? 32u : 16u, 32}, steps[2] = {1, 1};
     return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, c, dims, strides,
-                  box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                  box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                   CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -945,7 +985,7 @@ constexpr int PAIRS = 74;  // pairs of the 148 SMs
 
 // How a product is cut up.  Times are in clocks of one SM; the constants are measured.
 struct PairPlan {
-    int tile_n = 256, tiles_m = 0, tiles_n = 0, pairs = 0, whole_tiles = 0;
+    int tile_n = 256, tiles_m = 0, tiles_n = 0, pairs = 0, whole_tiles = 0, head = 0, helpers = 0;
     int64_t workspace = 0;
 };
 
@@ -960,23 +1000,23 @@ PairPlan plan_pairs(int64_t m, int64_t n, int64_t steps)
         plan.tiles_n = (int)ceil_div(n, tile_n);
         const int64_t tiles = (int64_t)plan.tiles_m * plan.tiles_n;
         plan.pairs = (int)std::min<int64_t>(PAIRS, tiles);
+        plan.whole_tiles = (int)tiles;
         // a step is bound by the products (2 clocks per column) or by its operands' way from L2
         const double step = std::max(2.0 * tile_n, 64.0 * 4 + tile_n * 1.0);
         const double gap = tile_n > PAIR_SCALES_AT / 2 ? 500.0 : 0.0;  // sets of sums that overlap
-        const double whole = (double)ceil_div(tiles, plan.pairs) * (steps * step + gap);
-        double time = whole;
-        plan.whole_tiles = (int)tiles;
-        // the last, unfilled round and one full round before it dealt out step by step, with a second
-        // launch that joins the partial sums
-        const int64_t kept = std::max<int64_t>(0, (tiles / PAIRS - 1) * PAIRS), dealt = tiles - kept;
-        if (dealt % PAIRS != 0 && dealt * steps >= 4 * PAIRS) {
-            const double join = 8000.0 + 2.0 * tile_n * 256 * 4 / 40.0;
-            const double shared = (double)(kept / PAIRS) * (steps * step + gap) + (double)dealt * steps / PAIRS * step + 2 * gap + join;
+        double time = (double)ceil_div(tiles, PAIRS) * (steps * step + gap);
+        // a last, unfilled round with its steps dealt out to all pairs, and a second launch that joins sums
+        const int64_t dealt = tiles % PAIRS, helpers = PAIRS - dealt, head = ceil_div(dealt * steps, PAIRS);
+        if (dealt > 0 && head < steps) {
+            const double join = 8000.0 + 3.0 * dealt * tile_n * 256 * 4 / 4000.0;
+            const double shared = (double)(tiles / PAIRS) * (steps * step + gap) + head * step + 2 * gap + join;
             if (shared < time) {
                 time = shared;
                 plan.pairs = PAIRS;
-                plan.whole_tiles = (int)kept;
-                plan.workspace = (int64_t)2 * PAIRS * PAIR_ROWS * tile_n * (int64_t)sizeof(float);
+                plan.whole_tiles = (int)(tiles - dealt);
+                plan.head = (int)head;
+                plan.helpers = (int)helpers;
+                plan.workspace = (2 * dealt + 2 * helpers) * PAIR_ROWS * tile_n * (int64_t)sizeof(float);
             }
         }
         if (best_time == 0.0 || time < best_time) {
@@ -1098,7 +1138,10 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     p.tile_n = plan.tile_n;
     p.tiles_m = plan.tiles_m;
     p.tiles_n = plan.tiles_n;
+    p.pairs = plan.pairs;
     p.whole_tiles = plan.whole_tiles;
+    p.head = plan.head;
+    p.helpers = plan.helpers;
     p.partial = static_cast<float *>(workspace);
     CUtensorMap a_map, b_map, c_map = {};
     if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, transpose_b ? plan.tile_n / 2 : 128)) return DIPACO_ECUDA;
@@ -1109,7 +1152,7 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
         return rc;
     const int64_t dealt = (int64_t)plan.tiles_m * plan.tiles_n - plan.whole_tiles;
     if (dealt > 0)
-        join_kernel<<<(unsigned)(dealt * 2 * (plan.tile_n / 32)), 256, 0, stream>>>(p, plan.pairs);
+        join_kernel<<<(unsigned)(dealt * 2 * (plan.tile_n / 32)), 256, 0, stream>>>(p);
     return launch_status();
 }
 
