@@ -111,6 +111,13 @@ __device__ __forceinline__ unsigned encode4(const float *f, float reciprocal)
 {
     return encode2(f[0], f[1], reciprocal) | (encode2(f[2], f[3], reciprocal) << 16);
 }
+// The same where no value is infinite.
+__device__ __forceinline__ unsigned encode4_finite(const float *f, float reciprocal)
+{
+    const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0] * reciprocal, f[1] * reciprocal), __NV_SATFINITE, __NV_E4M3);
+    const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2] * reciprocal, f[3] * reciprocal), __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
+}
 __device__ __forceinline__ float2 decode2(unsigned codes)
 {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);

@@ -15,8 +15,8 @@ namespace {
 
 // ------------------------------------------------------------------------------------------ sums over a row
 
-// Sum over the TPR threads of a row.  Rows of up to 32 threads lie inside a warp; of wider ones the
-// block holds blockDim/TPR, and every thread of the block takes part.
+// Sum over the TPR threads of a row.  Rows of up to 32 threads lie inside a warp; of wider ones every
+// thread of the block takes part, and `shared` (one slot per warp) is used once.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float *shared)
 {
@@ -25,7 +25,6 @@ __device__ __forceinline__ float row_sum(float v, float *shared)
     if constexpr (TPR > 32) {
         constexpr int WARPS = TPR / 32;
         const int warp = threadIdx.x >> 5;
-        __syncthreads();
         if ((threadIdx.x & 31) == 0) shared[warp] = v;
         __syncthreads();
         v = 0.0f;
@@ -48,49 +47,70 @@ struct NormArgs {
     bool params_bf16, gamma_aligned, beta_aligned;
 };
 
-// One row per TPR threads, the row in registers.  VEC: 16-byte accesses (rows on 16-byte boundaries).
-template <typename T, bool VEC, int TPR>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_rows_kernel(NormArgs a)
+// One row per TPR threads, the row in registers: NU units of 16 bytes per thread (VEC: rows on 16-byte
+// boundaries), or as many single values.  Bound by memory: about nine instructions per value, and enough
+// rows in flight with a warp per row up to 2048 values in bf16 (1024 in fp32); wider rows take a block.
+template <typename T, bool VEC, int TPR, int NU>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_rows_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
-    constexpr int E = 64 / (int)sizeof(T);
+    constexpr int E = NU * 16 / (int)sizeof(T);
     constexpr int UNITS = E / U;
-    __shared__ float shared[32];
+    __shared__ float shared[2][32];
     const int lane = threadIdx.x % TPR;
     const int row = blockIdx.x * (blockDim.x / TPR) + threadIdx.x / TPR;
     const bool live = row < a.rows;
+    const int cols = live ? a.cols : 0;
     const T *x = static_cast<const T *>(a.x) + (live ? row : 0) * a.x_stride;
 
     float v[E];
+    float sum = 0.0f;
+    if constexpr (VEC) {
+        uint4 raw[UNITS];
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int c = (j * TPR + lane) * U;
+            raw[j] = c < cols ? *reinterpret_cast<const uint4 *>(x + c) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int c = (j * TPR + lane) * U;
+            Unit<T>::widen(raw[j], v + j * U);
+            if (c < cols && c + U > cols) {
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+                    if (c + i >= cols) v[j * U + i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) sum += v[j * U + i];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int c = j * TPR + lane;
+            v[j] = c < cols ? widen1<T>(x[c]) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) sum += v[j];
+    }
+    const float mean = row_sum<TPR>(sum, shared[0]) / (float)a.cols;
+    sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < UNITS; ++j) {
         const int c = (j * TPR + lane) * U;
+        if (c < cols) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) v[j * U + i] = 0.0f;
-        if (c < a.cols && live) {
-            if constexpr (VEC) {
-                Unit<T>::widen(*reinterpret_cast<const uint4 *>(x + c), v + j * U);
+            for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
+            if (VEC && c + U > cols) {
 #pragma unroll
                 for (int i = 0; i < U; ++i)
-                    if (c + i >= a.cols) v[j * U + i] = 0.0f;
-            } else {
-                v[j] = widen1<T>(x[c]);
+                    if (c + i >= cols) v[j * U + i] = 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < U; ++i) sum = fmaf(v[j * U + i], v[j * U + i], sum);
         }
     }
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) sum += v[i];
-    const float mean = row_sum<TPR>(sum, shared) / (float)a.cols;
-    sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < UNITS; ++j)
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const float d = (j * TPR + lane) * U + i < a.cols ? v[j * U + i] - mean : 0.0f;
-            sum = fmaf(d, d, sum);
-        }
-    const float rstd = 1.0f / sqrtf(row_sum<TPR>(sum, shared) / (float)a.cols + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<TPR>(sum, shared[1]) / (float)a.cols + a.eps);
     if (!live) return;
     if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
@@ -101,28 +121,28 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_rows_kernel(NormAr
 #pragma unroll
     for (int j = 0; j < UNITS; ++j) {
         const int c = (j * TPR + lane) * U;
-        if (c >= a.cols) continue;
-        float r[U];
+        if (c >= cols) continue;
+        float *r = v + j * U;
 #pragma unroll
-        for (int i = 0; i < U; ++i) r[i] = (v[j * U + i] - mean) * rstd;
+        for (int i = 0; i < U; ++i) r[i] *= rstd;
         if constexpr (VEC) {
             float p[U];
             if (a.gamma) {
-                load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, a.cols, p);
+                load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, cols, p);
 #pragma unroll
                 for (int i = 0; i < U; ++i) r[i] *= p[i];
             }
             if (a.beta) {
-                load_params<U>(a.beta, a.params_bf16, a.beta_aligned, c, a.cols, p);
+                load_params<U>(a.beta, a.params_bf16, a.beta_aligned, c, cols, p);
 #pragma unroll
                 for (int i = 0; i < U; ++i) r[i] += p[i];
             }
-            if (c + U <= a.cols) {
+            if (c + U <= cols) {
                 *reinterpret_cast<uint4 *>(y + c) = Unit<T>::narrow(r);
             } else {
 #pragma unroll
                 for (int i = 0; i < U; ++i)
-                    if (c + i < a.cols) y[c + i] = narrow1<T>(r[i]);
+                    if (c + i < cols) y[c + i] = narrow1<T>(r[i]);
             }
         } else {
             if (a.gamma) r[0] *= load_param(a.gamma, a.params_bf16, c);
@@ -136,17 +156,17 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_rows_kernel(NormAr
 template <typename T>
 __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
 {
-    __shared__ float shared[32];
+    __shared__ float shared[2][32];
     const T *x = static_cast<const T *>(a.x) + (long long)blockIdx.x * a.x_stride;
     float sum = 0.0f;
     for (long long c = threadIdx.x; c < a.cols; c += 1024) sum += widen1<T>(x[c]);
-    const float mean = row_sum<1024>(sum, shared) / (float)a.cols;
+    const float mean = row_sum<1024>(sum, shared[0]) / (float)a.cols;
     sum = 0.0f;
     for (long long c = threadIdx.x; c < a.cols; c += 1024) {
         const float d = widen1<T>(x[c]) - mean;
         sum = fmaf(d, d, sum);
     }
-    const float rstd = 1.0f / sqrtf(row_sum<1024>(sum, shared) / (float)a.cols + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum<1024>(sum, shared[1]) / (float)a.cols + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean;
         if (a.rstd) a.rstd[blockIdx.x] = rstd;
@@ -164,22 +184,23 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
 template <typename T, bool VEC>
 void launch_norm(const NormArgs &a, cudaStream_t stream)
 {
-    constexpr int E = 64 / (int)sizeof(T);
-    const int need = (a.cols + E - 1) / E;  // threads per row
-#define NORM_CASE(TPR)                                                                                     \
-    if (need <= TPR) {                                                                                     \
-        constexpr int threads = TPR < 128 ? 128 : TPR;                                                     \
-        norm_rows_kernel<T, VEC, TPR><<<(unsigned)ceil_div(a.rows, threads / TPR), threads, 0, stream>>>(a); \
-        return;                                                                                            \
+    const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
+#define NORM_CASE(TPR, NU)                                                                                         \
+    if (units <= TPR * NU) {                                                                                       \
+        constexpr int threads = TPR < 128 ? 128 : TPR;                                                             \
+        norm_rows_kernel<T, VEC, TPR, NU><<<(unsigned)ceil_div(a.rows, threads / TPR), threads, 0, stream>>>(a);   \
+        return;                                                                                                    \
     }
-    NORM_CASE(8)
-    NORM_CASE(16)
-    NORM_CASE(32)
-    NORM_CASE(64)
-    NORM_CASE(128)
-    NORM_CASE(256)
-    NORM_CASE(512)
-    NORM_CASE(1024)
+    NORM_CASE(8, 1)
+    NORM_CASE(16, 1)
+    NORM_CASE(32, 1)
+    NORM_CASE(32, 2)
+    NORM_CASE(32, 4)
+    NORM_CASE(32, 8)
+    NORM_CASE(128, 4)
+    NORM_CASE(128, 8)
+    NORM_CASE(256, 8)
+    NORM_CASE(512, 8)
 #undef NORM_CASE
     norm_long_rows_kernel<T><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
 }
@@ -199,18 +220,93 @@ struct NormBackArgs {
     bool params_bf16, gamma_aligned;
 };
 
-// TPR threads per row, each with the same 16 columns of every row that its block passes over: the
-// sums of dgamma and dbeta stay in registers and leave the block once.
+// What a thread loads of a row, before conversion.
+template <typename T, bool PACKED, bool VEC> struct BackRow {
+    static constexpr int U = 16 / (int)sizeof(T);
+    static constexpr int E = 2 * U;
+    uint4 dy4[VEC ? 2 : 1], x4[VEC && !PACKED ? 2 : 1];
+    unsigned codes[VEC && PACKED ? 2 * U / 4 : 1];
+    float dy1[VEC ? 1 : E], x1[VEC ? 1 : E];
+    float scale[PACKED && VEC ? 2 : 1];
+    float mean, rstd;
+
+    __device__ __forceinline__ void load(const NormBackArgs &a, long long row, int lane, int threads)
+    {
+        mean = a.mean[row];
+        rstd = a.rstd[row];
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
+        const uint8_t *scales = PACKED ? a.scales + row / PACK_BLOCK * a.scale_cols : nullptr;
+        constexpr int STEPS = VEC ? 2 : E, W = VEC ? U : 1;
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            const int c = (j * threads + lane) * W;
+            if (c >= a.cols) continue;
+            if constexpr (VEC)
+                dy4[j] = *reinterpret_cast<const uint4 *>(dy + c);
+            else
+                dy1[j] = widen1<T>(dy[c]);
+            if constexpr (PACKED) {
+                const uint8_t *q = static_cast<const uint8_t *>(a.x) + row * a.x_stride + c;
+                const float s = scale_value(scales[c / PACK_BLOCK]);
+                if constexpr (VEC) scale[j] = s;
+                if constexpr (!VEC) {
+                    x1[j] = decode2(*q).x * s;
+                } else if constexpr (U == 8) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(q);
+                    codes[2 * j] = w.x;
+                    codes[2 * j + 1] = w.y;
+                } else {
+                    codes[j] = *reinterpret_cast<const unsigned *>(q);
+                }
+            } else {
+                const T *q = static_cast<const T *>(a.x) + row * a.x_stride + c;
+                if constexpr (VEC)
+                    x4[j] = *reinterpret_cast<const uint4 *>(q);
+                else
+                    x1[j] = widen1<T>(*q);
+            }
+        }
+    }
+    // dy and h of step j.
+    __device__ __forceinline__ void convert(int j, float *dy, float *hat) const
+    {
+        if constexpr (VEC) {
+            Unit<T>::widen(dy4[j], dy);
+            if constexpr (PACKED) {
+#pragma unroll
+                for (int i = 0; i < U; i += 4) {
+                    const float2 p = decode2(codes[(j * U + i) / 4] & 0xffffu), q = decode2(codes[(j * U + i) / 4] >> 16);
+                    hat[i] = fmaf(p.x, scale[j], -mean); hat[i + 1] = fmaf(p.y, scale[j], -mean);
+                    hat[i + 2] = fmaf(q.x, scale[j], -mean); hat[i + 3] = fmaf(q.y, scale[j], -mean);
+                }
+            } else {
+                Unit<T>::widen(x4[j], hat);
+#pragma unroll
+                for (int i = 0; i < U; ++i) hat[i] -= mean;
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) hat[i] *= rstd;
+        } else {
+            dy[0] = dy1[j];
+            hat[0] = (x1[j] - mean) * rstd;
+        }
+    }
+};
+
+// TPR threads per row, each with the same two units of 16 bytes of every row that its block passes over:
+// the sums of dgamma and dbeta stay in registers and leave the block once.  The next row is loaded while
+// this one is reduced.
 template <typename T, bool PACKED, bool VEC, int TPR>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_back_kernel(NormBackArgs a)
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR < 512 ? 2 : 1) norm_back_kernel(const __grid_constant__ NormBackArgs a)
 {
-    constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
-    constexpr int E = 16;
+    using Row = BackRow<T, PACKED, VEC>;
+    constexpr int E = Row::E;
+    constexpr int U = VEC ? Row::U : 1;
     constexpr int UNITS = E / U;
     constexpr int THREADS = TPR < 256 ? 256 : TPR;
     constexpr int GROUPS = THREADS / TPR;
     constexpr int WARPS = TPR / 32;
-    __shared__ float shared[2][THREADS / 32][2];
+    __shared__ float2 shared[2][THREADS / 32];
     __shared__ float columns[GROUPS > 1 ? 2 * TPR * E : 1];
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const float inv_cols = 1.0f / (float)a.cols;
@@ -233,102 +329,88 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_back_kernel(NormBa
         }
     }
 
+    const long long step = (long long)gridDim.x * GROUPS;
+    long long row = (long long)blockIdx.x * GROUPS + group;
+    Row now, ahead;
+    if (VEC && row < a.rows) now.load(a, row, lane, TPR);
     int parity = 0;
-    for (long long first = (long long)blockIdx.x * GROUPS; first < a.rows; first += (long long)gridDim.x * GROUPS) {
-        const long long row = first + group;
+    for (; row - group < a.rows; row += step) {
         const bool live = row < a.rows;
-        float hat[E], dy[E];
-        const float mean = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
+        if constexpr (VEC) {
+            if (row + step < a.rows) ahead.load(a, row + step, lane, TPR);
+        } else {
+            if (live) now.load(a, row, lane, TPR);
+        }
+        float hat[E], g[E];
+        float2 both = make_float2(0.0f, 0.0f);  // sums of g and of g h
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
             const int c = (j * TPR + lane) * U;
-#pragma unroll
-            for (int i = 0; i < U; ++i) hat[j * U + i] = dy[j * U + i] = 0.0f;
             if (c < a.cols && live) {
-                const T *d = static_cast<const T *>(a.dy) + row * a.dy_stride + c;
-                if constexpr (VEC)
-                    Unit<T>::widen(*reinterpret_cast<const uint4 *>(d), dy + j * U);
-                else
-                    dy[j] = widen1<T>(*d);
-                if constexpr (PACKED) {
-                    const uint8_t *q = static_cast<const uint8_t *>(a.x) + row * a.x_stride + c;
-                    const float scale = scale_value(a.scales[row / PACK_BLOCK * a.scale_cols + c / PACK_BLOCK]);
-                    if constexpr (VEC) {
+                now.convert(j, g + j * U, hat + j * U);
+                if (VEC && c + U > a.cols) {
 #pragma unroll
-                        for (int i = 0; i < U; i += 4)
-                            decode4(*reinterpret_cast<const unsigned *>(q + i), scale, hat + j * U + i);
-                    } else {
-                        hat[j] = decode2(*q).x * scale;
-                    }
-                } else {
-                    const T *q = static_cast<const T *>(a.x) + row * a.x_stride + c;
-                    if constexpr (VEC)
-                        Unit<T>::widen(*reinterpret_cast<const uint4 *>(q), hat + j * U);
-                    else
-                        hat[j] = widen1<T>(*q);
+                    for (int i = 0; i < U; ++i)
+                        if (c + i >= a.cols) g[j * U + i] = hat[j * U + i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int e = j * U + i;
+                    sum_g[e] = fmaf(g[e], hat[e], sum_g[e]);
+                    sum_b[e] += g[e];
+                    g[e] *= gamma[e];
+                    both.x += g[e];
+                    both.y = fmaf(g[e], hat[e], both.y);
                 }
             }
         }
-        float g1 = 0.0f, g2 = 0.0f;  // sums of g and of g h
-#pragma unroll
-        for (int j = 0; j < UNITS; ++j)
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int e = j * U + i;
-                const bool in = (j * TPR + lane) * U + i < a.cols && live;
-                hat[e] = in ? (hat[e] - mean) * rstd : 0.0f;
-                dy[e] = in ? dy[e] : 0.0f;
-                sum_g[e] = fmaf(dy[e], hat[e], sum_g[e]);
-                sum_b[e] += dy[e];
-                dy[e] *= gamma[e];
-                g1 += dy[e];
-                g2 = fmaf(dy[e], hat[e], g2);
-            }
 #pragma unroll
         for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
-            g1 += __shfl_xor_sync(0xffffffffu, g1, o);
-            g2 += __shfl_xor_sync(0xffffffffu, g2, o);
+            both.x += __shfl_xor_sync(0xffffffffu, both.x, o);
+            both.y += __shfl_xor_sync(0xffffffffu, both.y, o);
         }
         if constexpr (TPR > 32) {
-            // two sets of slots in turn: a slot is written again only after the barrier of the next
-            // row, which every thread reaches after it has read this row's
+            // two sets of slots in turn: a slot is written again only after the barrier of the next row,
+            // which every thread of the row's group reaches after it has read this row's
             const int warp = threadIdx.x >> 5;
-            if ((threadIdx.x & 31) == 0) {
-                shared[parity][warp][0] = g1;
-                shared[parity][warp][1] = g2;
-            }
-            __syncthreads();
-            g1 = g2 = 0.0f;
+            if ((threadIdx.x & 31) == 0) shared[parity][warp] = both;
+            if constexpr (GROUPS == 1)
+                __syncthreads();
+            else
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
+            both = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
-                g1 += shared[parity][group * WARPS + w][0];
-                g2 += shared[parity][group * WARPS + w][1];
+                const float2 s = shared[parity][group * WARPS + w];
+                both.x += s.x;
+                both.y += s.y;
             }
             parity ^= 1;
         }
-        if (!live || !a.dx) continue;
-        g1 *= inv_cols;
-        g2 *= inv_cols;
+        if (live && a.dx) {
+            const float g1 = both.x * inv_cols, g2 = both.y * inv_cols, rstd = now.rstd;
 #pragma unroll
-        for (int j = 0; j < UNITS; ++j) {
-            const int c = (j * TPR + lane) * U;
-            if (c >= a.cols) continue;
-            T *d = static_cast<T *>(a.dx) + row * a.dx_stride + c;
-            float r[U];
+            for (int j = 0; j < UNITS; ++j) {
+                const int c = (j * TPR + lane) * U;
+                if (c >= a.cols) continue;
+                T *d = static_cast<T *>(a.dx) + row * a.dx_stride + c;
+                float r[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i) r[i] = (dy[j * U + i] - g1 - hat[j * U + i] * g2) * rstd;
-            if constexpr (VEC) {
-                if (c + U <= a.cols) {
-                    *reinterpret_cast<uint4 *>(d) = Unit<T>::narrow(r);
+                for (int i = 0; i < U; ++i) r[i] = fmaf(-hat[j * U + i], g2, g[j * U + i] - g1) * rstd;
+                if constexpr (VEC) {
+                    if (c + U <= a.cols) {
+                        *reinterpret_cast<uint4 *>(d) = Unit<T>::narrow(r);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < U; ++i)
+                            if (c + i < a.cols) d[i] = narrow1<T>(r[i]);
+                    }
                 } else {
-#pragma unroll
-                    for (int i = 0; i < U; ++i)
-                        if (c + i < a.cols) d[i] = narrow1<T>(r[i]);
+                    *d = narrow1<T>(r[0]);
                 }
-            } else {
-                *d = narrow1<T>(r[0]);
             }
         }
+        if constexpr (VEC) now = ahead;
     }
 
     if (!a.dgamma && !a.dbeta) return;
@@ -376,7 +458,7 @@ __device__ __forceinline__ float back_value(const NormBackArgs &a, long long row
 template <typename T, bool PACKED>
 __global__ void __launch_bounds__(1024) norm_back_long_rows_kernel(NormBackArgs a)
 {
-    __shared__ float shared[32];
+    __shared__ float shared[2][32];
     const long long row = blockIdx.x;
     const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
     const float mean = a.mean[row], rstd = a.rstd[row];
@@ -386,8 +468,8 @@ __global__ void __launch_bounds__(1024) norm_back_long_rows_kernel(NormBackArgs 
         g1 += g;
         g2 = fmaf(g, (back_value<T, PACKED>(a, row, c) - mean) * rstd, g2);
     }
-    g1 = row_sum<1024>(g1, shared) / (float)a.cols;
-    g2 = row_sum<1024>(g2, shared) / (float)a.cols;
+    g1 = row_sum<1024>(g1, shared[0]) / (float)a.cols;
+    g2 = row_sum<1024>(g2, shared[1]) / (float)a.cols;
     T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
     for (long long c = threadIdx.x; c < a.cols; c += 1024) {
         const float g = widen1<T>(dy[c]) * (a.gamma ? load_param(a.gamma, a.params_bf16, c) : 1.0f);
@@ -423,6 +505,7 @@ __global__ void __launch_bounds__(1024) norm_back_join_kernel(const float *parts
     const long long c = (long long)blockIdx.x * 32 + tx;
     float sum = 0.0f;
     if (c < cols)
+#pragma unroll 10
         for (int p = ty; p < parts; p += 32) sum += parts_of[p * part_stride + c];
     shared[ty][tx] = sum;
     __syncthreads();
@@ -434,28 +517,29 @@ __global__ void __launch_bounds__(1024) norm_back_join_kernel(const float *parts
 }
 
 constexpr int BACK_BLOCKS = 296;       // two blocks of the row kernel on each of 148 SMs
-constexpr int BACK_REGISTER_COLS = 16384;  // widest row that a block holds
 constexpr int BACK_LONG_SHARES = 32;
 
-int back_threads_per_row(int64_t cols)
+// The widest row that a block holds, and the threads for a row: two units of 16 bytes each.
+int64_t back_widest(int dtype) { return dtype == DIPACO_BF16 ? 16384 : 8192; }
+int back_threads_per_row(int64_t cols, int dtype)
 {
     int tpr = 8;
-    while (tpr * 16 < cols) tpr *= 2;
+    while (tpr * (32 / dense_size(dtype)) < cols) tpr *= 2;
     return tpr;
 }
 
 // Blocks that write their own sums of dgamma and dbeta.
-int64_t back_parts(int64_t rows, int64_t cols)
+int64_t back_parts(int64_t rows, int64_t cols, int dtype)
 {
-    if (cols > BACK_REGISTER_COLS) return std::min<int64_t>(BACK_LONG_SHARES, ceil_div(rows, 64));
-    const int tpr = back_threads_per_row(cols);
+    if (cols > back_widest(dtype)) return std::min<int64_t>(BACK_LONG_SHARES, ceil_div(rows, 64));
+    const int tpr = back_threads_per_row(cols, dtype);
     return std::min<int64_t>(BACK_BLOCKS, ceil_div(rows, tpr < 256 ? 256 / tpr : 1));
 }
 
 template <typename T, bool PACKED, bool VEC>
 void launch_back(const NormBackArgs &a, int blocks, cudaStream_t stream)
 {
-    const int tpr = back_threads_per_row(a.cols);
+    const int tpr = back_threads_per_row(a.cols, sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32);
 #define BACK_CASE(TPR)                                                                              \
     case TPR:                                                                                       \
         norm_back_kernel<T, PACKED, VEC, TPR><<<blocks, TPR < 256 ? 256 : TPR, 0, stream>>>(a);     \
@@ -476,7 +560,7 @@ void launch_back(const NormBackArgs &a, int blocks, cudaStream_t stream)
 template <typename T, bool PACKED>
 void launch_back_any(const NormBackArgs &a, int blocks, bool vec, cudaStream_t stream)
 {
-    if (a.cols > BACK_REGISTER_COLS) {
+    if (a.cols > back_widest(sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32)) {
         if (a.dx) norm_back_long_rows_kernel<T, PACKED><<<a.rows, 1024, 0, stream>>>(a);
         if (a.dgamma || a.dbeta)
             norm_back_long_columns_kernel<T, PACKED>
@@ -524,7 +608,8 @@ int dipaco_layer_norm_workspace(int64_t rows, int64_t cols, int64_t *bytes)
 {
     if (!bytes) return DIPACO_EINVAL;
     if (const int rc = check_extents(rows, cols)) return rc;
-    const int64_t parts = rows == 0 || cols == 0 ? 0 : back_parts(rows, cols);
+    int64_t parts = 0;  // the most of either dtype
+    if (rows > 0 && cols > 0) parts = std::max(back_parts(rows, cols, DIPACO_F32), back_parts(rows, cols, DIPACO_BF16));
     *bytes = parts > 1 ? parts * 2 * cols * (int64_t)sizeof(float) : 0;
     return DIPACO_OK;
 }
@@ -561,7 +646,7 @@ int dipaco_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
         if (dbeta && cudaMemsetAsync(dbeta, 0, cols * sizeof(float), stream) != cudaSuccess) return launch_status();
         return DIPACO_OK;
     }
-    const int parts = (int)back_parts(rows, cols);
+    const int parts = (int)back_parts(rows, cols, dtype);
     NormBackArgs a = {};
     a.dy = dy;
     a.x = x_packed ? x_packed->codes : x;

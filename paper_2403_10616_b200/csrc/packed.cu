@@ -30,34 +30,89 @@ struct Extent {
     int rows, cols, block_cols;
 };
 
-// U values of a row from column c, those from `cols` on as zero.  Rows may start at any element.
-template <typename T>
-__device__ __forceinline__ void load_unit(const T *row, int c, int cols, bool aligned, float *f)
+// The unit of 16 bytes that starts at p, of which the first n values belong to the matrix.  Rows may
+// start at any element: the values are cut out of the aligned units that hold them, the second of which
+// is read only where it holds one.
+template <typename T> __device__ __forceinline__ uint4 load_unit(const T *p, int n, bool aligned)
 {
-    constexpr int U = Layout<T>::U;
-    const int n = min(cols - c, U);
-    if (aligned) {
-        Unit<T>::widen(__ldcs(reinterpret_cast<const uint4 *>(row + c)), f);
-    } else {
-        // the aligned 16-byte units that hold the values, the second only where it holds one
-        const uintptr_t at = reinterpret_cast<uintptr_t>(row + c);
-        const unsigned s = (unsigned)(at & 15u);
-        const uint4 *unit = reinterpret_cast<const uint4 *>(at - s);
-        const uint4 lo = unit[0];
-        uint4 hi = make_uint4(0u, 0u, 0u, 0u);
-        if (s + n * sizeof(T) > 16u) hi = unit[1];
-        Unit<T>::widen(cut16(lo, hi, s), f);
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-        if (i >= n) f[i] = 0.0f;
+    if (aligned) return *reinterpret_cast<const uint4 *>(p);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const unsigned s = (unsigned)(at & 15u);
+    const uint4 *unit = reinterpret_cast<const uint4 *>(at - s);
+    const uint4 lo = unit[0];
+    uint4 hi = make_uint4(0u, 0u, 0u, 0u);
+    if (s + n * sizeof(T) > 16u) hi = unit[1];
+    return cut16(lo, hi, s);
 }
 
-template <int U> __device__ __forceinline__ void store_codes(uint8_t *p, int n, const float *f, float reciprocal)
+// The first n values of a unit, the others zero.
+template <typename T> __device__ __forceinline__ uint4 keep_first(uint4 v, int n)
+{
+    float f[Layout<T>::U];
+    Unit<T>::widen(v, f);
+#pragma unroll
+    for (int i = 0; i < Layout<T>::U; ++i)
+        if (i >= n) f[i] = 0.0f;
+    return Unit<T>::narrow(f);  // exact
+}
+
+// The largest of the block's values, on every thread.
+__device__ __forceinline__ unsigned block_max(unsigned m, unsigned *shared)
+{
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, threadIdx.x % 32 < THREADS / 32 ? shared[threadIdx.x % 32] : 0u);
+}
+
+struct PackedOut {
+    uint8_t *codes, *scales;
+    long long stride;
+};
+
+// The thread's values of one matrix: as they were loaded, or computed in fp32.
+template <typename T> struct LoadedValues {
+    const uint4 *raw;
+    __device__ __forceinline__ void unit(int j, float *f) const { Unit<T>::widen(raw[j], f); }
+    // Bits of the largest magnitude; at least those of infinity if there is an infinity or NaN.
+    __device__ __forceinline__ unsigned largest() const
+    {
+        unsigned m = 0u;
+#pragma unroll
+        for (int j = 0; j < Layout<T>::UNITS; ++j) {
+            const unsigned w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 2)
+                    m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+                else
+                    m = max(m, w[i] & 0x7fffffffu);
+            }
+        }
+        return sizeof(T) == 2 ? max(m << 16, m & 0xffff0000u) : m;
+    }
+};
+template <typename T> struct ComputedValues {
+    const float *v;
+    __device__ __forceinline__ void unit(int j, float *f) const
+    {
+#pragma unroll
+        for (int i = 0; i < Layout<T>::U; ++i) f[i] = v[j * Layout<T>::U + i];
+    }
+    __device__ __forceinline__ unsigned largest() const  // of the values that are not NaN
+    {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) m = fmaxf(m, fabsf(v[i]));
+        return __float_as_uint(m);
+    }
+};
+
+template <int U, bool SPECIAL> __device__ __forceinline__ void store_codes(uint8_t *p, int n, const float *f, float reciprocal)
 {
     unsigned w[U / 4];
 #pragma unroll
-    for (int i = 0; i < U / 4; ++i) w[i] = encode4(f + 4 * i, reciprocal);
+    for (int i = 0; i < U / 4; ++i) w[i] = SPECIAL ? encode4(f + 4 * i, reciprocal) : encode4_finite(f + 4 * i, reciprocal);
     if (n >= U) {
         if constexpr (U == 8)
             *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
@@ -70,51 +125,59 @@ template <int U> __device__ __forceinline__ void store_codes(uint8_t *p, int n, 
     }
 }
 
-// The largest of the block's values, on every thread.
-__device__ __forceinline__ unsigned block_max(unsigned m, unsigned *shared)
+// Writes the block's codes and scale.  Infinities and NaN are rare: where the largest magnitude is not
+// finite, the block looks for the largest finite one and encodes with care for infinities.
+template <typename T, typename Values>
+__device__ __forceinline__ void write_block(const PackedOut &out, const Extent &x, int row0, int col, const Values &v,
+                                            unsigned *shared)
 {
-    m = __reduce_max_sync(0xffffffffu, m);
-    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
-    __syncthreads();
-    return __reduce_max_sync(0xffffffffu, threadIdx.x % 32 < THREADS / 32 ? shared[threadIdx.x % 32] : 0u);
-}
-
-template <int N> __device__ __forceinline__ unsigned largest(const float *v)
-{
-    unsigned m = 0u;
+    using L = Layout<T>;
+    unsigned m = block_max(v.largest(), shared);
+    const bool special = m >= 0x7f800000u;
+    if (special) {
+        m = 0u;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = max(m, finite_magnitude(v[i]));
-    return m;
-}
-
-struct PackedOut {
-    uint8_t *codes, *scales;
-    long long stride;
-};
-
-// Writes the thread's values v, whose block has the largest magnitude m.
-template <typename T>
-__device__ __forceinline__ void write_block(const PackedOut &out, const Extent &x, int row0, int col, int rows_from,
-                                            const float *v, unsigned m)
-{
-    constexpr int U = Layout<T>::U;
+        for (int j = 0; j < L::UNITS; ++j) {
+            float f[L::U];
+            v.unit(j, f);
+#pragma unroll
+            for (int i = 0; i < L::U; ++i) m = max(m, finite_magnitude(f[i]));
+        }
+        m = block_max(m, shared + THREADS / 32);
+    }
     const unsigned byte = scale_byte(m);
     const float reciprocal = scale_reciprocal(byte);
     if (threadIdx.x == 0) out.scales[blockIdx.x] = (uint8_t)byte;
+    if (col >= x.cols) return;
+    uint8_t *p = out.codes + (long long)row0 * out.stride + col;
 #pragma unroll
-    for (int j = 0; j < Layout<T>::UNITS; ++j) {
-        const long long r = (long long)row0 + rows_from + j * Layout<T>::STEP;
-        if (r < x.rows && col < x.cols)
-            store_codes<U>(out.codes + r * out.stride + col, x.cols - col, v + j * U, reciprocal);
+    for (int j = 0; j < L::UNITS; ++j) {
+        if (row0 + j * L::STEP < x.rows) {
+            float f[L::U];
+            v.unit(j, f);
+            if (special)
+                store_codes<L::U, true>(p, x.cols - col, f, reciprocal);
+            else
+                store_codes<L::U, false>(p, x.cols - col, f, reciprocal);
+        }
+        p += L::STEP * out.stride;
     }
 }
 
-// exp(-2u); 2u log2(e) = a (c1 + c3 a^2)
+// exp(-2u); 2u log2(e) = a (c1 + c3 a^2).  The approximations are good to two units in the last place.
 __device__ __forceinline__ float gelu_decay(float a)
 {
     constexpr float c1 = 2.0f * 0.7978845608028654f * 1.4426950408889634f;
     constexpr float c3 = c1 * 0.044715f;
-    return exp2f(-a * fmaf(c3, a * a, c1));
+    float d;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(-a * fmaf(c3, a * a, c1)));
+    return d;
+}
+__device__ __forceinline__ float reciprocal_of(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
 
 enum : int { OP_PACK, OP_NORM, OP_GELU, OP_GELU_BACK };
@@ -136,83 +199,101 @@ struct BlockArgs {
 };
 
 template <typename T, int OP>
-__global__ void __launch_bounds__(THREADS) block_kernel(BlockArgs a)
+__global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant__ BlockArgs a)
 {
     using L = Layout<T>;
     constexpr int U = L::U;
-    __shared__ unsigned shared[2][THREADS / 32];
-    const int row0 = (int)(blockIdx.x / a.extent.block_cols) * PACK_BLOCK;
+    __shared__ unsigned shared[2][2 * THREADS / 32];
+    const int rows = a.extent.rows, cols = a.extent.cols;
+    const int row0 = (int)(blockIdx.x / a.extent.block_cols) * PACK_BLOCK + (int)threadIdx.x / L::PER_ROW;
     const int col = (int)(blockIdx.x % a.extent.block_cols) * PACK_BLOCK + (int)(threadIdx.x % L::PER_ROW) * U;
-    const int rows_from = threadIdx.x / L::PER_ROW;
+    const bool edge = (int)(blockIdx.x % a.extent.block_cols + 1) * PACK_BLOCK > cols ||
+                      (int)(blockIdx.x / a.extent.block_cols + 1) * PACK_BLOCK > rows;  // the same for the whole block
 
-    float x[VALUES], y[OP == OP_PACK ? 1 : VALUES];
+    uint4 raw[L::UNITS];
+    const T *x = static_cast<const T *>(a.x) + (long long)row0 * a.x_stride + col;
 #pragma unroll
     for (int j = 0; j < L::UNITS; ++j) {
-        const long long r = (long long)row0 + rows_from + j * L::STEP;
-        if (r < a.extent.rows && col < a.extent.cols) {
-            load_unit<T>(static_cast<const T *>(a.x) + r * a.x_stride, col, a.extent.cols, a.aligned, x + j * U);
+        if (!edge) {
+            raw[j] = load_unit<T>(x, U, a.aligned);
+        } else if (row0 + j * L::STEP < rows && col < cols) {
+            raw[j] = keep_first<T>(load_unit<T>(x, cols - col, a.aligned), cols - col);
         } else {
-#pragma unroll
-            for (int i = 0; i < U; ++i) x[j * U + i] = 0.0f;
+            raw[j] = make_uint4(0u, 0u, 0u, 0u);
         }
+        x += L::STEP * a.x_stride;
     }
+    const LoadedValues<T> loaded = {raw};
+    if constexpr (OP == OP_PACK) {
+        write_block<T>(a.first, a.extent, row0, col, loaded, shared[0]);
+        return;
+    }
+
+    float y[VALUES];
     if constexpr (OP == OP_NORM) {
         float gamma[U], beta[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) { gamma[i] = 1.0f; beta[i] = 0.0f; }
-        if (a.gamma) load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, col, a.extent.cols, gamma);
-        if (a.beta) load_params<U>(a.beta, a.params_bf16, a.beta_aligned, col, a.extent.cols, beta);
+        if (a.gamma) load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, col, cols, gamma);
+        if (a.beta) load_params<U>(a.beta, a.params_bf16, a.beta_aligned, col, cols, beta);
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
-            const long long r = (long long)row0 + rows_from + j * L::STEP;
-            const bool in = r < a.extent.rows;
-            const float mean = in ? a.mean[r] : 0.0f, rstd = in ? a.rstd[r] : 0.0f;
+            const int r = row0 + j * L::STEP;
+            const float mean = r < rows ? a.mean[r] : 0.0f, rstd = r < rows ? a.rstd[r] : 0.0f;
+            float *f = y + j * U;
+            loaded.unit(j, f);
 #pragma unroll
-            for (int i = 0; i < U; ++i)
-                y[j * U + i] = in && col + i < a.extent.cols
-                                   ? (x[j * U + i] - mean) * rstd * gamma[i] + beta[i]
-                                   : 0.0f;
+            for (int i = 0; i < U; ++i) f[i] = fmaf((f[i] - mean) * rstd, gamma[i], beta[i]);
+            if (edge) {
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+                    if (r >= rows || col + i >= cols) f[i] = 0.0f;
+            }
         }
     } else if constexpr (OP == OP_GELU) {
 #pragma unroll
-        for (int e = 0; e < VALUES; ++e) y[e] = x[e] * __fdividef(1.0f, 1.0f + gelu_decay(x[e]));
-    } else if constexpr (OP == OP_GELU_BACK) {
+        for (int j = 0; j < L::UNITS; ++j) {
+            float *f = y + j * U;
+            loaded.unit(j, f);
+#pragma unroll
+            for (int i = 0; i < U; ++i) f[i] *= reciprocal_of(1.0f + gelu_decay(f[i]));
+        }
+    } else {
         constexpr float k = 2.0f * 0.7978845608028654f;
+        const float scale = scale_value(a.scales[blockIdx.x]);
+        const uint8_t *q = a.codes + (long long)row0 * a.codes_stride + col;
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
-            const long long r = (long long)row0 + rows_from + j * L::STEP;
-            const float scale = scale_value(a.scales[blockIdx.x]);
-            const bool in = r < a.extent.rows && col < a.extent.cols;
-            const uint8_t *q = a.codes + r * a.codes_stride + col;
+            float *f = y + j * U;
+            loaded.unit(j, f);
+            const bool in = !edge || (row0 + j * L::STEP < rows && col < cols);
 #pragma unroll
             for (int i = 0; i < U; i += 4) {
                 float v[4];
                 // rows of codes are padded to 16 bytes: four of them can be read wherever one can
-                decode4(in && col + i < a.extent.cols ? *reinterpret_cast<const unsigned *>(q + i) : 0u, scale, v);
+                decode4(in && (!edge || col + i < cols) ? *reinterpret_cast<const unsigned *>(q + i) : 0u, scale, v);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    const int e = j * U + i + t;
                     // s (1 - s) = d s^2 with d = exp(-2u): no cancellation where s is near 1
                     const float decay = gelu_decay(v[t]), d = decay > 3e38f ? 3e38f : decay;
-                    const float s = __fdividef(1.0f, 1.0f + d), w = d * s * s;
+                    const float s = reciprocal_of(1.0f + d), w = d * s * s;
                     // w is zero before its factors overflow (a code times its scale may itself exceed
                     // the largest fp32 value)
                     const float bend = w == 0.0f ? 0.0f : v[t] * w * fmaf(3.0f * 0.044715f * k, v[t] * v[t], k);
-                    const float slope = s + bend;
-                    y[e] = col + i + t < a.extent.cols ? x[e] * slope : 0.0f;
+                    f[i + t] *= s + bend;
                 }
             }
+            if (edge) {
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+                    if (col + i >= cols) f[i] = 0.0f;
+            }
+            q += L::STEP * a.codes_stride;
         }
     }
-
-    if constexpr (OP == OP_PACK) {
-        write_block<T>(a.first, a.extent, row0, col, rows_from, x, block_max(largest<VALUES>(x), shared[0]));
-    } else {
-        const unsigned m = block_max(largest<VALUES>(y), shared[0]);
-        write_block<T>(a.first, a.extent, row0, col, rows_from, y, m);
-        if (OP != OP_GELU_BACK && a.second.codes)
-            write_block<T>(a.second, a.extent, row0, col, rows_from, x, block_max(largest<VALUES>(x), shared[1]));
-    }
+    const ComputedValues<T> computed = {y};
+    write_block<T>(a.first, a.extent, row0, col, computed, shared[0]);
+    if (OP != OP_GELU_BACK && a.second.codes) write_block<T>(a.second, a.extent, row0, col, loaded, shared[1]);
 }
 
 // Four codes per thread.
