@@ -524,15 +524,18 @@ int dipaco_gelu_pack_backward(const void *dy, int64_t dy_stride, int32_t dtype, 
  * accumulate adds the product to C (gradients over several batches).
  *   workspace   16-byte aligned, at least the bytes that dipaco_packed_matmul_workspace reports for
  *               the product's extents C [m, n], contraction k (a host-only query; may be zero)
- * Every wait inside the kernel is bounded (4 s).  A wait that runs out ends the kernel in an orderly
- * way with undefined results; dipaco_packed_matmul_status synchronises the stream, returns
- * DIPACO_ETIMEOUT once if that has happened on the device since the last query, DIPACO_OK otherwise.
  */
 int dipaco_packed_matmul_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
 int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t transpose_a, int32_t transpose_b,
                          void *c, int64_t c_stride, int32_t dtype, int32_t accumulate, void *workspace,
                          int64_t workspace_bytes, int32_t device, void *cuda_stream);
-int dipaco_packed_matmul_status(int32_t device, void *cuda_stream);
+
+/*
+ * Every wait inside the kernels of this section is bounded (4 s).  A wait that runs out ends its kernel in
+ * an orderly way with undefined results.  This call synchronises the stream and returns DIPACO_ETIMEOUT
+ * once if that has happened on the device since the last query, DIPACO_OK otherwise.
+ */
+int dipaco_inner_status(int32_t device, void *cuda_stream);
 
 const char *dipaco_strerror(int status);
 

@@ -54,7 +54,7 @@ EXPORTS = [
     "dipaco_pack", "dipaco_unpack", "dipaco_layer_norm", "dipaco_layer_norm_pack",
     "dipaco_layer_norm_workspace", "dipaco_layer_norm_backward", "dipaco_gelu_pack",
     "dipaco_gelu_pack_backward", "dipaco_packed_matmul_workspace", "dipaco_packed_matmul",
-    "dipaco_packed_matmul_status",
+    "dipaco_inner_status",
 ]
 
 _lib = None
@@ -129,7 +129,7 @@ def load() -> ctypes.CDLL:
     lib.dipaco_gelu_pack_backward.argtypes = [vp, i64, i32, pk, pk, i32, vp]
     lib.dipaco_packed_matmul_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
     lib.dipaco_packed_matmul.argtypes = [pk, pk, i32, i32, vp, i64, i32, i32, vp, i64, i32, vp]
-    lib.dipaco_packed_matmul_status.argtypes = [i32, vp]
+    lib.dipaco_inner_status.argtypes = [i32, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("dipaco_strerror", "dipaco_launch_count"):
@@ -449,8 +449,8 @@ def dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype,
                                        workspace_ptr, workspace_bytes, device, stream), "dipaco_packed_matmul")
 
 
-def dipaco_packed_matmul_status(device, stream) -> int:
-    return int(load().dipaco_packed_matmul_status(device, stream))
+def dipaco_inner_status(device, stream) -> int:
+    return int(load().dipaco_inner_status(device, stream))
 
 
 # ------------------------------------------------------------------ convenience owner

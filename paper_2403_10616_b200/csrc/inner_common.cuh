@@ -7,6 +7,7 @@
 
 #include "../../include/dipaco.h"
 
+#include <cuda.h>
 #include <cuda_fp8.h>
 
 #include "kernels.cuh"
@@ -72,7 +73,49 @@ inline int launch_status()
     return err == cudaSuccess ? DIPACO_OK : err == cudaErrorMemoryAllocation ? DIPACO_ENOMEM : DIPACO_ECUDA;
 }
 
+// Tensor maps are encoded by the driver, whose entry point is looked up once.
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// A word that kernels set when a bounded wait runs out: reads and clears it.  False: a CUDA call failed.
+template <typename Symbol> bool take_error_word(const Symbol &symbol, bool &expired)
+{
+    int word = 0;
+    if (cudaMemcpyFromSymbol(&word, symbol, sizeof(int)) != cudaSuccess) return false;
+    if (word == 0) return true;
+    expired = true;
+    word = 0;
+    return cudaMemcpyToSymbol(symbol, &word, sizeof(int)) == cudaSuccess;
+}
+bool take_packing_error(bool &expired);  // of packed.cu
+bool take_norm_error(bool &expired);     // of layer_norm.cu
+
 // ------------------------------------------------------------------------------------------ device
+
+// True on one thread of the warp.  Asynchronous copies and products are issued under it: the compiler
+// then keeps their operands in uniform registers, which it does not under a test of the lane.
+__device__ __forceinline__ bool elect_one()
+{
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
 
 // The value of an e8m0 byte: 2^(b-127); 255 is NaN.
 __device__ __forceinline__ float scale_value(unsigned b)

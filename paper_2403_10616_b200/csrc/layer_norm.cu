@@ -7,7 +7,10 @@
 // registers, so it does not cancel for rows whose mean is large beside their spread.
 #include "inner_common.cuh"
 
+#include <algorithm>
 #include <cmath>
+#include <cstring>
+#include <type_traits>
 
 using namespace dipaco;
 
@@ -43,112 +46,128 @@ struct NormArgs {
     float *mean, *rstd;
     long long x_stride, y_stride;
     int rows, cols;
-    float eps;
+    float eps, inv_cols;
     bool params_bf16, gamma_aligned, beta_aligned;
 };
 
-// One row per TPR threads, the row in registers: NU units of 16 bytes per thread (VEC: rows on 16-byte
-// boundaries), or as many single values.  Bound by memory: about nine instructions per value, and enough
-// rows in flight with a warp per row up to 2048 values in bf16 (1024 in fp32); wider rows take a block.
-template <typename T, bool VEC, int TPR, int NU>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) norm_rows_kernel(const __grid_constant__ NormArgs a)
+// (v + eps)^-1/2, the approximation and one Newton step.
+__device__ __forceinline__ float inverse_root(float v, float eps)
+{
+    v = __fadd_rn(v, eps);  // not contracted: the same value wherever this is compiled
+    const float r = rsqrtf(v);
+    const float better = r * fmaf(-0.5f * v * r, r, 1.5f);
+    return v > 1e-30f && v < 1e30f ? better : 1.0f / sqrtf(v);  // where the step's products stay normal
+}
+
+// One row at a time per TPR threads, in registers: NU units of 16 bytes per thread (VEC: rows on 16-byte
+// boundaries), or as many single values.  Bound by memory: the next row is on its way while this one is
+// summed, and a warp per row up to 2048 values in bf16 (1024 in fp32) keeps the sums inside warps.
+// RAGGED: the last unit of a row is partly outside.  Sums run in four chains: one alone leaves the warp
+// waiting for its own additions (16384x2048: 71 us, ... us with four).
+template <typename T, bool VEC, bool RAGGED, int TPR, int NU>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU == 8 ? 4 : 6) norm_rows_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
     constexpr int E = NU * 16 / (int)sizeof(T);
     constexpr int UNITS = E / U;
-    __shared__ float shared[2][32];
+    constexpr int GROUPS = (TPR < 128 ? 128 : TPR) / TPR;
+    using Raw = typename std::conditional<VEC, uint4, T>::type;
+    __shared__ float shared[4][TPR > 32 ? TPR / 32 : 1];  // two sums of a row, of two rows in turn
     const int lane = threadIdx.x % TPR;
-    const int row = blockIdx.x * (blockDim.x / TPR) + threadIdx.x / TPR;
-    const bool live = row < a.rows;
-    const int cols = live ? a.cols : 0;
-    const T *x = static_cast<const T *>(a.x) + (live ? row : 0) * a.x_stride;
+    const long long step = (long long)gridDim.x * GROUPS;
+    long long row = (long long)blockIdx.x * GROUPS + threadIdx.x / TPR;
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride + lane * U;
+    T *y = static_cast<T *>(a.y) + row * a.y_stride + lane * U;
+    const int cols = a.cols - lane * U;  // a unit j of this thread is inside while j * TPR * U < cols
 
-    float v[E];
-    float sum = 0.0f;
-    if constexpr (VEC) {
-        uint4 raw[UNITS];
+    Raw raw[UNITS];
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j)
+        if (row < a.rows && j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
+    int turn = 0;
+    // rows beyond the last keep the warp together: they are read as zeros and not written
+    for (; row - threadIdx.x / TPR < a.rows; row += step) {
+        const bool live = row < a.rows;
+        float v[E], sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
-            const int c = (j * TPR + lane) * U;
-            raw[j] = c < cols ? *reinterpret_cast<const uint4 *>(x + c) : make_uint4(0u, 0u, 0u, 0u);
+            if (live && j * TPR * U < cols) {
+                if constexpr (VEC)
+                    Unit<T>::widen(raw[j], v + j * U);
+                else
+                    v[j] = widen1<T>(raw[j]);
+                if constexpr (RAGGED) {
+#pragma unroll
+                    for (int i = 1; i < U; ++i)
+                        if (j * TPR * U + i >= cols) v[j * U + i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] += v[j * U + i];
+            }
         }
+        x += step * a.x_stride;
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j)
+            if (row + step < a.rows && j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
+        // divided: the mean of equal values is that value
+        const float mean = row_sum<TPR>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared[turn]) / (float)a.cols;
+        sums[0] = sums[1] = sums[2] = sums[3] = 0.0f;
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
-            const int c = (j * TPR + lane) * U;
-            Unit<T>::widen(raw[j], v + j * U);
-            if (c < cols && c + U > cols) {
+            if (live && j * TPR * U < cols) {
 #pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (c + i >= cols) v[j * U + i] = 0.0f;
+                for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
+                if constexpr (RAGGED) {
+#pragma unroll
+                    for (int i = 1; i < U; ++i)
+                        if (j * TPR * U + i >= cols) v[j * U + i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] = fmaf(v[j * U + i], v[j * U + i], sums[(j * U + i) & 3]);
             }
-#pragma unroll
-            for (int i = 0; i < U; ++i) sum += v[j * U + i];
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < UNITS; ++j) {
-            const int c = j * TPR + lane;
-            v[j] = c < cols ? widen1<T>(x[c]) : 0.0f;
+        const float square = row_sum<TPR>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared[turn + 1]);
+        const float rstd = inverse_root(__fmul_rn(square, a.inv_cols), a.eps);
+        turn ^= 2;
+        if (live && lane == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
         }
+        if (a.y && live) {
 #pragma unroll
-        for (int j = 0; j < UNITS; ++j) sum += v[j];
-    }
-    const float mean = row_sum<TPR>(sum, shared[0]) / (float)a.cols;
-    sum = 0.0f;
+            for (int j = 0; j < UNITS; ++j) {
+                if (j * TPR * U >= cols) continue;
+                const int c = (j * TPR + lane) * U;
+                float *r = v + j * U;
 #pragma unroll
-    for (int j = 0; j < UNITS; ++j) {
-        const int c = (j * TPR + lane) * U;
-        if (c < cols) {
+                for (int i = 0; i < U; ++i) r[i] *= rstd;
+                if constexpr (VEC) {
+                    float p[U];
+                    if (a.gamma) {
+                        load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, a.cols, p);
 #pragma unroll
-            for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
-            if (VEC && c + U > cols) {
+                        for (int i = 0; i < U; ++i) r[i] *= p[i];
+                    }
+                    if (a.beta) {
+                        load_params<U>(a.beta, a.params_bf16, a.beta_aligned, c, a.cols, p);
 #pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (c + i >= cols) v[j * U + i] = 0.0f;
+                        for (int i = 0; i < U; ++i) r[i] += p[i];
+                    }
+                    if (!RAGGED || c + U <= a.cols) {
+                        *reinterpret_cast<uint4 *>(y + j * TPR * U) = Unit<T>::narrow(r);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < U; ++i)
+                            if (c + i < a.cols) y[j * TPR * U + i] = narrow1<T>(r[i]);
+                    }
+                } else {
+                    if (a.gamma) r[0] *= load_param(a.gamma, a.params_bf16, c);
+                    if (a.beta) r[0] += load_param(a.beta, a.params_bf16, c);
+                    y[j * TPR * U] = narrow1<T>(r[0]);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < U; ++i) sum = fmaf(v[j * U + i], v[j * U + i], sum);
         }
-    }
-    const float rstd = 1.0f / sqrtf(row_sum<TPR>(sum, shared[1]) / (float)a.cols + a.eps);
-    if (!live) return;
-    if (lane == 0) {
-        if (a.mean) a.mean[row] = mean;
-        if (a.rstd) a.rstd[row] = rstd;
-    }
-    if (!a.y) return;
-    T *y = static_cast<T *>(a.y) + row * a.y_stride;
-#pragma unroll
-    for (int j = 0; j < UNITS; ++j) {
-        const int c = (j * TPR + lane) * U;
-        if (c >= cols) continue;
-        float *r = v + j * U;
-#pragma unroll
-        for (int i = 0; i < U; ++i) r[i] *= rstd;
-        if constexpr (VEC) {
-            float p[U];
-            if (a.gamma) {
-                load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, cols, p);
-#pragma unroll
-                for (int i = 0; i < U; ++i) r[i] *= p[i];
-            }
-            if (a.beta) {
-                load_params<U>(a.beta, a.params_bf16, a.beta_aligned, c, cols, p);
-#pragma unroll
-                for (int i = 0; i < U; ++i) r[i] += p[i];
-            }
-            if (c + U <= cols) {
-                *reinterpret_cast<uint4 *>(y + c) = Unit<T>::narrow(r);
-            } else {
-#pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (c + i < cols) y[c + i] = narrow1<T>(r[i]);
-            }
-        } else {
-            if (a.gamma) r[0] *= load_param(a.gamma, a.params_bf16, c);
-            if (a.beta) r[0] += load_param(a.beta, a.params_bf16, c);
-            y[c] = narrow1<T>(r[0]);
-        }
+        y += step * a.y_stride;
     }
 }
 
@@ -166,7 +185,7 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
         const float d = widen1<T>(x[c]) - mean;
         sum = fmaf(d, d, sum);
     }
-    const float rstd = 1.0f / sqrtf(row_sum<1024>(sum, shared[1]) / (float)a.cols + a.eps);
+    const float rstd = inverse_root(__fmul_rn(row_sum<1024>(sum, shared[1]), a.inv_cols), a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean;
         if (a.rstd) a.rstd[blockIdx.x] = rstd;
@@ -181,14 +200,16 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool RAGGED>
 void launch_norm(const NormArgs &a, cudaStream_t stream)
 {
     const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
 #define NORM_CASE(TPR, NU)                                                                                         \
     if (units <= TPR * NU) {                                                                                       \
         constexpr int threads = TPR < 128 ? 128 : TPR;                                                             \
-        norm_rows_kernel<T, VEC, TPR, NU><<<(unsigned)ceil_div(a.rows, threads / TPR), threads, 0, stream>>>(a);   \
+        const int64_t full = 148 * (threads > 128 ? 1 : NU == 8 ? 4 : 6);                                          \
+        const unsigned grid = (unsigned)std::min<int64_t>(full, ceil_div(a.rows, threads / TPR));                  \
+        norm_rows_kernel<T, VEC, RAGGED, TPR, NU><<<grid, threads, 0, stream>>>(a);                                        \
         return;                                                                                                    \
     }
     NORM_CASE(8, 1)
@@ -220,197 +241,277 @@ struct NormBackArgs {
     bool params_bf16, gamma_aligned;
 };
 
-// What a thread loads of a row, before conversion.
-template <typename T, bool PACKED, bool VEC> struct BackRow {
-    static constexpr int U = 16 / (int)sizeof(T);
-    static constexpr int E = 2 * U;
-    uint4 dy4[VEC ? 2 : 1], x4[VEC && !PACKED ? 2 : 1];
-    unsigned codes[VEC && PACKED ? 2 * U / 4 : 1];
-    float dy1[VEC ? 1 : E], x1[VEC ? 1 : E];
-    float scale[PACKED && VEC ? 2 : 1];
-    float mean, rstd;
+// The first n of 16 bytes to shared memory, the others zero.
+__device__ __forceinline__ void copy_filled(void *to, const void *from, int n)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_addr(to)), "l"(from), "r"(n) : "memory");
+}
 
-    __device__ __forceinline__ void load(const NormBackArgs &a, long long row, int lane, int threads)
+static __device__ int g_norm_error;  // set by a bounded wait that ran out
+constexpr int BACK_MAX_STAGES = 4;
+
+// How the threads of a block share rows: TPR threads for a row, each with two units of 16 bytes of it (or 16
+// single values), GROUPS times ROWS rows at a time.
+template <typename T, bool PACKED, bool VEC, int TPR> struct BackShape {
+    static constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
+    static constexpr int E = VEC ? 2 * U : 16;
+    static constexpr int UNITS = E / U;
+    static constexpr int ROWS = VEC && TPR <= 256 ? 2 : 1;
+    static constexpr int THREADS = TPR < 128 ? 128 : TPR;
+    static constexpr int GROUPS = THREADS / TPR;
+    using Raw = typename std::conditional<VEC, uint4, T>::type;
+    using X = typename std::conditional<PACKED, uint8_t, T>::type;
+    using RawX = typename std::conditional<!PACKED, Raw, typename std::conditional<!VEC, uint8_t,
+                 typename std::conditional<U == 8, uint2, unsigned>::type>::type>::type;
+
+    static __device__ __forceinline__ void widen(const Raw &raw, float *f)
     {
-        mean = a.mean[row];
-        rstd = a.rstd[row];
-        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
-        const uint8_t *scales = PACKED ? a.scales + row / PACK_BLOCK * a.scale_cols : nullptr;
-        constexpr int STEPS = VEC ? 2 : E, W = VEC ? U : 1;
-#pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
-            const int c = (j * threads + lane) * W;
-            if (c >= a.cols) continue;
-            if constexpr (VEC)
-                dy4[j] = *reinterpret_cast<const uint4 *>(dy + c);
-            else
-                dy1[j] = widen1<T>(dy[c]);
-            if constexpr (PACKED) {
-                const uint8_t *q = static_cast<const uint8_t *>(a.x) + row * a.x_stride + c;
-                const float s = scale_value(scales[c / PACK_BLOCK]);
-                if constexpr (VEC) scale[j] = s;
-                if constexpr (!VEC) {
-                    x1[j] = decode2(*q).x * s;
-                } else if constexpr (U == 8) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(q);
-                    codes[2 * j] = w.x;
-                    codes[2 * j + 1] = w.y;
-                } else {
-                    codes[j] = *reinterpret_cast<const unsigned *>(q);
-                }
-            } else {
-                const T *q = static_cast<const T *>(a.x) + row * a.x_stride + c;
-                if constexpr (VEC)
-                    x4[j] = *reinterpret_cast<const uint4 *>(q);
-                else
-                    x1[j] = widen1<T>(*q);
-            }
-        }
+        if constexpr (VEC)
+            Unit<T>::widen(raw, f);
+        else
+            f[0] = widen1<T>(raw);
     }
-    // dy and h of step j.
-    __device__ __forceinline__ void convert(int j, float *dy, float *hat) const
+    // h of a unit of x.
+    static __device__ __forceinline__ void normalised(const RawX &x, float scale, float mean, float rstd, float *h)
     {
-        if constexpr (VEC) {
-            Unit<T>::widen(dy4[j], dy);
-            if constexpr (PACKED) {
-#pragma unroll
-                for (int i = 0; i < U; i += 4) {
-                    const float2 p = decode2(codes[(j * U + i) / 4] & 0xffffu), q = decode2(codes[(j * U + i) / 4] >> 16);
-                    hat[i] = fmaf(p.x, scale[j], -mean); hat[i + 1] = fmaf(p.y, scale[j], -mean);
-                    hat[i + 2] = fmaf(q.x, scale[j], -mean); hat[i + 3] = fmaf(q.y, scale[j], -mean);
-                }
+        if constexpr (PACKED) {
+            if constexpr (!VEC) {
+                h[0] = fmaf(decode2(x).x, scale, -mean);  // a code times its scale is exact
             } else {
-                Unit<T>::widen(x4[j], hat);
+                unsigned w[U / 4];
+                memcpy(w, &x, sizeof(w));
 #pragma unroll
-                for (int i = 0; i < U; ++i) hat[i] -= mean;
+                for (int i = 0; i < U; i += 2) {
+                    const float2 p = decode2(w[i / 4] >> (8 * (i % 4)) & 0xffffu);
+                    h[i] = fmaf(p.x, scale, -mean);
+                    h[i + 1] = fmaf(p.y, scale, -mean);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < U; ++i) hat[i] *= rstd;
         } else {
-            dy[0] = dy1[j];
-            hat[0] = (x1[j] - mean) * rstd;
+            widen(x, h);
+#pragma unroll
+            for (int i = 0; i < U; ++i) h[i] -= mean;
         }
+#pragma unroll
+        for (int i = 0; i < U; ++i) h[i] *= rstd;
     }
 };
 
-// TPR threads per row, each with the same two units of 16 bytes of every row that its block passes over:
-// the sums of dgamma and dbeta stay in registers and leave the block once.  The next row is loaded while
-// this one is reduced.
-template <typename T, bool PACKED, bool VEC, int TPR>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR, TPR < 512 ? 2 : 1) norm_back_kernel(const __grid_constant__ NormBackArgs a)
+// Sums over the warp of four values at once: afterwards lane l has the sum of value l / 8.  Each step
+// halves what a lane carries, which takes 6 exchanges instead of 20.
+__device__ __forceinline__ float warp_sum4(const float *v)
 {
-    using Row = BackRow<T, PACKED, VEC>;
-    constexpr int E = Row::E;
-    constexpr int U = VEC ? Row::U : 1;
-    constexpr int UNITS = E / U;
-    constexpr int THREADS = TPR < 256 ? 256 : TPR;
-    constexpr int GROUPS = THREADS / TPR;
+    const int lane = threadIdx.x & 31;
+    const bool high = lane & 16, upper = lane & 8;
+    const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, high ? v[0] : v[2], 16);
+    const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, high ? v[1] : v[3], 16);
+    float s = (upper ? b : a) + __shfl_xor_sync(0xffffffffu, upper ? a : b, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
+// The sums of dgamma and dbeta stay in registers, as each thread has the same columns of every row that its
+// block passes over, and leave the block once.  Two rows are taken at a time, which halves the work of
+// their reductions.  Rows on 16-byte boundaries (VEC) are brought to shared memory by bulk copies, a few
+// steps ahead: a thread has no registers to spare for them.  A last, partial unit of a row is copied by
+// itself and filled up with zeros, which take no part in any sum.
+template <typename T, bool PACKED, bool VEC, int TPR>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 128 ? 4 : TPR == 256 ? 2 : 1)
+    norm_back_kernel(const __grid_constant__ NormBackArgs a, int stages, int dy_bytes, int x_bytes)
+{
+    using S = BackShape<T, PACKED, VEC, TPR>;
+    constexpr int E = S::E, U = S::U, UNITS = S::UNITS, ROWS = S::ROWS, THREADS = S::THREADS, GROUPS = S::GROUPS;
     constexpr int WARPS = TPR / 32;
-    __shared__ float2 shared[2][THREADS / 32];
+    extern __shared__ uint8_t raw_ring[];
+    __shared__ uint64_t full[BACK_MAX_STAGES];
+    __shared__ float4 shared[2][THREADS / 32];
     __shared__ float columns[GROUPS > 1 ? 2 * TPR * E : 1];
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int column = lane * U, cols = a.cols - column;
     const float inv_cols = 1.0f / (float)a.cols;
+    uint8_t *ring = raw_ring + ((128u - (ptx::smem_addr(raw_ring) & 127u)) & 127u);
+    const int row_bytes = dy_bytes + x_bytes, stage_bytes = GROUPS * ROWS * row_bytes;
+    const int dy_tail = a.cols * (int)sizeof(T) & 15, x_tail = a.cols * (int)sizeof(typename S::X) & 15;
+    const int dy_whole = dy_bytes - (dy_tail ? 16 : 0), x_whole = x_bytes - (x_tail ? 16 : 0);
+
+    const long long step = (long long)gridDim.x * GROUPS * ROWS;
+    const long long block_row = (long long)blockIdx.x * GROUPS * ROWS;
+    // one thread: the rows from `first` on into a stage
+    const auto request = [&](long long first, int stage) {
+        const int rows = (int)min((long long)(GROUPS * ROWS), a.rows - first);
+        ptx::mbar_arrive_expect_tx(&full[stage], rows * (dy_whole + x_whole));
+        uint8_t *to = ring + stage * stage_bytes;
+        for (int r = 0; r < rows; ++r, to += row_bytes) {
+            const uint8_t *dy = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.dy) + (first + r) * a.dy_stride);
+            const uint8_t *x = reinterpret_cast<const uint8_t *>(static_cast<const typename S::X *>(a.x) + (first + r) * a.x_stride);
+            if (dy_whole) ptx::bulk_load(to, dy, dy_whole, &full[stage]);
+            if (x_whole) ptx::bulk_load(to + dy_bytes, x, x_whole, &full[stage]);
+            if (dy_tail) copy_filled(to + dy_whole, dy + dy_whole, dy_tail);
+            if (x_tail) copy_filled(to + dy_bytes + x_whole, x + x_whole, x_tail);
+        }
+        if (dy_tail || x_tail)  // arrives when this thread's own copies have landed
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(ptx::smem_addr(&full[stage])) : "memory");
+    };
+    if constexpr (VEC) {
+        if (threadIdx.x == 0) {
+            for (int s = 0; s < stages; ++s) ptx::mbar_init(&full[s], dy_tail || x_tail ? 2 : 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int s = 0; s < stages; ++s)
+                if (block_row + s * step < a.rows) request(block_row + s * step, s);
+    }
 
     float gamma[E], sum_g[E], sum_b[E];
 #pragma unroll
     for (int j = 0; j < UNITS; ++j) {
-        const int c = (j * TPR + lane) * U;
+        const int c = column + j * TPR * U;
 #pragma unroll
-        for (int i = 0; i < U; ++i) sum_g[j * U + i] = sum_b[j * U + i] = 0.0f;
-        if constexpr (VEC) {
-            if (a.gamma) {
+        for (int i = 0; i < U; ++i) {
+            sum_g[j * U + i] = sum_b[j * U + i] = 0.0f;
+            gamma[j * U + i] = 1.0f;
+        }
+        if (a.gamma && c < a.cols) {
+            if constexpr (VEC)
                 load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, a.cols, gamma + j * U);
-            } else {
-#pragma unroll
-                for (int i = 0; i < U; ++i) gamma[j * U + i] = 1.0f;
-            }
-        } else {
-            gamma[j] = !a.gamma ? 1.0f : c < a.cols ? load_param(a.gamma, a.params_bf16, c) : 0.0f;
+            else
+                gamma[j] = load_param(a.gamma, a.params_bf16, c);
         }
     }
 
-    const long long step = (long long)gridDim.x * GROUPS;
-    long long row = (long long)blockIdx.x * GROUPS + group;
-    Row now, ahead;
-    if (VEC && row < a.rows) now.load(a, row, lane, TPR);
-    int parity = 0;
-    for (; row - group < a.rows; row += step) {
-        const bool live = row < a.rows;
-        if constexpr (VEC) {
-            if (row + step < a.rows) ahead.load(a, row + step, lane, TPR);
-        } else {
-            if (live) now.load(a, row, lane, TPR);
-        }
-        float hat[E], g[E];
-        float2 both = make_float2(0.0f, 0.0f);  // sums of g and of g h
+    // of the next rows
+    float mean_ahead[ROWS], rstd_ahead[ROWS];
+    uint8_t scale_ahead[PACKED ? ROWS : 1][UNITS];
+    const auto look_ahead = [&](long long row) {
 #pragma unroll
-        for (int j = 0; j < UNITS; ++j) {
-            const int c = (j * TPR + lane) * U;
-            if (c < a.cols && live) {
-                now.convert(j, g + j * U, hat + j * U);
-                if (VEC && c + U > a.cols) {
+        for (int k = 0; k < ROWS; ++k) {
+            if (row + k < a.rows) {
+                mean_ahead[k] = a.mean[row + k];
+                rstd_ahead[k] = a.rstd[row + k];
+                if constexpr (PACKED) {
+                    const uint8_t *scales = a.scales + (row + k) / PACK_BLOCK * a.scale_cols;
 #pragma unroll
-                    for (int i = 0; i < U; ++i)
-                        if (c + i >= a.cols) g[j * U + i] = hat[j * U + i] = 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int e = j * U + i;
-                    sum_g[e] = fmaf(g[e], hat[e], sum_g[e]);
-                    sum_b[e] += g[e];
-                    g[e] *= gamma[e];
-                    both.x += g[e];
-                    both.y = fmaf(g[e], hat[e], both.y);
+                    for (int j = 0; j < UNITS; ++j)
+                        if (j * TPR * U < cols) scale_ahead[k][j] = scales[(column + j * TPR * U) / PACK_BLOCK];
                 }
             }
         }
-#pragma unroll
-        for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
-            both.x += __shfl_xor_sync(0xffffffffu, both.x, o);
-            both.y += __shfl_xor_sync(0xffffffffu, both.y, o);
+    };
+    long long row = block_row + group * ROWS;
+    look_ahead(row);
+    int parity = 0, stage = 0;
+    unsigned phase = 0;
+    for (long long first = block_row; first < a.rows; first += step, row += step) {
+        if constexpr (VEC) {
+            if (!bounded_wait(&full[stage], phase, &g_norm_error, 1)) {
+                for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
+                return;
+            }
         }
+        const uint8_t *mine = ring + stage * stage_bytes + group * ROWS * row_bytes;
+        float hat[ROWS][E];
+        typename S::Raw kept[VEC ? 1 : UNITS];  // of dy, where it is not in shared memory
+        float rstd[ROWS], sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // of g and g h, of either row
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            rstd[k] = rstd_ahead[k];
+            if (row + k < a.rows) {
+#pragma unroll
+                for (int j = 0; j < UNITS; ++j) {
+                    const int c = j * TPR * U;
+                    if (c < cols) {
+                        typename S::Raw dy;
+                        typename S::RawX x;
+                        if constexpr (VEC) {
+                            dy = reinterpret_cast<const typename S::Raw *>(mine + k * row_bytes)[lane + j * TPR];
+                            x = reinterpret_cast<const typename S::RawX *>(mine + k * row_bytes + dy_bytes)[lane + j * TPR];
+                        } else {
+                            dy = kept[j] = static_cast<const T *>(a.dy)[(row + k) * a.dy_stride + column + c];
+                            x = static_cast<const typename S::X *>(a.x)[(row + k) * a.x_stride + column + c];
+                        }
+                        float g[U], *h = hat[k] + j * U;
+                        S::widen(dy, g);
+                        S::normalised(x, PACKED ? scale_value(scale_ahead[PACKED ? k : 0][j]) : 0.0f, mean_ahead[k], rstd[k], h);
+#pragma unroll
+                        for (int i = 0; i < U; ++i) {
+                            const int e = j * U + i;
+                            const float p = g[i] * h[i];
+                            sum_g[e] += p;
+                            sum_b[e] += g[i];
+                            sums[2 * k] = fmaf(g[i], gamma[e], sums[2 * k]);
+                            sums[2 * k + 1] = fmaf(p, gamma[e], sums[2 * k + 1]);
+                        }
+                    }
+                }
+            }
+        }
+        look_ahead(row + step);
+        if constexpr (TPR < 32) {
+#pragma unroll
+            for (int i = 0; i < 2 * ROWS; ++i)
+#pragma unroll
+                for (int o = TPR / 2; o > 0; o >>= 1) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], o);
+        } else {
+            const float s = warp_sum4(sums);
+            if constexpr (TPR == 32) {
+#pragma unroll
+                for (int i = 0; i < 2 * ROWS; ++i) sums[i] = __shfl_sync(0xffffffffu, s, 8 * i);
+            } else {
+                const int warp = threadIdx.x >> 5;
+                if ((threadIdx.x & 7) == 0) reinterpret_cast<float *>(&shared[parity][warp])[(threadIdx.x & 31) >> 3] = s;
+            }
+        }
+        // Behind this barrier every thread is done with the rows before these: their stage is free, and so
+        // are the slots of `shared` that the next rows use.
+        if constexpr (VEC || TPR > 32) __syncthreads();
         if constexpr (TPR > 32) {
-            // two sets of slots in turn: a slot is written again only after the barrier of the next row,
-            // which every thread of the row's group reaches after it has read this row's
-            const int warp = threadIdx.x >> 5;
-            if ((threadIdx.x & 31) == 0) shared[parity][warp] = both;
-            if constexpr (GROUPS == 1)
-                __syncthreads();
-            else
-                asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
-            both = make_float2(0.0f, 0.0f);
+            sums[0] = sums[1] = sums[2] = sums[3] = 0.0f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
-                const float2 s = shared[parity][group * WARPS + w];
-                both.x += s.x;
-                both.y += s.y;
+                const float4 q = shared[parity][group * WARPS + w];
+                sums[0] += q.x; sums[1] += q.y; sums[2] += q.z; sums[3] += q.w;
             }
             parity ^= 1;
         }
-        if (live && a.dx) {
-            const float g1 = both.x * inv_cols, g2 = both.y * inv_cols, rstd = now.rstd;
+        if constexpr (VEC) {
+            const long long next = first + (stages - 1) * step;
+            if (threadIdx.x == 0 && first != block_row && next < a.rows) request(next, stage == 0 ? stages - 1 : stage - 1);
+        }
+        if (a.dx) {
 #pragma unroll
-            for (int j = 0; j < UNITS; ++j) {
-                const int c = (j * TPR + lane) * U;
-                if (c >= a.cols) continue;
-                T *d = static_cast<T *>(a.dx) + row * a.dx_stride + c;
-                float r[U];
+            for (int k = 0; k < ROWS; ++k) {
+                if (row + k >= a.rows) continue;
+                const float g1 = sums[2 * k] * inv_cols, g2 = sums[2 * k + 1] * inv_cols;
+                T *out = static_cast<T *>(a.dx) + (row + k) * a.dx_stride + column;
 #pragma unroll
-                for (int i = 0; i < U; ++i) r[i] = fmaf(-hat[j * U + i], g2, g[j * U + i] - g1) * rstd;
-                if constexpr (VEC) {
-                    if (c + U <= a.cols) {
-                        *reinterpret_cast<uint4 *>(d) = Unit<T>::narrow(r);
+                for (int j = 0; j < UNITS; ++j) {
+                    const int c = j * TPR * U;
+                    if (c >= cols) continue;
+                    float r[U];
+                    if constexpr (VEC)
+                        S::widen(reinterpret_cast<const typename S::Raw *>(mine + k * row_bytes)[lane + j * TPR], r);
+                    else
+                        S::widen(kept[j], r);
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        r[i] = fmaf(-hat[k][j * U + i], g2, fmaf(r[i], gamma[j * U + i], -g1)) * rstd[k];
+                    if constexpr (VEC) {
+                        if (c + U <= cols) {
+                            *reinterpret_cast<uint4 *>(out + c) = Unit<T>::narrow(r);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < U; ++i)
+                                if (c + i < cols) out[c + i] = narrow1<T>(r[i]);
+                        }
                     } else {
-#pragma unroll
-                        for (int i = 0; i < U; ++i)
-                            if (c + i < a.cols) d[i] = narrow1<T>(r[i]);
+                        out[c] = narrow1<T>(r[0]);
                     }
-                } else {
-                    *d = narrow1<T>(r[0]);
                 }
             }
         }
-        if constexpr (VEC) now = ahead;
+        if (++stage == stages) { stage = 0; phase ^= 1; }
     }
 
     if (!a.dgamma && !a.dbeta) return;
@@ -516,63 +617,78 @@ __global__ void __launch_bounds__(1024) norm_back_join_kernel(const float *parts
     if (tx == 0 && at < cols) out[at] = sum;
 }
 
-constexpr int BACK_BLOCKS = 296;       // two blocks of the row kernel on each of 148 SMs
+constexpr int BACK_THREADS = 512;      // of the row kernel on an SM
 constexpr int BACK_LONG_SHARES = 32;
 
-// The widest row that a block holds, and the threads for a row: two units of 16 bytes each.
+// The widest row that a block holds, and the threads for a row: two units of 16 bytes each, or 16 values.
 int64_t back_widest(int dtype) { return dtype == DIPACO_BF16 ? 16384 : 8192; }
-int back_threads_per_row(int64_t cols, int dtype)
+int back_threads_per_row(int64_t cols, int dtype, bool vec)
 {
     int tpr = 8;
-    while (tpr * (32 / dense_size(dtype)) < cols) tpr *= 2;
+    while (tpr * (vec ? 32 / dense_size(dtype) : 16) < cols) tpr *= 2;
     return tpr;
 }
 
 // Blocks that write their own sums of dgamma and dbeta.
-int64_t back_parts(int64_t rows, int64_t cols, int dtype)
+int64_t back_parts(int64_t rows, int64_t cols, int dtype, bool vec)
 {
     if (cols > back_widest(dtype)) return std::min<int64_t>(BACK_LONG_SHARES, ceil_div(rows, 64));
-    const int tpr = back_threads_per_row(cols, dtype);
-    return std::min<int64_t>(BACK_BLOCKS, ceil_div(rows, tpr < 256 ? 256 / tpr : 1));
+    const int tpr = back_threads_per_row(cols, dtype, vec), threads = std::max(tpr, 128);
+    const int64_t full = 148 * std::max(1, BACK_THREADS / threads);
+    return std::min(full, ceil_div(rows, threads / tpr * (vec ? 2 : 1)));
+}
+
+template <typename T, bool PACKED, bool VEC, int TPR>
+int launch_back_shape(const NormBackArgs &a, int blocks, cudaStream_t stream)
+{
+    using S = BackShape<T, PACKED, VEC, TPR>;
+    int stages = 1, dy_bytes = 0, x_bytes = 0, smem = 0;
+    if (VEC) {
+        dy_bytes = (int)ceil_div(a.cols * (int)sizeof(T), 16) * 16;
+        x_bytes = (int)ceil_div(a.cols * (int)sizeof(typename S::X), 16) * 16;
+        const int stage = S::GROUPS * S::ROWS * (dy_bytes + x_bytes);
+        const int resident = std::max(1, BACK_THREADS / S::THREADS);
+        stages = std::max(2, std::min(BACK_MAX_STAGES, 176 * 1024 / resident / stage));
+        smem = stages * stage + 128;
+        if (cudaFuncSetAttribute(norm_back_kernel<T, PACKED, VEC, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
+            cudaSuccess)
+            return launch_status();
+    }
+    norm_back_kernel<T, PACKED, VEC, TPR><<<blocks, S::THREADS, smem, stream>>>(a, stages, dy_bytes, x_bytes);
+    return launch_status();
 }
 
 template <typename T, bool PACKED, bool VEC>
-void launch_back(const NormBackArgs &a, int blocks, cudaStream_t stream)
+int launch_back(const NormBackArgs &a, int blocks, cudaStream_t stream)
 {
-    const int tpr = back_threads_per_row(a.cols, sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32);
-#define BACK_CASE(TPR)                                                                              \
-    case TPR:                                                                                       \
-        norm_back_kernel<T, PACKED, VEC, TPR><<<blocks, TPR < 256 ? 256 : TPR, 0, stream>>>(a);     \
-        return;
-    switch (tpr) {
-        BACK_CASE(8)
-        BACK_CASE(16)
-        BACK_CASE(32)
-        BACK_CASE(64)
-        BACK_CASE(128)
-        BACK_CASE(256)
-        BACK_CASE(512)
-        BACK_CASE(1024)
+    switch (back_threads_per_row(a.cols, sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32, VEC)) {
+    case 8: return launch_back_shape<T, PACKED, VEC, 8>(a, blocks, stream);
+    case 16: return launch_back_shape<T, PACKED, VEC, 16>(a, blocks, stream);
+    case 32: return launch_back_shape<T, PACKED, VEC, 32>(a, blocks, stream);
+    case 64: return launch_back_shape<T, PACKED, VEC, 64>(a, blocks, stream);
+    case 128: return launch_back_shape<T, PACKED, VEC, 128>(a, blocks, stream);
+    case 256: return launch_back_shape<T, PACKED, VEC, 256>(a, blocks, stream);
+    case 512: return launch_back_shape<T, PACKED, VEC, 512>(a, blocks, stream);
+    default: return launch_back_shape<T, PACKED, VEC, 1024>(a, blocks, stream);
     }
-#undef BACK_CASE
 }
 
 template <typename T, bool PACKED>
-void launch_back_any(const NormBackArgs &a, int blocks, bool vec, cudaStream_t stream)
+int launch_back_any(const NormBackArgs &a, int blocks, bool vec, cudaStream_t stream)
 {
     if (a.cols > back_widest(sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32)) {
         if (a.dx) norm_back_long_rows_kernel<T, PACKED><<<a.rows, 1024, 0, stream>>>(a);
         if (a.dgamma || a.dbeta)
             norm_back_long_columns_kernel<T, PACKED>
                 <<<dim3((unsigned)ceil_div(a.cols, 256), blocks), 256, 0, stream>>>(a);
-    } else if (vec) {
-        launch_back<T, PACKED, true>(a, blocks, stream);
-    } else {
-        launch_back<T, PACKED, false>(a, blocks, stream);
+        return launch_status();
     }
+    return vec ? launch_back<T, PACKED, true>(a, blocks, stream) : launch_back<T, PACKED, false>(a, blocks, stream);
 }
 
 } // namespace
+
+bool dipaco::take_norm_error(bool &expired) { return take_error_word(g_norm_error, expired); }
 
 extern "C" {
 
@@ -593,14 +709,19 @@ int dipaco_layer_norm(const void *x, int64_t x_stride, const void *gamma, const 
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    NormArgs a = {x, y, gamma, beta, mean, rstd, x_stride, y_stride, (int)rows, (int)cols, eps,
+    NormArgs a = {x, y, gamma, beta, mean, rstd, x_stride, y_stride, (int)rows, (int)cols, eps, 1.0f / (float)cols,
                   param_dtype == DIPACO_BF16, (uintptr_t)gamma % 16 == 0, (uintptr_t)beta % 16 == 0};
     const int size = dense_size(dtype);
     const bool vec = rows_aligned16(x, x_stride, rows, size) && (!y || rows_aligned16(y, y_stride, rows, size));
+    const bool ragged = cols * size % 16 != 0;
     if (dtype == DIPACO_BF16)
-        vec ? launch_norm<__nv_bfloat16, true>(a, stream) : launch_norm<__nv_bfloat16, false>(a, stream);
+        !vec     ? launch_norm<__nv_bfloat16, false, false>(a, stream)
+        : ragged ? launch_norm<__nv_bfloat16, true, true>(a, stream)
+                 : launch_norm<__nv_bfloat16, true, false>(a, stream);
     else
-        vec ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
+        !vec     ? launch_norm<float, false, false>(a, stream)
+        : ragged ? launch_norm<float, true, true>(a, stream)
+                 : launch_norm<float, true, false>(a, stream);
     return launch_status();
 }
 
@@ -608,8 +729,10 @@ int dipaco_layer_norm_workspace(int64_t rows, int64_t cols, int64_t *bytes)
 {
     if (!bytes) return DIPACO_EINVAL;
     if (const int rc = check_extents(rows, cols)) return rc;
-    int64_t parts = 0;  // the most of either dtype
-    if (rows > 0 && cols > 0) parts = std::max(back_parts(rows, cols, DIPACO_F32), back_parts(rows, cols, DIPACO_BF16));
+    int64_t parts = 0;  // the most of either dtype and alignment
+    if (rows > 0 && cols > 0)
+        for (int dtype : {DIPACO_F32, DIPACO_BF16})
+            for (bool vec : {false, true}) parts = std::max(parts, back_parts(rows, cols, dtype, vec));
     *bytes = parts > 1 ? parts * 2 * cols * (int64_t)sizeof(float) : 0;
     return DIPACO_OK;
 }
@@ -646,7 +769,10 @@ int dipaco_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
         if (dbeta && cudaMemsetAsync(dbeta, 0, cols * sizeof(float), stream) != cudaSuccess) return launch_status();
         return DIPACO_OK;
     }
-    const int parts = (int)back_parts(rows, cols, dtype);
+    const int size = dense_size(dtype);
+    const bool vec = rows_aligned16(dy, dy_stride, rows, size) && (!x || rows_aligned16(x, x_stride, rows, size)) &&
+                     (!dx || rows_aligned16(dx, dx_stride, rows, size));
+    const int parts = (int)back_parts(rows, cols, dtype, vec);
     NormBackArgs a = {};
     a.dy = dy;
     a.x = x_packed ? x_packed->codes : x;
@@ -672,14 +798,11 @@ int dipaco_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
         a.dgamma = dgamma;
         a.dbeta = dbeta;
     }
-    const int size = dense_size(dtype);
-    const bool vec = rows_aligned16(dy, dy_stride, rows, size) && (!x || rows_aligned16(x, x_stride, rows, size)) &&
-                     (!dx || rows_aligned16(dx, dx_stride, rows, size));
-    if (dtype == DIPACO_BF16)
-        x ? launch_back_any<__nv_bfloat16, false>(a, parts, vec, stream)
-          : launch_back_any<__nv_bfloat16, true>(a, parts, vec, stream);
-    else
-        x ? launch_back_any<float, false>(a, parts, vec, stream) : launch_back_any<float, true>(a, parts, vec, stream);
+    if (const int rc = dtype == DIPACO_BF16 ? (x ? launch_back_any<__nv_bfloat16, false>(a, parts, vec, stream)
+                                                 : launch_back_any<__nv_bfloat16, true>(a, parts, vec, stream))
+                                            : (x ? launch_back_any<float, false>(a, parts, vec, stream)
+                                                 : launch_back_any<float, true>(a, parts, vec, stream)))
+        return rc;
     if (parts > 1 && (dgamma || dbeta))
         norm_back_join_kernel<<<dim3((unsigned)ceil_div(cols, 32), 2), 1024, 0, stream>>>(
             a.dgamma, a.dbeta, parts, a.part_stride, (int)cols, dgamma, dbeta);

@@ -5,8 +5,12 @@
 //   gelu(a) = a s, s = 1 / (1 + exp(-2u)), u = sqrt(2/pi) (a + 0.044715 a^3)   (the tanh form: 2s = 1 + tanh u)
 //   gelu'(a) = s + a s (1 - s) 2 u',  u' = sqrt(2/pi) (1 + 3 * 0.044715 a^2)
 //
-// One block of threads per block of 128 x 128 values: the values are read once and stay in registers
-// while the block's largest magnitude is found.
+// One block of threads per block of 128 x 128 values, which is read once: the largest magnitude has to be
+// known before the first code is.
+//
+//   stream_kernel  bf16 rows on 16-byte boundaries: persistent, the copy engine brings the next blocks to
+//                  shared memory while one is worked on
+//   block_kernel   fp32, and rows at any alignment: the values are loaded to registers
 #include "inner_common.cuh"
 
 #include <cmath>
@@ -70,11 +74,25 @@ struct PackedOut {
     long long stride;
 };
 
+// Magnitudes of pairs of bf16 values: the larger of each half (NaN only where both are), and the larger half
+// as the bits of an fp32 value.
+__device__ __forceinline__ unsigned larger_bf16x2(unsigned magnitudes, unsigned w)
+{
+    w &= 0x7fff7fffu;
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&magnitudes),
+                                     *reinterpret_cast<const __nv_bfloat162 *>(&w));
+    return *reinterpret_cast<const unsigned *>(&m);
+}
+__device__ __forceinline__ unsigned wider_bf16x2(unsigned magnitudes)
+{
+    return max(magnitudes << 16, magnitudes & 0xffff0000u);
+}
+
 // The thread's values of one matrix: as they were loaded, or computed in fp32.
 template <typename T> struct LoadedValues {
     const uint4 *raw;
     __device__ __forceinline__ void unit(int j, float *f) const { Unit<T>::widen(raw[j], f); }
-    // Bits of the largest magnitude; at least those of infinity if there is an infinity or NaN.
+    // Bits of the largest magnitude; at least those of infinity if there is an infinity.
     __device__ __forceinline__ unsigned largest() const
     {
         unsigned m = 0u;
@@ -84,12 +102,12 @@ template <typename T> struct LoadedValues {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (sizeof(T) == 2)
-                    m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+                    m = larger_bf16x2(m, w[i]);
                 else
                     m = max(m, w[i] & 0x7fffffffu);
             }
         }
-        return sizeof(T) == 2 ? max(m << 16, m & 0xffff0000u) : m;
+        return sizeof(T) == 2 ? wider_bf16x2(m) : m;
     }
 };
 template <typename T> struct ComputedValues {
@@ -125,14 +143,13 @@ template <int U, bool SPECIAL> __device__ __forceinline__ void store_codes(uint8
     }
 }
 
-// Writes the block's codes and scale.  Infinities and NaN are rare: where the largest magnitude is not
-// finite, the block looks for the largest finite one and encodes with care for infinities.
+// Writes the codes and the scale of block `index`, given the bits m of its largest magnitude.  Infinities
+// are rare: where m is not finite, the block looks for its largest finite magnitude and encodes with care.
 template <typename T, typename Values>
-__device__ __forceinline__ void write_block(const PackedOut &out, const Extent &x, int row0, int col, const Values &v,
-                                            unsigned *shared)
+__device__ __forceinline__ void write_codes(const PackedOut &out, const Extent &x, long long index, int row0, int col,
+                                            const Values &v, unsigned m, unsigned *shared)
 {
     using L = Layout<T>;
-    unsigned m = block_max(v.largest(), shared);
     const bool special = m >= 0x7f800000u;
     if (special) {
         m = 0u;
@@ -143,11 +160,11 @@ __device__ __forceinline__ void write_block(const PackedOut &out, const Extent &
 #pragma unroll
             for (int i = 0; i < L::U; ++i) m = max(m, finite_magnitude(f[i]));
         }
-        m = block_max(m, shared + THREADS / 32);
+        m = block_max(m, shared);
     }
     const unsigned byte = scale_byte(m);
     const float reciprocal = scale_reciprocal(byte);
-    if (threadIdx.x == 0) out.scales[blockIdx.x] = (uint8_t)byte;
+    if (threadIdx.x == 0) out.scales[index] = (uint8_t)byte;
     if (col >= x.cols) return;
     uint8_t *p = out.codes + (long long)row0 * out.stride + col;
 #pragma unroll
@@ -180,6 +197,18 @@ __device__ __forceinline__ float reciprocal_of(float x)
     return r;
 }
 
+__device__ __forceinline__ float gelu(float a) { return a * reciprocal_of(1.0f + gelu_decay(a)); }
+
+// s + a s (1 - s) 2u' = s (1 + a d s 2u') with d = exp(-2u): no cancellation where s is near 1.  a is held
+// within +-10.03, NaN kept: there the slope is 1, or 0 (d is still finite and s flushed to zero).
+__device__ __forceinline__ float gelu_slope(float a)
+{
+    constexpr float k1 = 2.0f * 0.7978845608028654f, k3 = 3.0f * 0.044715f * k1;
+    asm("min.NaN.f32 %0, %0, 0f41208000;\n\tmax.NaN.f32 %0, %0, 0fC1208000;" : "+f"(a));
+    const float d = gelu_decay(a), s = reciprocal_of(1.0f + d);
+    return s * fmaf(d * s, a * fmaf(k3, a * a, k1), 1.0f);
+}
+
 enum : int { OP_PACK, OP_NORM, OP_GELU, OP_GELU_BACK };
 
 struct BlockArgs {
@@ -198,12 +227,21 @@ struct BlockArgs {
     bool params_bf16, gamma_aligned, beta_aligned;
 };
 
+// gamma and beta of U columns.
+template <int U> __device__ __forceinline__ void norm_params(const BlockArgs &a, int col, float *gamma, float *beta)
+{
+#pragma unroll
+    for (int i = 0; i < U; ++i) { gamma[i] = 1.0f; beta[i] = 0.0f; }
+    if (a.gamma) load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, col, a.extent.cols, gamma);
+    if (a.beta) load_params<U>(a.beta, a.params_bf16, a.beta_aligned, col, a.extent.cols, beta);
+}
+
 template <typename T, int OP>
 __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant__ BlockArgs a)
 {
     using L = Layout<T>;
     constexpr int U = L::U;
-    __shared__ unsigned shared[2][2 * THREADS / 32];
+    __shared__ unsigned shared[4][THREADS / 32];
     const int rows = a.extent.rows, cols = a.extent.cols;
     const int row0 = (int)(blockIdx.x / a.extent.block_cols) * PACK_BLOCK + (int)threadIdx.x / L::PER_ROW;
     const int col = (int)(blockIdx.x % a.extent.block_cols) * PACK_BLOCK + (int)(threadIdx.x % L::PER_ROW) * U;
@@ -225,17 +263,14 @@ __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant
     }
     const LoadedValues<T> loaded = {raw};
     if constexpr (OP == OP_PACK) {
-        write_block<T>(a.first, a.extent, row0, col, loaded, shared[0]);
+        write_codes<T>(a.first, a.extent, blockIdx.x, row0, col, loaded, block_max(loaded.largest(), shared[0]), shared[1]);
         return;
     }
 
     float y[VALUES];
     if constexpr (OP == OP_NORM) {
         float gamma[U], beta[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) { gamma[i] = 1.0f; beta[i] = 0.0f; }
-        if (a.gamma) load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, col, cols, gamma);
-        if (a.beta) load_params<U>(a.beta, a.params_bf16, a.beta_aligned, col, cols, beta);
+        norm_params<U>(a, col, gamma, beta);
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
             const int r = row0 + j * L::STEP;
@@ -256,10 +291,9 @@ __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant
             float *f = y + j * U;
             loaded.unit(j, f);
 #pragma unroll
-            for (int i = 0; i < U; ++i) f[i] *= reciprocal_of(1.0f + gelu_decay(f[i]));
+            for (int i = 0; i < U; ++i) f[i] = gelu(f[i]);
         }
     } else {
-        constexpr float k = 2.0f * 0.7978845608028654f;
         const float scale = scale_value(a.scales[blockIdx.x]);
         const uint8_t *q = a.codes + (long long)row0 * a.codes_stride + col;
 #pragma unroll
@@ -273,15 +307,7 @@ __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant
                 // rows of codes are padded to 16 bytes: four of them can be read wherever one can
                 decode4(in && (!edge || col + i < cols) ? *reinterpret_cast<const unsigned *>(q + i) : 0u, scale, v);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    // s (1 - s) = d s^2 with d = exp(-2u): no cancellation where s is near 1
-                    const float decay = gelu_decay(v[t]), d = decay > 3e38f ? 3e38f : decay;
-                    const float s = reciprocal_of(1.0f + d), w = d * s * s;
-                    // w is zero before its factors overflow (a code times its scale may itself exceed
-                    // the largest fp32 value)
-                    const float bend = w == 0.0f ? 0.0f : v[t] * w * fmaf(3.0f * 0.044715f * k, v[t] * v[t], k);
-                    f[i + t] *= s + bend;
-                }
+                for (int t = 0; t < 4; ++t) f[i + t] *= gelu_slope(v[t]);
             }
             if (edge) {
 #pragma unroll
@@ -292,8 +318,157 @@ __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant
         }
     }
     const ComputedValues<T> computed = {y};
-    write_block<T>(a.first, a.extent, row0, col, computed, shared[0]);
-    if (OP != OP_GELU_BACK && a.second.codes) write_block<T>(a.second, a.extent, row0, col, loaded, shared[1]);
+    write_codes<T>(a.first, a.extent, blockIdx.x, row0, col, computed, block_max(computed.largest(), shared[0]), shared[1]);
+    if (OP != OP_GELU_BACK && a.second.codes)
+        write_codes<T>(a.second, a.extent, blockIdx.x, row0, col, loaded, block_max(loaded.largest(), shared[2]), shared[3]);
+}
+
+// ------------------------------------------------------------------------------------------ streamed blocks
+
+static __device__ int g_packing_error;  // set by a bounded wait that ran out
+
+constexpr int DENSE_BYTES = PACK_BLOCK * PACK_BLOCK * 2;  // of a block in bf16
+constexpr int CODE_BYTES = PACK_BLOCK * PACK_BLOCK;
+
+// Buffers for blocks on their way.  A buffer is free once every thread is past the barrier of the block in
+// it (OP_GELU_BACK, which has read it then) or of the next block (the others read it again to pack it).
+template <int OP> struct Stream {
+    static constexpr int BUFFERS = OP == OP_GELU_BACK ? 2 : 3;
+    static constexpr int BYTES = DENSE_BYTES + (OP == OP_GELU_BACK ? CODE_BYTES : 0);
+    static constexpr int SMEM = BUFFERS * BYTES + 128;
+};
+
+// A thread's values in shared memory: as LoadedValues.
+struct SharedValues {
+    const uint4 *unit0;
+    __device__ __forceinline__ uint4 at(int j) const { return unit0[j * THREADS]; }
+    __device__ __forceinline__ void unit(int j, float *f) const { Unit<__nv_bfloat16>::widen(at(j), f); }
+};
+
+__device__ __forceinline__ void load_box(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+            ptx::smem_addr(to)),
+        "l"(map), "r"(x), "r"(y), "r"(ptx::smem_addr(bar))
+        : "memory");
+}
+
+template <int OP>
+__global__ void __launch_bounds__(THREADS, 2)
+    stream_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap codes_map,
+                  const __grid_constant__ BlockArgs a, int blocks)
+{
+    using T = __nv_bfloat16;
+    using L = Layout<T>;
+    using S = Stream<OP>;
+    constexpr int U = L::U;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[S::BUFFERS];
+    __shared__ unsigned maxima[2][2][THREADS / 32], special[2][THREADS / 32];
+    uint8_t *buffers = raw + ((128u - (ptx::smem_addr(raw) & 127u)) & 127u);
+    const int rows = a.extent.rows, cols = a.extent.cols;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+
+    if (threadIdx.x == 0) {
+        for (int b = 0; b < S::BUFFERS; ++b) ptx::mbar_init(&full[b], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const auto request = [&](int index, int buffer) {  // one thread
+        ptx::mbar_arrive_expect_tx(&full[buffer], S::BYTES);
+        const int x = index % a.extent.block_cols * PACK_BLOCK, y = index / a.extent.block_cols * PACK_BLOCK;
+        load_box(buffers + buffer * S::BYTES, &x_map, x, y, &full[buffer]);
+        if (OP == OP_GELU_BACK) load_box(buffers + buffer * S::BYTES + DENSE_BYTES, &codes_map, x, y, &full[buffer]);
+    };
+    if (threadIdx.x == 0)
+        for (int b = 0; b < S::BUFFERS; ++b)
+            if (blockIdx.x + (long long)b * gridDim.x < blocks) request(blockIdx.x + b * gridDim.x, b);
+
+    int buffer = 0, previous = S::BUFFERS - 1;
+    unsigned phase = 0, turn = 0;
+    for (int index = blockIdx.x; index < blocks; index += gridDim.x) {
+        const int row0 = index / a.extent.block_cols * PACK_BLOCK + (int)threadIdx.x / L::PER_ROW;
+        const int col0 = index % a.extent.block_cols * PACK_BLOCK;
+        const int col = col0 + (int)(threadIdx.x % L::PER_ROW) * U;
+        float gamma[U], beta[U], mean[L::UNITS], rstd[L::UNITS];
+        if constexpr (OP == OP_NORM) {
+            norm_params<U>(a, col, gamma, beta);
+#pragma unroll
+            for (int j = 0; j < L::UNITS; ++j) {
+                const int r = min(row0 + j * L::STEP, rows - 1);
+                mean[j] = a.mean[r];
+                rstd[j] = a.rstd[r];
+            }
+        }
+        const float scale = OP == OP_GELU_BACK ? scale_value(a.scales[index]) : 0.0f;
+        const SharedValues x = {reinterpret_cast<const uint4 *>(buffers + buffer * S::BYTES) + threadIdx.x};
+        if (!bounded_wait(&full[buffer], phase, &g_packing_error, 1)) {
+            for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
+            return;
+        }
+
+        float y[OP == OP_PACK ? 1 : VALUES];
+        unsigned mx = 0u;
+        float my = 0.0f;
+#pragma unroll
+        for (int j = 0; j < L::UNITS; ++j) {
+            const uint4 unit = x.at(j);  // zero outside the matrix
+            if constexpr (OP != OP_GELU_BACK) {
+                mx = larger_bf16x2(mx, unit.x);
+                mx = larger_bf16x2(mx, unit.y);
+                mx = larger_bf16x2(mx, unit.z);
+                mx = larger_bf16x2(mx, unit.w);
+            }
+            if constexpr (OP != OP_PACK) {
+                float *f = y + j * U;
+                Unit<T>::widen(unit, f);
+                if constexpr (OP == OP_NORM) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) f[i] = fmaf((f[i] - mean[j]) * rstd[j], gamma[i], beta[i]);
+                    if (col0 + PACK_BLOCK > cols || row0 + j * L::STEP >= rows) {
+#pragma unroll
+                        for (int i = 0; i < U; ++i)
+                            if (row0 + j * L::STEP >= rows || col + i >= cols) f[i] = 0.0f;
+                    }
+                } else if constexpr (OP == OP_GELU) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) f[i] = gelu(f[i]);
+                } else {
+                    const uint2 c = reinterpret_cast<const uint2 *>(buffers + buffer * S::BYTES + DENSE_BYTES)[threadIdx.x + j * THREADS];
+                    float v[U];
+                    decode4(c.x, scale, v);
+                    decode4(c.y, scale, v + 4);
+#pragma unroll
+                    for (int i = 0; i < U; ++i) f[i] *= gelu_slope(v[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i) my = fmaxf(my, fabsf(f[i]));
+            }
+        }
+        const unsigned wx = __reduce_max_sync(0xffffffffu, wider_bf16x2(mx));
+        const unsigned wy = __reduce_max_sync(0xffffffffu, __float_as_uint(my));
+        if (lane == 0) {
+            maxima[turn][0][warp] = wx;
+            maxima[turn][1][warp] = wy;
+        }
+        __syncthreads();
+        const int freed = OP == OP_GELU_BACK ? buffer : previous;
+        const long long next = index + (long long)gridDim.x * (OP == OP_GELU_BACK ? S::BUFFERS : S::BUFFERS - 1);
+        if (threadIdx.x == 0 && next < blocks && (OP == OP_GELU_BACK || index != (int)blockIdx.x)) request((int)next, freed);
+        if constexpr (OP != OP_PACK) {
+            const ComputedValues<T> computed = {y};
+            const unsigned m = __reduce_max_sync(0xffffffffu, maxima[turn][1][lane % (THREADS / 32)]);
+            write_codes<T>(a.first, a.extent, index, row0, col, computed, m, special[0]);
+        }
+        if (OP == OP_PACK || (OP != OP_GELU_BACK && a.second.codes)) {
+            const unsigned m = __reduce_max_sync(0xffffffffu, maxima[turn][0][lane % (THREADS / 32)]);
+            write_codes<T>(OP == OP_PACK ? a.first : a.second, a.extent, index, row0, col, x, m, special[1]);
+        }
+        previous = buffer;
+        if (++buffer == S::BUFFERS) { buffer = 0; phase ^= 1; }
+        turn ^= 1;
+    }
 }
 
 // Four codes per thread.
@@ -330,13 +505,40 @@ PackedOut packed_out(const dipaco_packed *p)
     return {static_cast<uint8_t *>(p->codes), static_cast<uint8_t *>(p->scales), p->stride};
 }
 
+bool box_map(CUtensorMap *map, const void *data, int64_t rows, int64_t cols, int64_t row_bytes, bool codes)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)row_bytes};
+    const cuuint32_t box[2] = {PACK_BLOCK, PACK_BLOCK}, steps[2] = {1, 1};
+    return encode(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+                  const_cast<void *>(data), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int OP> int launch_stream(const BlockArgs &a, int blocks, cudaStream_t stream)
+{
+    const int64_t rows = a.extent.rows, cols = a.extent.cols;
+    CUtensorMap x_map, codes_map = {};
+    // the stride of a single row is never used, but has to be a possible one
+    const int64_t x_bytes = rows == 1 ? ceil_div(cols, 8) * 16 : a.x_stride * 2;
+    if (!box_map(&x_map, a.x, rows, cols, x_bytes, false)) return DIPACO_ECUDA;
+    if (OP == OP_GELU_BACK && !box_map(&codes_map, a.codes, rows, cols, a.codes_stride, true)) return DIPACO_ECUDA;
+    if (cudaFuncSetAttribute(stream_kernel<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Stream<OP>::SMEM) != cudaSuccess)
+        return launch_status();
+    stream_kernel<OP><<<std::min(blocks, 296), THREADS, Stream<OP>::SMEM, stream>>>(x_map, codes_map, a, blocks);
+    return launch_status();
+}
+
 template <int OP>
 int launch_blocks(BlockArgs a, int dtype, int64_t rows, int64_t cols, cudaStream_t stream)
 {
     const int64_t block_cols = ceil_div(cols, PACK_BLOCK), blocks = ceil_div(rows, PACK_BLOCK) * block_cols;
-    if (blocks > INT32_MAX) return DIPACO_ELIMIT;
+    if (blocks > INT32_MAX - 4096) return DIPACO_ELIMIT;
     a.extent = {(int)rows, (int)cols, (int)block_cols};
     a.aligned = rows_aligned16(a.x, a.x_stride, rows, dense_size(dtype));
+    if (dtype == DIPACO_BF16 && a.aligned) return launch_stream<OP>(a, (int)blocks, stream);
     if (dtype == DIPACO_BF16)
         block_kernel<__nv_bfloat16, OP><<<(unsigned)blocks, THREADS, 0, stream>>>(a);
     else
@@ -352,6 +554,8 @@ int check_dense(const void *x, int64_t stride, int64_t rows, int64_t cols, int d
 }
 
 } // namespace
+
+bool dipaco::take_packing_error(bool &expired) { return take_error_word(g_packing_error, expired); }
 
 extern "C" {
 

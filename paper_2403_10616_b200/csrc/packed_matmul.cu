@@ -13,8 +13,6 @@
 //                  contraction shared by the blocks of a cluster
 #include "inner_common.cuh"
 
-#include <cuda.h>
-
 #include <algorithm>
 #include <cmath>
 
@@ -26,14 +24,6 @@ static __device__ int g_product_error;  // set by a bounded wait that ran out
 
 // ------------------------------------------------------------------------------------------ PTX
 
-// True on one thread of the warp.  Asynchronous copies and products are issued under it: the compiler
-// then keeps their operands in uniform registers, which it does not under a test of the lane.
-__device__ __forceinline__ bool elect_one()
-{
-    unsigned ok;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
-    return ok != 0;
-}
 // An address of this block's shared memory as seen from, or for, block `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t address, unsigned rank)
 {
@@ -935,25 +925,6 @@ __global__ void __launch_bounds__(SKINNY_THREADS)
 
 // ------------------------------------------------------------------------------------------ host
 
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled()
-{
-    static const EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
 // Boxes of `rows` x 128 codes in the 128-byte swizzle; codes outside the matrix read as zero.
 bool operand_map(CUtensorMap *map, const dipaco_packed *x, int rows)
 {
@@ -1156,18 +1127,16 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     return launch_status();
 }
 
-int dipaco_packed_matmul_status(int32_t device, void *cuda_stream)
+int dipaco_inner_status(int32_t device, void *cuda_stream)
 {
     if (device < 0) return DIPACO_EINVAL;
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return DIPACO_ECUDA;
-    int word = 0;
-    if (cudaMemcpyFromSymbol(&word, g_product_error, sizeof(int)) != cudaSuccess) return launch_status();
-    if (word == 0) return DIPACO_OK;
-    word = 0;
-    cudaMemcpyToSymbol(g_product_error, &word, sizeof(int));
-    return DIPACO_ETIMEOUT;
+    bool expired = false;
+    if (!take_error_word(g_product_error, expired) || !take_packing_error(expired) || !take_norm_error(expired))
+        return launch_status();
+    return expired ? DIPACO_ETIMEOUT : DIPACO_OK;
 }
 
 } // extern "C"

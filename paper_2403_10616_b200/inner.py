@@ -213,8 +213,8 @@ def packed_matmul(a: Packed, b: Packed, transpose_a: bool = False, transpose_b: 
     return out
 
 
-def packed_matmul_status(device=None) -> int:
+def inner_status(device=None) -> int:
     """Waits for the current stream and reports DIPACO_OK, or DIPACO_ETIMEOUT once after a bounded
-    wait inside a product ran out."""
+    wait inside one of these operators ran out."""
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    return B.dipaco_packed_matmul_status(dev.index or 0, torch.cuda.current_stream(dev).cuda_stream)
+    return B.dipaco_inner_status(dev.index or 0, torch.cuda.current_stream(dev).cuda_stream)

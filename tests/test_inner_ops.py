@@ -432,7 +432,7 @@ def test_product_of_packed_matrices(m, n, k, form):
     want = av @ bv
     for dtype in (F32, BF16):
         got = inner.packed_matmul(a, b, ta, tb, dtype)
-        assert inner.packed_matmul_status() == B.DIPACO_OK
+        assert inner.inner_status() == B.DIPACO_OK
         assert_within(got, want, product_tolerance(av, bv, k), str(dtype), dtype)
         # into a slice of a wider buffer at odd offsets, and added to what is there
         hold = torch.full((m, n + 5), 3.0, dtype=dtype, device=DEV)
@@ -471,7 +471,7 @@ def test_product_of_larger_packed_matrices(m, n, k, form):
     want = av @ bv
     for dtype in (F32, BF16):
         got = inner.packed_matmul(a, b, ta, tb, dtype)
-        assert inner.packed_matmul_status() == B.DIPACO_OK
+        assert inner.inner_status() == B.DIPACO_OK
         tol = product_tolerance(av, bv, k)
         err, tol = (got.double() - want).abs(), tol + half(dtype, want.abs() + tol)
         assert bool((err <= tol).all()), (dtype, float((err / tol).max()))
