@@ -15,7 +15,7 @@
 namespace dipaco {
 
 constexpr int PACK_BLOCK = 128;
-constexpr int64_t MAX_EXTENT = (int64_t)INT32_MAX - 1024;  // rows or columns of one matrix
+constexpr int64_t MAX_EXTENT = (int64_t)INT32_MAX - 65536;  // rows or columns: steps beyond the last fit an int
 
 // ------------------------------------------------------------------------------------------ host
 
@@ -117,10 +117,80 @@ __device__ __forceinline__ bool elect_one()
     return ok != 0;
 }
 
-// The value of an e8m0 byte: 2^(b-127); 255 is NaN.
+// Two fp32 values in one register pair: additions and products take one issue slot for both.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair_of(float lo, float hi)
+{
+    f32x2 p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ f32x2 pair_of(float both) { return pair_of(both, both); }
+__device__ __forceinline__ float2 values_of(f32x2 p)
+{
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float sum_of(f32x2 p)
+{
+    const float2 v = values_of(p);
+    return v.x + v.y;
+}
+// 16 bytes to pairs, and pairs to 16 bytes (rounded).
+template <typename T> __device__ __forceinline__ void widen_pairs(const uint4 &v, f32x2 *p)
+{
+    float f[Unit<T>::UE];
+    Unit<T>::widen(v, f);
+#pragma unroll
+    for (int i = 0; i < Unit<T>::UE / 2; ++i) p[i] = pair_of(f[2 * i], f[2 * i + 1]);
+}
+template <typename T> __device__ __forceinline__ uint4 narrow_pairs(const f32x2 *p)
+{
+    float f[Unit<T>::UE];
+#pragma unroll
+    for (int i = 0; i < Unit<T>::UE / 2; ++i) {
+        const float2 v = values_of(p[i]);
+        f[2 * i] = v.x;
+        f[2 * i + 1] = v.y;
+    }
+    return Unit<T>::narrow(f);
+}
+
+// The first n of a unit's values, the others zero.
+template <int U> __device__ __forceinline__ void keep_inside(f32x2 *p, int n)
+{
+#pragma unroll
+    for (int i = 0; i < U / 2; ++i) {
+        const float2 v = values_of(p[i]);
+        p[i] = pair_of(2 * i < n ? v.x : 0.0f, 2 * i + 1 < n ? v.y : 0.0f);
+    }
+}
+
+// The value of an e8m0 byte: 2^(b-127), which bf16 holds; 255 is NaN.
 __device__ __forceinline__ float scale_value(unsigned b)
 {
-    return b == 0u ? __uint_as_float(0x00400000u) : b == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(b << 23);
+    unsigned r;
+    asm("cvt.rn.bf16x2.ue8m0x2 %0, %1;" : "=r"(r) : "h"((unsigned short)b));
+    return __uint_as_float(r << 16);
 }
 
 // Magnitude bits that take part in a block's maximum: those of infinities and NaN do not.
@@ -155,16 +225,21 @@ __device__ __forceinline__ unsigned encode4(const float *f, float reciprocal)
     return encode2(f[0], f[1], reciprocal) | (encode2(f[2], f[3], reciprocal) << 16);
 }
 // The same where no value is infinite.
-__device__ __forceinline__ unsigned encode4_finite(const float *f, float reciprocal)
+__device__ __forceinline__ unsigned encode4_finite(const f32x2 *p, f32x2 reciprocal)
 {
-    const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0] * reciprocal, f[1] * reciprocal), __NV_SATFINITE, __NV_E4M3);
-    const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2] * reciprocal, f[3] * reciprocal), __NV_SATFINITE, __NV_E4M3);
-    return lo | (hi << 16);
+    const unsigned lo = __nv_cvt_float2_to_fp8x2(values_of(mul2(p[0], reciprocal)), __NV_SATFINITE, __NV_E4M3);
+    const unsigned hi = __nv_cvt_float2_to_fp8x2(values_of(mul2(p[1], reciprocal)), __NV_SATFINITE, __NV_E4M3);
+    return __byte_perm(lo, hi, 0x5410);
 }
 __device__ __forceinline__ float2 decode2(unsigned codes)
 {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
     return __half22float2(__half2(h));
+}
+__device__ __forceinline__ f32x2 decode_pair(unsigned codes)
+{
+    const float2 v = decode2(codes & 0xffffu);
+    return pair_of(v.x, v.y);
 }
 __device__ __forceinline__ void decode4(unsigned codes, float scale, float *f)
 {
@@ -211,6 +286,15 @@ __device__ __forceinline__ void load_params(const void *p, bool bf16, bool align
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) f[i] = c + i < cols ? load_param(p, bf16, c + i) : 0.0f;
+}
+
+template <int U>
+__device__ __forceinline__ void param_pairs(const void *p, bool bf16, bool aligned, int c, int cols, f32x2 *pairs)
+{
+    float f[U];
+    load_params<U>(p, bf16, aligned, c, cols, f);
+#pragma unroll
+    for (int i = 0; i < U / 2; ++i) pairs[i] = pair_of(f[2 * i], f[2 * i + 1]);
 }
 
 } // namespace dipaco

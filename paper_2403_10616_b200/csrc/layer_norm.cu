@@ -59,111 +59,130 @@ __device__ __forceinline__ float inverse_root(float v, float eps)
     return v > 1e-30f && v < 1e30f ? better : 1.0f / sqrtf(v);  // where the step's products stay normal
 }
 
-// One row at a time per TPR threads, in registers: NU units of 16 bytes per thread (VEC: rows on 16-byte
-// boundaries), or as many single values.  Bound by memory: the next row is on its way while this one is
-// summed, and a warp per row up to 2048 values in bf16 (1024 in fp32) keeps the sums inside warps.
-// RAGGED: the last unit of a row is partly outside.  Sums run in four chains: one alone leaves the warp
-// waiting for its own additions (16384x2048: 71 us, ... us with four).
-template <typename T, bool VEC, bool RAGGED, int TPR, int NU>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU == 8 ? 4 : 6) norm_rows_kernel(const __grid_constant__ NormArgs a)
+template <typename T> __device__ __forceinline__ void store_first(T *p, const uint4 &v, int n)
 {
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(T); ++i)
+        if (i < n) store_element(p + i, v, i);
+}
+
+constexpr int NORM_WIDEST = 16384;  // values of a row with gamma and beta in shared memory
+
+// How rows are read: by single values, by units of 16 bytes, or by units of which a row's last is partly outside.
+enum : int { ROWS_SINGLE, ROWS_UNITS, ROWS_RAGGED };
+
+// One row at a time per TPR threads, in registers: NU units of 16 bytes per thread, of which the last PART
+// may lie outside the row, or as many single values.  Bound by memory, if little else is done: the next row
+// is on its way while this one is summed, sums run in four chains, and gamma and beta wait in shared memory
+// in fp32 (with both read and widened for every row: 16384x2048 43 us).  A warp per row up to 2048 values
+// in bf16 (1024 in fp32) keeps sums inside warps.
+template <typename T, int MODE, int TPR, int NU, int PART>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU > 4 ? 4 : 6)
+    norm_rows_kernel(const __grid_constant__ NormArgs a)
+{
+    constexpr bool VEC = MODE != ROWS_SINGLE;
     constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
     constexpr int E = NU * 16 / (int)sizeof(T);
-    constexpr int UNITS = E / U;
-    constexpr int GROUPS = (TPR < 128 ? 128 : TPR) / TPR;
+    constexpr int UNITS = E / U, SURE = VEC ? NU - PART : 0;  // units that are inside for certain
+    constexpr int THREADS = TPR < 128 ? 128 : TPR, GROUPS = THREADS / TPR;
     using Raw = typename std::conditional<VEC, uint4, T>::type;
+    extern __shared__ float params[];  // gamma, beta, each padded to whole units
     __shared__ float shared[4][TPR > 32 ? TPR / 32 : 1];  // two sums of a row, of two rows in turn
     const int lane = threadIdx.x % TPR;
-    const long long step = (long long)gridDim.x * GROUPS;
-    long long row = (long long)blockIdx.x * GROUPS + threadIdx.x / TPR;
+    const int step = (int)gridDim.x * GROUPS;
+    int row = (int)blockIdx.x * GROUPS + (int)threadIdx.x / TPR;
     const T *x = static_cast<const T *>(a.x) + row * a.x_stride + lane * U;
     T *y = static_cast<T *>(a.y) + row * a.y_stride + lane * U;
     const int cols = a.cols - lane * U;  // a unit j of this thread is inside while j * TPR * U < cols
+    const int padded = (a.cols + 7) & ~7;
 
     Raw raw[UNITS];
 #pragma unroll
-    for (int j = 0; j < UNITS; ++j)
-        if (row < a.rows && j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
+    for (int j = 0; j < UNITS; ++j) {
+        if constexpr (VEC) raw[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < a.rows && (j < SURE || j * TPR * U < cols)) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
+    }
+    if (a.y) {
+        for (int c = threadIdx.x; c < padded; c += THREADS) {
+            const bool in = c < a.cols;
+            params[c] = !in ? 0.0f : a.gamma ? load_param(a.gamma, a.params_bf16, c) : 1.0f;
+            params[padded + c] = in && a.beta ? load_param(a.beta, a.params_bf16, c) : 0.0f;
+        }
+        __syncthreads();
+    }
     int turn = 0;
-    // rows beyond the last keep the warp together: they are read as zeros and not written
-    for (; row - threadIdx.x / TPR < a.rows; row += step) {
-        const bool live = row < a.rows;
+    // rows beyond the last keep the warp together: what they compute is not written
+    for (int first = (int)blockIdx.x * GROUPS; first < a.rows; first += step, row += step) {
         float v[E], sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
-            if (live && j * TPR * U < cols) {
-                if constexpr (VEC)
-                    Unit<T>::widen(raw[j], v + j * U);
-                else
-                    v[j] = widen1<T>(raw[j]);
-                if constexpr (RAGGED) {
+            if constexpr (VEC)
+                Unit<T>::widen(raw[j], v + j * U);
+            else
+                v[j] = j * TPR < cols ? widen1<T>(raw[j]) : 0.0f;
+            if constexpr (MODE == ROWS_RAGGED) {
+                if (j >= SURE) {
 #pragma unroll
                     for (int i = 1; i < U; ++i)
                         if (j * TPR * U + i >= cols) v[j * U + i] = 0.0f;
                 }
-#pragma unroll
-                for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] += v[j * U + i];
             }
+#pragma unroll
+            for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] += v[j * U + i];
         }
         x += step * a.x_stride;
+        if (row + step < a.rows) {
 #pragma unroll
-        for (int j = 0; j < UNITS; ++j)
-            if (row + step < a.rows && j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
+            for (int j = 0; j < UNITS; ++j)
+                if (j < SURE || j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
+        }
         // divided: the mean of equal values is that value
         const float mean = row_sum<TPR>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared[turn]) / (float)a.cols;
         sums[0] = sums[1] = sums[2] = sums[3] = 0.0f;
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
-            if (live && j * TPR * U < cols) {
 #pragma unroll
-                for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
-                if constexpr (RAGGED) {
+            for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
+            if (j >= SURE) {  // what lies outside does not count
 #pragma unroll
-                    for (int i = 1; i < U; ++i)
-                        if (j * TPR * U + i >= cols) v[j * U + i] = 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] = fmaf(v[j * U + i], v[j * U + i], sums[(j * U + i) & 3]);
+                for (int i = 0; i < U; ++i)
+                    if (j * TPR * U + (MODE == ROWS_RAGGED ? i : 0) >= cols) v[j * U + i] = 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] = fmaf(v[j * U + i], v[j * U + i], sums[(j * U + i) & 3]);
         }
         const float square = row_sum<TPR>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared[turn + 1]);
         const float rstd = inverse_root(__fmul_rn(square, a.inv_cols), a.eps);
         turn ^= 2;
-        if (live && lane == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
-        if (a.y && live) {
+        if (row < a.rows) {
+            if (lane == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
+            if (a.y) {
+                const float *gamma = params + lane * U, *beta = gamma + padded;
 #pragma unroll
-            for (int j = 0; j < UNITS; ++j) {
-                if (j * TPR * U >= cols) continue;
-                const int c = (j * TPR + lane) * U;
-                float *r = v + j * U;
+                for (int j = 0; j < UNITS; ++j) {
+                    if (j >= SURE && j * TPR * U >= cols) continue;
+                    float *r = v + j * U;
+                    if constexpr (VEC) {
 #pragma unroll
-                for (int i = 0; i < U; ++i) r[i] *= rstd;
-                if constexpr (VEC) {
-                    float p[U];
-                    if (a.gamma) {
-                        load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, a.cols, p);
-#pragma unroll
-                        for (int i = 0; i < U; ++i) r[i] *= p[i];
-                    }
-                    if (a.beta) {
-                        load_params<U>(a.beta, a.params_bf16, a.beta_aligned, c, a.cols, p);
-#pragma unroll
-                        for (int i = 0; i < U; ++i) r[i] += p[i];
-                    }
-                    if (!RAGGED || c + U <= a.cols) {
-                        *reinterpret_cast<uint4 *>(y + j * TPR * U) = Unit<T>::narrow(r);
+                        for (int i = 0; i < U; i += 4) {
+                            const float4 g = *reinterpret_cast<const float4 *>(gamma + j * TPR * U + i);
+                            const float4 b = *reinterpret_cast<const float4 *>(beta + j * TPR * U + i);
+                            r[i] = fmaf(r[i] * rstd, g.x, b.x);
+                            r[i + 1] = fmaf(r[i + 1] * rstd, g.y, b.y);
+                            r[i + 2] = fmaf(r[i + 2] * rstd, g.z, b.z);
+                            r[i + 3] = fmaf(r[i + 3] * rstd, g.w, b.w);
+                        }
+                        const uint4 out = Unit<T>::narrow(r);
+                        if (MODE != ROWS_RAGGED || j < SURE || j * TPR * U + U <= cols)
+                            *reinterpret_cast<uint4 *>(y + j * TPR * U) = out;
+                        else
+                            store_first(y + j * TPR * U, out, cols - j * TPR * U);
                     } else {
-#pragma unroll
-                        for (int i = 0; i < U; ++i)
-                            if (c + i < a.cols) y[j * TPR * U + i] = narrow1<T>(r[i]);
+                        y[j * TPR] = narrow1<T>(fmaf(r[0] * rstd, gamma[j * TPR], beta[j * TPR]));
                     }
-                } else {
-                    if (a.gamma) r[0] *= load_param(a.gamma, a.params_bf16, c);
-                    if (a.beta) r[0] += load_param(a.beta, a.params_bf16, c);
-                    y[j * TPR * U] = narrow1<T>(r[0]);
                 }
             }
         }
@@ -200,30 +219,42 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
     }
 }
 
-template <typename T, bool VEC, bool RAGGED>
-void launch_norm(const NormArgs &a, cudaStream_t stream)
+template <typename T, int MODE, int TPR, int NU, int PART>
+int launch_norm_shape(const NormArgs &a, cudaStream_t stream)
+{
+    constexpr int threads = TPR < 128 ? 128 : TPR;
+    const int64_t full = 148 * (threads > 128 ? 1 : NU > 4 ? 4 : 6);
+    const unsigned grid = (unsigned)std::min<int64_t>(full, ceil_div(a.rows, threads / TPR));
+    const int smem = a.y ? 2 * (int)ceil_div(a.cols, 8) * 8 * (int)sizeof(float) : 0;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(norm_rows_kernel<T, MODE, TPR, NU, PART>,
+                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+        return launch_status();
+    norm_rows_kernel<T, MODE, TPR, NU, PART><<<grid, threads, smem, stream>>>(a);
+    return launch_status();
+}
+
+// Up to 2048 values in bf16 the units are dealt out so that only a thread's last can lie outside.
+template <typename T, int MODE> int launch_norm(const NormArgs &a, cudaStream_t stream)
 {
     const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
-#define NORM_CASE(TPR, NU)                                                                                         \
-    if (units <= TPR * NU) {                                                                                       \
-        constexpr int threads = TPR < 128 ? 128 : TPR;                                                             \
-        const int64_t full = 148 * (threads > 128 ? 1 : NU == 8 ? 4 : 6);                                          \
-        const unsigned grid = (unsigned)std::min<int64_t>(full, ceil_div(a.rows, threads / TPR));                  \
-        norm_rows_kernel<T, VEC, RAGGED, TPR, NU><<<grid, threads, 0, stream>>>(a);                                        \
-        return;                                                                                                    \
+    if (units <= 8) return launch_norm_shape<T, MODE, 8, 1, 1>(a, stream);
+    if (units <= 16) return launch_norm_shape<T, MODE, 16, 1, 1>(a, stream);
+    switch (ceil_div(units, 32)) {
+    case 1: return launch_norm_shape<T, MODE, 32, 1, 1>(a, stream);
+    case 2: return launch_norm_shape<T, MODE, 32, 2, 1>(a, stream);
+    case 3: return launch_norm_shape<T, MODE, 32, 3, 1>(a, stream);
+    case 4: return launch_norm_shape<T, MODE, 32, 4, 1>(a, stream);
+    case 5: return launch_norm_shape<T, MODE, 32, 5, 1>(a, stream);
+    case 6: return launch_norm_shape<T, MODE, 32, 6, 1>(a, stream);
+    case 7: return launch_norm_shape<T, MODE, 32, 7, 1>(a, stream);
+    case 8: return launch_norm_shape<T, MODE, 32, 8, 1>(a, stream);
     }
-    NORM_CASE(8, 1)
-    NORM_CASE(16, 1)
-    NORM_CASE(32, 1)
-    NORM_CASE(32, 2)
-    NORM_CASE(32, 4)
-    NORM_CASE(32, 8)
-    NORM_CASE(128, 4)
-    NORM_CASE(128, 8)
-    NORM_CASE(256, 8)
-    NORM_CASE(512, 8)
-#undef NORM_CASE
+    if (units <= 128 * 4) return launch_norm_shape<T, MODE, 128, 4, 2>(a, stream);
+    if (units <= 128 * 8) return launch_norm_shape<T, MODE, 128, 8, 4>(a, stream);
+    if (units <= 256 * 8) return launch_norm_shape<T, MODE, 256, 8, 4>(a, stream);
+    if (a.cols <= NORM_WIDEST) return launch_norm_shape<T, MODE, 512, 8, 4>(a, stream);
     norm_long_rows_kernel<T><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
+    return launch_status();
 }
 
 // ------------------------------------------------------------------------------------------ backward
@@ -251,49 +282,40 @@ static __device__ int g_norm_error;  // set by a bounded wait that ran out
 constexpr int BACK_MAX_STAGES = 4;
 
 // How the threads of a block share rows: TPR threads for a row, each with two units of 16 bytes of it (or 16
-// single values), GROUPS times ROWS rows at a time.
+// single values), ROWS rows at a time.  SYNC threads go together; the block's others go their own way.
 template <typename T, bool PACKED, bool VEC, int TPR> struct BackShape {
     static constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
     static constexpr int E = VEC ? 2 * U : 16;
     static constexpr int UNITS = E / U;
     static constexpr int ROWS = VEC && TPR <= 256 ? 2 : 1;
-    static constexpr int THREADS = TPR < 128 ? 128 : TPR;
+    static constexpr int THREADS = TPR < 512 ? 512 : TPR;
     static constexpr int GROUPS = THREADS / TPR;
+    static constexpr int SYNC = TPR < 32 ? 32 : TPR;  // threads that take rows together: whole warps
+    static constexpr int SYNCS = THREADS / SYNC;
+    static constexpr int TAKEN = SYNC / TPR * ROWS;   // rows at a time
     using Raw = typename std::conditional<VEC, uint4, T>::type;
     using X = typename std::conditional<PACKED, uint8_t, T>::type;
     using RawX = typename std::conditional<!PACKED, Raw, typename std::conditional<!VEC, uint8_t,
                  typename std::conditional<U == 8, uint2, unsigned>::type>::type>::type;
 
-    static __device__ __forceinline__ void widen(const Raw &raw, float *f)
+    // x - mean of a unit, or of two single values.
+    static __device__ __forceinline__ void centred(const RawX *x, float scale, float scale1, float mean, f32x2 *h)
     {
-        if constexpr (VEC)
-            Unit<T>::widen(raw, f);
-        else
-            f[0] = widen1<T>(raw);
-    }
-    // h of a unit of x.
-    static __device__ __forceinline__ void normalised(const RawX &x, float scale, float mean, float rstd, float *h)
-    {
-        if constexpr (PACKED) {
-            if constexpr (!VEC) {
-                h[0] = fmaf(decode2(x).x, scale, -mean);  // a code times its scale is exact
-            } else {
-                unsigned w[U / 4];
-                memcpy(w, &x, sizeof(w));
+        const f32x2 minus = pair_of(-mean);
+        if constexpr (PACKED && VEC) {  // a code times its scale is exact
+            unsigned w[U / 4];
+            memcpy(w, x, sizeof(w));
 #pragma unroll
-                for (int i = 0; i < U; i += 2) {
-                    const float2 p = decode2(w[i / 4] >> (8 * (i % 4)) & 0xffffu);
-                    h[i] = fmaf(p.x, scale, -mean);
-                    h[i + 1] = fmaf(p.y, scale, -mean);
-                }
-            }
+            for (int i = 0; i < U / 2; ++i) h[i] = fma2(decode_pair(w[i / 2] >> (16 * (i & 1))), pair_of(scale), minus);
+        } else if constexpr (PACKED) {
+            h[0] = fma2(pair_of(decode2(x[0]).x, decode2(x[1]).x), pair_of(scale, scale1), minus);
+        } else if constexpr (VEC) {
+            widen_pairs<T>(*x, h);
+#pragma unroll
+            for (int i = 0; i < U / 2; ++i) h[i] = add2(h[i], minus);
         } else {
-            widen(x, h);
-#pragma unroll
-            for (int i = 0; i < U; ++i) h[i] -= mean;
+            h[0] = add2(pair_of(widen1<T>(x[0]), widen1<T>(x[1])), minus);
         }
-#pragma unroll
-        for (int i = 0; i < U; ++i) h[i] *= rstd;
     }
 };
 
@@ -317,136 +339,168 @@ __device__ __forceinline__ float warp_sum4(const float *v)
 // steps ahead: a thread has no registers to spare for them.  A last, partial unit of a row is copied by
 // itself and filled up with zeros, which take no part in any sum.
 template <typename T, bool PACKED, bool VEC, int TPR>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 128 ? 4 : TPR == 256 ? 2 : 1)
+__global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
     norm_back_kernel(const __grid_constant__ NormBackArgs a, int stages, int dy_bytes, int x_bytes)
 {
     using S = BackShape<T, PACKED, VEC, TPR>;
     constexpr int E = S::E, U = S::U, UNITS = S::UNITS, ROWS = S::ROWS, THREADS = S::THREADS, GROUPS = S::GROUPS;
     constexpr int WARPS = TPR / 32;
+    constexpr int PAIRS = VEC ? U / 2 : 1, SINGLE = VEC ? 1 : 2;  // of a unit; single values that make a pair
     extern __shared__ uint8_t raw_ring[];
-    __shared__ uint64_t full[BACK_MAX_STAGES];
+    __shared__ uint64_t bars[S::SYNCS][BACK_MAX_STAGES];
     __shared__ float4 shared[2][THREADS / 32];
     __shared__ float columns[GROUPS > 1 ? 2 * TPR * E : 1];
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int sync = threadIdx.x / S::SYNC, in_sync = threadIdx.x % S::SYNC;
+    uint64_t *full = bars[sync];
     const int column = lane * U, cols = a.cols - column;
     const float inv_cols = 1.0f / (float)a.cols;
-    uint8_t *ring = raw_ring + ((128u - (ptx::smem_addr(raw_ring) & 127u)) & 127u);
-    const int row_bytes = dy_bytes + x_bytes, stage_bytes = GROUPS * ROWS * row_bytes;
+    const int row_bytes = dy_bytes + x_bytes, stage_bytes = S::TAKEN * row_bytes;
+    uint8_t *ring = raw_ring + ((128u - (ptx::smem_addr(raw_ring) & 127u)) & 127u) + sync * stages * stage_bytes;
     const int dy_tail = a.cols * (int)sizeof(T) & 15, x_tail = a.cols * (int)sizeof(typename S::X) & 15;
     const int dy_whole = dy_bytes - (dy_tail ? 16 : 0), x_whole = x_bytes - (x_tail ? 16 : 0);
 
-    const long long step = (long long)gridDim.x * GROUPS * ROWS;
-    const long long block_row = (long long)blockIdx.x * GROUPS * ROWS;
+    const int step = (int)gridDim.x * S::SYNCS * S::TAKEN, begin = ((int)blockIdx.x * S::SYNCS + sync) * S::TAKEN;
     // one thread: the rows from `first` on into a stage
-    const auto request = [&](long long first, int stage) {
-        const int rows = (int)min((long long)(GROUPS * ROWS), a.rows - first);
+    const auto request = [&](int first, int stage) {
+        const int rows = min(S::TAKEN, a.rows - first);
         ptx::mbar_arrive_expect_tx(&full[stage], rows * (dy_whole + x_whole));
         uint8_t *to = ring + stage * stage_bytes;
-        for (int r = 0; r < rows; ++r, to += row_bytes) {
-            const uint8_t *dy = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.dy) + (first + r) * a.dy_stride);
-            const uint8_t *x = reinterpret_cast<const uint8_t *>(static_cast<const typename S::X *>(a.x) + (first + r) * a.x_stride);
+        const uint8_t *dy = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.dy) + first * a.dy_stride);
+        const uint8_t *x = reinterpret_cast<const uint8_t *>(static_cast<const typename S::X *>(a.x) + first * a.x_stride);
+        for (int r = 0; r < rows; ++r) {
             if (dy_whole) ptx::bulk_load(to, dy, dy_whole, &full[stage]);
             if (x_whole) ptx::bulk_load(to + dy_bytes, x, x_whole, &full[stage]);
             if (dy_tail) copy_filled(to + dy_whole, dy + dy_whole, dy_tail);
             if (x_tail) copy_filled(to + dy_bytes + x_whole, x + x_whole, x_tail);
+            to += row_bytes;
+            dy += a.dy_stride * (long long)sizeof(T);
+            x += a.x_stride * (long long)sizeof(typename S::X);
         }
         if (dy_tail || x_tail)  // arrives when this thread's own copies have landed
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(ptx::smem_addr(&full[stage])) : "memory");
     };
     if constexpr (VEC) {
-        if (threadIdx.x == 0) {
+        if (in_sync == 0) {
             for (int s = 0; s < stages; ++s) ptx::mbar_init(&full[s], dy_tail || x_tail ? 2 : 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
-        if (threadIdx.x == 0)
+        if (in_sync == 0)
             for (int s = 0; s < stages; ++s)
-                if (block_row + s * step < a.rows) request(block_row + s * step, s);
+                if (begin + s * (long long)step < a.rows) request(begin + s * step, s);
     }
 
-    float gamma[E], sum_g[E], sum_b[E];
+    f32x2 gamma[E / 2], sum_g[E / 2], sum_b[E / 2];
 #pragma unroll
-    for (int j = 0; j < UNITS; ++j) {
-        const int c = column + j * TPR * U;
+    for (int e = 0; e < E / 2; ++e) {
+        sum_g[e] = sum_b[e] = 0ull;
+        gamma[e] = pair_of(1.0f);
+    }
+    if (a.gamma) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            sum_g[j * U + i] = sum_b[j * U + i] = 0.0f;
-            gamma[j * U + i] = 1.0f;
-        }
-        if (a.gamma && c < a.cols) {
-            if constexpr (VEC)
-                load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, a.cols, gamma + j * U);
-            else
-                gamma[j] = load_param(a.gamma, a.params_bf16, c);
+        for (int j = 0; j < UNITS; j += SINGLE) {
+            const int c = column + j * TPR * U;
+            if constexpr (VEC) {
+                if (c < a.cols) param_pairs<U>(a.gamma, a.params_bf16, a.gamma_aligned, c, a.cols, gamma + j * PAIRS);
+            } else {
+                gamma[j / 2] = pair_of(c < a.cols ? load_param(a.gamma, a.params_bf16, c) : 0.0f,
+                                       c + TPR < a.cols ? load_param(a.gamma, a.params_bf16, c + TPR) : 0.0f);
+            }
         }
     }
 
-    // of the next rows
+    int row = begin + in_sync / TPR * ROWS;
+    // of the next rows; two rows that are taken together lie in one row of scales
     float mean_ahead[ROWS], rstd_ahead[ROWS];
-    uint8_t scale_ahead[PACKED ? ROWS : 1][UNITS];
-    const auto look_ahead = [&](long long row) {
+    uint8_t scale_ahead[PACKED ? UNITS : 1];
+    const auto look_ahead = [&](int row) {
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
             if (row + k < a.rows) {
                 mean_ahead[k] = a.mean[row + k];
                 rstd_ahead[k] = a.rstd[row + k];
-                if constexpr (PACKED) {
-                    const uint8_t *scales = a.scales + (row + k) / PACK_BLOCK * a.scale_cols;
-#pragma unroll
-                    for (int j = 0; j < UNITS; ++j)
-                        if (j * TPR * U < cols) scale_ahead[k][j] = scales[(column + j * TPR * U) / PACK_BLOCK];
-                }
             }
         }
+        if (PACKED && row < a.rows) {
+            const uint8_t *scales = a.scales + (long long)(row / PACK_BLOCK) * a.scale_cols + column / PACK_BLOCK;
+#pragma unroll
+            for (int j = 0; j < UNITS; ++j)
+                if (j * TPR * U < cols)
+                    scale_ahead[PACKED ? j : 0] = TPR * U % PACK_BLOCK == 0 ? scales[j * (TPR * U / PACK_BLOCK)]
+                                                                          : scales[(column + j * TPR * U) / PACK_BLOCK - column / PACK_BLOCK];
+        }
     };
-    long long row = block_row + group * ROWS;
     look_ahead(row);
+    T *dx = static_cast<T *>(a.dx) + row * a.dx_stride + column;
+    const T *dy_row = static_cast<const T *>(a.dy) + row * a.dy_stride + column;
+    const typename S::X *x_row = static_cast<const typename S::X *>(a.x) + row * a.x_stride + column;
     int parity = 0, stage = 0;
     unsigned phase = 0;
-    for (long long first = block_row; first < a.rows; first += step, row += step) {
+    for (int first = begin; first < a.rows; first += step, row += step) {
         if constexpr (VEC) {
             if (!bounded_wait(&full[stage], phase, &g_norm_error, 1)) {
                 for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
                 return;
             }
         }
-        const uint8_t *mine = ring + stage * stage_bytes + group * ROWS * row_bytes;
-        float hat[ROWS][E];
-        typename S::Raw kept[VEC ? 1 : UNITS];  // of dy, where it is not in shared memory
-        float rstd[ROWS], sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // of g and g h, of either row
+        const uint8_t *mine = ring + stage * stage_bytes + in_sync / TPR * ROWS * row_bytes;
+        f32x2 hat[ROWS][E / 2];
+        f32x2 kept[VEC ? 1 : E / 2];  // dy, where it is not in shared memory
+        T dy1[VEC ? 1 : UNITS];
+        typename S::X x1[VEC ? 1 : UNITS];
+        if constexpr (!VEC) {  // all loads at once; beyond the row its first value of this thread
+            if (row < a.rows) {
+#pragma unroll
+                for (int j = 0; j < UNITS; ++j) {
+                    const int c = j * TPR < cols ? j * TPR : 0;
+                    if (cols > 0) {
+                        dy1[j] = dy_row[c];
+                        x1[j] = x_row[c];
+                    }
+                }
+            }
+        }
+        f32x2 sum2[4] = {0ull, 0ull, 0ull, 0ull};  // of g and g h, of either row
+        float rstd[ROWS];
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
             rstd[k] = rstd_ahead[k];
             if (row + k < a.rows) {
 #pragma unroll
-                for (int j = 0; j < UNITS; ++j) {
+                for (int j = 0; j < UNITS; j += SINGLE) {
                     const int c = j * TPR * U;
                     if (c < cols) {
-                        typename S::Raw dy;
-                        typename S::RawX x;
+                        f32x2 dy[PAIRS], *h = hat[k] + j * PAIRS / SINGLE;
                         if constexpr (VEC) {
-                            dy = reinterpret_cast<const typename S::Raw *>(mine + k * row_bytes)[lane + j * TPR];
-                            x = reinterpret_cast<const typename S::RawX *>(mine + k * row_bytes + dy_bytes)[lane + j * TPR];
+                            const uint8_t *at = mine + k * row_bytes;
+                            widen_pairs<T>(reinterpret_cast<const uint4 *>(at)[lane + j * TPR], dy);
+                            const typename S::RawX x = reinterpret_cast<const typename S::RawX *>(at + dy_bytes)[lane + j * TPR];
+                            S::centred(&x, PACKED ? scale_value(scale_ahead[PACKED ? j : 0]) : 0.0f, 0.0f, mean_ahead[k], h);
                         } else {
-                            dy = kept[j] = static_cast<const T *>(a.dy)[(row + k) * a.dy_stride + column + c];
-                            x = static_cast<const typename S::X *>(a.x)[(row + k) * a.x_stride + column + c];
+                            const bool both = c + TPR < cols;  // the second value is inside too
+                            dy[0] = kept[j / 2] = pair_of(widen1<T>(dy1[j]), both ? widen1<T>(dy1[j + 1]) : 0.0f);
+                            S::centred(reinterpret_cast<const typename S::RawX *>(x1 + j),
+                                       PACKED ? scale_value(scale_ahead[PACKED ? j : 0]) : 0.0f,
+                                       PACKED ? scale_value(scale_ahead[PACKED ? (both ? j + 1 : j) : 0]) : 0.0f, mean_ahead[k], h);
                         }
-                        float g[U], *h = hat[k] + j * U;
-                        S::widen(dy, g);
-                        S::normalised(x, PACKED ? scale_value(scale_ahead[PACKED ? k : 0][j]) : 0.0f, mean_ahead[k], rstd[k], h);
 #pragma unroll
-                        for (int i = 0; i < U; ++i) {
-                            const int e = j * U + i;
-                            const float p = g[i] * h[i];
-                            sum_g[e] += p;
-                            sum_b[e] += g[i];
-                            sums[2 * k] = fmaf(g[i], gamma[e], sums[2 * k]);
-                            sums[2 * k + 1] = fmaf(p, gamma[e], sums[2 * k + 1]);
+                        for (int i = 0; i < PAIRS; ++i) {
+                            const int e = j * PAIRS / SINGLE + i;
+                            h[i] = mul2(h[i], pair_of(rstd[k]));
+                            const f32x2 p = mul2(dy[i], h[i]);
+                            sum_g[e] = add2(sum_g[e], p);
+                            sum_b[e] = add2(sum_b[e], dy[i]);
+                            sum2[2 * k] = fma2(dy[i], gamma[e], sum2[2 * k]);
+                            sum2[2 * k + 1] = fma2(p, gamma[e], sum2[2 * k + 1]);
                         }
                     }
                 }
             }
         }
+        float sums[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[i] = sum_of(sum2[i]);
         look_ahead(row + step);
         if constexpr (TPR < 32) {
 #pragma unroll
@@ -465,7 +519,12 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 128 ? 4 : TPR ==
         }
         // Behind this barrier every thread is done with the rows before these: their stage is free, and so
         // are the slots of `shared` that the next rows use.
-        if constexpr (VEC || TPR > 32) __syncthreads();
+        if constexpr (TPR <= 32)
+            __syncwarp();
+        else if constexpr (GROUPS == 1)
+            __syncthreads();
+        else
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + sync), "n"(S::SYNC) : "memory");
         if constexpr (TPR > 32) {
             sums[0] = sums[1] = sums[2] = sums[3] = 0.0f;
 #pragma unroll
@@ -476,54 +535,62 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 128 ? 4 : TPR ==
             parity ^= 1;
         }
         if constexpr (VEC) {
-            const long long next = first + (stages - 1) * step;
-            if (threadIdx.x == 0 && first != block_row && next < a.rows) request(next, stage == 0 ? stages - 1 : stage - 1);
+            const long long next = first + (stages - 1) * (long long)step;
+            if (in_sync == 0 && first != begin && next < a.rows) request((int)next, stage == 0 ? stages - 1 : stage - 1);
         }
         if (a.dx) {
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
                 if (row + k >= a.rows) continue;
-                const float g1 = sums[2 * k] * inv_cols, g2 = sums[2 * k + 1] * inv_cols;
-                T *out = static_cast<T *>(a.dx) + (row + k) * a.dx_stride + column;
+                const f32x2 g1 = pair_of(-sums[2 * k] * inv_cols), g2 = pair_of(-sums[2 * k + 1] * inv_cols);
+                T *out = dx + k * a.dx_stride;
 #pragma unroll
-                for (int j = 0; j < UNITS; ++j) {
+                for (int j = 0; j < UNITS; j += SINGLE) {
                     const int c = j * TPR * U;
                     if (c >= cols) continue;
-                    float r[U];
+                    f32x2 r[PAIRS];
                     if constexpr (VEC)
-                        S::widen(reinterpret_cast<const typename S::Raw *>(mine + k * row_bytes)[lane + j * TPR], r);
+                        widen_pairs<T>(reinterpret_cast<const uint4 *>(mine + k * row_bytes)[lane + j * TPR], r);
                     else
-                        S::widen(kept[j], r);
+                        r[0] = kept[j / 2];
 #pragma unroll
-                    for (int i = 0; i < U; ++i)
-                        r[i] = fmaf(-hat[k][j * U + i], g2, fmaf(r[i], gamma[j * U + i], -g1)) * rstd[k];
+                    for (int i = 0; i < PAIRS; ++i) {
+                        const int e = j * PAIRS / SINGLE + i;
+                        r[i] = mul2(fma2(hat[k][e], g2, fma2(r[i], gamma[e], g1)), pair_of(rstd[k]));
+                    }
                     if constexpr (VEC) {
-                        if (c + U <= cols) {
-                            *reinterpret_cast<uint4 *>(out + c) = Unit<T>::narrow(r);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < U; ++i)
-                                if (c + i < cols) out[c + i] = narrow1<T>(r[i]);
-                        }
+                        const uint4 unit = narrow_pairs<T>(r);
+                        if (c + U <= cols)
+                            *reinterpret_cast<uint4 *>(out + c) = unit;
+                        else
+                            store_first(out + c, unit, cols - c);
                     } else {
-                        out[c] = narrow1<T>(r[0]);
+                        const float2 v = values_of(r[0]);
+                        out[c] = narrow1<T>(v.x);
+                        if (c + TPR < cols) out[c + TPR] = narrow1<T>(v.y);
                     }
                 }
             }
         }
+        dx += step * a.dx_stride;
+        dy_row += step * a.dy_stride;
+        x_row += step * a.x_stride;
         if (++stage == stages) { stage = 0; phase ^= 1; }
     }
 
     if (!a.dgamma && !a.dbeta) return;
+    // the column of value e of this thread
+    const auto column_of = [&](int e) { return VEC ? (e / U * TPR + lane) * U + e % U : e * TPR + lane; };
     if constexpr (GROUPS > 1) {  // the block's groups in ascending order
         for (int g = 0; g < GROUPS; ++g) {
             __syncthreads();
             if (group == g) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const int at = (e / U * TPR + lane) * U + e % U;
-                    columns[at] = (g ? columns[at] : 0.0f) + sum_g[e];
-                    columns[TPR * E + at] = (g ? columns[TPR * E + at] : 0.0f) + sum_b[e];
+                    const int at = column_of(e);
+                    const float2 vg = values_of(sum_g[e / 2]), vb = values_of(sum_b[e / 2]);
+                    columns[at] = (g ? columns[at] : 0.0f) + (e & 1 ? vg.y : vg.x);
+                    columns[TPR * E + at] = (g ? columns[TPR * E + at] : 0.0f) + (e & 1 ? vb.y : vb.x);
                 }
             }
         }
@@ -535,10 +602,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR <= 128 ? 4 : TPR ==
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int c = (e / U * TPR + lane) * U + e % U;
+            const int c = column_of(e);
+            const float2 vg = values_of(sum_g[e / 2]), vb = values_of(sum_b[e / 2]);
             if (c < a.cols) {
-                if (a.dgamma) a.dgamma[blockIdx.x * a.part_stride + c] = sum_g[e];
-                if (a.dbeta) a.dbeta[blockIdx.x * a.part_stride + c] = sum_b[e];
+                if (a.dgamma) a.dgamma[blockIdx.x * a.part_stride + c] = e & 1 ? vg.y : vg.x;
+                if (a.dbeta) a.dbeta[blockIdx.x * a.part_stride + c] = e & 1 ? vb.y : vb.x;
             }
         }
     }
@@ -617,7 +685,6 @@ __global__ void __launch_bounds__(1024) norm_back_join_kernel(const float *parts
     if (tx == 0 && at < cols) out[at] = sum;
 }
 
-constexpr int BACK_THREADS = 512;      // of the row kernel on an SM
 constexpr int BACK_LONG_SHARES = 32;
 
 // The widest row that a block holds, and the threads for a row: two units of 16 bytes each, or 16 values.
@@ -633,9 +700,8 @@ int back_threads_per_row(int64_t cols, int dtype, bool vec)
 int64_t back_parts(int64_t rows, int64_t cols, int dtype, bool vec)
 {
     if (cols > back_widest(dtype)) return std::min<int64_t>(BACK_LONG_SHARES, ceil_div(rows, 64));
-    const int tpr = back_threads_per_row(cols, dtype, vec), threads = std::max(tpr, 128);
-    const int64_t full = 148 * std::max(1, BACK_THREADS / threads);
-    return std::min(full, ceil_div(rows, threads / tpr * (vec ? 2 : 1)));
+    const int tpr = back_threads_per_row(cols, dtype, vec), rows_at_once = vec && tpr <= 256 ? 2 : 1;
+    return std::min<int64_t>(148, ceil_div(rows, std::max(tpr, 512) / tpr * rows_at_once));
 }
 
 template <typename T, bool PACKED, bool VEC, int TPR>
@@ -646,9 +712,8 @@ int launch_back_shape(const NormBackArgs &a, int blocks, cudaStream_t stream)
     if (VEC) {
         dy_bytes = (int)ceil_div(a.cols * (int)sizeof(T), 16) * 16;
         x_bytes = (int)ceil_div(a.cols * (int)sizeof(typename S::X), 16) * 16;
-        const int stage = S::GROUPS * S::ROWS * (dy_bytes + x_bytes);
-        const int resident = std::max(1, BACK_THREADS / S::THREADS);
-        stages = std::max(2, std::min(BACK_MAX_STAGES, 176 * 1024 / resident / stage));
+        const int stage = S::SYNCS * S::TAKEN * (dy_bytes + x_bytes);
+        stages = std::max(2, std::min(BACK_MAX_STAGES, 192 * 1024 / stage));
         smem = stages * stage + 128;
         if (cudaFuncSetAttribute(norm_back_kernel<T, PACKED, VEC, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
             cudaSuccess)
@@ -713,16 +778,14 @@ int dipaco_layer_norm(const void *x, int64_t x_stride, const void *gamma, const 
                   param_dtype == DIPACO_BF16, (uintptr_t)gamma % 16 == 0, (uintptr_t)beta % 16 == 0};
     const int size = dense_size(dtype);
     const bool vec = rows_aligned16(x, x_stride, rows, size) && (!y || rows_aligned16(y, y_stride, rows, size));
-    const bool ragged = cols * size % 16 != 0;
+    const int mode = !vec ? ROWS_SINGLE : cols * size % 16 ? ROWS_RAGGED : ROWS_UNITS;
     if (dtype == DIPACO_BF16)
-        !vec     ? launch_norm<__nv_bfloat16, false, false>(a, stream)
-        : ragged ? launch_norm<__nv_bfloat16, true, true>(a, stream)
-                 : launch_norm<__nv_bfloat16, true, false>(a, stream);
-    else
-        !vec     ? launch_norm<float, false, false>(a, stream)
-        : ragged ? launch_norm<float, true, true>(a, stream)
-                 : launch_norm<float, true, false>(a, stream);
-    return launch_status();
+        return mode == ROWS_SINGLE  ? launch_norm<__nv_bfloat16, ROWS_SINGLE>(a, stream)
+               : mode == ROWS_UNITS ? launch_norm<__nv_bfloat16, ROWS_UNITS>(a, stream)
+                                    : launch_norm<__nv_bfloat16, ROWS_RAGGED>(a, stream);
+    return mode == ROWS_SINGLE  ? launch_norm<float, ROWS_SINGLE>(a, stream)
+           : mode == ROWS_UNITS ? launch_norm<float, ROWS_UNITS>(a, stream)
+                                : launch_norm<float, ROWS_RAGGED>(a, stream);
 }
 
 int dipaco_layer_norm_workspace(int64_t rows, int64_t cols, int64_t *bytes)

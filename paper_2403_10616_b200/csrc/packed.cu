@@ -78,20 +78,34 @@ struct PackedOut {
 // as the bits of an fp32 value.
 __device__ __forceinline__ unsigned larger_bf16x2(unsigned magnitudes, unsigned w)
 {
-    w &= 0x7fff7fffu;
-    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&magnitudes),
-                                     *reinterpret_cast<const __nv_bfloat162 *>(&w));
-    return *reinterpret_cast<const unsigned *>(&m);
+    asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(magnitudes) : "r"(w));  // the sign is not used
+    return magnitudes;
 }
 __device__ __forceinline__ unsigned wider_bf16x2(unsigned magnitudes)
 {
+    magnitudes &= 0x7fff7fffu;
     return max(magnitudes << 16, magnitudes & 0xffff0000u);
+}
+
+__device__ __forceinline__ float larger(float magnitude, f32x2 p)  // NaN does not count
+{
+    const float2 v = values_of(p);
+    asm("max.abs.f32 %0, %0, %1, %2;" : "+f"(magnitude) : "f"(v.x), "f"(v.y));
+    return magnitude;
 }
 
 // The thread's values of one matrix: as they were loaded, or computed in fp32.
 template <typename T> struct LoadedValues {
     const uint4 *raw;
-    __device__ __forceinline__ void unit(int j, float *f) const { Unit<T>::widen(raw[j], f); }
+    __device__ __forceinline__ void unit(int j, f32x2 *p) const { widen_pairs<T>(raw[j], p); }
+    __device__ __forceinline__ void unit_at(int j, f32x2 *p) const  // j not known when compiling
+    {
+        uint4 r = raw[0];
+#pragma unroll
+        for (int k = 1; k < Layout<T>::UNITS; ++k)
+            if (j == k) r = raw[k];
+        widen_pairs<T>(r, p);
+    }
     // Bits of the largest magnitude; at least those of infinity if there is an infinity.
     __device__ __forceinline__ unsigned largest() const
     {
@@ -111,26 +125,42 @@ template <typename T> struct LoadedValues {
     }
 };
 template <typename T> struct ComputedValues {
-    const float *v;
-    __device__ __forceinline__ void unit(int j, float *f) const
+    const f32x2 *v;
+    __device__ __forceinline__ void unit(int j, f32x2 *p) const
     {
 #pragma unroll
-        for (int i = 0; i < Layout<T>::U; ++i) f[i] = v[j * Layout<T>::U + i];
+        for (int i = 0; i < Layout<T>::U / 2; ++i) p[i] = v[j * Layout<T>::U / 2 + i];
+    }
+    __device__ __forceinline__ void unit_at(int j, f32x2 *p) const
+    {
+        unit(0, p);
+#pragma unroll
+        for (int k = 1; k < Layout<T>::UNITS; ++k)
+            if (j == k) unit(k, p);
     }
     __device__ __forceinline__ unsigned largest() const  // of the values that are not NaN
     {
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < VALUES; ++i) m = fmaxf(m, fabsf(v[i]));
+        for (int i = 0; i < VALUES / 2; ++i) m = larger(m, v[i]);
         return __float_as_uint(m);
     }
 };
 
-template <int U, bool SPECIAL> __device__ __forceinline__ void store_codes(uint8_t *p, int n, const float *f, float reciprocal)
+template <int U, bool SPECIAL>
+__device__ __forceinline__ void store_codes(uint8_t *p, int n, const f32x2 *v, float reciprocal)
 {
     unsigned w[U / 4];
 #pragma unroll
-    for (int i = 0; i < U / 4; ++i) w[i] = SPECIAL ? encode4(f + 4 * i, reciprocal) : encode4_finite(f + 4 * i, reciprocal);
+    for (int i = 0; i < U / 4; ++i) {
+        if constexpr (SPECIAL) {
+            const float2 a = values_of(v[2 * i]), b = values_of(v[2 * i + 1]);
+            const float f[4] = {a.x, a.y, b.x, b.y};
+            w[i] = encode4(f, reciprocal);
+        } else {
+            w[i] = encode4_finite(v + 2 * i, pair_of(reciprocal));
+        }
+    }
     if (n >= U) {
         if constexpr (U == 8)
             *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
@@ -147,7 +177,7 @@ template <int U, bool SPECIAL> __device__ __forceinline__ void store_codes(uint8
 // are rare: where m is not finite, the block looks for its largest finite magnitude and encodes with care.
 template <typename T, typename Values>
 __device__ __forceinline__ void write_codes(const PackedOut &out, const Extent &x, long long index, int row0, int col,
-                                            const Values &v, unsigned m, unsigned *shared)
+                                            bool edge, const Values &v, unsigned m, unsigned *shared)
 {
     using L = Layout<T>;
     const bool special = m >= 0x7f800000u;
@@ -155,40 +185,47 @@ __device__ __forceinline__ void write_codes(const PackedOut &out, const Extent &
         m = 0u;
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
-            float f[L::U];
+            f32x2 f[L::U / 2];
             v.unit(j, f);
 #pragma unroll
-            for (int i = 0; i < L::U; ++i) m = max(m, finite_magnitude(f[i]));
+            for (int i = 0; i < L::U / 2; ++i)
+                m = max(m, max(finite_magnitude(values_of(f[i]).x), finite_magnitude(values_of(f[i]).y)));
         }
         m = block_max(m, shared);
     }
     const unsigned byte = scale_byte(m);
     const float reciprocal = scale_reciprocal(byte);
     if (threadIdx.x == 0) out.scales[index] = (uint8_t)byte;
-    if (col >= x.cols) return;
-    uint8_t *p = out.codes + (long long)row0 * out.stride + col;
+    uint8_t *p = out.codes + row0 * out.stride + col;
+    const long long step = L::STEP * out.stride;
+    if (!edge && !special) {
 #pragma unroll
+        for (int j = 0; j < L::UNITS; ++j) {
+            f32x2 f[L::U / 2];
+            v.unit(j, f);
+            store_codes<L::U, false>(p, L::U, f, reciprocal);
+            p += step;
+        }
+        return;
+    }
+    if (col >= x.cols) return;
+#pragma unroll 1
     for (int j = 0; j < L::UNITS; ++j) {
         if (row0 + j * L::STEP < x.rows) {
-            float f[L::U];
-            v.unit(j, f);
-            if (special)
-                store_codes<L::U, true>(p, x.cols - col, f, reciprocal);
-            else
-                store_codes<L::U, false>(p, x.cols - col, f, reciprocal);
+            f32x2 f[L::U / 2];
+            v.unit_at(j, f);
+            store_codes<L::U, true>(p, x.cols - col, f, reciprocal);
         }
-        p += L::STEP * out.stride;
+        p += step;
     }
 }
 
-// exp(-2u); 2u log2(e) = a (c1 + c3 a^2).  The approximations are good to two units in the last place.
-__device__ __forceinline__ float gelu_decay(float a)
+// The approximations are good to two units in the last place.
+__device__ __forceinline__ float exp2_of(float x)
 {
-    constexpr float c1 = 2.0f * 0.7978845608028654f * 1.4426950408889634f;
-    constexpr float c3 = c1 * 0.044715f;
-    float d;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(-a * fmaf(c3, a * a, c1)));
-    return d;
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
 __device__ __forceinline__ float reciprocal_of(float x)
 {
@@ -196,17 +233,37 @@ __device__ __forceinline__ float reciprocal_of(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-
-__device__ __forceinline__ float gelu(float a) { return a * reciprocal_of(1.0f + gelu_decay(a)); }
+// d = exp(-2u) and s = 1 / (1 + d) of two values; -2u log2(e) = a (c1 + c3 a^2).
+__device__ __forceinline__ void gelu_share(f32x2 a, f32x2 square, f32x2 &d, f32x2 &s)
+{
+    constexpr float c1 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, c3 = c1 * 0.044715f;
+    const float2 e = values_of(mul2(a, fma2(square, pair_of(c3), pair_of(c1))));
+    d = pair_of(exp2_of(e.x), exp2_of(e.y));
+    const float2 t = values_of(add2(d, pair_of(1.0f)));
+    s = pair_of(reciprocal_of(t.x), reciprocal_of(t.y));
+}
+__device__ __forceinline__ f32x2 gelu(f32x2 a)
+{
+    f32x2 d, s;
+    gelu_share(a, mul2(a, a), d, s);
+    return mul2(a, s);
+}
 
 // s + a s (1 - s) 2u' = s (1 + a d s 2u') with d = exp(-2u): no cancellation where s is near 1.  a is held
 // within +-10.03, NaN kept: there the slope is 1, or 0 (d is still finite and s flushed to zero).
-__device__ __forceinline__ float gelu_slope(float a)
+__device__ __forceinline__ float held(float a)
+{
+    asm("min.NaN.f32 %0, %0, 0f41208000;\n\tmax.NaN.f32 %0, %0, 0fC1208000;" : "+f"(a));
+    return a;
+}
+__device__ __forceinline__ f32x2 gelu_slope(f32x2 value)
 {
     constexpr float k1 = 2.0f * 0.7978845608028654f, k3 = 3.0f * 0.044715f * k1;
-    asm("min.NaN.f32 %0, %0, 0f41208000;\n\tmax.NaN.f32 %0, %0, 0fC1208000;" : "+f"(a));
-    const float d = gelu_decay(a), s = reciprocal_of(1.0f + d);
-    return s * fmaf(d * s, a * fmaf(k3, a * a, k1), 1.0f);
+    const float2 v = values_of(value);
+    const f32x2 a = pair_of(held(v.x), held(v.y)), square = mul2(a, a);
+    f32x2 d, s;
+    gelu_share(a, square, d, s);
+    return mul2(s, fma2(mul2(d, s), mul2(a, fma2(square, pair_of(k3), pair_of(k1))), pair_of(1.0f)));
 }
 
 enum : int { OP_PACK, OP_NORM, OP_GELU, OP_GELU_BACK };
@@ -228,12 +285,18 @@ struct BlockArgs {
 };
 
 // gamma and beta of U columns.
-template <int U> __device__ __forceinline__ void norm_params(const BlockArgs &a, int col, float *gamma, float *beta)
+template <int U> __device__ __forceinline__ void norm_params(const BlockArgs &a, int col, f32x2 *gamma, f32x2 *beta)
 {
 #pragma unroll
-    for (int i = 0; i < U; ++i) { gamma[i] = 1.0f; beta[i] = 0.0f; }
-    if (a.gamma) load_params<U>(a.gamma, a.params_bf16, a.gamma_aligned, col, a.extent.cols, gamma);
-    if (a.beta) load_params<U>(a.beta, a.params_bf16, a.beta_aligned, col, a.extent.cols, beta);
+    for (int i = 0; i < U / 2; ++i) { gamma[i] = pair_of(1.0f); beta[i] = 0ull; }
+    if (a.gamma) param_pairs<U>(a.gamma, a.params_bf16, a.gamma_aligned, col, a.extent.cols, gamma);
+    if (a.beta) param_pairs<U>(a.beta, a.params_bf16, a.beta_aligned, col, a.extent.cols, beta);
+}
+template <int U>
+__device__ __forceinline__ void normalise(f32x2 *f, float mean, float rstd, const f32x2 *gamma, const f32x2 *beta)
+{
+#pragma unroll
+    for (int i = 0; i < U / 2; ++i) f[i] = fma2(mul2(add2(f[i], pair_of(-mean)), pair_of(rstd)), gamma[i], beta[i]);
 }
 
 template <typename T, int OP>
@@ -263,64 +326,54 @@ __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant
     }
     const LoadedValues<T> loaded = {raw};
     if constexpr (OP == OP_PACK) {
-        write_codes<T>(a.first, a.extent, blockIdx.x, row0, col, loaded, block_max(loaded.largest(), shared[0]), shared[1]);
+        write_codes<T>(a.first, a.extent, blockIdx.x, row0, col, edge, loaded, block_max(loaded.largest(), shared[0]), shared[1]);
         return;
     }
 
-    float y[VALUES];
+    f32x2 y[VALUES / 2];
     if constexpr (OP == OP_NORM) {
-        float gamma[U], beta[U];
+        f32x2 gamma[U / 2], beta[U / 2];
         norm_params<U>(a, col, gamma, beta);
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
             const int r = row0 + j * L::STEP;
             const float mean = r < rows ? a.mean[r] : 0.0f, rstd = r < rows ? a.rstd[r] : 0.0f;
-            float *f = y + j * U;
+            f32x2 *f = y + j * U / 2;
             loaded.unit(j, f);
-#pragma unroll
-            for (int i = 0; i < U; ++i) f[i] = fmaf((f[i] - mean) * rstd, gamma[i], beta[i]);
-            if (edge) {
-#pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (r >= rows || col + i >= cols) f[i] = 0.0f;
-            }
+            normalise<U>(f, mean, rstd, gamma, beta);
+            if (edge) keep_inside<U>(f, r < rows ? cols - col : 0);
         }
     } else if constexpr (OP == OP_GELU) {
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
-            float *f = y + j * U;
+            f32x2 *f = y + j * U / 2;
             loaded.unit(j, f);
 #pragma unroll
-            for (int i = 0; i < U; ++i) f[i] = gelu(f[i]);
+            for (int i = 0; i < U / 2; ++i) f[i] = gelu(f[i]);
         }
     } else {
-        const float scale = scale_value(a.scales[blockIdx.x]);
+        const f32x2 scale = pair_of(scale_value(a.scales[blockIdx.x]));
         const uint8_t *q = a.codes + (long long)row0 * a.codes_stride + col;
 #pragma unroll
         for (int j = 0; j < L::UNITS; ++j) {
-            float *f = y + j * U;
+            f32x2 *f = y + j * U / 2;
             loaded.unit(j, f);
             const bool in = !edge || (row0 + j * L::STEP < rows && col < cols);
 #pragma unroll
             for (int i = 0; i < U; i += 4) {
-                float v[4];
                 // rows of codes are padded to 16 bytes: four of them can be read wherever one can
-                decode4(in && (!edge || col + i < cols) ? *reinterpret_cast<const unsigned *>(q + i) : 0u, scale, v);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) f[i + t] *= gelu_slope(v[t]);
+                const unsigned w = in && (!edge || col + i < cols) ? *reinterpret_cast<const unsigned *>(q + i) : 0u;
+                f[i / 2] = mul2(f[i / 2], gelu_slope(mul2(decode_pair(w), scale)));
+                f[i / 2 + 1] = mul2(f[i / 2 + 1], gelu_slope(mul2(decode_pair(w >> 16), scale)));
             }
-            if (edge) {
-#pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (col + i >= cols) f[i] = 0.0f;
-            }
+            if (edge) keep_inside<U>(f, cols - col);
             q += L::STEP * a.codes_stride;
         }
     }
     const ComputedValues<T> computed = {y};
-    write_codes<T>(a.first, a.extent, blockIdx.x, row0, col, computed, block_max(computed.largest(), shared[0]), shared[1]);
+    write_codes<T>(a.first, a.extent, blockIdx.x, row0, col, edge, computed, block_max(computed.largest(), shared[0]), shared[1]);
     if (OP != OP_GELU_BACK && a.second.codes)
-        write_codes<T>(a.second, a.extent, blockIdx.x, row0, col, loaded, block_max(loaded.largest(), shared[2]), shared[3]);
+        write_codes<T>(a.second, a.extent, blockIdx.x, row0, col, edge, loaded, block_max(loaded.largest(), shared[2]), shared[3]);
 }
 
 // ------------------------------------------------------------------------------------------ streamed blocks
@@ -342,7 +395,8 @@ template <int OP> struct Stream {
 struct SharedValues {
     const uint4 *unit0;
     __device__ __forceinline__ uint4 at(int j) const { return unit0[j * THREADS]; }
-    __device__ __forceinline__ void unit(int j, float *f) const { Unit<__nv_bfloat16>::widen(at(j), f); }
+    __device__ __forceinline__ void unit(int j, f32x2 *p) const { widen_pairs<__nv_bfloat16>(at(j), p); }
+    __device__ __forceinline__ void unit_at(int j, f32x2 *p) const { unit(j, p); }
 };
 
 __device__ __forceinline__ void load_box(void *to, const CUtensorMap *map, int x, int y, uint64_t *bar)
@@ -391,7 +445,8 @@ __global__ void __launch_bounds__(THREADS, 2)
         const int row0 = index / a.extent.block_cols * PACK_BLOCK + (int)threadIdx.x / L::PER_ROW;
         const int col0 = index % a.extent.block_cols * PACK_BLOCK;
         const int col = col0 + (int)(threadIdx.x % L::PER_ROW) * U;
-        float gamma[U], beta[U], mean[L::UNITS], rstd[L::UNITS];
+        f32x2 gamma[U / 2], beta[U / 2];
+        float mean[L::UNITS], rstd[L::UNITS];
         if constexpr (OP == OP_NORM) {
             norm_params<U>(a, col, gamma, beta);
 #pragma unroll
@@ -401,14 +456,15 @@ __global__ void __launch_bounds__(THREADS, 2)
                 rstd[j] = a.rstd[r];
             }
         }
-        const float scale = OP == OP_GELU_BACK ? scale_value(a.scales[index]) : 0.0f;
+        const f32x2 scale = pair_of(OP == OP_GELU_BACK ? scale_value(a.scales[index]) : 0.0f);
+        const bool edge = col0 + PACK_BLOCK > cols || (index / a.extent.block_cols + 1) * PACK_BLOCK > rows;
         const SharedValues x = {reinterpret_cast<const uint4 *>(buffers + buffer * S::BYTES) + threadIdx.x};
         if (!bounded_wait(&full[buffer], phase, &g_packing_error, 1)) {
             for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
             return;
         }
 
-        float y[OP == OP_PACK ? 1 : VALUES];
+        f32x2 y[OP == OP_PACK ? 1 : VALUES / 2];
         unsigned mx = 0u;
         float my = 0.0f;
 #pragma unroll
@@ -421,29 +477,23 @@ __global__ void __launch_bounds__(THREADS, 2)
                 mx = larger_bf16x2(mx, unit.w);
             }
             if constexpr (OP != OP_PACK) {
-                float *f = y + j * U;
-                Unit<T>::widen(unit, f);
+                f32x2 *f = y + j * U / 2;
+                widen_pairs<T>(unit, f);
                 if constexpr (OP == OP_NORM) {
-#pragma unroll
-                    for (int i = 0; i < U; ++i) f[i] = fmaf((f[i] - mean[j]) * rstd[j], gamma[i], beta[i]);
-                    if (col0 + PACK_BLOCK > cols || row0 + j * L::STEP >= rows) {
-#pragma unroll
-                        for (int i = 0; i < U; ++i)
-                            if (row0 + j * L::STEP >= rows || col + i >= cols) f[i] = 0.0f;
-                    }
+                    normalise<U>(f, mean[j], rstd[j], gamma, beta);
+                    if (col0 + PACK_BLOCK > cols || row0 + j * L::STEP >= rows)
+                        keep_inside<U>(f, row0 + j * L::STEP < rows ? cols - col : 0);
                 } else if constexpr (OP == OP_GELU) {
 #pragma unroll
-                    for (int i = 0; i < U; ++i) f[i] = gelu(f[i]);
+                    for (int i = 0; i < U / 2; ++i) f[i] = gelu(f[i]);
                 } else {
                     const uint2 c = reinterpret_cast<const uint2 *>(buffers + buffer * S::BYTES + DENSE_BYTES)[threadIdx.x + j * THREADS];
-                    float v[U];
-                    decode4(c.x, scale, v);
-                    decode4(c.y, scale, v + 4);
 #pragma unroll
-                    for (int i = 0; i < U; ++i) f[i] *= gelu_slope(v[i]);
+                    for (int i = 0; i < U / 2; ++i)
+                        f[i] = mul2(f[i], gelu_slope(mul2(decode_pair((i < 2 ? c.x : c.y) >> (16 * (i & 1))), scale)));
                 }
 #pragma unroll
-                for (int i = 0; i < U; ++i) my = fmaxf(my, fabsf(f[i]));
+                for (int i = 0; i < U / 2; ++i) my = larger(my, f[i]);
             }
         }
         const unsigned wx = __reduce_max_sync(0xffffffffu, wider_bf16x2(mx));
@@ -459,11 +509,11 @@ __global__ void __launch_bounds__(THREADS, 2)
         if constexpr (OP != OP_PACK) {
             const ComputedValues<T> computed = {y};
             const unsigned m = __reduce_max_sync(0xffffffffu, maxima[turn][1][lane % (THREADS / 32)]);
-            write_codes<T>(a.first, a.extent, index, row0, col, computed, m, special[0]);
+            write_codes<T>(a.first, a.extent, index, row0, col, edge, computed, m, special[0]);
         }
         if (OP == OP_PACK || (OP != OP_GELU_BACK && a.second.codes)) {
             const unsigned m = __reduce_max_sync(0xffffffffu, maxima[turn][0][lane % (THREADS / 32)]);
-            write_codes<T>(OP == OP_PACK ? a.first : a.second, a.extent, index, row0, col, x, m, special[1]);
+            write_codes<T>(OP == OP_PACK ? a.first : a.second, a.extent, index, row0, col, edge, x, m, special[1]);
         }
         previous = buffer;
         if (++buffer == S::BUFFERS) { buffer = 0; phase ^= 1; }
