@@ -9,8 +9,7 @@
 //
 //   pair_kernel    persistent; two SMs share a tile of 256 rows and up to 256 columns (cta_group::2):
 //                  each loads half of A and half of B and keeps half of the sums
-//   skinny_kernel  products with at most 64 rows or columns: 128 of the long side per block, the
-//                  contraction shared by the blocks of a cluster
+//   few_kernel     a few tokens through a weight: every weight is read once and multiplied in registers
 #include "inner_common.cuh"
 
 #include <algorithm>
@@ -78,22 +77,14 @@ __device__ __forceinline__ bool wait_cluster(uint64_t *bar, unsigned parity, int
         }
     }
 }
-// GROUP: blocks that share a product (cta_group).  With 2 the barrier may be the other block's.
-template <int GROUP>
+// Of a pair's block; the barrier may be the other block's.
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
-    if constexpr (GROUP == 1)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
-            "[%4];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+        "[%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y)
 {
@@ -101,67 +92,39 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
                  "r"(y), "r"(src)
                  : "memory");
 }
-template <int GROUP> __device__ __forceinline__ void tmem_alloc(uint32_t *result, int columns)
+__device__ __forceinline__ void tmem_alloc(uint32_t *result, int columns)
 {
-    if constexpr (GROUP == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_addr(result)),
-                     "r"(columns)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_addr(result)),
-                     "r"(columns)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    }
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ptx::smem_addr(result)),
+                 "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
 }
-template <int GROUP> __device__ __forceinline__ void tmem_free(uint32_t address, int columns)
+__device__ __forceinline__ void tmem_free(uint32_t address, int columns)
 {
-    if constexpr (GROUP == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
-    else
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
 }
-// 32 lanes x 16 bytes of shared memory to four columns of each 32-lane quarter of tensor memory
-template <int GROUP> __device__ __forceinline__ void tmem_copy_scales(uint32_t address, uint64_t desc)
+// 32 lanes x 16 bytes of shared memory to four columns of each 32-lane quarter of tensor memory, in both blocks
+__device__ __forceinline__ void tmem_copy_scales(uint32_t address, uint64_t desc)
 {
-    if constexpr (GROUP == 1)
-        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(address), "l"(desc) : "memory");
-    else
-        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(address), "l"(desc) : "memory");
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(address), "l"(desc) : "memory");
 }
-template <int GROUP>
 __device__ __forceinline__ void mma_block_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a,
                                                  uint32_t scale_b, bool add)
 {
-    if constexpr (GROUP == 1)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
-                d),
-            "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"((unsigned)add)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
-                d),
-            "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"((unsigned)add)
-            : "memory");
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"((unsigned)add)
+        : "memory");
 }
-// Arrives on the barrier, of both blocks of a pair, once the products issued so far are done.
-template <int GROUP> __device__ __forceinline__ void mma_commit(uint64_t *bar)
+// Arrives on the barrier of both blocks of the pair once the products issued so far are done.
+__device__ __forceinline__ void mma_commit(uint64_t *bar)
 {
-    if constexpr (GROUP == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-                         ptx::smem_addr(bar))
-                     : "memory");
-    else
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-                ptx::smem_addr(bar)),
-            "h"((unsigned short)3)
-            : "memory");
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            ptx::smem_addr(bar)),
+        "h"((unsigned short)3)
+        : "memory");
 }
 __device__ __forceinline__ void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -216,7 +179,7 @@ struct ProductArgs {
     int transpose_a, transpose_b;  // A is stored [K, M]; B is stored [N, K]
     int m, n, steps;
     void *c;
-    long long c_row, c_col;  // strides of C in elements
+    long long c_row;  // stride of C in elements
     int c_bf16, accumulate;
     // pair_kernel
     int tile_n, tiles_m, tiles_n;
@@ -240,7 +203,7 @@ __device__ __forceinline__ uint32_t byte_at(uint32_t word, int shift) { return w
 
 __device__ __forceinline__ void store_c(const ProductArgs &p, long long row, long long col, float v)
 {
-    const long long at = row * p.c_row + col * p.c_col;
+    const long long at = row * p.c_row + col;
     if (p.c_bf16) {
         __nv_bfloat16 *c = static_cast<__nv_bfloat16 *>(p.c) + at;
         if (p.accumulate) v += __bfloat162float(*c);
@@ -430,7 +393,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
     const unsigned rank = cluster_rank();
     const int pair = blockIdx.x >> 1;
 
-    if (warp == 0) tmem_alloc<2>(&tmem_base, 512);
+    if (warp == 0) tmem_alloc(&tmem_base, 512);
     if (threadIdx.x == 32) {
         for (int s = 0; s < PAIR_STAGES; ++s) {
             ptx::mbar_init(&full[s], 1);
@@ -471,13 +434,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     const uint32_t bar = cluster_addr(ptx::smem_addr(&full[stage]), 0);
                     if (rank == 0) ptx::mbar_arrive_expect_tx(&full[stage], 2 * (PAIR_OPERAND_BYTES + b_bytes));
                     if (p.transpose_a)
-                        tma_load_2d<2>(to, &a_map, m0, i * STEP, bar);
+                        tma_load_2d(to, &a_map, m0, i * STEP, bar);
                     else
-                        tma_load_2d<2>(to, &a_map, i * STEP, m0, bar);
+                        tma_load_2d(to, &a_map, i * STEP, m0, bar);
                     if (p.transpose_b)
-                        tma_load_2d<2>(to + PAIR_OPERAND_BYTES, &b_map, i * STEP, nb, bar);
+                        tma_load_2d(to + PAIR_OPERAND_BYTES, &b_map, i * STEP, nb, bar);
                     else
-                        tma_load_2d<2>(to + PAIR_OPERAND_BYTES, &b_map, nb, i * STEP, bar);
+                        tma_load_2d(to + PAIR_OPERAND_BYTES, &b_map, nb, i * STEP, bar);
                 }
                 __syncwarp();
                 if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
@@ -599,20 +562,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                         if (in_words % QUAD == 0) {
                             const uint32_t words =
                                 base + PAIR_WORDS_AT + words_set * PAIR_WORDS_SET + in_words / QUAD * PAIR_WORDS_BYTES;
-                            tmem_copy_scales<2>(scale_a, scales_desc(words));
-                            tmem_copy_scales<2>(scale_b, scales_desc(words + SCALE_BYTES));
-                            if (p.tile_n > 128) tmem_copy_scales<2>(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
+                            tmem_copy_scales(scale_a, scales_desc(words));
+                            tmem_copy_scales(scale_b, scales_desc(words + SCALE_BYTES));
+                            if (p.tile_n > 128) tmem_copy_scales(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
                         }
                         const uint32_t desc = idesc | scale_byte_desc(in_words % QUAD);
                         const uint64_t da = operand_desc(at), db = operand_desc(at + PAIR_OPERAND_BYTES);
                         const uint32_t sums = tmem + ((sets & 1) ? second_set : 0);
 #pragma unroll
                         for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
-                            mma_block_scaled<2>(sums, da + j * step_a, db + j * step_b, desc, scale_a, scale_b,
+                            mma_block_scaled(sums, da + j * step_a, db + j * step_b, desc, scale_a, scale_b,
                                                 in_set + j > 0);
-                        mma_commit<2>(&empty[stage]);
-                        if (words_end) mma_commit<2>(&words_empty[words_set]);
-                        if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) mma_commit<2>(&sums_full[sets & 1]);
+                        mma_commit(&empty[stage]);
+                        if (words_end) mma_commit(&words_empty[words_set]);
+                        if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) mma_commit(&sums_full[sets & 1]);
                     }
                     __syncwarp();
                     if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) ++sets;
@@ -627,7 +590,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                 }
             }
             if (!ok) {  // products in flight end before the tensor memory is freed
-                if (elect_one()) mma_commit<2>(&ended);
+                if (elect_one()) mma_commit(&ended);
                 bounded_wait(&ended, 0, &g_product_error, 10);
             }
         }
@@ -714,7 +677,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
     fence_before_sync();
     cluster_sync();
     fence_after_sync();
-    if (warp == 0) tmem_free<2>(tmem, 512);
+    if (warp == 0) tmem_free(tmem, 512);
 }
 
 // Tiles whose steps were dealt out: their partial sums in the order of the steps.  A block joins 32
@@ -758,168 +721,154 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Produ
             store_c(p, row0 + r, col, shared[r][threadIdx.x & 31]);
 }
 
-// ------------------------------------------------------------------------------------------ few rows or columns
+// ------------------------------------------------------------------------------------------ a few rows
 
-// 128 of the long side ("rows") against all of the short side ("columns", 16, 32 or 64 of them).  The
-// blocks of a cluster share the contraction; block 0 adds the sums up in their order.
-constexpr int SKINNY_STAGES = 4;
-constexpr int SKINNY_MAX_N = 64;
-constexpr int SKINNY_COLUMN_BYTES = 128 * STEP;  // of a stage, where the short side is across rows of codes
-constexpr int SKINNY_THREADS = 192;              // four epilogue warps, load warp, issuing warp
-constexpr int SKINNY_MAX_CLUSTER = 8;
-constexpr int SKINNY_MAX_COLLECTED = 112 * 1024; // other blocks' sums in block 0: leaves room for two blocks per SM
-constexpr int SKINNY_TMEM = 128;                 // 64 of sums, 8 of scales for each of four quads
+// Up to four rows of A (tokens) against the rows of B^T (a weight's outputs), both contracted along their
+// rows: bound by reading the weight once.  The tokens wait in shared memory in f16, which holds every code;
+// a warp takes two outputs, 16 codes per lane and step, all within one block, and multiplies in fp32.  The
+// tensor cores' path takes 9.3 us for one token through 3584x896 and 20 us through 8192x8192.
+constexpr int FEW_MAX = 4;
+constexpr int FEW_THREADS = 256;
+constexpr int FEW_OUTPUTS = 2;  // of a warp
+constexpr int FEW_SMEM = 96 * 1024;
 
-__host__ __device__ constexpr int skinny_stage_bytes(int column_bytes) { return 128 * STEP + column_bytes + 2 * SCALE_BYTES; }
+struct FewArgs {
+    const uint8_t *tokens, *token_scales, *weight, *weight_scales;
+    long long token_stride, weight_stride;
+    int outputs, k, steps;
+    void *c;
+    long long c_token, c_output;  // strides of C
+    int c_bf16, accumulate;
+};
 
-__global__ void __launch_bounds__(SKINNY_THREADS)
-    skinny_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
-                  const __grid_constant__ ProductArgs p, int shares, int column_bytes)
+__device__ __forceinline__ void store_few(const FewArgs &p, int token, int output, float v)
 {
-    extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[SKINNY_STAGES], empty[SKINNY_STAGES], done, drained;
-    __shared__ uint32_t tmem_base;
-    const uint32_t base = (ptx::smem_addr(raw) + 1023u) & ~1023u;
-    uint8_t *aligned = raw + (base - ptx::smem_addr(raw));
-    const int stage_bytes = skinny_stage_bytes(column_bytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tile = blockIdx.x / shares, share = blockIdx.x % shares;
-    const int first = (int)((long long)p.steps * share / shares), last = (int)((long long)p.steps * (share + 1) / shares);
-    const int steps = last - first;
-
-    if (warp == 5) tmem_alloc<1>(&tmem_base, SKINNY_TMEM);
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < SKINNY_STAGES; ++s) {
-            ptx::mbar_init(&full[s], 2);
-            ptx::mbar_init(&empty[s], 1);
-        }
-        ptx::mbar_init(&done, 1);
-        ptx::mbar_init(&drained, 128);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    fence_before_sync();
-    __syncthreads();
-    fence_after_sync();
-    const uint32_t tmem = tmem_base;
-    float sum[SKINNY_MAX_N];
-    bool ok = true;
-
-    if (warp == 4) {
-        int issued = 0;
-        unsigned held_a = 127, held_b = 127;  // scale bytes of 32 steps, one per lane
-        for (int i = 0; i < steps; ++i) {
-            const int s = i % SKINNY_STAGES;
-            ok = bounded_wait(&empty[s], ((i / SKINNY_STAGES) & 1) ^ 1, &g_product_error, 1);
-            if (!ok) break;
-            const int k0 = (first + i) * STEP;
-            if (elect_one()) {
-                ptx::mbar_arrive_expect_tx(&full[s], 128 * STEP + column_bytes);
-                const uint32_t at = base + s * stage_bytes, bar = ptx::smem_addr(&full[s]);
-                tma_load_2d<1>(at, &a_map, p.transpose_a ? tile * 128 : k0, p.transpose_a ? k0 : tile * 128, bar);
-                tma_load_2d<1>(at + 128 * STEP, &b_map, p.transpose_b ? k0 : 0, p.transpose_b ? 0 : k0, bar);
-            }
-            ++issued;
-            if (i % 32 == 0 && i + lane < steps) {
-                const long long kb = first + i + lane;
-                held_a = p.a_scales[p.transpose_a ? kb * p.a_scale_cols + tile : (long long)tile * p.a_scale_cols + kb];
-                held_b = p.b_scales[p.transpose_b ? kb : kb * p.b_scale_cols];
-            }
-            if (i % QUAD == 0) {
-                unsigned wa = 0u, wb = 0u;  // after the last step: not used
-#pragma unroll
-                for (int j = 0; j < QUAD; ++j) {
-                    wa |= __shfl_sync(0xffffffffu, held_a, i % 32 + j) << 8 * j;
-                    wb |= __shfl_sync(0xffffffffu, held_b, i % 32 + j) << 8 * j;
-                }
-                uint4 *words = reinterpret_cast<uint4 *>(aligned + s * stage_bytes + 128 * STEP + column_bytes);
-                words[lane] = make_uint4(wa, wa, wa, wa);
-                words[32 + lane] = make_uint4(wb, wb, wb, wb);
-                ptx::fence_proxy_async();
-            }
-            __syncwarp();
-            if (elect_one()) ptx::mbar_arrive(&full[s]);
-        }
-        if (!ok)  // copies in flight end before the block does
-            for (int i = max(0, issued - SKINNY_STAGES); i < issued; ++i)
-                bounded_wait(&full[i % SKINNY_STAGES], (i / SKINNY_STAGES) & 1, &g_product_error, 2);
-    } else if (warp == 5) {
-        const uint32_t idesc = instruction_desc(p, 128, p.tile_n);
-        const uint32_t step_a = (p.transpose_a ? CONTRACTED_PER_MMA * 128 : CONTRACTED_PER_MMA) >> 4;
-        const uint32_t step_b = (p.transpose_b ? CONTRACTED_PER_MMA : CONTRACTED_PER_MMA * 128) >> 4;
-        for (int i = 0; i < steps; ++i) {
-            const int s = i % SKINNY_STAGES;
-            ok = bounded_wait(&full[s], (i / SKINNY_STAGES) & 1, &g_product_error, 3);
-            if (ok && i > 0 && i % CHUNK == 0) ok = bounded_wait(&drained, (i / CHUNK - 1) & 1, &g_product_error, 5);
-            if (!ok) break;
-            fence_after_sync();
-            if (elect_one()) {
-                const uint32_t at = base + s * stage_bytes, words = at + 128 * STEP + column_bytes;
-                // four slots: the step that begins a quad is loaded where the step four before it was
-                const uint32_t scale_a = tmem + SKINNY_MAX_N + i / QUAD % SKINNY_STAGES * 8, scale_b = scale_a + 4;
-                if (i % QUAD == 0) {
-                    tmem_copy_scales<1>(scale_a, scales_desc(words));
-                    tmem_copy_scales<1>(scale_b, scales_desc(words + SCALE_BYTES));
-                }
-                const uint32_t desc = idesc | scale_byte_desc(i % QUAD);
-                const uint64_t da = operand_desc(at), db = operand_desc(at + 128 * STEP);
-#pragma unroll
-                for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
-                    mma_block_scaled<1>(tmem, da + j * step_a, db + j * step_b, desc, scale_a, scale_b, i % CHUNK + j > 0);
-                mma_commit<1>(&empty[s]);
-                if (i + 1 == steps || i % CHUNK == CHUNK - 1) mma_commit<1>(&done);
-            }
-            __syncwarp();
-        }
+    const long long at = token * p.c_token + output * p.c_output;
+    if (p.c_bf16) {
+        __nv_bfloat16 *c = static_cast<__nv_bfloat16 *>(p.c) + at;
+        *c = __float2bfloat16_rn(p.accumulate ? v + __bfloat162float(*c) : v);
     } else {
+        float *c = static_cast<float *>(p.c) + at;
+        *c = p.accumulate ? v + *c : v;
+    }
+}
+
+// v times the product of two scales, whose exponents are added first: two halves of the sum are always
+// exponents of fp32, where the scales' product itself might not be.
+__device__ __forceinline__ float scaled(float v, unsigned a, unsigned b)
+{
+    if (a == 255u || b == 255u) return __uint_as_float(0x7fc00000u);
+    const int e = (int)(a + b) - 254, half = e >> 1;
+    return v * __uint_as_float((unsigned)(half + 127) << 23) * __uint_as_float((unsigned)(e - half + 127) << 23);
+}
+
+// The products of 16 codes of each output and each token, added to the sums.
+template <int M>
+__device__ __forceinline__ void few_products(const uint4 *codes, const unsigned *scale, unsigned token_scale,
+                                             const __half *tokens, int padded, int k, float (*sums)[M])
+{
+                float part[FEW_OUTPUTS][M] = {};
 #pragma unroll
-        for (int i = 0; i < SKINNY_MAX_N; ++i) sum[i] = 0.0f;
-        for (int chunk = 0; chunk * CHUNK < steps; ++chunk) {
-            ok = bounded_wait(&done, chunk & 1, &g_product_error, 4);
-            if (!ok) break;
-            fence_after_sync();
+                for (int q = 0; q < 2; ++q) {
+                    float w[FEW_OUTPUTS][8];
 #pragma unroll
-            for (int c0 = 0; c0 < SKINNY_MAX_N; c0 += 32) {
-                if (c0 < p.tile_n) {  // of 16 columns the other 16 are read and dropped
-                    uint32_t r[32];
-                    tmem_load32(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
+                    for (int r = 0; r < FEW_OUTPUTS; ++r) {
+                        decode4(q ? codes[r].z : codes[r].x, 1.0f, w[r]);
+                        decode4(q ? codes[r].w : codes[r].y, 1.0f, w[r] + 4);
+                    }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) sum[c0 + i] += __uint_as_float(r[i]);
+                    for (int t = 0; t < M; ++t) {
+                        const uint4 raw = *reinterpret_cast<const uint4 *>(tokens + t * padded + q * (padded / 2) + k / 2);
+                        const unsigned words[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&words[i]));
+#pragma unroll
+                            for (int r = 0; r < FEW_OUTPUTS; ++r) {
+                                part[r][t] = fmaf(w[r][2 * i], v.x, part[r][t]);
+                                part[r][t] = fmaf(w[r][2 * i + 1], v.y, part[r][t]);
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < FEW_OUTPUTS; ++r)
+#pragma unroll
+                    for (int t = 0; t < M; ++t) sums[r][t] += scaled(part[r][t], scale[r], token_scale);
+}
+
+template <int M> __global__ void __launch_bounds__(FEW_THREADS) few_kernel(const __grid_constant__ FewArgs p)
+{
+    // [M][2][padded / 16][8]: the halves of every 16 codes apart, so that a warp's loads do not conflict; then
+    // the tokens' scale bytes
+    extern __shared__ __align__(16) __half tokens[];
+    const int padded = p.steps * STEP, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t *token_scales = reinterpret_cast<uint8_t *>(tokens + M * padded);
+    for (int i = threadIdx.x; i < M * padded / 4; i += FEW_THREADS) {
+        const int t = i * 4 / padded, k = i * 4 % padded;
+        unsigned w = 0u;
+        if (k < p.k) {
+            w = *reinterpret_cast<const unsigned *>(p.tokens + t * p.token_stride + k);
+            if (k + 4 > p.k) w &= 0xffffffffu >> 8 * (k + 4 - p.k);
+        }
+        const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffffu), __NV_E4M3);
+        const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+        *reinterpret_cast<uint2 *>(tokens + t * padded + (k >> 3 & 1) * (padded / 2) + (k >> 4) * 8 + (k & 7)) =
+            make_uint2(lo.x | (unsigned)lo.y << 16, hi.x | (unsigned)hi.y << 16);
+    }
+    for (int i = threadIdx.x; i < p.steps; i += FEW_THREADS) token_scales[i] = p.token_scales[i];  // one block of rows
+    __syncthreads();
+
+    const int step = gridDim.x * (FEW_THREADS / 32) * FEW_OUTPUTS;
+    for (int first = (blockIdx.x * (FEW_THREADS / 32) + warp) * FEW_OUTPUTS; first < p.outputs; first += step) {
+        float sums[FEW_OUTPUTS][M] = {};
+        const uint8_t *rows[FEW_OUTPUTS], *scales[FEW_OUTPUTS];
+#pragma unroll
+        for (int r = 0; r < FEW_OUTPUTS; ++r) {
+            const int row = min(first + r, p.outputs - 1);
+            rows[r] = p.weight + row * p.weight_stride;
+            scales[r] = p.weight_scales + (long long)(row / PACK_BLOCK) * p.steps;
+        }
+        const int whole = p.k / 512 * 512;
+#pragma unroll(M == 1 ? 4 : 2)
+        for (int k = lane * 16; k < whole; k += 512) {
+            uint4 codes[FEW_OUTPUTS];
+            unsigned scale[FEW_OUTPUTS];
+#pragma unroll
+            for (int r = 0; r < FEW_OUTPUTS; ++r) {
+                codes[r] = __ldcs(reinterpret_cast<const uint4 *>(rows[r] + k));
+                scale[r] = scales[r][k / STEP];
+            }
+            few_products<M>(codes, scale, token_scales[k / STEP], tokens, padded, k, sums);
+        }
+        if (const int k = whole + lane * 16; k < p.k) {
+            uint4 codes[FEW_OUTPUTS];
+            unsigned scale[FEW_OUTPUTS];
+#pragma unroll
+            for (int r = 0; r < FEW_OUTPUTS; ++r) {
+                codes[r] = __ldcs(reinterpret_cast<const uint4 *>(rows[r] + k));
+                scale[r] = scales[r][k / STEP];
+            }
+            if (k + 16 > p.k) {  // rows of codes are padded to 16 bytes with anything
+                const int n = p.k - k;
+#pragma unroll
+                for (int r = 0; r < FEW_OUTPUTS; ++r) {
+                    codes[r].x &= n >= 4 ? ~0u : (1u << 8 * n) - 1u;
+                    codes[r].y &= n >= 8 ? ~0u : n > 4 ? (1u << 8 * (n - 4)) - 1u : 0u;
+                    codes[r].z &= n >= 12 ? ~0u : n > 8 ? (1u << 8 * (n - 8)) - 1u : 0u;
+                    codes[r].w &= n > 12 ? (1u << 8 * (n - 12)) - 1u : 0u;
                 }
             }
-            fence_before_sync();
-            ptx::mbar_arrive(&drained);
+            few_products<M>(codes, scale, token_scales[k / STEP], tokens, padded, k, sums);
         }
-    }
-    fence_before_sync();
-    __syncthreads();
-    fence_after_sync();
-    if (warp == 5) tmem_free<1>(tmem, SKINNY_TMEM);
-
-    // the stages are free: block 0 collects the other blocks' sums there, [share][column][128 rows]
-    float *sums_of = reinterpret_cast<float *>(aligned);
-    const int columns = min(p.tile_n, p.n);
-    if (shares > 1) {
-        cluster_sync();  // every block's stages are idle
-        if (warp < 4 && share > 0) {
-            const uint32_t to = cluster_addr(base, 0) + ((share - 1) * p.tile_n * 128 + warp * 32 + lane) * 4;
 #pragma unroll
-            for (int i = 0; i < SKINNY_MAX_N; ++i)
-                if (i < columns)
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + i * 512), "f"(sum[i]) : "memory");
-        }
-        cluster_sync();
-        if (share > 0) return;
-    }
-    if (warp < 4) {
-        const long long row = (long long)tile * 128 + warp * 32 + lane;
+        for (int r = 0; r < FEW_OUTPUTS; ++r)
 #pragma unroll
-        for (int i = 0; i < SKINNY_MAX_N; ++i) {
-            if (i < columns && row < p.m) {
-                float v = sum[i];
-                for (int q = 1; q < shares; ++q) v += sums_of[((q - 1) * p.tile_n + i) * 128 + warp * 32 + lane];
-                store_c(p, row, i, v);
+            for (int t = 0; t < M; ++t) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sums[r][t] += __shfl_xor_sync(0xffffffffu, sums[r][t], o);
+                if (lane == 0 && first + r < p.outputs) store_few(p, t, first + r, sums[r][t]);
             }
-        }
     }
 }
 
@@ -998,47 +947,32 @@ PairPlan plan_pairs(int64_t m, int64_t n, int64_t steps)
     return best;
 }
 
-bool is_skinny(int64_t m, int64_t n) { return std::min(m, n) <= SKINNY_MAX_N; }
-
-int launch_skinny(const dipaco_packed *a, const dipaco_packed *b, ProductArgs p, int64_t k, cudaStream_t stream)
+// Tokens of few_kernel: the shorter side, where both operands are contracted along their rows.
+bool are_few(int64_t m, int64_t n, int64_t k, bool transpose_a, bool transpose_b)
 {
-    if (p.m < p.n) {  // C^T = op(B)^T op(A)^T: the long side gives the rows
-        std::swap(a, b);
-        std::swap(p.a_scales, p.b_scales);
-        std::swap(p.a_scale_cols, p.b_scale_cols);
-        std::swap(p.m, p.n);
-        std::swap(p.c_row, p.c_col);
-        const int ta = p.transpose_a;
-        p.transpose_a = !p.transpose_b;
-        p.transpose_b = !ta;
-    }
-    p.tile_n = p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
-    const int column_bytes = p.transpose_b ? p.tile_n * STEP : SKINNY_COLUMN_BYTES;
-    const int64_t tiles = ceil_div(p.m, 128);
-    // enough blocks for two on every SM, at least two steps each
-    const int sums_bytes = p.tile_n * 128 * (int)sizeof(float);
-    const int shares = (int)std::min<int64_t>(
-        {SKINNY_MAX_CLUSTER, ceil_div(p.steps, 2), ceil_div(296, tiles), 1 + SKINNY_MAX_COLLECTED / sums_bytes});
-    const int collected = (shares - 1) * sums_bytes;
-    const int smem = std::max(SKINNY_STAGES * skinny_stage_bytes(column_bytes), collected) + 1024;
-    if (tiles * shares > INT32_MAX) return DIPACO_ELIMIT;
-    CUtensorMap a_map, b_map;
-    if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, p.transpose_b ? p.tile_n : 128)) return DIPACO_ECUDA;
-    if (cudaFuncSetAttribute(skinny_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    // more than two tokens only through smaller weights: four through 3584x896 take 6.5 us here and 8.7 us on
+    // the tensor cores, four through 8192x8192 41 us and 29 us
+    const int64_t few = std::min(m, n);
+    return (few <= 2 || (few <= FEW_MAX && std::max(m, n) * k <= (int64_t)1 << 24)) && !transpose_a && transpose_b && few * ceil_div(k, STEP) * STEP * 2 + ceil_div(k, STEP) <= FEW_SMEM;
+}
+
+int launch_few(const dipaco_packed *a, const dipaco_packed *b, void *c, int64_t c_stride, int dtype, bool accumulate,
+               cudaStream_t stream)
+{
+    const bool tokens_first = a->rows <= b->rows;
+    const dipaco_packed *tokens = tokens_first ? a : b, *weight = tokens_first ? b : a;
+    FewArgs p = {static_cast<const uint8_t *>(tokens->codes), static_cast<const uint8_t *>(tokens->scales),
+                 static_cast<const uint8_t *>(weight->codes), static_cast<const uint8_t *>(weight->scales),
+                 tokens->stride, weight->stride, (int)weight->rows, (int)weight->cols, (int)ceil_div(weight->cols, STEP),
+                 c, tokens_first ? c_stride : 1, tokens_first ? 1 : c_stride, dtype == DIPACO_BF16, accumulate};
+    const int m = (int)tokens->rows;
+    const int smem = m * p.steps * STEP * 2 + p.steps;
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(p.outputs, FEW_THREADS / 32 * FEW_OUTPUTS), 148 * 2);
+    const auto kernel = m == 1 ? few_kernel<1> : m == 2 ? few_kernel<2> : m == 3 ? few_kernel<3> : few_kernel<4>;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
         return launch_status();
-    cudaLaunchAttribute cluster = {};
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = shares;
-    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3((unsigned)(tiles * shares));
-    config.blockDim = dim3(SKINNY_THREADS);
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    config.attrs = &cluster;
-    config.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&config, skinny_kernel, a_map, b_map, p, shares, column_bytes);
-    return err == cudaSuccess ? DIPACO_OK : launch_status();
+    kernel<<<grid, FEW_THREADS, smem, stream>>>(p);
+    return launch_status();
 }
 
 template <bool CHUNKED>
@@ -1060,7 +994,7 @@ int dipaco_packed_matmul_workspace(int64_t m, int64_t n, int64_t k, int64_t *byt
     if (!bytes || k < 0) return DIPACO_EINVAL;
     if (const int rc = check_extents(m, n)) return rc;
     if (k > MAX_EXTENT) return DIPACO_ELIMIT;
-    *bytes = m == 0 || n == 0 || k == 0 || is_skinny(m, n) ? 0 : plan_pairs(m, n, ceil_div(k, STEP)).workspace;
+    *bytes = m == 0 || n == 0 || k == 0 ? 0 : plan_pairs(m, n, ceil_div(k, STEP)).workspace;
     return DIPACO_OK;
 }
 
@@ -1076,7 +1010,8 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     if (const int rc = dipaco_packed_matmul_workspace(m, n, k, &need)) return rc;
     if (!packed_ok(a, a->rows, a->cols) || !packed_ok(b, b->rows, b->cols)) return DIPACO_EINVAL;
     if (!dense_ok(c, c_stride, m, n, dtype)) return DIPACO_EINVAL;
-    if (need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < need)) return DIPACO_EINVAL;
+    const bool few = are_few(m, n, k, transpose_a, transpose_b);
+    if (!few && need > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < need)) return DIPACO_EINVAL;
     if (m == 0 || n == 0 || (k == 0 && accumulate)) return DIPACO_OK;
 
     DeviceScope scope(device);
@@ -1087,6 +1022,7 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
         const size_t pitch = m == 1 ? n * size : c_stride * size;
         return cudaMemset2DAsync(c, pitch, 0, n * size, m, stream) == cudaSuccess ? DIPACO_OK : launch_status();
     }
+    if (few) return launch_few(a, b, c, c_stride, dtype, accumulate != 0, stream);
     ProductArgs p = {};
     p.a_scales = static_cast<const uint8_t *>(a->scales);
     p.b_scales = static_cast<const uint8_t *>(b->scales);
@@ -1099,10 +1035,8 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     p.steps = (int)ceil_div(k, STEP);
     p.c = c;
     p.c_row = c_stride;
-    p.c_col = 1;
     p.c_bf16 = dtype == DIPACO_BF16;
     p.accumulate = accumulate != 0;
-    if (is_skinny(m, n)) return launch_skinny(a, b, p, k, stream);
 
     if (ceil_div(m, PAIR_ROWS) * ceil_div(n, 64) > INT32_MAX) return DIPACO_ELIMIT;
     const PairPlan plan = plan_pairs(m, n, p.steps);
@@ -1117,7 +1051,7 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     CUtensorMap a_map, b_map, c_map = {};
     if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, transpose_b ? plan.tile_n / 2 : 128)) return DIPACO_ECUDA;
     p.store_by_tma = !accumulate && rows_aligned16(c, c_stride, m, dense_size(dtype));
-    if (p.store_by_tma && !result_map(&c_map, c, m, n, c_stride, dtype)) return DIPACO_ECUDA;
+    if (p.store_by_tma && !result_map(&c_map, c, m, n, m == 1 ? ceil_div(n, 8) * 8 : c_stride, dtype)) return DIPACO_ECUDA;
     if (const int rc = p.c_bf16 ? launch_pairs<false>(a_map, b_map, c_map, p, plan.pairs, stream)
                                 : launch_pairs<true>(a_map, b_map, c_map, p, plan.pairs, stream))
         return rc;

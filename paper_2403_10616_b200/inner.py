@@ -15,7 +15,9 @@ import torch
 from . import binding as B
 
 BLOCK = 128  # one scale per BLOCK x BLOCK values
+_F32, _E4M3, _E8M0 = torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu
 _CODES = {torch.float32: B.DIPACO_F32, torch.bfloat16: B.DIPACO_BF16}
+_stream = torch._C._cuda_getCurrentRawStream  # of a device index
 
 
 class Packed:
@@ -40,10 +42,8 @@ class Packed:
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Packed":
-        stride = -(-cols // 16) * 16
-        codes = torch.empty((rows, stride), dtype=torch.float8_e4m3fn, device=device)
-        scales = torch.empty((-(-rows // BLOCK), -(-cols // BLOCK)), dtype=torch.float8_e8m0fnu, device=device)
-        return cls(codes if stride == cols else codes[:, :cols], scales)
+        """A packed matrix with nothing in it yet."""
+        return _packed_beside(torch.empty(0, device=device), rows, cols)
 
     @property
     def shape(self) -> Tuple[int, int]:
@@ -54,8 +54,16 @@ class Packed:
         return self.codes.device
 
 
-def _stream(device: torch.device) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index)
+def _packed_beside(x: torch.Tensor, rows: int, cols: int) -> Packed:
+    """An empty packed matrix on x's device."""
+    stride = (cols + 15) & ~15
+    codes = x.new_empty((rows, stride), dtype=_E4M3)
+    scales = x.new_empty(((rows + 127) >> 7, (cols + 127) >> 7), dtype=_E8M0)
+    p = object.__new__(Packed)
+    p.codes = codes if stride == cols else codes[:, :cols]
+    p.scales = scales
+    p.struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
+    return p
 
 
 def _dense(name: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
@@ -64,31 +72,37 @@ def _dense(name: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
     if code is None or x.dim() != 2 or not x.is_cuda:
         raise ValueError("%s must be a float32 or bfloat16 matrix on a CUDA device" % name)
     rows, cols = x.shape
-    if cols > 1 and x.stride(1) != 1:
+    stride, unit = x.stride()
+    if unit != 1 and cols > 1:
         raise ValueError("%s must be row-major" % name)
-    return rows, cols, x.stride(0), code
+    return rows, cols, stride, code
 
 
-def _params(cols: int, device, gamma, beta) -> Tuple[Optional[int], Optional[int], int]:
+def _param(cols: int, dev: int, t: torch.Tensor) -> Tuple[int, int]:
+    """(pointer, dtype code) of gamma or beta."""
+    code = _CODES.get(t.dtype)
+    if code is None or t.shape != (cols,) or t.get_device() != dev or (cols > 1 and t.stride(0) != 1):
+        raise ValueError("gamma and beta must be contiguous float32 or bfloat16 vectors of the row's length")
+    return t.data_ptr(), code
+
+
+def _params(cols: int, dev: int, gamma, beta) -> Tuple[Optional[int], Optional[int], int]:
     """Pointers of gamma and beta and their common dtype code."""
-    code = None
-    for t in (gamma, beta):
-        if t is None:
-            continue
-        if t.shape != (cols,) or t.dtype not in _CODES or t.device != device or (cols > 1 and t.stride(0) != 1):
-            raise ValueError("gamma and beta must be contiguous float32 or bfloat16 vectors of the row's length")
-        if code not in (None, _CODES[t.dtype]):
-            raise ValueError("gamma and beta must have one dtype")
-        code = _CODES[t.dtype]
-    return (None if gamma is None else gamma.data_ptr(), None if beta is None else beta.data_ptr(),
-            B.DIPACO_F32 if code is None else code)
+    g, code = (None, B.DIPACO_F32) if gamma is None else _param(cols, dev, gamma)
+    if beta is None:
+        return g, None, code
+    b, beta_code = _param(cols, dev, beta)
+    if gamma is not None and beta_code != code:
+        raise ValueError("gamma and beta must have one dtype")
+    return g, b, beta_code
 
 
 def pack(x: torch.Tensor) -> Packed:
     """The packed form of a dense matrix."""
     rows, cols, stride, code = _dense("x", x)
-    out = Packed.empty(rows, cols, x.device)
-    B.dipaco_pack(x.data_ptr(), stride, code, out.struct, x.device.index, _stream(x.device))
+    dev = x.get_device()
+    out = _packed_beside(x, rows, cols)
+    B.dipaco_pack(x.data_ptr(), stride, code, out.struct, dev, _stream(dev))
     return out
 
 
@@ -96,8 +110,9 @@ def unpack(x: Packed, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values that a packed matrix stands for."""
     if dtype not in _CODES:
         raise ValueError("dtype must be float32 or bfloat16")
-    y = torch.empty(x.shape, dtype=dtype, device=x.device)
-    B.dipaco_unpack(x.struct, y.data_ptr(), y.stride(0), _CODES[dtype], x.device.index, _stream(x.device))
+    dev = x.codes.get_device()
+    y = x.codes.new_empty(x.shape, dtype=dtype)
+    B.dipaco_unpack(x.struct, y.data_ptr(), y.stride(0), _CODES[dtype], dev, _stream(dev))
     return y
 
 
@@ -105,16 +120,16 @@ def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Opti
                eps: float = 1e-5, stats: bool = False):
     """The norm of every row of x, in x's dtype; with ``stats`` (y, mean, rstd) for the backward pass."""
     rows, cols, stride, code = _dense("x", x)
-    dev = x.device
+    dev = x.get_device()
     g, b, pcode = _params(cols, dev, gamma, beta)
-    y = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    y = x.new_empty((rows, cols))
     if not stats:
         B.dipaco_layer_norm(x.data_ptr(), stride, g, b, y.data_ptr(), cols, None, None, rows, cols, eps, code, pcode,
-                            dev.index, _stream(dev))
+                            dev, _stream(dev))
         return y
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    mean, rstd = x.new_empty((2, rows), dtype=_F32).unbind(0)
     B.dipaco_layer_norm(x.data_ptr(), stride, g, b, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), rows, cols,
-                        eps, code, pcode, dev.index, _stream(dev))
+                        eps, code, pcode, dev, _stream(dev))
     return y, mean, rstd
 
 
@@ -123,13 +138,13 @@ def layer_norm_pack(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta:
     """(y, x, mean, rstd): the norm of every row of x, packed, and x itself packed as the checkpoint
     that ``layer_norm_backward`` reads (None without ``keep``)."""
     rows, cols, stride, code = _dense("x", x)
-    dev = x.device
+    dev = x.get_device()
     g, b, pcode = _params(cols, dev, gamma, beta)
-    y = Packed.empty(rows, cols, dev)
-    kept = Packed.empty(rows, cols, dev) if keep else None
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    y = _packed_beside(x, rows, cols)
+    kept = _packed_beside(x, rows, cols) if keep else None
+    mean, rstd = x.new_empty((2, rows), dtype=_F32).unbind(0)
     B.dipaco_layer_norm_pack(x.data_ptr(), stride, g, b, y.struct, kept.struct if keep else None, mean.data_ptr(),
-                             rstd.data_ptr(), eps, code, pcode, dev.index, _stream(dev))
+                             rstd.data_ptr(), eps, code, pcode, dev, _stream(dev))
     return y, kept, mean, rstd
 
 
@@ -137,28 +152,28 @@ def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], mean: 
                         gamma: Optional[torch.Tensor] = None):
     """(dx, dgamma, dbeta) from the norm's input or its packed checkpoint; dgamma and dbeta are fp32."""
     rows, cols, stride, code = _dense("dy", dy)
-    dev = dy.device
+    dev = dy.get_device()
     g, _, pcode = _params(cols, dev, gamma, None)
-    if tuple(x.shape) != (rows, cols) or x.device != dev:
-        raise ValueError("x and dy must have one shape and device")
     for t in (mean, rstd):
-        if t.shape != (rows,) or t.dtype != torch.float32 or t.device != dev or not t.is_contiguous():
+        if t.shape != (rows,) or t.dtype != _F32 or t.get_device() != dev or not t.is_contiguous():
             raise ValueError("mean and rstd must be contiguous float32 vectors with one entry per row")
-    x_ptr, x_stride, packed = None, 0, None
     if isinstance(x, Packed):
-        packed = x.struct
+        x_ptr, x_stride, packed = None, 0, x.struct
+        x_shape, x_dev = x.shape, x.codes.get_device()
     else:
-        _, _, x_stride, x_code = _dense("x", x)
+        *x_shape, x_stride, x_code = _dense("x", x)
         if x_code != code:
             raise ValueError("x and dy must have one dtype")
-        x_ptr = x.data_ptr()
-    dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
-    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dev).unbind(0)
+        x_ptr, packed, x_dev = x.data_ptr(), None, x.get_device()
+    if tuple(x_shape) != (rows, cols) or x_dev != dev:
+        raise ValueError("x and dy must have one shape and device")
+    dx = dy.new_empty((rows, cols))
+    dgamma, dbeta = dy.new_empty((2, cols), dtype=_F32).unbind(0)
     need = B.dipaco_layer_norm_workspace(rows, cols)
-    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    work = dy.new_empty(need, dtype=torch.uint8) if need else None
     B.dipaco_layer_norm_backward(dy.data_ptr(), stride, x_ptr, x_stride, packed, mean.data_ptr(), rstd.data_ptr(), g,
                                  dx.data_ptr(), cols, dgamma.data_ptr(), dbeta.data_ptr(), rows, cols, code, pcode,
-                                 work.data_ptr() if need else None, need, dev.index, _stream(dev))
+                                 work.data_ptr() if need else None, need, dev, _stream(dev))
     return dx, dgamma, dbeta
 
 
@@ -166,21 +181,21 @@ def gelu_pack(x: torch.Tensor, keep: bool = True):
     """(y, x): the GELU of x, packed, and x itself packed as the checkpoint that
     ``gelu_pack_backward`` reads (None without ``keep``)."""
     rows, cols, stride, code = _dense("x", x)
-    y = Packed.empty(rows, cols, x.device)
-    kept = Packed.empty(rows, cols, x.device) if keep else None
-    B.dipaco_gelu_pack(x.data_ptr(), stride, code, y.struct, kept.struct if keep else None, x.device.index,
-                       _stream(x.device))
+    dev = x.get_device()
+    y = _packed_beside(x, rows, cols)
+    kept = _packed_beside(x, rows, cols) if keep else None
+    B.dipaco_gelu_pack(x.data_ptr(), stride, code, y.struct, kept.struct if keep else None, dev, _stream(dev))
     return y, kept
 
 
 def gelu_pack_backward(dy: torch.Tensor, x: Packed) -> Packed:
     """dy * gelu'(x), packed, from the GELU's packed input."""
     rows, cols, stride, code = _dense("dy", dy)
-    if x.shape != (rows, cols) or x.device != dy.device:
+    dev = dy.get_device()
+    if x.shape != (rows, cols) or x.codes.get_device() != dev:
         raise ValueError("x and dy must have one shape and device")
-    dx = Packed.empty(rows, cols, dy.device)
-    B.dipaco_gelu_pack_backward(dy.data_ptr(), stride, code, x.struct, dx.struct, dy.device.index,
-                                _stream(dy.device))
+    dx = _packed_beside(dy, rows, cols)
+    B.dipaco_gelu_pack_backward(dy.data_ptr(), stride, code, x.struct, dx.struct, dev, _stream(dev))
     return dx
 
 
@@ -195,26 +210,27 @@ def packed_matmul(a: Packed, b: Packed, transpose_a: bool = False, transpose_b: 
         m, k = k, m
     if transpose_b:
         k2, n = n, k2
-    dev = a.device
-    if k != k2 or b.device != dev:
+    dev = a.codes.get_device()
+    if k != k2 or b.codes.get_device() != dev:
         raise ValueError("the operands' contracted extents (%d and %d) and devices must agree" % (k, k2))
     if out is None:
-        if accumulate or out_dtype not in _CODES:
+        code = _CODES.get(out_dtype)
+        if accumulate or code is None:
             raise ValueError("accumulate needs out, and out_dtype is float32 or bfloat16")
-        out, stride, code = torch.empty((m, n), dtype=out_dtype, device=dev), n, _CODES[out_dtype]
+        out, stride = a.codes.new_empty((m, n), dtype=out_dtype), n
     else:
         rows, cols, stride, code = _dense("out", out)
-        if (rows, cols) != (m, n) or out.device != dev:
+        if (rows, cols) != (m, n) or out.get_device() != dev:
             raise ValueError("out must be [%d, %d] on the operands' device" % (m, n))
     need = B.dipaco_packed_matmul_workspace(m, n, k)
-    work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    work = a.codes.new_empty(need, dtype=torch.uint8) if need else None
     B.dipaco_packed_matmul(a.struct, b.struct, transpose_a, transpose_b, out.data_ptr(), stride, code, accumulate,
-                           work.data_ptr() if need else None, need, dev.index, _stream(dev))
+                           work.data_ptr() if need else None, need, dev, _stream(dev))
     return out
 
 
 def inner_status(device=None) -> int:
     """Waits for the current stream and reports DIPACO_OK, or DIPACO_ETIMEOUT once after a bounded
     wait inside one of these operators ran out."""
-    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    return B.dipaco_inner_status(dev.index or 0, torch.cuda.current_stream(dev).cuda_stream)
+    dev = torch.cuda.current_device() if device is None else torch.device(device).index or 0
+    return B.dipaco_inner_status(dev, _stream(dev))
