@@ -272,6 +272,9 @@ struct NormBackArgs {
     bool params_bf16, gamma_aligned;
 };
 
+// Bytes of the 16-byte units that hold n bytes at p.
+__device__ __forceinline__ int around(const uint8_t *p, int n) { return ((int)((uintptr_t)p & 15) + n + 15) & ~15; }
+
 // The first n of 16 bytes to shared memory, the others zero.
 __device__ __forceinline__ void copy_filled(void *to, const void *from, int n)
 {
@@ -281,13 +284,13 @@ __device__ __forceinline__ void copy_filled(void *to, const void *from, int n)
 static __device__ int g_norm_error;  // set by a bounded wait that ran out
 constexpr int BACK_MAX_STAGES = 4;
 
-// How the threads of a block share rows: TPR threads for a row, each with two units of 16 bytes of it (or 16
-// single values), ROWS rows at a time.  SYNC threads go together; the block's others go their own way.
+// How the threads of a block share rows: TPR threads for a row, each with 32 bytes of it (two
+// units of 16, or single values), ROWS rows at a time.  SYNC threads go together; the block's others go their own way.
 template <typename T, bool PACKED, bool VEC, int TPR> struct BackShape {
     static constexpr int U = VEC ? 16 / (int)sizeof(T) : 1;
-    static constexpr int E = VEC ? 2 * U : 16;
+    static constexpr int E = 32 / (int)sizeof(T);
     static constexpr int UNITS = E / U;
-    static constexpr int ROWS = VEC && TPR <= 256 ? 2 : 1;
+    static constexpr int ROWS = TPR <= 256 ? 2 : 1;
     static constexpr int THREADS = TPR < 512 ? 512 : TPR;
     static constexpr int GROUPS = THREADS / TPR;
     static constexpr int SYNC = TPR < 32 ? 32 : TPR;  // threads that take rows together: whole warps
@@ -335,9 +338,10 @@ __device__ __forceinline__ float warp_sum4(const float *v)
 
 // The sums of dgamma and dbeta stay in registers, as each thread has the same columns of every row that its
 // block passes over, and leave the block once.  Two rows are taken at a time, which halves the work of
-// their reductions.  Rows on 16-byte boundaries (VEC) are brought to shared memory by bulk copies, a few
-// steps ahead: a thread has no registers to spare for them.  A last, partial unit of a row is copied by
-// itself and filled up with zeros, which take no part in any sum.
+// their reductions.  Rows are brought to shared memory by bulk copies, a few steps ahead: a thread has no
+// registers to spare for them (4999x2047 in fp32 from registers: 50 us).  On 16-byte boundaries (VEC) a last,
+// partial unit of a row is copied by itself and filled up with zeros, which take no part in any sum; rows
+// elsewhere are copied with the 16-byte units around them and read value by value.
 template <typename T, bool PACKED, bool VEC, int TPR>
 __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
     norm_back_kernel(const __grid_constant__ NormBackArgs a, int stages, int dy_bytes, int x_bytes)
@@ -357,39 +361,48 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
     const float inv_cols = 1.0f / (float)a.cols;
     const int row_bytes = dy_bytes + x_bytes, stage_bytes = S::TAKEN * row_bytes;
     uint8_t *ring = raw_ring + ((128u - (ptx::smem_addr(raw_ring) & 127u)) & 127u) + sync * stages * stage_bytes;
-    const int dy_tail = a.cols * (int)sizeof(T) & 15, x_tail = a.cols * (int)sizeof(typename S::X) & 15;
-    const int dy_whole = dy_bytes - (dy_tail ? 16 : 0), x_whole = x_bytes - (x_tail ? 16 : 0);
+    constexpr bool X_UNITS = VEC || PACKED;  // rows of x on 16-byte boundaries
+    const int dy_row_bytes = a.cols * (int)sizeof(T), x_row_bytes = a.cols * (int)sizeof(typename S::X);
+    const int dy_tail = VEC ? dy_row_bytes & 15 : 0, x_tail = VEC ? x_row_bytes & 15 : 0;
 
     const int step = (int)gridDim.x * S::SYNCS * S::TAKEN, begin = ((int)blockIdx.x * S::SYNCS + sync) * S::TAKEN;
     // one thread: the rows from `first` on into a stage
     const auto request = [&](int first, int stage) {
         const int rows = min(S::TAKEN, a.rows - first);
-        ptx::mbar_arrive_expect_tx(&full[stage], rows * (dy_whole + x_whole));
         uint8_t *to = ring + stage * stage_bytes;
         const uint8_t *dy = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.dy) + first * a.dy_stride);
         const uint8_t *x = reinterpret_cast<const uint8_t *>(static_cast<const typename S::X *>(a.x) + first * a.x_stride);
-        for (int r = 0; r < rows; ++r) {
-            if (dy_whole) ptx::bulk_load(to, dy, dy_whole, &full[stage]);
-            if (x_whole) ptx::bulk_load(to + dy_bytes, x, x_whole, &full[stage]);
-            if (dy_tail) copy_filled(to + dy_whole, dy + dy_whole, dy_tail);
-            if (x_tail) copy_filled(to + dy_bytes + x_whole, x + x_whole, x_tail);
-            to += row_bytes;
-            dy += a.dy_stride * (long long)sizeof(T);
-            x += a.x_stride * (long long)sizeof(typename S::X);
+        const long long dy_step = a.dy_stride * (long long)sizeof(T), x_step = a.x_stride * (long long)sizeof(typename S::X);
+        if constexpr (VEC) {
+            const int dy_whole = dy_row_bytes & ~15, x_whole = x_row_bytes & ~15;
+            ptx::mbar_arrive_expect_tx(&full[stage], rows * (dy_whole + x_whole));
+            for (int r = 0; r < rows; ++r, to += row_bytes, dy += dy_step, x += x_step) {
+                if (dy_whole) ptx::bulk_load(to, dy, dy_whole, &full[stage]);
+                if (x_whole) ptx::bulk_load(to + dy_bytes, x, x_whole, &full[stage]);
+                if (dy_tail) copy_filled(to + dy_whole, dy + dy_whole, dy_tail);
+                if (x_tail) copy_filled(to + dy_bytes + x_whole, x + x_whole, x_tail);
+            }
+            if (dy_tail || x_tail)  // arrives when this thread's own copies have landed
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(ptx::smem_addr(&full[stage])) : "memory");
+        } else {
+            int bytes = 0;
+            for (int r = 0; r < rows; ++r)
+                bytes += around(dy + r * dy_step, dy_row_bytes) + around(x + r * x_step, x_row_bytes);
+            ptx::mbar_arrive_expect_tx(&full[stage], bytes);
+            for (int r = 0; r < rows; ++r, to += row_bytes, dy += dy_step, x += x_step) {
+                ptx::bulk_load(to, dy - ((uintptr_t)dy & 15), around(dy, dy_row_bytes), &full[stage]);
+                ptx::bulk_load(to + dy_bytes, x - ((uintptr_t)x & 15), around(x, x_row_bytes), &full[stage]);
+            }
         }
-        if (dy_tail || x_tail)  // arrives when this thread's own copies have landed
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(ptx::smem_addr(&full[stage])) : "memory");
     };
-    if constexpr (VEC) {
-        if (in_sync == 0) {
-            for (int s = 0; s < stages; ++s) ptx::mbar_init(&full[s], dy_tail || x_tail ? 2 : 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        __syncthreads();
-        if (in_sync == 0)
-            for (int s = 0; s < stages; ++s)
-                if (begin + s * (long long)step < a.rows) request(begin + s * step, s);
+    if (in_sync == 0) {
+        for (int s = 0; s < stages; ++s) ptx::mbar_init(&full[s], dy_tail || x_tail ? 2 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncthreads();
+    if (in_sync == 0)
+        for (int s = 0; s < stages; ++s)
+            if (begin + s * (long long)step < a.rows) request(begin + s * step, s);
 
     f32x2 gamma[E / 2], sum_g[E / 2], sum_b[E / 2];
 #pragma unroll
@@ -433,34 +446,29 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
     };
     look_ahead(row);
     T *dx = static_cast<T *>(a.dx) + row * a.dx_stride + column;
-    const T *dy_row = static_cast<const T *>(a.dy) + row * a.dy_stride + column;
-    const typename S::X *x_row = static_cast<const typename S::X *>(a.x) + row * a.x_stride + column;
+    // where a row starts inside its first unit
+    unsigned dy_at = (unsigned)(uintptr_t)(static_cast<const T *>(a.dy) + row * a.dy_stride);
+    unsigned x_at = (unsigned)(uintptr_t)(static_cast<const typename S::X *>(a.x) + row * a.x_stride);
+    const unsigned dy_step = (unsigned)(a.dy_stride * (long long)sizeof(T)), x_step = (unsigned)(a.x_stride * (long long)sizeof(typename S::X));
     int parity = 0, stage = 0;
     unsigned phase = 0;
     for (int first = begin; first < a.rows; first += step, row += step) {
-        if constexpr (VEC) {
-            if (!bounded_wait(&full[stage], phase, &g_norm_error, 1)) {
-                for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
-                return;
-            }
+        if (!bounded_wait(&full[stage], phase, &g_norm_error, 1)) {
+            for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
+            return;
         }
         const uint8_t *mine = ring + stage * stage_bytes + in_sync / TPR * ROWS * row_bytes;
-        f32x2 hat[ROWS][E / 2];
-        f32x2 kept[VEC ? 1 : E / 2];  // dy, where it is not in shared memory
-        T dy1[VEC ? 1 : UNITS];
-        typename S::X x1[VEC ? 1 : UNITS];
-        if constexpr (!VEC) {  // all loads at once; beyond the row its first value of this thread
-            if (row < a.rows) {
-#pragma unroll
-                for (int j = 0; j < UNITS; ++j) {
-                    const int c = j * TPR < cols ? j * TPR : 0;
-                    if (cols > 0) {
-                        dy1[j] = dy_row[c];
-                        x1[j] = x_row[c];
-                    }
-                }
+        // the pairs of dy of unit j, or of single values j and j + 1, of row k
+        const auto dy_pairs = [&](int k, int j, f32x2 *p) {
+            if constexpr (VEC) {
+                widen_pairs<T>(reinterpret_cast<const uint4 *>(mine + k * row_bytes)[lane + j * TPR], p);
+            } else {
+                const T *r = reinterpret_cast<const T *>(mine + k * row_bytes + (dy_at + k * dy_step & 15u)) + column + j * TPR;
+                const bool both = (j + 1) * TPR < cols;
+                p[0] = pair_of(widen1<T>(r[0]), both ? widen1<T>(r[TPR]) : 0.0f);
             }
-        }
+        };
+        f32x2 hat[ROWS][E / 2];
         f32x2 sum2[4] = {0ull, 0ull, 0ull, 0ull};  // of g and g h, of either row
         float rstd[ROWS];
 #pragma unroll
@@ -472,16 +480,17 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
                     const int c = j * TPR * U;
                     if (c < cols) {
                         f32x2 dy[PAIRS], *h = hat[k] + j * PAIRS / SINGLE;
+                        dy_pairs(k, j, dy);
+                        const uint8_t *at = mine + k * row_bytes + dy_bytes;
                         if constexpr (VEC) {
-                            const uint8_t *at = mine + k * row_bytes;
-                            widen_pairs<T>(reinterpret_cast<const uint4 *>(at)[lane + j * TPR], dy);
-                            const typename S::RawX x = reinterpret_cast<const typename S::RawX *>(at + dy_bytes)[lane + j * TPR];
+                            const typename S::RawX x = reinterpret_cast<const typename S::RawX *>(at)[lane + j * TPR];
                             S::centred(&x, PACKED ? scale_value(scale_ahead[PACKED ? j : 0]) : 0.0f, 0.0f, mean_ahead[k], h);
                         } else {
+                            const typename S::RawX *r =
+                                reinterpret_cast<const typename S::RawX *>(at + (X_UNITS ? 0u : x_at + k * x_step & 15u)) + column + c;
                             const bool both = c + TPR < cols;  // the second value is inside too
-                            dy[0] = kept[j / 2] = pair_of(widen1<T>(dy1[j]), both ? widen1<T>(dy1[j + 1]) : 0.0f);
-                            S::centred(reinterpret_cast<const typename S::RawX *>(x1 + j),
-                                       PACKED ? scale_value(scale_ahead[PACKED ? j : 0]) : 0.0f,
+                            const typename S::RawX x[2] = {r[0], r[both ? TPR : 0]};
+                            S::centred(x, PACKED ? scale_value(scale_ahead[PACKED ? j : 0]) : 0.0f,
                                        PACKED ? scale_value(scale_ahead[PACKED ? (both ? j + 1 : j) : 0]) : 0.0f, mean_ahead[k], h);
                         }
 #pragma unroll
@@ -534,10 +543,8 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
             }
             parity ^= 1;
         }
-        if constexpr (VEC) {
-            const long long next = first + (stages - 1) * (long long)step;
-            if (in_sync == 0 && first != begin && next < a.rows) request((int)next, stage == 0 ? stages - 1 : stage - 1);
-        }
+        const long long next = first + (stages - 1) * (long long)step;
+        if (in_sync == 0 && first != begin && next < a.rows) request((int)next, stage == 0 ? stages - 1 : stage - 1);
         if (a.dx) {
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
@@ -549,10 +556,7 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
                     const int c = j * TPR * U;
                     if (c >= cols) continue;
                     f32x2 r[PAIRS];
-                    if constexpr (VEC)
-                        widen_pairs<T>(reinterpret_cast<const uint4 *>(mine + k * row_bytes)[lane + j * TPR], r);
-                    else
-                        r[0] = kept[j / 2];
+                    dy_pairs(k, j, r);
 #pragma unroll
                     for (int i = 0; i < PAIRS; ++i) {
                         const int e = j * PAIRS / SINGLE + i;
@@ -573,8 +577,8 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
             }
         }
         dx += step * a.dx_stride;
-        dy_row += step * a.dy_stride;
-        x_row += step * a.x_stride;
+        dy_at += step * dy_step;
+        x_at += step * x_step;
         if (++stage == stages) { stage = 0; phase ^= 1; }
     }
 
@@ -687,20 +691,20 @@ __global__ void __launch_bounds__(1024) norm_back_join_kernel(const float *parts
 
 constexpr int BACK_LONG_SHARES = 32;
 
-// The widest row that a block holds, and the threads for a row: two units of 16 bytes each, or 16 values.
+// The widest row that a block holds, and the threads for a row: 32 bytes each.
 int64_t back_widest(int dtype) { return dtype == DIPACO_BF16 ? 16384 : 8192; }
-int back_threads_per_row(int64_t cols, int dtype, bool vec)
+int back_threads_per_row(int64_t cols, int dtype)
 {
     int tpr = 8;
-    while (tpr * (vec ? 32 / dense_size(dtype) : 16) < cols) tpr *= 2;
+    while (tpr * (32 / dense_size(dtype)) < cols) tpr *= 2;
     return tpr;
 }
 
 // Blocks that write their own sums of dgamma and dbeta.
-int64_t back_parts(int64_t rows, int64_t cols, int dtype, bool vec)
+int64_t back_parts(int64_t rows, int64_t cols, int dtype)
 {
     if (cols > back_widest(dtype)) return std::min<int64_t>(BACK_LONG_SHARES, ceil_div(rows, 64));
-    const int tpr = back_threads_per_row(cols, dtype, vec), rows_at_once = vec && tpr <= 256 ? 2 : 1;
+    const int tpr = back_threads_per_row(cols, dtype), rows_at_once = tpr <= 256 ? 2 : 1;
     return std::min<int64_t>(148, ceil_div(rows, std::max(tpr, 512) / tpr * rows_at_once));
 }
 
@@ -708,17 +712,14 @@ template <typename T, bool PACKED, bool VEC, int TPR>
 int launch_back_shape(const NormBackArgs &a, int blocks, cudaStream_t stream)
 {
     using S = BackShape<T, PACKED, VEC, TPR>;
-    int stages = 1, dy_bytes = 0, x_bytes = 0, smem = 0;
-    if (VEC) {
-        dy_bytes = (int)ceil_div(a.cols * (int)sizeof(T), 16) * 16;
-        x_bytes = (int)ceil_div(a.cols * (int)sizeof(typename S::X), 16) * 16;
-        const int stage = S::SYNCS * S::TAKEN * (dy_bytes + x_bytes);
-        stages = std::max(2, std::min(BACK_MAX_STAGES, 192 * 1024 / stage));
-        smem = stages * stage + 128;
-        if (cudaFuncSetAttribute(norm_back_kernel<T, PACKED, VEC, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
-            cudaSuccess)
-            return launch_status();
-    }
+    // of a row in shared memory; rows that start inside a unit can take one more
+    const int dy_bytes = (int)ceil_div(a.cols * (int)sizeof(T), 16) * 16 + (VEC ? 0 : 16);
+    const int x_bytes = (int)ceil_div(a.cols * (int)sizeof(typename S::X), 16) * 16 + (VEC || PACKED ? 0 : 16);
+    const int stage = S::SYNCS * S::TAKEN * (dy_bytes + x_bytes);
+    const int stages = std::max(2, std::min(BACK_MAX_STAGES, 192 * 1024 / stage)), smem = stages * stage + 128;
+    if (cudaFuncSetAttribute(norm_back_kernel<T, PACKED, VEC, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
+        cudaSuccess)
+        return launch_status();
     norm_back_kernel<T, PACKED, VEC, TPR><<<blocks, S::THREADS, smem, stream>>>(a, stages, dy_bytes, x_bytes);
     return launch_status();
 }
@@ -726,7 +727,7 @@ int launch_back_shape(const NormBackArgs &a, int blocks, cudaStream_t stream)
 template <typename T, bool PACKED, bool VEC>
 int launch_back(const NormBackArgs &a, int blocks, cudaStream_t stream)
 {
-    switch (back_threads_per_row(a.cols, sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32, VEC)) {
+    switch (back_threads_per_row(a.cols, sizeof(T) == 2 ? DIPACO_BF16 : DIPACO_F32)) {
     case 8: return launch_back_shape<T, PACKED, VEC, 8>(a, blocks, stream);
     case 16: return launch_back_shape<T, PACKED, VEC, 16>(a, blocks, stream);
     case 32: return launch_back_shape<T, PACKED, VEC, 32>(a, blocks, stream);
@@ -792,10 +793,8 @@ int dipaco_layer_norm_workspace(int64_t rows, int64_t cols, int64_t *bytes)
 {
     if (!bytes) return DIPACO_EINVAL;
     if (const int rc = check_extents(rows, cols)) return rc;
-    int64_t parts = 0;  // the most of either dtype and alignment
-    if (rows > 0 && cols > 0)
-        for (int dtype : {DIPACO_F32, DIPACO_BF16})
-            for (bool vec : {false, true}) parts = std::max(parts, back_parts(rows, cols, dtype, vec));
+    int64_t parts = 0;  // the most of either dtype
+    if (rows > 0 && cols > 0) parts = std::max(back_parts(rows, cols, DIPACO_F32), back_parts(rows, cols, DIPACO_BF16));
     *bytes = parts > 1 ? parts * 2 * cols * (int64_t)sizeof(float) : 0;
     return DIPACO_OK;
 }
@@ -835,7 +834,7 @@ int dipaco_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
     const int size = dense_size(dtype);
     const bool vec = rows_aligned16(dy, dy_stride, rows, size) && (!x || rows_aligned16(x, x_stride, rows, size)) &&
                      (!dx || rows_aligned16(dx, dx_stride, rows, size));
-    const int parts = (int)back_parts(rows, cols, dtype, vec);
+    const int parts = (int)back_parts(rows, cols, dtype);
     NormBackArgs a = {};
     a.dy = dy;
     a.x = x_packed ? x_packed->codes : x;
