@@ -382,6 +382,27 @@ def test_gelu_of_extreme_values(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gelu_of_values_far_below_zero_beside_others(dtype):
+    """Large negative values, infinities and NaN share pairs, warps and blocks with ordinary ones."""
+    x = torch.randn(256, 256, generator=gen(4)) * 2
+    x[5, 10:20] = torch.tensor([-7.0, -8.0, -9.0, -9.9, -10.5, -20.0, -1e4, -1e30, -7.6, -7.7])
+    x[130:140] = -9.0 - torch.rand(10, 256, generator=gen(5))
+    x[200, ::2] = -30.0
+    x = x.to(dtype)
+    y, _ = inner.gelu_pack(place(x))
+    want = ref.gelu(x)
+    ref.assert_packed_close(y.codes, y.scales, want, 16 * U * want.abs() + 8 * U * x.double().abs() *
+                            (2.0 * x.double() ** 2 + 4).clamp(max=64.0) * torch.exp(-x.double().abs()))
+    clean = ref.values(y.codes, y.scales)
+    x[5, 11], x[60, 3], x[61, 7] = math.nan, math.inf, -math.inf
+    y, _ = inner.gelu_pack(place(x))
+    got = ref.values(y.codes, y.scales)
+    assert int(torch.isnan(got).sum()) == 3
+    assert torch.equal(torch.nan_to_num(got)[~torch.isnan(got)], clean[~torch.isnan(got)])
+
+
+@pytest.mark.gpu
 def test_gelu_gradient_against_differences():
     """dy * gelu' from the checkpoint against central differences of the 64-bit GELU at its values."""
     x, xd = matrix(8, 256, 128, F32, 2.0)
