@@ -62,6 +62,19 @@ __device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, unsigned parity)
         : "memory");
     return ok != 0;
 }
+// Whether the phase is over, without waiting.
+__device__ __forceinline__ bool test_arrived(uint64_t *bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(ptx::smem_addr(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 // Bounded, and ordered after what other blocks of the cluster did before they arrived.
 __device__ __forceinline__ bool wait_cluster(uint64_t *bar, unsigned parity, int code)
 {
@@ -140,7 +153,16 @@ __device__ __forceinline__ void tmem_load32(uint32_t address, uint32_t *r)
           "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(address));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// Waits for the loads so far; names the registers, which hold nothing before.
+__device__ __forceinline__ void tmem_wait(uint32_t *r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+                   "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                   "+r"(r[30]), "+r"(r[31])::"memory");
 }
 
 // ------------------------------------------------------------------------------------------ descriptors
@@ -222,7 +244,7 @@ __device__ __forceinline__ void store_c(const ProductArgs &p, long long row, lon
 // first set's last columns are the second's first.  They are read out first, and the products of the
 // next tile start as soon as that is done; with fewer columns the sets are apart and the next tile's
 // products only wait for the tile before the last to be read out.
-constexpr int PAIR_STAGES = 6;
+constexpr int PAIR_STAGES = 5;
 constexpr int PAIR_OPERAND_BYTES = 128 * STEP;
 constexpr int PAIR_STAGE_BYTES = 2 * PAIR_OPERAND_BYTES;
 constexpr int PAIR_WORDS_BYTES = 3 * SCALE_BYTES;  // scale words of a quad: of A, and of B twice four columns
@@ -231,10 +253,11 @@ constexpr int PAIR_WORDS_BYTES = 3 * SCALE_BYTES;  // scale words of a quad: of 
 constexpr int PAIR_WORDS_STEPS = 8;
 constexpr int PAIR_WORDS_SET = PAIR_WORDS_STEPS / QUAD * PAIR_WORDS_BYTES;
 constexpr int PAIR_EPILOGUE_WARPS = 8;
-constexpr int PAIR_STAGING_BYTES = 2048;  // per epilogue warp: 32 rows of 64 bytes
+constexpr int PAIR_STAGING = 3;           // buffers of an epilogue warp
+constexpr int PAIR_STAGING_BYTES = 2048;  // of one: 32 rows of 64 bytes
 // shared memory: operands and staging on 1024-byte boundaries (the swizzle goes by address), then scale words
 constexpr int PAIR_STAGING_AT = PAIR_STAGES * PAIR_STAGE_BYTES;
-constexpr int PAIR_WORDS_AT = PAIR_STAGING_AT + PAIR_EPILOGUE_WARPS * PAIR_STAGING_BYTES;
+constexpr int PAIR_WORDS_AT = PAIR_STAGING_AT + PAIR_EPILOGUE_WARPS * PAIR_STAGING * PAIR_STAGING_BYTES;
 constexpr int PAIR_SMEM = PAIR_WORDS_AT + 2 * PAIR_WORDS_SET + 1024;
 constexpr int PAIR_THREADS = (PAIR_EPILOGUE_WARPS + 3) * 32;  // + loads, products, scale words
 // Scale columns are written again five quads later, when the last step of the quad that had them is done:
@@ -244,7 +267,7 @@ constexpr int PAIR_SCALE_COLUMNS = 12;
 constexpr int PAIR_SCALE_SLOTS = 5;
 constexpr int PAIR_SCALES_AT = 512 - PAIR_SCALE_SLOTS * PAIR_SCALE_COLUMNS;
 // With 256 columns the sets of sums share 60, the first two groups of 32 that are read out.
-static_assert(PAIR_SCALE_SLOTS < PAIR_STAGES && 2 * 256 - PAIR_SCALES_AT <= 64 && 2 * 224 <= PAIR_SCALES_AT, "tensor memory");
+static_assert(PAIR_WORDS_STEPS == 2 * QUAD && CHUNK % QUAD == 0 && PAIR_SCALE_SLOTS <= PAIR_STAGES && 2 * 256 - PAIR_SCALES_AT <= 64 && 2 * 224 <= PAIR_SCALES_AT, "quads and tensor memory");
 constexpr int PAIR_MAX_N = 256;
 constexpr int PAIR_ROWS = 256;
 constexpr int RASTER = 8;  // row tiles that share column tiles while those are in L2
@@ -322,9 +345,12 @@ __device__ __forceinline__ long long partial_offset(const ProductArgs &p, int sl
 
 // Where an epilogue warp puts 32 columns of its 32 rows.
 __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUtensorMap &c_map, const PairItem &item,
-                                               unsigned rank, int quarter, int lane, int c0, const float *v,
-                                               uint8_t *staging)
+                                               unsigned rank, int quarter, int lane, int c0, const uint32_t *words,
+                                               uint8_t *staging, int &buffer)
 {
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(words[i]);
     if (item.slot >= 0) {
         float *out = p.partial + partial_offset(p, item.slot, rank) + (long long)c0 * 128 + quarter * 32 + lane;
 #pragma unroll
@@ -337,8 +363,10 @@ __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUten
         // rows of 64 bytes in the copy engine's swizzle of that width: no bank conflicts
         const int parts = p.c_bf16 ? 1 : 2;
         for (int part = 0; part < parts; ++part) {
-            ptx::bulk_wait_read_all();
+            asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PAIR_STAGING - 1) : "memory");  // the buffer's last
             __syncwarp();
+            uint8_t *at = staging + buffer * PAIR_STAGING_BYTES;
+            if (++buffer == PAIR_STAGING) buffer = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint4 unit;
@@ -348,14 +376,14 @@ __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUten
                     unit = Unit<float>::narrow(v + 4 * i);
                 else
                     unit = Unit<float>::narrow(v + 16 + 4 * i);
-                *reinterpret_cast<uint4 *>(staging + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) = unit;
+                *reinterpret_cast<uint4 *>(at + lane * 64 + ((i ^ ((lane >> 1) & 3)) * 16)) = unit;
             }
             ptx::fence_proxy_async();
             __syncwarp();
             // columns and rows outside C are not written
             const int col = col0 + part * 16;
             if (elect_one()) {
-                if (row0 < p.m && col < p.n) tma_store_2d(&c_map, ptx::smem_addr(staging), col, row0);
+                if (row0 < p.m && col < p.n) tma_store_2d(&c_map, ptx::smem_addr(at), col, row0);
                 ptx::bulk_commit();
             }
             __syncwarp();
@@ -519,12 +547,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             if (++set == 2) { set = 0; phase ^= 1; }
         }
     } else if (warp == PAIR_EPILOGUE_WARPS + 1) {
-        // ---- products: one thread of the first block issues them for both
+        // ---- products: one thread of the first block issues them for both.  This warp's own instructions
+        // bound the kernel if there are many: what can be is done once for a quad, and whether the next
+        // step has been loaded is asked for while this one is issued.
         if (rank == 0) {
             const uint32_t idesc = instruction_desc(p, PAIR_ROWS, p.tile_n);
             // 32 contracted values further on: 32 bytes along a row, or 32 rows of 128 bytes
             const uint32_t step_a = (p.transpose_a ? CONTRACTED_PER_MMA * 128 : CONTRACTED_PER_MMA) >> 4;
             const uint32_t step_b = (p.transpose_b ? CONTRACTED_PER_MMA : CONTRACTED_PER_MMA * 128) >> 4;
+            const uint64_t desc_a = operand_desc(base), desc_b = operand_desc(base + PAIR_OPERAND_BYTES);
+            const bool wide = p.tile_n > 128;
             PairWalk walk(p, pair);
             PairItem item;
             int stage = 0, sets = 0;  // sets of sums begun
@@ -532,61 +564,65 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             int issued = 0;  // steps
             int ends[PAIR_SCALE_SLOTS] = {};  // where the last quads ended, the latest first
             unsigned phase = 0, words_phase = 0;
-            bool ok = true;
+            bool ok = true, loaded = false;  // loaded: the next step is known to be
             while (ok && walk.take(p, pair, item)) {
-                for (int i = item.first; i < item.last; ++i) {
-                    const int in_words = (i - item.first) % PAIR_WORDS_STEPS;
-                    const bool words_end = in_words == PAIR_WORDS_STEPS - 1 || i + 1 == item.last;
-                    if (in_words == 0) ok = wait_cluster(&words_full[words_set], words_phase, 9);
-                    if (!ok) break;
-                    const int in_set = CHUNKED ? (i - item.first) % CHUNK : i - item.first;
-                    if (in_set == 0) {
+                for (int at = 0; at < item.last - item.first; at += QUAD) {
+                    const int left = item.last - item.first - at;
+                    const bool words_begin = at % PAIR_WORDS_STEPS == 0;
+                    const bool words_end = left <= QUAD || at % PAIR_WORDS_STEPS == PAIR_WORDS_STEPS - QUAD;
+                    const bool set_begin = CHUNKED ? at % CHUNK == 0 : at == 0;
+                    const bool set_end = left <= QUAD || (CHUNKED && at % CHUNK == CHUNK - QUAD);
+                    if (words_begin) ok = wait_cluster(&words_full[words_set], words_phase, 9);
+                    if (set_begin) {
                         // the set before this one (its shared columns), or the one before that, has been read
                         const int before = sets - (apart ? 2 : 1);
-                        if (before >= 0) ok = bounded_wait(&sums_read[before & 1], (before >> 1) & 1, &g_product_error, 5);
-                        if (!ok) break;
+                        if (ok && before >= 0) ok = bounded_wait(&sums_read[before & 1], (before >> 1) & 1, &g_product_error, 5);
                     }
-                    if (in_words % QUAD == 0) {
-                        const int last = ends[PAIR_SCALE_SLOTS - 1] - 1;
-                        if (last >= 0 && last > issued - PAIR_STAGES)
-                            ok = bounded_wait(&empty[last % PAIR_STAGES], last / PAIR_STAGES & 1, &g_product_error, 6);
-                        if (!ok) break;
-                    }
-                    ok = bounded_wait(&full[stage], phase, &g_product_error, 3);
+                    const int last = ends[PAIR_SCALE_SLOTS - 1] - 1;
+                    if (ok && last >= 0 && last > issued - PAIR_STAGES)
+                        ok = bounded_wait(&empty[last % PAIR_STAGES], last / PAIR_STAGES & 1, &g_product_error, 6);
                     if (!ok) break;
-                    ++issued;
-                    fence_after_sync();
-                    if (elect_one()) {
-                        const uint32_t at = base + stage * PAIR_STAGE_BYTES;
-                        const uint32_t scale_a = tmem + PAIR_SCALES_AT + slot * PAIR_SCALE_COLUMNS, scale_b = scale_a + 4;
-                        if (in_words % QUAD == 0) {
-                            const uint32_t words =
-                                base + PAIR_WORDS_AT + words_set * PAIR_WORDS_SET + in_words / QUAD * PAIR_WORDS_BYTES;
-                            tmem_copy_scales(scale_a, scales_desc(words));
-                            tmem_copy_scales(scale_b, scales_desc(words + SCALE_BYTES));
-                            if (p.tile_n > 128) tmem_copy_scales(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
+                    const uint32_t sums = tmem + ((sets & 1) ? second_set : 0);
+                    const uint32_t scale_a = tmem + PAIR_SCALES_AT + slot * PAIR_SCALE_COLUMNS, scale_b = scale_a + 4;
+#pragma unroll
+                    for (int i = 0; i < QUAD; ++i) {
+                        if (i >= left) break;
+                        if (!loaded) ok = bounded_wait(&full[stage], phase, &g_product_error, 3);
+                        if (!ok) break;
+                        const int ahead = stage + 1 == PAIR_STAGES ? 0 : stage + 1;
+                        loaded = test_arrived(&full[ahead], ahead ? phase : phase ^ 1);
+                        fence_after_sync();
+                        if (elect_one()) {
+                            if (i == 0) {
+                                const uint32_t words = base + PAIR_WORDS_AT + words_set * PAIR_WORDS_SET +
+                                                       (words_begin ? 0 : PAIR_WORDS_BYTES);
+                                tmem_copy_scales(scale_a, scales_desc(words));
+                                tmem_copy_scales(scale_b, scales_desc(words + SCALE_BYTES));
+                                if (wide) tmem_copy_scales(scale_b + 4, scales_desc(words + 2 * SCALE_BYTES));
+                            }
+                            const uint64_t da = desc_a + (uint32_t)(stage * (PAIR_STAGE_BYTES >> 4));
+                            const uint64_t db = desc_b + (uint32_t)(stage * (PAIR_STAGE_BYTES >> 4));
+#pragma unroll
+                            for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
+                                mma_block_scaled(sums, da + j * step_a, db + j * step_b, idesc | scale_byte_desc(i), scale_a,
+                                                 scale_b, i + j > 0 || !set_begin);
+                            mma_commit(&empty[stage]);
+                            if (i + 1 == QUAD || i + 1 == left) {
+                                if (words_end) mma_commit(&words_empty[words_set]);
+                                if (set_end) mma_commit(&sums_full[sets & 1]);
+                            }
                         }
-                        const uint32_t desc = idesc | scale_byte_desc(in_words % QUAD);
-                        const uint64_t da = operand_desc(at), db = operand_desc(at + PAIR_OPERAND_BYTES);
-                        const uint32_t sums = tmem + ((sets & 1) ? second_set : 0);
-#pragma unroll
-                        for (int j = 0; j < STEP / CONTRACTED_PER_MMA; ++j)
-                            mma_block_scaled(sums, da + j * step_a, db + j * step_b, desc, scale_a, scale_b,
-                                                in_set + j > 0);
-                        mma_commit(&empty[stage]);
-                        if (words_end) mma_commit(&words_empty[words_set]);
-                        if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) mma_commit(&sums_full[sets & 1]);
+                        __syncwarp();
+                        stage = ahead;
+                        if (ahead == 0) phase ^= 1;
                     }
-                    __syncwarp();
-                    if (i + 1 == item.last || (CHUNKED && in_set == CHUNK - 1)) ++sets;
+                    issued += min(left, QUAD);
+                    if (set_end) ++sets;
                     if (words_end && ++words_set == 2) { words_set = 0; words_phase ^= 1; }
-                    if (words_end || in_words % QUAD == QUAD - 1) {
-                        if (++slot == PAIR_SCALE_SLOTS) slot = 0;
+                    if (++slot == PAIR_SCALE_SLOTS) slot = 0;
 #pragma unroll
-                        for (int q = PAIR_SCALE_SLOTS - 1; q > 0; --q) ends[q] = ends[q - 1];
-                        ends[0] = issued;
-                    }
-                    if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
+                    for (int q = PAIR_SCALE_SLOTS - 1; q > 0; --q) ends[q] = ends[q - 1];
+                    ends[0] = issued;
                 }
             }
             if (!ok) {  // products in flight end before the tensor memory is freed
@@ -597,13 +633,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
     } else {
         // ---- epilogue: a warp reads its quarter of the rows and every other group of 32 columns
         const int quarter = warp & 3, odd = warp >> 2;
-        uint8_t *staging = aligned + PAIR_STAGING_AT + warp * PAIR_STAGING_BYTES;
+        uint8_t *staging = aligned + PAIR_STAGING_AT + warp * PAIR_STAGING * PAIR_STAGING_BYTES;
         const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&sums_read[0]), 0),
                                        cluster_addr(ptx::smem_addr(&sums_read[1]), 0)};
         const int groups = p.tile_n / 32;
         PairWalk walk(p, pair);
         PairItem item;
-        int sets = 0;
+        int sets = 0, buffer = 0;
         bool ok = true;
         float total[CHUNKED ? 128 : 1];
         while (ok && walk.take(p, pair, item)) {
@@ -619,9 +655,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                 const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? second_set : 0);
                 const bool down = !(sets & 1);  // the columns shared with the other set come first
                 const uint32_t read_bar = down ? read_bars[0] : read_bars[1];
+                if constexpr (CHUNKED) {
 #pragma unroll
-                for (int t = 0; t < PAIR_MAX_N / 64; ++t) {
-                    if constexpr (CHUNKED) {
+                    for (int t = 0; t < PAIR_MAX_N / 64; ++t) {
                         // the total's registers need fixed indexes: both orders are written out
 #pragma unroll
                         for (int order = 0; order < 2; ++order) {
@@ -629,30 +665,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                             if (down == (order == 1) && g < groups) {
                                 uint32_t r[32];
                                 tmem_load32(from + g * 32, r);
+                                tmem_wait(r);
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) total[u * 32 + i] += __uint_as_float(r[i]);
                             }
                         }
-                    } else {
-                        const int g = 2 * (down ? PAIR_MAX_N / 64 - 1 - t : t) + odd;
-                        if (g < groups) {
-                            uint32_t r[32];
-                            tmem_load32(from + g * 32, r);
-                            if (!apart && t == 0) {
-                                fence_before_sync();
-                                if (lane == 0) arrive_remote(read_bar);
-                                __syncwarp();
-                            }
-                            float v[32];
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-                            finish_columns(p, c_map, item, rank, quarter, lane, g * 32, v, staging);
+                        if (!apart && t == 0) {
+                            fence_before_sync();
+                            if (lane == 0) arrive_remote(read_bar);
+                            __syncwarp();
                         }
                     }
-                    if (CHUNKED && !apart && t == 0) {
-                        fence_before_sync();
-                        if (lane == 0) arrive_remote(read_bar);
-                        __syncwarp();
+                } else {
+                    // the next group is on its way while one is rounded and stored
+                    const int own = (groups - odd + 1) / 2;  // of this warp: odd, odd + 2, ...
+                    const auto group = [&](int t) { return 2 * (down ? own - 1 - t : t) + odd; };
+                    uint32_t r[2][32];
+                    tmem_load32(from + group(0) * 32, r[0]);
+#pragma unroll
+                    for (int t = 0; t < PAIR_MAX_N / 64; ++t) {
+                        if (t >= own) break;
+                        tmem_wait(r[t & 1]);
+                        if (!apart && t == 0) {
+                            fence_before_sync();
+                            if (lane == 0) arrive_remote(read_bar);
+                            __syncwarp();
+                        }
+                        if (t + 1 < own) tmem_load32(from + group(t + 1) * 32, r[~t & 1]);
+                        finish_columns(p, c_map, item, rank, quarter, lane, group(t) * 32, r[t & 1], staging, buffer);
                     }
                 }
                 if (apart) {
@@ -666,8 +706,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
 #pragma unroll
                     for (int u = 0; u < PAIR_MAX_N / 64; ++u)
                         if (2 * u + odd < groups)
-                            finish_columns(p, c_map, item, rank, quarter, lane, (2 * u + odd) * 32, total + u * 32,
-                                           staging);
+                            finish_columns(p, c_map, item, rank, quarter, lane, (2 * u + odd) * 32,
+                                           reinterpret_cast<const uint32_t *>(total + u * 32),
+                                           staging, buffer);
                 }
             }
         }
