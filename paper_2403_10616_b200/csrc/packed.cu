@@ -439,16 +439,18 @@ __global__ void __launch_bounds__(THREADS, 2)
         for (int b = 0; b < S::BUFFERS; ++b)
             if (blockIdx.x + (long long)b * gridDim.x < blocks) request(blockIdx.x + b * gridDim.x, b);
 
+    f32x2 gamma[U / 2], beta[U / 2];  // of the columns from `held` on
+    int held = -1;
     int buffer = 0, previous = S::BUFFERS - 1;
     unsigned phase = 0, turn = 0;
     for (int index = blockIdx.x; index < blocks; index += gridDim.x) {
         const int row0 = index / a.extent.block_cols * PACK_BLOCK + (int)threadIdx.x / L::PER_ROW;
         const int col0 = index % a.extent.block_cols * PACK_BLOCK;
         const int col = col0 + (int)(threadIdx.x % L::PER_ROW) * U;
-        f32x2 gamma[U / 2], beta[U / 2];
         float mean[L::UNITS], rstd[L::UNITS];
         if constexpr (OP == OP_NORM) {
-            norm_params<U>(a, col, gamma, beta);
+            if (col0 != held) norm_params<U>(a, col, gamma, beta);
+            held = col0;
 #pragma unroll
             for (int j = 0; j < L::UNITS; ++j) {
                 const int r = min(row0 + j * L::STEP, rows - 1);
@@ -481,8 +483,6 @@ __global__ void __launch_bounds__(THREADS, 2)
                 widen_pairs<T>(unit, f);
                 if constexpr (OP == OP_NORM) {
                     normalise<U>(f, mean[j], rstd[j], gamma, beta);
-                    if (col0 + PACK_BLOCK > cols || row0 + j * L::STEP >= rows)
-                        keep_inside<U>(f, row0 + j * L::STEP < rows ? cols - col : 0);
                 } else if constexpr (OP == OP_GELU) {
 #pragma unroll
                     for (int i = 0; i < U / 2; ++i) f[i] = gelu(f[i]);
@@ -494,6 +494,14 @@ __global__ void __launch_bounds__(THREADS, 2)
                 }
 #pragma unroll
                 for (int i = 0; i < U / 2; ++i) my = larger(my, f[i]);
+            }
+        }
+        if (OP == OP_NORM && edge) {  // what lies outside is not zero here: the maximum again, without it
+            my = 0.0f;
+#pragma unroll
+            for (int e = 0; e < (OP == OP_NORM ? VALUES : 0); ++e) {
+                const float2 v = values_of(y[e / 2]);
+                if (row0 + e / U * L::STEP < rows && col + e % U < cols) my = fmaxf(my, fabsf(e & 1 ? v.y : v.x));
             }
         }
         const unsigned wx = __reduce_max_sync(0xffffffffu, wider_bf16x2(mx));
@@ -577,7 +585,10 @@ template <int OP> int launch_stream(const BlockArgs &a, int blocks, cudaStream_t
     if (OP == OP_GELU_BACK && !box_map(&codes_map, a.codes, rows, cols, a.codes_stride, true)) return DIPACO_ECUDA;
     if (cudaFuncSetAttribute(stream_kernel<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Stream<OP>::SMEM) != cudaSuccess)
         return launch_status();
-    stream_kernel<OP><<<std::min(blocks, 296), THREADS, Stream<OP>::SMEM, stream>>>(x_map, codes_map, a, blocks);
+    int grid = 296;  // two on each SM
+    // with few blocks in a row of them, a block of threads keeps to one column of blocks, and to its parameters
+    if (OP == OP_NORM && a.extent.block_cols <= 16) grid = grid / a.extent.block_cols * a.extent.block_cols;
+    stream_kernel<OP><<<std::min(blocks, grid), THREADS, Stream<OP>::SMEM, stream>>>(x_map, codes_map, a, blocks);
     return launch_status();
 }
 

@@ -28,14 +28,16 @@ class Packed:
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         rows, cols = codes.shape
-        if codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu:
+        stride, unit = codes.stride()
+        if codes.dtype != _E4M3 or scales.dtype != _E8M0:
             raise ValueError("codes must be float8_e4m3fn and scales float8_e8m0fnu")
-        if scales.shape != (-(-rows // BLOCK), -(-cols // BLOCK)) or not scales.is_contiguous():
+        if scales.shape != ((rows + 127) >> 7, (cols + 127) >> 7) or not scales.is_contiguous():
             raise ValueError("scales must be contiguous with one entry per block of 128 x 128")
-        if cols > 1 and codes.stride(1) != 1:
+        if unit != 1 and cols > 1:
             raise ValueError("codes must be row-major")
-        stride = codes.stride(0) if rows > 1 else -(-max(cols, 1) // 16) * 16
-        if not codes.is_cuda or scales.device != codes.device:
+        if rows == 1:
+            stride = (cols + 15) & ~15
+        if not codes.is_cuda or scales.get_device() != codes.get_device():
             raise ValueError("codes and scales must be on one CUDA device")
         self.codes, self.scales = codes, scales
         self.struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
