@@ -501,12 +501,14 @@ __global__ void __launch_bounds__(THREADS, 2)
                 for (int i = 0; i < U / 2; ++i) my = larger(my, f[i]);
             }
         }
-        if (OP == OP_NORM && edge) {  // what lies outside is not zero here: the maximum again, without it
+        if (OP == OP_NORM && edge) {  // what lies outside is not zero here: it is made so, and the maximum taken again
             my = 0.0f;
 #pragma unroll
-            for (int e = 0; e < (OP == OP_NORM ? VALUES : 0); ++e) {
-                const float2 v = values_of(y[e / 2]);
-                if (row0 + e / U * L::STEP < rows && col + e % U < cols) my = fmaxf(my, fabsf(e & 1 ? v.y : v.x));
+            for (int j = 0; j < (OP == OP_NORM ? L::UNITS : 0); ++j) {
+                f32x2 *f = y + j * U / 2;
+                keep_inside<U>(f, row0 + j * L::STEP < rows ? cols - col : 0);
+#pragma unroll
+                for (int i = 0; i < U / 2; ++i) my = larger(my, f[i]);
             }
         }
         const unsigned wx = __reduce_max_sync(0xffffffffu, wider_bf16x2(mx));

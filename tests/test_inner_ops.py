@@ -276,6 +276,23 @@ def test_packed_norm_with_infinities_and_nan():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [200, 128])
+def test_packed_norm_scales_an_edge_with_infinities_by_what_is_inside(rows, dtype):
+    # rows far from zero: a row of zeros beyond the last, normed like it, would be thousands
+    x = (1000 + 4 * torch.randn(rows, 200, generator=gen(31))).to(dtype)
+    gamma = torch.ones(200)
+    gamma[3] = gamma[150] = math.inf
+    y, _, mean, rstd = inner.layer_norm_pack(place(x), gamma.to(DEV))
+    want = ref.layer_norm(x, gamma, None, 1e-5)[0]
+    largest = torch.where(torch.isfinite(want), want, torch.zeros_like(want)).abs()
+    blocks = torch.stack([torch.stack([largest[i:i + 128, j:j + 128].max() for j in (0, 128)]) for i in range(0, rows, 128)])
+    # the largest finite value needs at least half of the codes' range, and fits in it up to its own rounding
+    scales = y.scales.cpu().double()
+    assert bool((blocks <= 448 * scales * (1 + 2.0 ** -10)).all()) and bool((blocks > 224 * scales * (1 - 2.0 ** -10)).all())
+
+
+@pytest.mark.gpu
 def test_norm_gradient_against_differences():
     """<dx, v> and <dgamma, w> against central differences of the kernel's own forward pass in fp32."""
     rows, cols, eps = 12, 300, 1e-2
