@@ -438,11 +438,12 @@ int dipaco_module_sync_static(float *theta, float *momentum, int64_t numel, int3
  *
  * Conventions.  All pointers are device pointers; the calls are asynchronous on cuda_stream, allocate
  * nothing and can be captured in a CUDA graph.  Arguments are checked before anything is launched
- * (DIPACO_EINVAL, or DIPACO_ELIMIT for extents beyond 2^31).  A dense matrix is row-major with a row
- * stride in elements, at any element alignment; 16-byte aligned rows are fastest.  dtype and
+ * (DIPACO_EINVAL, or DIPACO_ELIMIT for extents of about 2^31 and more).  A dense matrix is row-major
+ * with a row stride in elements, at any element alignment; 16-byte aligned rows are fastest, and rows
+ * at other alignments are read in the aligned 16-byte units that hold their values.  dtype and
  * param_dtype are DIPACO_F32 or DIPACO_BF16.  Outputs must not overlap inputs.  Extents of zero are
- * allowed.  Every sum is fp32 and taken in an order that depends on the shapes alone: results are
- * bitwise reproducible.
+ * allowed.  Every sum is fp32 and taken in an order that depends on shapes, types and alignment alone:
+ * results are bitwise reproducible.
  *
  * Packed matrices.  8-bit codes (e4m3: 4 exponent and 3 mantissa bits, largest value 448, no infinity)
  * with one scale for each block of 128 x 128 values, itself an 8-bit power of two (e8m0: byte b is
@@ -471,7 +472,7 @@ int dipaco_unpack(const dipaco_packed *x, void *y, int64_t y_stride, int32_t dty
  * rstd = 1 / sqrt(var + eps),  y = (x - mean) * rstd * gamma + beta.
  *   gamma, beta  [cols] of param_dtype; NULL = ones, zeros
  *   y            NULL = statistics only
- *   mean, rstd   [rows] fp32, kept for the backward pass; NULL where not wanted
+ *   mean, rstd   [rows] fp32, kept for the backward pass; NULL where not wanted; NaN for rows of no values
  */
 int dipaco_layer_norm(const void *x, int64_t x_stride, const void *gamma, const void *beta, void *y,
                       int64_t y_stride, float *mean, float *rstd, int64_t rows, int64_t cols, float eps,

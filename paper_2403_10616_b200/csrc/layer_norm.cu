@@ -775,11 +775,16 @@ int dipaco_layer_norm(const void *x, int64_t x_stride, const void *gamma, const 
     const int psize = dense_size(param_dtype);
     if (!vector_ok(gamma, psize) || !vector_ok(beta, psize) || !vector_ok(mean, 4) || !vector_ok(rstd, 4))
         return DIPACO_EINVAL;
-    if (rows == 0 || cols == 0) return DIPACO_OK;
+    if (rows == 0 || (cols == 0 && !mean && !rstd)) return DIPACO_OK;
 
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (cols == 0) {  // statistics of nothing: bytes of ones are a NaN
+        if (mean && cudaMemsetAsync(mean, 0xff, rows * sizeof(float), stream) != cudaSuccess) return launch_status();
+        if (rstd && cudaMemsetAsync(rstd, 0xff, rows * sizeof(float), stream) != cudaSuccess) return launch_status();
+        return DIPACO_OK;
+    }
     NormArgs a = {x, y, gamma, beta, mean, rstd, x_stride, y_stride, (int)rows, (int)cols, eps, 1.0f / (float)cols,
                   param_dtype == DIPACO_BF16, (uintptr_t)gamma % 16 == 0, (uintptr_t)beta % 16 == 0};
     const int size = dense_size(dtype);

@@ -680,11 +680,12 @@ int dipaco_layer_norm_pack(const void *x, int64_t x_stride, const void *gamma, c
     const int psize = dense_size(param_dtype);
     if (!vector_ok(gamma, psize) || !vector_ok(beta, psize) || !vector_ok(mean, 4) || !vector_ok(rstd, 4))
         return DIPACO_EINVAL;
-    if (rows == 0 || cols == 0) return DIPACO_OK;
+    if (rows == 0) return DIPACO_OK;
     if (!mean || !rstd) return DIPACO_EINVAL;
     if (const int rc = dipaco_layer_norm(x, x_stride, nullptr, nullptr, nullptr, 0, mean, rstd, rows, cols, eps,
                                          dtype, param_dtype, device, cuda_stream))
         return rc;
+    if (cols == 0) return DIPACO_OK;
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     BlockArgs a = {};

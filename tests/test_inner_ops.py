@@ -293,6 +293,15 @@ def test_packed_norm_scales_an_edge_with_infinities_by_what_is_inside(rows, dtyp
 
 
 @pytest.mark.gpu
+def test_norm_of_rows_without_values():
+    x = torch.empty(5, 0, device=DEV)
+    empty = torch.ones(1 << 12, device=DEV)  # what uninitialised statistics would be
+    del empty
+    for _, mean, rstd in (inner.layer_norm(x, stats=True), inner.layer_norm_pack(x)[1:]):
+        assert bool(torch.isnan(mean).all()) and bool(torch.isnan(rstd).all())
+
+
+@pytest.mark.gpu
 def test_norm_gradient_against_differences():
     """<dx, v> and <dgamma, w> against central differences of the kernel's own forward pass in fp32."""
     rows, cols, eps = 12, 300, 1e-2
