@@ -228,8 +228,10 @@ int launch_norm_shape(const NormArgs &a, cudaStream_t stream)
     const int64_t full = 148 * (threads > 128 ? 1 : NU > 4 ? 4 : 6);
     const unsigned grid = (unsigned)std::min<int64_t>(full, ceil_div(a.rows, threads / TPR));
     const int smem = a.y ? 2 * (int)ceil_div(a.cols, 8) * 8 * (int)sizeof(float) : 0;
+    // always the largest there can be: threads that launch different sizes share the attribute
     if (smem > 48 * 1024 && cudaFuncSetAttribute(norm_rows_kernel<T, MODE, TPR, NU, PART>,
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 2 * NORM_WIDEST * (int)sizeof(float)) != cudaSuccess)
         return launch_status();
     norm_rows_kernel<T, MODE, TPR, NU, PART><<<grid, threads, smem, stream>>>(a);
     return launch_status();
@@ -695,6 +697,7 @@ __global__ void __launch_bounds__(1024) norm_back_join_kernel(const float *parts
 }
 
 constexpr int BACK_LONG_SHARES = 32;
+constexpr int BACK_RING = 192 * 1024;  // bytes of shared memory for rows on their way
 
 // The widest row that a block holds, and the threads for a row: 32 bytes each.
 int64_t back_widest(int dtype) { return dtype == DIPACO_BF16 ? 16384 : 8192; }
@@ -721,9 +724,11 @@ int launch_back_shape(const NormBackArgs &a, int blocks, cudaStream_t stream)
     const int dy_bytes = (int)ceil_div(a.cols * (int)sizeof(T), 16) * 16 + (VEC ? 0 : 16);
     const int x_bytes = (int)ceil_div(a.cols * (int)sizeof(typename S::X), 16) * 16 + (VEC || PACKED ? 0 : 16);
     const int stage = S::SYNCS * S::TAKEN * (dy_bytes + x_bytes);
-    const int stages = std::max(2, std::min(BACK_MAX_STAGES, 192 * 1024 / stage)), smem = stages * stage + 128;
-    if (cudaFuncSetAttribute(norm_back_kernel<T, PACKED, VEC, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
-        cudaSuccess)
+    // a stage takes 64 KB and some for rows off 16-byte boundaries at most
+    const int stages = std::max(2, std::min(BACK_MAX_STAGES, BACK_RING / stage)), smem = stages * stage + 128;
+    // always the largest there can be: threads that launch different sizes share the attribute
+    if (cudaFuncSetAttribute(norm_back_kernel<T, PACKED, VEC, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             BACK_RING + 128) != cudaSuccess)
         return launch_status();
     norm_back_kernel<T, PACKED, VEC, TPR><<<blocks, S::THREADS, smem, stream>>>(a, stages, dy_bytes, x_bytes);
     return launch_status();

@@ -1018,7 +1018,8 @@ int launch_few(const dipaco_packed *a, const dipaco_packed *b, void *c, int64_t 
     const int smem = m * p.steps * STEP * 2 + p.steps;
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(p.outputs, FEW_THREADS / 32 * FEW_OUTPUTS), 148 * 2);
     const auto kernel = m == 1 ? few_kernel<1> : m == 2 ? few_kernel<2> : m == 3 ? few_kernel<3> : few_kernel<4>;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    // always the largest there can be: threads that launch different sizes share the attribute
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM) != cudaSuccess)
         return launch_status();
     kernel<<<grid, FEW_THREADS, smem, stream>>>(p);
     return launch_status();

@@ -7,6 +7,7 @@ A result in bf16 adds half a unit of its last place, a packed one half the spaci
 """
 from __future__ import annotations
 
+import concurrent.futures
 import ctypes
 import itertools
 import math
@@ -612,6 +613,27 @@ def test_products_over_nothing():
 
 
 # ------------------------------------------------------------------ streams, repeats, graphs
+
+@pytest.mark.gpu
+def test_threads_that_launch_different_sizes_do_not_disturb_one_another():
+    # sizes that need different amounts of shared memory of one kernel
+    def work(i, cols):
+        rows = torch.ones(2, cols, device=DEV)
+        tokens, weight = inner.pack(rows), inner.pack(torch.ones(4, cols, device=DEV))
+        stat = torch.zeros(2, device=DEV)
+        for _ in range(300):
+            results[i].append((inner.layer_norm(rows), inner.packed_matmul(tokens, weight, transpose_b=True, out_dtype=F32),
+                               inner.layer_norm_backward(rows, rows, stat, stat)[2]))
+        torch.cuda.synchronize()
+
+    sizes, results = [7000, 16000, 8000, 15000], [[], [], [], []]
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:
+        for done in [pool.submit(work, i, cols) for i, cols in enumerate(sizes)]:
+            done.result()
+    for cols, got in zip(sizes, results):
+        for y, product, dbeta in got[::30]:
+            assert bool((y == 0).all()) and bool((product == cols).all()) and bool((dbeta == 2).all())
+
 
 @pytest.mark.gpu
 def test_operators_follow_the_current_stream_and_repeat_bitwise():
