@@ -459,8 +459,11 @@ __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
     int parity = 0, stage = 0;
     unsigned phase = 0;
     for (int first = begin; first < a.rows; first += step, row += step) {
-        if (!bounded_wait(&full[stage], phase, &g_norm_error, 1)) {
+        if (!__all_sync(0xffffffffu, bounded_wait(&full[stage], phase, &g_norm_error, 1))) {
             for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
+            // other warps may have seen the rows arrive: the barriers that they come to are met
+            if constexpr (TPR > 32 && GROUPS > 1)
+                for (; first < a.rows; first += step) asm volatile("bar.sync %0, %1;" ::"r"(1 + sync), "n"(S::SYNC) : "memory");
             return;
         }
         const uint8_t *mine = ring + stage * stage_bytes + in_sync / TPR * ROWS * row_bytes;

@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(THREADS, 2)
         const f32x2 scale = pair_of(OP == OP_GELU_BACK ? scale_value(a.scales[index]) : 0.0f);
         const bool edge = col0 + PACK_BLOCK > cols || (index / a.extent.block_cols + 1) * PACK_BLOCK > rows;
         const SharedValues x = {reinterpret_cast<const uint4 *>(buffers + buffer * S::BYTES) + threadIdx.x};
-        if (!bounded_wait(&full[buffer], phase, &g_packing_error, 1)) {
+        if (!__all_sync(0xffffffffu, bounded_wait(&full[buffer], phase, &g_packing_error, 1))) {  // whole warps leave
             for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
             return;
         }

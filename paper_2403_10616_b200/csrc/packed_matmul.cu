@@ -67,7 +67,7 @@ __device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, unsigned parity)
         : "memory");
     return ok != 0;
 }
-// Whether the phase is over, without waiting.
+// Whether the phase is over, without waiting: the same answer on the whole warp.
 __device__ __forceinline__ bool test_arrived(uint64_t *bar, unsigned parity)
 {
     unsigned ok;
@@ -78,18 +78,23 @@ __device__ __forceinline__ bool test_arrived(uint64_t *bar, unsigned parity)
         : "=r"(ok)
         : "r"(ptx::smem_addr(bar)), "r"(parity)
         : "memory");
-    return ok != 0;
+    return __all_sync(0xffffffffu, ok);
 }
-// Bounded, and ordered after what other blocks of the cluster did before they arrived.
-__device__ __forceinline__ bool wait_cluster(uint64_t *bar, unsigned parity, int code)
+// Bounded wait of a whole warp, which agrees on how it ended: what follows takes all its lanes.  CLUSTER:
+// ordered after what the other block of the pair did before it arrived.
+template <bool CLUSTER = false> __device__ __forceinline__ bool warp_wait(uint64_t *bar, unsigned parity, int code)
 {
-    if (try_wait_cluster(bar, parity)) return true;
+    const auto arrived = [&] {
+        const bool ok = CLUSTER ? try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity);
+        return __all_sync(0xffffffffu, ok) != 0;
+    };
+    if (arrived()) return true;
     const unsigned long long t0 = ptx::global_timer_ns();
     for (;;) {
 #pragma unroll 1
         for (int i = 0; i < 256; ++i)
-            if (try_wait_cluster(bar, parity)) return true;
-        if (ptx::global_timer_ns() - t0 > BULK_WAIT_LIMIT_NS) {
+            if (arrived()) return true;
+        if (__any_sync(0xffffffffu, ptx::global_timer_ns() - t0 > BULK_WAIT_LIMIT_NS)) {
             atomicCAS(&g_product_error, 0, code);
             return false;
         }
@@ -460,7 +465,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
         while (ok && walk.take(p, pair, item)) {
             const int m0 = item.tile_m * PAIR_ROWS + (int)rank * 128, nb = item.tile_n * p.tile_n + (int)rank * half_n;
             for (int i = item.first; i < item.last; ++i) {
-                ok = bounded_wait(&empty[stage], phase ^ 1, &g_product_error, 1);
+                ok = warp_wait(&empty[stage], phase ^ 1, 1);
                 if (!ok) break;
                 if (elect_one()) {
                     const uint32_t to = base + stage * PAIR_STAGE_BYTES;
@@ -481,7 +486,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
         }
         // the barriers of the last stages are arrived on from the first block: both stay until then
         for (int s = 0; ok && s < PAIR_STAGES; ++s) {
-            ok = bounded_wait(&empty[stage], phase ^ 1, &g_product_error, 2);
+            ok = warp_wait(&empty[stage], phase ^ 1, 2);
             if (++stage == PAIR_STAGES) { stage = 0; phase ^= 1; }
         }
         if (!ok)  // a wait ran out: let the copies in flight land before the block ends
@@ -515,7 +520,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                         held |= byte << (8 * b + 8);
                     }
                 }
-                ok = bounded_wait(&words_empty[set], phase ^ 1, &g_product_error, 7);
+                ok = warp_wait(&words_empty[set], phase ^ 1, 7);
                 if (!ok) break;
                 uint4 *words = reinterpret_cast<uint4 *>(aligned + PAIR_WORDS_AT + set * PAIR_WORDS_SET) + lane;
                 for (int i = 0; i < PAIR_WORDS_STEPS && i0 + i < item.last; i += QUAD) {
@@ -548,7 +553,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             }
         }
         for (int s = 0; ok && s < 2; ++s) {  // as for the stages
-            ok = bounded_wait(&words_empty[set], phase ^ 1, &g_product_error, 8);
+            ok = warp_wait(&words_empty[set], phase ^ 1, 8);
             if (++set == 2) { set = 0; phase ^= 1; }
         }
     } else if (warp == PAIR_EPILOGUE_WARPS + 1) {
@@ -577,22 +582,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     const bool words_end = left <= QUAD || at % PAIR_WORDS_STEPS == PAIR_WORDS_STEPS - QUAD;
                     const bool set_begin = CHUNKED ? at % CHUNK == 0 : at == 0;
                     const bool set_end = left <= QUAD || (CHUNKED && at % CHUNK == CHUNK - QUAD);
-                    if (words_begin) ok = wait_cluster(&words_full[words_set], words_phase, 9);
+                    if (words_begin) ok = warp_wait<true>(&words_full[words_set], words_phase, 9);
                     if (set_begin) {
                         // the set before this one (its shared columns), or the one before that, has been read
                         const int before = sets - (apart ? 2 : 1);
-                        if (ok && before >= 0) ok = bounded_wait(&sums_read[before & 1], (before >> 1) & 1, &g_product_error, 5);
+                        if (ok && before >= 0) ok = warp_wait(&sums_read[before & 1], (before >> 1) & 1, 5);
                     }
                     const int last = ends[PAIR_SCALE_SLOTS - 1] - 1;
                     if (ok && last >= 0 && last > issued - PAIR_STAGES)
-                        ok = bounded_wait(&empty[last % PAIR_STAGES], last / PAIR_STAGES & 1, &g_product_error, 6);
+                        ok = warp_wait(&empty[last % PAIR_STAGES], last / PAIR_STAGES & 1, 6);
                     if (!ok) break;
                     const uint32_t sums = tmem + ((sets & 1) ? second_set : 0);
                     const uint32_t scale_a = tmem + PAIR_SCALES_AT + slot * PAIR_SCALE_COLUMNS, scale_b = scale_a + 4;
 #pragma unroll
                     for (int i = 0; i < QUAD; ++i) {
                         if (i >= left) break;
-                        if (!loaded) ok = bounded_wait(&full[stage], phase, &g_product_error, 3);
+                        if (!loaded) ok = warp_wait(&full[stage], phase, 3);
                         if (!ok) break;
                         const int ahead = stage + 1 == PAIR_STAGES ? 0 : stage + 1;
                         loaded = test_arrived(&full[ahead], ahead ? phase : phase ^ 1);
@@ -621,6 +626,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                         stage = ahead;
                         if (ahead == 0) phase ^= 1;
                     }
+                    if (!ok) break;
                     issued += min(left, QUAD);
                     if (set_end) ++sets;
                     if (words_end && ++words_set == 2) { words_set = 0; words_phase ^= 1; }
@@ -632,7 +638,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
             }
             if (!ok) {  // products in flight end before the tensor memory is freed
                 if (elect_one()) mma_commit(&ended);
-                bounded_wait(&ended, 0, &g_product_error, 10);
+                warp_wait(&ended, 0, 10);
             }
         }
     } else {
@@ -654,7 +660,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                 for (int i = 0; i < 128; ++i) total[i] = 0.0f;
             }
             for (int part = 0; part < parts; ++part, ++sets) {
-                ok = bounded_wait(&sums_full[sets & 1], (sets >> 1) & 1, &g_product_error, 4);
+                ok = warp_wait(&sums_full[sets & 1], (sets >> 1) & 1, 4);
                 if (!ok) break;
                 fence_after_sync();
                 const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? second_set : 0);
