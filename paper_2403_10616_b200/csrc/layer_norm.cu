@@ -76,10 +76,14 @@ enum : int { ROWS_SINGLE, ROWS_UNITS, ROWS_RAGGED };
 // is on its way while this one is summed, sums run in four chains, and gamma and beta wait in shared memory
 // in fp32 (with both read and widened for every row: 16384x2048 43 us).  A warp per row up to 2048 values
 // in bf16 (1024 in fp32) keeps sums inside warps; two or four warps per row took 35 and 37 us there.
-// Measured: 16384x2048 in bf16 with statistics 32.9 us, 4.1 TB/s; what is left is the warps' waiting for
+// STATS (nothing written but mean and rstd) sums in fp32 pairs and takes fewer registers, for more warps: the
+// first launch of the packed norm, 32768x896, 15 -> 13 us; with y to write pairs were slower.
+// Measured: 16384x2048 in bf16 with statistics 32 us, 4.2 TB/s; what is left is the warps' waiting for
 // their own chains of sums and exchanges (they issue in a third of the cycles), not instructions.
-template <typename T, int MODE, int TPR, int NU, int PART>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU > 4 ? 4 : 6)
+constexpr int norm_blocks(int tpr, int nu, bool stats) { return tpr > 128 ? 1 : nu > 4 ? 4 : stats ? 8 : 6; }  // on an SM
+
+template <typename T, int MODE, int TPR, int NU, int PART, bool STATS>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, STATS))
     norm_rows_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr bool VEC = MODE != ROWS_SINGLE;
@@ -104,7 +108,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU > 4 
         if constexpr (VEC) raw[j] = make_uint4(0u, 0u, 0u, 0u);
         if (row < a.rows && (j < SURE || j * TPR * U < cols)) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
     }
-    if (a.y) {
+    if constexpr (!STATS) {
         for (int c = threadIdx.x; c < padded; c += THREADS) {
             const bool in = c < a.cols;
             params[c] = !in ? 0.0f : a.gamma ? load_param(a.gamma, a.params_bf16, c) : 1.0f;
@@ -115,22 +119,32 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU > 4 
     int turn = 0;
     // rows beyond the last keep the warp together: what they compute is not written
     for (int first = (int)blockIdx.x * GROUPS; first < a.rows; first += step, row += step) {
-        float v[E], sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        // statistics alone: the same sums in fp32 pairs
+        f32x2 pairs[STATS && VEC ? E / 2 : 1], sum2[2] = {0ull, 0ull};
+        float v[STATS && VEC ? 1 : E], sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
-            if constexpr (VEC)
-                Unit<T>::widen(raw[j], v + j * U);
-            else
-                v[j] = j * TPR < cols ? widen1<T>(raw[j]) : 0.0f;
-            if constexpr (MODE == ROWS_RAGGED) {
-                if (j >= SURE) {
+            if constexpr (STATS && VEC) {
+                f32x2 *p = pairs + j * U / 2;
+                widen_pairs<T>(raw[j], p);
+                if (MODE == ROWS_RAGGED && j >= SURE) keep_inside<U>(p, cols - j * TPR * U);
 #pragma unroll
-                    for (int i = 1; i < U; ++i)
-                        if (j * TPR * U + i >= cols) v[j * U + i] = 0.0f;
+                for (int i = 0; i < U / 2; ++i) sum2[i & 1] = add2(sum2[i & 1], p[i]);
+            } else {
+                if constexpr (VEC)
+                    Unit<T>::widen(raw[j], v + j * U);
+                else
+                    v[j] = j * TPR < cols ? widen1<T>(raw[j]) : 0.0f;
+                if constexpr (MODE == ROWS_RAGGED) {
+                    if (j >= SURE) {
+#pragma unroll
+                        for (int i = 1; i < U; ++i)
+                            if (j * TPR * U + i >= cols) v[j * U + i] = 0.0f;
+                    }
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] += v[j * U + i];
+                for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] += v[j * U + i];
+            }
         }
         x += step * a.x_stride;
         if (row + step < a.rows) {
@@ -139,21 +153,32 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU > 4 
                 if (j < SURE || j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
         }
         // divided: the mean of equal values is that value
-        const float mean = row_sum<TPR>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared[turn]) / (float)a.cols;
+        const auto sum = [&] { return STATS && VEC ? sum_of(sum2[0]) + sum_of(sum2[1]) : (sums[0] + sums[1]) + (sums[2] + sums[3]); };
+        const float mean = row_sum<TPR>(sum(), shared[turn]) / (float)a.cols;
+        sum2[0] = sum2[1] = 0ull;
         sums[0] = sums[1] = sums[2] = sums[3] = 0.0f;
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
+            if constexpr (STATS && VEC) {
+                f32x2 *p = pairs + j * U / 2;
 #pragma unroll
-            for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
-            if (j >= SURE) {  // what lies outside does not count
+                for (int i = 0; i < U / 2; ++i) p[i] = add2(p[i], pair_of(-mean));
+                if (j >= SURE) keep_inside<U>(p, cols - j * TPR * U);
 #pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (j * TPR * U + (MODE == ROWS_RAGGED ? i : 0) >= cols) v[j * U + i] = 0.0f;
+                for (int i = 0; i < U / 2; ++i) sum2[i & 1] = fma2(p[i], p[i], sum2[i & 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
+                if (j >= SURE) {  // what lies outside does not count
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+                        if (j * TPR * U + (MODE == ROWS_RAGGED ? i : 0) >= cols) v[j * U + i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] = fmaf(v[j * U + i], v[j * U + i], sums[(j * U + i) & 3]);
             }
-#pragma unroll
-            for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] = fmaf(v[j * U + i], v[j * U + i], sums[(j * U + i) & 3]);
         }
-        const float square = row_sum<TPR>((sums[0] + sums[1]) + (sums[2] + sums[3]), shared[turn + 1]);
+        const float square = row_sum<TPR>(sum(), shared[turn + 1]);
         const float rstd = inverse_root(__fmul_rn(square, a.inv_cols), a.eps);
         turn ^= 2;
         if (row < a.rows) {
@@ -161,7 +186,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR > 128 ? 1 : NU > 4 
                 if (a.mean) a.mean[row] = mean;
                 if (a.rstd) a.rstd[row] = rstd;
             }
-            if (a.y) {
+            if constexpr (!STATS) {
                 const float *gamma = params + lane * U, *beta = gamma + padded;
 #pragma unroll
                 for (int j = 0; j < UNITS; ++j) {
@@ -221,20 +246,26 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
     }
 }
 
-template <typename T, int MODE, int TPR, int NU, int PART>
-int launch_norm_shape(const NormArgs &a, cudaStream_t stream)
+template <typename T, int MODE, int TPR, int NU, int PART, bool STATS>
+int launch_norm_kernel(const NormArgs &a, cudaStream_t stream)
 {
     constexpr int threads = TPR < 128 ? 128 : TPR;
-    const int64_t full = 148 * (threads > 128 ? 1 : NU > 4 ? 4 : 6);
+    const auto kernel = norm_rows_kernel<T, MODE, TPR, NU, PART, STATS>;
+    const int64_t full = 148 * norm_blocks(TPR, NU, STATS);
     const unsigned grid = (unsigned)std::min<int64_t>(full, ceil_div(a.rows, threads / TPR));
-    const int smem = a.y ? 2 * (int)ceil_div(a.cols, 8) * 8 * (int)sizeof(float) : 0;
+    const int smem = STATS ? 0 : 2 * (int)ceil_div(a.cols, 8) * 8 * (int)sizeof(float);
     // always the largest there can be: threads that launch different sizes share the attribute
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(norm_rows_kernel<T, MODE, TPR, NU, PART>,
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  2 * NORM_WIDEST * (int)sizeof(float)) != cudaSuccess)
         return launch_status();
-    norm_rows_kernel<T, MODE, TPR, NU, PART><<<grid, threads, smem, stream>>>(a);
+    kernel<<<grid, threads, smem, stream>>>(a);
     return launch_status();
+}
+
+template <typename T, int MODE, int TPR, int NU, int PART> int launch_norm_shape(const NormArgs &a, cudaStream_t stream)
+{
+    return a.y ? launch_norm_kernel<T, MODE, TPR, NU, PART, false>(a, stream)
+               : launch_norm_kernel<T, MODE, TPR, NU, PART, true>(a, stream);
 }
 
 // Up to 2048 values in bf16 the units are dealt out so that only a thread's last can lie outside.

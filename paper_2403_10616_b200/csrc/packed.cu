@@ -15,7 +15,7 @@
 // Measured on 32768x3584 in bf16: pack 59 us (6.0 TB/s: bound by memory), GELU with both results 103 us and
 // its gradient 103 us (4.6 TB/s).  Those two are bound by the unit that has powers and reciprocals, two for
 // a value, beside memory: without them they take 86 and 91 us.  The norm's two launches on 32768x896 take
-// 43 us, 15 of them for the statistics; its second reads x from L2.
+// 42 us, 13 of them for the statistics; its second reads x from L2.
 #include "inner_common.cuh"
 
 #include <cmath>
