@@ -448,9 +448,12 @@ __global__ void __launch_bounds__(THREADS, 2)
     int held = -1;
     int buffer = 0, previous = S::BUFFERS - 1;
     unsigned phase = 0, turn = 0;
+    // the block's place among the blocks, moved on without a division
+    const int rows_on = gridDim.x / a.extent.block_cols * PACK_BLOCK, cols_on = gridDim.x % a.extent.block_cols * PACK_BLOCK;
+    const int all_cols = a.extent.block_cols * PACK_BLOCK;
+    int first_row = blockIdx.x / a.extent.block_cols * PACK_BLOCK, col0 = blockIdx.x % a.extent.block_cols * PACK_BLOCK;
     for (int index = blockIdx.x; index < blocks; index += gridDim.x) {
-        const int row0 = index / a.extent.block_cols * PACK_BLOCK + (int)threadIdx.x / L::PER_ROW;
-        const int col0 = index % a.extent.block_cols * PACK_BLOCK;
+        const int row0 = first_row + (int)threadIdx.x / L::PER_ROW;
         const int col = col0 + (int)(threadIdx.x % L::PER_ROW) * U;
         float mean[L::UNITS], rstd[L::UNITS];
         if constexpr (OP == OP_NORM) {
@@ -464,7 +467,7 @@ __global__ void __launch_bounds__(THREADS, 2)
             }
         }
         const f32x2 scale = pair_of(OP == OP_GELU_BACK ? scale_value(a.scales[index]) : 0.0f);
-        const bool edge = col0 + PACK_BLOCK > cols || (index / a.extent.block_cols + 1) * PACK_BLOCK > rows;
+        const bool edge = col0 + PACK_BLOCK > cols || first_row + PACK_BLOCK > rows;
         const SharedValues x = {reinterpret_cast<const uint4 *>(buffers + buffer * S::BYTES) + threadIdx.x};
         if (!__all_sync(0xffffffffu, bounded_wait(&full[buffer], phase, &g_packing_error, 1))) {  // whole warps leave
             for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies in flight land before the block ends
@@ -533,6 +536,9 @@ __global__ void __launch_bounds__(THREADS, 2)
         previous = buffer;
         if (++buffer == S::BUFFERS) { buffer = 0; phase ^= 1; }
         turn ^= 1;
+        first_row += rows_on;
+        col0 += cols_on;
+        if (col0 >= all_cols) { col0 -= all_cols; first_row += PACK_BLOCK; }
     }
 }
 
