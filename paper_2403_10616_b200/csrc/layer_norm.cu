@@ -50,12 +50,16 @@ struct NormArgs {
     bool params_bf16, gamma_aligned, beta_aligned;
 };
 
-// (v + eps)^-1/2, the approximation and one Newton step.
-__device__ __forceinline__ float inverse_root(float v, float eps)
+// (square / cols + eps)^-1/2.  Its error is that of every value of the row, so it is kept to the last rounding:
+// the product with 1 / cols is corrected by its remainder, and one Newton step takes the approximation's
+// residual with what the product v r rounds off (rms error 2.8e-8 instead of 5.3e-8 without either).
+__device__ __forceinline__ float inverse_root(float square, float cols, float inv_cols, float eps)
 {
+    float v = __fmul_rn(square, inv_cols);
+    if (v < 1e30f) v = fmaf(fmaf(-v, cols, square), inv_cols, v);
     v = __fadd_rn(v, eps);  // not contracted: the same value wherever this is compiled
-    const float r = rsqrtf(v);
-    const float better = r * fmaf(-0.5f * v * r, r, 1.5f);
+    const float r = rsqrtf(v), t = __fmul_rn(v, r), rest = fmaf(v, r, -t);
+    const float better = fmaf(0.5f * r, fmaf(-rest, r, fmaf(-t, r, 1.0f)), r);
     return v > 1e-30f && v < 1e30f ? better : 1.0f / sqrtf(v);  // where the step's products stay normal
 }
 
@@ -179,7 +183,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
             }
         }
         const float square = row_sum<TPR>(sum(), shared[turn + 1]);
-        const float rstd = inverse_root(__fmul_rn(square, a.inv_cols), a.eps);
+        const float rstd = inverse_root(square, (float)a.cols, a.inv_cols, a.eps);
         turn ^= 2;
         if (row < a.rows) {
             if (lane == 0) {
@@ -231,7 +235,7 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
         const float d = widen1<T>(x[c]) - mean;
         sum = fmaf(d, d, sum);
     }
-    const float rstd = inverse_root(__fmul_rn(row_sum<1024>(sum, shared[1]), a.inv_cols), a.eps);
+    const float rstd = inverse_root(row_sum<1024>(sum, shared[1]), (float)a.cols, a.inv_cols, a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean;
         if (a.rstd) a.rstd[blockIdx.x] = rstd;
