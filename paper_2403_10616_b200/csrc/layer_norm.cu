@@ -382,7 +382,8 @@ __device__ __forceinline__ float warp_sum4(const float *v)
 // partial unit of a row is copied by itself and filled up with zeros, which take no part in any sum; rows
 // elsewhere are copied with the 16-byte units around them and read value by value.  fp32 arithmetic goes in
 // pairs (f32x2): without, 32768x2048 from 8 bits takes 97 us.  Bound by instructions, about 24 for a value:
-// 32768x2048 88 us from 8 bits (3.8 TB/s) and 78 us from bf16 (5.1 TB/s), 4999x2047 in fp32 39 us.
+// 32768x2048 86 us from 8 bits (3.9 TB/s) and 78 us from bf16 (5.1 TB/s), 4999x2047 in fp32 31 us (rows of
+// stride 2049, inputs in L2: 39 us from memory).
 template <typename T, bool PACKED, bool VEC, int TPR>
 __global__ void __launch_bounds__(TPR < 512 ? 512 : TPR, 1)
     norm_back_kernel(const __grid_constant__ NormBackArgs a, int stages, int dy_bytes, int x_bytes)

@@ -12,10 +12,10 @@
 //                  shared memory while one is worked on
 //   block_kernel   fp32, and rows at any alignment: the values are loaded to registers
 //
-// Measured on 32768x3584 in bf16: pack 59 us (6.0 TB/s: bound by memory), GELU with both results 103 us and
-// its gradient 103 us (4.6 TB/s).  Those two are bound by the unit that has powers and reciprocals, two for
-// a value, beside memory: without them they take 86 and 91 us.  The norm's two launches on 32768x896 take
-// 42 us, 13 of them for the statistics; its second reads x from L2.
+// Measured on 32768x3584 in bf16: pack 59 us (6.0 TB/s: bound by memory), GELU with both results 98 us and
+// its gradient 99 us (4.8 TB/s).  Those two are bound by the unit that has powers and reciprocals, two for
+// a value, and by instructions, beside memory.  The norm's two launches on 32768x896 take 40 us, 13 of them
+// for the statistics; its second reads x from L2.
 #include "inner_common.cuh"
 
 #include <cmath>
