@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
     constexpr int UNITS = E / U, SURE = VEC ? NU - PART : 0;  // units that are inside for certain
     constexpr int THREADS = TPR < 128 ? 128 : TPR, GROUPS = THREADS / TPR;
     using Raw = typename std::conditional<VEC, uint4, T>::type;
-    extern __shared__ float params[];  // gamma, beta, each padded to whole units
+    extern __shared__ __align__(16) float params[];  // gamma, beta, each padded to whole units
     __shared__ float shared[4][TPR > 32 ? TPR / 32 : 1];  // two sums of a row, of two rows in turn
     const int lane = threadIdx.x % TPR;
     const int step = (int)gridDim.x * GROUPS;
