@@ -4,7 +4,9 @@
 //   g = dy gamma, h = (x - mean) rstd, dx = rstd (g - mean(g) - h mean(g h)), dgamma = sum dy h, dbeta = sum dy
 //
 // All sums are fp32.  The variance is summed from the centred values of the row, which is held in
-// registers, so it does not cancel for rows whose mean is large beside their spread.
+// registers, so it does not cancel for rows whose mean is large beside their spread.  The mean of fp32
+// values is corrected by the mean of x - mean: its own roundings, up to some units in the last place, can
+// be more than the spread (a row of 1000.1 had results up to 0.15 instead of 0 at eps = 1e-5).
 #include "inner_common.cuh"
 
 #include <algorithm>
@@ -37,6 +39,30 @@ __device__ __forceinline__ float row_sum(float v, float *shared)
     return v;
 }
 
+// Two sums at once.
+template <int TPR> __device__ __forceinline__ float2 row_sums(float a, float b, float2 *shared)
+{
+#pragma unroll
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    if constexpr (TPR > 32) {
+        constexpr int WARPS = TPR / 32;
+        const int warp = threadIdx.x >> 5;
+        if ((threadIdx.x & 31) == 0) shared[warp] = make_float2(a, b);
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float2 v = shared[warp / WARPS * WARPS + w];
+            a += v.x;
+            b += v.y;
+        }
+    }
+    return make_float2(a, b);
+}
+
 // ------------------------------------------------------------------------------------------ forward
 
 struct NormArgs {
@@ -61,6 +87,18 @@ __device__ __forceinline__ float inverse_root(float square, float cols, float in
     const float r = rsqrtf(v), t = __fmul_rn(v, r), rest = fmaf(v, r, -t);
     const float better = fmaf(0.5f * r, fmaf(-rest, r, fmaf(-t, r, 1.0f)), r);
     return v > 1e-30f && v < 1e30f ? better : 1.0f / sqrtf(v);  // where the step's products stay normal
+}
+
+// Corrects a mean and the sum of squares around it by `rest`, the sum of the values less that mean, and returns
+// what the values less that mean still have to lose.  Where sums leave the range of fp32 nothing is corrected.
+__device__ __forceinline__ float correct_mean(float &mean, float &square, float rest, float cols)
+{
+    const float shift = rest / cols;
+    if (!(fabsf(shift) < 1e30f)) return 0.0f;
+    mean += shift;
+    const float less = fmaf(-shift, rest, square);
+    if (less < square) square = fmaxf(less, 0.0f);
+    return shift;
 }
 
 template <typename T> __device__ __forceinline__ void store_first(T *p, const uint4 &v, int n)
@@ -97,7 +135,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
     constexpr int THREADS = TPR < 128 ? 128 : TPR, GROUPS = THREADS / TPR;
     using Raw = typename std::conditional<VEC, uint4, T>::type;
     extern __shared__ __align__(16) float params[];  // gamma, beta, each padded to whole units
-    __shared__ float shared[4][TPR > 32 ? TPR / 32 : 1];  // two sums of a row, of two rows in turn
+    // bf16: the sums of equal values, or of others of one size, are exact up to 2^16 of them
+    constexpr bool CORRECT = std::is_same<T, float>::value;
+    __shared__ float shared[2][TPR > 32 ? TPR / 32 : 1];  // the first sum of a row, of two rows in turn
+    __shared__ float2 shared2[2][TPR > 32 ? TPR / 32 : 1];  // the sums around its mean
     const int lane = threadIdx.x % TPR;
     const int step = (int)gridDim.x * GROUPS;
     int row = (int)blockIdx.x * GROUPS + (int)threadIdx.x / TPR;
@@ -156,9 +197,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
             for (int j = 0; j < UNITS; ++j)
                 if (j < SURE || j * TPR * U < cols) raw[j] = *reinterpret_cast<const Raw *>(x + j * TPR * U);
         }
-        // divided: the mean of equal values is that value
+        // divided, not multiplied: the mean of equal values is that value where their sum is exact
         const auto sum = [&] { return STATS && VEC ? sum_of(sum2[0]) + sum_of(sum2[1]) : (sums[0] + sums[1]) + (sums[2] + sums[3]); };
-        const float mean = row_sum<TPR>(sum(), shared[turn]) / (float)a.cols;
+        float mean = row_sum<TPR>(sum(), shared[turn]) / (float)a.cols;
+        f32x2 rest2 = 0ull;
+        float rest = 0.0f;
         sum2[0] = sum2[1] = 0ull;
         sums[0] = sums[1] = sums[2] = sums[3] = 0.0f;
 #pragma unroll
@@ -169,7 +212,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
                 for (int i = 0; i < U / 2; ++i) p[i] = add2(p[i], pair_of(-mean));
                 if (j >= SURE) keep_inside<U>(p, cols - j * TPR * U);
 #pragma unroll
-                for (int i = 0; i < U / 2; ++i) sum2[i & 1] = fma2(p[i], p[i], sum2[i & 1]);
+                for (int i = 0; i < U / 2; ++i) {
+                    sum2[i & 1] = fma2(p[i], p[i], sum2[i & 1]);
+                    if constexpr (CORRECT) rest2 = add2(rest2, p[i]);
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < U; ++i) v[j * U + i] -= mean;
@@ -180,11 +226,23 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
                 }
 #pragma unroll
                 for (int i = 0; i < U; ++i) sums[(j * U + i) & 3] = fmaf(v[j * U + i], v[j * U + i], sums[(j * U + i) & 3]);
+                if constexpr (CORRECT) {
+#pragma unroll
+                    for (int i = 0; i < U; ++i) rest += v[j * U + i];
+                }
             }
         }
-        const float square = row_sum<TPR>(sum(), shared[turn + 1]);
+        float square, shift = 0.0f;
+        if constexpr (CORRECT) {
+            const float2 both = row_sums<TPR>(sum(), STATS && VEC ? sum_of(rest2) : rest, shared2[turn]);
+            square = both.x;
+            shift = correct_mean(mean, square, both.y, (float)a.cols);
+        } else {
+            square = row_sum<TPR>(sum(), &shared2[turn][0].x);
+        }
         const float rstd = inverse_root(square, (float)a.cols, a.inv_cols, a.eps);
-        turn ^= 2;
+        const float loss = shift == 0.0f ? 0.0f : -shift * rstd;  // of (x - mean) rstd
+        turn ^= 1;
         if (row < a.rows) {
             if (lane == 0) {
                 if (a.mean) a.mean[row] = mean;
@@ -192,6 +250,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
             }
             if constexpr (!STATS) {
                 const float *gamma = params + lane * U, *beta = gamma + padded;
+                const auto hat = [&](float d) { return CORRECT ? fmaf(d, rstd, loss) : d * rstd; };
 #pragma unroll
                 for (int j = 0; j < UNITS; ++j) {
                     if (j >= SURE && j * TPR * U >= cols) continue;
@@ -201,10 +260,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
                         for (int i = 0; i < U; i += 4) {
                             const float4 g = *reinterpret_cast<const float4 *>(gamma + j * TPR * U + i);
                             const float4 b = *reinterpret_cast<const float4 *>(beta + j * TPR * U + i);
-                            r[i] = fmaf(r[i] * rstd, g.x, b.x);
-                            r[i + 1] = fmaf(r[i + 1] * rstd, g.y, b.y);
-                            r[i + 2] = fmaf(r[i + 2] * rstd, g.z, b.z);
-                            r[i + 3] = fmaf(r[i + 3] * rstd, g.w, b.w);
+                            r[i] = fmaf(hat(r[i]), g.x, b.x);
+                            r[i + 1] = fmaf(hat(r[i + 1]), g.y, b.y);
+                            r[i + 2] = fmaf(hat(r[i + 2]), g.z, b.z);
+                            r[i + 3] = fmaf(hat(r[i + 3]), g.w, b.w);
                         }
                         const uint4 out = Unit<T>::narrow(r);
                         if (MODE != ROWS_RAGGED || j < SURE || j * TPR * U + U <= cols)
@@ -212,7 +271,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
                         else
                             store_first(y + j * TPR * U, out, cols - j * TPR * U);
                     } else {
-                        y[j * TPR] = narrow1<T>(fmaf(r[0] * rstd, gamma[j * TPR], beta[j * TPR]));
+                        y[j * TPR] = narrow1<T>(fmaf(hat(r[0]), gamma[j * TPR], beta[j * TPR]));
                     }
                 }
             }
@@ -225,17 +284,22 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, norm_blocks(TPR, NU, ST
 template <typename T>
 __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
 {
-    __shared__ float shared[2][32];
+    __shared__ float shared[32];
+    __shared__ float2 shared2[32];
     const T *x = static_cast<const T *>(a.x) + (long long)blockIdx.x * a.x_stride;
-    float sum = 0.0f;
+    float sum = 0.0f, rest = 0.0f;
     for (long long c = threadIdx.x; c < a.cols; c += 1024) sum += widen1<T>(x[c]);
-    const float mean = row_sum<1024>(sum, shared[0]) / (float)a.cols;
+    const float first = row_sum<1024>(sum, shared) / (float)a.cols;
     sum = 0.0f;
     for (long long c = threadIdx.x; c < a.cols; c += 1024) {
-        const float d = widen1<T>(x[c]) - mean;
+        const float d = widen1<T>(x[c]) - first;
         sum = fmaf(d, d, sum);
+        rest += d;
     }
-    const float rstd = inverse_root(row_sum<1024>(sum, shared[1]), (float)a.cols, a.inv_cols, a.eps);
+    const float2 both = row_sums<1024>(sum, rest, shared2);
+    float mean = first, square = both.x;
+    const float shift = correct_mean(mean, square, both.y, (float)a.cols);
+    const float rstd = inverse_root(square, (float)a.cols, a.inv_cols, a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean;
         if (a.rstd) a.rstd[blockIdx.x] = rstd;
@@ -243,7 +307,7 @@ __global__ void __launch_bounds__(1024) norm_long_rows_kernel(NormArgs a)
     if (!a.y) return;
     T *y = static_cast<T *>(a.y) + (long long)blockIdx.x * a.y_stride;
     for (long long c = threadIdx.x; c < a.cols; c += 1024) {
-        float r = (widen1<T>(x[c]) - mean) * rstd;
+        float r = (widen1<T>(x[c]) - first - shift) * rstd;
         if (a.gamma) r *= load_param(a.gamma, a.params_bf16, c);
         if (a.beta) r += load_param(a.beta, a.params_bf16, c);
         y[c] = narrow1<T>(r);

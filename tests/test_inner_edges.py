@@ -1,0 +1,46 @@
+"""Where the inner phase's operators have gone wrong, or lost something without a word."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2403_10616_b200 import inner
+from tests import inner_reference as ref
+from tests.test_inner_ops import CHAIN, DEV, F32, U, gen, place
+
+# ------------------------------------------------------------------ norm of rows that hardly vary
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,pad", [(40, 7, 0), (40, 100, 0), (40, 896, 0), (40, 1000, 0), (40, 1021, 3), (40, 1024, 0),
+                                           (40, 2047, 0), (40, 2045, 3), (33, 5000, 0), (20, 8190, 2), (7, 16381, 3),
+                                           (5, 20001, 0)])
+def test_norm_of_rows_of_one_fp32_value_is_zero(rows, cols, pad):
+    """The mean of equal values is that value, whatever the roundings of their sum: a mean that is off by
+    d = (n + 16) u of the value (n additions in a chain), left as it is, gives y = d / sqrt(eps).  Corrected by
+    the mean of x - mean, whose own error is that much of d again, the mean rounds to the value itself."""
+    value = torch.cat([torch.tensor([1000.1, 0.1, -3.3e4, 1e-3]), 1000 * torch.randn(rows - 4, generator=gen(cols))])
+    x = value[:, None].expand(rows, cols)
+    y, mean, rstd = inner.layer_norm(place(x, pad), stats=True)
+    big = value.double().abs()
+    twice = CHAIN * CHAIN * big + 4 * U * CHAIN * big    # of the mean of x - mean, and of y's own products
+    assert torch.equal(mean.cpu(), value)
+    assert bool((y.cpu().double().abs() <= 2 * (twice / 1e-5 ** 0.5)[:, None]).all())
+    assert bool(((rstd.cpu().double() * 1e-5 ** 0.5 - 1).abs() <= 4 * U + CHAIN * (CHAIN * big) ** 2 / 1e-5).all())
+    packed, _, mean, _ = inner.layer_norm_pack(place(x, pad))
+    assert torch.equal(mean.cpu(), value) and not bool(packed.codes.float().any())
+    dy = torch.randn(rows, cols, generator=gen(1))
+    dx, dgamma, _ = inner.layer_norm_backward(place(dy, pad), place(x, pad), mean, rstd)
+    assert not bool(dgamma.any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols,pad", [(100, 0), (896, 0), (2047, 1), (5000, 0), (20001, 0)])
+def test_norm_of_fp32_rows_whose_spread_is_small_beside_their_mean(cols, pad):
+    x = 1000.0 + 1e-3 * torch.randn(50, cols, generator=gen(cols))
+    y, mean, rstd = inner.layer_norm(place(x, pad), eps=1e-7, stats=True)
+    wy, wmean, wrstd = ref.layer_norm(x, None, None, 1e-7)
+    # the values less their mean: exact but for the mean's second error; then y's roundings and those of the variance
+    slack = 4 * CHAIN * wy.abs() + wrstd[:, None] * 1001 * (CHAIN * CHAIN + 4 * U * CHAIN)
+    assert bool(((y.cpu().double() - wy).abs() <= slack).all())
+    assert bool(((mean.cpu().double() - wmean).abs() <= 1001 * (U + CHAIN * CHAIN)).all())
