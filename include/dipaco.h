@@ -517,7 +517,10 @@ int dipaco_gelu_pack_backward(const void *dy, int64_t dy_stride, int32_t dtype, 
 
 /*
  * Product of two packed matrices on the tensor cores, C = op(A) op(B) with fp32 sums, rounded once to
- * dtype.  op transposes its argument where the flag is nonzero.  For a layer y = x W^T with x
+ * dtype.  The tensor cores truncate when they add, 32 products at a time: a sum of one sign loses up to
+ * 2^-24 of itself each time.  Sums are joined in fp32 from parts of 2048 values for results in fp32 (which
+ * lose 2^-18 at most, under 1e-6 where signs mix) and of 65536 for results in bf16 (2^-13, beside 2^-9 of
+ * rounding).  op transposes its argument where the flag is nonzero.  For a layer y = x W^T with x
  * [tokens, in] and W [out, in]:
  *   forward          y  = x  W^T    transpose_b
  *   input gradient   dx = dy W      neither

@@ -199,11 +199,13 @@ constexpr int SCALE_BYTES = 512;          // of shared memory for four columns: 
 // words are copied to tensor memory once for four steps.  Copies take the tensor cores' time: one for
 // each step cost 20 % (8192^3: 555 us, 445 without any copy).
 constexpr int QUAD = 4;
-// The tensor cores truncate when they add to an fp32 sum, which drifts by about 1.2e-8 of the sum for
-// every 32 contracted values (2.4e-5 over 65501).  Sums that are returned in fp32 are therefore taken
-// out of tensor memory every CHUNK steps, 2048 values, and added up in registers: under 1e-6.  A result
-// in bf16 has 2e-3 of rounding of its own and keeps one sum.
-constexpr int CHUNK = 16;
+// The tensor cores truncate when they add to an fp32 sum.  Every 32 contracted values lose up to 2^-24 of it
+// if all products have one sign, and less where signs mix (2.4e-5 over 65501).  Sums that are returned in fp32 are
+// therefore taken out of tensor memory every 16 steps, 2048 values, and added up in registers: under 1e-6.  A result
+// in bf16 has 2^-9 of rounding of its own: its sums are taken out every 512 steps, 65536 values, which lose less than
+// 2^-13.  (In one sum 2^21 positive products were off by a unit everywhere, 0.8 %.  Every 16 steps cost a product in
+// bf16 up to 8 %: 8192x2048x131072 1570 -> 1700 us.)
+constexpr int CHUNK_F32 = 16, CHUNK_BF16 = 512;  // powers of two
 
 struct ProductArgs {
     const uint8_t *a_scales, *b_scales;
@@ -214,6 +216,7 @@ struct ProductArgs {
     long long c_row;  // stride of C in elements
     int c_bf16, accumulate;
     // pair_kernel
+    int chunk;  // steps after which a sum is taken out of tensor memory
     int tile_n, tiles_m, tiles_n;
     int pairs;
     int whole_tiles;  // tiles that one pair computes from end to end
@@ -277,7 +280,7 @@ constexpr int PAIR_SCALE_COLUMNS = 12;
 constexpr int PAIR_SCALE_SLOTS = 5;
 constexpr int PAIR_SCALES_AT = 512 - PAIR_SCALE_SLOTS * PAIR_SCALE_COLUMNS;
 // With 256 columns the sets of sums share 60, the first two groups of 32 that are read out.
-static_assert(PAIR_WORDS_STEPS == 2 * QUAD && CHUNK % QUAD == 0 && PAIR_SCALE_SLOTS <= PAIR_STAGES && 2 * 256 - PAIR_SCALES_AT <= 64 && 2 * 224 <= PAIR_SCALES_AT, "quads and tensor memory");
+static_assert(PAIR_WORDS_STEPS == 2 * QUAD && CHUNK_F32 % QUAD == 0 && CHUNK_BF16 % QUAD == 0 && PAIR_SCALE_SLOTS <= PAIR_STAGES && 2 * 256 - PAIR_SCALES_AT <= 64 && 2 * 224 <= PAIR_SCALES_AT, "quads and tensor memory");
 constexpr int PAIR_MAX_N = 256;
 constexpr int PAIR_ROWS = 256;
 constexpr int RASTER = 8;  // row tiles that share column tiles while those are in L2
@@ -580,8 +583,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
                     const int left = item.last - item.first - at;
                     const bool words_begin = at % PAIR_WORDS_STEPS == 0;
                     const bool words_end = left <= QUAD || at % PAIR_WORDS_STEPS == PAIR_WORDS_STEPS - QUAD;
-                    const bool set_begin = CHUNKED ? at % CHUNK == 0 : at == 0;
-                    const bool set_end = left <= QUAD || (CHUNKED && at % CHUNK == CHUNK - QUAD);
+                    const bool set_begin = CHUNKED ? (at & (p.chunk - 1)) == 0 : at == 0;
+                    const bool set_end = left <= QUAD || (CHUNKED && (at & (p.chunk - 1)) == p.chunk - QUAD);
                     if (words_begin) ok = warp_wait<true>(&words_full[words_set], words_phase, 9);
                     if (set_begin) {
                         // the set before this one (its shared columns), or the one before that, has been read
@@ -654,7 +657,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
         bool ok = true;
         float total[CHUNKED ? 128 : 1];
         while (ok && walk.take(p, pair, item)) {
-            const int parts = CHUNKED ? (item.last - item.first + CHUNK - 1) / CHUNK : 1;
+            const int parts = CHUNKED ? (item.last - item.first + p.chunk - 1) / p.chunk : 1;
             if constexpr (CHUNKED) {
 #pragma unroll
                 for (int i = 0; i < 128; ++i) total[i] = 0.0f;
@@ -1108,8 +1111,10 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, transpose_b ? plan.tile_n / 2 : 128)) return DIPACO_ECUDA;
     p.store_by_tma = !accumulate && rows_aligned16(c, c_stride, m, dense_size(dtype));
     if (p.store_by_tma && !result_map(&c_map, c, m, n, m == 1 ? ceil_div(n, 8) * 8 : c_stride, dtype)) return DIPACO_ECUDA;
-    if (const int rc = p.c_bf16 ? launch_pairs<false>(a_map, b_map, c_map, p, plan.pairs, stream)
-                                : launch_pairs<true>(a_map, b_map, c_map, p, plan.pairs, stream))
+    p.chunk = p.c_bf16 ? CHUNK_BF16 : CHUNK_F32;
+    const bool chunked = !p.c_bf16 || p.steps > p.chunk;
+    if (const int rc = chunked ? launch_pairs<true>(a_map, b_map, c_map, p, plan.pairs, stream)
+                               : launch_pairs<false>(a_map, b_map, c_map, p, plan.pairs, stream))
         return rc;
     const int64_t dealt = (int64_t)plan.tiles_m * plan.tiles_n - plan.whole_tiles;
     if (dealt > 0)

@@ -4,9 +4,10 @@ from __future__ import annotations
 import pytest
 import torch
 
+from paper_2403_10616_b200 import binding as B
 from paper_2403_10616_b200 import inner
 from tests import inner_reference as ref
-from tests.test_inner_ops import CHAIN, DEV, F32, U, gen, place
+from tests.test_inner_ops import BF16, CHAIN, DEV, U, gen, half, place
 
 # ------------------------------------------------------------------ norm of rows that hardly vary
 
@@ -44,3 +45,30 @@ def test_norm_of_fp32_rows_whose_spread_is_small_beside_their_mean(cols, pad):
     slack = 4 * CHAIN * wy.abs() + wrstd[:, None] * 1001 * (CHAIN * CHAIN + 4 * U * CHAIN)
     assert bool(((y.cpu().double() - wy).abs() <= slack).all())
     assert bool(((mean.cpu().double() - wmean).abs() <= 1001 * (U + CHAIN * CHAIN)).all())
+
+
+# ------------------------------------------------------------------ products over many values
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [65536, 2 ** 20 + 40])
+def test_long_sums_in_bf16_do_not_drift(k):
+    """Positive products, added up by truncation on the tensor cores: 32 of them lose up to 2^-24 of the sum, 2^-13
+    over the 65536 that are added there at most; the parts are joined in fp32.  74 row tiles of one column tile:
+    no pair of SMs leaves its sum to others."""
+    m, n = 74 * 256, 32
+    g = torch.Generator(device=DEV)
+    g.manual_seed(k)
+
+    def operand(codes, rows):
+        hold = torch.empty(rows, -(-k // 16) * 16, dtype=torch.float8_e4m3fn, device=DEV)[:, :k]
+        hold.copy_(codes.expand(rows, k))
+        return inner.Packed(hold, torch.ones(-(-rows // 128), -(-k // 128), device=DEV).to(torch.float8_e8m0fnu))
+
+    a = (torch.randn(1, k, device=DEV, generator=g) * 20).abs().to(torch.float8_e4m3fn)
+    b = (torch.randn(n, k, device=DEV, generator=g) * 20).abs().to(torch.float8_e4m3fn)
+    want = a.double() @ b.double().t()
+    got = inner.packed_matmul(operand(a, m), operand(b, n), transpose_b=True)
+    assert inner.inner_status() == B.DIPACO_OK
+    drift = 2.0 ** -13 + k / 65536 * U
+    assert bool(((got.double() - want).abs() <= half(BF16, want * (1 + drift)) + drift * want).all())
