@@ -541,6 +541,13 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
  */
 int dipaco_inner_status(int32_t device, void *cuda_stream);
 
+/*
+ * Diagnostic: make a bounded wait of the norms (operators = 0), of the packing kernels (1) or of the
+ * products (2) run out on purpose, harmlessly: one warp waits at most limit_ns (1 .. 1e9) on a barrier that
+ * nothing will complete; no copy is in flight and no buffer of the caller is involved.
+ */
+int dipaco_selftest_inner_wait_expiry(int32_t operators, int64_t limit_ns, int32_t device, void *cuda_stream);
+
 const char *dipaco_strerror(int status);
 
 #ifdef __cplusplus

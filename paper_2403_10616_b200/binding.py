@@ -54,7 +54,7 @@ EXPORTS = [
     "dipaco_pack", "dipaco_unpack", "dipaco_layer_norm", "dipaco_layer_norm_pack",
     "dipaco_layer_norm_workspace", "dipaco_layer_norm_backward", "dipaco_gelu_pack",
     "dipaco_gelu_pack_backward", "dipaco_packed_matmul_workspace", "dipaco_packed_matmul",
-    "dipaco_inner_status",
+    "dipaco_inner_status", "dipaco_selftest_inner_wait_expiry",
 ]
 
 _lib = None
@@ -130,6 +130,7 @@ def load() -> ctypes.CDLL:
     lib.dipaco_packed_matmul_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
     lib.dipaco_packed_matmul.argtypes = [pk, pk, i32, i32, vp, i64, i32, i32, vp, i64, i32, vp]
     lib.dipaco_inner_status.argtypes = [i32, vp]
+    lib.dipaco_selftest_inner_wait_expiry.argtypes = [i32, i64, i32, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("dipaco_strerror", "dipaco_launch_count"):
@@ -451,6 +452,11 @@ def dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype,
 
 def dipaco_inner_status(device, stream) -> int:
     return int(load().dipaco_inner_status(device, stream))
+
+
+def dipaco_selftest_inner_wait_expiry(operators, limit_ns, device, stream) -> None:
+    _check(load().dipaco_selftest_inner_wait_expiry(operators, limit_ns, device, stream),
+           "dipaco_selftest_inner_wait_expiry")
 
 
 # ------------------------------------------------------------------ convenience owner

@@ -106,6 +106,10 @@ template <typename Symbol> bool take_error_word(const Symbol &symbol, bool &expi
 bool take_packing_error(bool &expired);  // of packed.cu
 bool take_norm_error(bool &expired);     // of layer_norm.cu
 
+// Launches of a warp whose wait runs out (dipaco_selftest_inner_wait_expiry).
+int expire_packing_wait(unsigned long long limit_ns, cudaStream_t stream);
+int expire_norm_wait(unsigned long long limit_ns, cudaStream_t stream);
+
 // ------------------------------------------------------------------------------------------ device
 
 // True on one thread of the warp.  Asynchronous copies and products are issued under it: the compiler

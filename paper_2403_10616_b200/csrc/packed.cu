@@ -627,9 +627,27 @@ int check_dense(const void *x, int64_t stride, int64_t rows, int64_t cols, int d
     return dense_ok(x, stride, rows, cols, dtype) ? DIPACO_OK : DIPACO_EINVAL;
 }
 
+// A warp waits, for a limited time, on a barrier that nothing completes: no copy is in flight.
+__global__ void __launch_bounds__(32) wait_expiry_kernel(unsigned long long limit_ns)
+{
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    __all_sync(0xffffffffu, bounded_wait(&bar, 0, &g_packing_error, 9, limit_ns));
+}
+
 } // namespace
 
 bool dipaco::take_packing_error(bool &expired) { return take_error_word(g_packing_error, expired); }
+
+int dipaco::expire_packing_wait(unsigned long long limit_ns, cudaStream_t stream)
+{
+    wait_expiry_kernel<<<1, 32, 0, stream>>>(limit_ns);
+    return launch_status();
+}
 
 extern "C" {
 

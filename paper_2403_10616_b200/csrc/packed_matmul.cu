@@ -82,7 +82,8 @@ __device__ __forceinline__ bool test_arrived(uint64_t *bar, unsigned parity)
 }
 // Bounded wait of a whole warp, which agrees on how it ended: what follows takes all its lanes.  CLUSTER:
 // ordered after what the other block of the pair did before it arrived.
-template <bool CLUSTER = false> __device__ __forceinline__ bool warp_wait(uint64_t *bar, unsigned parity, int code)
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, unsigned parity, int code, unsigned long long limit_ns = BULK_WAIT_LIMIT_NS)
 {
     const auto arrived = [&] {
         const bool ok = CLUSTER ? try_wait_cluster(bar, parity) : ptx::mbar_try_wait(bar, parity);
@@ -94,7 +95,7 @@ template <bool CLUSTER = false> __device__ __forceinline__ bool warp_wait(uint64
 #pragma unroll 1
         for (int i = 0; i < 256; ++i)
             if (arrived()) return true;
-        if (__any_sync(0xffffffffu, ptx::global_timer_ns() - t0 > BULK_WAIT_LIMIT_NS)) {
+        if (__any_sync(0xffffffffu, ptx::global_timer_ns() - t0 > limit_ns)) {
             atomicCAS(&g_product_error, 0, code);
             return false;
         }
@@ -928,6 +929,18 @@ template <int M> __global__ void __launch_bounds__(FEW_THREADS) few_kernel(const
     }
 }
 
+// A warp waits, for a limited time, on a barrier that nothing completes: no copy is in flight.
+__global__ void __launch_bounds__(32) wait_expiry_kernel(unsigned long long limit_ns)
+{
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    warp_wait(&bar, 0, 9, limit_ns);
+}
+
 // ------------------------------------------------------------------------------------------ host
 
 // Boxes of `rows` x 128 codes in the 128-byte swizzle; codes outside the matrix read as zero.
@@ -1119,6 +1132,18 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     const int64_t dealt = (int64_t)plan.tiles_m * plan.tiles_n - plan.whole_tiles;
     if (dealt > 0)
         join_kernel<<<(unsigned)(dealt * 2 * (plan.tile_n / 32)), 256, 0, stream>>>(p);
+    return launch_status();
+}
+
+int dipaco_selftest_inner_wait_expiry(int32_t operators, int64_t limit_ns, int32_t device, void *cuda_stream)
+{
+    if (operators < 0 || operators > 2 || limit_ns < 1 || limit_ns > 1000000000ll || device < 0) return DIPACO_EINVAL;
+    DeviceScope scope(device);
+    if (!scope.ok) return DIPACO_ECUDA;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (operators == 0) return expire_norm_wait(limit_ns, stream);
+    if (operators == 1) return expire_packing_wait(limit_ns, stream);
+    wait_expiry_kernel<<<1, 32, 0, stream>>>(limit_ns);
     return launch_status();
 }
 

@@ -5,9 +5,10 @@ import pytest
 import torch
 
 from paper_2403_10616_b200 import binding as B
+from paper_2403_10616_b200 import build as libbuild
 from paper_2403_10616_b200 import inner
 from tests import inner_reference as ref
-from tests.test_inner_ops import BF16, CHAIN, DEV, U, gen, half, place
+from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, gen, half, place
 
 # ------------------------------------------------------------------ norm of rows that hardly vary
 
@@ -72,3 +73,45 @@ def test_long_sums_in_bf16_do_not_drift(k):
     assert inner.inner_status() == B.DIPACO_OK
     drift = 2.0 ** -13 + k / 65536 * U
     assert bool(((got.double() - want).abs() <= half(BF16, want * (1 + drift)) + drift * want).all())
+
+
+# ------------------------------------------------------------------ waits that run out
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("operators", [0, 1, 2])  # norms, packing, products: each has an error word of its own
+def test_a_wait_that_ran_out_is_reported_once(operators):
+    """The diagnostic entry point makes a wait of 1 ms run out on a barrier of its own.  The kernel ends by
+    itself, the status says so once, and the operators work as before."""
+    x = torch.randn(300, 256, device=DEV)
+    w = inner.pack(torch.randn(200, 256, device=DEV))
+
+    def step():
+        y, kept, mean, rstd = inner.layer_norm_pack(x)
+        return (inner.packed_matmul(y, w, transpose_b=True, out_dtype=F32), *inner.layer_norm_backward(x, kept, mean, rstd))
+
+    want = step()
+    assert inner.inner_status() == B.DIPACO_OK
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    B.dipaco_selftest_inner_wait_expiry(operators, 1_000_000, 0, stream())
+    end.record()
+    torch.cuda.synchronize()
+    assert 0.9 <= start.elapsed_time(end) < 100.0
+    assert inner.inner_status() == B.DIPACO_ETIMEOUT
+    assert inner.inner_status() == B.DIPACO_OK
+    for got, before in zip(step(), want):
+        assert torch.equal(got, before)
+    assert inner.inner_status() == B.DIPACO_OK
+
+
+def test_the_waits_diagnostic_refuses():
+    libbuild.build()
+    for bad in ((-1, 1000, 0), (3, 1000, 0), (0, 0, 0), (0, 2 * 10 ** 9, 0), (0, 1000, -1)):
+        with pytest.raises(B.DipacoError) as e:
+            B.dipaco_selftest_inner_wait_expiry(*bad, None)
+        assert e.value.status == B.DIPACO_EINVAL
