@@ -536,8 +536,9 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
 
 /*
  * Every wait inside the kernels of this section is bounded (4 s).  A wait that runs out ends its kernel in
- * an orderly way with undefined results.  This call synchronises the stream and returns DIPACO_ETIMEOUT
- * once if that has happened on the device since the last query, DIPACO_OK otherwise.
+ * an orderly way with undefined results; later calls work again.  This call synchronises the stream and
+ * returns DIPACO_ETIMEOUT if that has happened on the device, on whatever stream, since it was last called
+ * for this stream (or ever, the first time), DIPACO_OK otherwise: no stream takes the news from another.
  */
 int dipaco_inner_status(int32_t device, void *cuda_stream);
 

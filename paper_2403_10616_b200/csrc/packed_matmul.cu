@@ -19,6 +19,10 @@
 
 #include <algorithm>
 #include <cmath>
+#include <exception>
+#include <map>
+#include <mutex>
+#include <utility>
 
 using namespace dipaco;
 
@@ -1153,10 +1157,23 @@ int dipaco_inner_status(int32_t device, void *cuda_stream)
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return DIPACO_ECUDA;
-    bool expired = false;
-    if (!take_error_word(g_product_error, expired) || !take_packing_error(expired) || !take_norm_error(expired))
-        return launch_status();
-    return expired ? DIPACO_ETIMEOUT : DIPACO_OK;
+    try {
+        // A word is cleared by whoever reads it first, so that the news is kept here for the streams that ask later.
+        static std::mutex mutex;
+        static std::map<int32_t, uint64_t> &happened = *new std::map<int32_t, uint64_t>;  // time-outs on a device
+        static std::map<std::pair<int32_t, void *>, uint64_t> &told = *new std::map<std::pair<int32_t, void *>, uint64_t>;
+        const std::lock_guard<std::mutex> lock(mutex);
+        uint64_t &count = happened[device], &known = told[{device, cuda_stream}];
+        bool expired = false;
+        const bool read = take_error_word(g_product_error, expired) && take_packing_error(expired) && take_norm_error(expired);
+        if (expired) ++count;
+        if (!read) return launch_status();
+        if (known == count) return DIPACO_OK;
+        known = count;
+        return DIPACO_ETIMEOUT;
+    } catch (const std::exception &) {  // no memory for the books: nothing has been read
+        return DIPACO_ENOMEM;
+    }
 }
 
 } // extern "C"

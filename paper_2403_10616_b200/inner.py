@@ -232,8 +232,8 @@ def packed_matmul(a: Packed, b: Packed, transpose_a: bool = False, transpose_b: 
 
 
 def inner_status(device=None) -> int:
-    """Waits for the current stream and reports DIPACO_OK, or DIPACO_ETIMEOUT once after a bounded
-    wait inside one of these operators ran out."""
+    """Waits for the current stream and reports DIPACO_OK, or DIPACO_ETIMEOUT once (to each stream that
+    asks) after a bounded wait inside one of these operators ran out on the device."""
     dev = None if device is None else torch.device(device).index
     dev = torch.cuda.current_device() if dev is None else dev
     return B.dipaco_inner_status(dev, _stream(dev))

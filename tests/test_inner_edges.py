@@ -109,6 +109,25 @@ def test_a_wait_that_ran_out_is_reported_once(operators):
     assert inner.inner_status() == B.DIPACO_OK
 
 
+@pytest.mark.gpu
+def test_no_stream_takes_the_news_of_a_time_out_from_another():
+    mine, other = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def status(of):
+        with torch.cuda.stream(of):
+            return inner.inner_status()
+
+    for s in (mine, other):  # whatever happened before
+        status(s)
+        assert status(s) == B.DIPACO_OK
+    with torch.cuda.stream(mine):
+        B.dipaco_selftest_inner_wait_expiry(2, 1_000_000, 0, stream())
+    torch.cuda.synchronize()
+    assert status(other) == B.DIPACO_ETIMEOUT and status(mine) == B.DIPACO_ETIMEOUT
+    assert status(other) == B.DIPACO_OK and status(mine) == B.DIPACO_OK
+    assert inner.inner_status() == B.DIPACO_ETIMEOUT and inner.inner_status() == B.DIPACO_OK
+
+
 def test_the_waits_diagnostic_refuses():
     libbuild.build()
     for bad in ((-1, 1000, 0), (3, 1000, 0), (0, 0, 0), (0, 2 * 10 ** 9, 0), (0, 1000, -1)):
