@@ -5,6 +5,10 @@ the products), the GELU that writes and reads such checkpoints, and the product 
 on the tensor cores.  Each function allocates its results (and workspace) with torch, launches on the
 current stream of the tensors' device, and raises ``ValueError`` for shapes and dtypes that do not
 fit together or ``binding.DipacoError`` with the library's status.  There is no CPU path.
+
+Autograd records nothing of these calls: the gradients are calls of their own.  A tensor that requires a
+gradient is refused while gradients are being recorded; inside ``torch.no_grad()`` or a
+``torch.autograd.Function``, or detached, it is taken.
 """
 from __future__ import annotations
 
@@ -39,6 +43,8 @@ class Packed:
             stride = (cols + 15) & ~15
         if not codes.is_cuda or scales.get_device() != codes.get_device():
             raise ValueError("codes and scales must be on one CUDA device")
+        if codes.requires_grad or scales.requires_grad:
+            _refuse_gradient("codes or scales")
         self.codes, self.scales = codes, scales
         self.struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
 
@@ -68,8 +74,16 @@ def _packed_beside(x: torch.Tensor, rows: int, cols: int) -> Packed:
     return p
 
 
+def _refuse_gradient(name: str) -> None:
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, which these operators do not record: detach it, or call under "
+                         "torch.no_grad()" % name)
+
+
 def _dense(name: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
     """(rows, cols, row stride, dtype code) of a row-major matrix on a CUDA device."""
+    if x.requires_grad:
+        _refuse_gradient(name)
     code = _CODES.get(x.dtype)
     if code is None or x.dim() != 2 or not x.is_cuda:
         raise ValueError("%s must be a float32 or bfloat16 matrix on a CUDA device" % name)
@@ -82,6 +96,8 @@ def _dense(name: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
 
 def _param(cols: int, dev: int, t: torch.Tensor) -> Tuple[int, int]:
     """(pointer, dtype code) of gamma or beta."""
+    if t.requires_grad:
+        _refuse_gradient("gamma or beta")
     code = _CODES.get(t.dtype)
     if code is None or t.shape != (cols,) or t.get_device() != dev or (cols > 1 and t.stride(0) != 1):
         raise ValueError("gamma and beta must be contiguous float32 or bfloat16 vectors of the row's length")
@@ -159,6 +175,8 @@ def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], mean: 
     for t in (mean, rstd):
         if t.shape != (rows,) or t.dtype != _F32 or t.get_device() != dev or not t.is_contiguous():
             raise ValueError("mean and rstd must be contiguous float32 vectors with one entry per row")
+        if t.requires_grad:
+            _refuse_gradient("mean or rstd")
     if isinstance(x, Packed):
         x_ptr, x_stride, packed = None, 0, x.struct
         x_shape, x_dev = x.shape, x.codes.get_device()

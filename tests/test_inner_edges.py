@@ -134,3 +134,52 @@ def test_the_waits_diagnostic_refuses():
         with pytest.raises(B.DipacoError) as e:
             B.dipaco_selftest_inner_wait_expiry(*bad, None)
         assert e.value.status == B.DIPACO_EINVAL
+
+
+# ------------------------------------------------------------------ gradients that would not be recorded
+
+
+@pytest.mark.gpu
+def test_tensors_that_require_a_gradient_are_refused_while_it_is_recorded():
+    x, g = torch.randn(32, 64, device=DEV), torch.ones(64, device=DEV)
+    leaf, weight = x.clone().requires_grad_(), g.clone().requires_grad_()
+    stat = torch.ones(32, device=DEV)
+    p, q = inner.pack(x), inner.pack(x.t().contiguous())
+    out = torch.zeros(32, 32, device=DEV, requires_grad=True)
+    calls = [lambda: inner.pack(leaf), lambda: inner.pack(leaf * 2), lambda: inner.layer_norm(leaf), lambda: inner.layer_norm(x, weight),
+             lambda: inner.layer_norm(x, g, weight, stats=True), lambda: inner.layer_norm_pack(leaf),
+             lambda: inner.layer_norm_pack(x, weight, g), lambda: inner.layer_norm_backward(leaf, x, stat, stat),
+             lambda: inner.layer_norm_backward(x, leaf, stat, stat), lambda: inner.layer_norm_backward(x, p, stat, stat, weight),
+             lambda: inner.layer_norm_backward(x, p, stat.clone().requires_grad_(), stat), lambda: inner.gelu_pack(leaf),
+             lambda: inner.gelu_pack_backward(leaf, p), lambda: inner.packed_matmul(p, q, out=out)]
+    for call in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    with torch.inference_mode():
+        inner.layer_norm(leaf, weight)
+    assert torch.equal(inner.layer_norm(leaf.detach(), weight.detach()), inner.layer_norm(x, g))
+
+
+@pytest.mark.gpu
+def test_the_operators_serve_an_autograd_function():
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, gamma, beta):
+            y, mean, rstd = inner.layer_norm(x, gamma, beta, stats=True)
+            ctx.save_for_backward(x, mean, rstd, gamma)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return inner.layer_norm_backward(dy.contiguous(), *ctx.saved_tensors)
+
+    x = torch.randn(40, 100, generator=gen(1)).to(DEV).requires_grad_()
+    gamma, beta = (torch.randn(100, generator=gen(i)).to(DEV).requires_grad_() for i in (2, 3))
+    dy = torch.randn(40, 100, generator=gen(4)).to(DEV)
+    Norm.apply(x, gamma, beta).backward(dy)
+    with torch.no_grad():
+        _, mean, rstd = inner.layer_norm(x, gamma, beta, stats=True)
+        for got, want in zip((x.grad, gamma.grad, beta.grad), inner.layer_norm_backward(dy, x, mean, rstd, gamma)):
+            assert torch.equal(got, want)
