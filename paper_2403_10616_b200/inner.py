@@ -26,9 +26,12 @@ _stream = torch._C._cuda_getCurrentRawStream  # of a device index
 
 class Packed:
     """A matrix in 8 bits: ``codes`` [rows, cols] float8_e4m3fn, row stride a multiple of 16, and
-    ``scales`` [ceil(rows/128), ceil(cols/128)] float8_e8m0fnu, contiguous; value = code * scale."""
+    ``scales`` [ceil(rows/128), ceil(cols/128)] float8_e8m0fnu, contiguous; value = code * scale.
 
-    __slots__ = ("codes", "scales", "struct")
+    The tensors cannot be exchanged for others: ``struct`` holds the addresses of their data, which has to
+    stay where it is.  Copies (``copy``, ``pickle``) are built anew from their own tensors."""
+
+    __slots__ = ("_codes", "_scales", "_struct")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         rows, cols = codes.shape
@@ -45,8 +48,23 @@ class Packed:
             raise ValueError("codes and scales must be on one CUDA device")
         if codes.requires_grad or scales.requires_grad:
             _refuse_gradient("codes or scales")
-        self.codes, self.scales = codes, scales
-        self.struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
+        self._codes, self._scales = codes, scales
+        self._struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
+
+    def __reduce__(self):  # as bytes: torch does not pickle e8m0
+        return _packed_of_bytes, (self._codes.view(torch.uint8), self._scales.view(torch.uint8))
+
+    @property
+    def codes(self) -> torch.Tensor:
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        return self._scales
+
+    @property
+    def struct(self) -> B.PackedStruct:
+        return self._struct
 
     @classmethod
     def empty(cls, rows: int, cols: int, device) -> "Packed":
@@ -55,11 +73,15 @@ class Packed:
 
     @property
     def shape(self) -> Tuple[int, int]:
-        return self.struct.rows, self.struct.cols
+        return self._struct.rows, self._struct.cols
 
     @property
     def device(self) -> torch.device:
-        return self.codes.device
+        return self._codes.device
+
+
+def _packed_of_bytes(codes: torch.Tensor, scales: torch.Tensor) -> Packed:
+    return Packed(codes.view(_E4M3), scales.view(_E8M0))
 
 
 def _packed_beside(x: torch.Tensor, rows: int, cols: int) -> Packed:
@@ -68,9 +90,9 @@ def _packed_beside(x: torch.Tensor, rows: int, cols: int) -> Packed:
     codes = x.new_empty((rows, stride), dtype=_E4M3)
     scales = x.new_empty(((rows + 127) >> 7, (cols + 127) >> 7), dtype=_E8M0)
     p = object.__new__(Packed)
-    p.codes = codes if stride == cols else codes[:, :cols]
-    p.scales = scales
-    p.struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
+    p._codes = codes if stride == cols else codes[:, :cols]
+    p._scales = scales
+    p._struct = B.PackedStruct(codes.data_ptr(), scales.data_ptr(), rows, cols, stride)
     return p
 
 

@@ -1,6 +1,9 @@
 """Where the inner phase's operators have gone wrong, or lost something without a word."""
 from __future__ import annotations
 
+import copy
+import pickle
+
 import pytest
 import torch
 
@@ -183,3 +186,32 @@ def test_the_operators_serve_an_autograd_function():
         _, mean, rstd = inner.layer_norm(x, gamma, beta, stats=True)
         for got, want in zip((x.grad, gamma.grad, beta.grad), inner.layer_norm_backward(dy, x, mean, rstd, gamma)):
             assert torch.equal(got, want)
+
+
+# ------------------------------------------------------------------ packed matrices as objects
+
+
+@pytest.mark.gpu
+def test_a_packed_matrix_keeps_its_tensors():
+    """The kernels go by addresses taken when the object was made: other tensors would not reach them."""
+    p, q = inner.pack(torch.ones(64, 100, device=DEV)), inner.pack(torch.zeros(64, 100, device=DEV))
+    for name in ("codes", "scales", "struct"):
+        with pytest.raises(AttributeError):
+            setattr(p, name, getattr(q, name))
+    p.codes.copy_(q.codes)  # in place: the same data
+    assert not bool(inner.unpack(p).any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [(64, 100), (1, 100), (300, 256), (3, 0), (0, 3)])
+def test_a_packed_matrix_can_be_copied(rows, cols):
+    x = torch.randn(rows, cols, generator=gen(rows)).to(DEV)
+    p = inner.pack(x)
+    want = inner.unpack(p, F32)
+    shared = copy.copy(p)
+    deep, read = copy.deepcopy(p), pickle.loads(pickle.dumps(p))
+    p.codes.view(torch.uint8).zero_()
+    for other in (deep, read):
+        assert other.shape == (rows, cols) and torch.equal(inner.unpack(other, F32), want)
+        assert rows * cols == 0 or other.struct.codes not in (p.struct.codes, shared.struct.codes)
+    assert not bool(inner.unpack(shared, F32).any())
