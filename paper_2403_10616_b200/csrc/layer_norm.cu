@@ -73,7 +73,7 @@ struct NormArgs {
     long long x_stride, y_stride;
     int rows, cols;
     float eps, inv_cols;
-    bool params_bf16, gamma_aligned, beta_aligned;
+    bool params_bf16;
 };
 
 // (square / cols + eps)^-1/2.  Its error is that of every value of the row, so it is kept to the last rounding:
@@ -355,7 +355,8 @@ template <typename T, int MODE> int launch_norm(const NormArgs &a, cudaStream_t 
     if (units <= 128 * 4) return launch_norm_shape<T, MODE, 128, 4, 2>(a, stream);
     if (units <= 128 * 8) return launch_norm_shape<T, MODE, 128, 8, 4>(a, stream);
     if (units <= 256 * 8) return launch_norm_shape<T, MODE, 256, 8, 4>(a, stream);
-    if (a.cols <= NORM_WIDEST) return launch_norm_shape<T, MODE, 512, 8, 4>(a, stream);
+    if constexpr (sizeof(T) == 4)  // in bf16 256 threads hold the widest row
+        if (a.cols <= NORM_WIDEST) return launch_norm_shape<T, MODE, 512, 8, 4>(a, stream);
     norm_long_rows_kernel<T><<<(unsigned)a.rows, 1024, 0, stream>>>(a);
     return launch_status();
 }
@@ -912,7 +913,7 @@ int dipaco_layer_norm(const void *x, int64_t x_stride, const void *gamma, const 
         return DIPACO_OK;
     }
     NormArgs a = {x, y, gamma, beta, mean, rstd, x_stride, y_stride, (int)rows, (int)cols, eps, 1.0f / (float)cols,
-                  param_dtype == DIPACO_BF16, (uintptr_t)gamma % 16 == 0, (uintptr_t)beta % 16 == 0};
+                  param_dtype == DIPACO_BF16};
     const int size = dense_size(dtype);
     const bool vec = rows_aligned16(x, x_stride, rows, size) && (!y || rows_aligned16(y, y_stride, rows, size));
     const int mode = !vec ? ROWS_SINGLE : cols * size % 16 ? ROWS_RAGGED : ROWS_UNITS;
