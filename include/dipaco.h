@@ -439,8 +439,9 @@ int dipaco_module_sync_static(float *theta, float *momentum, int64_t numel, int3
  * Conventions.  All pointers are device pointers; the calls are asynchronous on cuda_stream, allocate
  * nothing and can be captured in a CUDA graph.  Arguments are checked before anything is launched
  * (DIPACO_EINVAL, or DIPACO_ELIMIT for extents of about 2^31 and more).  A dense matrix is row-major
- * with a row stride in elements, at any element alignment; 16-byte aligned rows are fastest, and rows
- * at other alignments are read in the aligned 16-byte units that hold their values.  dtype and
+ * with a row stride in elements, at any element alignment; 16-byte aligned rows are fastest.  Rows at
+ * other alignments are read in the aligned 16-byte units that hold their values, except by the forward
+ * norm, which reads and writes them value by value unless both x and y are aligned.  dtype and
  * param_dtype are DIPACO_F32 or DIPACO_BF16.  Outputs must not overlap inputs.  Extents of zero are
  * allowed.  Every sum is fp32 and taken in an order that depends on shapes, types and alignment alone:
  * results are bitwise reproducible.
@@ -461,7 +462,8 @@ typedef struct dipaco_packed {
     int64_t rows, cols, stride;
 } dipaco_packed;
 
-/* Dense to packed, and back (a code times its scale, rounded once to dtype). */
+/* Dense to packed, and back (a code times its scale, rounded once to dtype: an infinity for 2^128, to which
+ * magnitudes near the largest fp32 value round). */
 int dipaco_pack(const void *x, int64_t x_stride, int32_t dtype, const dipaco_packed *out, int32_t device,
                 void *cuda_stream);
 int dipaco_unpack(const dipaco_packed *x, void *y, int64_t y_stride, int32_t dtype, int32_t device,

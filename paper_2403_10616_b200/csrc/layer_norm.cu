@@ -122,6 +122,10 @@ enum : int { ROWS_SINGLE, ROWS_UNITS, ROWS_RAGGED };
 // first launch of the packed norm, 32768x896, 15 -> 13 us; with y to write pairs were slower.
 // Measured: 16384x2048 in bf16 with statistics 32 us, 4.2 TB/s; what is left is the warps' waiting for
 // their own chains of sums and exchanges (they issue in a third of the cycles), not instructions.
+// The blocks on an SM are those of widths to 2048 with y written; from 7161 bf16 values on gamma and beta leave room in
+// shared memory for fewer than the grid assumes, and its last blocks run in a second wave (8192x7000 86 us).
+// Rows off 16 bytes are read by single values and spill registers: 16384x2048 in bf16 98 us.  fp32: 16384x2048
+// 51 us, 32768x896 46 us (with the mean corrected; 45 without).
 constexpr int norm_blocks(int tpr, int nu, bool stats) { return tpr > 128 ? 1 : nu > 4 ? 4 : stats ? 8 : 6; }  // on an SM
 
 template <typename T, int MODE, int TPR, int NU, int PART, bool STATS>

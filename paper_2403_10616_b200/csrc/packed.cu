@@ -12,10 +12,11 @@
 //                  shared memory while one is worked on
 //   block_kernel   fp32, and rows at any alignment: the values are loaded to registers
 //
-// Measured on 32768x3584 in bf16: pack 59 us (6.0 TB/s: bound by memory), GELU with both results 98 us and
-// its gradient 99 us (4.8 TB/s).  Those two are bound by the unit that has powers and reciprocals, two for
-// a value, and by instructions, beside memory.  The norm's two launches on 32768x896 take 40 us, 13 of them
-// for the statistics; its second reads x from L2.
+// Measured on 32768x3584 in bf16: pack 59 us (6.0 TB/s: bound by memory), GELU with both results 102 to 104 us
+// and its gradient 102 to 106 us (4.5 TB/s).  Powers and reciprocals, two for a value, would take 52 us of those two,
+// instructions 60 and memory 72: the three overlap in part.  The norm's two launches on 32768x896 take
+// 41 us, 13 of them for the statistics; its second reads x from L2.  From fp32 (block_kernel) the GELU and its
+// gradient take 182 and 214 us, and the norm of 32768x896 takes 85 us with its statistics: they spill registers.
 #include "inner_common.cuh"
 
 #include <cmath>
@@ -542,7 +543,8 @@ __global__ void __launch_bounds__(THREADS, 2)
     }
 }
 
-// Four codes per thread; bound by memory.
+// Four codes per thread.  32768x3584 to bf16 107 us, to fp32 125 us (3.3 and 4.7 TB/s): bound by instructions (22 for a
+// value, 71 % of the issue slots, a division of 64-bit numbers among them), with DRAM at 34 % for bf16.
 template <typename T>
 __global__ void __launch_bounds__(256) unpack_kernel(const uint8_t *codes, long long codes_stride,
                                                      const uint8_t *scales, T *y, long long y_stride, int rows,

@@ -11,10 +11,12 @@
 //                  each loads half of A and half of B and keeps half of the sums
 //   few_kernel     a few tokens through a weight: every weight is read once and multiplied in registers
 //
-// Measured: 8192^3 380 us in short runs (2.9 PFLOP/s) and 455 us under the 1000 W cap, 16384x2048x8192 189
-// and 226 us, 32768x3584x896 102 and 123 us.  In long runs power sets the clock (1.3 to 1.45 GHz), not the
-// instruction stream or memory.  The weight's gradient 3584x896 over 65501 takes 245 us, 12 of them to join
-// partial sums.
+// Measured: 8192^3 380 us in short runs (2.9 PFLOP/s) and 455 us under the 1000 W cap, 16384x2048x8192 176
+// and 227 us, 32768x3584x896 100 and 124 us, the weight's gradient 3584x896 over 65501 198 and 244 us, 12 of them
+// to join partial sums.  In long runs power sets the clock (1.3 to 1.45 GHz).  The tensor cores are busy for 86 %
+// of the second's cycles, 52 % of the third's (seven steps to a tile, whose operands come from L2: 1.28 GB in 108 us,
+// and 235 MB of results) and 65 % of the last's.  Adding to C takes longer, a dependent read of C for every row of a
+// group of 32 columns: 32768x3584x896 in bf16 1.33 ms instead of 0.10, 16384x2048x8192 0.49.
 #include "inner_common.cuh"
 
 #include <algorithm>
