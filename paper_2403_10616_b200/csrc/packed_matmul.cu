@@ -229,6 +229,7 @@ struct ProductArgs {
     int whole_tiles;  // tiles that one pair computes from end to end
     int head, helpers;  // of the others a pair does the first `head` steps, and `helpers` pairs share the rest
     int store_by_tma;
+    int whole_n;  // columns in whole units of 16 bytes: the copy engine's
     float *partial;
 };
 
@@ -363,6 +364,22 @@ __device__ __forceinline__ long long partial_offset(const ProductArgs &p, int sl
     return ((long long)slot * 2 + rank) * p.tile_n * 128;
 }
 
+// The first bytes of a unit, an even number of them.
+__device__ __forceinline__ void store_head(uint8_t *to, uint4 unit, int bytes)
+{
+    if (bytes & 8) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(unit.x, unit.y);
+        unit = make_uint4(unit.z, unit.w, 0u, 0u);
+        to += 8;
+    }
+    if (bytes & 4) {
+        *reinterpret_cast<unsigned *>(to) = unit.x;
+        unit.x = unit.y;
+        to += 4;
+    }
+    if (bytes & 2) *reinterpret_cast<unsigned short *>(to) = (unsigned short)unit.x;
+}
+
 // Where an epilogue warp puts 32 columns of its 32 rows.
 __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUtensorMap &c_map, const PairItem &item,
                                                unsigned rank, int quarter, int lane, int c0, const uint32_t *words,
@@ -400,13 +417,24 @@ __device__ __forceinline__ void finish_columns(const ProductArgs &p, const CUten
             }
             ptx::fence_proxy_async();
             __syncwarp();
-            // columns and rows outside C are not written
+            // rows outside C and columns from whole_n on are not written
             const int col = col0 + part * 16;
             if (elect_one()) {
-                if (row0 < p.m && col < p.n) tma_store_2d(&c_map, ptx::smem_addr(at), col, row0);
+                if (row0 < p.m && col < p.whole_n) tma_store_2d(&c_map, ptx::smem_addr(at), col, row0);
                 ptx::bulk_commit();
             }
             __syncwarp();
+        }
+        if (p.whole_n < p.n) {
+            // the unit that C's rows end in: the copy engine would write it whole, with zeros behind them
+            const int size = p.c_bf16 ? 2 : 4, ahead = (p.whole_n - col0) * size;
+            if (ahead >= 0 && ahead < 64 * parts && row0 + lane < p.m) {
+                int of = buffer - parts + (ahead >> 6);
+                if (of < 0) of += PAIR_STAGING;
+                const uint8_t *at = staging + of * PAIR_STAGING_BYTES + lane * 64 + ((ahead & 48) ^ ((lane >> 1) & 3) * 16);
+                store_head(static_cast<uint8_t *>(p.c) + ((row0 + lane) * p.c_row + p.whole_n) * size,
+                           *reinterpret_cast<const uint4 *>(at), (p.n - p.whole_n) * size);
+            }
         }
         return;
     }
@@ -962,7 +990,7 @@ bool operand_map(CUtensorMap *map, const dipaco_packed *x, int rows)
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Boxes of 32 rows of 64 bytes of results, in the swizzle of that width.
+// Boxes of 32 rows of 64 bytes of results, in the swizzle of that width.  n is a multiple of 16 bytes.
 bool result_map(CUtensorMap *map, void *c, int64_t m, int64_t n, int64_t stride, int dtype)
 {
     const EncodeTiled encode = encode_tiled();
@@ -1128,8 +1156,9 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
     p.partial = static_cast<float *>(workspace);
     CUtensorMap a_map, b_map, c_map = {};
     if (!operand_map(&a_map, a, 128) || !operand_map(&b_map, b, transpose_b ? plan.tile_n / 2 : 128)) return DIPACO_ECUDA;
-    p.store_by_tma = !accumulate && rows_aligned16(c, c_stride, m, dense_size(dtype));
-    if (p.store_by_tma && !result_map(&c_map, c, m, n, m == 1 ? ceil_div(n, 8) * 8 : c_stride, dtype)) return DIPACO_ECUDA;
+    p.whole_n = (int)(n / (16 / dense_size(dtype)) * (16 / dense_size(dtype)));
+    p.store_by_tma = !accumulate && p.whole_n > 0 && rows_aligned16(c, c_stride, m, dense_size(dtype));
+    if (p.store_by_tma && !result_map(&c_map, c, m, p.whole_n, m == 1 ? ceil_div(n, 8) * 8 : c_stride, dtype)) return DIPACO_ECUDA;
     p.chunk = p.c_bf16 ? CHUNK_BF16 : CHUNK_F32;
     const bool chunked = !p.c_bf16 || p.steps > p.chunk;
     if (const int rc = chunked ? launch_pairs<true>(a_map, b_map, c_map, p, plan.pairs, stream)

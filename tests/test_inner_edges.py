@@ -215,3 +215,26 @@ def test_a_packed_matrix_can_be_copied(rows, cols):
         assert other.shape == (rows, cols) and torch.equal(inner.unpack(other, F32), want)
         assert rows * cols == 0 or other.struct.codes not in (p.struct.codes, shared.struct.codes)
     assert not bool(inner.unpack(shared, F32).any())
+
+
+# ------------------------------------------------------------------ products into a part of a buffer
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(1, 27, 30), (1, 1, 5), (8, 3, 100), (8, 25, 2318), (60, 41, 64), (30, 1001, 870), (300, 300, 300),
+                                   (257, 333, 129), (2000, 1795, 900), (4100, 1021, 260), (1000, 510, 9000)])
+def test_product_writes_nothing_beside_its_result(m, n, k, dtype):
+    """Rows on 16-byte boundaries that end inside 16 bytes, with another's data behind them."""
+    a, b = inner.pack(torch.randn(k, m, device=DEV)), inner.pack(torch.randn(n, k, device=DEV))
+    want = inner.packed_matmul(a, b, True, True, dtype)
+    for stride in {-(-n // 8) * 8, -(-n // 8) * 8 + 8, n}:
+        for start in (0, 8):
+            buffer = torch.full((start + (m - 1) * stride + n + 40,), 3.0, dtype=dtype, device=DEV)
+            view = buffer.as_strided((m, n), (stride, 1), start)
+            for accumulate in (False, True):
+                view.fill_(0.0 if accumulate else 7.0)
+                inner.packed_matmul(a, b, True, True, out=view, accumulate=accumulate)
+                assert torch.equal(view, want)
+                view.fill_(3.0)
+                assert bool((buffer == 3.0).all()), (stride, start, accumulate)
