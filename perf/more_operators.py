@@ -45,40 +45,40 @@ MOST_GRADIENTS = 144_000_000
 def listed():
     return [
         # one token goes through the widening layer of a block when a path answers: latency of one call
-        {"name": "linear, one token", "op": "linear", "form": "pack", "m": 1, "n": 3584, "k": 896,
+        {"name": "linear: one token", "op": "linear", "form": "pack", "m": 1, "n": 3584, "k": 896,
          "activation": "gelu", "bias": "bf16", "keep": False},
         # the widening layer of a training step, 32 sequences of 1024 tokens: operand and checkpoint
-        {"name": "linear, widening", "op": "linear", "form": "pack", "m": 32768, "n": 3584, "k": 896,
+        {"name": "linear: widening", "op": "linear", "form": "pack", "m": 32768, "n": 3584, "k": 896,
          "activation": "gelu", "bias": "bf16", "keep": True},
         # the narrowing layer of the wide model, added to the residual stream
-        {"name": "linear, narrowing", "op": "linear", "form": "dense", "m": 16384, "n": 2048, "k": 8192,
+        {"name": "linear: narrowing", "op": "linear", "form": "dense", "m": 16384, "n": 2048, "k": 8192,
          "activation": None, "bias": "bf16", "residual": True, "out": "bf16"},
         # the backward pass through the narrowing layer and the activation before it
-        {"name": "linear, activation gradient", "op": "linear", "form": "back", "m": 32768, "n": 3584, "k": 896,
+        {"name": "linear: activation gradient", "op": "linear", "form": "back", "m": 32768, "n": 3584, "k": 896,
          "activation": "gelu", "bias": "f32"},
         # a ragged batch through a layer of odd widths, in 32 bits
-        {"name": "linear, odd sizes", "op": "linear", "form": "dense", "m": 4999, "n": 1001, "k": 2047,
+        {"name": "linear: odd sizes", "op": "linear", "form": "dense", "m": 4999, "n": 1001, "k": 2047,
          "activation": "silu", "bias": "f32", "residual": True, "out": "f32"},
         # one token between two blocks when a path answers
-        {"name": "norms, one token", "op": "norms", "rows": 1, "cols": 896, "pad": 0, "dtype": "bf16",
+        {"name": "norms: one token", "op": "norms", "rows": 1, "cols": 896, "pad": 0, "dtype": "bf16",
          "params": "bf16", "gate": "cols", "packed": False},
         # between two blocks of the wide model, 16 sequences of 1024 tokens, kept in bf16
-        {"name": "norms, wide model", "op": "norms", "rows": 16384, "cols": 2048, "pad": 0, "dtype": "bf16",
+        {"name": "norms: wide model", "op": "norms", "rows": 16384, "cols": 2048, "pad": 0, "dtype": "bf16",
          "params": "bf16", "gate": "cols", "packed": False},
         # between two blocks of a training step that keeps 8-bit checkpoints
-        {"name": "norms, 8-bit checkpoints", "op": "norms", "rows": 32768, "cols": 896, "pad": 0, "dtype": "bf16",
+        {"name": "norms: 8-bit checkpoints", "op": "norms", "rows": 32768, "cols": 896, "pad": 0, "dtype": "bf16",
          "params": "bf16", "gate": "cols", "packed": True},
         # their gradient in the wide model
-        {"name": "norms back, wide model", "op": "norms back", "rows": 16384, "cols": 2048, "pad": 0,
+        {"name": "norms back: wide model", "op": "norms back", "rows": 16384, "cols": 2048, "pad": 0,
          "dtype": "bf16", "params": "bf16", "gate": "cols", "packed": False},
         # a ragged batch of an odd width, gated token by token, in 32 bits
-        {"name": "norms back, odd sizes", "op": "norms back", "rows": 4999, "cols": 2047, "pad": 0, "dtype": "f32",
+        {"name": "norms back: odd sizes", "op": "norms back", "rows": 4999, "cols": 2047, "pad": 0, "dtype": "f32",
          "params": "f32", "gate": "rows", "packed": False},
         # the six gradients of one feed-forward block of a small mixture
-        {"name": "clip, one block", "op": "clip", "width": 256, "blocks": 1, "vocabulary": 0, "odd": 0,
+        {"name": "clip: one block", "op": "clip", "width": 256, "blocks": 1, "vocabulary": 0, "odd": 0,
          "dtype": "f32", "share": 0.5},
         # all gradients of a path: 12 blocks and the embedding
-        {"name": "clip, a path", "op": "clip", "width": 896, "blocks": 12, "vocabulary": 32000, "odd": 0,
+        {"name": "clip: a path", "op": "clip", "width": 896, "blocks": 12, "vocabulary": 32000, "odd": 0,
          "dtype": "f32", "share": 0.1},
     ]
 
@@ -262,7 +262,7 @@ def prepare(case, seed):
     if case["gate"] == "cols":
         state["gate"] = _vector(gen, c, params, 0.3, 0.1)
     elif case["gate"] == "rows":
-        state["gate"] = torch.sigmoid(_vector(gen, r, "f32", 0.0, 1.0))
+        state["gate"] = torch.sigmoid(_vector(gen, r, "f32", 0.0, 1.0)).view(r, 1)
     else:
         state["gate"] = torch.sigmoid(_rows(gen, case, 1.0).float()).to(DTYPES[case["dtype"]])
     state["f"] = _rows(gen, case, 0.5, outliers=True)
@@ -319,16 +319,11 @@ def _normal_back(dy, hat, rstd):
     return (dy - dy.mean(1, keepdim=True) - hat * (dy * hat).mean(1, keepdim=True)) * rstd[:, None]
 
 
-def _wide_gate(gate, kind):
-    gate = gate.float()
-    return gate[:, None] if kind == "rows" else gate
-
-
 def _plain_norms(s, case):
     x, f = s["x"].float(), s["f"].float()
     hat, mean_f, rstd_f = _normal(f)
     p = hat * s["post_gamma"].float() + s["post_beta"].float()
-    z = (s["scale"] * x + _wide_gate(s["gate"], case["gate"]) * p).to(s["x"].dtype)
+    z = (s["scale"] * x + s["gate"].float() * p).to(s["x"].dtype)
     hat, mean_z, rstd_z = _normal(z.float())
     n = hat * s["gamma"].float() + s["beta"].float()
     stats = torch.stack((mean_f, rstd_f, mean_z, rstd_z))
@@ -341,7 +336,7 @@ def _plain_norms_back(s, case):
     f = _values(s["f"]) if case["packed"] else s["f"].float()
     z = _values(s["z"]) if case["packed"] else s["z"].float()
     mean_f, rstd_f, mean_z, rstd_z = s["stats"]
-    dn, gate, gamma, post = s["dn"].float(), _wide_gate(s["gate"], case["gate"]), s["gamma"].float(), s["post_gamma"].float()
+    dn, gate, gamma, post = (s[t].float() for t in ("dn", "gate", "gamma", "post_gamma"))
     hat_f, hat_z = (f - mean_f[:, None]) * rstd_f[:, None], (z - mean_z[:, None]) * rstd_z[:, None]
     dz = s["dz"].float() + _normal_back(dn * gamma, hat_z, rstd_z)
     dp = dz * gate
@@ -349,7 +344,7 @@ def _plain_norms_back(s, case):
     if case["gate"] == "full":
         dgate = dgate.to(s["dn"].dtype)
     else:
-        dgate = dgate.sum(0 if case["gate"] == "cols" else 1)
+        dgate = dgate.sum(0) if case["gate"] == "cols" else dgate.sum(1, keepdim=True)
     df = _normal_back(dp * post, hat_f, rstd_f)
     return ((s["scale"] * dz).to(s["dn"].dtype), df.to(s["dn"].dtype), dgate, (dn * hat_z).sum(0), dn.sum(0),
             (dp * hat_f).sum(0), dp.sum(0))
@@ -483,7 +478,6 @@ def exact(case, seed):
         norm = torch.linalg.vector_norm(flat)
         return flat * min(1.0, s["most"] / float(norm)), norm
     gate, scale = s["gate"].double(), s["scale"]
-    gate = gate.unsqueeze(1) if case["gate"] == "rows" else gate
     gamma, beta, post, shift = (s[name].double() for name in ("gamma", "beta", "post_gamma", "post_beta"))
     if op == "norms":
         hat, mean_f, rstd_f = _standardised(s["f"].double())
@@ -498,7 +492,7 @@ def exact(case, seed):
     dn = s["dn"].double()
     dz = s["dz"].double() + _through_norm(dn * gamma, z, rstd_z)
     sums = {"cols": "rc,rc->c", "rows": "rc,rc->r", "full": "rc,rc->rc"}[case["gate"]]
-    dgate = torch.einsum(sums, dz, torch.addcmul(shift, f, post))
+    dgate = torch.einsum(sums, dz, torch.addcmul(shift, f, post)).reshape(gate.shape)
     dp = dz * gate
     return (scale * dz, _through_norm(dp * post, f, rstd_f), dgate, torch.einsum("rc,rc->c", dn, z), dn.sum(0),
             torch.einsum("rc,rc->c", dp, f), dp.sum(0))
