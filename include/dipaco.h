@@ -507,6 +507,57 @@ int dipaco_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
                                int64_t workspace_bytes, int32_t device, void *cuda_stream);
 
 /*
+ * The norms after and before a block with its gate and its scaled residual, for a block's result f and the
+ * residual stream x, LN being the norm above without parameters:
+ *   p = LN(f) post_gamma + post_beta   (p = f without post_norm)
+ *   z = residual_scale x + gate p      (rounded to dtype: what the stream holds)
+ *   n = LN(z) gamma + beta             (of the z that the stream holds; not computed without norm)
+ *   gate           DIPACO_GATE_NONE (1), or one gate for a column ([cols]), a row ([rows]) or a value ([rows,
+ *                  cols] with row stride gate_stride, of dtype); [cols] and [rows] of gate_dtype
+ *   gamma, beta, post_gamma, post_beta   [cols] of param_dtype; NULL = ones, zeros; none without their norm
+ *   stats          [4][rows] fp32, kept for the backward pass: mean and rstd of f, mean and rstd of z; 0 and 1
+ *                  for a norm that is left out, NaN for rows of no values
+ */
+enum { DIPACO_GATE_NONE = 0, DIPACO_GATE_COLS = 1, DIPACO_GATE_ROWS = 2, DIPACO_GATE_FULL = 3 };
+typedef struct dipaco_residual_norm_args {
+    int64_t rows, cols;
+    const void *gamma, *beta, *post_gamma, *post_beta, *gate;
+    int64_t gate_stride;
+    int32_t gate_kind, gate_dtype, dtype, param_dtype;
+    int32_t post_norm, norm;  /* nonzero: with that norm */
+    float residual_scale, eps;
+} dipaco_residual_norm_args;
+
+/* n is dense (n; NULL = statistics only) or packed (n_packed), with z packed as a checkpoint beside it unless z_packed is
+ * NULL; z itself is always written. */
+int dipaco_residual_norm(const dipaco_residual_norm_args *args, const void *x, int64_t x_stride, const void *f,
+                         int64_t f_stride, void *z, int64_t z_stride, void *n, int64_t n_stride,
+                         const dipaco_packed *n_packed, const dipaco_packed *z_packed, float *stats, int32_t device,
+                         void *cuda_stream);
+
+/*
+ * Gradients from those of n (dn; with norm only) and z (dz; NULL = none).  With h = (v - mean) rstd of z or f:
+ *   d = dz + rstd_z (u - mean(u) - h_z mean(u h_z)),  u = dn gamma;   dx = residual_scale d
+ *   df = rstd_f (q - mean(q) - h_f mean(q h_f)),  q = d gate post_gamma   (q itself without post_norm)
+ *   dgate = d p, summed over what shares a gate;  dpost_gamma = sum d gate h_f,  dpost_beta = sum d gate,
+ *   dgamma = sum dn h_z,  dbeta = sum dn, over rows
+ *   f or f_packed, z or z_packed   exactly one of each: the forward call's, or 8-bit checkpoints of them (z with norm
+ *                  only)
+ *   dx, df         of dtype; NULL where not wanted, as the following
+ *   dgate          [cols] or [rows] fp32, or [rows, cols] of dtype with row stride dgate_stride
+ *   dgamma ...     [cols] fp32; overwritten, zero for no rows
+ *   workspace      16-byte aligned, at least the bytes that dipaco_residual_norm_workspace reports (host only)
+ */
+int dipaco_residual_norm_workspace(int64_t rows, int64_t cols, int64_t *bytes);
+int dipaco_residual_norm_backward(const dipaco_residual_norm_args *args, const void *dn, int64_t dn_stride, const void *dz,
+                                  int64_t dz_stride, const void *f, int64_t f_stride, const dipaco_packed *f_packed,
+                                  const void *z, int64_t z_stride, const dipaco_packed *z_packed, const float *stats,
+                                  void *dx, int64_t dx_stride, void *df, int64_t df_stride, void *dgate,
+                                  int64_t dgate_stride, float *dgamma, float *dbeta, float *dpost_gamma,
+                                  float *dpost_beta, void *workspace, int64_t workspace_bytes, int32_t device,
+                                  void *cuda_stream);
+
+/*
  * GELU in its tanh form, gelu(x) = x * s with s = 1 / (1 + exp(-2u)), u = sqrt(2/pi) (x + 0.044715 x^3),
  * packed from its fp32 value, and, unless x_packed is NULL, its input packed as a checkpoint.
  * The backward call reads that checkpoint and packs dy * gelu'(x) for the two products that follow,
@@ -535,6 +586,24 @@ int dipaco_packed_matmul_workspace(int64_t m, int64_t n, int64_t k, int64_t *byt
 int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t transpose_a, int32_t transpose_b,
                          void *c, int64_t c_stride, int32_t dtype, int32_t accumulate, void *workspace,
                          int64_t workspace_bytes, int32_t device, void *cuda_stream);
+
+/*
+ * The norm of several gradients together, sqrt of the sum of all their squares, and the gradients times
+ * min(1, max_norm / norm).  Squares are added in fp32 for at most 40 values and in fp64 beyond, or in fp64 where
+ * fp32 would overflow or lose them.  A norm that is not finite shows: with a NaN all results are NaN, with an infinity
+ * they are zero, or NaN where the gradient is infinite.
+ *   grads        HOST array [count] of device pointers, gradient i being numel[i] contiguous values of dtypes[i]
+ *   out          HOST array of device pointers to as many values of out_dtypes[i]; a result is its own gradient's
+ *                tensor (in place, of the same type) or overlaps nothing else; NULL = the norm alone
+ *   max_norm     >= 0; infinity = no clipping (results are copies)
+ *   norm         fp32, before clipping; may be NULL
+ *   workspace    16-byte aligned, at least the bytes that dipaco_clip_gradients_workspace reports (host only)
+ * The arrays are read before the call returns.
+ */
+int dipaco_clip_gradients_workspace(const int64_t *numel, int32_t count, int64_t *bytes);
+int dipaco_clip_gradients(const void *const *grads, void *const *out, const int64_t *numel, const int32_t *dtypes,
+                          const int32_t *out_dtypes, int32_t count, double max_norm, float *norm, void *workspace,
+                          int64_t workspace_bytes, int32_t device, void *cuda_stream);
 
 /*
  * Every wait inside the kernels of this section is bounded (4 s).  A wait that runs out ends its kernel in

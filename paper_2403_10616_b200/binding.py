@@ -37,6 +37,11 @@ DIPACO_OPT_ADAM = 3
 DIPACO_INPUT_COPIES = 0
 DIPACO_INPUT_GRADIENTS = 1
 
+DIPACO_GATE_NONE = 0
+DIPACO_GATE_COLS = 1
+DIPACO_GATE_ROWS = 2
+DIPACO_GATE_FULL = 3
+
 DIPACO_KERNEL_AUTO = 0
 DIPACO_KERNEL_VECTOR = 1
 DIPACO_KERNEL_SCALAR = 2
@@ -55,6 +60,8 @@ EXPORTS = [
     "dipaco_layer_norm_workspace", "dipaco_layer_norm_backward", "dipaco_gelu_pack",
     "dipaco_gelu_pack_backward", "dipaco_packed_matmul_workspace", "dipaco_packed_matmul",
     "dipaco_inner_status", "dipaco_selftest_inner_wait_expiry",
+    "dipaco_residual_norm", "dipaco_residual_norm_workspace", "dipaco_residual_norm_backward",
+    "dipaco_clip_gradients_workspace", "dipaco_clip_gradients",
 ]
 
 _lib = None
@@ -64,6 +71,16 @@ class PackedStruct(ctypes.Structure):
     """``dipaco_packed``: 8-bit codes with one scale per block of 128 x 128 (device pointers)."""
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
                 ("cols", ctypes.c_int64), ("stride", ctypes.c_int64)]
+
+
+class ResidualNormStruct(ctypes.Structure):
+    """``dipaco_residual_norm_args``."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("gamma", ctypes.c_void_p),
+                ("beta", ctypes.c_void_p), ("post_gamma", ctypes.c_void_p), ("post_beta", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("gate_kind", ctypes.c_int32),
+                ("gate_dtype", ctypes.c_int32), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("post_norm", ctypes.c_int32), ("norm", ctypes.c_int32), ("residual_scale", ctypes.c_float),
+                ("eps", ctypes.c_float)]
 
 
 class DipacoError(RuntimeError):
@@ -129,6 +146,13 @@ def load() -> ctypes.CDLL:
     lib.dipaco_gelu_pack_backward.argtypes = [vp, i64, i32, pk, pk, i32, vp]
     lib.dipaco_packed_matmul_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
     lib.dipaco_packed_matmul.argtypes = [pk, pk, i32, i32, vp, i64, i32, i32, vp, i64, i32, vp]
+    rn = ctypes.POINTER(ResidualNormStruct)
+    lib.dipaco_residual_norm.argtypes = [rn, vp, i64, vp, i64, vp, i64, vp, i64, pk, pk, vp, i32, vp]
+    lib.dipaco_residual_norm_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    lib.dipaco_residual_norm_backward.argtypes = [rn, vp, i64, vp, i64, vp, i64, pk, vp, i64, pk, vp, vp, i64, vp, i64,
+                                                  vp, i64, vp, vp, vp, vp, vp, i64, i32, vp]
+    lib.dipaco_clip_gradients_workspace.argtypes = [vp, i32, ctypes.POINTER(i64)]
+    lib.dipaco_clip_gradients.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.c_double, vp, vp, i64, i32, vp]
     lib.dipaco_inner_status.argtypes = [i32, vp]
     lib.dipaco_selftest_inner_wait_expiry.argtypes = [i32, i64, i32, vp]
     for name in EXPORTS:
@@ -448,6 +472,41 @@ def dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype,
                          workspace_bytes, device, stream) -> None:
     _check(load().dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype, accumulate,
                                        workspace_ptr, workspace_bytes, device, stream), "dipaco_packed_matmul")
+
+
+def dipaco_residual_norm(args, x_ptr, x_stride, f_ptr, f_stride, z_ptr, z_stride, n_ptr, n_stride, n_packed, z_packed,
+                         stats_ptr, device, stream) -> None:
+    _check(load().dipaco_residual_norm(args, x_ptr, x_stride, f_ptr, f_stride, z_ptr, z_stride, n_ptr, n_stride,
+                                       n_packed, z_packed, stats_ptr, device, stream), "dipaco_residual_norm")
+
+
+def dipaco_residual_norm_workspace(rows, cols) -> int:
+    size = ctypes.c_int64()
+    _check(load().dipaco_residual_norm_workspace(rows, cols, size), "dipaco_residual_norm_workspace")
+    return size.value
+
+
+def dipaco_residual_norm_backward(args, dn_ptr, dn_stride, dz_ptr, dz_stride, f_ptr, f_stride, f_packed, z_ptr, z_stride,
+                                  z_packed, stats_ptr, dx_ptr, dx_stride, df_ptr, df_stride, dgate_ptr, dgate_stride,
+                                  dgamma_ptr, dbeta_ptr, dpost_gamma_ptr, dpost_beta_ptr, workspace_ptr,
+                                  workspace_bytes, device, stream) -> None:
+    _check(load().dipaco_residual_norm_backward(args, dn_ptr, dn_stride, dz_ptr, dz_stride, f_ptr, f_stride, f_packed,
+                                                z_ptr, z_stride, z_packed, stats_ptr, dx_ptr, dx_stride, df_ptr,
+                                                df_stride, dgate_ptr, dgate_stride, dgamma_ptr, dbeta_ptr,
+                                                dpost_gamma_ptr, dpost_beta_ptr, workspace_ptr, workspace_bytes,
+                                                device, stream), "dipaco_residual_norm_backward")
+
+
+def dipaco_clip_gradients_workspace(numel, count) -> int:
+    size = ctypes.c_int64()
+    _check(load().dipaco_clip_gradients_workspace(numel, count, size), "dipaco_clip_gradients_workspace")
+    return size.value
+
+
+def dipaco_clip_gradients(grad_ptrs, out_ptrs, numel, dtypes, out_dtypes, count, max_norm, norm_ptr, workspace_ptr,
+                          workspace_bytes, device, stream) -> None:
+    _check(load().dipaco_clip_gradients(grad_ptrs, out_ptrs, numel, dtypes, out_dtypes, count, max_norm, norm_ptr,
+                                        workspace_ptr, workspace_bytes, device, stream), "dipaco_clip_gradients")
 
 
 def dipaco_inner_status(device, stream) -> int:

@@ -651,6 +651,25 @@ int dipaco::expire_packing_wait(unsigned long long limit_ns, cudaStream_t stream
     return launch_status();
 }
 
+int dipaco::pack_normalised(const void *x, int64_t x_stride, int dtype, const float *mean, const float *rstd,
+                            const void *gamma, const void *beta, int param_dtype, const dipaco_packed *y,
+                            const dipaco_packed *x_packed, cudaStream_t stream)
+{
+    BlockArgs a = {};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.first = packed_out(y);
+    a.second = packed_out(x_packed);
+    a.mean = mean;
+    a.rstd = rstd;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.params_bf16 = param_dtype == DIPACO_BF16;
+    a.gamma_aligned = (uintptr_t)gamma % 16 == 0;
+    a.beta_aligned = (uintptr_t)beta % 16 == 0;
+    return launch_blocks<OP_NORM>(a, dtype, y->rows, y->cols, stream);
+}
+
 extern "C" {
 
 int dipaco_pack(const void *x, int64_t x_stride, int32_t dtype, const dipaco_packed *out, int32_t device,
@@ -714,19 +733,8 @@ int dipaco_layer_norm_pack(const void *x, int64_t x_stride, const void *gamma, c
     if (cols == 0) return DIPACO_OK;
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
-    BlockArgs a = {};
-    a.x = x;
-    a.x_stride = x_stride;
-    a.first = packed_out(y);
-    a.second = packed_out(x_packed);
-    a.mean = mean;
-    a.rstd = rstd;
-    a.gamma = gamma;
-    a.beta = beta;
-    a.params_bf16 = param_dtype == DIPACO_BF16;
-    a.gamma_aligned = (uintptr_t)gamma % 16 == 0;
-    a.beta_aligned = (uintptr_t)beta % 16 == 0;
-    return launch_blocks<OP_NORM>(a, dtype, rows, cols, static_cast<cudaStream_t>(cuda_stream));
+    return pack_normalised(x, x_stride, dtype, mean, rstd, gamma, beta, param_dtype, y, x_packed,
+                           static_cast<cudaStream_t>(cuda_stream));
 }
 
 int dipaco_gelu_pack(const void *x, int64_t x_stride, int32_t dtype, const dipaco_packed *y,

@@ -1,8 +1,8 @@
 """Operators of a path's inner phase on torch CUDA tensors (declared in ``include/dipaco.h``).
 
 Layer norm with its gradient, matrices packed in 8 bits (activation checkpoints and the operands of
-the products), the GELU that writes and reads such checkpoints, and the product of packed matrices
-on the tensor cores.  Each function allocates its results (and workspace) with torch, launches on the
+the products), the GELU that writes and reads such checkpoints, the product of packed matrices on the
+tensor cores, the norms around a block with its gate and residual, and the clipping of gradients.  Each function allocates its results (and workspace) with torch, launches on the
 current stream of the tensors' device, and raises ``ValueError`` for shapes and dtypes that do not
 fit together or ``binding.DipacoError`` with the library's status.  There is no CPU path.
 
@@ -12,7 +12,9 @@ gradient is refused while gradients are being recorded; inside ``torch.no_grad()
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple, Union
+import ctypes
+import math
+from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -269,6 +271,241 @@ def packed_matmul(a: Packed, b: Packed, transpose_a: bool = False, transpose_b: 
     B.dipaco_packed_matmul(a.struct, b.struct, transpose_a, transpose_b, out.data_ptr(), stride, code, accumulate,
                            work.data_ptr() if need else None, need, dev, _stream(dev))
     return out
+
+
+class ResidualNormGradients(NamedTuple):
+    """Gradients of ``residual_norm``; None for what the call does not have."""
+    x: torch.Tensor
+    f: torch.Tensor
+    gate: Optional[torch.Tensor]        # of the gate's shape: fp32, or in dn's dtype for a gate of every value
+    gamma: Optional[torch.Tensor]       # fp32, as the following
+    beta: Optional[torch.Tensor]
+    post_gamma: Optional[torch.Tensor]
+    post_beta: Optional[torch.Tensor]
+
+
+def _gate(gate: Optional[torch.Tensor], rows: int, cols: int, dev: int, code: int) -> Tuple[int, Optional[int], int, int]:
+    """(kind, pointer, row stride, dtype code) of a gate [cols], [rows, 1] or [rows, cols]."""
+    if gate is None:
+        return B.DIPACO_GATE_NONE, None, 0, B.DIPACO_F32
+    if gate.requires_grad:
+        _refuse_gradient("gate")
+    own = _CODES.get(gate.dtype)
+    if own is None or gate.get_device() != dev:
+        raise ValueError("gate must be float32 or bfloat16, on the rows' device")
+    if gate.shape == (cols,):
+        if cols > 1 and gate.stride(0) != 1:
+            raise ValueError("a gate of columns must be contiguous")
+        return B.DIPACO_GATE_COLS, gate.data_ptr(), 0, own
+    if gate.shape == (rows, 1):
+        if rows > 1 and gate.stride(0) != 1:
+            raise ValueError("a gate of rows must be contiguous")
+        return B.DIPACO_GATE_ROWS, gate.data_ptr(), 0, own
+    if gate.shape == (rows, cols):
+        if own != code or (cols > 1 and gate.stride(1) != 1):
+            raise ValueError("a gate of all values must be row-major and have the rows' dtype")
+        return B.DIPACO_GATE_FULL, gate.data_ptr(), gate.stride(0), own
+    raise ValueError("gate must be [cols], [rows, 1] or [rows, cols]")
+
+
+def _residual_norm_args(rows, cols, dev, code, gamma, beta, post_gamma, post_beta, gate, residual_scale, post_norm, norm,
+                        eps) -> B.ResidualNormStruct:
+    if not norm and (gamma is not None or beta is not None):
+        raise ValueError("gamma and beta belong to the norm that is left out")
+    if not post_norm and (post_gamma is not None or post_beta is not None):
+        raise ValueError("post_gamma and post_beta belong to the norm that is left out")
+    given, pcode = [], None
+    for p in (gamma, beta, post_gamma, post_beta):
+        if p is None:
+            given.append(None)
+            continue
+        ptr, p_code = _param(cols, dev, p)
+        if pcode is not None and p_code != pcode:
+            raise ValueError("the norms' parameters must have one dtype")
+        given.append(ptr)
+        pcode = p_code
+    kind, gate_ptr, gate_stride, gate_code = _gate(gate, rows, cols, dev, code)
+    return B.ResidualNormStruct(rows, cols, *given, gate_ptr, gate_stride, kind, gate_code, code,
+                                B.DIPACO_F32 if pcode is None else pcode, post_norm, norm, residual_scale, eps)
+
+
+def _like(name: str, x: torch.Tensor, shape: Tuple[int, int], dev: int, code: int) -> Tuple[int, int]:
+    """(pointer, row stride) of a dense matrix that has to go with others."""
+    rows, cols, stride, own = _dense(name, x)
+    if (rows, cols) != shape or own != code or x.get_device() != dev:
+        raise ValueError("%s must have the other matrices' shape, dtype and device" % name)
+    return x.data_ptr(), stride
+
+
+def residual_norm(x: torch.Tensor, f: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                  beta: Optional[torch.Tensor] = None, post_gamma: Optional[torch.Tensor] = None,
+                  post_beta: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                  residual_scale: float = 1.0, post_norm: bool = True, norm: bool = True, eps: float = 1e-5):
+    """(z, n, stats) of a residual stream x and a block's result f:
+
+        z = residual_scale * x + gate * (LN(f) * post_gamma + post_beta),   n = LN(z) * gamma + beta,
+
+    the norm after the block, its gate and residual, and the norm before the next one, of z as it is held in x's
+    dtype.  ``gate`` is [cols], [rows, 1] or [rows, cols].  Without ``post_norm`` f goes in as it is; without ``norm``
+    n is None.  stats [4, rows] is for ``residual_norm_backward``."""
+    rows, cols, x_stride, code = _dense("x", x)
+    dev = x.get_device()
+    f_ptr, f_stride = _like("f", f, (rows, cols), dev, code)
+    args = _residual_norm_args(rows, cols, dev, code, gamma, beta, post_gamma, post_beta, gate, residual_scale,
+                               post_norm, norm, eps)
+    z = x.new_empty((rows, cols))
+    n = x.new_empty((rows, cols)) if norm else None
+    stats = x.new_empty((4, rows), dtype=_F32)
+    B.dipaco_residual_norm(args, x.data_ptr(), x_stride, f_ptr, f_stride, z.data_ptr(), cols,
+                           n.data_ptr() if norm else None, cols, None, None, stats.data_ptr(), dev, _stream(dev))
+    return z, n, stats
+
+
+def residual_norm_pack(x: torch.Tensor, f: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                       beta: Optional[torch.Tensor] = None, post_gamma: Optional[torch.Tensor] = None,
+                       post_beta: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                       residual_scale: float = 1.0, post_norm: bool = True, eps: float = 1e-5, keep: bool = True):
+    """(z, n, kept, stats): ``residual_norm`` with n packed, and z packed too as the checkpoint that
+    ``residual_norm_backward`` reads (None without ``keep``)."""
+    rows, cols, x_stride, code = _dense("x", x)
+    dev = x.get_device()
+    f_ptr, f_stride = _like("f", f, (rows, cols), dev, code)
+    args = _residual_norm_args(rows, cols, dev, code, gamma, beta, post_gamma, post_beta, gate, residual_scale,
+                               post_norm, True, eps)
+    z = x.new_empty((rows, cols))
+    n = _packed_beside(x, rows, cols)
+    kept = _packed_beside(x, rows, cols) if keep else None
+    stats = x.new_empty((4, rows), dtype=_F32)
+    B.dipaco_residual_norm(args, x.data_ptr(), x_stride, f_ptr, f_stride, z.data_ptr(), cols, None, 0, n.struct,
+                           kept.struct if keep else None, stats.data_ptr(), dev, _stream(dev))
+    return z, n, kept, stats
+
+
+def residual_norm_backward(dn: Optional[torch.Tensor], dz: Optional[torch.Tensor], f: Union[torch.Tensor, Packed],
+                           z: Union[torch.Tensor, Packed, None], stats: torch.Tensor,
+                           gamma: Optional[torch.Tensor] = None, post_gamma: Optional[torch.Tensor] = None,
+                           post_beta: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                           residual_scale: float = 1.0, post_norm: bool = True) -> ResidualNormGradients:
+    """Gradients of ``residual_norm`` from those of n (dn; None without ``norm``, and then z may be None) and of z
+    (dz; None where z goes nowhere else).  f and z are the forward pass's, or packed checkpoints of them."""
+    like = dn if dn is not None else dz
+    if like is None:
+        raise ValueError("dn or dz must be given")
+    rows, cols, stride, code = _dense("dn" if dn is not None else "dz", like)
+    dev = like.get_device()
+    norm = dn is not None
+    dz_ptr, dz_stride = (None, 0) if dz is None else _like("dz", dz, (rows, cols), dev, code)
+    if stats.shape != (4, rows) or stats.dtype != _F32 or stats.get_device() != dev or not stats.is_contiguous():
+        raise ValueError("stats must be the contiguous float32 [4, rows] of the forward call")
+    if stats.requires_grad:
+        _refuse_gradient("stats")
+    read = []
+    for name, t in (("f", f), ("z", z if norm else None)):
+        if isinstance(t, Packed):
+            if t.shape != (rows, cols) or t.codes.get_device() != dev:
+                raise ValueError("%s must have the other matrices' shape and device" % name)
+            read += [None, 0, t.struct]
+        elif t is not None:
+            read += [*_like(name, t, (rows, cols), dev, code), None]
+        elif name == "z" and not norm:
+            read += [None, 0, None]
+        else:
+            raise ValueError("%s must be given" % name)
+    args = _residual_norm_args(rows, cols, dev, code, gamma, None, post_gamma, post_beta, gate, residual_scale,
+                               post_norm, norm, 0.0)
+    dx, df = like.new_empty((rows, cols)), like.new_empty((rows, cols))
+    dgate = None if gate is None else gate.new_empty(
+        gate.shape, dtype=gate.dtype if args.gate_kind == B.DIPACO_GATE_FULL else _F32)
+    sums = like.new_empty((4, cols), dtype=_F32).unbind(0)
+    dgamma, dbeta = sums[:2] if norm else (None, None)
+    dpost_gamma, dpost_beta = sums[2:] if post_norm else (None, None)
+    need = B.dipaco_residual_norm_workspace(rows, cols)
+    work = like.new_empty(need, dtype=torch.uint8) if need else None
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    B.dipaco_residual_norm_backward(args, ptr(dn), stride, dz_ptr, dz_stride, *read, stats.data_ptr(), dx.data_ptr(), cols,
+                                    df.data_ptr(), cols, ptr(dgate), cols, ptr(dgamma), ptr(dbeta), ptr(dpost_gamma),
+                                    ptr(dpost_beta), ptr(work), need, dev, _stream(dev))
+    return ResidualNormGradients(dx, df, dgate, dgamma, dbeta, dpost_gamma, dpost_beta)
+
+
+def _dense_in_some_order(t: torch.Tensor) -> bool:
+    """Whether t's values fill the memory from its first to its last without gaps."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size != 1:
+            if stride != step:
+                return False
+            step *= size
+    return True
+
+
+def _gradients(grads: Sequence[torch.Tensor], any_order: bool):
+    """(tensors, device, numels, pointers, dtype codes) of gradients that are taken as they lie in memory."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("there must be a gradient")
+    dev = grads[0].get_device()
+    codes = []
+    for t in grads:
+        code = _CODES.get(t.dtype)
+        if code is None or dev < 0 or t.get_device() != dev:
+            raise ValueError("gradients must be float32 or bfloat16 tensors on one CUDA device")
+        if not (t.is_contiguous() or (any_order and _dense_in_some_order(t))):
+            raise ValueError("gradients must be contiguous")
+        if t.requires_grad:
+            _refuse_gradient("a gradient")
+        codes.append(code)
+    return grads, dev, [t.numel() for t in grads], [t.data_ptr() for t in grads], codes
+
+
+def _clip(grads, dev, numels, ptrs, codes, out_ptrs, out_codes, max_norm: float) -> torch.Tensor:
+    count = len(grads)
+    numel, dtypes = (ctypes.c_int64 * count)(*numels), (ctypes.c_int32 * count)(*codes)
+    norm = grads[0].new_empty((), dtype=_F32)
+    need = B.dipaco_clip_gradients_workspace(numel, count)
+    work = norm.new_empty(need, dtype=torch.uint8) if need else None
+    out = None if out_ptrs is None else (ctypes.c_void_p * count)(*out_ptrs)
+    out_dtypes = None if out_ptrs is None else (ctypes.c_int32 * count)(*out_codes)
+    B.dipaco_clip_gradients((ctypes.c_void_p * count)(*ptrs), out, numel, dtypes, out_dtypes, count, max_norm,
+                            norm.data_ptr(), work.data_ptr() if need else None, need, dev, _stream(dev))
+    return norm
+
+
+def _most(max_norm: float) -> float:
+    max_norm = float(max_norm)
+    if not max_norm >= 0.0:
+        raise ValueError("max_norm must not be negative")
+    return max_norm
+
+
+def gradient_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
+    """The norm of all gradients together, a float32 scalar on their device."""
+    return _clip(*_gradients(grads, True), None, None, math.inf)
+
+
+def clip_gradients(grads: Sequence[torch.Tensor], max_norm: float) -> torch.Tensor:
+    """Multiplies the gradients by min(1, max_norm / norm) in place and returns their norm before that.  No two may
+    share memory."""
+    grads, dev, numels, ptrs, codes = _gradients(grads, True)
+    return _clip(grads, dev, numels, ptrs, codes, ptrs, codes, _most(max_norm))
+
+
+def gather_gradients(grads: Sequence[torch.Tensor], max_norm: Optional[float] = None,
+                     dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(flat, norm): the gradients one after another in a vector, as the modules lie in a path's copy, clipped to
+    ``max_norm`` unless it is None, and their norm before that."""
+    if dtype not in _CODES:
+        raise ValueError("dtype must be float32 or bfloat16")
+    most = math.inf if max_norm is None else _most(max_norm)
+    grads, dev, numels, ptrs, codes = _gradients(grads, False)
+    flat = grads[0].new_empty(sum(numels), dtype=dtype)
+    at, size, out = flat.data_ptr(), flat.element_size(), []
+    for n in numels:
+        out.append(at)
+        at += n * size
+    return flat, _clip(grads, dev, numels, ptrs, codes, out, [_CODES[dtype]] * len(grads), most)
 
 
 def inner_status(device=None) -> int:
