@@ -588,6 +588,40 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
                          int64_t workspace_bytes, int32_t device, void *cuda_stream);
 
 /*
+ * Linear layers on packed matrices: the products above with what surrounds them in a block done on their fp32
+ * sums.  x [tokens, in], w [out, in], bias [out] of bias_dtype or NULL.
+ *   linear                y = act(x w^T + bias) + residual, rounded once to dtype (that of a residual; NULL = none).
+ *                         The sums are those of dipaco_packed_matmul, and so is the workspace (of its query for m =
+ *                         tokens, n = out, k = in).
+ *   linear_pack           a = x w^T + bias and y = act(a), both packed from their fp32 values: y for the next
+ *                         layer, a as the checkpoint that the backward call reads (NULL = not wanted)
+ *   linear_pack_backward  da = (dy w) act'(a), packed, for dy [tokens, out] packed and a [tokens, in] as linear_pack
+ *                         left it for the layer before (not read without an activation), and dbias = sum of da
+ *                         over the tokens, of its fp32 values ([in] fp32, zero for no tokens; NULL = not wanted).
+ *                         workspace: of its query for m = tokens, n = in, k = out; only needed for dbias
+ * Activations: relu(a) = max(a, 0); silu(a) = a / (1 + exp(-a)); gelu as above.  An infinity of a is NaN once it is
+ * packed, and makes silu and gelu NaN or infinite; NaN stays NaN.  relu'(0) = 0.
+ * The packed forms take their sums in one go: contractions over 65536 are refused (DIPACO_ELIMIT).
+ */
+enum {
+    DIPACO_ACTIVATION_NONE = 0,
+    DIPACO_ACTIVATION_RELU = 1,
+    DIPACO_ACTIVATION_SILU = 2,
+    DIPACO_ACTIVATION_GELU = 3
+};
+int dipaco_packed_linear(const dipaco_packed *x, const dipaco_packed *w, const void *bias, int32_t bias_dtype,
+                         int32_t activation, const void *residual, int64_t residual_stride, void *y, int64_t y_stride,
+                         int32_t dtype, void *workspace, int64_t workspace_bytes, int32_t device, void *cuda_stream);
+int dipaco_packed_linear_pack_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+int dipaco_packed_linear_pack(const dipaco_packed *x, const dipaco_packed *w, const void *bias, int32_t bias_dtype,
+                              int32_t activation, const dipaco_packed *y, const dipaco_packed *a, void *workspace,
+                              int64_t workspace_bytes, int32_t device, void *cuda_stream);
+int dipaco_packed_linear_pack_backward_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_packed *w, const dipaco_packed *a,
+                                       int32_t activation, const dipaco_packed *da, float *dbias, void *workspace,
+                                       int64_t workspace_bytes, int32_t device, void *cuda_stream);
+
+/*
  * The norm of several gradients together, sqrt of the sum of all their squares, and the gradients times
  * min(1, max_norm / norm).  Squares are added in fp32 for at most 40 values and in fp64 beyond, or in fp64 where
  * fp32 would overflow or lose them.  A norm that is not finite shows: with a NaN all results are NaN, with an infinity
@@ -615,7 +649,7 @@ int dipaco_inner_status(int32_t device, void *cuda_stream);
 
 /*
  * Diagnostic: make a bounded wait of the norms (operators = 0), of the packing kernels (1) or of the
- * products (2) run out on purpose, harmlessly: one warp waits at most limit_ns (1 .. 1e9) on a barrier that
+ * products and linear layers (2, one after the other) run out on purpose, harmlessly: one warp waits at most limit_ns (1 .. 1e9) on a barrier that
  * nothing will complete; no copy is in flight and no buffer of the caller is involved.
  */
 int dipaco_selftest_inner_wait_expiry(int32_t operators, int64_t limit_ns, int32_t device, void *cuda_stream);

@@ -37,6 +37,11 @@ DIPACO_OPT_ADAM = 3
 DIPACO_INPUT_COPIES = 0
 DIPACO_INPUT_GRADIENTS = 1
 
+DIPACO_ACTIVATION_NONE = 0
+DIPACO_ACTIVATION_RELU = 1
+DIPACO_ACTIVATION_SILU = 2
+DIPACO_ACTIVATION_GELU = 3
+
 DIPACO_GATE_NONE = 0
 DIPACO_GATE_COLS = 1
 DIPACO_GATE_ROWS = 2
@@ -62,6 +67,8 @@ EXPORTS = [
     "dipaco_inner_status", "dipaco_selftest_inner_wait_expiry",
     "dipaco_residual_norm", "dipaco_residual_norm_workspace", "dipaco_residual_norm_backward",
     "dipaco_clip_gradients_workspace", "dipaco_clip_gradients",
+    "dipaco_packed_linear", "dipaco_packed_linear_pack_workspace", "dipaco_packed_linear_pack",
+    "dipaco_packed_linear_pack_backward_workspace", "dipaco_packed_linear_pack_backward",
 ]
 
 _lib = None
@@ -146,6 +153,11 @@ def load() -> ctypes.CDLL:
     lib.dipaco_gelu_pack_backward.argtypes = [vp, i64, i32, pk, pk, i32, vp]
     lib.dipaco_packed_matmul_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
     lib.dipaco_packed_matmul.argtypes = [pk, pk, i32, i32, vp, i64, i32, i32, vp, i64, i32, vp]
+    lib.dipaco_packed_linear.argtypes = [pk, pk, vp, i32, i32, vp, i64, vp, i64, i32, vp, i64, i32, vp]
+    lib.dipaco_packed_linear_pack_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
+    lib.dipaco_packed_linear_pack.argtypes = [pk, pk, vp, i32, i32, pk, pk, vp, i64, i32, vp]
+    lib.dipaco_packed_linear_pack_backward_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
+    lib.dipaco_packed_linear_pack_backward.argtypes = [pk, pk, pk, i32, pk, vp, vp, i64, i32, vp]
     rn = ctypes.POINTER(ResidualNormStruct)
     lib.dipaco_residual_norm.argtypes = [rn, vp, i64, vp, i64, vp, i64, vp, i64, pk, pk, vp, i32, vp]
     lib.dipaco_residual_norm_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
@@ -472,6 +484,39 @@ def dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype,
                          workspace_bytes, device, stream) -> None:
     _check(load().dipaco_packed_matmul(a, b, transpose_a, transpose_b, c_ptr, c_stride, dtype, accumulate,
                                        workspace_ptr, workspace_bytes, device, stream), "dipaco_packed_matmul")
+
+
+def dipaco_packed_linear(x, w, bias_ptr, bias_dtype, activation, residual_ptr, residual_stride, y_ptr, y_stride, dtype,
+                         workspace_ptr, workspace_bytes, device, stream) -> None:
+    _check(load().dipaco_packed_linear(x, w, bias_ptr, bias_dtype, activation, residual_ptr, residual_stride, y_ptr,
+                                       y_stride, dtype, workspace_ptr, workspace_bytes, device, stream),
+           "dipaco_packed_linear")
+
+
+def dipaco_packed_linear_pack_workspace(m, n, k) -> int:
+    size = ctypes.c_int64()
+    _check(load().dipaco_packed_linear_pack_workspace(m, n, k, size), "dipaco_packed_linear_pack_workspace")
+    return size.value
+
+
+def dipaco_packed_linear_pack(x, w, bias_ptr, bias_dtype, activation, y, a, workspace_ptr, workspace_bytes, device,
+                              stream) -> None:
+    _check(load().dipaco_packed_linear_pack(x, w, bias_ptr, bias_dtype, activation, y, a, workspace_ptr,
+                                            workspace_bytes, device, stream), "dipaco_packed_linear_pack")
+
+
+def dipaco_packed_linear_pack_backward_workspace(m, n, k) -> int:
+    size = ctypes.c_int64()
+    _check(load().dipaco_packed_linear_pack_backward_workspace(m, n, k, size),
+           "dipaco_packed_linear_pack_backward_workspace")
+    return size.value
+
+
+def dipaco_packed_linear_pack_backward(dy, w, a, activation, da, dbias_ptr, workspace_ptr, workspace_bytes, device,
+                                       stream) -> None:
+    _check(load().dipaco_packed_linear_pack_backward(dy, w, a, activation, da, dbias_ptr, workspace_ptr,
+                                                     workspace_bytes, device, stream),
+           "dipaco_packed_linear_pack_backward")
 
 
 def dipaco_residual_norm(args, x_ptr, x_stride, f_ptr, f_stride, z_ptr, z_stride, n_ptr, n_stride, n_packed, z_packed,

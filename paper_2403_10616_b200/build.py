@@ -9,8 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdipaco.so")
 SOURCES = ["dipaco.cu", "static_sync.cu", "layer_norm.cu", "packed.cu", "packed_matmul.cu",
-           "residual_norm.cu", "clip.cu"]
+           "packed_linear.cu", "residual_norm.cu", "clip.cu"]
 DEPENDS = SOURCES + ["kernels.cuh", "plan.hpp", "host_mode.inl", "inner_common.cuh",
+           "activations.cuh", "product_pairs.cuh",
            os.path.join("..", "..", "include", "dipaco.h")]
 
 

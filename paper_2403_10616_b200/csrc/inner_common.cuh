@@ -105,6 +105,7 @@ template <typename Symbol> bool take_error_word(const Symbol &symbol, bool &expi
 }
 bool take_packing_error(bool &expired);  // of packed.cu
 bool take_norm_error(bool &expired);     // of layer_norm.cu
+bool take_linear_error(bool &expired);   // of packed_linear.cu
 
 // The norm of rows whose statistics are known, and unless x_packed is NULL the rows themselves, packed (of packed.cu):
 // checked arguments, the device current, values to work on.
@@ -112,9 +113,14 @@ int pack_normalised(const void *x, int64_t x_stride, int dtype, const float *mea
                     const void *beta, int param_dtype, const dipaco_packed *y, const dipaco_packed *x_packed,
                     cudaStream_t stream);
 
+// The activation of dense fp32 rows, and unless x_packed is NULL the rows themselves, packed (of packed.cu): as above.
+int pack_activated(const float *x, int64_t x_stride, int activation, const dipaco_packed *y, const dipaco_packed *x_packed,
+                   cudaStream_t stream);
+
 // Launches of a warp whose wait runs out (dipaco_selftest_inner_wait_expiry).
 int expire_packing_wait(unsigned long long limit_ns, cudaStream_t stream);
 int expire_norm_wait(unsigned long long limit_ns, cudaStream_t stream);
+int expire_linear_wait(unsigned long long limit_ns, cudaStream_t stream);
 
 // ------------------------------------------------------------------------------------------ device
 

@@ -17,6 +17,7 @@
 // instructions 60 and memory 72: the three overlap in part.  The norm's two launches on 32768x896 take
 // 41 us, 13 of them for the statistics; its second reads x from L2.  From fp32 (block_kernel) the GELU and its
 // gradient take 182 and 214 us, and the norm of 32768x896 takes 85 us with its statistics: they spill registers.
+#include "activations.cuh"
 #include "inner_common.cuh"
 
 #include <cmath>
@@ -226,53 +227,7 @@ __device__ __forceinline__ void write_codes(const PackedOut &out, const Extent &
     }
 }
 
-// The approximations are good to two units in the last place.
-__device__ __forceinline__ float exp2_of(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ float reciprocal_of(float x)
-{
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-// d = exp(-2u) and s = 1 / (1 + d) of two values; -2u log2(e) = a (c1 + c3 a^2).
-__device__ __forceinline__ void gelu_share(f32x2 a, f32x2 square, f32x2 &d, f32x2 &s)
-{
-    constexpr float c1 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, c3 = c1 * 0.044715f;
-    const float2 e = values_of(mul2(a, fma2(square, pair_of(c3), pair_of(c1))));
-    d = pair_of(exp2_of(e.x), exp2_of(e.y));
-    const float2 t = values_of(add2(d, pair_of(1.0f)));
-    s = pair_of(reciprocal_of(t.x), reciprocal_of(t.y));
-}
-__device__ __forceinline__ f32x2 gelu(f32x2 a)
-{
-    f32x2 d, s;
-    gelu_share(a, mul2(a, a), d, s);
-    return mul2(a, s);
-}
-
-// s + a s (1 - s) 2u' = s (1 + a d s 2u') with d = exp(-2u): no cancellation where s is near 1.  a is held
-// within +-10.03, NaN kept: there the slope is 1, or 0 (d is still finite and s flushed to zero).
-__device__ __forceinline__ float held(float a)
-{
-    asm("min.NaN.f32 %0, %0, 0f41208000;\n\tmax.NaN.f32 %0, %0, 0fC1208000;" : "+f"(a));
-    return a;
-}
-__device__ __forceinline__ f32x2 gelu_slope(f32x2 value)
-{
-    constexpr float k1 = 2.0f * 0.7978845608028654f, k3 = 3.0f * 0.044715f * k1;
-    const float2 v = values_of(value);
-    const f32x2 a = pair_of(held(v.x), held(v.y)), square = mul2(a, a);
-    f32x2 d, s;
-    gelu_share(a, square, d, s);
-    return mul2(s, fma2(mul2(d, s), mul2(a, fma2(square, pair_of(k3), pair_of(k1))), pair_of(1.0f)));
-}
-
-enum : int { OP_PACK, OP_NORM, OP_GELU, OP_GELU_BACK };
+enum : int { OP_PACK, OP_NORM, OP_GELU, OP_GELU_BACK, OP_ACTIVATE };  // OP_ACTIVATE: of block_kernel
 
 struct BlockArgs {
     const void *x;  // dense input (the gradient for OP_GELU_BACK)
@@ -280,7 +235,8 @@ struct BlockArgs {
     bool aligned;
     Extent extent;
     PackedOut first;   // the packed result
-    PackedOut second;  // the packed input (OP_NORM, OP_GELU); codes NULL: not wanted
+    PackedOut second;  // the packed input (OP_NORM, OP_GELU, OP_ACTIVATE); codes NULL: not wanted
+    int activation;    // OP_ACTIVATE
     // OP_GELU_BACK: the packed input of the GELU
     const uint8_t *codes, *scales;
     long long codes_stride;
@@ -356,6 +312,16 @@ __global__ void __launch_bounds__(THREADS, 2) block_kernel(const __grid_constant
             loaded.unit(j, f);
 #pragma unroll
             for (int i = 0; i < U / 2; ++i) f[i] = gelu(f[i]);
+        }
+    } else if constexpr (OP == OP_ACTIVATE) {
+#pragma unroll
+        for (int j = 0; j < L::UNITS; ++j) {
+            f32x2 *f = y + j * U / 2;
+            loaded.unit(j, f);
+#pragma unroll
+            for (int i = 0; i < U / 2; ++i)
+                f[i] = a.activation == DIPACO_ACTIVATION_SILU ? activate<DIPACO_ACTIVATION_SILU>(f[i])
+                                                              : activate<DIPACO_ACTIVATION_RELU>(f[i]);
         }
     } else {
         const f32x2 scale = pair_of(scale_value(a.scales[blockIdx.x]));
@@ -668,6 +634,32 @@ int dipaco::pack_normalised(const void *x, int64_t x_stride, int dtype, const fl
     a.gamma_aligned = (uintptr_t)gamma % 16 == 0;
     a.beta_aligned = (uintptr_t)beta % 16 == 0;
     return launch_blocks<OP_NORM>(a, dtype, y->rows, y->cols, stream);
+}
+
+int dipaco::pack_activated(const float *x, int64_t x_stride, int activation, const dipaco_packed *y,
+                           const dipaco_packed *x_packed, cudaStream_t stream)
+{
+    BlockArgs a = {};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.first = packed_out(y);
+    a.second = packed_out(x_packed);
+    a.activation = activation;
+    if (activation == DIPACO_ACTIVATION_GELU) return launch_blocks<OP_GELU>(a, DIPACO_F32, y->rows, y->cols, stream);
+    if (activation == DIPACO_ACTIVATION_NONE) {
+        if (x_packed) {
+            BlockArgs b = a;
+            b.first = a.second;
+            if (const int rc = launch_blocks<OP_PACK>(b, DIPACO_F32, y->rows, y->cols, stream)) return rc;
+        }
+        return launch_blocks<OP_PACK>(a, DIPACO_F32, y->rows, y->cols, stream);
+    }
+    const int64_t block_cols = ceil_div(y->cols, PACK_BLOCK), blocks = ceil_div(y->rows, PACK_BLOCK) * block_cols;
+    if (blocks > INT32_MAX - 4096) return DIPACO_ELIMIT;
+    a.extent = {(int)y->rows, (int)y->cols, (int)block_cols};
+    a.aligned = rows_aligned16(x, x_stride, y->rows, 4);
+    block_kernel<float, OP_ACTIVATE><<<(unsigned)blocks, THREADS, 0, stream>>>(a);
+    return launch_status();
 }
 
 extern "C" {

@@ -2,7 +2,7 @@
 
 Layer norm with its gradient, matrices packed in 8 bits (activation checkpoints and the operands of
 the products), the GELU that writes and reads such checkpoints, the product of packed matrices on the
-tensor cores, the norms around a block with its gate and residual, and the clipping of gradients.  Each function allocates its results (and workspace) with torch, launches on the
+tensor cores, linear layers with bias, activation and residual, the norms around a block with its gate and residual, and the clipping of gradients.  Each function allocates its results (and workspace) with torch, launches on the
 current stream of the tensors' device, and raises ``ValueError`` for shapes and dtypes that do not
 fit together or ``binding.DipacoError`` with the library's status.  There is no CPU path.
 
@@ -23,6 +23,8 @@ from . import binding as B
 BLOCK = 128  # one scale per BLOCK x BLOCK values
 _F32, _E4M3, _E8M0 = torch.float32, torch.float8_e4m3fn, torch.float8_e8m0fnu
 _CODES = {torch.float32: B.DIPACO_F32, torch.bfloat16: B.DIPACO_BF16}
+_ACTIVATIONS = {None: B.DIPACO_ACTIVATION_NONE, "relu": B.DIPACO_ACTIVATION_RELU,
+                "silu": B.DIPACO_ACTIVATION_SILU, "gelu": B.DIPACO_ACTIVATION_GELU}
 _stream = torch._C._cuda_getCurrentRawStream  # of a device index
 
 
@@ -271,6 +273,91 @@ def packed_matmul(a: Packed, b: Packed, transpose_a: bool = False, transpose_b: 
     B.dipaco_packed_matmul(a.struct, b.struct, transpose_a, transpose_b, out.data_ptr(), stride, code, accumulate,
                            work.data_ptr() if need else None, need, dev, _stream(dev))
     return out
+
+
+def _activation(name: Optional[str]) -> int:
+    code = _ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError("activation must be None, 'relu', 'silu' or 'gelu'")
+    return code
+
+
+def _layer(x: Packed, w: Packed, bias: Optional[torch.Tensor]) -> Tuple[int, int, int, int, Optional[int], int]:
+    """(tokens, out, in, device, pointer of the bias, its dtype code) of x [tokens, in] through w [out, in]."""
+    m, k = x.shape
+    n, k2 = w.shape
+    dev = x.codes.get_device()
+    if k != k2 or w.codes.get_device() != dev:
+        raise ValueError("x and w must have one inner extent (%d and %d) and device" % (k, k2))
+    if bias is None:
+        return m, n, k, dev, None, B.DIPACO_F32
+    if bias.requires_grad:
+        _refuse_gradient("bias")
+    code = _CODES.get(bias.dtype)
+    if code is None or bias.shape != (n,) or bias.get_device() != dev or (n > 1 and bias.stride(0) != 1):
+        raise ValueError("bias must be a contiguous float32 or bfloat16 vector with one entry per output")
+    return m, n, k, dev, bias.data_ptr(), code
+
+
+def packed_linear(x: Packed, w: Packed, bias: Optional[torch.Tensor] = None, activation: Optional[str] = None,
+                  residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """act(x w^T + bias) + residual for x [tokens, in] and w [out, in], with fp32 sums, rounded once to ``out_dtype``
+    (the residual's, or bfloat16).  ``activation`` is None, "relu", "silu" or "gelu"."""
+    m, n, k, dev, bias_ptr, bias_code = _layer(x, w, bias)
+    act = _activation(activation)
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if residual is None else residual.dtype
+    code = _CODES.get(out_dtype)
+    if code is None:
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    r_ptr, r_stride = (None, 0) if residual is None else _like("residual", residual, (m, n), dev, code)
+    y = x.codes.new_empty((m, n), dtype=out_dtype)
+    need = B.dipaco_packed_matmul_workspace(m, n, k)
+    work = y.new_empty(need, dtype=torch.uint8) if need else None
+    B.dipaco_packed_linear(x.struct, w.struct, bias_ptr, bias_code, act, r_ptr, r_stride, y.data_ptr(), n, code,
+                           work.data_ptr() if need else None, need, dev, _stream(dev))
+    return y
+
+
+def packed_linear_pack(x: Packed, w: Packed, bias: Optional[torch.Tensor] = None, activation: Optional[str] = None,
+                       keep: bool = True):
+    """(y, a): y = act(a) of a = x w^T + bias, packed, and a itself packed as the checkpoint that
+    ``packed_linear_pack_backward`` reads (None without ``keep``, and without an activation, where y is a)."""
+    m, n, k, dev, bias_ptr, bias_code = _layer(x, w, bias)
+    act = _activation(activation)
+    y = _packed_beside(x.codes, m, n)
+    a = _packed_beside(x.codes, m, n) if keep and act else None
+    need = B.dipaco_packed_linear_pack_workspace(m, n, k)
+    work = x.codes.new_empty(need, dtype=torch.uint8) if need else None
+    B.dipaco_packed_linear_pack(x.struct, w.struct, bias_ptr, bias_code, act, y.struct, a.struct if a else None,
+                                work.data_ptr() if need else None, need, dev, _stream(dev))
+    return y, a
+
+
+def packed_linear_pack_backward(dy: Packed, w: Packed, a: Optional[Packed] = None, activation: Optional[str] = None,
+                                bias: bool = True):
+    """(da, dbias) from the gradient dy [tokens, out] of a layer w [out, in]: da = (dy w) act'(a), packed, for the
+    checkpoint a [tokens, in] of the layer before, whose bias has the gradient dbias, the sum of da over the tokens in
+    float32 (None without ``bias``)."""
+    act = _activation(activation)
+    m, k = dy.shape
+    k2, n = w.shape
+    dev = dy.codes.get_device()
+    if k != k2 or w.codes.get_device() != dev:
+        raise ValueError("dy and w must have one outer extent (%d and %d) and device" % (k, k2))
+    if act:
+        if a is None or a.shape != (m, n) or a.codes.get_device() != dev:
+            raise ValueError("a must be the packed input [%d, %d] of the activation, on dy's device" % (m, n))
+    elif a is not None:
+        raise ValueError("a is only read for an activation")
+    da = _packed_beside(dy.codes, m, n)
+    dbias = dy.codes.new_empty(n, dtype=_F32) if bias else None
+    need = B.dipaco_packed_linear_pack_backward_workspace(m, n, k) if bias else 0
+    work = da.codes.new_empty(need, dtype=torch.uint8) if need else None
+    B.dipaco_packed_linear_pack_backward(dy.struct, w.struct, a.struct if act else None, act, da.struct,
+                                         dbias.data_ptr() if bias else None, work.data_ptr() if need else None, need, dev,
+                                         _stream(dev))
+    return da, dbias
 
 
 class ResidualNormGradients(NamedTuple):
