@@ -9,7 +9,8 @@
 //   dg = d (h_f post_gamma + post_beta), summed where g is broadcast
 //   dgamma = sum dn h_z,  dbeta = sum dn,  dpost_gamma = sum d g h_f,  dpost_beta = sum d g   (over rows)
 //
-//   rows_kernel       a block per row, which is read once for every sum: any width
+//   group_rows_kernel a group of warps per row, which stays in their registers: up to 8192 columns
+//   rows_kernel       a block per row, which is read again for every sum: any width
 //   back_rows_kernel  the same for dx, df and the two means that d needs; back_columns_kernel the sums over rows
 #include "inner_common.cuh"
 
@@ -148,6 +149,393 @@ template <typename T> __global__ void __launch_bounds__(ROW_THREADS) rows_kernel
         }
     }
 }
+
+// ------------------------------------------------------------------------------------------ rows in registers
+
+// A group of `warps` warps has a row, eight values for each thread: consecutive ones where rows are on 16-byte
+// boundaries (VEC), else every (32 * warps)-th, so that a warp's accesses stay whole.  What does not change from row
+// to row, the columns' parameters, stays in registers too (HOLD), and the next row is loaded while one is worked on.
+
+constexpr int PER_THREAD = 8;
+
+struct Group {
+    int warps, index, warp, lane, thread;  // thread: of the group
+    int other;                             // the warp whose values this lane joins
+    float count;                           // how many values that warp has; 0: none to join
+    float of_first, of_warp, of_row;       // 1 / number of values of the warp's first lane, of the warp, of the row
+    float2 *slots;                         // [2][warps][rows], shared
+    int parity = 0;
+
+    // A barrier of this group's own.
+    __device__ __forceinline__ void sync() const
+    {
+        asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
+    }
+};
+
+template <bool VEC> __device__ __forceinline__ int column(const Group &g, int j)
+{
+    return VEC ? g.thread * PER_THREAD + j : j * g.warps * 32 + g.thread;
+}
+// Which of the thread's values belong to the row.
+template <bool VEC> __device__ __forceinline__ unsigned valid_values(const Group &g, int cols)
+{
+    unsigned valid = 0u;
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j)
+        if (column<VEC>(g, j) < cols) valid |= 1u << j;
+    return valid;
+}
+constexpr unsigned ALL_VALID = (1u << PER_THREAD) - 1u;
+
+// A thread's values of a row as they are in memory.
+template <typename T> struct RowRaw {
+    unsigned w[PER_THREAD * sizeof(T) / 4];
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_row(const T *row, const Group &g, unsigned valid, RowRaw<T> &raw)
+{
+    constexpr int UE = Unit<T>::UE;
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < PER_THREAD / UE; ++i) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (valid >> (i * UE) & 1u) v = __ldcs(reinterpret_cast<const uint4 *>(row + g.thread * PER_THREAD) + i);
+            raw.w[4 * i] = v.x; raw.w[4 * i + 1] = v.y; raw.w[4 * i + 2] = v.z; raw.w[4 * i + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER_THREAD; ++j) {
+            unsigned v = 0u;
+            if (valid >> j & 1u) {
+                if constexpr (sizeof(T) == 2)
+                    v = __ldcs(reinterpret_cast<const unsigned short *>(row) + column<false>(g, j));
+                else
+                    v = __ldcs(reinterpret_cast<const unsigned *>(row) + column<false>(g, j));
+            }
+            if (sizeof(T) == 4)
+                raw.w[j] = v;
+            else if (j & 1)
+                raw.w[j / 2] |= v << 16;
+            else
+                raw.w[j / 2] = v;
+        }
+    }
+}
+// Values that do not belong to the row are zero.
+template <typename T> __device__ __forceinline__ void widen_row(const RowRaw<T> &raw, unsigned valid, f32x2 *v)
+{
+    constexpr int UE = Unit<T>::UE;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD / UE; ++i)
+        widen_pairs<T>(make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]), v + i * UE / 2);
+    if (valid != ALL_VALID) {
+#pragma unroll
+        for (int i = 0; i < PER_THREAD / 2; ++i) {
+            const float2 w = values_of(v[i]);
+            v[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ void narrow_row(const f32x2 *v, RowRaw<T> &raw)
+{
+    constexpr int UE = Unit<T>::UE;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD / UE; ++i) {
+        const uint4 u = narrow_pairs<T>(v + i * UE / 2);
+        raw.w[4 * i] = u.x; raw.w[4 * i + 1] = u.y; raw.w[4 * i + 2] = u.z; raw.w[4 * i + 3] = u.w;
+    }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_row(T *row, const Group &g, unsigned valid, const RowRaw<T> &raw)
+{
+    constexpr int UE = Unit<T>::UE;
+    if constexpr (VEC) {
+        if (valid == ALL_VALID) {
+#pragma unroll
+            for (int i = 0; i < PER_THREAD / UE; ++i)
+                reinterpret_cast<uint4 *>(row + g.thread * PER_THREAD)[i] =
+                    make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]);
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j)
+        if (valid >> j & 1u) {
+            if constexpr (sizeof(T) == 2)
+                reinterpret_cast<unsigned short *>(row)[column<VEC>(g, j)] = (unsigned short)(raw.w[j / 2] >> 16 * (j & 1));
+            else
+                reinterpret_cast<unsigned *>(row)[column<VEC>(g, j)] = raw.w[j];
+        }
+}
+// Parameters of the thread's columns.
+template <bool VEC>
+__device__ __forceinline__ void load_columns(const void *p, bool bf16, const Group &g, int cols, float otherwise, f32x2 *v)
+{
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < PER_THREAD / 2; ++i) v[i] = pair_of(otherwise);
+    } else if (VEC) {
+        param_pairs<PER_THREAD>(p, bf16, reinterpret_cast<uintptr_t>(p) % 16 == 0, g.thread * PER_THREAD, cols, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER_THREAD / 2; ++i) {
+            const int c0 = column<VEC>(g, 2 * i), c1 = column<VEC>(g, 2 * i + 1);
+            v[i] = pair_of(c0 < cols ? load_param(p, bf16, c0) : 0.0f, c1 < cols ? load_param(p, bf16, c1) : 0.0f);
+        }
+    }
+}
+
+__device__ __forceinline__ float sum_pairs(const f32x2 *v)
+{
+    return sum_of(add2(add2(v[0], v[1]), add2(v[2], v[3])));
+}
+
+// Sums of pairs of values over the group, R at a time, on every thread: over warps in shared memory, in two sets that
+// take turns, so that a set is written again only after everyone has read it.  Up to eight warps are joined in three
+// steps by every eight lanes, more in five.
+template <int R> __device__ __forceinline__ void join_warps(const Group &g, float2 *sums)
+{
+    for (int o = g.warps <= 8 ? 4 : 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sums[r].x += __shfl_xor_sync(0xffffffffu, sums[r].x, o);
+            sums[r].y += __shfl_xor_sync(0xffffffffu, sums[r].y, o);
+        }
+}
+template <int R> __device__ __forceinline__ void warp_sums(float2 *sums)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sums[r].x += __shfl_xor_sync(0xffffffffu, sums[r].x, o);
+            sums[r].y += __shfl_xor_sync(0xffffffffu, sums[r].y, o);
+        }
+}
+// Hands the warps' values round: [warp][row].
+template <int R> __device__ __forceinline__ const float2 *exchange(Group &g, const float2 *own)
+{
+    float2 *slots = g.slots + g.parity * g.warps * R;
+    if (g.lane == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) slots[g.warp * R + r] = own[r];
+    }
+    g.sync();
+    g.parity ^= 1;
+    return slots;
+}
+
+// Mean and 1 / sqrt(var + eps) of the group's R rows.  Differences are taken from the mean of the warp's first lane's
+// values: it is exact where all values are equal, and no farther from the warp's mean than the spread of its 256
+// values times sqrt(32), so that the squares lose five bits at most.  The warps are joined about the first one's mean.
+template <int R, bool VEC>
+__device__ __forceinline__ void group_statistics(Group &g, const f32x2 (*v)[PER_THREAD / 2], unsigned valid, float eps, float2 *found)
+{
+    float2 sums[R];
+    float centre[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) centre[r] = __shfl_sync(0xffffffffu, sum_pairs(v[r]) * g.of_first, 0);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        f32x2 d[PER_THREAD / 2], squares = 0ull;
+#pragma unroll
+        for (int i = 0; i < PER_THREAD / 2; ++i) d[i] = add2(v[r][i], pair_of(-centre[r]));
+        if (valid != ALL_VALID) {
+#pragma unroll
+            for (int i = 0; i < PER_THREAD / 2; ++i) {
+                const float2 w = values_of(d[i]);
+                d[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PER_THREAD / 2; ++i) squares = fma2(d[i], d[i], squares);
+        sums[r] = make_float2(sum_pairs(d), sum_of(squares));
+    }
+    warp_sums<R>(sums);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const float off = sums[r].x * g.of_warp;
+        sums[r] = make_float2(centre[r] + off, fmaxf(fmaf(-off, sums[r].x, sums[r].y), 0.0f));
+    }
+    if (g.warps > 1) {
+        const float2 *slots = exchange<R>(g, sums);
+        float first[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            first[r] = slots[r].x;
+            const float2 of = slots[g.other * R + r];
+            const float apart = of.x - first[r];
+            sums[r] = g.count > 0.0f ? make_float2(g.count * apart, fmaf(g.count * apart, apart, of.y)) : make_float2(0.0f, 0.0f);
+        }
+        join_warps<R>(g, sums);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float off = sums[r].x * g.of_row;
+            sums[r] = make_float2(first[r] + off, fmaxf(fmaf(-off, sums[r].x, sums[r].y), 0.0f));
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) found[r] = make_float2(sums[r].x, rsqrtf(fmaf(sums[r].y, g.of_row, eps)));
+}
+
+// How many values a warp of the group has, and its first lane.
+template <bool VEC> __device__ __forceinline__ int values_of_warp(int warps, int warp, int cols)
+{
+    if (VEC) return min(max(cols - warp * 32 * PER_THREAD, 0), 32 * PER_THREAD);
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j) n += min(max(cols - (j * warps + warp) * 32, 0), 32);
+    return n;
+}
+template <bool VEC> __device__ __forceinline__ int values_of_first_lane(int warps, int warp, int cols)
+{
+    if (VEC) return min(max(cols - warp * 32 * PER_THREAD, 0), PER_THREAD);
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < PER_THREAD; ++j) n += (j * warps + warp) * 32 < cols;
+    return n;
+}
+
+// A group of the block, with `slots` of 2 * rows float2 for each of the block's warps.
+template <bool VEC> __device__ __forceinline__ Group make_group(int warps, int cols, float2 *slots, int rows)
+{
+    Group g;
+    g.warps = warps;
+    g.lane = threadIdx.x & 31;
+    g.index = (int)(threadIdx.x >> 5) / warps;
+    g.warp = (int)(threadIdx.x >> 5) - g.index * warps;
+    g.thread = g.warp * 32 + g.lane;
+    g.slots = slots + 2 * g.index * warps * rows;
+    const int joined = warps <= 8 ? g.lane & 7 : g.lane;
+    g.other = min(joined, warps - 1);
+    g.count = joined < warps ? (float)values_of_warp<VEC>(warps, joined, cols) : 0.0f;
+    g.of_first = 1.0f / (float)values_of_first_lane<VEC>(warps, g.warp, cols);
+    g.of_warp = 1.0f / (float)values_of_warp<VEC>(warps, g.warp, cols);
+    g.of_row = 1.0f / (float)cols;
+    return g;
+}
+
+// GATE: what a thread needs for it.
+enum : int { GATE_IN_COLUMNS, GATE_OF_ROW, GATE_OF_VALUES };
+
+constexpr int MAX_GROUP_COLS = 32 * 32 * PER_THREAD;
+
+// HOLD: blocks of up to 16 warps; R rows at a time.
+template <typename T, bool VEC, int GATE, bool HOLD, int R>
+__global__ void __launch_bounds__(HOLD ? 512 : 1024, 1)
+    group_rows_kernel(const __grid_constant__ NormArgs a, int warps)
+{
+    __shared__ float2 slots[2 * 32 * R];
+    Group g = make_group<VEC>(warps, a.cols, slots, R);
+    const int groups = (int)(blockDim.x >> 5) / warps;
+    const unsigned valid = valid_values<VEC>(g, a.cols);
+    // p = h factor + shift, a gate of columns in both
+    f32x2 factor[PER_THREAD / 2], shift[PER_THREAD / 2], gamma[PER_THREAD / 2], beta[PER_THREAD / 2];
+    const auto load_block_columns = [&] {
+        load_columns<VEC>(a.post_gamma, a.params_bf16, g, a.cols, 1.0f, factor);
+        load_columns<VEC>(a.post_beta, a.params_bf16, g, a.cols, 0.0f, shift);
+        if (GATE == GATE_IN_COLUMNS && a.gate_kind == DIPACO_GATE_COLS) {
+            f32x2 gate[PER_THREAD / 2];
+            load_columns<VEC>(a.gate, a.gate_bf16, g, a.cols, 1.0f, gate);
+#pragma unroll
+            for (int i = 0; i < PER_THREAD / 2; ++i) {
+                factor[i] = mul2(factor[i], gate[i]);
+                shift[i] = mul2(shift[i], gate[i]);
+            }
+        }
+    };
+    const auto load_next_columns = [&] {
+        load_columns<VEC>(a.gamma, a.params_bf16, g, a.cols, 1.0f, gamma);
+        load_columns<VEC>(a.beta, a.params_bf16, g, a.cols, 0.0f, beta);
+    };
+    const long long between = (long long)gridDim.x * groups, step = between * R;  // the R rows are `between` apart
+    long long row = (long long)blockIdx.x * groups + g.index;
+    RowRaw<T> next_x[R], next_f[R];
+    const auto load_next = [&](long long first) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const long long at = min(first + r * between, (long long)a.rows - 1);  // the last row again where there is none
+            load_row<T, VEC>(static_cast<const T *>(a.f.dense) + at * a.f.stride, g, valid, next_f[r]);
+            load_row<T, VEC>(static_cast<const T *>(a.x.dense) + at * a.x.stride, g, valid, next_x[r]);
+        }
+    };
+    if (row < a.rows) load_next(row);
+    if (HOLD) {
+        load_block_columns();
+        if (a.n) load_next_columns();
+    }
+    for (; row < a.rows; row += step) {
+        f32x2 v[R][PER_THREAD / 2];
+        RowRaw<T> x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            widen_row<T>(next_f[r], valid, v[r]);
+            x[r] = next_x[r];
+        }
+        if (row + step < a.rows) load_next(row + step);
+        float2 of_f[R], of_z[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) of_f[r] = of_z[r] = make_float2(0.0f, 1.0f);
+        if (a.post_norm) group_statistics<R, VEC>(g, v, valid, a.eps, of_f);
+        if (!HOLD) load_block_columns();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const long long at = row + r * between;
+            if (R > 1 && at >= a.rows) break;
+            f32x2 gate[PER_THREAD / 2], stream[PER_THREAD / 2];
+            if (GATE == GATE_OF_ROW) {
+                const float of_row = load_param(a.gate, a.gate_bf16, at);
+#pragma unroll
+                for (int i = 0; i < PER_THREAD / 2; ++i) gate[i] = pair_of(of_row);
+            } else if (GATE == GATE_OF_VALUES) {
+                RowRaw<T> raw;
+                load_row<T, VEC>(static_cast<const T *>(a.gate) + at * a.gate_stride, g, valid, raw);
+                widen_row<T>(raw, valid, gate);
+            }
+            widen_row<T>(x[r], valid, stream);
+#pragma unroll
+            for (int i = 0; i < PER_THREAD / 2; ++i) {
+                const f32x2 scaled = mul2(stream[i], pair_of(a.scale));
+                const f32x2 p = fma2(mul2(add2(v[r][i], pair_of(-of_f[r].x)), pair_of(of_f[r].y)), factor[i], shift[i]);
+                v[r][i] = GATE == GATE_IN_COLUMNS ? add2(p, scaled) : fma2(gate[i], p, scaled);
+            }
+            RowRaw<T> raw;
+            narrow_row<T>(v[r], raw);
+            store_row<T, VEC>(static_cast<T *>(a.z_out) + at * a.z_stride, g, valid, raw);
+            widen_row<T>(raw, valid, v[r]);
+        }
+        if (a.norm) {
+            group_statistics<R, VEC>(g, v, valid, a.eps, of_z);
+            if (a.n) {
+                if (!HOLD) load_next_columns();
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const long long at = row + r * between;
+                    if (R > 1 && at >= a.rows) break;
+#pragma unroll
+                    for (int i = 0; i < PER_THREAD / 2; ++i)
+                        v[r][i] = fma2(mul2(add2(v[r][i], pair_of(-of_z[r].x)), pair_of(of_z[r].y)), gamma[i], beta[i]);
+                    RowRaw<T> raw;
+                    narrow_row<T>(v[r], raw);
+                    store_row<T, VEC>(static_cast<T *>(a.n) + at * a.n_stride, g, valid, raw);
+                }
+            }
+        }
+        if (g.thread < R) {
+            const long long at = row + g.thread * between;
+            const float2 f = R > 1 && g.thread ? of_f[R - 1] : of_f[0], z = R > 1 && g.thread ? of_z[R - 1] : of_z[0];
+            if (at < a.rows) {
+                a.stats[at] = f.x;
+                a.stats[a.rows + at] = f.y;
+                a.stats[2ll * a.rows + at] = z.x;
+                a.stats[3ll * a.rows + at] = z.y;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ gradients
 
 // What a row's statistics and the means of its gradient say about its values.
 struct RowOf {
@@ -378,6 +766,39 @@ NormArgs norm_args(const dipaco_residual_norm_args *a)
     return n;
 }
 
+template <typename T, bool VEC, int GATE> int launch_groups(const NormArgs &a, cudaStream_t stream)
+{
+    const int warps = (int)ceil_div(a.cols, 32 * PER_THREAD);
+    const int groups = (warps <= 16 ? 16 : 32) / warps;
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.rows, groups), 148), threads = groups * warps * 32;
+    if (warps > 16)
+        group_rows_kernel<T, VEC, GATE, false, 1><<<grid, threads, 0, stream>>>(a, warps);
+    else if (a.rows <= (int64_t)grid * groups)
+        group_rows_kernel<T, VEC, GATE, true, 1><<<grid, threads, 0, stream>>>(a, warps);
+    else
+        group_rows_kernel<T, VEC, GATE, true, 2><<<grid, threads, 0, stream>>>(a, warps);
+    return launch_status();
+}
+
+template <typename T> int launch_rows(const NormArgs &a, cudaStream_t stream)
+{
+    if (a.cols > MAX_GROUP_COLS) {
+        rows_kernel<T><<<(unsigned)std::min<int64_t>(a.rows, 148 * 8), ROW_THREADS, 0, stream>>>(a);
+        return launch_status();
+    }
+    const auto aligned = [&](const void *p, long long stride) { return !p || rows_aligned16(p, stride, a.rows, sizeof(T)); };
+    const bool vec = aligned(a.x.dense, a.x.stride) && aligned(a.f.dense, a.f.stride) && aligned(a.z_out, a.z_stride) &&
+                     aligned(a.n, a.n_stride) && (a.gate_kind != DIPACO_GATE_FULL || aligned(a.gate, a.gate_stride));
+    switch (a.gate_kind) {
+    case DIPACO_GATE_ROWS:
+        return vec ? launch_groups<T, true, GATE_OF_ROW>(a, stream) : launch_groups<T, false, GATE_OF_ROW>(a, stream);
+    case DIPACO_GATE_FULL:
+        return vec ? launch_groups<T, true, GATE_OF_VALUES>(a, stream) : launch_groups<T, false, GATE_OF_VALUES>(a, stream);
+    default:
+        return vec ? launch_groups<T, true, GATE_IN_COLUMNS>(a, stream) : launch_groups<T, false, GATE_IN_COLUMNS>(a, stream);
+    }
+}
+
 struct BackPlan {
     int parts;
     int64_t partial_bytes, bytes;
@@ -429,12 +850,7 @@ int dipaco_residual_norm(const dipaco_residual_norm_args *args, const void *x, i
     a.n = n;
     a.n_stride = n_stride;
     a.stats = stats;
-    const unsigned grid = (unsigned)std::min<int64_t>(rows, 148 * 8);
-    if (args->dtype == DIPACO_BF16)
-        rows_kernel<__nv_bfloat16><<<grid, ROW_THREADS, 0, stream>>>(a);
-    else
-        rows_kernel<float><<<grid, ROW_THREADS, 0, stream>>>(a);
-    if (const int rc = launch_status()) return rc;
+    if (const int rc = args->dtype == DIPACO_BF16 ? launch_rows<__nv_bfloat16>(a, stream) : launch_rows<float>(a, stream)) return rc;
     if (!n_packed) return DIPACO_OK;
     return pack_normalised(z, z_stride, args->dtype, stats + 2 * rows, stats + 3 * rows, args->gamma, args->beta,
                            args->param_dtype, n_packed, z_packed, stream);
