@@ -11,7 +11,8 @@
 //
 //   group_rows_kernel a group of warps per row, which stays in their registers: up to 8192 columns
 //   rows_kernel       a block per row, which is read again for every sum: any width
-//   back_rows_kernel  the same for dx, df and the two means that d needs; back_columns_kernel the sums over rows
+//   group_back_kernel every gradient in one pass, a row in the registers of a group: up to 4096 columns
+//   back_rows_kernel  as rows_kernel for dx, df and the two means that d needs; back_columns_kernel the sums over rows
 #include "inner_common.cuh"
 
 #include <algorithm>
@@ -187,6 +188,16 @@ template <bool VEC> __device__ __forceinline__ unsigned valid_values(const Group
     return valid;
 }
 constexpr unsigned ALL_VALID = (1u << PER_THREAD) - 1u;
+// Makes the others zero.
+__device__ __forceinline__ void keep_valid(unsigned valid, f32x2 *v)
+{
+    if (valid == ALL_VALID) return;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD / 2; ++i) {
+        const float2 w = values_of(v[i]);
+        v[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
+    }
+}
 
 // A thread's values of a row as they are in memory.
 template <typename T> struct RowRaw {
@@ -229,13 +240,7 @@ template <typename T> __device__ __forceinline__ void widen_row(const RowRaw<T> 
 #pragma unroll
     for (int i = 0; i < PER_THREAD / UE; ++i)
         widen_pairs<T>(make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]), v + i * UE / 2);
-    if (valid != ALL_VALID) {
-#pragma unroll
-        for (int i = 0; i < PER_THREAD / 2; ++i) {
-            const float2 w = values_of(v[i]);
-            v[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
-        }
-    }
+    keep_valid(valid, v);
 }
 template <typename T> __device__ __forceinline__ void narrow_row(const f32x2 *v, RowRaw<T> &raw)
 {
@@ -341,13 +346,7 @@ __device__ __forceinline__ void group_statistics(Group &g, const f32x2 (*v)[PER_
         f32x2 d[PER_THREAD / 2], squares = 0ull;
 #pragma unroll
         for (int i = 0; i < PER_THREAD / 2; ++i) d[i] = add2(v[r][i], pair_of(-centre[r]));
-        if (valid != ALL_VALID) {
-#pragma unroll
-            for (int i = 0; i < PER_THREAD / 2; ++i) {
-                const float2 w = values_of(d[i]);
-                d[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
-            }
-        }
+        keep_valid(valid, d);
 #pragma unroll
         for (int i = 0; i < PER_THREAD / 2; ++i) squares = fma2(d[i], d[i], squares);
         sums[r] = make_float2(sum_pairs(d), sum_of(squares));
@@ -626,6 +625,216 @@ template <typename T> __global__ void __launch_bounds__(ROW_THREADS) back_rows_k
     }
 }
 
+// A row of f or z: as load_row, or eight codes.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_source(const Source &s, long long row, const Group &g, unsigned valid, RowRaw<T> &raw)
+{
+    if (s.dense) {
+        load_row<T, VEC>(static_cast<const T *>(s.dense) + row * s.stride, g, valid, raw);
+        return;
+    }
+    const uint8_t *codes = s.codes + row * s.stride;
+    raw.w[0] = raw.w[1] = 0u;
+    if constexpr (VEC) {
+        if (valid) {  // rows of codes are padded to 16 bytes
+            const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(codes) + g.thread);
+            raw.w[0] = v.x;
+            raw.w[1] = v.y;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER_THREAD; ++j)
+            if (valid >> j & 1u) raw.w[j / 4] |= (unsigned)__ldcs(codes + column<false>(g, j)) << 8 * (j % 4);
+    }
+}
+// Their values (zero outside the row).
+template <typename T, bool VEC>
+__device__ __forceinline__ void widen_source(const Source &s, long long row, const Group &g, unsigned valid, const RowRaw<T> &raw, f32x2 *v)
+{
+    if (s.dense) {
+        widen_row<T>(raw, valid, v);
+        return;
+    }
+    const uint8_t *scales = s.scales + row / PACK_BLOCK * s.scale_cols;
+    const f32x2 one = VEC && valid ? pair_of(scale_value(scales[g.thread * PER_THREAD / PACK_BLOCK])) : 0ull;
+#pragma unroll
+    for (int i = 0; i < PER_THREAD / 2; ++i) {
+        f32x2 scale = one;
+        if (!VEC)
+            scale = pair_of(valid >> (2 * i) & 1u ? scale_value(scales[column<VEC>(g, 2 * i) / PACK_BLOCK]) : 0.0f,
+                            valid >> (2 * i + 1) & 1u ? scale_value(scales[column<VEC>(g, 2 * i + 1) / PACK_BLOCK]) : 0.0f);
+        v[i] = mul2(decode_pair(raw.w[i / 2] >> 16 * (i & 1)), scale);
+    }
+    keep_valid(valid, v);
+}
+
+// Sums of pairs over the group, on every thread.
+template <int R> __device__ __forceinline__ void group_sums(Group &g, float2 *sums)
+{
+    warp_sums<R>(sums);
+    if (g.warps == 1) return;
+    const float2 *slots = exchange<R>(g, sums);
+#pragma unroll
+    for (int r = 0; r < R; ++r) sums[r] = g.count > 0.0f ? slots[g.other * R + r] : make_float2(0.0f, 0.0f);
+    join_warps<R>(g, sums);
+}
+
+constexpr int MAX_BACK_COLS = 16 * 32 * PER_THREAD;
+
+// A persistent block of groups, each with a row at a time; a thread keeps the sums over its rows of its columns.  The
+// next row's values are loaded where this row's have been used for the last time.
+template <typename T, bool VEC, int GATE>
+__global__ void __launch_bounds__(512, 1) group_back_kernel(const __grid_constant__ NormArgs a, int warps)
+{
+    constexpr int P = PER_THREAD / 2;
+    __shared__ float2 slots[2 * 16 * 2];
+    __shared__ float joined[MAX_BACK_COLS];
+    Group g = make_group<VEC>(warps, a.cols, slots, 2);
+    const int groups = (int)(blockDim.x >> 5) / warps;
+    const unsigned valid = valid_values<VEC>(g, a.cols);
+    const long long step = (long long)gridDim.x * groups;
+    long long row = (long long)blockIdx.x * groups + g.index;
+    RowRaw<T> dn = {}, dz = {}, z = {}, f = {};
+    const auto load_z = [&](long long at) {
+        if (a.norm) {
+            load_row<T, VEC>(static_cast<const T *>(a.dn.dense) + at * a.dn.stride, g, valid, dn);
+            load_source<T, VEC>(a.z, at, g, valid, z);
+        }
+        if (a.dz.dense) load_row<T, VEC>(static_cast<const T *>(a.dz.dense) + at * a.dz.stride, g, valid, dz);
+    };
+    if (row < a.rows) {
+        load_z(row);
+        load_source<T, VEC>(a.f, row, g, valid, f);
+    }
+    f32x2 gamma[P], factor[P], shift[P];  // factor: post_gamma, times a gate of columns
+    load_columns<VEC>(a.gamma, a.params_bf16, g, a.cols, 1.0f, gamma);
+    load_columns<VEC>(a.post_gamma, a.params_bf16, g, a.cols, 1.0f, factor);
+    if (GATE == GATE_IN_COLUMNS) {
+        if (a.gate_kind == DIPACO_GATE_COLS) {
+            f32x2 gate[P];
+            load_columns<VEC>(a.gate, a.gate_bf16, g, a.cols, 1.0f, gate);
+#pragma unroll
+            for (int i = 0; i < P; ++i) factor[i] = mul2(factor[i], gate[i]);
+        }
+    } else {
+        load_columns<VEC>(a.post_beta, a.params_bf16, g, a.cols, 0.0f, shift);
+    }
+    f32x2 sums[4][P];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < P; ++i) sums[q][i] = 0ull;
+
+    for (; row < a.rows; row += step) {
+        const bool more = row + step < a.rows;
+        f32x2 d[P], h[P];
+        widen_row<T>(dz, valid, d);
+        if (a.norm) {
+            const float mean = a.saved[2ll * a.rows + row], rstd = a.saved[3ll * a.rows + row];
+            f32x2 u[P];
+            widen_row<T>(dn, valid, u);
+            widen_source<T, VEC>(a.z, row, g, valid, z, h);
+            f32x2 all[2] = {0ull, 0ull};
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                h[i] = mul2(add2(h[i], pair_of(-mean)), pair_of(rstd));
+                sums[0][i] = fma2(u[i], h[i], sums[0][i]);
+                sums[1][i] = add2(sums[1][i], u[i]);
+                u[i] = mul2(u[i], gamma[i]);
+                all[0] = add2(all[0], u[i]);
+                all[1] = fma2(u[i], h[i], all[1]);
+            }
+            float2 of[1] = {make_float2(sum_of(all[0]), sum_of(all[1]))};
+            group_sums<1>(g, of);
+            const f32x2 mean_u = pair_of(-of[0].x * g.of_row), mean_uh = pair_of(-of[0].y * g.of_row);
+#pragma unroll
+            for (int i = 0; i < P; ++i) d[i] = fma2(fma2(h[i], mean_uh, add2(u[i], mean_u)), pair_of(rstd), d[i]);
+            keep_valid(valid, d);
+        }
+        if (more) load_z(row + step);
+        f32x2 out[P];
+        RowRaw<T> raw;
+        if (a.dx) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) out[i] = mul2(d[i], pair_of(a.scale));
+            narrow_row<T>(out, raw);
+            store_row<T, VEC>(static_cast<T *>(a.dx) + row * a.dx_stride, g, valid, raw);
+        }
+        const float mean = a.post_norm ? a.saved[row] : 0.0f, rstd = a.post_norm ? a.saved[a.rows + row] : 1.0f;
+        widen_source<T, VEC>(a.f, row, g, valid, f, h);
+#pragma unroll
+        for (int i = 0; i < P; ++i) h[i] = mul2(add2(h[i], pair_of(-mean)), pair_of(rstd));
+        if (more) load_source<T, VEC>(a.f, row + step, g, valid, f);
+        f32x2 of_gate = 0ull;
+        if (GATE != GATE_IN_COLUMNS) {
+            f32x2 gate[P];
+            if (GATE == GATE_OF_ROW) {
+                const float of_row = load_param(a.gate, a.gate_bf16, row);
+#pragma unroll
+                for (int i = 0; i < P; ++i) gate[i] = pair_of(of_row);
+            } else {
+                load_row<T, VEC>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);
+                widen_row<T>(raw, valid, gate);
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                out[i] = mul2(d[i], fma2(h[i], factor[i], shift[i]));
+                if (GATE == GATE_OF_ROW) of_gate = add2(of_gate, out[i]);
+                d[i] = mul2(d[i], gate[i]);
+            }
+            if (GATE == GATE_OF_VALUES && a.dgate) {
+                narrow_row<T>(out, raw);
+                store_row<T, VEC>(static_cast<T *>(a.dgate) + row * a.dgate_stride, g, valid, raw);
+            }
+        }
+        f32x2 all[2] = {0ull, 0ull};
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            sums[2][i] = fma2(d[i], h[i], sums[2][i]);
+            sums[3][i] = add2(sums[3][i], d[i]);
+            d[i] = mul2(d[i], factor[i]);
+            all[0] = add2(all[0], d[i]);
+            all[1] = fma2(d[i], h[i], all[1]);
+        }
+        float2 of[2] = {make_float2(sum_of(all[0]), sum_of(all[1])), make_float2(sum_of(of_gate), 0.0f)};
+        if (GATE == GATE_OF_ROW) {
+            group_sums<2>(g, of);
+            if (g.thread == 0 && a.dgate) static_cast<float *>(a.dgate)[row] = of[1].x;
+        } else if (a.post_norm) {
+            group_sums<1>(g, of);
+        }
+        if (a.df) {
+            if (a.post_norm) {
+                const f32x2 mean_q = pair_of(-of[0].x * g.of_row), mean_qh = pair_of(-of[0].y * g.of_row);
+#pragma unroll
+                for (int i = 0; i < P; ++i) d[i] = mul2(fma2(h[i], mean_qh, add2(d[i], mean_q)), pair_of(rstd));
+            }
+            narrow_row<T>(d, raw);
+            store_row<T, VEC>(static_cast<T *>(a.df) + row * a.df_stride, g, valid, raw);
+        }
+    }
+    // the groups' sums, one group after another
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        for (int turn = 0; turn < groups; ++turn) {
+            if (g.index == turn) {
+#pragma unroll
+                for (int j = 0; j < PER_THREAD; ++j) {
+                    const float2 w = values_of(sums[q][j / 2]);
+                    const float own = j & 1 ? w.y : w.x;
+                    if (valid >> j & 1u) {
+                        float &at = joined[column<VEC>(g, j)];
+                        at = turn ? at + own : own;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < a.cols; c += blockDim.x) a.partial[((long long)blockIdx.x * 4 + q) * a.cols + c] = joined[c];
+        __syncthreads();
+    }
+}
+
 // A gate that is one for all rows leaves the sums over rows of d h_f and d for join_kernel, any other goes into them.
 __device__ __forceinline__ bool gate_at_the_end(const NormArgs &a)
 {
@@ -800,17 +1009,54 @@ template <typename T> int launch_rows(const NormArgs &a, cudaStream_t stream)
 }
 
 struct BackPlan {
+    int groups;  // of a block of group_back_kernel; 0: the kernels for any width
     int parts;
     int64_t partial_bytes, bytes;
 };
 BackPlan plan_back(int64_t rows, int64_t cols)
 {
-    const int64_t columns = std::max<int64_t>(1, ceil_div(cols, COLUMN_THREADS));
     BackPlan p;
+    if (cols <= MAX_BACK_COLS) {
+        const int64_t warps = std::max<int64_t>(1, ceil_div(cols, 32 * PER_THREAD));
+        p.groups = (int)(16 / warps);
+        p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(148, ceil_div(rows, p.groups)));
+        p.partial_bytes = p.bytes = (int64_t)p.parts * 4 * cols * 4;
+        return p;
+    }
+    const int64_t columns = ceil_div(cols, COLUMN_THREADS);
+    p.groups = 0;
     p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({MAX_PARTS, ceil_div(rows, 16), ceil_div(148 * 8, columns)}));
     p.partial_bytes = (int64_t)p.parts * 4 * cols * 4;
     p.bytes = ceil_div(p.partial_bytes, 16) * 16 + rows * 8;
     return p;
+}
+
+template <typename T, bool VEC> int launch_back_groups(const NormArgs &a, const BackPlan &plan, cudaStream_t stream)
+{
+    const int warps = (int)ceil_div(a.cols, 32 * PER_THREAD), threads = plan.groups * warps * 32;
+    if (a.gate_kind == DIPACO_GATE_ROWS)
+        group_back_kernel<T, VEC, GATE_OF_ROW><<<plan.parts, threads, 0, stream>>>(a, warps);
+    else if (a.gate_kind == DIPACO_GATE_FULL)
+        group_back_kernel<T, VEC, GATE_OF_VALUES><<<plan.parts, threads, 0, stream>>>(a, warps);
+    else
+        group_back_kernel<T, VEC, GATE_IN_COLUMNS><<<plan.parts, threads, 0, stream>>>(a, warps);
+    return launch_status();
+}
+
+template <typename T> int launch_back(const NormArgs &a, const BackPlan &plan, cudaStream_t stream)
+{
+    if (plan.groups == 0) {
+        back_rows_kernel<T><<<(unsigned)std::min<int64_t>(a.rows, 148 * 8), ROW_THREADS, 0, stream>>>(a);
+        if (const int rc = launch_status()) return rc;
+        const dim3 columns((unsigned)ceil_div(a.cols, COLUMN_THREADS), (unsigned)plan.parts);
+        back_columns_kernel<T><<<columns, COLUMN_THREADS, 0, stream>>>(a);
+        return launch_status();
+    }
+    const auto aligned = [&](const void *p, long long stride) { return !p || rows_aligned16(p, stride, a.rows, sizeof(T)); };
+    const bool vec = aligned(a.dn.dense, a.dn.stride) && aligned(a.dz.dense, a.dz.stride) && aligned(a.f.dense, a.f.stride) &&
+                     aligned(a.z.dense, a.z.stride) && aligned(a.dx, a.dx_stride) && aligned(a.df, a.df_stride) &&
+                     (a.gate_kind != DIPACO_GATE_FULL || (aligned(a.gate, a.gate_stride) && aligned(a.dgate, a.dgate_stride)));
+    return vec ? launch_back_groups<T, true>(a, plan, stream) : launch_back_groups<T, false>(a, plan, stream);
 }
 
 } // namespace
@@ -925,16 +1171,7 @@ int dipaco_residual_norm_backward(const dipaco_residual_norm_args *args, const v
     a.partial = static_cast<float *>(workspace);
     a.row_means = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + ceil_div(plan.partial_bytes, 16) * 16);
     a.parts = plan.parts;
-    const unsigned grid = (unsigned)std::min<int64_t>(rows, 148 * 8);
-    const dim3 columns((unsigned)ceil_div(cols, COLUMN_THREADS), (unsigned)plan.parts);
-    if (dtype == DIPACO_BF16) {
-        back_rows_kernel<__nv_bfloat16><<<grid, ROW_THREADS, 0, stream>>>(a);
-        back_columns_kernel<__nv_bfloat16><<<columns, COLUMN_THREADS, 0, stream>>>(a);
-    } else {
-        back_rows_kernel<float><<<grid, ROW_THREADS, 0, stream>>>(a);
-        back_columns_kernel<float><<<columns, COLUMN_THREADS, 0, stream>>>(a);
-    }
-    if (const int rc = launch_status()) return rc;
+    if (const int rc = dtype == DIPACO_BF16 ? launch_back<__nv_bfloat16>(a, plan, stream) : launch_back<float>(a, plan, stream)) return rc;
     if (!dgate_cols && !dgamma && !dbeta && !dpost_gamma && !dpost_beta) return DIPACO_OK;
     JoinArgs j = {};
     j.partial = a.partial;
