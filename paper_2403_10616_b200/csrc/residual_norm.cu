@@ -11,7 +11,7 @@
 //
 //   group_rows_kernel a group of warps per row, which stays in their registers: up to 8192 columns
 //   rows_kernel       a block per row, which is read again for every sum: any width
-//   group_back_kernel every gradient in one pass, a row in the registers of a group: up to 4096 columns
+//   group_back_kernel every gradient in one pass, a row in the registers of a group: up to 8192 columns
 //   back_rows_kernel  as rows_kernel for dx, df and the two means that d needs; back_columns_kernel the sums over rows
 #include "inner_common.cuh"
 
@@ -153,76 +153,93 @@ template <typename T> __global__ void __launch_bounds__(ROW_THREADS) rows_kernel
 
 // ------------------------------------------------------------------------------------------ rows in registers
 
-// A group of `warps` warps has a row, eight values for each thread: consecutive ones where rows are on 16-byte
-// boundaries (VEC), else every (32 * warps)-th, so that a warp's accesses stay whole.  What does not change from row
-// to row, the columns' parameters, stays in registers too (HOLD), and the next row is loaded while one is worked on.
-
-constexpr int PER_THREAD = 8;
+// A group of warps has a row, 8 U values for each thread, which stay in registers from the first sum to the last
+// result.  VEC (rows on 16-byte boundaries, of whole units of eight): a thread's units are `threads` units apart; else a
+// thread has every `threads`-th value, so that a warp's accesses stay whole.  Parameters wait in shared memory.
 
 struct Group {
-    int warps, index, warp, lane, thread;  // thread: of the group
-    int other;                             // the warp whose values this lane joins
-    float count;                           // how many values that warp has; 0: none to join
-    float of_first, of_warp, of_row;       // 1 / number of values of the warp's first lane, of the warp, of the row
-    float2 *slots;                         // [2][warps][rows], shared
+    int warps, index, warp, lane;
+    int thread, threads;              // of the group
+    int other;                        // the warp whose values this lane joins
+    float count;                      // how many values that warp has; 0: none to join
+    float of_first, of_warp, of_row;  // 1 / number of values of the warp's first lane, of the warp, of the row
+    float2 *slots;                    // [2][warps][rows], shared
     int parity = 0;
 
     // A barrier of this group's own.
     __device__ __forceinline__ void sync() const
     {
-        asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(warps * 32) : "memory");
+        asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(threads) : "memory");
     }
 };
 
-template <bool VEC> __device__ __forceinline__ int column(const Group &g, int j)
+// Value j of a thread of the group, and whether it belongs to the row.
+template <bool VEC> __device__ __forceinline__ int column(int threads, int thread, int j)
 {
-    return VEC ? g.thread * PER_THREAD + j : j * g.warps * 32 + g.thread;
+    return VEC ? ((j >> 3) * threads + thread) * 8 + (j & 7) : j * threads + thread;
 }
-// Which of the thread's values belong to the row.
-template <bool VEC> __device__ __forceinline__ unsigned valid_values(const Group &g, int cols)
+template <bool VEC, int U> __device__ __forceinline__ unsigned valid_values(int threads, int thread, int cols)
 {
     unsigned valid = 0u;
 #pragma unroll
-    for (int j = 0; j < PER_THREAD; ++j)
-        if (column<VEC>(g, j) < cols) valid |= 1u << j;
+    for (int j = 0; j < 8 * U; ++j)
+        if (column<VEC>(threads, thread, j) < cols) valid |= 1u << j;
     return valid;
 }
-constexpr unsigned ALL_VALID = (1u << PER_THREAD) - 1u;
-// Makes the others zero.
-__device__ __forceinline__ void keep_valid(unsigned valid, f32x2 *v)
+
+template <bool VEC, int U>
+__device__ __forceinline__ Group make_group(int warps, int cols, float2 *slots, int rows)
 {
-    if (valid == ALL_VALID) return;
+    Group g;
+    g.warps = warps;
+    g.threads = warps * 32;
+    g.lane = threadIdx.x & 31;
+    g.index = (int)(threadIdx.x >> 5) / warps;
+    g.warp = (int)(threadIdx.x >> 5) - g.index * warps;
+    g.thread = g.warp * 32 + g.lane;
+    g.slots = slots + 2 * g.index * warps * rows;
+    const auto values_of_warp = [&](int warp) {  // its 32 threads' runs of units, or of values
+        int n = 0;
 #pragma unroll
-    for (int i = 0; i < PER_THREAD / 2; ++i) {
-        const float2 w = values_of(v[i]);
-        v[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
-    }
+        for (int u = 0; u < (VEC ? U : 8 * U); ++u) {
+            constexpr int run = VEC ? 8 : 1;
+            n += min(max(cols - (u * g.threads + warp * 32) * run, 0), 32 * run);
+        }
+        return n;
+    };
+    const int joined = warps <= 8 ? g.lane & 7 : g.lane;
+    g.other = min(joined, warps - 1);
+    g.count = joined < warps ? (float)values_of_warp(joined) : 0.0f;
+    g.of_first = 1.0f / (float)__popc(valid_values<VEC, U>(g.threads, g.warp * 32, cols));
+    g.of_warp = 1.0f / (float)values_of_warp(g.warp);
+    g.of_row = 1.0f / (float)cols;
+    return g;
 }
 
 // A thread's values of a row as they are in memory.
-template <typename T> struct RowRaw {
-    unsigned w[PER_THREAD * sizeof(T) / 4];
+template <typename T, int U> struct RowRaw {
+    unsigned w[8 * U * sizeof(T) / 4];
 };
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_row(const T *row, const Group &g, unsigned valid, RowRaw<T> &raw)
+template <typename T, bool VEC, int U>
+__device__ __forceinline__ void load_row(const void *row, const Group &g, unsigned valid, RowRaw<T, U> &raw)
 {
     constexpr int UE = Unit<T>::UE;
     if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < PER_THREAD / UE; ++i) {
+        for (int i = 0; i < 8 * U / UE; ++i) {
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (valid >> (i * UE) & 1u) v = __ldcs(reinterpret_cast<const uint4 *>(row + g.thread * PER_THREAD) + i);
+            if (valid >> (i * UE) & 1u) v = __ldcs(static_cast<const uint4 *>(row) + column<true>(g.threads, g.thread, i * UE) / UE);
             raw.w[4 * i] = v.x; raw.w[4 * i + 1] = v.y; raw.w[4 * i + 2] = v.z; raw.w[4 * i + 3] = v.w;
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < PER_THREAD; ++j) {
+        for (int j = 0; j < 8 * U; ++j) {
             unsigned v = 0u;
             if (valid >> j & 1u) {
                 if constexpr (sizeof(T) == 2)
-                    v = __ldcs(reinterpret_cast<const unsigned short *>(row) + column<false>(g, j));
+                    v = __ldcs(static_cast<const unsigned short *>(row) + column<false>(g.threads, g.thread, j));
                 else
-                    v = __ldcs(reinterpret_cast<const unsigned *>(row) + column<false>(g, j));
+                    v = __ldcs(static_cast<const unsigned *>(row) + column<false>(g.threads, g.thread, j));
             }
             if (sizeof(T) == 4)
                 raw.w[j] = v;
@@ -233,92 +250,105 @@ __device__ __forceinline__ void load_row(const T *row, const Group &g, unsigned 
         }
     }
 }
-// Values that do not belong to the row are zero.
-template <typename T> __device__ __forceinline__ void widen_row(const RowRaw<T> &raw, unsigned valid, f32x2 *v)
+template <typename T, int U> __device__ __forceinline__ void widen_row(const RowRaw<T, U> &raw, f32x2 *v)
 {
     constexpr int UE = Unit<T>::UE;
 #pragma unroll
-    for (int i = 0; i < PER_THREAD / UE; ++i)
+    for (int i = 0; i < 8 * U / UE; ++i)
         widen_pairs<T>(make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]), v + i * UE / 2);
-    keep_valid(valid, v);
 }
-template <typename T> __device__ __forceinline__ void narrow_row(const f32x2 *v, RowRaw<T> &raw)
+template <typename T, int U> __device__ __forceinline__ void narrow_row(const f32x2 *v, RowRaw<T, U> &raw)
 {
     constexpr int UE = Unit<T>::UE;
 #pragma unroll
-    for (int i = 0; i < PER_THREAD / UE; ++i) {
+    for (int i = 0; i < 8 * U / UE; ++i) {
         const uint4 u = narrow_pairs<T>(v + i * UE / 2);
         raw.w[4 * i] = u.x; raw.w[4 * i + 1] = u.y; raw.w[4 * i + 2] = u.z; raw.w[4 * i + 3] = u.w;
     }
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_row(T *row, const Group &g, unsigned valid, const RowRaw<T> &raw)
+template <typename T, bool VEC, int U>
+__device__ __forceinline__ void store_row(void *row, const Group &g, unsigned valid, const RowRaw<T, U> &raw)
 {
     constexpr int UE = Unit<T>::UE;
     if constexpr (VEC) {
-        if (valid == ALL_VALID) {
 #pragma unroll
-            for (int i = 0; i < PER_THREAD / UE; ++i)
-                reinterpret_cast<uint4 *>(row + g.thread * PER_THREAD)[i] =
+        for (int i = 0; i < 8 * U / UE; ++i)
+            if (valid >> (i * UE) & 1u)
+                static_cast<uint4 *>(row)[column<true>(g.threads, g.thread, i * UE) / UE] =
                     make_uint4(raw.w[4 * i], raw.w[4 * i + 1], raw.w[4 * i + 2], raw.w[4 * i + 3]);
-            return;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < PER_THREAD; ++j)
-        if (valid >> j & 1u) {
-            if constexpr (sizeof(T) == 2)
-                reinterpret_cast<unsigned short *>(row)[column<VEC>(g, j)] = (unsigned short)(raw.w[j / 2] >> 16 * (j & 1));
-            else
-                reinterpret_cast<unsigned *>(row)[column<VEC>(g, j)] = raw.w[j];
-        }
-}
-// Parameters of the thread's columns.
-template <bool VEC>
-__device__ __forceinline__ void load_columns(const void *p, bool bf16, const Group &g, int cols, float otherwise, f32x2 *v)
-{
-    if (!p) {
-#pragma unroll
-        for (int i = 0; i < PER_THREAD / 2; ++i) v[i] = pair_of(otherwise);
-    } else if (VEC) {
-        param_pairs<PER_THREAD>(p, bf16, reinterpret_cast<uintptr_t>(p) % 16 == 0, g.thread * PER_THREAD, cols, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < PER_THREAD / 2; ++i) {
-            const int c0 = column<VEC>(g, 2 * i), c1 = column<VEC>(g, 2 * i + 1);
-            v[i] = pair_of(c0 < cols ? load_param(p, bf16, c0) : 0.0f, c1 < cols ? load_param(p, bf16, c1) : 0.0f);
-        }
+        for (int j = 0; j < 8 * U; ++j)
+            if (valid >> j & 1u) {
+                if constexpr (sizeof(T) == 2)
+                    static_cast<unsigned short *>(row)[column<false>(g.threads, g.thread, j)] = (unsigned short)(raw.w[j / 2] >> 16 * (j & 1));
+                else
+                    static_cast<unsigned *>(row)[column<false>(g.threads, g.thread, j)] = raw.w[j];
+            }
     }
 }
 
-__device__ __forceinline__ float sum_pairs(const f32x2 *v)
+// A vector of parameters in shared memory, as the threads read it: in VEC form the first and the last four of every
+// unit apart, so that a warp's loads do not conflict.
+template <bool VEC> __device__ __forceinline__ int param_place(int col, int cols)
 {
-    return sum_of(add2(add2(v[0], v[1]), add2(v[2], v[3])));
+    return VEC ? ((col >> 2 & 1) * (cols >> 3) + (col >> 3)) * 4 + (col & 3) : col;
+}
+template <bool VEC, int U>
+__device__ __forceinline__ void held_columns(const float *held, const Group &g, unsigned valid, int cols, int unit, f32x2 *v)
+{
+    if constexpr (VEC) {
+        const int at = min(unit * g.threads + g.thread, (cols >> 3) - 1);  // any that is there, where there is no value
+        const float4 *p = reinterpret_cast<const float4 *>(held);
+        const float4 lo = p[at], hi = p[(cols >> 3) + at];
+        v[0] = pair_of(lo.x, lo.y); v[1] = pair_of(lo.z, lo.w);
+        v[2] = pair_of(hi.x, hi.y); v[3] = pair_of(hi.z, hi.w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = pair_of(held[min(column<false>(g.threads, g.thread, 8 * unit + 2 * i), cols - 1)],
+                           held[min(column<false>(g.threads, g.thread, 8 * unit + 2 * i + 1), cols - 1)]);
+    }
 }
 
-// Sums of pairs of values over the group, R at a time, on every thread: over warps in shared memory, in two sets that
-// take turns, so that a set is written again only after everyone has read it.  Up to eight warps are joined in three
-// steps by every eight lanes, more in five.
+// What a unit adds to a sum: nothing from values that are not the row's.
+template <bool VEC> __device__ __forceinline__ void keep_valid(unsigned valid, int unit, f32x2 *v)  // before the sum
+{
+    if constexpr (!VEC) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 w = values_of(v[i]);
+            v[i] = pair_of(valid >> (8 * unit + 2 * i) & 1u ? w.x : 0.0f, valid >> (8 * unit + 2 * i + 1) & 1u ? w.y : 0.0f);
+        }
+    }
+}
+template <bool VEC> __device__ __forceinline__ f32x2 if_valid(unsigned valid, int unit, f32x2 sum)  // after it
+{
+    return !VEC || (valid >> (8 * unit) & 1u) ? sum : 0ull;
+}
+__device__ __forceinline__ f32x2 sum4(const f32x2 *v) { return add2(add2(v[0], v[1]), add2(v[2], v[3])); }
+
+// Sums of R pairs of values over the warp.
+template <int R, int FROM = 16> __device__ __forceinline__ void warp_sums(float2 *sums)
+{
+#pragma unroll
+    for (int o = FROM; o > 0; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sums[r].x += __shfl_xor_sync(0xffffffffu, sums[r].x, o);
+            sums[r].y += __shfl_xor_sync(0xffffffffu, sums[r].y, o);
+        }
+}
+// The same of what lanes have of the warps: of up to eight by every eight lanes.
 template <int R> __device__ __forceinline__ void join_warps(const Group &g, float2 *sums)
 {
-    for (int o = g.warps <= 8 ? 4 : 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            sums[r].x += __shfl_xor_sync(0xffffffffu, sums[r].x, o);
-            sums[r].y += __shfl_xor_sync(0xffffffffu, sums[r].y, o);
-        }
+    if (g.warps <= 8)
+        warp_sums<R, 4>(sums);
+    else
+        warp_sums<R>(sums);
 }
-template <int R> __device__ __forceinline__ void warp_sums(float2 *sums)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            sums[r].x += __shfl_xor_sync(0xffffffffu, sums[r].x, o);
-            sums[r].y += __shfl_xor_sync(0xffffffffu, sums[r].y, o);
-        }
-}
-// Hands the warps' values round: [warp][row].
+// Hands the warps' values round, [warp][R], in two sets that take turns: a set is written again only after everyone
+// has read it.
 template <int R> __device__ __forceinline__ const float2 *exchange(Group &g, const float2 *own)
 {
     float2 *slots = g.slots + g.parity * g.warps * R;
@@ -331,205 +361,139 @@ template <int R> __device__ __forceinline__ const float2 *exchange(Group &g, con
     return slots;
 }
 
-// Mean and 1 / sqrt(var + eps) of the group's R rows.  Differences are taken from the mean of the warp's first lane's
-// values: it is exact where all values are equal, and no farther from the warp's mean than the spread of its 256
+// Mean and 1 / sqrt(var + eps) of the group's row.  Differences are taken from the mean of the warp's first lane's
+// values: it is exact where all values are equal, and no farther from the warp's mean than the spread of the warp's
 // values times sqrt(32), so that the squares lose five bits at most.  The warps are joined about the first one's mean.
-template <int R, bool VEC>
-__device__ __forceinline__ void group_statistics(Group &g, const f32x2 (*v)[PER_THREAD / 2], unsigned valid, float eps, float2 *found)
+template <bool VEC, int U>
+__device__ __forceinline__ float2 group_statistics(Group &g, const f32x2 *v, unsigned valid, float eps)
 {
-    float2 sums[R];
-    float centre[R];
+    f32x2 first = sum4(v);
 #pragma unroll
-    for (int r = 0; r < R; ++r) centre[r] = __shfl_sync(0xffffffffu, sum_pairs(v[r]) * g.of_first, 0);
+    for (int u = 1; u < U; ++u) first = add2(first, sum4(v + 4 * u));
+    const float centre = __shfl_sync(0xffffffffu, sum_of(first) * g.of_first, 0);
+    f32x2 all = 0ull, squares = 0ull;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        f32x2 d[PER_THREAD / 2], squares = 0ull;
+    for (int u = 0; u < U; ++u) {
+        f32x2 d[4];
 #pragma unroll
-        for (int i = 0; i < PER_THREAD / 2; ++i) d[i] = add2(v[r][i], pair_of(-centre[r]));
-        keep_valid(valid, d);
+        for (int i = 0; i < 4; ++i) d[i] = add2(v[4 * u + i], pair_of(-centre));
+        keep_valid<VEC>(valid, u, d);
+        f32x2 s = mul2(d[0], d[0]);
 #pragma unroll
-        for (int i = 0; i < PER_THREAD / 2; ++i) squares = fma2(d[i], d[i], squares);
-        sums[r] = make_float2(sum_pairs(d), sum_of(squares));
+        for (int i = 1; i < 4; ++i) s = fma2(d[i], d[i], s);
+        all = add2(all, if_valid<VEC>(valid, u, sum4(d)));
+        squares = add2(squares, if_valid<VEC>(valid, u, s));
     }
-    warp_sums<R>(sums);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const float off = sums[r].x * g.of_warp;
-        sums[r] = make_float2(centre[r] + off, fmaxf(fmaf(-off, sums[r].x, sums[r].y), 0.0f));
-    }
+    float2 sums = make_float2(sum_of(all), sum_of(squares));
+    warp_sums<1>(&sums);
+    float off = sums.x * g.of_warp;
+    sums = make_float2(centre + off, fmaxf(fmaf(-off, sums.x, sums.y), 0.0f));
     if (g.warps > 1) {
-        const float2 *slots = exchange<R>(g, sums);
-        float first[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            first[r] = slots[r].x;
-            const float2 of = slots[g.other * R + r];
-            const float apart = of.x - first[r];
-            sums[r] = g.count > 0.0f ? make_float2(g.count * apart, fmaf(g.count * apart, apart, of.y)) : make_float2(0.0f, 0.0f);
-        }
-        join_warps<R>(g, sums);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float off = sums[r].x * g.of_row;
-            sums[r] = make_float2(first[r] + off, fmaxf(fmaf(-off, sums[r].x, sums[r].y), 0.0f));
-        }
+        const float2 *slots = exchange<1>(g, &sums);
+        const float about = slots[0].x;
+        const float2 of = slots[g.other];
+        const float apart = of.x - about;
+        sums = g.count > 0.0f ? make_float2(g.count * apart, fmaf(g.count * apart, apart, of.y)) : make_float2(0.0f, 0.0f);
+        join_warps<1>(g, &sums);
+        off = sums.x * g.of_row;
+        sums = make_float2(about + off, fmaxf(fmaf(-off, sums.x, sums.y), 0.0f));
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r) found[r] = make_float2(sums[r].x, rsqrtf(fmaf(sums[r].y, g.of_row, eps)));
-}
-
-// How many values a warp of the group has, and its first lane.
-template <bool VEC> __device__ __forceinline__ int values_of_warp(int warps, int warp, int cols)
-{
-    if (VEC) return min(max(cols - warp * 32 * PER_THREAD, 0), 32 * PER_THREAD);
-    int n = 0;
-#pragma unroll
-    for (int j = 0; j < PER_THREAD; ++j) n += min(max(cols - (j * warps + warp) * 32, 0), 32);
-    return n;
-}
-template <bool VEC> __device__ __forceinline__ int values_of_first_lane(int warps, int warp, int cols)
-{
-    if (VEC) return min(max(cols - warp * 32 * PER_THREAD, 0), PER_THREAD);
-    int n = 0;
-#pragma unroll
-    for (int j = 0; j < PER_THREAD; ++j) n += (j * warps + warp) * 32 < cols;
-    return n;
-}
-
-// A group of the block, with `slots` of 2 * rows float2 for each of the block's warps.
-template <bool VEC> __device__ __forceinline__ Group make_group(int warps, int cols, float2 *slots, int rows)
-{
-    Group g;
-    g.warps = warps;
-    g.lane = threadIdx.x & 31;
-    g.index = (int)(threadIdx.x >> 5) / warps;
-    g.warp = (int)(threadIdx.x >> 5) - g.index * warps;
-    g.thread = g.warp * 32 + g.lane;
-    g.slots = slots + 2 * g.index * warps * rows;
-    const int joined = warps <= 8 ? g.lane & 7 : g.lane;
-    g.other = min(joined, warps - 1);
-    g.count = joined < warps ? (float)values_of_warp<VEC>(warps, joined, cols) : 0.0f;
-    g.of_first = 1.0f / (float)values_of_first_lane<VEC>(warps, g.warp, cols);
-    g.of_warp = 1.0f / (float)values_of_warp<VEC>(warps, g.warp, cols);
-    g.of_row = 1.0f / (float)cols;
-    return g;
+    return make_float2(sums.x, rsqrtf(fmaf(sums.y, g.of_row, eps)));
 }
 
 // GATE: what a thread needs for it.
 enum : int { GATE_IN_COLUMNS, GATE_OF_ROW, GATE_OF_VALUES };
 
-constexpr int MAX_GROUP_COLS = 32 * 32 * PER_THREAD;
+constexpr int MAX_GROUP_COLS = 8192;  // 128 KB of parameters in shared memory
 
-// HOLD: blocks of up to 16 warps; R rows at a time.
-template <typename T, bool VEC, int GATE, bool HOLD, int R>
-__global__ void __launch_bounds__(HOLD ? 512 : 1024, 1)
-    group_rows_kernel(const __grid_constant__ NormArgs a, int warps)
+// How many units of eight values a thread has: few for narrow rows, as many as the registers allow for wide ones.
+template <typename T> constexpr int ROW_UNITS = sizeof(T) == 2 ? 4 : 2;
+
+template <typename T, bool VEC, int GATE, int U>
+__global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constant__ NormArgs a, int warps)
 {
-    __shared__ float2 slots[2 * 32 * R];
-    Group g = make_group<VEC>(warps, a.cols, slots, R);
+    constexpr int P = 4 * U;
+    extern __shared__ __align__(16) float held[];  // [4][cols]: p = h factor + shift, a gate of columns in both; gamma, beta
+    __shared__ float2 slots[2 * 16];
+    Group g = make_group<VEC, U>(warps, a.cols, slots, 1);
     const int groups = (int)(blockDim.x >> 5) / warps;
-    const unsigned valid = valid_values<VEC>(g, a.cols);
-    // p = h factor + shift, a gate of columns in both
-    f32x2 factor[PER_THREAD / 2], shift[PER_THREAD / 2], gamma[PER_THREAD / 2], beta[PER_THREAD / 2];
-    const auto load_block_columns = [&] {
-        load_columns<VEC>(a.post_gamma, a.params_bf16, g, a.cols, 1.0f, factor);
-        load_columns<VEC>(a.post_beta, a.params_bf16, g, a.cols, 0.0f, shift);
-        if (GATE == GATE_IN_COLUMNS && a.gate_kind == DIPACO_GATE_COLS) {
-            f32x2 gate[PER_THREAD / 2];
-            load_columns<VEC>(a.gate, a.gate_bf16, g, a.cols, 1.0f, gate);
-#pragma unroll
-            for (int i = 0; i < PER_THREAD / 2; ++i) {
-                factor[i] = mul2(factor[i], gate[i]);
-                shift[i] = mul2(shift[i], gate[i]);
-            }
-        }
-    };
-    const auto load_next_columns = [&] {
-        load_columns<VEC>(a.gamma, a.params_bf16, g, a.cols, 1.0f, gamma);
-        load_columns<VEC>(a.beta, a.params_bf16, g, a.cols, 0.0f, beta);
-    };
-    const long long between = (long long)gridDim.x * groups, step = between * R;  // the R rows are `between` apart
-    long long row = (long long)blockIdx.x * groups + g.index;
-    RowRaw<T> next_x[R], next_f[R];
-    const auto load_next = [&](long long first) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const long long at = min(first + r * between, (long long)a.rows - 1);  // the last row again where there is none
-            load_row<T, VEC>(static_cast<const T *>(a.f.dense) + at * a.f.stride, g, valid, next_f[r]);
-            load_row<T, VEC>(static_cast<const T *>(a.x.dense) + at * a.x.stride, g, valid, next_x[r]);
-        }
-    };
-    if (row < a.rows) load_next(row);
-    if (HOLD) {
-        load_block_columns();
-        if (a.n) load_next_columns();
+    const unsigned valid = valid_values<VEC, U>(g.threads, g.thread, a.cols);
+    const int row_step = gridDim.x * groups;
+    int row = blockIdx.x * groups + g.index;
+    const T *f_row = static_cast<const T *>(a.f.dense) + row * a.f.stride, *x_row = static_cast<const T *>(a.x.dense) + row * a.x.stride;
+    const long long f_step = row_step * a.f.stride, x_step = row_step * a.x.stride;
+    RowRaw<T, U> next_x, next_f;
+    if (row < a.rows) {
+        load_row<T, VEC, U>(f_row, g, valid, next_f);
+        load_row<T, VEC, U>(x_row, g, valid, next_x);
     }
-    for (; row < a.rows; row += step) {
-        f32x2 v[R][PER_THREAD / 2];
-        RowRaw<T> x[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            widen_row<T>(next_f[r], valid, v[r]);
-            x[r] = next_x[r];
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+        const float gate = a.gate_kind == DIPACO_GATE_COLS ? load_param(a.gate, a.gate_bf16, c) : 1.0f;
+        const int at = param_place<VEC>(c, a.cols);
+        held[at] = gate * param_or(a.post_gamma, a.params_bf16, c, 1.0f);
+        held[a.cols + at] = gate * param_or(a.post_beta, a.params_bf16, c, 0.0f);
+        held[2 * a.cols + at] = param_or(a.gamma, a.params_bf16, c, 1.0f);
+        held[3 * a.cols + at] = param_or(a.beta, a.params_bf16, c, 0.0f);
+    }
+    __syncthreads();
+    for (; row < a.rows; row += row_step) {
+        f32x2 v[P];
+        widen_row<T, U>(next_f, v);
+        const RowRaw<T, U> x = next_x;
+        if (row < a.rows - row_step) {
+            f_row += f_step;
+            x_row += x_step;
+            load_row<T, VEC, U>(f_row, g, valid, next_f);
+            load_row<T, VEC, U>(x_row, g, valid, next_x);
         }
-        if (row + step < a.rows) load_next(row + step);
-        float2 of_f[R], of_z[R];
+        float2 of_f = make_float2(0.0f, 1.0f), of_z = make_float2(0.0f, 1.0f);
+        if (a.post_norm) of_f = group_statistics<VEC, U>(g, v, valid, a.eps);
+        RowRaw<T, U> raw;
+        if (GATE == GATE_OF_VALUES) load_row<T, VEC, U>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);
+        const f32x2 of_row = pair_of(GATE == GATE_OF_ROW ? load_param(a.gate, a.gate_bf16, row) : 0.0f);
+        f32x2 stream[P], gate[P];
+        widen_row<T, U>(x, stream);
+        if (GATE == GATE_OF_VALUES) widen_row<T, U>(raw, gate);
 #pragma unroll
-        for (int r = 0; r < R; ++r) of_f[r] = of_z[r] = make_float2(0.0f, 1.0f);
-        if (a.post_norm) group_statistics<R, VEC>(g, v, valid, a.eps, of_f);
-        if (!HOLD) load_block_columns();
+        for (int u = 0; u < U; ++u) {
+            f32x2 factor[4], shift[4];
+            held_columns<VEC, U>(held, g, valid, a.cols, u, factor);
+            held_columns<VEC, U>(held + a.cols, g, valid, a.cols, u, shift);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const long long at = row + r * between;
-            if (R > 1 && at >= a.rows) break;
-            f32x2 gate[PER_THREAD / 2], stream[PER_THREAD / 2];
-            if (GATE == GATE_OF_ROW) {
-                const float of_row = load_param(a.gate, a.gate_bf16, at);
-#pragma unroll
-                for (int i = 0; i < PER_THREAD / 2; ++i) gate[i] = pair_of(of_row);
-            } else if (GATE == GATE_OF_VALUES) {
-                RowRaw<T> raw;
-                load_row<T, VEC>(static_cast<const T *>(a.gate) + at * a.gate_stride, g, valid, raw);
-                widen_row<T>(raw, valid, gate);
+            for (int i = 0; i < 4; ++i) {
+                const int k = 4 * u + i;
+                const f32x2 p = fma2(mul2(add2(v[k], pair_of(-of_f.x)), pair_of(of_f.y)), factor[i], shift[i]);
+                if (GATE == GATE_IN_COLUMNS)
+                    v[k] = fma2(stream[k], pair_of(a.scale), p);
+                else
+                    v[k] = fma2(GATE == GATE_OF_ROW ? of_row : gate[k], p, mul2(stream[k], pair_of(a.scale)));
             }
-            widen_row<T>(x[r], valid, stream);
-#pragma unroll
-            for (int i = 0; i < PER_THREAD / 2; ++i) {
-                const f32x2 scaled = mul2(stream[i], pair_of(a.scale));
-                const f32x2 p = fma2(mul2(add2(v[r][i], pair_of(-of_f[r].x)), pair_of(of_f[r].y)), factor[i], shift[i]);
-                v[r][i] = GATE == GATE_IN_COLUMNS ? add2(p, scaled) : fma2(gate[i], p, scaled);
-            }
-            RowRaw<T> raw;
-            narrow_row<T>(v[r], raw);
-            store_row<T, VEC>(static_cast<T *>(a.z_out) + at * a.z_stride, g, valid, raw);
-            widen_row<T>(raw, valid, v[r]);
+            keep_valid<VEC>(valid, u, v + 4 * u);
         }
+        narrow_row<T, U>(v, raw);
+        store_row<T, VEC, U>(static_cast<T *>(a.z_out) + row * a.z_stride, g, valid, raw);
         if (a.norm) {
-            group_statistics<R, VEC>(g, v, valid, a.eps, of_z);
+            widen_row<T, U>(raw, v);
+            of_z = group_statistics<VEC, U>(g, v, valid, a.eps);
             if (a.n) {
-                if (!HOLD) load_next_columns();
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const long long at = row + r * between;
-                    if (R > 1 && at >= a.rows) break;
+                for (int u = 0; u < U; ++u) {
+                    f32x2 gamma[4], beta[4];
+                    held_columns<VEC, U>(held + 2 * a.cols, g, valid, a.cols, u, gamma);
+                    held_columns<VEC, U>(held + 3 * a.cols, g, valid, a.cols, u, beta);
 #pragma unroll
-                    for (int i = 0; i < PER_THREAD / 2; ++i)
-                        v[r][i] = fma2(mul2(add2(v[r][i], pair_of(-of_z[r].x)), pair_of(of_z[r].y)), gamma[i], beta[i]);
-                    RowRaw<T> raw;
-                    narrow_row<T>(v[r], raw);
-                    store_row<T, VEC>(static_cast<T *>(a.n) + at * a.n_stride, g, valid, raw);
+                    for (int i = 0; i < 4; ++i)
+                        v[4 * u + i] = fma2(mul2(add2(v[4 * u + i], pair_of(-of_z.x)), pair_of(of_z.y)), gamma[i], beta[i]);
                 }
+                narrow_row<T, U>(v, raw);
+                store_row<T, VEC, U>(static_cast<T *>(a.n) + row * a.n_stride, g, valid, raw);
             }
         }
-        if (g.thread < R) {
-            const long long at = row + g.thread * between;
-            const float2 f = R > 1 && g.thread ? of_f[R - 1] : of_f[0], z = R > 1 && g.thread ? of_z[R - 1] : of_z[0];
-            if (at < a.rows) {
-                a.stats[at] = f.x;
-                a.stats[a.rows + at] = f.y;
-                a.stats[2ll * a.rows + at] = z.x;
-                a.stats[3ll * a.rows + at] = z.y;
-            }
+        if (g.thread == 0) {
+            a.stats[row] = of_f.x;
+            a.stats[a.rows + row] = of_f.y;
+            a.stats[2ll * a.rows + row] = of_z.x;
+            a.stats[3ll * a.rows + row] = of_z.y;
         }
     }
 }
@@ -625,50 +589,64 @@ template <typename T> __global__ void __launch_bounds__(ROW_THREADS) back_rows_k
     }
 }
 
-// A row of f or z: as load_row, or eight codes.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load_source(const Source &s, long long row, const Group &g, unsigned valid, RowRaw<T> &raw)
+// A row of f or z: as load_row, or codes.
+template <typename T, bool VEC, int U>
+__device__ __forceinline__ void load_source(const Source &s, const void *row, const Group &g, unsigned valid, RowRaw<T, U> &raw)
 {
     if (s.dense) {
-        load_row<T, VEC>(static_cast<const T *>(s.dense) + row * s.stride, g, valid, raw);
+        load_row<T, VEC, U>(row, g, valid, raw);
         return;
     }
-    const uint8_t *codes = s.codes + row * s.stride;
-    raw.w[0] = raw.w[1] = 0u;
-    if constexpr (VEC) {
-        if (valid) {  // rows of codes are padded to 16 bytes
-            const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(codes) + g.thread);
-            raw.w[0] = v.x;
-            raw.w[1] = v.y;
-        }
-    } else {
+    const uint8_t *codes = static_cast<const uint8_t *>(row);
 #pragma unroll
-        for (int j = 0; j < PER_THREAD; ++j)
-            if (valid >> j & 1u) raw.w[j / 4] |= (unsigned)__ldcs(codes + column<false>(g, j)) << 8 * (j % 4);
+    for (int u = 0; u < U; ++u) {
+        raw.w[2 * u] = raw.w[2 * u + 1] = 0u;
+        if constexpr (VEC) {
+            if (valid >> (8 * u) & 1u) {
+                const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(codes) + u * g.threads + g.thread);
+                raw.w[2 * u] = v.x;
+                raw.w[2 * u + 1] = v.y;
+            }
+        } else {
+#pragma unroll
+            for (int j = 8 * u; j < 8 * u + 8; ++j)
+                if (valid >> j & 1u) raw.w[j / 4] |= (unsigned)__ldcs(codes + column<false>(g.threads, g.thread, j)) << 8 * (j % 4);
+        }
     }
 }
-// Their values (zero outside the row).
-template <typename T, bool VEC>
-__device__ __forceinline__ void widen_source(const Source &s, long long row, const Group &g, unsigned valid, const RowRaw<T> &raw, f32x2 *v)
+// Their values.
+template <typename T, bool VEC, int U>
+__device__ __forceinline__ void widen_source(const Source &s, int row, const Group &g, unsigned valid, const RowRaw<T, U> &raw, f32x2 *v)
 {
     if (s.dense) {
-        widen_row<T>(raw, valid, v);
+        widen_row<T, U>(raw, v);
         return;
     }
-    const uint8_t *scales = s.scales + row / PACK_BLOCK * s.scale_cols;
-    const f32x2 one = VEC && valid ? pair_of(scale_value(scales[g.thread * PER_THREAD / PACK_BLOCK])) : 0ull;
+    const uint8_t *scales = s.scales + (long long)(row / PACK_BLOCK) * s.scale_cols;
+    const auto scale_of = [&](int j) {
+        return valid >> j & 1u ? scale_value(scales[column<VEC>(g.threads, g.thread, j) / PACK_BLOCK]) : 0.0f;
+    };
 #pragma unroll
-    for (int i = 0; i < PER_THREAD / 2; ++i) {
-        f32x2 scale = one;
-        if (!VEC)
-            scale = pair_of(valid >> (2 * i) & 1u ? scale_value(scales[column<VEC>(g, 2 * i) / PACK_BLOCK]) : 0.0f,
-                            valid >> (2 * i + 1) & 1u ? scale_value(scales[column<VEC>(g, 2 * i + 1) / PACK_BLOCK]) : 0.0f);
-        v[i] = mul2(decode_pair(raw.w[i / 2] >> 16 * (i & 1)), scale);
+    for (int u = 0; u < U; ++u) {
+        const f32x2 one = pair_of(VEC ? scale_of(8 * u) : 0.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 scale = VEC ? one : pair_of(scale_of(8 * u + 2 * i), scale_of(8 * u + 2 * i + 1));
+            v[4 * u + i] = mul2(decode_pair(raw.w[2 * u + i / 2] >> 16 * (i & 1)), scale);
+        }
     }
-    keep_valid(valid, v);
+}
+// The start of a row of codes or values of T, and the bytes from row to row.
+template <typename T> __device__ __forceinline__ const uint8_t *source_row(const Source &s, long long row)
+{
+    return s.codes ? s.codes + row * s.stride : static_cast<const uint8_t *>(s.dense) + row * s.stride * (long long)sizeof(T);
+}
+template <typename T> __device__ __forceinline__ long long source_step(const Source &s, long long rows)
+{
+    return rows * s.stride * (s.codes ? 1 : (long long)sizeof(T));
 }
 
-// Sums of pairs over the group, on every thread.
+// Sums of R pairs over the group, on every thread.
 template <int R> __device__ __forceinline__ void group_sums(Group &g, float2 *sums)
 {
     warp_sums<R>(sums);
@@ -679,122 +657,141 @@ template <int R> __device__ __forceinline__ void group_sums(Group &g, float2 *su
     join_warps<R>(g, sums);
 }
 
-constexpr int MAX_BACK_COLS = 16 * 32 * PER_THREAD;
+constexpr int MAX_BACK_COLS = 8192;
 
 // A persistent block of groups, each with a row at a time; a thread keeps the sums over its rows of its columns.  The
 // next row's values are loaded where this row's have been used for the last time.
-template <typename T, bool VEC, int GATE>
-__global__ void __launch_bounds__(512, 1) group_back_kernel(const __grid_constant__ NormArgs a, int warps)
+template <typename T, bool VEC, int GATE, int U, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_constant__ NormArgs a, int warps)
 {
-    constexpr int P = PER_THREAD / 2;
+    constexpr int P = 4 * U;
+    extern __shared__ __align__(16) float held[];  // [3][cols]: gamma; post_gamma, times a gate of columns; post_beta
     __shared__ float2 slots[2 * 16 * 2];
-    __shared__ float joined[MAX_BACK_COLS];
-    Group g = make_group<VEC>(warps, a.cols, slots, 2);
+    Group g = make_group<VEC, U>(warps, a.cols, slots, 2);
     const int groups = (int)(blockDim.x >> 5) / warps;
-    const unsigned valid = valid_values<VEC>(g, a.cols);
-    const long long step = (long long)gridDim.x * groups;
-    long long row = (long long)blockIdx.x * groups + g.index;
-    RowRaw<T> dn = {}, dz = {}, z = {}, f = {};
-    const auto load_z = [&](long long at) {
+    const unsigned valid = valid_values<VEC, U>(g.threads, g.thread, a.cols);
+    const int row_step = gridDim.x * groups;
+    int row = blockIdx.x * groups + g.index;
+    const uint8_t *dn_row = source_row<T>(a.dn, row), *dz_row = source_row<T>(a.dz, row), *z_row = source_row<T>(a.z, row),
+                  *f_row = source_row<T>(a.f, row);
+    RowRaw<T, U> dn = {}, dz = {}, z = {}, f = {};
+    const auto load_z = [&] {
         if (a.norm) {
-            load_row<T, VEC>(static_cast<const T *>(a.dn.dense) + at * a.dn.stride, g, valid, dn);
-            load_source<T, VEC>(a.z, at, g, valid, z);
+            load_row<T, VEC, U>(dn_row, g, valid, dn);
+            load_source<T, VEC, U>(a.z, z_row, g, valid, z);
         }
-        if (a.dz.dense) load_row<T, VEC>(static_cast<const T *>(a.dz.dense) + at * a.dz.stride, g, valid, dz);
+        if (a.dz.dense) load_row<T, VEC, U>(dz_row, g, valid, dz);
     };
     if (row < a.rows) {
-        load_z(row);
-        load_source<T, VEC>(a.f, row, g, valid, f);
+        load_z();
+        load_source<T, VEC, U>(a.f, f_row, g, valid, f);
     }
-    f32x2 gamma[P], factor[P], shift[P];  // factor: post_gamma, times a gate of columns
-    load_columns<VEC>(a.gamma, a.params_bf16, g, a.cols, 1.0f, gamma);
-    load_columns<VEC>(a.post_gamma, a.params_bf16, g, a.cols, 1.0f, factor);
-    if (GATE == GATE_IN_COLUMNS) {
-        if (a.gate_kind == DIPACO_GATE_COLS) {
-            f32x2 gate[P];
-            load_columns<VEC>(a.gate, a.gate_bf16, g, a.cols, 1.0f, gate);
-#pragma unroll
-            for (int i = 0; i < P; ++i) factor[i] = mul2(factor[i], gate[i]);
-        }
-    } else {
-        load_columns<VEC>(a.post_beta, a.params_bf16, g, a.cols, 0.0f, shift);
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+        const float gate = a.gate_kind == DIPACO_GATE_COLS ? load_param(a.gate, a.gate_bf16, c) : 1.0f;
+        const int at = param_place<VEC>(c, a.cols);
+        held[at] = param_or(a.gamma, a.params_bf16, c, 1.0f);
+        held[a.cols + at] = gate * param_or(a.post_gamma, a.params_bf16, c, 1.0f);
+        held[2 * a.cols + at] = param_or(a.post_beta, a.params_bf16, c, 0.0f);
     }
+    __syncthreads();
     f32x2 sums[4][P];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
         for (int i = 0; i < P; ++i) sums[q][i] = 0ull;
 
-    for (; row < a.rows; row += step) {
-        const bool more = row + step < a.rows;
+    for (; row < a.rows; row += row_step) {
+        const bool more = row < a.rows - row_step;
         f32x2 d[P], h[P];
-        widen_row<T>(dz, valid, d);
+        widen_row<T, U>(dz, d);
         if (a.norm) {
             const float mean = a.saved[2ll * a.rows + row], rstd = a.saved[3ll * a.rows + row];
-            f32x2 u[P];
-            widen_row<T>(dn, valid, u);
-            widen_source<T, VEC>(a.z, row, g, valid, z, h);
-            f32x2 all[2] = {0ull, 0ull};
+            f32x2 y[P], all[2] = {0ull, 0ull};
+            widen_row<T, U>(dn, y);
+            widen_source<T, VEC, U>(a.z, row, g, valid, z, h);
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
-                h[i] = mul2(add2(h[i], pair_of(-mean)), pair_of(rstd));
-                sums[0][i] = fma2(u[i], h[i], sums[0][i]);
-                sums[1][i] = add2(sums[1][i], u[i]);
-                u[i] = mul2(u[i], gamma[i]);
-                all[0] = add2(all[0], u[i]);
-                all[1] = fma2(u[i], h[i], all[1]);
+            for (int u = 0; u < U; ++u) {
+                f32x2 gamma[4];
+                held_columns<VEC, U>(held, g, valid, a.cols, u, gamma);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {  // dn is zero outside the row
+                    const int k = 4 * u + i;
+                    h[k] = mul2(add2(h[k], pair_of(-mean)), pair_of(rstd));
+                    sums[0][k] = fma2(y[k], h[k], sums[0][k]);
+                    sums[1][k] = add2(sums[1][k], y[k]);
+                    y[k] = mul2(y[k], gamma[i]);
+                    all[0] = add2(all[0], y[k]);
+                    all[1] = fma2(y[k], h[k], all[1]);
+                }
             }
-            float2 of[1] = {make_float2(sum_of(all[0]), sum_of(all[1]))};
-            group_sums<1>(g, of);
-            const f32x2 mean_u = pair_of(-of[0].x * g.of_row), mean_uh = pair_of(-of[0].y * g.of_row);
+            float2 of = make_float2(sum_of(all[0]), sum_of(all[1]));
+            group_sums<1>(g, &of);
+            const f32x2 mean_u = pair_of(-of.x * g.of_row), mean_uh = pair_of(-of.y * g.of_row);
 #pragma unroll
-            for (int i = 0; i < P; ++i) d[i] = fma2(fma2(h[i], mean_uh, add2(u[i], mean_u)), pair_of(rstd), d[i]);
-            keep_valid(valid, d);
+            for (int k = 0; k < P; ++k) d[k] = fma2(fma2(h[k], mean_uh, add2(y[k], mean_u)), pair_of(rstd), d[k]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                keep_valid<VEC>(valid, u, d + 4 * u);
+                if (VEC) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[4 * u + i] = if_valid<VEC>(valid, u, d[4 * u + i]);
+                }
+            }
         }
-        if (more) load_z(row + step);
-        f32x2 out[P];
-        RowRaw<T> raw;
+        if (more) {
+            dn_row += source_step<T>(a.dn, row_step);
+            dz_row += source_step<T>(a.dz, row_step);
+            z_row += source_step<T>(a.z, row_step);
+            load_z();
+        }
+        RowRaw<T, U> raw;
         if (a.dx) {
+            f32x2 out[P];
 #pragma unroll
-            for (int i = 0; i < P; ++i) out[i] = mul2(d[i], pair_of(a.scale));
-            narrow_row<T>(out, raw);
-            store_row<T, VEC>(static_cast<T *>(a.dx) + row * a.dx_stride, g, valid, raw);
+            for (int k = 0; k < P; ++k) out[k] = mul2(d[k], pair_of(a.scale));
+            narrow_row<T, U>(out, raw);
+            store_row<T, VEC, U>(static_cast<T *>(a.dx) + row * a.dx_stride, g, valid, raw);
         }
         const float mean = a.post_norm ? a.saved[row] : 0.0f, rstd = a.post_norm ? a.saved[a.rows + row] : 1.0f;
-        widen_source<T, VEC>(a.f, row, g, valid, f, h);
+        widen_source<T, VEC, U>(a.f, row, g, valid, f, h);
+        if (more) {
+            f_row += source_step<T>(a.f, row_step);
+            load_source<T, VEC, U>(a.f, f_row, g, valid, f);
+        }
+        f32x2 gate[P], of_gate = 0ull, all[2] = {0ull, 0ull};
+        if (GATE == GATE_OF_ROW) {
+            const float of_row = load_param(a.gate, a.gate_bf16, row);
 #pragma unroll
-        for (int i = 0; i < P; ++i) h[i] = mul2(add2(h[i], pair_of(-mean)), pair_of(rstd));
-        if (more) load_source<T, VEC>(a.f, row + step, g, valid, f);
-        f32x2 of_gate = 0ull;
-        if (GATE != GATE_IN_COLUMNS) {
-            f32x2 gate[P];
-            if (GATE == GATE_OF_ROW) {
-                const float of_row = load_param(a.gate, a.gate_bf16, row);
+            for (int k = 0; k < P; ++k) gate[k] = pair_of(of_row);
+        } else if (GATE == GATE_OF_VALUES) {
+            load_row<T, VEC, U>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);
+            widen_row<T, U>(raw, gate);
+        }
 #pragma unroll
-                for (int i = 0; i < P; ++i) gate[i] = pair_of(of_row);
-            } else {
-                load_row<T, VEC>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);
-                widen_row<T>(raw, valid, gate);
-            }
+        for (int u = 0; u < U; ++u) {
+            f32x2 factor[4], shift[4];
+            held_columns<VEC, U>(held + a.cols, g, valid, a.cols, u, factor);
+            if (GATE != GATE_IN_COLUMNS) held_columns<VEC, U>(held + 2 * a.cols, g, valid, a.cols, u, shift);
 #pragma unroll
-            for (int i = 0; i < P; ++i) {
-                out[i] = mul2(d[i], fma2(h[i], factor[i], shift[i]));
-                if (GATE == GATE_OF_ROW) of_gate = add2(of_gate, out[i]);
-                d[i] = mul2(d[i], gate[i]);
-            }
-            if (GATE == GATE_OF_VALUES && a.dgate) {
-                narrow_row<T>(out, raw);
-                store_row<T, VEC>(static_cast<T *>(a.dgate) + row * a.dgate_stride, g, valid, raw);
+            for (int i = 0; i < 4; ++i) {  // d is zero outside the row
+                const int k = 4 * u + i;
+                h[k] = mul2(add2(h[k], pair_of(-mean)), pair_of(rstd));
+                if (GATE != GATE_IN_COLUMNS) {
+                    const f32x2 dp = mul2(d[k], fma2(h[k], factor[i], shift[i]));
+                    d[k] = mul2(d[k], gate[k]);
+                    gate[k] = dp;
+                    if (GATE == GATE_OF_ROW) of_gate = add2(of_gate, dp);
+                }
+                sums[2][k] = fma2(d[k], h[k], sums[2][k]);
+                sums[3][k] = add2(sums[3][k], d[k]);
+                d[k] = mul2(d[k], factor[i]);
+                all[0] = add2(all[0], d[k]);
+                all[1] = fma2(d[k], h[k], all[1]);
             }
         }
-        f32x2 all[2] = {0ull, 0ull};
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            sums[2][i] = fma2(d[i], h[i], sums[2][i]);
-            sums[3][i] = add2(sums[3][i], d[i]);
-            d[i] = mul2(d[i], factor[i]);
-            all[0] = add2(all[0], d[i]);
-            all[1] = fma2(d[i], h[i], all[1]);
+        if (GATE == GATE_OF_VALUES && a.dgate) {
+            narrow_row<T, U>(gate, raw);
+            store_row<T, VEC, U>(static_cast<T *>(a.dgate) + row * a.dgate_stride, g, valid, raw);
         }
         float2 of[2] = {make_float2(sum_of(all[0]), sum_of(all[1])), make_float2(sum_of(of_gate), 0.0f)};
         if (GATE == GATE_OF_ROW) {
@@ -807,31 +804,32 @@ __global__ void __launch_bounds__(512, 1) group_back_kernel(const __grid_constan
             if (a.post_norm) {
                 const f32x2 mean_q = pair_of(-of[0].x * g.of_row), mean_qh = pair_of(-of[0].y * g.of_row);
 #pragma unroll
-                for (int i = 0; i < P; ++i) d[i] = mul2(fma2(h[i], mean_qh, add2(d[i], mean_q)), pair_of(rstd));
+                for (int k = 0; k < P; ++k) d[k] = mul2(fma2(h[k], mean_qh, add2(d[k], mean_q)), pair_of(rstd));
             }
-            narrow_row<T>(d, raw);
-            store_row<T, VEC>(static_cast<T *>(a.df) + row * a.df_stride, g, valid, raw);
+            narrow_row<T, U>(d, raw);
+            store_row<T, VEC, U>(static_cast<T *>(a.df) + row * a.df_stride, g, valid, raw);
         }
     }
-    // the groups' sums, one group after another
+    // the groups' sums, one group after another, in the place of the parameters
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
+        __syncthreads();
         for (int turn = 0; turn < groups; ++turn) {
             if (g.index == turn) {
 #pragma unroll
-                for (int j = 0; j < PER_THREAD; ++j) {
+                for (int j = 0; j < 8 * U; ++j) {
                     const float2 w = values_of(sums[q][j / 2]);
                     const float own = j & 1 ? w.y : w.x;
                     if (valid >> j & 1u) {
-                        float &at = joined[column<VEC>(g, j)];
+                        float &at = held[param_place<VEC>(column<VEC>(g.threads, g.thread, j), a.cols)];
                         at = turn ? at + own : own;
                     }
                 }
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < a.cols; c += blockDim.x) a.partial[((long long)blockIdx.x * 4 + q) * a.cols + c] = joined[c];
-        __syncthreads();
+        for (int c = threadIdx.x; c < a.cols; c += blockDim.x)
+            a.partial[((long long)blockIdx.x * 4 + q) * a.cols + c] = held[param_place<VEC>(c, a.cols)];
     }
 }
 
@@ -975,18 +973,19 @@ NormArgs norm_args(const dipaco_residual_norm_args *a)
     return n;
 }
 
+template <typename T, bool VEC, int GATE, int U> int launch_groups(const NormArgs &a, cudaStream_t stream)
+{
+    const auto kernel = group_rows_kernel<T, VEC, GATE, U>;
+    const int warps = (int)ceil_div(a.cols, 256 * U), groups = 16 / warps;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_GROUP_COLS * 16) != cudaSuccess) return launch_status();
+    kernel<<<(unsigned)std::min<int64_t>(ceil_div(a.rows, groups), 148), groups * warps * 32, a.cols * 16, stream>>>(a, warps);
+    return launch_status();
+}
 template <typename T, bool VEC, int GATE> int launch_groups(const NormArgs &a, cudaStream_t stream)
 {
-    const int warps = (int)ceil_div(a.cols, 32 * PER_THREAD);
-    const int groups = (warps <= 16 ? 16 : 32) / warps;
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.rows, groups), 148), threads = groups * warps * 32;
-    if (warps > 16)
-        group_rows_kernel<T, VEC, GATE, false, 1><<<grid, threads, 0, stream>>>(a, warps);
-    else if (a.rows <= (int64_t)grid * groups)
-        group_rows_kernel<T, VEC, GATE, true, 1><<<grid, threads, 0, stream>>>(a, warps);
-    else
-        group_rows_kernel<T, VEC, GATE, true, 2><<<grid, threads, 0, stream>>>(a, warps);
-    return launch_status();
+    if (a.cols <= 256) return launch_groups<T, VEC, GATE, 1>(a, stream);
+    if (a.cols <= 512 || ROW_UNITS<T> == 2) return launch_groups<T, VEC, GATE, 2>(a, stream);
+    return launch_groups<T, VEC, GATE, ROW_UNITS<T>>(a, stream);
 }
 
 template <typename T> int launch_rows(const NormArgs &a, cudaStream_t stream)
@@ -996,7 +995,7 @@ template <typename T> int launch_rows(const NormArgs &a, cudaStream_t stream)
         return launch_status();
     }
     const auto aligned = [&](const void *p, long long stride) { return !p || rows_aligned16(p, stride, a.rows, sizeof(T)); };
-    const bool vec = aligned(a.x.dense, a.x.stride) && aligned(a.f.dense, a.f.stride) && aligned(a.z_out, a.z_stride) &&
+    const bool vec = a.cols % 8 == 0 && aligned(a.x.dense, a.x.stride) && aligned(a.f.dense, a.f.stride) && aligned(a.z_out, a.z_stride) &&
                      aligned(a.n, a.n_stride) && (a.gate_kind != DIPACO_GATE_FULL || aligned(a.gate, a.gate_stride));
     switch (a.gate_kind) {
     case DIPACO_GATE_ROWS:
@@ -1009,43 +1008,58 @@ template <typename T> int launch_rows(const NormArgs &a, cudaStream_t stream)
 }
 
 struct BackPlan {
-    int groups;  // of a block of group_back_kernel; 0: the kernels for any width
+    bool grouped;  // group_back_kernel; else the kernels for any width
     int parts;
     int64_t partial_bytes, bytes;
 };
 BackPlan plan_back(int64_t rows, int64_t cols)
 {
     BackPlan p;
-    if (cols <= MAX_BACK_COLS) {
-        const int64_t warps = std::max<int64_t>(1, ceil_div(cols, 32 * PER_THREAD));
-        p.groups = (int)(16 / warps);
-        p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(148, ceil_div(rows, p.groups)));
+    if (cols <= MAX_BACK_COLS) {  // as many groups as any type's, so that the workspace does not depend on it
+        p.grouped = true;
+        p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(148, rows));
         p.partial_bytes = p.bytes = (int64_t)p.parts * 4 * cols * 4;
         return p;
     }
     const int64_t columns = ceil_div(cols, COLUMN_THREADS);
-    p.groups = 0;
+    p.grouped = false;
     p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({MAX_PARTS, ceil_div(rows, 16), ceil_div(148 * 8, columns)}));
     p.partial_bytes = (int64_t)p.parts * 4 * cols * 4;
     p.bytes = ceil_div(p.partial_bytes, 16) * 16 + rows * 8;
     return p;
 }
 
-template <typename T, bool VEC> int launch_back_groups(const NormArgs &a, const BackPlan &plan, cudaStream_t stream)
+template <typename T, bool VEC, int GATE, int U, int THREADS> int launch_back_groups(NormArgs &a, cudaStream_t stream)
 {
-    const int warps = (int)ceil_div(a.cols, 32 * PER_THREAD), threads = plan.groups * warps * 32;
-    if (a.gate_kind == DIPACO_GATE_ROWS)
-        group_back_kernel<T, VEC, GATE_OF_ROW><<<plan.parts, threads, 0, stream>>>(a, warps);
-    else if (a.gate_kind == DIPACO_GATE_FULL)
-        group_back_kernel<T, VEC, GATE_OF_VALUES><<<plan.parts, threads, 0, stream>>>(a, warps);
-    else
-        group_back_kernel<T, VEC, GATE_IN_COLUMNS><<<plan.parts, threads, 0, stream>>>(a, warps);
+    const auto kernel = group_back_kernel<T, VEC, GATE, U, THREADS>;
+    const int warps = (int)ceil_div(a.cols, 256 * U), groups = THREADS / 32 / warps;
+    a.parts = (int)std::min<int64_t>(ceil_div(a.rows, groups), a.parts);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_BACK_COLS * 12) != cudaSuccess) return launch_status();
+    kernel<<<a.parts, groups * warps * 32, a.cols * 12, stream>>>(a, warps);
     return launch_status();
 }
-
-template <typename T> int launch_back(const NormArgs &a, const BackPlan &plan, cudaStream_t stream)
+// Narrow rows: one unit for a thread.  Wide ones: two in bf16, for which a thread takes 168 registers, three quarters
+// of the threads; from 6145 columns on these are too few for a row, and some registers are spilled.
+template <typename T, bool VEC, int GATE> int launch_back_groups(NormArgs &a, cudaStream_t stream)
 {
-    if (plan.groups == 0) {
+    if constexpr (sizeof(T) == 2) {
+        if (a.cols > 6144) return launch_back_groups<T, VEC, GATE, 2, 512>(a, stream);
+        if (a.cols > 256) return launch_back_groups<T, VEC, GATE, 2, 384>(a, stream);
+    }
+    if (a.cols > 4096) return launch_back_groups<T, VEC, GATE, 2, 512>(a, stream);
+    return launch_back_groups<T, VEC, GATE, 1, 512>(a, stream);
+}
+template <typename T, bool VEC> int launch_back_groups(NormArgs &a, cudaStream_t stream)
+{
+    if (a.gate_kind == DIPACO_GATE_ROWS) return launch_back_groups<T, VEC, GATE_OF_ROW>(a, stream);
+    if (a.gate_kind == DIPACO_GATE_FULL) return launch_back_groups<T, VEC, GATE_OF_VALUES>(a, stream);
+    return launch_back_groups<T, VEC, GATE_IN_COLUMNS>(a, stream);
+}
+
+// a.parts: how many parts there may be, and then are.
+template <typename T> int launch_back(NormArgs &a, const BackPlan &plan, cudaStream_t stream)
+{
+    if (!plan.grouped) {
         back_rows_kernel<T><<<(unsigned)std::min<int64_t>(a.rows, 148 * 8), ROW_THREADS, 0, stream>>>(a);
         if (const int rc = launch_status()) return rc;
         const dim3 columns((unsigned)ceil_div(a.cols, COLUMN_THREADS), (unsigned)plan.parts);
@@ -1053,10 +1067,10 @@ template <typename T> int launch_back(const NormArgs &a, const BackPlan &plan, c
         return launch_status();
     }
     const auto aligned = [&](const void *p, long long stride) { return !p || rows_aligned16(p, stride, a.rows, sizeof(T)); };
-    const bool vec = aligned(a.dn.dense, a.dn.stride) && aligned(a.dz.dense, a.dz.stride) && aligned(a.f.dense, a.f.stride) &&
+    const bool vec = a.cols % 8 == 0 && aligned(a.dn.dense, a.dn.stride) && aligned(a.dz.dense, a.dz.stride) && aligned(a.f.dense, a.f.stride) &&
                      aligned(a.z.dense, a.z.stride) && aligned(a.dx, a.dx_stride) && aligned(a.df, a.df_stride) &&
                      (a.gate_kind != DIPACO_GATE_FULL || (aligned(a.gate, a.gate_stride) && aligned(a.dgate, a.dgate_stride)));
-    return vec ? launch_back_groups<T, true>(a, plan, stream) : launch_back_groups<T, false>(a, plan, stream);
+    return vec ? launch_back_groups<T, true>(a, stream) : launch_back_groups<T, false>(a, stream);
 }
 
 } // namespace
@@ -1175,7 +1189,7 @@ int dipaco_residual_norm_backward(const dipaco_residual_norm_args *args, const v
     if (!dgate_cols && !dgamma && !dbeta && !dpost_gamma && !dpost_beta) return DIPACO_OK;
     JoinArgs j = {};
     j.partial = a.partial;
-    j.parts = plan.parts;
+    j.parts = a.parts;
     j.cols = a.cols;
     j.gate = args->gate;
     j.gate_cols = args->gate_kind == DIPACO_GATE_COLS;
