@@ -648,8 +648,8 @@ int dipaco_clip_gradients(const void *const *grads, void *const *out, const int6
 int dipaco_inner_status(int32_t device, void *cuda_stream);
 
 /*
- * Diagnostic: make a bounded wait of the norms (operators = 0), of the packing kernels (1) or of the
- * products and linear layers (2, one after the other) run out on purpose, harmlessly: one warp waits at most limit_ns (1 .. 1e9) on a barrier that
+ * Diagnostic: make a bounded wait of the norms (operators = 0; of the plain ones, then of those around a block), of
+ * the packing kernels (1) or of the products and then the linear layers (2) run out on purpose, harmlessly: one warp waits at most limit_ns (1 .. 1e9) on a barrier that
  * nothing will complete; no copy is in flight and no buffer of the caller is involved.
  */
 int dipaco_selftest_inner_wait_expiry(int32_t operators, int64_t limit_ns, int32_t device, void *cuda_stream);

@@ -106,6 +106,7 @@ template <typename Symbol> bool take_error_word(const Symbol &symbol, bool &expi
 bool take_packing_error(bool &expired);  // of packed.cu
 bool take_norm_error(bool &expired);     // of layer_norm.cu
 bool take_linear_error(bool &expired);   // of packed_linear.cu
+bool take_residual_norm_error(bool &expired);  // of residual_norm.cu
 
 // The norm of rows whose statistics are known, and unless x_packed is NULL the rows themselves, packed (of packed.cu):
 // checked arguments, the device current, values to work on.
@@ -121,6 +122,7 @@ int pack_activated(const float *x, int64_t x_stride, int activation, const dipac
 int expire_packing_wait(unsigned long long limit_ns, cudaStream_t stream);
 int expire_norm_wait(unsigned long long limit_ns, cudaStream_t stream);
 int expire_linear_wait(unsigned long long limit_ns, cudaStream_t stream);
+int expire_residual_norm_wait(unsigned long long limit_ns, cudaStream_t stream);
 
 // ------------------------------------------------------------------------------------------ device
 

@@ -91,7 +91,10 @@ int dipaco_selftest_inner_wait_expiry(int32_t operators, int64_t limit_ns, int32
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (operators == 0) return expire_norm_wait(limit_ns, stream);
+    if (operators == 0) {
+        if (const int rc = expire_norm_wait(limit_ns, stream)) return rc;
+        return expire_residual_norm_wait(limit_ns, stream);
+    }
     if (operators == 1) return expire_packing_wait(limit_ns, stream);
     wait_expiry_kernel<<<1, 32, 0, stream>>>(limit_ns);
     if (const int rc = launch_status()) return rc;
@@ -113,7 +116,7 @@ int dipaco_inner_status(int32_t device, void *cuda_stream)
         uint64_t &count = happened[device], &known = told[{device, cuda_stream}];
         bool expired = false;
         const bool read = take_error_word(g_product_error, expired) && take_packing_error(expired) && take_norm_error(expired) &&
-                          take_linear_error(expired);
+                          take_linear_error(expired) && take_residual_norm_error(expired);
         if (expired) ++count;
         if (!read) return launch_status();
         if (known == count) return DIPACO_OK;

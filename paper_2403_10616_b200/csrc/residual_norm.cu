@@ -589,61 +589,85 @@ template <typename T> __global__ void __launch_bounds__(ROW_THREADS) back_rows_k
     }
 }
 
-// A row of f or z: as load_row, or codes.
-template <typename T, bool VEC, int U>
-__device__ __forceinline__ void load_source(const Source &s, const void *row, const Group &g, unsigned valid, RowRaw<T, U> &raw)
+static __device__ int g_residual_norm_error;  // set by a bounded wait that ran out
+
+// Rows on their way to shared memory: bulk copies of the 16-byte units that hold a row, a stage of the ring for a row of
+// dn, z, dz and f.
+struct Feed {
+    const uint8_t *first;  // row 0
+    long long step;        // bytes from row to row
+    int bytes;             // of a row; 0: not there
+
+    __device__ __forceinline__ const uint8_t *row(long long at) const { return first + at * step; }
+    // How far into its first unit a row begins.
+    __device__ __forceinline__ int ahead(long long at) const { return (int)(reinterpret_cast<uintptr_t>(row(at)) & 15u); }
+    __device__ __forceinline__ unsigned copied(long long at) const { return (unsigned)(ahead(at) + bytes + 15) & ~15u; }
+};
+template <typename T> __device__ __forceinline__ Feed make_feed(const Source &s, int cols)
 {
-    if (s.dense) {
-        load_row<T, VEC, U>(row, g, valid, raw);
-        return;
-    }
-    const uint8_t *codes = static_cast<const uint8_t *>(row);
+    if (s.codes) return {s.codes, s.stride, cols};
+    return {static_cast<const uint8_t *>(s.dense), s.stride * (long long)sizeof(T), s.dense ? cols * (int)sizeof(T) : 0};
+}
+
+// A row's values in shared memory; where there are none, any of the row.
+template <typename T, bool VEC, int U>
+__device__ __forceinline__ void read_row(const uint8_t *at, const Group &g, int cols, f32x2 *v)
+{
+    constexpr int UE = Unit<T>::UE;
+    if constexpr (VEC) {
+        const int last = cols / 8 - 1;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        raw.w[2 * u] = raw.w[2 * u + 1] = 0u;
-        if constexpr (VEC) {
-            if (valid >> (8 * u) & 1u) {
-                const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(codes) + u * g.threads + g.thread);
-                raw.w[2 * u] = v.x;
-                raw.w[2 * u + 1] = v.y;
-            }
-        } else {
+        for (int u = 0; u < U; ++u) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(at) + min(u * g.threads + g.thread, last) * (8 / UE);
 #pragma unroll
-            for (int j = 8 * u; j < 8 * u + 8; ++j)
-                if (valid >> j & 1u) raw.w[j / 4] |= (unsigned)__ldcs(codes + column<false>(g.threads, g.thread, j)) << 8 * (j % 4);
+            for (int i = 0; i < 8 / UE; ++i) widen_pairs<T>(p[i], v + 4 * u + i * UE / 2);
         }
+    } else {
+        const T *p = reinterpret_cast<const T *>(at);
+#pragma unroll
+        for (int i = 0; i < 4 * U; ++i)
+            v[i] = pair_of(widen1<T>(p[min(column<false>(g.threads, g.thread, 2 * i), cols - 1)]),
+                           widen1<T>(p[min(column<false>(g.threads, g.thread, 2 * i + 1), cols - 1)]));
     }
 }
-// Their values.
 template <typename T, bool VEC, int U>
-__device__ __forceinline__ void widen_source(const Source &s, int row, const Group &g, unsigned valid, const RowRaw<T, U> &raw, f32x2 *v)
+__device__ __forceinline__ void read_source(const Source &s, int row, const uint8_t *at, const Group &g, int cols, f32x2 *v)
 {
     if (s.dense) {
-        widen_row<T, U>(raw, v);
+        read_row<T, VEC, U>(at, g, cols, v);
         return;
     }
     const uint8_t *scales = s.scales + (long long)(row / PACK_BLOCK) * s.scale_cols;
-    const auto scale_of = [&](int j) {
-        return valid >> j & 1u ? scale_value(scales[column<VEC>(g.threads, g.thread, j) / PACK_BLOCK]) : 0.0f;
-    };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const f32x2 one = pair_of(VEC ? scale_of(8 * u) : 0.0f);
+        if constexpr (VEC) {
+            const int unit = min(u * g.threads + g.thread, cols / 8 - 1);
+            const uint2 w = reinterpret_cast<const uint2 *>(at)[unit];
+            const f32x2 scale = pair_of(scale_value(scales[unit * 8 / PACK_BLOCK]));
+            v[4 * u] = mul2(decode_pair(w.x), scale);
+            v[4 * u + 1] = mul2(decode_pair(w.x >> 16), scale);
+            v[4 * u + 2] = mul2(decode_pair(w.y), scale);
+            v[4 * u + 3] = mul2(decode_pair(w.y >> 16), scale);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x2 scale = VEC ? one : pair_of(scale_of(8 * u + 2 * i), scale_of(8 * u + 2 * i + 1));
-            v[4 * u + i] = mul2(decode_pair(raw.w[2 * u + i / 2] >> 16 * (i & 1)), scale);
+            for (int i = 0; i < 4; ++i) {
+                const int c0 = min(column<false>(g.threads, g.thread, 8 * u + 2 * i), cols - 1);
+                const int c1 = min(column<false>(g.threads, g.thread, 8 * u + 2 * i + 1), cols - 1);
+                v[4 * u + i] = mul2(decode_pair(at[c0] | (unsigned)at[c1] << 8),
+                                    pair_of(scale_value(scales[c0 / PACK_BLOCK]), scale_value(scales[c1 / PACK_BLOCK])));
+            }
         }
     }
 }
-// The start of a row of codes or values of T, and the bytes from row to row.
-template <typename T> __device__ __forceinline__ const uint8_t *source_row(const Source &s, long long row)
+// Zeros where there are no values.
+template <bool VEC, int U> __device__ __forceinline__ void keep_valid_row(unsigned valid, f32x2 *v)
 {
-    return s.codes ? s.codes + row * s.stride : static_cast<const uint8_t *>(s.dense) + row * s.stride * (long long)sizeof(T);
-}
-template <typename T> __device__ __forceinline__ long long source_step(const Source &s, long long rows)
-{
-    return rows * s.stride * (s.codes ? 1 : (long long)sizeof(T));
+    if (valid == (1u << (8 * U)) - 1u) return;
+#pragma unroll
+    for (int i = 0; i < 4 * U; ++i) {
+        const float2 w = values_of(v[i]);
+        v[i] = pair_of(valid >> (2 * i) & 1u ? w.x : 0.0f, valid >> (2 * i + 1) & 1u ? w.y : 0.0f);
+    }
 }
 
 // Sums of R pairs over the group, on every thread.
@@ -658,33 +682,43 @@ template <int R> __device__ __forceinline__ void group_sums(Group &g, float2 *su
 }
 
 constexpr int MAX_BACK_COLS = 8192;
+constexpr int MAX_STAGES = 4;
+constexpr int BACK_SMEM = 226 * 1024;
 
-// A persistent block of groups, each with a row at a time; a thread keeps the sums over its rows of its columns.  The
-// next row's values are loaded where this row's have been used for the last time.
+// A persistent block of groups, each with a row at a time; a thread keeps the sums over its rows of its columns.  A
+// ring of `stages` rows on their way for each group.
 template <typename T, bool VEC, int GATE, int U, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_constant__ NormArgs a, int warps)
+__global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_constant__ NormArgs a, int warps, int stages, int buffer)
 {
     constexpr int P = 4 * U;
     extern __shared__ __align__(16) float held[];  // [3][cols]: gamma; post_gamma, times a gate of columns; post_beta
     __shared__ float2 slots[2 * 16 * 2];
+    __shared__ uint64_t full[16 * MAX_STAGES];
     Group g = make_group<VEC, U>(warps, a.cols, slots, 2);
     const int groups = (int)(blockDim.x >> 5) / warps;
     const unsigned valid = valid_values<VEC, U>(g.threads, g.thread, a.cols);
     const int row_step = gridDim.x * groups;
     int row = blockIdx.x * groups + g.index;
-    const uint8_t *dn_row = source_row<T>(a.dn, row), *dz_row = source_row<T>(a.dz, row), *z_row = source_row<T>(a.z, row),
-                  *f_row = source_row<T>(a.f, row);
-    RowRaw<T, U> dn = {}, dz = {}, z = {}, f = {};
-    const auto load_z = [&] {
+    uint8_t *ring = reinterpret_cast<uint8_t *>(held) + (a.cols * 12 + 15) / 16 * 16 + g.index * stages * 4 * buffer;
+    uint64_t *arrived = full + g.index * stages;
+    const Feed dn = make_feed<T>(a.dn, a.cols), z = make_feed<T>(a.z, a.cols), dz = make_feed<T>(a.dz, a.cols), f = make_feed<T>(a.f, a.cols);
+    const auto request = [&](int at, int stage) {  // one thread
+        uint8_t *to = ring + stage * 4 * buffer;
+        unsigned bytes = f.copied(at);
+        if (a.norm) bytes += dn.copied(at) + z.copied(at);
+        if (dz.bytes) bytes += dz.copied(at);
+        ptx::mbar_arrive_expect_tx(&arrived[stage], bytes);
         if (a.norm) {
-            load_row<T, VEC, U>(dn_row, g, valid, dn);
-            load_source<T, VEC, U>(a.z, z_row, g, valid, z);
+            ptx::bulk_load(to, dn.row(at) - dn.ahead(at), dn.copied(at), &arrived[stage]);
+            ptx::bulk_load(to + buffer, z.row(at) - z.ahead(at), z.copied(at), &arrived[stage]);
         }
-        if (a.dz.dense) load_row<T, VEC, U>(dz_row, g, valid, dz);
+        if (dz.bytes) ptx::bulk_load(to + 2 * buffer, dz.row(at) - dz.ahead(at), dz.copied(at), &arrived[stage]);
+        ptx::bulk_load(to + 3 * buffer, f.row(at) - f.ahead(at), f.copied(at), &arrived[stage]);
     };
-    if (row < a.rows) {
-        load_z();
-        load_source<T, VEC, U>(a.f, f_row, g, valid, f);
+    if (g.thread == 0) {
+        for (int s = 0; s < stages; ++s) ptx::mbar_init(&arrived[s], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < stages && row + (long long)s * row_step < a.rows; ++s) request(row + s * row_step, s);
     }
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
         const float gate = a.gate_kind == DIPACO_GATE_COLS ? load_param(a.gate, a.gate_bf16, c) : 1.0f;
@@ -700,23 +734,43 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
 #pragma unroll
         for (int i = 0; i < P; ++i) sums[q][i] = 0ull;
 
+    int stage = 0;
+    unsigned phase = 0;
+    bool ok = true;  // a wait that runs out leaves the results undefined, but every barrier is met
     for (; row < a.rows; row += row_step) {
-        const bool more = row < a.rows - row_step;
-        f32x2 d[P], h[P];
-        widen_row<T, U>(dz, d);
+        const uint8_t *from = ring + stage * 4 * buffer;
+        float mean_f = 0.0f, rstd_f = 1.0f, mean_z = 0.0f, rstd_z = 1.0f;
+        if (a.post_norm) {
+            mean_f = a.saved[row];
+            rstd_f = a.saved[a.rows + row];
+        }
         if (a.norm) {
-            const float mean = a.saved[2ll * a.rows + row], rstd = a.saved[3ll * a.rows + row];
+            mean_z = a.saved[2ll * a.rows + row];
+            rstd_z = a.saved[3ll * a.rows + row];
+        }
+        const float of_row = GATE == GATE_OF_ROW ? load_param(a.gate, a.gate_bf16, row) : 1.0f;
+        if (ok) ok = bounded_wait(&arrived[stage], phase, &g_residual_norm_error, 1);
+        __syncwarp();
+        f32x2 d[P], h[P];
+        if (dz.bytes) {
+            read_row<T, VEC, U>(from + 2 * buffer + dz.ahead(row), g, a.cols, d);
+        } else {
+#pragma unroll
+            for (int k = 0; k < P; ++k) d[k] = 0ull;
+        }
+        if (a.norm) {
             f32x2 y[P], all[2] = {0ull, 0ull};
-            widen_row<T, U>(dn, y);
-            widen_source<T, VEC, U>(a.z, row, g, valid, z, h);
+            read_row<T, VEC, U>(from + dn.ahead(row), g, a.cols, y);
+            read_source<T, VEC, U>(a.z, row, from + buffer + z.ahead(row), g, a.cols, h);
+            keep_valid_row<VEC, U>(valid, y);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 f32x2 gamma[4];
                 held_columns<VEC, U>(held, g, valid, a.cols, u, gamma);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {  // dn is zero outside the row
+                for (int i = 0; i < 4; ++i) {
                     const int k = 4 * u + i;
-                    h[k] = mul2(add2(h[k], pair_of(-mean)), pair_of(rstd));
+                    h[k] = mul2(add2(h[k], pair_of(-mean_z)), pair_of(rstd_z));
                     sums[0][k] = fma2(y[k], h[k], sums[0][k]);
                     sums[1][k] = add2(sums[1][k], y[k]);
                     y[k] = mul2(y[k], gamma[i]);
@@ -728,22 +782,9 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             group_sums<1>(g, &of);
             const f32x2 mean_u = pair_of(-of.x * g.of_row), mean_uh = pair_of(-of.y * g.of_row);
 #pragma unroll
-            for (int k = 0; k < P; ++k) d[k] = fma2(fma2(h[k], mean_uh, add2(y[k], mean_u)), pair_of(rstd), d[k]);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                keep_valid<VEC>(valid, u, d + 4 * u);
-                if (VEC) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) d[4 * u + i] = if_valid<VEC>(valid, u, d[4 * u + i]);
-                }
-            }
+            for (int k = 0; k < P; ++k) d[k] = fma2(fma2(h[k], mean_uh, add2(y[k], mean_u)), pair_of(rstd_z), d[k]);
         }
-        if (more) {
-            dn_row += source_step<T>(a.dn, row_step);
-            dz_row += source_step<T>(a.dz, row_step);
-            z_row += source_step<T>(a.z, row_step);
-            load_z();
-        }
+        keep_valid_row<VEC, U>(valid, d);
         RowRaw<T, U> raw;
         if (a.dx) {
             f32x2 out[P];
@@ -752,18 +793,9 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             narrow_row<T, U>(out, raw);
             store_row<T, VEC, U>(static_cast<T *>(a.dx) + row * a.dx_stride, g, valid, raw);
         }
-        const float mean = a.post_norm ? a.saved[row] : 0.0f, rstd = a.post_norm ? a.saved[a.rows + row] : 1.0f;
-        widen_source<T, VEC, U>(a.f, row, g, valid, f, h);
-        if (more) {
-            f_row += source_step<T>(a.f, row_step);
-            load_source<T, VEC, U>(a.f, f_row, g, valid, f);
-        }
+        read_source<T, VEC, U>(a.f, row, from + 3 * buffer + f.ahead(row), g, a.cols, h);
         f32x2 gate[P], of_gate = 0ull, all[2] = {0ull, 0ull};
-        if (GATE == GATE_OF_ROW) {
-            const float of_row = load_param(a.gate, a.gate_bf16, row);
-#pragma unroll
-            for (int k = 0; k < P; ++k) gate[k] = pair_of(of_row);
-        } else if (GATE == GATE_OF_VALUES) {
+        if (GATE == GATE_OF_VALUES) {
             load_row<T, VEC, U>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);
             widen_row<T, U>(raw, gate);
         }
@@ -775,12 +807,14 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
 #pragma unroll
             for (int i = 0; i < 4; ++i) {  // d is zero outside the row
                 const int k = 4 * u + i;
-                h[k] = mul2(add2(h[k], pair_of(-mean)), pair_of(rstd));
+                h[k] = mul2(add2(h[k], pair_of(-mean_f)), pair_of(rstd_f));
                 if (GATE != GATE_IN_COLUMNS) {
                     const f32x2 dp = mul2(d[k], fma2(h[k], factor[i], shift[i]));
-                    d[k] = mul2(d[k], gate[k]);
-                    gate[k] = dp;
-                    if (GATE == GATE_OF_ROW) of_gate = add2(of_gate, dp);
+                    d[k] = mul2(d[k], GATE == GATE_OF_ROW ? pair_of(of_row) : gate[k]);
+                    if (GATE == GATE_OF_ROW)
+                        of_gate = add2(of_gate, dp);
+                    else
+                        gate[k] = dp;
                 }
                 sums[2][k] = fma2(d[k], h[k], sums[2][k]);
                 sums[3][k] = add2(sums[3][k], d[k]);
@@ -799,17 +833,25 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             if (g.thread == 0 && a.dgate) static_cast<float *>(a.dgate)[row] = of[1].x;
         } else if (a.post_norm) {
             group_sums<1>(g, of);
+        } else if (g.warps > 1) {
+            g.sync();
         }
+        // every warp of the group is past its reads of this stage
+        __syncwarp();
+        if (g.thread == 0 && ok && row + (long long)stages * row_step < a.rows) request(row + stages * row_step, stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
         if (a.df) {
             if (a.post_norm) {
                 const f32x2 mean_q = pair_of(-of[0].x * g.of_row), mean_qh = pair_of(-of[0].y * g.of_row);
 #pragma unroll
-                for (int k = 0; k < P; ++k) d[k] = mul2(fma2(h[k], mean_qh, add2(d[k], mean_q)), pair_of(rstd));
+                for (int k = 0; k < P; ++k) d[k] = mul2(fma2(h[k], mean_qh, add2(d[k], mean_q)), pair_of(rstd_f));
             }
             narrow_row<T, U>(d, raw);
             store_row<T, VEC, U>(static_cast<T *>(a.df) + row * a.df_stride, g, valid, raw);
         }
     }
+    if (!ok)  // a wait ran out: let the copies in flight land before the block ends
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     // the groups' sums, one group after another, in the place of the parameters
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -1034,8 +1076,11 @@ template <typename T, bool VEC, int GATE, int U, int THREADS> int launch_back_gr
     const auto kernel = group_back_kernel<T, VEC, GATE, U, THREADS>;
     const int warps = (int)ceil_div(a.cols, 256 * U), groups = THREADS / 32 / warps;
     a.parts = (int)std::min<int64_t>(ceil_div(a.rows, groups), a.parts);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_BACK_COLS * 12) != cudaSuccess) return launch_status();
-    kernel<<<a.parts, groups * warps * 32, a.cols * 12, stream>>>(a, warps);
+    // a row of any kind and alignment, and how many fit beside the parameters
+    const int buffer = (a.cols * (int)sizeof(T) + 30) / 16 * 16, parameters = (a.cols * 12 + 15) / 16 * 16;
+    const int stages = std::min(MAX_STAGES, (BACK_SMEM - parameters) / (groups * 4 * buffer));
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BACK_SMEM) != cudaSuccess) return launch_status();
+    kernel<<<a.parts, groups * warps * 32, parameters + groups * stages * 4 * buffer, stream>>>(a, warps, stages, buffer);
     return launch_status();
 }
 // Narrow rows: one unit for a thread.  Wide ones: two in bf16, for which a thread takes 168 registers, three quarters
@@ -1073,7 +1118,27 @@ template <typename T> int launch_back(NormArgs &a, const BackPlan &plan, cudaStr
     return vec ? launch_back_groups<T, true>(a, stream) : launch_back_groups<T, false>(a, stream);
 }
 
+// A warp waits, for a limited time, on a barrier that nothing completes: no copy is in flight.
+__global__ void __launch_bounds__(32) wait_expiry_kernel(unsigned long long limit_ns)
+{
+    __shared__ uint64_t bar;
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    __all_sync(0xffffffffu, bounded_wait(&bar, 0, &g_residual_norm_error, 9, limit_ns));
+}
+
 } // namespace
+
+bool dipaco::take_residual_norm_error(bool &expired) { return take_error_word(g_residual_norm_error, expired); }
+
+int dipaco::expire_residual_norm_wait(unsigned long long limit_ns, cudaStream_t stream)
+{
+    wait_expiry_kernel<<<1, 32, 0, stream>>>(limit_ns);
+    return launch_status();
+}
 
 extern "C" {
 
