@@ -916,7 +916,7 @@ struct JoinArgs {
     float *dgate, *dgamma, *dbeta, *dpost_gamma, *dpost_beta;
 };
 
-constexpr int JOIN_SLICES = 8;
+constexpr int JOIN_SLICES = 32;
 
 // The parts' sums in order, 32 columns of a block in JOIN_SLICES slices of parts, and the gradients they make.
 __global__ void __launch_bounds__(32 * JOIN_SLICES) join_kernel(const __grid_constant__ JoinArgs a)
