@@ -26,7 +26,7 @@ struct Linear {
     const void *bias, *residual;
     long long residual_row;
     int activation;
-    bool bias_bf16, bias_aligned, residual_bf16, residual_aligned;
+    bool bias_bf16, residual_bf16, residual_aligned;
 
     __device__ __forceinline__ f32x2 act(f32x2 v) const
     {
@@ -44,43 +44,13 @@ struct Linear {
         if (residual) v += load_param(residual, residual_bf16, row * residual_row + col);
         return v;
     }
-    // 32 columns of a row
-    __device__ __forceinline__ void columns(float *v, long long row, int col, int m, int n) const
+    // of 32 columns
+    __device__ __forceinline__ void act32(f32x2 *v) const
     {
-        f32x2 p[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = pair_of(v[2 * i], v[2 * i + 1]);
-        if (bias) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f32x2 b[4];
-                param_pairs<8>(bias, bias_bf16, bias_aligned, col + 8 * i, n, b);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) p[4 * i + j] = add2(p[4 * i + j], b[j]);
-            }
-        }
         switch (activation) {
-        case DIPACO_ACTIVATION_RELU: each<DIPACO_ACTIVATION_RELU>(p); break;
-        case DIPACO_ACTIVATION_SILU: each<DIPACO_ACTIVATION_SILU>(p); break;
-        case DIPACO_ACTIVATION_GELU: each<DIPACO_ACTIVATION_GELU>(p); break;
-        }
-        if (residual && row < m) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f32x2 r[4];
-                const long long at = row * residual_row + col + 8 * i;
-                const void *from = residual_bf16 ? static_cast<const void *>(static_cast<const __nv_bfloat16 *>(residual) + at)
-                                                 : static_cast<const void *>(static_cast<const float *>(residual) + at);
-                param_pairs<8>(from, residual_bf16, residual_aligned, 0, n - (col + 8 * i), r);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) p[4 * i + j] = add2(p[4 * i + j], r[j]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 w = values_of(p[i]);
-            v[2 * i] = w.x;
-            v[2 * i + 1] = w.y;
+        case DIPACO_ACTIVATION_RELU: each<DIPACO_ACTIVATION_RELU>(v); break;
+        case DIPACO_ACTIVATION_SILU: each<DIPACO_ACTIVATION_SILU>(v); break;
+        case DIPACO_ACTIVATION_GELU: each<DIPACO_ACTIVATION_GELU>(v); break;
         }
     }
     template <int ACTIVATION> static __device__ __forceinline__ void each(f32x2 *p)
@@ -89,6 +59,270 @@ struct Linear {
         for (int i = 0; i < 16; ++i) p[i] = activate<ACTIVATION>(p[i]);
     }
 };
+
+constexpr int EPILOGUE_WARPS = 8;
+constexpr int SUBS = EPILOGUE_WARPS / 4;           // warps that share a quarter of the rows
+constexpr int GROUPS = PAIR_MAX_N / 32 / SUBS;     // of 32 columns, of one warp
+constexpr int OF_BLOCK = 4 / SUBS;                 // of them in a block of 128 columns
+
+// A warp's way through a tile: its quarter of the rows, every SUBS-th group of 32 columns, first those columns that the
+// sets of sums share.
+struct TileWalk {
+    int sub, own;  // the first group, how many
+    bool down;
+    __device__ __forceinline__ int slot(int t) const { return down ? own - 1 - t : t; }  // which of its groups is t-th
+    __device__ __forceinline__ int column(int slot) const { return (SUBS * slot + sub) * 32; }
+    __device__ __forceinline__ int group(int t) const { return SUBS * slot(t) + sub; }
+};
+
+// Parameters of the warp's columns from n0 on, for all lanes to read: the next tile's are on their way while one is
+// worked on.
+__device__ __forceinline__ void load_next_columns(const void *p, bool bf16, const TileWalk &walk, int n0, int n, int lane, float *next)
+{
+#pragma unroll
+    for (int s = 0; s < GROUPS; ++s) {
+        const int col = n0 + walk.column(s) + lane;
+        next[s] = s < walk.own && p && col < n ? load_param(p, bf16, col) : 0.0f;
+    }
+}
+__device__ __forceinline__ void put_next_columns(const float *next, int lane, float (*to)[32])
+{
+    __syncwarp();
+#pragma unroll
+    for (int s = 0; s < GROUPS; ++s) to[s][lane] = next[s];
+    __syncwarp();
+}
+__device__ __forceinline__ void add_columns(const float *columns, const uint32_t *r, f32x2 *v)
+{
+    const float4 *add = reinterpret_cast<const float4 *>(columns);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float4 w = add[i];
+        v[2 * i] = add2(pair_of(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1])), pair_of(w.x, w.y));
+        v[2 * i + 1] = add2(pair_of(__uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3])), pair_of(w.z, w.w));
+    }
+}
+
+// The residual of 32 rows and 64 bytes of columns, as a warp loads it whole: lane l has unit l % 4 of rows l / 4 + 8 i.
+__device__ __forceinline__ void load_residual(const DenseArgs<Linear> &p, int row0, int col, int lane, uint4 *units)
+{
+    const int size = p.c_bf16 ? 2 : 4, at = col + (lane & 3) * (16 / size);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + (lane >> 2) + 8 * i;
+        units[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < p.m && at < p.n)
+            units[i] = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.finish.residual) +
+                                                              (row * p.finish.residual_row + at) * size));
+    }
+}
+
+// 32 columns of the warp's rows to C.  units: the residual of the first 64 bytes, where it is read that way.
+__device__ __forceinline__ void finish_linear(const DenseArgs<Linear> &p, const CUtensorMap &c_map, const PairItem &item,
+                                              int row0, int quarter, unsigned rank, int lane, int group, const uint32_t *sums,
+                                              const float *bias, uint4 *units, bool by_units, uint8_t *buffers, int &buffer)
+{
+    if (item.slot >= 0) {
+        float *out = p.partial + partial_offset(p, item.slot, rank) + (long long)group * 32 * 128 + quarter * 32 + lane;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) out[i * 128] = __uint_as_float(sums[i]);
+        return;
+    }
+    const int col0 = item.tile_n * p.tile_n + group * 32;
+    f32x2 v[16];
+    add_columns(bias, sums, v);
+    p.finish.act32(v);
+    if (p.store_by_tma) {
+        if (p.finish.residual && !by_units && row0 + lane < p.m) {  // a residual at another alignment
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const long long at = (row0 + lane) * p.finish.residual_row + col0 + 2 * i;
+                v[i] = add2(v[i], pair_of(col0 + 2 * i < p.n ? load_param(p.finish.residual, p.finish.residual_bf16, at) : 0.0f,
+                                          col0 + 2 * i + 1 < p.n ? load_param(p.finish.residual, p.finish.residual_bf16, at + 1) : 0.0f));
+            }
+        }
+        // rows of 64 bytes in the copy engine's swizzle of that width
+        const int parts = p.c_bf16 ? 1 : 2, size = p.c_bf16 ? 2 : 4;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            if (part >= parts) break;
+            const int col = col0 + part * 16;
+            asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PAIR_STAGING - 1) : "memory");  // the buffer's last
+            __syncwarp();
+            uint8_t *staging = buffers + buffer * PAIR_STAGING_BYTES;
+            if (++buffer == PAIR_STAGING) buffer = 0;
+            const auto place = [&](int row, int unit) {
+                return reinterpret_cast<uint4 *>(staging + row * 64 + ((unit ^ ((row >> 1) & 3)) * 16));
+            };
+            if (by_units) {
+                if (part == 1) load_residual(p, row0, col, lane, units);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *place((lane >> 2) + 8 * i, lane & 3) = units[i];
+                __syncwarp();
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint4 *at = place(lane, i);
+                if (p.c_bf16) {
+                    f32x2 r[4];
+                    if (by_units) {
+                        widen_pairs<__nv_bfloat16>(*at, r);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[4 * i + j] = add2(v[4 * i + j], r[j]);
+                    }
+                    *at = narrow_pairs<__nv_bfloat16>(v + 4 * i);
+                } else {
+                    f32x2 *w = v + 8 * part + 2 * i, r[2];
+                    if (by_units) {
+                        widen_pairs<float>(*at, r);
+                        w[0] = add2(w[0], r[0]);
+                        w[1] = add2(w[1], r[1]);
+                    }
+                    *at = narrow_pairs<float>(w);
+                }
+            }
+            ptx::fence_proxy_async();
+            __syncwarp();
+            // rows outside C and columns from whole_n on are not written
+            if (elect_one()) {
+                if (row0 < p.m && col < p.whole_n) tma_store_2d(&c_map, ptx::smem_addr(staging), col, row0);
+                ptx::bulk_commit();
+            }
+            __syncwarp();
+            const int ahead = (p.whole_n - col) * size;
+            if (p.whole_n < p.n && ahead >= 0 && ahead < 64 && row0 + lane < p.m)  // the unit that C's rows end in
+                store_head(static_cast<uint8_t *>(p.c) + ((row0 + lane) * p.c_row + p.whole_n) * size, *place(lane, ahead >> 4),
+                           (p.n - p.whole_n) * size);
+        }
+        return;
+    }
+    // any alignment: rows through shared memory, a lane per column
+    float *at = reinterpret_cast<float *>(buffers);
+    for (int part = 0; part < 2; ++part) {  // 16 rows at a time
+        __syncwarp();
+        if (lane >> 4 == part) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 w = values_of(v[i]);
+                at[(lane & 15) * 32 + ((2 * i + lane) & 31)] = w.x;
+                at[(lane & 15) * 32 + ((2 * i + 1 + lane) & 31)] = w.y;
+            }
+        }
+        __syncwarp();
+        const int first = row0 + part * 16, rows = min(16, p.m - first);
+        if (col0 + lane >= p.n) continue;
+#pragma unroll
+        for (int r0 = 0; r0 < 16; r0 += 8) {
+            float add[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                add[r] = p.finish.residual && r0 + r < rows
+                             ? load_param(p.finish.residual, p.finish.residual_bf16, (first + r0 + r) * p.finish.residual_row + col0 + lane)
+                             : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r0 + r < rows)
+                    store_c(p, first + r0 + r, col0 + lane, at[(r0 + r) * 32 + ((lane + part * 16 + r0 + r) & 31)] + add[r]);
+        }
+    }
+}
+
+template <bool CHUNKED>
+__device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, const CUtensorMap &c_map, const PairBlock &b,
+                                                float (*columns)[GROUPS][32])
+{
+    const int lane = b.lane, quarter = b.warp & 3;
+    float (*bias)[32] = columns[b.warp];
+    uint8_t *staging = b.aligned + PAIR_STAGING_AT + b.warp * PAIR_STAGING * PAIR_STAGING_BYTES;
+    int buffer = 0;
+    const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&b.sums_read[0]), 0),
+                                   cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
+    const bool by_units = p.finish.residual && p.store_by_tma && p.finish.residual_aligned;
+    TileWalk walk = {b.warp >> 2, (p.tile_n / 32 - (b.warp >> 2) + SUBS - 1) / SUBS, false};
+    PairWalk items(p, b.pair);
+    PairItem item, ahead;
+    bool more = items.take(p, b.pair, ahead);
+    float next[GROUPS];
+    if (more) load_next_columns(p.finish.bias, p.finish.bias_bf16, walk, ahead.tile_n * p.tile_n, p.n, lane, next);
+    int sets = 0;
+    while (more) {
+        item = ahead;
+        const int n0 = item.tile_n * p.tile_n, row0 = item.tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32;
+        put_next_columns(next, lane, bias);
+        more = items.take(p, b.pair, ahead);
+        if (more) load_next_columns(p.finish.bias, p.finish.bias_bf16, walk, ahead.tile_n * p.tile_n, p.n, lane, next);
+        const int chunks = CHUNKED ? (item.last - item.first + p.chunk - 1) / p.chunk : 1;
+        const bool units_of = by_units && item.slot < 0;
+        uint4 units[4];
+        float total[CHUNKED ? GROUPS : 1][32];
+        if constexpr (CHUNKED) {
+#pragma unroll
+            for (int s = 0; s < GROUPS; ++s)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) total[s][i] = 0.0f;
+        }
+        for (int chunk = 0; chunk < chunks; ++chunk, ++sets) {
+            walk.down = !(sets & 1);
+            if (!CHUNKED && units_of && walk.own > 0) load_residual(p, row0, n0 + walk.column(walk.slot(0)), lane, units);
+            if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
+            fence_after_sync();
+            const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
+            const auto read_over = [&] {
+                fence_before_sync();
+                if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                __syncwarp();
+            };
+            uint32_t r[32];
+            if constexpr (CHUNKED) {
+#pragma unroll
+                for (int t = 0; t < GROUPS; ++t) {
+                    if (t < walk.own) {
+                        tmem_load32(from + walk.column(walk.slot(t)), r);
+                        tmem_wait(r);
+                    }
+                    // shared columns have been read after the first group, all of a set that shares none after the last
+                    if (t == (b.apart ? GROUPS - 1 : 0)) read_over();
+                    if (t >= walk.own) continue;
+#pragma unroll
+                    for (int s = 0; s < GROUPS; ++s)  // the total's registers need fixed indexes
+                        if (walk.slot(t) == s) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) total[s][i] += __uint_as_float(r[i]);
+                        }
+                }
+            } else {
+#pragma unroll 1
+                for (int t = 0; t < walk.own; ++t) {
+                    tmem_load32(from + walk.column(walk.slot(t)), r);
+                    tmem_wait(r);
+                    if (t == (b.apart ? walk.own - 1 : 0)) read_over();
+                    finish_linear(p, c_map, item, row0, quarter, b.rank, lane, walk.group(t), r, bias[walk.slot(t)], units, units_of, staging, buffer);
+                    if (units_of && t + 1 < walk.own) load_residual(p, row0, n0 + walk.column(walk.slot(t + 1)), lane, units);
+                }
+            }
+        }
+        if constexpr (CHUNKED) {
+#pragma unroll
+            for (int s = 0; s < GROUPS; ++s) {
+                if (s >= walk.own) break;
+                const int group = SUBS * s + walk.sub;
+                if (units_of) load_residual(p, row0, n0 + group * 32, lane, units);
+                finish_linear(p, c_map, item, row0, quarter, b.rank, lane, group, reinterpret_cast<const uint32_t *>(total[s]), bias[s], units,
+                              units_of, staging, buffer);
+            }
+        }
+    }
+    ptx::bulk_wait_all();
+}
+
+template <bool CHUNKED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGUE_WARPS), 1)
+    linear_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                       const __grid_constant__ CUtensorMap c_map, const __grid_constant__ DenseArgs<Linear> p)
+{
+    __shared__ __align__(16) float columns[EPILOGUE_WARPS][GROUPS][32];
+    run_pair<CHUNKED, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) { linear_epilogue<CHUNKED>(p, c_map, b, columns); });
+}
 
 // Nothing is contracted: every sum is zero.
 template <typename T> __global__ void __launch_bounds__(256) empty_sums_kernel(T *y, long long y_row, long long m, int n, Linear finish)
@@ -122,7 +356,7 @@ struct PackArgs : ProductArgs {
 // ahead of another, so that two sets of maxima do.
 struct PackShared {
     uint64_t exchanged;
-    unsigned maxima[2][2][2][PAIR_EPILOGUE_WARPS];  // [exchange][block][of act(a), of a]
+    unsigned maxima[2][2][2][EPILOGUE_WARPS];  // [exchange][block][of act(a), of a]
 };
 
 // 32 codes of a row, of which the first `left` are the matrix's.
@@ -168,10 +402,10 @@ __device__ __forceinline__ float larger3(float most, f32x2 p)  // NaN does not c
     asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(v.x), "f"(v.y));
     return most;
 }
-__device__ __forceinline__ float larger_magnitude(float most, f32x2 p)
+__device__ __forceinline__ float larger_magnitude(float most, f32x2 p)  // NaN stays
 {
     const float2 v = values_of(p);
-    asm("max.abs.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(v.x), "f"(v.y));
+    asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(v.x), "f"(v.y));
     return most;
 }
 __device__ __forceinline__ unsigned finite_magnitudes(unsigned most, f32x2 p)
@@ -206,97 +440,79 @@ struct Exchange {
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                most[b][q] = b < blocks ? __reduce_max_sync(0xffffffffu, shared.maxima[count & 1][b][q][lane & 7]) : 0u;
+                most[b][q] = b < blocks ? __reduce_max_sync(0xffffffffu, shared.maxima[count & 1][b][q][lane & (EPILOGUE_WARPS - 1)]) : 0u;
         ++count;
         return true;
     }
 };
 
-// A warp's way through a tile: its quarter of the rows, every other group of 32 columns, from the columns that the
-// sets of sums share.
-struct TileWalk {
-    int own, blocks;  // groups of this warp, blocks of 128 columns
-    int odd;
-    bool down;
-    __device__ __forceinline__ int group(int t) const { return 2 * (down ? own - 1 - t : t) + odd; }
-};
-
 template <int ACTIVATION>
-__device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock &b, PackShared &shared,
-                                              float (*bias)[PAIR_MAX_N / 64][32])
+__device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock &b, PackShared &shared, float (*columns)[GROUPS][32])
 {
     constexpr bool GROWS = ACTIVATION == DIPACO_ACTIVATION_GELU || ACTIVATION == DIPACO_ACTIVATION_SILU;
     const int lane = b.lane, quarter = b.warp & 3;
+    float (*bias)[32] = columns[b.warp];
     const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&b.sums_read[0]), 0),
                                    cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
-    const int scale_cols = (p.n + 127) / 128;
+    const int scale_cols = (p.n + 127) / 128, blocks = p.tile_n / 128;
     const bool keep = p.second.codes != nullptr;
-    TileWalk walk = {p.tile_n / 64, p.tile_n / 128, b.warp >> 2, false};
+    TileWalk walk = {b.warp >> 2, blocks * OF_BLOCK, false};
     Exchange exchange = {shared, b.warp, lane};
-    PairWalk items(p, b.pair);
-    PairItem item;
-    for (int sets = 0; items.take(p, b.pair, item); ++sets) {
-        const int n0 = item.tile_n * p.tile_n, row0 = item.tile_m * PAIR_ROWS + (int)b.rank * 128;
+    float next[GROUPS];
+    int tile_m, tile_n, sets = 0;
+    PairWalk::place(p, b.pair, tile_m, tile_n);
+    load_next_columns(p.bias, p.bias_bf16, walk, tile_n * p.tile_n, p.n, lane, next);
+    for (int tile = b.pair; tile < p.whole_tiles; tile += p.pairs, ++sets) {  // as PairWalk takes them
+        const int n0 = tile_n * p.tile_n, row0 = tile_m * PAIR_ROWS + (int)b.rank * 128;
         const int row = row0 + quarter * 32 + lane;
-        float (*columns_bias)[32] = bias[b.warp];
-        __syncwarp();
-#pragma unroll
-        for (int t = 0; t < PAIR_MAX_N / 64; ++t) {
-            const int col = n0 + (2 * t + walk.odd) * 32 + lane;
-            columns_bias[t][lane] = t < walk.own && p.bias && col < p.n ? load_param(p.bias, p.bias_bf16, col) : 0.0f;
+        put_next_columns(next, lane, bias);
+        if (tile + p.pairs < p.whole_tiles) {
+            PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
+            load_next_columns(p.bias, p.bias_bf16, walk, tile_n * p.tile_n, p.n, lane, next);
         }
-        __syncwarp();
         if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
         fence_after_sync();
         const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
         walk.down = !(sets & 1);
-        const uint32_t read_bar = read_bars[sets & 1];
-        // a of a group
-        const auto with_bias = [&](int group, const uint32_t *r, f32x2 *a) {
-            const float4 *add = reinterpret_cast<const float4 *>(columns_bias[group >> 1]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 w = add[i];
-                a[2 * i] = add2(pair_of(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1])), pair_of(w.x, w.y));
-                a[2 * i + 1] = add2(pair_of(__uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3])), pair_of(w.z, w.w));
-            }
-        };
-        uint32_t held[32];  // the group whose columns the next tile's products overwrite
+        uint32_t held[32], r[32];  // held: the first group, whose columns the next tile's products overwrite
         f32x2 a[16];
+        tmem_load32(from + walk.column(walk.slot(0)), held);
+        tmem_wait(held);
+        if (!b.apart) {
+            fence_before_sync();
+            if (lane == 0) arrive_remote(read_bars[sets & 1]);
+            __syncwarp();
+        }
         unsigned most[2][2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half >= walk.blocks) break;
+        add_columns(bias[walk.slot(0)], held, a);
+#pragma unroll 1
+        for (int k = 0; k < blocks; ++k) {
             float top = 0.0f, magnitude = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int group = walk.group(2 * half + i);
-                uint32_t other[32];
-                uint32_t *r = half + i == 0 ? held : other;
-                tmem_load32(from + group * 32, r);
-                tmem_wait(r);
-                if (half + i == 0 && !b.apart) {
-                    fence_before_sync();
-                    if (lane == 0) arrive_remote(read_bar);
-                    __syncwarp();
-                }
-                with_bias(group, r, a);
+            for (int i = 0; i < OF_BLOCK; ++i) {
+                const int t = k * OF_BLOCK + i;
+                if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     if (ACTIVATION != DIPACO_ACTIVATION_NONE) top = larger3(top, a[j]);
                     magnitude = larger_magnitude(magnitude, a[j]);
                 }
+                if (t + 1 < walk.own) {
+                    tmem_wait(r);
+                    add_columns(bias[walk.slot(t + 1)], r, a);
+                }
             }
             if (row >= p.m) top = magnitude = 0.0f;  // the bias is not the matrix's there
-            exchange.put(walk.down ? walk.blocks - 1 - half : half, __float_as_uint(top), __float_as_uint(magnitude));
+            exchange.put(walk.down ? blocks - 1 - k : k, __float_as_uint(top), __float_as_uint(magnitude));
         }
-        if (!exchange.meet(walk.blocks, most)) return;
-        bool careful = false;
+        if (!exchange.meet(blocks, most)) return;
+        bool careful = false, in_pairs = true;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            if (k >= walk.blocks || n0 + k * 128 >= p.n || row0 >= p.m) continue;
+            if (k >= blocks || n0 + k * 128 >= p.n || row0 >= p.m) continue;
             careful |= most[k][1] >= 0x7f800000u;
             if (GROWS) careful |= most[k][0] < __float_as_uint(grows_from<ACTIVATION>());
+            in_pairs &= most[k][1] <= __float_as_uint(pairs_up_to<ACTIVATION>());
             if (ACTIVATION == DIPACO_ACTIVATION_NONE)
                 most[k][0] = most[k][1];
             else
@@ -304,18 +520,16 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
         }
         if (careful) {  // the same for all epilogue warps of the block
 #pragma unroll 1
-            for (int half = 0; half < walk.blocks; ++half) {
+            for (int k = 0; k < blocks; ++k) {
                 unsigned of_y = 0u, of_a = 0u;
 #pragma unroll 1
-                for (int i = 0; i < 2; ++i) {
-                    const int group = walk.group(2 * half + i);
-                    if (half + i == 0) {
-                        with_bias(group, held, a);
+                for (int t = k * OF_BLOCK; t < (k + 1) * OF_BLOCK; ++t) {
+                    if (t == 0) {
+                        add_columns(bias[walk.slot(0)], held, a);
                     } else {
-                        uint32_t r[32];
-                        tmem_load32(from + group * 32, r);
+                        tmem_load32(from + walk.column(walk.slot(t)), r);
                         tmem_wait(r);
-                        with_bias(group, r, a);
+                        add_columns(bias[walk.slot(t)], r, a);
                     }
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
@@ -324,56 +538,60 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
                     }
                 }
                 if (row >= p.m) of_y = of_a = 0u;
-                exchange.put(walk.down ? walk.blocks - 1 - half : half, of_y, of_a);
+                exchange.put(walk.down ? blocks - 1 - k : k, of_y, of_a);
             }
-            if (!exchange.meet(walk.blocks, most)) return;
+            if (!exchange.meet(blocks, most)) return;
         }
-        unsigned bytes[2][2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            bytes[k][0] = scale_byte(most[k][0]);
-            bytes[k][1] = scale_byte(most[k][1]);
+            most[k][0] = scale_byte(most[k][0]);
+            most[k][1] = scale_byte(most[k][1]);
         }
-        if (b.warp == 0 && lane < walk.blocks && n0 + lane * 128 < p.n && row0 < p.m) {
+        if (b.warp == 0 && lane < blocks && n0 + lane * 128 < p.n && row0 < p.m) {
             const long long at = (long long)(row0 / 128) * scale_cols + n0 / 128 + lane;
-            p.first.scales[at] = (uint8_t)(lane ? bytes[1][0] : bytes[0][0]);
-            if (keep) p.second.scales[at] = (uint8_t)(lane ? bytes[1][1] : bytes[0][1]);
+            p.first.scales[at] = (uint8_t)(lane ? most[1][0] : most[0][0]);
+            if (keep) p.second.scales[at] = (uint8_t)(lane ? most[1][1] : most[0][1]);
         }
-        const auto store = [&](int group) {
-            const int left = p.n - (n0 + group * 32);
-            const bool inside = row < p.m && left > 0;
-            const float by_y = scale_reciprocal(group >> 2 ? bytes[1][0] : bytes[0][0]);
+        add_columns(bias[walk.slot(0)], held, a);
+#pragma unroll 1
+        for (int t = 0; t < walk.own; ++t) {
+            const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
+            const bool inside = row < p.m && left > 0, second = slot >= OF_BLOCK;
+            if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
             unsigned w[8];
             if (keep) {
-                const float by_a = scale_reciprocal(group >> 2 ? bytes[1][1] : bytes[0][1]);
+                const float by = scale_reciprocal(second ? most[1][1] : most[0][1]);
                 if (careful)
-                    encode32<true>(a, by_a, w);
+                    encode32<true>(a, by, w);
                 else
-                    encode32<false>(a, by_a, w);
-                if (inside) store_codes(p.second, row, n0 + group * 32, left, w);
+                    encode32<false>(a, by, w);
+                if (inside) store_codes(p.second, row, col, left, w);
             }
+            const float by = scale_reciprocal(second ? most[1][0] : most[0][0]);
+            if (careful || !in_pairs) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) a[j] = activate<ACTIVATION>(a[j]);
-            if (careful)
-                encode32<true>(a, by_y, w);
-            else
-                encode32<false>(a, by_y, w);
-            if (inside) store_codes(p.first, row, n0 + group * 32, left, w);
-        };
-        with_bias(walk.group(0), held, a);
-        store(walk.group(0));
-#pragma unroll 1
-        for (int t = 1; t < walk.own; ++t) {
-            uint32_t r[32];
-            tmem_load32(from + walk.group(t) * 32, r);
-            tmem_wait(r);
-            if (b.apart && t + 1 == walk.own) {
-                fence_before_sync();
-                if (lane == 0) arrive_remote(read_bar);
-                __syncwarp();
+                for (int j = 0; j < 16; ++j) a[j] = activate<ACTIVATION>(a[j]);
+                encode32<true>(a, by, w);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) a[j] = activate_in_pairs<ACTIVATION>(a[j]);
+                encode32<false>(a, by, w);
             }
-            with_bias(walk.group(t), r, a);
-            store(walk.group(t));
+            if (inside) store_codes(p.first, row, col, left, w);
+            if (t + 1 < walk.own) {
+                tmem_wait(r);
+                if (b.apart && t + 2 == walk.own) {
+                    fence_before_sync();
+                    if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                    __syncwarp();
+                }
+                add_columns(bias[walk.slot(t + 1)], r, a);
+            }
+        }
+        if (b.apart && walk.own == 1) {  // read at the start
+            fence_before_sync();
+            if (lane == 0) arrive_remote(read_bars[sets & 1]);
+            __syncwarp();
         }
     }
 }
@@ -422,158 +640,162 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
     const int lane = b.lane, quarter = b.warp & 3;
     const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&b.sums_read[0]), 0),
                                    cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
-    const int scale_cols = (p.n + 127) / 128;
-    TileWalk walk = {p.tile_n / 64, p.tile_n / 128, b.warp >> 2, false};
+    const int scale_cols = (p.n + 127) / 128, blocks = p.tile_n / 128;
+    TileWalk walk = {b.warp >> 2, blocks * OF_BLOCK, false};
     Exchange exchange = {shared, b.warp, lane};
-    PairWalk items(p, b.pair);
-    PairItem item;
-    for (int sets = 0; items.take(p, b.pair, item); ++sets) {
-        const int n0 = item.tile_n * p.tile_n, row0 = item.tile_m * PAIR_ROWS + (int)b.rank * 128;
-        const int row = row0 + quarter * 32 + lane;
-        walk.down = !(sets & 1);
-        // codes of a, two units of 16 for a group (rows of codes are padded to whole units), and their scales
-        const auto load_codes = [&](int group, uint4 *codes) {
-            if constexpr (ACTIVATION == DIPACO_ACTIVATION_NONE) return;
-            const uint8_t *at = p.a_codes + row * p.a_stride + n0 + group * 32;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                codes[h] = row < p.m && n0 + group * 32 + 16 * h < p.n ? __ldcs(reinterpret_cast<const uint4 *>(at + 16 * h))
-                                                                       : make_uint4(0u, 0u, 0u, 0u);
-        };
-        uint4 codes[2] = {};
-        load_codes(walk.group(0), codes);
-        float scales[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int block = n0 / 128 + k;
-            scales[k] = ACTIVATION != DIPACO_ACTIVATION_NONE && k < walk.blocks && block < scale_cols && row0 < p.m
-                            ? scale_value(p.of_a_scales[(long long)(row0 / 128) * scale_cols + block])
-                            : 0.0f;
+    // a group's codes of a, two units of 16 (rows of codes are padded to whole units), and their scale
+    const auto load_codes = [&](int row, int col, uint4 *codes, float &scale) {
+        codes[0] = codes[1] = make_uint4(0u, 0u, 0u, 0u);
+        scale = 0.0f;
+        if constexpr (ACTIVATION != DIPACO_ACTIVATION_NONE) {
+            const uint8_t *at = p.a_codes + row * p.a_stride + col;
+            if (row < p.m && col < p.n) codes[0] = __ldcs(reinterpret_cast<const uint4 *>(at));
+            if (row < p.m && col + 16 < p.n) codes[1] = __ldcs(reinterpret_cast<const uint4 *>(at + 16));
+            if (row < p.m && col < p.n) scale = scale_value(p.of_a_scales[(long long)(row / 128) * scale_cols + col / 128]);
         }
+    };
+    int tile_m, tile_n, sets = 0;
+    PairWalk::place(p, b.pair, tile_m, tile_n);
+    uint4 codes[2];
+    float scale;
+    walk.down = true;
+    load_codes(tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32 + lane, tile_n * p.tile_n + walk.column(walk.slot(0)), codes, scale);
+    for (int tile = b.pair; tile < p.whole_tiles; tile += p.pairs, ++sets) {  // as PairWalk takes them
+        const int n0 = tile_n * p.tile_n, row0 = tile_m * PAIR_ROWS + (int)b.rank * 128;
+        const int row = row0 + quarter * 32 + lane;
         if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
         fence_after_sync();
         const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
-        const uint32_t read_bar = read_bars[sets & 1];
-        f32x2 held[16];
+        walk.down = !(sets & 1);
+        f32x2 held[16], v[16];  // held: the first group's results, as the next tile's products overwrite its columns
         unsigned most[2][2];
+        float magnitude = 0.0f;
+#pragma unroll 1
+        for (int t = 0; t < walk.own; ++t) {
+            const int slot = walk.slot(t);
+            uint32_t r[32];
+            tmem_load32(from + walk.column(slot), r);
+            const unsigned words[8] = {codes[0].x, codes[0].y, codes[0].z, codes[0].w, codes[1].x, codes[1].y, codes[1].z, codes[1].w};
+            const f32x2 scales = pair_of(scale);
+            if (t + 1 < walk.own) {
+                load_codes(row, n0 + walk.column(walk.slot(t + 1)), codes, scale);
+            } else if (tile + p.pairs < p.whole_tiles) {  // the next tile's first
+                PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
+                TileWalk then = walk;
+                then.down = !walk.down;
+                load_codes(tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32 + lane, tile_n * p.tile_n + then.column(then.slot(0)), codes, scale);
+            }
+            tmem_wait(r);
+            if (t == 0 && !b.apart) {
+                fence_before_sync();
+                if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                __syncwarp();
+            }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (half >= walk.blocks) break;
-            float magnitude = 0.0f;
+            for (int j = 0; j < 16; ++j) {
+                v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                if constexpr (ACTIVATION != DIPACO_ACTIVATION_NONE)
+                    v[j] = mul2(v[j], slope<ACTIVATION>(mul2(decode_pair(words[j / 2] >> 16 * (j & 1)), scales)));
+                magnitude = larger_magnitude(magnitude, v[j]);
+            }
+            if (row >= p.m) {  // zero times a NaN of the weights
+                magnitude = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int t = 2 * half + i, group = walk.group(t);
-                uint32_t r[32];
-                tmem_load32(from + group * 32, r);
-                tmem_wait(r);
-                if (t == 0 && !b.apart) {
-                    fence_before_sync();
-                    if (lane == 0) arrive_remote(read_bar);
-                    __syncwarp();
-                }
-                const unsigned words[8] = {codes[0].x, codes[0].y, codes[0].z, codes[0].w,
-                                           codes[1].x, codes[1].y, codes[1].z, codes[1].w};
-                if (t + 1 < walk.own) load_codes(walk.group(t + 1), codes);
-                const f32x2 scale = pair_of(group >> 2 ? scales[1] : scales[0]);
-                f32x2 other[16];
-                f32x2 *v = t == 0 ? held : other;
+                for (int j = 0; j < 16; ++j) v[j] = 0ull;
+            }
+            if (t > 0) {
+                tmem_store32(from + walk.column(slot), v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) held[j] = v[j];
+            }
+            if (p.row_sums) {
+                float f[32];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-                    if constexpr (ACTIVATION != DIPACO_ACTIVATION_NONE)
-                        v[j] = mul2(v[j], slope<ACTIVATION>(mul2(decode_pair(words[j / 2] >> 16 * (j & 1)), scale)));
-                    if (row >= p.m) v[j] = 0ull;
-                    magnitude = larger_magnitude(magnitude, v[j]);
+                    const float2 w = values_of(v[j]);
+                    f[2 * j] = w.x;
+                    f[2 * j + 1] = w.y;
                 }
-                if (t > 0) tmem_store32(from + group * 32, v);
-                if (p.row_sums) {
-                    float f[32];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float2 w = values_of(v[j]);
-                        f[2 * j] = w.x;
-                        f[2 * j + 1] = w.y;
-                    }
-                    sums[sets & 1][group][quarter][lane] = column_sums(f, lane);
-                }
+                sums[sets & 1][walk.group(t)][quarter][lane] = column_sums(f, lane);
             }
-            exchange.put(walk.down ? walk.blocks - 1 - half : half, __float_as_uint(magnitude), 0u);
+            if ((t + 1) % OF_BLOCK == 0) {
+                exchange.put(slot / OF_BLOCK, __float_as_uint(magnitude), 0u);
+                magnitude = 0.0f;
+            }
         }
         tmem_stored();
-        if (!exchange.meet(walk.blocks, most)) return;
+        if (!exchange.meet(blocks, most)) return;
         if (p.row_sums && b.warp < p.tile_n / 32 && row0 < p.m && n0 + b.warp * 32 + lane < p.n) {
             const float(*s)[32] = sums[sets & 1][b.warp];
             p.row_sums[(long long)(row0 / 128) * p.n + n0 + b.warp * 32 + lane] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
         }
+        // the results of the t-th group
+        const auto results = [&](int t) {
+            if (t == 0) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = held[j];
+            } else {
+                uint32_t r[32];
+                tmem_load32(from + walk.column(walk.slot(t)), r);
+                tmem_wait(r);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+            }
+        };
         const bool careful = most[0][0] >= 0x7f800000u || most[1][0] >= 0x7f800000u;
         if (careful) {  // the same for all epilogue warps of the block
 #pragma unroll 1
-            for (int half = 0; half < walk.blocks; ++half) {
+            for (int k = 0; k < blocks; ++k) {
                 unsigned finite = 0u;
 #pragma unroll 1
-                for (int i = 0; i < 2; ++i) {
-                    const int group = walk.group(2 * half + i);
-                    if (half + i == 0) {
+                for (int t = k * OF_BLOCK; t < (k + 1) * OF_BLOCK; ++t) {
+                    results(t);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) finite = finite_magnitudes(finite, held[j]);
-                    } else {
-                        uint32_t r[32];
-                        tmem_load32(from + group * 32, r);
-                        tmem_wait(r);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) finite = max(finite, finite_magnitude(__uint_as_float(r[j])));
-                    }
+                    for (int j = 0; j < 16; ++j) finite = finite_magnitudes(finite, v[j]);
                 }
-                exchange.put(walk.down ? walk.blocks - 1 - half : half, finite, 0u);
+                exchange.put(walk.down ? blocks - 1 - k : k, finite, 0u);
             }
-            if (!exchange.meet(walk.blocks, most)) return;
+            if (!exchange.meet(blocks, most)) return;
         }
         const unsigned bytes[2] = {scale_byte(most[0][0]), scale_byte(most[1][0])};
-        if (b.warp == 0 && lane < walk.blocks && n0 + lane * 128 < p.n && row0 < p.m)
+        if (b.warp == 0 && lane < blocks && n0 + lane * 128 < p.n && row0 < p.m)
             p.first.scales[(long long)(row0 / 128) * scale_cols + n0 / 128 + lane] = (uint8_t)(lane ? bytes[1] : bytes[0]);
-        const auto store = [&](int group, const f32x2 *v) {
-            const int left = p.n - (n0 + group * 32);
-            const float by = scale_reciprocal(group >> 2 ? bytes[1] : bytes[0]);
+#pragma unroll 1
+        for (int t = 0; t < walk.own; ++t) {
+            const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
+            results(t);
+            if (b.apart && t + 1 == walk.own) {
+                fence_before_sync();
+                if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                __syncwarp();
+            }
+            if (left <= 0) continue;
+            const float by = scale_reciprocal(slot >= OF_BLOCK ? bytes[1] : bytes[0]);
             unsigned w[8];
             if (careful)
                 encode32<true>(v, by, w);
             else
                 encode32<false>(v, by, w);
-            if (row < p.m && left > 0) store_codes(p.first, row, n0 + group * 32, left, w);
-        };
-        store(walk.group(0), held);
-#pragma unroll 1
-        for (int t = 1; t < walk.own; ++t) {
-            uint32_t r[32];
-            tmem_load32(from + walk.group(t) * 32, r);
-            tmem_wait(r);
-            if (b.apart && t + 1 == walk.own) {
-                fence_before_sync();
-                if (lane == 0) arrive_remote(read_bar);
-                __syncwarp();
-            }
-            f32x2 v[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-            store(walk.group(t), v);
+            if (row < p.m) store_codes(p.first, row, col, left, w);
         }
     }
 }
 
 template <int ACTIVATION, bool BACK>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGUE_WARPS), 1)
     packed_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                        const __grid_constant__ PackArgs p)
 {
     __shared__ PackShared shared;
     // biases of the warps' columns; or sums over rows of the tile's columns, for two tiles
-    __shared__ __align__(16) float columns[BACK ? 2 * PAIR_MAX_N * 4 : PAIR_EPILOGUE_WARPS * PAIR_MAX_N / 2];
-    if (threadIdx.x == 64) ptx::mbar_init(&shared.exchanged, PAIR_EPILOGUE_WARPS);  // seen after run_pair's first barrier
-    run_pair<false>(a_map, b_map, p, [&](const PairBlock &b) {
+    __shared__ __align__(16) float columns[BACK ? 2 * PAIR_MAX_N * 4 : EPILOGUE_WARPS * GROUPS * 32];
+    if (threadIdx.x == 64) ptx::mbar_init(&shared.exchanged, EPILOGUE_WARPS);  // seen after run_pair's first barrier
+    run_pair<false, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) {
         if constexpr (BACK)
             back_epilogue<ACTIVATION>(p, b, shared, reinterpret_cast<float(*)[PAIR_MAX_N / 32][4][32]>(columns));
         else
-            pack_epilogue<ACTIVATION>(p, b, shared, reinterpret_cast<float(*)[PAIR_MAX_N / 64][32]>(columns));
+            pack_epilogue<ACTIVATION>(p, b, shared, reinterpret_cast<float(*)[GROUPS][32]>(columns));
     });
 }
 
@@ -644,7 +866,7 @@ template <bool BACK> int launch_packed(const CUtensorMap &a_map, const CUtensorM
                         : activation == DIPACO_ACTIVATION_GELU ? packed_pair_kernel<DIPACO_ACTIVATION_GELU, BACK>
                                                                : packed_pair_kernel<DIPACO_ACTIVATION_NONE, BACK>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM) != cudaSuccess) return launch_status();
-    kernel<<<2 * p.pairs, PAIR_THREADS, PAIR_SMEM, stream>>>(a_map, b_map, p);
+    kernel<<<2 * p.pairs, pair_threads(EPILOGUE_WARPS), PAIR_SMEM, stream>>>(a_map, b_map, p);
     return launch_status();
 }
 
@@ -699,7 +921,7 @@ int dipaco_packed_linear(const dipaco_packed *x, const dipaco_packed *w, const v
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const Linear finish = {bias, residual, residual_stride, activation, bias_dtype == DIPACO_BF16, (uintptr_t)bias % 16 == 0,
+    const Linear finish = {bias, residual, residual_stride, activation, bias_dtype == DIPACO_BF16,
                            dtype == DIPACO_BF16, rows_aligned16(residual, residual_stride, m, dense_size(dtype))};
     if (k == 0) {
         const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(m, 256) * n, 148 * 8);
@@ -710,7 +932,8 @@ int dipaco_packed_linear(const dipaco_packed *x, const dipaco_packed *w, const v
         return launch_status();
     }
     if (few) return launch_few(x, w, y, y_stride, dtype, false, finish, stream);
-    return launch_product(x, w, false, true, y, y_stride, dtype, false, finish, workspace, stream);
+    const DenseKernels<Linear> kernels = {linear_pair_kernel<false>, linear_pair_kernel<true>, pair_threads(EPILOGUE_WARPS)};
+    return launch_product(x, w, false, true, y, y_stride, dtype, false, finish, kernels, workspace, stream);
 }
 
 int dipaco_packed_linear_pack_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes)
@@ -737,7 +960,7 @@ int dipaco_packed_linear_pack(const dipaco_packed *x, const dipaco_packed *w, co
     if (!scope.ok) return DIPACO_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (need > 0) {
-        const Linear finish = {bias, nullptr, 0, DIPACO_ACTIVATION_NONE, bias_dtype == DIPACO_BF16, (uintptr_t)bias % 16 == 0, false, false};
+        const Linear finish = {bias, nullptr, 0, DIPACO_ACTIVATION_NONE, bias_dtype == DIPACO_BF16, false, false};
         float *sums = static_cast<float *>(workspace);
         const int64_t stride = ceil_div(n, 4) * 4;
         if (k == 0) {

@@ -268,7 +268,7 @@ constexpr int PAIR_STAGING_BYTES = 2048;  // of one: 32 rows of 64 bytes
 constexpr int PAIR_STAGING_AT = PAIR_STAGES * PAIR_STAGE_BYTES;
 constexpr int PAIR_WORDS_AT = PAIR_STAGING_AT + PAIR_EPILOGUE_WARPS * PAIR_STAGING * PAIR_STAGING_BYTES;
 constexpr int PAIR_SMEM = PAIR_WORDS_AT + 2 * PAIR_WORDS_SET + 1024;
-constexpr int PAIR_THREADS = (PAIR_EPILOGUE_WARPS + 3) * 32;  // + loads, products, scale words
+constexpr int pair_threads(int epilogue_warps) { return (epilogue_warps + 3) * 32; }  // + loads, products, scale words
 // Scale columns are written again five quads later, when the last step of the quad that had them is done:
 // the step that begins the new quad has been loaded where the step PAIR_STAGES before it was, which is
 // thus done, and only quads of single steps (short contractions) are closer together than that.
@@ -385,7 +385,6 @@ __device__ __forceinline__ void finish_columns(const DenseArgs<F> &p, const CUte
     }
     const int row0 = item.tile_m * PAIR_ROWS + (int)rank * 128 + quarter * 32;
     const int col0 = item.tile_n * p.tile_n + c0;
-    if constexpr (!F::NOTHING) p.finish.columns(v, row0 + lane, col0, p.m, p.n);
     if (p.store_by_tma) {
         // rows of 64 bytes in the copy engine's swizzle of that width: no bank conflicts
         const int parts = p.c_bf16 ? 1 : 2;
@@ -458,8 +457,8 @@ struct PairBlock {
 };
 
 // A block of a pair: loads, scale words and products each by a warp, and epilogue(PairBlock) by the first
-// PAIR_EPILOGUE_WARPS.
-template <bool CHUNKED, class Epilogue>
+// EPILOGUE_WARPS.
+template <bool CHUNKED, int EPILOGUE_WARPS, class Epilogue>
 __device__ __forceinline__ void run_pair(const CUtensorMap &a_map, const CUtensorMap &b_map, const ProductArgs &p,
                                          const Epilogue &epilogue)
 {
@@ -481,7 +480,7 @@ __device__ __forceinline__ void run_pair(const CUtensorMap &a_map, const CUtenso
         }
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(&sums_full[s], 1);
-            ptx::mbar_init(&sums_read[s], 2 * PAIR_EPILOGUE_WARPS);
+            ptx::mbar_init(&sums_read[s], 2 * EPILOGUE_WARPS);
             ptx::mbar_init(&words_full[s], 2);  // of either block
             ptx::mbar_init(&words_empty[s], 1);
         }
@@ -496,7 +495,7 @@ __device__ __forceinline__ void run_pair(const CUtensorMap &a_map, const CUtenso
     const bool apart = second_set >= p.tile_n;
     const int half_n = p.tile_n / 2;
 
-    if (warp == PAIR_EPILOGUE_WARPS) {
+    if (warp == EPILOGUE_WARPS) {
         // ---- loads: this block's halves of A and B
         const unsigned b_bytes = p.transpose_b ? half_n * STEP : PAIR_OPERAND_BYTES;
         PairWalk walk(p, pair);
@@ -533,7 +532,7 @@ __device__ __forceinline__ void run_pair(const CUtensorMap &a_map, const CUtenso
         }
         if (!ok)  // a wait ran out: let the copies in flight land before the block ends
             for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    } else if (warp == PAIR_EPILOGUE_WARPS + 2) {
+    } else if (warp == EPILOGUE_WARPS + 2) {
         // ---- scale words of this block's tensor memory
         const int a_blocks = (p.m + 127) / 128, b_blocks = (p.n + 127) / 128;
         PairWalk walk(p, pair);
@@ -598,7 +597,7 @@ __device__ __forceinline__ void run_pair(const CUtensorMap &a_map, const CUtenso
             ok = warp_wait(&words_empty[set], phase ^ 1, 8);
             if (++set == 2) { set = 0; phase ^= 1; }
         }
-    } else if (warp == PAIR_EPILOGUE_WARPS + 1) {
+    } else if (warp == EPILOGUE_WARPS + 1) {
         // ---- products: one thread of the first block issues them for both.  This warp's own instructions
         // bound the kernel if there are many: what can be is done once for a quad, and whether the next
         // step has been loaded is asked for while this one is issued.
@@ -784,11 +783,11 @@ __device__ __forceinline__ void dense_epilogue(const DenseArgs<F> &p, const CUte
 }
 
 template <bool CHUNKED, class F>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PAIR_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(PAIR_EPILOGUE_WARPS), 1)
     pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                 const __grid_constant__ CUtensorMap c_map, const __grid_constant__ DenseArgs<F> p)
 {
-    run_pair<CHUNKED>(a_map, b_map, p, [&](const PairBlock &b) { dense_epilogue<CHUNKED>(p, c_map, b); });
+    run_pair<CHUNKED, PAIR_EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) { dense_epilogue<CHUNKED>(p, c_map, b); });
 }
 
 // Tiles whose steps were dealt out: their partial sums in the order of the steps.  A block joins 32
@@ -1099,15 +1098,12 @@ int launch_few(const dipaco_packed *a, const dipaco_packed *b, void *c, int64_t 
     return launch_status();
 }
 
-template <bool CHUNKED, class F>
-int launch_pairs(const CUtensorMap &a_map, const CUtensorMap &b_map, const CUtensorMap &c_map, const DenseArgs<F> &p,
-                 int pairs, cudaStream_t stream)
-{
-    if (cudaFuncSetAttribute(pair_kernel<CHUNKED, F>, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM) != cudaSuccess)
-        return launch_status();
-    pair_kernel<CHUNKED, F><<<2 * pairs, PAIR_THREADS, PAIR_SMEM, stream>>>(a_map, b_map, c_map, p);
-    return launch_status();
-}
+// The kernels of a product that stores to a dense matrix, whose sums are taken in one go or in chunks.
+template <class F> struct DenseKernels {
+    using Kernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, DenseArgs<F>);
+    Kernel whole, chunked;
+    int threads;
+};
 
 inline void set_operands(ProductArgs &p, const dipaco_packed *a, const dipaco_packed *b, bool transpose_a, bool transpose_b)
 {
@@ -1125,7 +1121,8 @@ inline void set_operands(ProductArgs &p, const dipaco_packed *a, const dipaco_pa
 // The product of checked operands with something to contract, finished and stored to C.
 template <class F>
 int launch_product(const dipaco_packed *a, const dipaco_packed *b, bool transpose_a, bool transpose_b, void *c,
-                   int64_t c_stride, int dtype, bool accumulate, const F &finish, void *workspace, cudaStream_t stream)
+                   int64_t c_stride, int dtype, bool accumulate, const F &finish, const DenseKernels<F> &kernels,
+                   void *workspace, cudaStream_t stream)
 {
     DenseArgs<F> p = {};
     set_operands(p, a, b, transpose_a, transpose_b);
@@ -1153,9 +1150,10 @@ int launch_product(const dipaco_packed *a, const dipaco_packed *b, bool transpos
     if (p.store_by_tma && !result_map(&c_map, c, m, p.whole_n, m == 1 ? ceil_div(n, 8) * 8 : c_stride, dtype)) return DIPACO_ECUDA;
     p.chunk = p.c_bf16 ? CHUNK_BF16 : CHUNK_F32;
     const bool chunked = !p.c_bf16 || p.steps > p.chunk;
-    if (const int rc = chunked ? launch_pairs<true>(a_map, b_map, c_map, p, plan.pairs, stream)
-                               : launch_pairs<false>(a_map, b_map, c_map, p, plan.pairs, stream))
-        return rc;
+    const auto kernel = chunked ? kernels.chunked : kernels.whole;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM) != cudaSuccess) return launch_status();
+    kernel<<<2 * plan.pairs, kernels.threads, PAIR_SMEM, stream>>>(a_map, b_map, c_map, p);
+    if (const int rc = launch_status()) return rc;
     const int64_t dealt = (int64_t)plan.tiles_m * plan.tiles_n - plan.whole_tiles;
     if (dealt > 0)
         join_kernel<F><<<(unsigned)(dealt * 2 * (plan.tile_n / 32)), 256, 0, stream>>>(p);
