@@ -14,6 +14,7 @@
 #include "product_pairs.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace dipaco {
 namespace {
@@ -60,10 +61,11 @@ struct Linear {
     }
 };
 
-constexpr int EPILOGUE_WARPS = 8;
-constexpr int SUBS = EPILOGUE_WARPS / 4;           // warps that share a quarter of the rows
-constexpr int GROUPS = PAIR_MAX_N / 32 / SUBS;     // of 32 columns, of one warp
-constexpr int OF_BLOCK = 4 / SUBS;                 // of them in a block of 128 columns
+constexpr int EPILOGUE_WARPS = 8;                         // with 168 registers a thread: 12 and 16 spill, and are no faster
+constexpr int SUBS = EPILOGUE_WARPS / 4;                  // warps that share a quarter of the rows
+constexpr int GROUPS = (PAIR_MAX_N / 32 + SUBS - 1) / SUBS;  // of 32 columns, of one warp, at most
+constexpr int BUFFERS = 3;                                // of a warp, for results on their way out
+static_assert(EPILOGUE_WARPS * BUFFERS <= PAIR_EPILOGUE_WARPS * PAIR_STAGING, "staging");
 
 // A warp's way through a tile: its quarter of the rows, every SUBS-th group of 32 columns, first those columns that the
 // sets of sums share.
@@ -73,7 +75,14 @@ struct TileWalk {
     __device__ __forceinline__ int slot(int t) const { return down ? own - 1 - t : t; }  // which of its groups is t-th
     __device__ __forceinline__ int column(int slot) const { return (SUBS * slot + sub) * 32; }
     __device__ __forceinline__ int group(int t) const { return SUBS * slot(t) + sub; }
+    __device__ __forceinline__ int block(int t) const { return group(t) >> 2; }  // of 128 columns
+    __device__ __forceinline__ bool ends_block(int t) const { return t + 1 == own || block(t + 1) != block(t); }
 };
+__device__ __forceinline__ TileWalk make_walk(int warp, int tile_n)
+{
+    const int sub = warp >> 2;
+    return {sub, (tile_n / 32 - sub + SUBS - 1) / SUBS, false};
+}
 
 // Parameters of the warp's columns from n0 on, for all lanes to read: the next tile's are on their way while one is
 // worked on.
@@ -147,10 +156,10 @@ __device__ __forceinline__ void finish_linear(const DenseArgs<Linear> &p, const 
         for (int part = 0; part < 2; ++part) {
             if (part >= parts) break;
             const int col = col0 + part * 16;
-            asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PAIR_STAGING - 1) : "memory");  // the buffer's last
+            asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BUFFERS - 1) : "memory");  // the buffer's last
             __syncwarp();
             uint8_t *staging = buffers + buffer * PAIR_STAGING_BYTES;
-            if (++buffer == PAIR_STAGING) buffer = 0;
+            if (++buffer == BUFFERS) buffer = 0;
             const auto place = [&](int row, int unit) {
                 return reinterpret_cast<uint4 *>(staging + row * 64 + ((unit ^ ((row >> 1) & 3)) * 16));
             };
@@ -233,12 +242,12 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
 {
     const int lane = b.lane, quarter = b.warp & 3;
     float (*bias)[32] = columns[b.warp];
-    uint8_t *staging = b.aligned + PAIR_STAGING_AT + b.warp * PAIR_STAGING * PAIR_STAGING_BYTES;
+    uint8_t *staging = b.aligned + PAIR_STAGING_AT + b.warp * BUFFERS * PAIR_STAGING_BYTES;
     int buffer = 0;
     const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&b.sums_read[0]), 0),
                                    cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
     const bool by_units = p.finish.residual && p.store_by_tma && p.finish.residual_aligned;
-    TileWalk walk = {b.warp >> 2, (p.tile_n / 32 - (b.warp >> 2) + SUBS - 1) / SUBS, false};
+    TileWalk walk = make_walk(b.warp, p.tile_n);
     PairWalk items(p, b.pair);
     PairItem item, ahead;
     bool more = items.take(p, b.pair, ahead);
@@ -275,21 +284,14 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
             uint32_t r[32];
             if constexpr (CHUNKED) {
 #pragma unroll
-                for (int t = 0; t < GROUPS; ++t) {
-                    if (t < walk.own) {
-                        tmem_load32(from + walk.column(walk.slot(t)), r);
-                        tmem_wait(r);
-                    }
-                    // shared columns have been read after the first group, all of a set that shares none after the last
-                    if (t == (b.apart ? GROUPS - 1 : 0)) read_over();
-                    if (t >= walk.own) continue;
+                for (int s = 0; s < GROUPS; ++s) {  // in any order: a chunk's products take longer than this
+                    if (s >= walk.own) break;
+                    tmem_load32(from + walk.column(s), r);
+                    tmem_wait(r);
 #pragma unroll
-                    for (int s = 0; s < GROUPS; ++s)  // the total's registers need fixed indexes
-                        if (walk.slot(t) == s) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) total[s][i] += __uint_as_float(r[i]);
-                        }
+                    for (int i = 0; i < 32; ++i) total[s][i] += __uint_as_float(r[i]);
                 }
+                read_over();
             } else {
 #pragma unroll 1
                 for (int t = 0; t < walk.own; ++t) {
@@ -395,7 +397,6 @@ template <bool CAREFUL> __device__ __forceinline__ void encode32(const f32x2 *v,
         }
     }
 }
-
 __device__ __forceinline__ float larger3(float most, f32x2 p)  // NaN does not count
 {
     const float2 v = values_of(p);
@@ -430,19 +431,27 @@ struct Exchange {
             shared.maxima[count & 1][block][1][warp] = second;
         }
     }
-    // All warps' largest, once every warp has put its own; false if the wait ran out.
-    __device__ __forceinline__ bool meet(int blocks, unsigned (*most)[2])
+    __device__ __forceinline__ void arrive()
     {
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&shared.exchanged);
+    }
+    // All warps' largest, once every warp has put its own and arrived; false if the wait ran out.
+    __device__ __forceinline__ bool take(int blocks, unsigned (*most)[2])
+    {
         if (!warp_wait(&shared.exchanged, count & 1, 11)) return false;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                most[b][q] = b < blocks ? __reduce_max_sync(0xffffffffu, shared.maxima[count & 1][b][q][lane & (EPILOGUE_WARPS - 1)]) : 0u;
+                most[b][q] = b < blocks ? __reduce_max_sync(0xffffffffu, shared.maxima[count & 1][b][q][min(lane, EPILOGUE_WARPS - 1)]) : 0u;
         ++count;
         return true;
+    }
+    __device__ __forceinline__ bool meet(int blocks, unsigned (*most)[2])
+    {
+        arrive();
+        return take(blocks, most);
     }
 };
 
@@ -456,7 +465,7 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
                                    cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
     const int scale_cols = (p.n + 127) / 128, blocks = p.tile_n / 128;
     const bool keep = p.second.codes != nullptr;
-    TileWalk walk = {b.warp >> 2, blocks * OF_BLOCK, false};
+    TileWalk walk = make_walk(b.warp, p.tile_n);
     Exchange exchange = {shared, b.warp, lane};
     float next[GROUPS];
     int tile_m, tile_n, sets = 0;
@@ -466,10 +475,6 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
         const int n0 = tile_n * p.tile_n, row0 = tile_m * PAIR_ROWS + (int)b.rank * 128;
         const int row = row0 + quarter * 32 + lane;
         put_next_columns(next, lane, bias);
-        if (tile + p.pairs < p.whole_tiles) {
-            PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
-            load_next_columns(p.bias, p.bias_bf16, walk, tile_n * p.tile_n, p.n, lane, next);
-        }
         if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
         fence_after_sync();
         const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
@@ -485,27 +490,32 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
         }
         unsigned most[2][2];
         add_columns(bias[walk.slot(0)], held, a);
+        float top = 0.0f, magnitude = 0.0f;
 #pragma unroll 1
-        for (int k = 0; k < blocks; ++k) {
-            float top = 0.0f, magnitude = 0.0f;
+        for (int t = 0; t < walk.own; ++t) {
+            if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
 #pragma unroll
-            for (int i = 0; i < OF_BLOCK; ++i) {
-                const int t = k * OF_BLOCK + i;
-                if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (ACTIVATION != DIPACO_ACTIVATION_NONE) top = larger3(top, a[j]);
-                    magnitude = larger_magnitude(magnitude, a[j]);
-                }
-                if (t + 1 < walk.own) {
-                    tmem_wait(r);
-                    add_columns(bias[walk.slot(t + 1)], r, a);
-                }
+            for (int j = 0; j < 16; ++j) {
+                if (ACTIVATION != DIPACO_ACTIVATION_NONE) top = larger3(top, a[j]);
+                magnitude = larger_magnitude(magnitude, a[j]);
             }
-            if (row >= p.m) top = magnitude = 0.0f;  // the bias is not the matrix's there
-            exchange.put(walk.down ? blocks - 1 - k : k, __float_as_uint(top), __float_as_uint(magnitude));
+            if (walk.ends_block(t)) {
+                if (row >= p.m) top = magnitude = 0.0f;  // the bias is not the matrix's there
+                exchange.put(walk.block(t), __float_as_uint(top), __float_as_uint(magnitude));
+                top = magnitude = 0.0f;
+            }
+            if (t + 1 < walk.own) {
+                tmem_wait(r);
+                add_columns(bias[walk.slot(t + 1)], r, a);
+            }
         }
-        if (!exchange.meet(blocks, most)) return;
+        exchange.arrive();
+        // the next tile's place and biases while the others arrive
+        if (tile + p.pairs < p.whole_tiles) {
+            PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
+            load_next_columns(p.bias, p.bias_bf16, walk, tile_n * p.tile_n, p.n, lane, next);
+        }
+        if (!exchange.take(blocks, most)) return;
         bool careful = false, in_pairs = true;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -519,26 +529,26 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
                 most[k][0] = __float_as_uint(values_of(activate<ACTIVATION>(pair_of(__uint_as_float(most[k][0])))).x);
         }
         if (careful) {  // the same for all epilogue warps of the block
+            unsigned of_y = 0u, of_a = 0u;
 #pragma unroll 1
-            for (int k = 0; k < blocks; ++k) {
-                unsigned of_y = 0u, of_a = 0u;
-#pragma unroll 1
-                for (int t = k * OF_BLOCK; t < (k + 1) * OF_BLOCK; ++t) {
-                    if (t == 0) {
-                        add_columns(bias[walk.slot(0)], held, a);
-                    } else {
-                        tmem_load32(from + walk.column(walk.slot(t)), r);
-                        tmem_wait(r);
-                        add_columns(bias[walk.slot(t)], r, a);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        of_y = finite_magnitudes(of_y, activate<ACTIVATION>(a[j]));
-                        of_a = finite_magnitudes(of_a, a[j]);
-                    }
+            for (int t = 0; t < walk.own; ++t) {
+                if (t == 0) {
+                    add_columns(bias[walk.slot(0)], held, a);
+                } else {
+                    tmem_load32(from + walk.column(walk.slot(t)), r);
+                    tmem_wait(r);
+                    add_columns(bias[walk.slot(t)], r, a);
                 }
-                if (row >= p.m) of_y = of_a = 0u;
-                exchange.put(walk.down ? blocks - 1 - k : k, of_y, of_a);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    of_y = finite_magnitudes(of_y, activate<ACTIVATION>(a[j]));
+                    of_a = finite_magnitudes(of_a, a[j]);
+                }
+                if (walk.ends_block(t)) {
+                    if (row >= p.m) of_y = of_a = 0u;
+                    exchange.put(walk.block(t), of_y, of_a);
+                    of_y = of_a = 0u;
+                }
             }
             if (!exchange.meet(blocks, most)) return;
         }
@@ -552,64 +562,45 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
             p.first.scales[at] = (uint8_t)(lane ? most[1][0] : most[0][0]);
             if (keep) p.second.scales[at] = (uint8_t)(lane ? most[1][1] : most[0][1]);
         }
-        add_columns(bias[walk.slot(0)], held, a);
+        // One loop for the ordinary blocks and another for the rare ones: code that is jumped over costs instruction cache.
+        const auto encode_tile = [&](auto rare) {
+            constexpr bool RARE = decltype(rare)::value;
+            add_columns(bias[walk.slot(0)], held, a);
 #pragma unroll 1
-        for (int t = 0; t < walk.own; ++t) {
-            const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
-            const bool inside = row < p.m && left > 0, second = slot >= OF_BLOCK;
-            if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
-            unsigned w[8];
-            if (keep) {
-                const float by = scale_reciprocal(second ? most[1][1] : most[0][1]);
-                if (careful)
-                    encode32<true>(a, by, w);
-                else
-                    encode32<false>(a, by, w);
-                if (inside) store_codes(p.second, row, col, left, w);
-            }
-            const float by = scale_reciprocal(second ? most[1][0] : most[0][0]);
-            if (careful || !in_pairs) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) a[j] = activate<ACTIVATION>(a[j]);
-                encode32<true>(a, by, w);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) a[j] = activate_in_pairs<ACTIVATION>(a[j]);
-                encode32<false>(a, by, w);
-            }
-            if (inside) store_codes(p.first, row, col, left, w);
-            if (t + 1 < walk.own) {
-                tmem_wait(r);
-                if (b.apart && t + 2 == walk.own) {
-                    fence_before_sync();
-                    if (lane == 0) arrive_remote(read_bars[sets & 1]);
-                    __syncwarp();
+            for (int t = 0; t < walk.own; ++t) {
+                const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
+                const bool inside = row < p.m && left > 0, second = walk.block(t);
+                if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
+                unsigned w[8];
+                if (keep) {
+                    encode32<RARE>(a, scale_reciprocal(second ? most[1][1] : most[0][1]), w);
+                    if (inside) store_codes(p.second, row, col, left, w);
                 }
-                add_columns(bias[walk.slot(t + 1)], r, a);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) a[j] = RARE ? activate<ACTIVATION>(a[j]) : activate_in_pairs<ACTIVATION>(a[j]);
+                encode32<RARE>(a, scale_reciprocal(second ? most[1][0] : most[0][0]), w);
+                if (inside) store_codes(p.first, row, col, left, w);
+                if (t + 1 < walk.own) {
+                    tmem_wait(r);
+                    if (b.apart && t + 2 == walk.own) {
+                        fence_before_sync();
+                        if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                        __syncwarp();
+                    }
+                    add_columns(bias[walk.slot(t + 1)], r, a);
+                }
             }
-        }
+        };
+        if (careful || !in_pairs)
+            encode_tile(std::true_type());
+        else
+            encode_tile(std::false_type());
         if (b.apart && walk.own == 1) {  // read at the start
             fence_before_sync();
             if (lane == 0) arrive_remote(read_bars[sets & 1]);
             __syncwarp();
         }
     }
-}
-
-// Sums over the warp's 32 rows of 32 columns, a column for a lane: at each step a lane hands on the half of its
-// values that the lane across keeps.
-__device__ __forceinline__ float column_sums(float *v, int lane)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const bool upper = lane & o;
-#pragma unroll
-        for (int i = 0; i < o; ++i) {
-            const float give = upper ? v[i] : v[i + o];
-            v[i] = (upper ? v[i + o] : v[i]) + __shfl_xor_sync(0xffffffffu, give, o);
-        }
-    }
-    return v[0];
 }
 
 __device__ __forceinline__ void tmem_store32(uint32_t address, const f32x2 *v)
@@ -633,33 +624,102 @@ __device__ __forceinline__ void tmem_store32(uint32_t address, const f32x2 *v)
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-template <int ACTIVATION>
-__device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock &b, PackShared &shared,
-                                              float (*sums)[PAIR_MAX_N / 32][4][32])
+// 16 of the warp's rows of 32 columns of tensor memory: lane l has columns 8 i + 2 (l % 4) + {0, 1} of two of them, of the
+// four lanes that share l % 4 in every other register pair.
+__device__ __forceinline__ void tmem_load_across(uint32_t address, uint32_t *r)
 {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(address));
+}
+
+// Sums over the warp's 32 rows of 32 columns that are in tensor memory, a column for a lane.  Read across, a lane has
+// eight columns' values of four rows, so that three exchanges are left; with a row for a lane it would take five.
+__device__ __forceinline__ float column_sums(uint32_t address, int lane)
+{
+    uint32_t r[32];
+    tmem_load_across(address, r);
+    tmem_load_across(address + (16u << 16), r + 16);
+    tmem_wait(r);
+    float s[8];  // columns 8 (i / 2) + 2 (lane % 4) + i % 2
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = i / 2 * 4 + i % 2;
+        s[i] = (__uint_as_float(r[at]) + __uint_as_float(r[at + 2])) + (__uint_as_float(r[at + 16]) + __uint_as_float(r[at + 18]));
+    }
+    // a lane hands on the half of its columns that the lane across keeps
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+        const bool upper = lane & (4 * o);
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+            const float give = upper ? s[i] : s[i + o];
+            s[i] = (upper ? s[i + o] : s[i]) + __shfl_xor_sync(0xffffffffu, give, 4 * o);
+        }
+    }
+    return s[0];
+}
+// Which column that is.
+__device__ __forceinline__ int column_of_sum(int lane) { return (lane >> 3) * 8 + 2 * (lane & 3) + (lane >> 2 & 1); }
+
+// What the epilogue warps of the gradient share, where the others have their results' buffers.
+struct BackShared {
+    float sums[2][PAIR_MAX_N / 32][4][32];  // over 32 rows, for two tiles
+    // The slopes at all values that a code stands for in the tile's blocks of a, for two tiles: a block has one scale, so
+    // that a value's slope is looked up in place of two powers and reciprocals and 13 products for every pair.
+    float slopes[2][2][256];
+};
+static_assert(sizeof(BackShared) <= PAIR_EPILOGUE_WARPS * PAIR_STAGING * PAIR_STAGING_BYTES, "in the place of the buffers");
+
+template <int ACTIVATION>
+__device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock &b, PackShared &shared)
+{
+    BackShared &of_tiles = *reinterpret_cast<BackShared *>(b.aligned + PAIR_STAGING_AT);
     const int lane = b.lane, quarter = b.warp & 3;
     const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&b.sums_read[0]), 0),
                                    cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
     const int scale_cols = (p.n + 127) / 128, blocks = p.tile_n / 128;
-    TileWalk walk = {b.warp >> 2, blocks * OF_BLOCK, false};
+    TileWalk walk = make_walk(b.warp, p.tile_n);
     Exchange exchange = {shared, b.warp, lane};
-    // a group's codes of a, two units of 16 (rows of codes are padded to whole units), and their scale
-    const auto load_codes = [&](int row, int col, uint4 *codes, float &scale) {
+    constexpr bool SLOPES = ACTIVATION != DIPACO_ACTIVATION_NONE;
+    // a group's codes of a, two units of 16 (rows of codes are padded to whole units)
+    const auto load_codes = [&](int row, int col, uint4 *codes) {
         codes[0] = codes[1] = make_uint4(0u, 0u, 0u, 0u);
-        scale = 0.0f;
-        if constexpr (ACTIVATION != DIPACO_ACTIVATION_NONE) {
-            const uint8_t *at = p.a_codes + row * p.a_stride + col;
-            if (row < p.m && col < p.n) codes[0] = __ldcs(reinterpret_cast<const uint4 *>(at));
-            if (row < p.m && col + 16 < p.n) codes[1] = __ldcs(reinterpret_cast<const uint4 *>(at + 16));
-            if (row < p.m && col < p.n) scale = scale_value(p.of_a_scales[(long long)(row / 128) * scale_cols + col / 128]);
+        if (!SLOPES || row >= p.m) return;
+        const uint4 *at = reinterpret_cast<const uint4 *>(p.a_codes + row * p.a_stride + col);
+        if (col < p.n) codes[0] = __ldcs(at);
+        if (col + 16 < p.n) codes[1] = __ldcs(at + 1);
+    };
+    // the scales of a tile's blocks of a, and the slopes of this thread's code in them
+    const auto load_scales = [&](int tile_m, int tile_n, float *scales) {
+        const int row = tile_m * PAIR_ROWS + (int)b.rank * 128;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int block = tile_n * p.tile_n / 128 + k;
+            scales[k] = SLOPES && k < blocks && row < p.m && block < scale_cols ? scale_value(p.of_a_scales[(long long)(row / 128) * scale_cols + block]) : 0.0f;
         }
+    };
+    const auto put_slopes = [&](int set, const float *scales) {
+        static_assert(EPILOGUE_WARPS * 32 == 256, "a code for a thread");
+        const int code = b.warp * 32 + lane;
+        const float v = decode2((unsigned)code).x;
+        const float2 s = values_of(slope<ACTIVATION>(mul2(pair_of(v), pair_of(scales[0], scales[1]))));
+        of_tiles.slopes[set][0][code] = s.x;
+        of_tiles.slopes[set][1][code] = s.y;
     };
     int tile_m, tile_n, sets = 0;
     PairWalk::place(p, b.pair, tile_m, tile_n);
     uint4 codes[2];
-    float scale;
+    float scales[2];
+    unsigned most[2][2];
     walk.down = true;
-    load_codes(tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32 + lane, tile_n * p.tile_n + walk.column(walk.slot(0)), codes, scale);
+    load_codes(tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32 + lane, tile_n * p.tile_n + walk.column(walk.slot(0)), codes);
+    load_scales(tile_m, tile_n, scales);
+    if (SLOPES) put_slopes(0, scales);
+    if (!exchange.meet(0, most)) return;
     for (int tile = b.pair; tile < p.whole_tiles; tile += p.pairs, ++sets) {  // as PairWalk takes them
         const int n0 = tile_n * p.tile_n, row0 = tile_m * PAIR_ROWS + (int)b.rank * 128;
         const int row = row0 + quarter * 32 + lane;
@@ -667,67 +727,68 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
         fence_after_sync();
         const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
         walk.down = !(sets & 1);
+        const bool more = tile + p.pairs < p.whole_tiles;
+        if (more) {
+            PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
+            load_scales(tile_m, tile_n, scales);
+        }
         f32x2 held[16], v[16];  // held: the first group's results, as the next tile's products overwrite its columns
-        unsigned most[2][2];
         float magnitude = 0.0f;
+        uint32_t r[32];
+        tmem_load32(from + walk.column(walk.slot(0)), r);
 #pragma unroll 1
         for (int t = 0; t < walk.own; ++t) {
             const int slot = walk.slot(t);
-            uint32_t r[32];
-            tmem_load32(from + walk.column(slot), r);
             const unsigned words[8] = {codes[0].x, codes[0].y, codes[0].z, codes[0].w, codes[1].x, codes[1].y, codes[1].z, codes[1].w};
-            const f32x2 scales = pair_of(scale);
             if (t + 1 < walk.own) {
-                load_codes(row, n0 + walk.column(walk.slot(t + 1)), codes, scale);
-            } else if (tile + p.pairs < p.whole_tiles) {  // the next tile's first
-                PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
+                load_codes(row, n0 + walk.column(walk.slot(t + 1)), codes);
+            } else if (more) {  // the next tile's first
                 TileWalk then = walk;
                 then.down = !walk.down;
-                load_codes(tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32 + lane, tile_n * p.tile_n + then.column(then.slot(0)), codes, scale);
+                load_codes(tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32 + lane, tile_n * p.tile_n + then.column(then.slot(0)), codes);
             }
             tmem_wait(r);
-            if (t == 0 && !b.apart) {
-                fence_before_sync();
-                if (lane == 0) arrive_remote(read_bars[sets & 1]);
-                __syncwarp();
-            }
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-                if constexpr (ACTIVATION != DIPACO_ACTIVATION_NONE)
-                    v[j] = mul2(v[j], slope<ACTIVATION>(mul2(decode_pair(words[j / 2] >> 16 * (j & 1)), scales)));
-                magnitude = larger_magnitude(magnitude, v[j]);
+            for (int j = 0; j < 16; ++j) v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+            if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
+            if constexpr (SLOPES) {
+                const float *slopes = of_tiles.slopes[sets & 1][walk.block(t)];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const unsigned w = words[j / 2] >> 16 * (j & 1);
+                    v[j] = mul2(v[j], pair_of(slopes[w & 255u], slopes[w >> 8 & 255u]));
+                }
             }
             if (row >= p.m) {  // zero times a NaN of the weights
-                magnitude = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[j] = 0ull;
             }
-            if (t > 0) {
-                tmem_store32(from + walk.column(slot), v);
-            } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) magnitude = larger_magnitude(magnitude, v[j]);
+            if (t > 0 || p.row_sums) tmem_store32(from + walk.column(slot), v);
+            if (p.row_sums) {
+                tmem_stored();
+                of_tiles.sums[sets & 1][walk.group(t)][quarter][column_of_sum(lane)] = column_sums(from + walk.column(slot), lane);
+            }
+            if (t == 0) {
+                if (!b.apart) {
+                    fence_before_sync();
+                    if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int j = 0; j < 16; ++j) held[j] = v[j];
             }
-            if (p.row_sums) {
-                float f[32];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float2 w = values_of(v[j]);
-                    f[2 * j] = w.x;
-                    f[2 * j + 1] = w.y;
-                }
-                sums[sets & 1][walk.group(t)][quarter][lane] = column_sums(f, lane);
-            }
-            if ((t + 1) % OF_BLOCK == 0) {
-                exchange.put(slot / OF_BLOCK, __float_as_uint(magnitude), 0u);
+            if (walk.ends_block(t)) {
+                exchange.put(walk.block(t), __float_as_uint(magnitude), 0u);
                 magnitude = 0.0f;
             }
         }
         tmem_stored();
+        if (SLOPES && more) put_slopes(~sets & 1, scales);
         if (!exchange.meet(blocks, most)) return;
         if (p.row_sums && b.warp < p.tile_n / 32 && row0 < p.m && n0 + b.warp * 32 + lane < p.n) {
-            const float(*s)[32] = sums[sets & 1][b.warp];
+            const float(*s)[32] = of_tiles.sums[sets & 1][b.warp];
             p.row_sums[(long long)(row0 / 128) * p.n + n0 + b.warp * 32 + lane] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
         }
         // the results of the t-th group
@@ -736,7 +797,6 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[j] = held[j];
             } else {
-                uint32_t r[32];
                 tmem_load32(from + walk.column(walk.slot(t)), r);
                 tmem_wait(r);
 #pragma unroll
@@ -745,40 +805,42 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
         };
         const bool careful = most[0][0] >= 0x7f800000u || most[1][0] >= 0x7f800000u;
         if (careful) {  // the same for all epilogue warps of the block
+            unsigned finite = 0u;
 #pragma unroll 1
-            for (int k = 0; k < blocks; ++k) {
-                unsigned finite = 0u;
-#pragma unroll 1
-                for (int t = k * OF_BLOCK; t < (k + 1) * OF_BLOCK; ++t) {
-                    results(t);
+            for (int t = 0; t < walk.own; ++t) {
+                results(t);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) finite = finite_magnitudes(finite, v[j]);
+                for (int j = 0; j < 16; ++j) finite = finite_magnitudes(finite, v[j]);
+                if (walk.ends_block(t)) {
+                    exchange.put(walk.block(t), finite, 0u);
+                    finite = 0u;
                 }
-                exchange.put(walk.down ? blocks - 1 - k : k, finite, 0u);
             }
             if (!exchange.meet(blocks, most)) return;
         }
         const unsigned bytes[2] = {scale_byte(most[0][0]), scale_byte(most[1][0])};
         if (b.warp == 0 && lane < blocks && n0 + lane * 128 < p.n && row0 < p.m)
             p.first.scales[(long long)(row0 / 128) * scale_cols + n0 / 128 + lane] = (uint8_t)(lane ? bytes[1] : bytes[0]);
+        const auto encode_tile = [&](auto rare) {
 #pragma unroll 1
-        for (int t = 0; t < walk.own; ++t) {
-            const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
-            results(t);
-            if (b.apart && t + 1 == walk.own) {
-                fence_before_sync();
-                if (lane == 0) arrive_remote(read_bars[sets & 1]);
-                __syncwarp();
+            for (int t = 0; t < walk.own; ++t) {
+                const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
+                results(t);
+                if (b.apart && t + 1 == walk.own) {
+                    fence_before_sync();
+                    if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                    __syncwarp();
+                }
+                if (left <= 0) continue;
+                unsigned w[8];
+                encode32<decltype(rare)::value>(v, scale_reciprocal(walk.block(t) ? bytes[1] : bytes[0]), w);
+                if (row < p.m) store_codes(p.first, row, col, left, w);
             }
-            if (left <= 0) continue;
-            const float by = scale_reciprocal(slot >= OF_BLOCK ? bytes[1] : bytes[0]);
-            unsigned w[8];
-            if (careful)
-                encode32<true>(v, by, w);
-            else
-                encode32<false>(v, by, w);
-            if (row < p.m) store_codes(p.first, row, col, left, w);
-        }
+        };
+        if (careful)
+            encode_tile(std::true_type());
+        else
+            encode_tile(std::false_type());
     }
 }
 
@@ -788,14 +850,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGU
                        const __grid_constant__ PackArgs p)
 {
     __shared__ PackShared shared;
-    // biases of the warps' columns; or sums over rows of the tile's columns, for two tiles
-    __shared__ __align__(16) float columns[BACK ? 2 * PAIR_MAX_N * 4 : EPILOGUE_WARPS * GROUPS * 32];
+    __shared__ __align__(16) float columns[EPILOGUE_WARPS][GROUPS][32];  // biases of the warps' columns
     if (threadIdx.x == 64) ptx::mbar_init(&shared.exchanged, EPILOGUE_WARPS);  // seen after run_pair's first barrier
     run_pair<false, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) {
         if constexpr (BACK)
-            back_epilogue<ACTIVATION>(p, b, shared, reinterpret_cast<float(*)[PAIR_MAX_N / 32][4][32]>(columns));
+            back_epilogue<ACTIVATION>(p, b, shared);
         else
-            pack_epilogue<ACTIVATION>(p, b, shared, reinterpret_cast<float(*)[GROUPS][32]>(columns));
+            pack_epilogue<ACTIVATION>(p, b, shared, columns);
     });
 }
 
