@@ -2,7 +2,8 @@
 //
 // The gradients are cut into chunks, each of one tensor, which blocks take in turn: sums_kernel leaves one sum of
 // squares for each block, scale_kernel joins them in every block and goes through the chunks again, the last
-// first, as those are the ones still in L2.  Tensors are listed in the kernels' arguments, so that a call
+// first, as those are the ones still in L2.  Few values take one launch of a cluster of blocks instead, whose sums
+// meet in distributed shared memory (cluster_kernel).  Tensors are listed in the kernels' arguments, so that a call
 // copies nothing and can be captured; longer lists take several launches.
 #include "inner_common.cuh"
 
@@ -16,6 +17,8 @@ namespace {
 
 constexpr int CHUNK = 8192;  // values
 constexpr int THREADS = 256;
+constexpr int CLUSTER = 8, CLUSTER_THREADS = 512;
+constexpr int CLUSTER_CHUNKS = 128;  // up to a million values: 2 MB take the eight SMs as long as a second launch
 constexpr int FEW_TENSORS = 64, MANY_TENSORS = 640;  // 2 and 20 KB of arguments
 constexpr int MAX_BLOCKS = 148 * 8;
 constexpr int MAX_JOINED = 4096;  // sums that every block of scale_kernel joins by itself
@@ -82,37 +85,52 @@ template <typename T> __device__ __forceinline__ uint4 load_masked(const Units<T
     return v;
 }
 
-// The sum of squares of this thread's values of a chunk.  Squares are added in fp32, at most 32 (in bf16; 40
-// with the ends) of them, and where that overflows or loses small values, once more in fp64.
-template <typename T> __device__ __forceinline__ double chunk_squares(const void *p, long long begin, long long end)
+template <typename T> __device__ __forceinline__ void add_squares(const uint4 &v, f32x2 *sum, unsigned &bits)
 {
+    bits |= v.x | v.y | v.z | v.w;
+    f32x2 w[Unit<T>::UE / 2];
+    widen_pairs<T>(v, w);
+#pragma unroll
+    for (int i = 0; i < Unit<T>::UE / 2; ++i) sum[i & 1] = fma2(w[i], w[i], sum[i & 1]);
+}
+
+// The sum of squares of this thread's values of a chunk.  Squares are added in fp32, at most 40 of them, and where that
+// overflows or loses small values, once more in fp64.
+template <typename T, int N> __device__ __forceinline__ double chunk_squares(const void *p, long long begin, long long end)
+{
+    constexpr int UE = Unit<T>::UE, EACH = CHUNK / UE / N;  // units of a thread
     const Units<T> units(p, begin, end);
     f32x2 sum[2] = {0ull, 0ull};
     unsigned bits = 0u;
-#pragma unroll 4
-    for (int u = threadIdx.x; u < units.count; u += THREADS) {
-        const uint4 v = load_masked(units, u);
-        bits |= v.x | v.y | v.z | v.w;
-        f32x2 w[Unit<T>::UE / 2];
-        widen_pairs<T>(v, w);
+    if (units.lead == 0 && units.values == CHUNK) {  // all loads at once
+        uint4 v[EACH];
 #pragma unroll
-        for (int i = 0; i < Unit<T>::UE / 2; ++i) sum[i & 1] = fma2(w[i], w[i], sum[i & 1]);
+        for (int i = 0; i < EACH; ++i) v[i] = __ldg(units.first + threadIdx.x + i * N);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) add_squares<T>(v[i], sum, bits);
+    } else {
+#pragma unroll 4
+        for (int u = threadIdx.x; u < units.count; u += N) add_squares<T>(load_masked(units, u), sum, bits);
     }
     const float s = sum_of(add2(sum[0], sum[1]));
     const bool nothing = (bits & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) == 0u;
     if ((s >= 1e-28f && s <= 1e38f) || nothing) return s;
     double exact = 0.0;
-    for (int u = threadIdx.x; u < units.count; u += THREADS) {
-        float f[Unit<T>::UE];
+    for (int u = threadIdx.x; u < units.count; u += N) {
+        float f[UE];
         Unit<T>::widen(load_masked(units, u), f);
 #pragma unroll
-        for (int i = 0; i < Unit<T>::UE; ++i) exact = fma((double)f[i], (double)f[i], exact);
+        for (int i = 0; i < UE; ++i) exact = fma((double)f[i], (double)f[i], exact);
     }
     return exact;
 }
+template <int N> __device__ __forceinline__ double piece_squares(const Piece &p, long long begin, long long end)
+{
+    return p.in_bf16 ? chunk_squares<__nv_bfloat16, N>(p.in, begin, end) : chunk_squares<float, N>(p.in, begin, end);
+}
 
 // The sum over the block, on every thread.
-__device__ __forceinline__ double block_sum(double v, double *shared)
+template <int N = THREADS> __device__ __forceinline__ double block_sum(double v, double *shared)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -120,7 +138,7 @@ __device__ __forceinline__ double block_sum(double v, double *shared)
     __syncthreads();
     v = 0.0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) v += shared[w];
+    for (int w = 0; w < N / 32; ++w) v += shared[w];
     return v;
 }
 
@@ -132,7 +150,7 @@ __global__ void __launch_bounds__(THREADS) sums_kernel(const __grid_constant__ P
     for (unsigned c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, c, begin, end);
-        sum += p.in_bf16 ? chunk_squares<__nv_bfloat16>(p.in, begin, end) : chunk_squares<float>(p.in, begin, end);
+        sum += piece_squares<THREADS>(p, begin, end);
     }
     sum = block_sum(sum, shared);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -160,38 +178,76 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const double *sums, int c
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
-template <typename T, typename O>
-__device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, long long end, float by)
+// A unit of values times `by`, to q.
+template <typename T, typename O> __device__ __forceinline__ void store_scaled(const uint4 &v, float by, O *q)
 {
     constexpr int UE = Unit<T>::UE, OE = Unit<O>::UE;
+    float f[UE];
+    Unit<T>::widen(v, f);
+#pragma unroll
+    for (int i = 0; i < UE; ++i) f[i] *= by;
+    if constexpr (UE < OE) {  // four values to 8 bytes
+        __stcs(reinterpret_cast<uint2 *>(q), make_uint2(Unit<O>::pack(f[0], f[1]), Unit<O>::pack(f[2], f[3])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < UE / OE; ++i) __stcs(reinterpret_cast<uint4 *>(q) + i, Unit<O>::narrow(f + i * OE));
+    }
+}
+
+template <typename T, typename O, int N>
+__device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, long long end, float by)
+{
+    constexpr int UE = Unit<T>::UE, EACH = CHUNK / UE / N;
     const T *in = static_cast<const T *>(p.in);
     O *out = static_cast<O *>(p.out);
     const Units<T> units(in, begin, end);
     O *const to = out + begin - units.lead;  // where the first unit's first value would go
     if (reinterpret_cast<uintptr_t>(to) % (UE * sizeof(O) < 16 ? UE * sizeof(O) : 16) == 0) {
-#pragma unroll 4
-        for (int u = threadIdx.x; u < units.count; u += THREADS) {
-            float f[UE];
-            Unit<T>::widen(__ldcs(units.first + u), f);
+        if (units.lead == 0 && units.values == CHUNK) {
+            uint4 v[EACH];
 #pragma unroll
-            for (int i = 0; i < UE; ++i) f[i] *= by;
+            for (int i = 0; i < EACH; ++i) v[i] = __ldcs(units.first + threadIdx.x + i * N);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) store_scaled<T, O>(v[i], by, to + (threadIdx.x + i * N) * UE);
+            return;
+        }
+        for (int u = threadIdx.x; u < units.count; u += N) {
+            const uint4 v = __ldcs(units.first + u);
             O *q = to + (long long)u * UE;
-            if (!units.whole(u)) {
+            if (units.whole(u)) {
+                store_scaled<T, O>(v, by, q);
+            } else {
+                float f[UE];
+                Unit<T>::widen(v, f);
 #pragma unroll
                 for (int i = 0; i < UE; ++i)
-                    if (units.holds(u, i)) q[i] = narrow1<O>(f[i]);
-            } else if constexpr (UE < OE) {  // four values to 8 bytes
-                *reinterpret_cast<uint2 *>(q) = make_uint2(Unit<O>::pack(f[0], f[1]), Unit<O>::pack(f[2], f[3]));
-            } else {
-#pragma unroll
-                for (int i = 0; i < UE / OE; ++i) __stcs(reinterpret_cast<uint4 *>(q) + i, Unit<O>::narrow(f + i * OE));
+                    if (units.holds(u, i)) q[i] = narrow1<O>(f[i] * by);
             }
         }
         return;
     }
     // results at another place within 16 bytes than the values: a value per thread
 #pragma unroll 8
-    for (long long i = begin + threadIdx.x; i < end; i += THREADS) out[i] = narrow1<O>(widen1<T>(in[i]) * by);
+    for (long long i = begin + threadIdx.x; i < end; i += N) out[i] = narrow1<O>(widen1<T>(in[i]) * by);
+}
+template <int N> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, float by)
+{
+    if (p.in == p.out && by == 1.0f) return;
+    if (p.in_bf16) {
+        if (p.out_bf16)
+            scale_chunk<__nv_bfloat16, __nv_bfloat16, N>(p, begin, end, by);
+        else
+            scale_chunk<__nv_bfloat16, float, N>(p, begin, end, by);
+    } else {
+        if (p.out_bf16)
+            scale_chunk<float, __nv_bfloat16, N>(p, begin, end, by);
+        else
+            scale_chunk<float, float, N>(p, begin, end, by);
+    }
+}
+__device__ __forceinline__ float factor(double norm, double most)
+{
+    return norm <= most ? 1.0f : (float)(most / norm);  // a NaN makes all results NaN
 }
 
 template <int CAPACITY>
@@ -201,23 +257,50 @@ __global__ void __launch_bounds__(THREADS)
     __shared__ double shared[THREADS / 32];
     const double of_all = sqrt(joined(sums, count, shared));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)of_all;
-    const float by = of_all <= most ? 1.0f : (float)(most / of_all);  // NaN: all results are
+    const float by = factor(of_all, most);
     for (unsigned i = blockIdx.x; i < t.chunks; i += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, t.chunks - 1 - i, begin, end);
-        if (p.in == p.out && by == 1.0f) continue;
-        if (p.in_bf16) {
-            if (p.out_bf16)
-                scale_chunk<__nv_bfloat16, __nv_bfloat16>(p, begin, end, by);
-            else
-                scale_chunk<__nv_bfloat16, float>(p, begin, end, by);
-        } else {
-            if (p.out_bf16)
-                scale_chunk<float, __nv_bfloat16>(p, begin, end, by);
-            else
-                scale_chunk<float, float>(p, begin, end, by);
+        scale_piece<THREADS>(p, begin, end, by);
+    }
+}
+
+// Everything at once, on one cluster: its blocks' sums are read from one another's shared memory.
+__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(CLUSTER_THREADS, 1)
+    cluster_kernel(const __grid_constant__ Pieces<FEW_TENSORS> t, bool scale, double most, float *norm)
+{
+    __shared__ double shared[CLUSTER_THREADS / 32], of_block;
+    double sum = 0.0;
+    for (unsigned c = blockIdx.x; c < t.chunks; c += CLUSTER) {
+        long long begin, end;
+        const Piece &p = find_chunk(t, c, begin, end);
+        sum += piece_squares<CLUSTER_THREADS>(p, begin, end);
+    }
+    sum = block_sum<CLUSTER_THREADS>(sum, shared);
+    if (threadIdx.x == 0) of_block = sum;
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    sum = 0.0;
+#pragma unroll
+    for (int r = 0; r < CLUSTER; ++r) {
+        uint32_t at;
+        double v;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(ptx::smem_addr(&of_block)), "r"(r));
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(at) : "memory");
+        sum += v;
+    }
+    // no block ends while its sum may still be read
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const double of_all = sqrt(sum);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)of_all;
+    if (scale) {
+        const float by = factor(of_all, most);
+        for (unsigned c = blockIdx.x; c < t.chunks; c += CLUSTER) {
+            long long begin, end;
+            const Piece &p = find_chunk(t, c, begin, end);
+            scale_piece<CLUSTER_THREADS>(p, begin, end, by);
         }
     }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -226,7 +309,8 @@ __global__ void __launch_bounds__(THREADS)
 struct Launches {
     std::vector<int> tensors;  // with values, in order
     int per_launch = 0, launches = 0;
-    int64_t sums = 0;
+    bool one_cluster = false;
+    int64_t sums = 0;  // of the workspace
 };
 
 int64_t chunks_of(int64_t numel) { return ceil_div(numel, CHUNK); }
@@ -246,7 +330,8 @@ int plan(const int64_t *numel, int32_t count, Launches &plan)
     const int tensors = (int)plan.tensors.size();
     plan.per_launch = tensors <= FEW_TENSORS ? FEW_TENSORS : MANY_TENSORS;
     plan.launches = (int)ceil_div(tensors, plan.per_launch);
-    plan.sums = (int64_t)plan.launches * MAX_BLOCKS;
+    plan.one_cluster = tensors <= FEW_TENSORS && chunks <= CLUSTER_CHUNKS;
+    plan.sums = plan.one_cluster ? 0 : (int64_t)plan.launches * MAX_BLOCKS;
     return DIPACO_OK;
 }
 
@@ -292,6 +377,13 @@ int launch(const Launches &plan, const void *const *grads, void *const *out, con
             t.chunks += (unsigned)chunks_of(numel[i]);
         }
     };
+    if constexpr (CAPACITY == FEW_TENSORS) {
+        if (plan.one_cluster) {
+            fill(0);
+            cluster_kernel<<<CLUSTER, CLUSTER_THREADS, 0, stream>>>(t, out != nullptr, most, norm);
+            return launch_status();
+        }
+    }
     int count = 0;
     for (int l = 0; l < plan.launches; ++l) {
         fill(l);

@@ -534,29 +534,30 @@ def _gradients(grads: Sequence[torch.Tensor], any_order: bool):
     if not grads:
         raise ValueError("there must be a gradient")
     dev = grads[0].get_device()
-    codes = []
-    for t in grads:
-        code = _CODES.get(t.dtype)
+    codes = [_CODES.get(t.dtype) for t in grads]
+    for t, code in zip(grads, codes):
         if code is None or dev < 0 or t.get_device() != dev:
             raise ValueError("gradients must be float32 or bfloat16 tensors on one CUDA device")
-        if not (t.is_contiguous() or (any_order and _dense_in_some_order(t))):
+        if not t.is_contiguous() and not (any_order and _dense_in_some_order(t)):
             raise ValueError("gradients must be contiguous")
         if t.requires_grad:
             _refuse_gradient("a gradient")
-        codes.append(code)
     return grads, dev, [t.numel() for t in grads], [t.data_ptr() for t in grads], codes
 
 
-def _clip(grads, dev, numels, ptrs, codes, out_ptrs, out_codes, max_norm: float) -> torch.Tensor:
-    count = len(grads)
-    numel, dtypes = (ctypes.c_int64 * count)(*numels), (ctypes.c_int32 * count)(*codes)
-    norm = grads[0].new_empty((), dtype=_F32)
+def _clip(like: torch.Tensor, dev, numels, ptrs, codes, out_ptrs, out_codes, max_norm: float) -> torch.Tensor:
+    count = len(numels)
+    words, longs = ctypes.c_int32 * count, ctypes.c_int64 * count
+    numel, dtypes, grads = longs(*numels), words(*codes), longs(*ptrs)
+    out = out_dtypes = None
+    if out_ptrs is not None:
+        out = grads if out_ptrs is ptrs else longs(*out_ptrs)
+        out_dtypes = dtypes if out_codes is codes else words(*out_codes)
+    norm = like.new_empty((), dtype=_F32)
     need = B.dipaco_clip_gradients_workspace(numel, count)
     work = norm.new_empty(need, dtype=torch.uint8) if need else None
-    out = None if out_ptrs is None else (ctypes.c_void_p * count)(*out_ptrs)
-    out_dtypes = None if out_ptrs is None else (ctypes.c_int32 * count)(*out_codes)
-    B.dipaco_clip_gradients((ctypes.c_void_p * count)(*ptrs), out, numel, dtypes, out_dtypes, count, max_norm,
-                            norm.data_ptr(), work.data_ptr() if need else None, need, dev, _stream(dev))
+    B.dipaco_clip_gradients(grads, out, numel, dtypes, out_dtypes, count, max_norm, norm.data_ptr(),
+                            work.data_ptr() if need else None, need, dev, _stream(dev))
     return norm
 
 
@@ -569,14 +570,15 @@ def _most(max_norm: float) -> float:
 
 def gradient_norm(grads: Sequence[torch.Tensor]) -> torch.Tensor:
     """The norm of all gradients together, a float32 scalar on their device."""
-    return _clip(*_gradients(grads, True), None, None, math.inf)
+    grads, dev, numels, ptrs, codes = _gradients(grads, True)
+    return _clip(grads[0], dev, numels, ptrs, codes, None, None, math.inf)
 
 
 def clip_gradients(grads: Sequence[torch.Tensor], max_norm: float) -> torch.Tensor:
     """Multiplies the gradients by min(1, max_norm / norm) in place and returns their norm before that.  No two may
     share memory."""
     grads, dev, numels, ptrs, codes = _gradients(grads, True)
-    return _clip(grads, dev, numels, ptrs, codes, ptrs, codes, _most(max_norm))
+    return _clip(grads[0], dev, numels, ptrs, codes, ptrs, codes, _most(max_norm))
 
 
 def gather_gradients(grads: Sequence[torch.Tensor], max_norm: Optional[float] = None,
@@ -592,7 +594,7 @@ def gather_gradients(grads: Sequence[torch.Tensor], max_norm: Optional[float] = 
     for n in numels:
         out.append(at)
         at += n * size
-    return flat, _clip(grads, dev, numels, ptrs, codes, out, [_CODES[dtype]] * len(grads), most)
+    return flat, _clip(flat, dev, numels, ptrs, codes, out, [_CODES[dtype]] * len(out), most)
 
 
 def inner_status(device=None) -> int:
