@@ -9,7 +9,7 @@
 //   back   da = (dy w) act'(a) packed, and its sums over rows.  The products with the slope go back to tensor memory
 //          until the block's largest is known.
 //
-// Few tokens through a weight: their sums go to fp32 and are packed by a second launch.
+// Few tokens through a weight, packed: few_pack_kernel, in one launch.
 #include "activations.cuh"
 #include "product_pairs.cuh"
 
@@ -860,6 +860,84 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGU
     });
 }
 
+// Few tokens through a weight, packed: a cluster of eight blocks has a block of 128 columns, whose largest values its
+// blocks read from one another's shared memory.
+constexpr int FEW_CLUSTER = 8;
+static_assert(FEW_CLUSTER * FEW_THREADS / 32 * FEW_OUTPUTS == PACK_BLOCK && FEW_OUTPUTS == 2, "a block of columns");
+
+struct FewPackArgs : FewArgs {
+    Linear finish;  // bias and activation
+    PackedCodes first, second;
+};
+
+template <int M>
+__global__ void __cluster_dims__(FEW_CLUSTER, 1, 1) __launch_bounds__(FEW_THREADS) few_pack_kernel(const __grid_constant__ FewPackArgs p)
+{
+    extern __shared__ __align__(16) __half tokens[];
+    __shared__ unsigned of_warps[2][FEW_THREADS / 32], of_block[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t *token_scales = reinterpret_cast<uint8_t *>(tokens + M * p.steps * STEP);
+    const int col = (int)(blockIdx.x * (FEW_THREADS / 32) + warp) * FEW_OUTPUTS;  // and the next
+    few_tokens<M>(p, tokens, token_scales);
+    __syncthreads();
+    float a[FEW_OUTPUTS][M] = {}, y[FEW_OUTPUTS][M];
+    if (col < p.outputs) few_sums<M>(p, tokens, token_scales, col, lane, a);
+    unsigned most[2] = {0u, 0u};
+#pragma unroll
+    for (int r = 0; r < FEW_OUTPUTS; ++r) {
+        const float bias = p.finish.bias && col + r < p.outputs ? load_param(p.finish.bias, p.finish.bias_bf16, col + r) : 0.0f;
+#pragma unroll
+        for (int t = 0; t < M; ++t) {
+            a[r][t] += bias;
+            y[r][t] = values_of(p.finish.act(pair_of(a[r][t]))).x;
+            if (col + r < p.outputs) {
+                most[0] = max(most[0], finite_magnitude(y[r][t]));
+                most[1] = max(most[1], finite_magnitude(a[r][t]));
+            }
+        }
+    }
+    if (lane == 0) {
+        of_warps[0][warp] = most[0];
+        of_warps[1][warp] = most[1];
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        unsigned m = 0u;
+        for (int w = 0; w < FEW_THREADS / 32; ++w) m = max(m, of_warps[threadIdx.x][w]);
+        of_block[threadIdx.x] = m;
+    }
+    cluster_sync();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        unsigned m = 0u;
+        if (lane < FEW_CLUSTER)
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(m) : "r"(cluster_addr(ptx::smem_addr(&of_block[q]), lane)) : "memory");
+        most[q] = scale_byte(__reduce_max_sync(0xffffffffu, m));
+    }
+    // no block ends while its values may still be read
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const int block = (int)blockIdx.x / FEW_CLUSTER;
+    if (threadIdx.x == 0 && blockIdx.x % FEW_CLUSTER == 0) {
+        p.first.scales[block] = (uint8_t)most[0];
+        if (p.second.codes) p.second.scales[block] = (uint8_t)most[1];
+    }
+    const auto store = [&](const PackedCodes &out, unsigned scale, const float (*v)[M]) {
+#pragma unroll
+        for (int t = 0; t < M; ++t) {
+            const unsigned codes = encode2(v[0][t], v[1][t], scale_reciprocal(scale));
+            uint8_t *at = out.codes + t * out.stride + col;
+            if (lane != t || col >= p.outputs) continue;
+            if (col + 1 < p.outputs)
+                *reinterpret_cast<unsigned short *>(at) = (unsigned short)codes;
+            else
+                *at = (uint8_t)codes;
+        }
+    };
+    store(p.first, most[0], y);
+    if (p.second.codes) store(p.second, most[1], a);
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 constexpr int SLICES = 8;
 
 // The sums over all rows from those over blocks of 128, in a fixed order.
@@ -941,8 +1019,16 @@ int check_contraction(int64_t m, int64_t n, int64_t k)
     return k > (int64_t)CHUNK_BF16 * STEP || ceil_div(m, PAIR_ROWS) * ceil_div(n, 128) > INT32_MAX ? DIPACO_ELIMIT : DIPACO_OK;
 }
 
-// Few tokens, and sums over nothing, are packed from fp32.
-bool by_way_of_fp32(int64_t m, int64_t n, int64_t k) { return k == 0 || (m <= n && are_few(m, n, k, false, true)); }
+int launch_few_pack(const FewPackArgs &p, int tokens, cudaStream_t stream)
+{
+    const auto kernel = tokens == 1 ? few_pack_kernel<1> : tokens == 2 ? few_pack_kernel<2> : tokens == 3 ? few_pack_kernel<3> : few_pack_kernel<4>;
+    const int smem = few_smem(p, tokens);
+    // always the largest there can be, as in launch_few
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM) != cudaSuccess)
+        return launch_status();
+    kernel<<<(unsigned)ceil_div(p.outputs, PACK_BLOCK) * FEW_CLUSTER, FEW_THREADS, smem, stream>>>(p);
+    return launch_status();
+}
 
 bool workspace_ok(const void *workspace, int64_t bytes, int64_t need)
 {
@@ -1001,7 +1087,7 @@ int dipaco_packed_linear_pack_workspace(int64_t m, int64_t n, int64_t k, int64_t
 {
     if (!bytes) return DIPACO_EINVAL;
     if (const int rc = check_contraction(m, n, k)) return rc;
-    *bytes = by_way_of_fp32(m, n, k) ? m * ceil_div(n, 4) * 16 : 0;
+    *bytes = k == 0 ? m * ceil_div(n, 4) * 16 : 0;  // sums over nothing are packed from fp32
     return DIPACO_OK;
 }
 
@@ -1020,17 +1106,19 @@ int dipaco_packed_linear_pack(const dipaco_packed *x, const dipaco_packed *w, co
     DeviceScope scope(device);
     if (!scope.ok) return DIPACO_ECUDA;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (need > 0) {
-        const Linear finish = {bias, nullptr, 0, DIPACO_ACTIVATION_NONE, bias_dtype == DIPACO_BF16, false, false};
+    const Linear finish = {bias, nullptr, 0, activation, bias_dtype == DIPACO_BF16, false, false};
+    if (k == 0) {
+        Linear sums_finish = finish;
+        sums_finish.activation = DIPACO_ACTIVATION_NONE;
         float *sums = static_cast<float *>(workspace);
         const int64_t stride = ceil_div(n, 4) * 4;
-        if (k == 0) {
-            empty_sums_kernel<<<(unsigned)std::min<int64_t>(ceil_div(m, 256) * n, 148 * 8), 256, 0, stream>>>(sums, stride, m, (int)n, finish);
-            if (const int rc = launch_status()) return rc;
-        } else if (const int rc = launch_few(x, w, sums, stride, DIPACO_F32, false, finish, stream)) {
-            return rc;
-        }
+        empty_sums_kernel<<<(unsigned)std::min<int64_t>(ceil_div(m, 256) * n, 148 * 8), 256, 0, stream>>>(sums, stride, m, (int)n, sums_finish);
+        if (const int rc = launch_status()) return rc;
         return pack_activated(sums, stride, activation, y, a, stream);
+    }
+    if (m <= n && are_few(m, n, k, false, true)) {
+        FewPackArgs p = {few_args(x, w), finish, packed_codes(y), packed_codes(a)};
+        return launch_few_pack(p, (int)m, stream);
     }
     PackArgs p = {};
     set_operands(p, x, w, false, true);

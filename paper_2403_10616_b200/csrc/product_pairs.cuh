@@ -915,13 +915,11 @@ __device__ __forceinline__ void few_products(const uint4 *codes, const unsigned 
                     for (int t = 0; t < M; ++t) sums[r][t] += scaled(part[r][t], scale[r], token_scale);
 }
 
-template <int M, class F> __global__ void __launch_bounds__(FEW_THREADS) few_kernel(const __grid_constant__ FinishedFew<F> p)
+// The tokens in shared memory, [M][2][padded / 16][8]: the halves of every 16 codes apart, so that a warp's loads do not
+// conflict; and their scale bytes.
+template <int M> __device__ __forceinline__ void few_tokens(const FewArgs &p, __half *tokens, uint8_t *token_scales)
 {
-    // [M][2][padded / 16][8]: the halves of every 16 codes apart, so that a warp's loads do not conflict; then
-    // the tokens' scale bytes
-    extern __shared__ __align__(16) __half tokens[];
-    const int padded = p.steps * STEP, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint8_t *token_scales = reinterpret_cast<uint8_t *>(tokens + M * padded);
+    const int padded = p.steps * STEP;
     for (int i = threadIdx.x; i < M * padded / 4; i += FEW_THREADS) {
         const int t = i * 4 / padded, k = i * 4 % padded;
         unsigned w = 0u;
@@ -935,58 +933,78 @@ template <int M, class F> __global__ void __launch_bounds__(FEW_THREADS) few_ker
             make_uint2(lo.x | (unsigned)lo.y << 16, hi.x | (unsigned)hi.y << 16);
     }
     for (int i = threadIdx.x; i < p.steps; i += FEW_THREADS) token_scales[i] = p.token_scales[i];  // one block of rows
+}
+
+// The products of outputs first, first + 1, ... with every token, on all lanes of the warp.
+template <int M>
+__device__ __forceinline__ void few_sums(const FewArgs &p, const __half *tokens, const uint8_t *token_scales, int first, int lane,
+                                         float (*sums)[M])
+{
+    const int padded = p.steps * STEP;
+    const uint8_t *rows[FEW_OUTPUTS], *scales[FEW_OUTPUTS];
+#pragma unroll
+    for (int r = 0; r < FEW_OUTPUTS; ++r) {
+        const int row = min(first + r, p.outputs - 1);
+        rows[r] = p.weight + row * p.weight_stride;
+        scales[r] = p.weight_scales + (long long)(row / PACK_BLOCK) * p.steps;
+    }
+    const int whole = p.k / 512 * 512;
+#pragma unroll(M == 1 ? 4 : 2)
+    for (int k = lane * 16; k < whole; k += 512) {
+        uint4 codes[FEW_OUTPUTS];
+        unsigned scale[FEW_OUTPUTS];
+#pragma unroll
+        for (int r = 0; r < FEW_OUTPUTS; ++r) {
+            codes[r] = __ldcs(reinterpret_cast<const uint4 *>(rows[r] + k));
+            scale[r] = scales[r][k / STEP];
+        }
+        few_products<M>(codes, scale, token_scales[k / STEP], tokens, padded, k, sums);
+    }
+    if (const int k = whole + lane * 16; k < p.k) {
+        uint4 codes[FEW_OUTPUTS];
+        unsigned scale[FEW_OUTPUTS];
+#pragma unroll
+        for (int r = 0; r < FEW_OUTPUTS; ++r) {
+            codes[r] = __ldcs(reinterpret_cast<const uint4 *>(rows[r] + k));
+            scale[r] = scales[r][k / STEP];
+        }
+        if (k + 16 > p.k) {  // rows of codes are padded to 16 bytes with anything
+            const int n = p.k - k;
+#pragma unroll
+            for (int r = 0; r < FEW_OUTPUTS; ++r) {
+                codes[r].x &= n >= 4 ? ~0u : (1u << 8 * n) - 1u;
+                codes[r].y &= n >= 8 ? ~0u : n > 4 ? (1u << 8 * (n - 4)) - 1u : 0u;
+                codes[r].z &= n >= 12 ? ~0u : n > 8 ? (1u << 8 * (n - 8)) - 1u : 0u;
+                codes[r].w &= n > 12 ? (1u << 8 * (n - 12)) - 1u : 0u;
+            }
+        }
+        few_products<M>(codes, scale, token_scales[k / STEP], tokens, padded, k, sums);
+    }
+#pragma unroll
+    for (int r = 0; r < FEW_OUTPUTS; ++r)
+#pragma unroll
+        for (int t = 0; t < M; ++t)
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sums[r][t] += __shfl_xor_sync(0xffffffffu, sums[r][t], o);
+}
+
+template <int M, class F> __global__ void __launch_bounds__(FEW_THREADS) few_kernel(const __grid_constant__ FinishedFew<F> p)
+{
+    extern __shared__ __align__(16) __half tokens[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t *token_scales = reinterpret_cast<uint8_t *>(tokens + M * p.steps * STEP);
+    few_tokens<M>(p, tokens, token_scales);
     __syncthreads();
 
     const int step = gridDim.x * (FEW_THREADS / 32) * FEW_OUTPUTS;
     for (int first = (blockIdx.x * (FEW_THREADS / 32) + warp) * FEW_OUTPUTS; first < p.outputs; first += step) {
         float sums[FEW_OUTPUTS][M] = {};
-        const uint8_t *rows[FEW_OUTPUTS], *scales[FEW_OUTPUTS];
-#pragma unroll
-        for (int r = 0; r < FEW_OUTPUTS; ++r) {
-            const int row = min(first + r, p.outputs - 1);
-            rows[r] = p.weight + row * p.weight_stride;
-            scales[r] = p.weight_scales + (long long)(row / PACK_BLOCK) * p.steps;
-        }
-        const int whole = p.k / 512 * 512;
-#pragma unroll(M == 1 ? 4 : 2)
-        for (int k = lane * 16; k < whole; k += 512) {
-            uint4 codes[FEW_OUTPUTS];
-            unsigned scale[FEW_OUTPUTS];
-#pragma unroll
-            for (int r = 0; r < FEW_OUTPUTS; ++r) {
-                codes[r] = __ldcs(reinterpret_cast<const uint4 *>(rows[r] + k));
-                scale[r] = scales[r][k / STEP];
-            }
-            few_products<M>(codes, scale, token_scales[k / STEP], tokens, padded, k, sums);
-        }
-        if (const int k = whole + lane * 16; k < p.k) {
-            uint4 codes[FEW_OUTPUTS];
-            unsigned scale[FEW_OUTPUTS];
-#pragma unroll
-            for (int r = 0; r < FEW_OUTPUTS; ++r) {
-                codes[r] = __ldcs(reinterpret_cast<const uint4 *>(rows[r] + k));
-                scale[r] = scales[r][k / STEP];
-            }
-            if (k + 16 > p.k) {  // rows of codes are padded to 16 bytes with anything
-                const int n = p.k - k;
-#pragma unroll
-                for (int r = 0; r < FEW_OUTPUTS; ++r) {
-                    codes[r].x &= n >= 4 ? ~0u : (1u << 8 * n) - 1u;
-                    codes[r].y &= n >= 8 ? ~0u : n > 4 ? (1u << 8 * (n - 4)) - 1u : 0u;
-                    codes[r].z &= n >= 12 ? ~0u : n > 8 ? (1u << 8 * (n - 8)) - 1u : 0u;
-                    codes[r].w &= n > 12 ? (1u << 8 * (n - 12)) - 1u : 0u;
-                }
-            }
-            few_products<M>(codes, scale, token_scales[k / STEP], tokens, padded, k, sums);
-        }
+        few_sums<M>(p, tokens, token_scales, first, lane, sums);
 #pragma unroll
         for (int r = 0; r < FEW_OUTPUTS; ++r)
 #pragma unroll
-            for (int t = 0; t < M; ++t) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sums[r][t] += __shfl_xor_sync(0xffffffffu, sums[r][t], o);
+            for (int t = 0; t < M; ++t)
                 if (lane == 0 && first + r < p.outputs) store_few(p, t, first + r, sums[r][t]);
-            }
     }
 }
 
@@ -1076,19 +1094,38 @@ inline bool are_few(int64_t m, int64_t n, int64_t k, bool transpose_a, bool tran
     return (few <= 2 || (few <= FEW_MAX && std::max(m, n) * k <= (int64_t)1 << 24)) && !transpose_a && transpose_b && few * ceil_div(k, STEP) * STEP * 2 + ceil_div(k, STEP) <= FEW_SMEM;
 }
 
+// Arguments for few tokens; the rest is for those who store.
+inline FewArgs few_args(const dipaco_packed *tokens, const dipaco_packed *weight)
+{
+    FewArgs p = {};
+    p.tokens = static_cast<const uint8_t *>(tokens->codes);
+    p.token_scales = static_cast<const uint8_t *>(tokens->scales);
+    p.weight = static_cast<const uint8_t *>(weight->codes);
+    p.weight_scales = static_cast<const uint8_t *>(weight->scales);
+    p.token_stride = tokens->stride;
+    p.weight_stride = weight->stride;
+    p.outputs = (int)weight->rows;
+    p.k = (int)weight->cols;
+    p.steps = (int)ceil_div(weight->cols, STEP);
+    return p;
+}
+inline int few_smem(const FewArgs &p, int64_t tokens) { return (int)tokens * p.steps * STEP * 2 + p.steps; }
+
 template <class F>
 int launch_few(const dipaco_packed *a, const dipaco_packed *b, void *c, int64_t c_stride, int dtype, bool accumulate,
                const F &finish, cudaStream_t stream)
 {
     const bool tokens_first = a->rows <= b->rows;
     const dipaco_packed *tokens = tokens_first ? a : b, *weight = tokens_first ? b : a;
-    FinishedFew<F> p = {{static_cast<const uint8_t *>(tokens->codes), static_cast<const uint8_t *>(tokens->scales),
-                 static_cast<const uint8_t *>(weight->codes), static_cast<const uint8_t *>(weight->scales),
-                 tokens->stride, weight->stride, (int)weight->rows, (int)weight->cols, (int)ceil_div(weight->cols, STEP),
-                 c, tokens_first ? c_stride : 1, tokens_first ? 1 : c_stride, dtype == DIPACO_BF16, accumulate, tokens_first},
-                        finish};
+    FinishedFew<F> p = {few_args(tokens, weight), finish};
+    p.c = c;
+    p.c_token = tokens_first ? c_stride : 1;
+    p.c_output = tokens_first ? 1 : c_stride;
+    p.c_bf16 = dtype == DIPACO_BF16;
+    p.accumulate = accumulate;
+    p.tokens_first = tokens_first;
     const int m = (int)tokens->rows;
-    const int smem = m * p.steps * STEP * 2 + p.steps;
+    const int smem = few_smem(p, m);
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(p.outputs, FEW_THREADS / 32 * FEW_OUTPUTS), 148 * 2);
     const auto kernel = m == 1 ? few_kernel<1, F> : m == 2 ? few_kernel<2, F> : m == 3 ? few_kernel<3, F> : few_kernel<4, F>;
     // always the largest there can be: threads that launch different sizes share the attribute

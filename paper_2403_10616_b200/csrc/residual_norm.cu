@@ -1019,7 +1019,9 @@ template <typename T, bool VEC, int GATE, int U> int launch_groups(const NormArg
 {
     const auto kernel = group_rows_kernel<T, VEC, GATE, U>;
     const int warps = (int)ceil_div(a.cols, 256 * U), groups = 16 / warps;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_GROUP_COLS * 16) != cudaSuccess) return launch_status();
+    if (a.cols * 16 > 48 * 1024 &&
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_GROUP_COLS * 16) != cudaSuccess)
+        return launch_status();
     kernel<<<(unsigned)std::min<int64_t>(ceil_div(a.rows, groups), 148), groups * warps * 32, a.cols * 16, stream>>>(a, warps);
     return launch_status();
 }

@@ -401,16 +401,14 @@ def _residual_norm_args(rows, cols, dev, code, gamma, beta, post_gamma, post_bet
         raise ValueError("gamma and beta belong to the norm that is left out")
     if not post_norm and (post_gamma is not None or post_beta is not None):
         raise ValueError("post_gamma and post_beta belong to the norm that is left out")
-    given, pcode = [], None
-    for p in (gamma, beta, post_gamma, post_beta):
-        if p is None:
-            given.append(None)
-            continue
-        ptr, p_code = _param(cols, dev, p)
-        if pcode is not None and p_code != pcode:
-            raise ValueError("the norms' parameters must have one dtype")
-        given.append(ptr)
-        pcode = p_code
+    given, pcode = [None] * 4, None
+    for i, p in enumerate((gamma, beta, post_gamma, post_beta)):
+        if p is not None:
+            given[i], p_code = _param(cols, dev, p)
+            if pcode is None:
+                pcode = p_code
+            elif p_code != pcode:
+                raise ValueError("the norms' parameters must have one dtype")
     kind, gate_ptr, gate_stride, gate_code = _gate(gate, rows, cols, dev, code)
     return B.ResidualNormStruct(rows, cols, *given, gate_ptr, gate_stride, kind, gate_code, code,
                                 B.DIPACO_F32 if pcode is None else pcode, post_norm, norm, residual_scale, eps)
