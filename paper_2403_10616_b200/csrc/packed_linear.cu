@@ -126,7 +126,8 @@ __device__ __forceinline__ void load_residual(const DenseArgs<Linear> &p, int ro
     }
 }
 
-// 32 columns of the warp's rows to C.  units: the residual of the first 64 bytes, where it is read that way.
+// 32 columns of the warp's rows to C, by the copy engine (TMA) or at any alignment.  units: the residual of the first 64 bytes, where it is read that way.
+template <bool TMA>
 __device__ __forceinline__ void finish_linear(const DenseArgs<Linear> &p, const CUtensorMap &c_map, const PairItem &item,
                                               int row0, int quarter, unsigned rank, int lane, int group, const uint32_t *sums,
                                               const float *bias, uint4 *units, bool by_units, uint8_t *buffers, int &buffer)
@@ -140,8 +141,10 @@ __device__ __forceinline__ void finish_linear(const DenseArgs<Linear> &p, const 
     const int col0 = item.tile_n * p.tile_n + group * 32;
     f32x2 v[16];
     add_columns(bias, sums, v);
+    uint4 second[4];  // the residual of the other 64 bytes, in fp32
+    if (by_units && !p.c_bf16) load_residual(p, row0, col0 + 16, lane, second);
     p.finish.act32(v);
-    if (p.store_by_tma) {
+    if constexpr (TMA) {
         if (p.finish.residual && !by_units && row0 + lane < p.m) {  // a residual at another alignment
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -164,9 +167,8 @@ __device__ __forceinline__ void finish_linear(const DenseArgs<Linear> &p, const 
                 return reinterpret_cast<uint4 *>(staging + row * 64 + ((unit ^ ((row >> 1) & 3)) * 16));
             };
             if (by_units) {
-                if (part == 1) load_residual(p, row0, col, lane, units);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) *place((lane >> 2) + 8 * i, lane & 3) = units[i];
+                for (int i = 0; i < 4; ++i) *place((lane >> 2) + 8 * i, lane & 3) = part ? second[i] : units[i];
                 __syncwarp();
             }
 #pragma unroll
@@ -220,23 +222,25 @@ __device__ __forceinline__ void finish_linear(const DenseArgs<Linear> &p, const 
         __syncwarp();
         const int first = row0 + part * 16, rows = min(16, p.m - first);
         if (col0 + lane >= p.n) continue;
-#pragma unroll
-        for (int r0 = 0; r0 < 16; r0 += 8) {
+        const auto sum = [&](int r) { return at[r * 32 + ((lane + part * 16 + r) & 31)]; };
+        if (!p.finish.residual) {
+            for (int r = 0; r < rows; ++r) store_c(p, first + r, col0 + lane, sum(r));
+            continue;
+        }
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += 8) {
             float add[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r)
-                add[r] = p.finish.residual && r0 + r < rows
-                             ? load_param(p.finish.residual, p.finish.residual_bf16, (first + r0 + r) * p.finish.residual_row + col0 + lane)
-                             : 0.0f;
+                add[r] = load_param(p.finish.residual, p.finish.residual_bf16, (long long)min(first + r0 + r, p.m - 1) * p.finish.residual_row + col0 + lane);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
-                if (r0 + r < rows)
-                    store_c(p, first + r0 + r, col0 + lane, at[(r0 + r) * 32 + ((lane + part * 16 + r0 + r) & 31)] + add[r]);
+                if (r0 + r < rows) store_c(p, first + r0 + r, col0 + lane, sum(r0 + r) + add[r]);
         }
     }
 }
 
-template <bool CHUNKED>
+template <bool CHUNKED, bool TMA>
 __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, const CUtensorMap &c_map, const PairBlock &b,
                                                 float (*columns)[GROUPS][32])
 {
@@ -246,7 +250,7 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
     int buffer = 0;
     const uint32_t read_bars[2] = {cluster_addr(ptx::smem_addr(&b.sums_read[0]), 0),
                                    cluster_addr(ptx::smem_addr(&b.sums_read[1]), 0)};
-    const bool by_units = p.finish.residual && p.store_by_tma && p.finish.residual_aligned;
+    const bool by_units = TMA && p.finish.residual && p.finish.residual_aligned;
     TileWalk walk = make_walk(b.warp, p.tile_n);
     PairWalk items(p, b.pair);
     PairItem item, ahead;
@@ -254,6 +258,12 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
     float next[GROUPS];
     if (more) load_next_columns(p.finish.bias, p.finish.bias_bf16, walk, ahead.tile_n * p.tile_n, p.n, lane, next);
     int sets = 0;
+    uint4 units[4], units_ahead[4] = {};  // of this group and of the next one
+    const auto load_first = [&](bool down) {  // of the next tile
+        const int slot = down ? walk.own - 1 : 0;
+        load_residual(p, ahead.tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32, ahead.tile_n * p.tile_n + walk.column(slot), lane, units_ahead);
+    };
+    if (by_units && more && ahead.slot < 0) load_first(!CHUNKED);
     while (more) {
         item = ahead;
         const int n0 = item.tile_n * p.tile_n, row0 = item.tile_m * PAIR_ROWS + (int)b.rank * 128 + quarter * 32;
@@ -262,7 +272,6 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
         if (more) load_next_columns(p.finish.bias, p.finish.bias_bf16, walk, ahead.tile_n * p.tile_n, p.n, lane, next);
         const int chunks = CHUNKED ? (item.last - item.first + p.chunk - 1) / p.chunk : 1;
         const bool units_of = by_units && item.slot < 0;
-        uint4 units[4];
         float total[CHUNKED ? GROUPS : 1][32];
         if constexpr (CHUNKED) {
 #pragma unroll
@@ -272,7 +281,6 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
         }
         for (int chunk = 0; chunk < chunks; ++chunk, ++sets) {
             walk.down = !(sets & 1);
-            if (!CHUNKED && units_of && walk.own > 0) load_residual(p, row0, n0 + walk.column(walk.slot(0)), lane, units);
             if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
             fence_after_sync();
             const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
@@ -298,32 +306,45 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
                     tmem_load32(from + walk.column(walk.slot(t)), r);
                     tmem_wait(r);
                     if (t == (b.apart ? walk.own - 1 : 0)) read_over();
-                    finish_linear(p, c_map, item, row0, quarter, b.rank, lane, walk.group(t), r, bias[walk.slot(t)], units, units_of, staging, buffer);
-                    if (units_of && t + 1 < walk.own) load_residual(p, row0, n0 + walk.column(walk.slot(t + 1)), lane, units);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) units[i] = units_ahead[i];
+                    if (units_of && t + 1 < walk.own)
+                        load_residual(p, row0, n0 + walk.column(walk.slot(t + 1)), lane, units_ahead);
+                    else if (by_units && t + 1 == walk.own && more && ahead.slot < 0)
+                        load_first(!walk.down);
+                    finish_linear<TMA>(p, c_map, item, row0, quarter, b.rank, lane, walk.group(t), r, bias[walk.slot(t)], units, units_of, staging, buffer);
                 }
             }
         }
         if constexpr (CHUNKED) {
-#pragma unroll
-            for (int s = 0; s < GROUPS; ++s) {
-                if (s >= walk.own) break;
+#pragma unroll 1
+            for (int s = 0; s < walk.own; ++s) {  // on total[0]
                 const int group = SUBS * s + walk.sub;
-                if (units_of) load_residual(p, row0, n0 + group * 32, lane, units);
-                finish_linear(p, c_map, item, row0, quarter, b.rank, lane, group, reinterpret_cast<const uint32_t *>(total[s]), bias[s], units,
+#pragma unroll
+                for (int i = 0; i < 4; ++i) units[i] = units_ahead[i];
+                if (units_of && s + 1 < walk.own)
+                    load_residual(p, row0, n0 + walk.column(s + 1), lane, units_ahead);
+                else if (by_units && s + 1 == walk.own && more && ahead.slot < 0)
+                    load_first(false);
+                finish_linear<TMA>(p, c_map, item, row0, quarter, b.rank, lane, group, reinterpret_cast<const uint32_t *>(total[0]), bias[s], units,
                               units_of, staging, buffer);
+#pragma unroll
+                for (int j = 0; j + 1 < GROUPS; ++j)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) total[j][i] = total[j + 1][i];
             }
         }
     }
     ptx::bulk_wait_all();
 }
 
-template <bool CHUNKED>
+template <bool CHUNKED, bool TMA>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGUE_WARPS), 1)
     linear_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                        const __grid_constant__ CUtensorMap c_map, const __grid_constant__ DenseArgs<Linear> p)
 {
     __shared__ __align__(16) float columns[EPILOGUE_WARPS][GROUPS][32];
-    run_pair<CHUNKED, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) { linear_epilogue<CHUNKED>(p, c_map, b, columns); });
+    run_pair<CHUNKED, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) { linear_epilogue<CHUNKED, TMA>(p, c_map, b, columns); });
 }
 
 // Nothing is contracted: every sum is zero.
@@ -1079,7 +1100,10 @@ int dipaco_packed_linear(const dipaco_packed *x, const dipaco_packed *w, const v
         return launch_status();
     }
     if (few) return launch_few(x, w, y, y_stride, dtype, false, finish, stream);
-    const DenseKernels<Linear> kernels = {linear_pair_kernel<false>, linear_pair_kernel<true>, pair_threads(EPILOGUE_WARPS)};
+    const DenseKernels<Linear> kernels = {{linear_pair_kernel<false, false>, linear_pair_kernel<false, true>},
+                                          {linear_pair_kernel<true, false>, linear_pair_kernel<true, true>},
+                                          pair_threads(EPILOGUE_WARPS),
+                                          true};
     return launch_product(x, w, false, true, y, y_stride, dtype, false, finish, kernels, workspace, stream);
 }
 

@@ -81,7 +81,10 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
         return cudaMemset2DAsync(c, pitch, 0, n * size, m, stream) == cudaSuccess ? DIPACO_OK : launch_status();
     }
     if (few) return launch_few(a, b, c, c_stride, dtype, accumulate != 0, AsItIs{}, stream);
-    const DenseKernels<AsItIs> kernels = {pair_kernel<false, AsItIs>, pair_kernel<true, AsItIs>, pair_threads(PAIR_EPILOGUE_WARPS)};
+    const DenseKernels<AsItIs> kernels = {{pair_kernel<false, AsItIs>, pair_kernel<false, AsItIs>},
+                                          {pair_kernel<true, AsItIs>, pair_kernel<true, AsItIs>},
+                                          pair_threads(PAIR_EPILOGUE_WARPS),
+                                          false};
     return launch_product(a, b, transpose_a != 0, transpose_b != 0, c, c_stride, dtype, accumulate != 0, AsItIs{}, kernels,
                           workspace, stream);
 }

@@ -1138,8 +1138,9 @@ int launch_few(const dipaco_packed *a, const dipaco_packed *b, void *c, int64_t 
 // The kernels of a product that stores to a dense matrix, whose sums are taken in one go or in chunks.
 template <class F> struct DenseKernels {
     using Kernel = void (*)(CUtensorMap, CUtensorMap, CUtensorMap, DenseArgs<F>);
-    Kernel whole, chunked;
+    Kernel whole[2], chunked[2];  // [1]: where the copy engine stores the results
     int threads;
+    bool whole_f32;  // results in fp32 take the first too where there is one chunk
 };
 
 inline void set_operands(ProductArgs &p, const dipaco_packed *a, const dipaco_packed *b, bool transpose_a, bool transpose_b)
@@ -1186,8 +1187,8 @@ int launch_product(const dipaco_packed *a, const dipaco_packed *b, bool transpos
     p.store_by_tma = !accumulate && p.whole_n > 0 && rows_aligned16(c, c_stride, m, dense_size(dtype));
     if (p.store_by_tma && !result_map(&c_map, c, m, p.whole_n, m == 1 ? ceil_div(n, 8) * 8 : c_stride, dtype)) return DIPACO_ECUDA;
     p.chunk = p.c_bf16 ? CHUNK_BF16 : CHUNK_F32;
-    const bool chunked = !p.c_bf16 || p.steps > p.chunk;
-    const auto kernel = chunked ? kernels.chunked : kernels.whole;
+    const bool chunked = (!p.c_bf16 && !kernels.whole_f32) || p.steps > p.chunk;
+    const auto kernel = (chunked ? kernels.chunked : kernels.whole)[p.store_by_tma != 0];
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM) != cudaSuccess) return launch_status();
     kernel<<<2 * plan.pairs, kernels.threads, PAIR_SMEM, stream>>>(a_map, b_map, c_map, p);
     if (const int rc = launch_status()) return rc;
