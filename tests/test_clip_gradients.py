@@ -196,11 +196,14 @@ def test_bad_arguments_are_refused():
     two = dict(grads=(p, 4 * p), numel=(8, 8), dtypes=(0, 0), out_dtypes=(0, 0))
     for bad in (dict(most=-1.0), dict(most=math.nan), dict(count=-1), dict(grads=None), dict(dtypes=None), dict(out_dtypes=None),
                 dict(numel=(-1,)), dict(dtypes=(2,)), dict(out_dtypes=(-1,)), dict(grads=(None,)), dict(out=(None,)), dict(grads=(p + 2,)),
-                dict(out=(p + 3,)), dict(norm=p + 1), dict(work=None), dict(work=p + 8), dict(size=64), dict(device=-1),
+                dict(out=(p + 3,)), dict(norm=p + 1), dict(device=-1),
                 dict(out=(p + 4,)), dict(out=(p - 4,)), dict(out=(p,), out_dtypes=(1,)),   # over its own gradient, not in place
                 dict(**two, out=(p, p)), dict(**two, out=(8 * p, 8 * p + 28)),              # over one another
                 dict(**two, out=(8 * p, p)), dict(**two, out=(4 * p, p))):                  # over another's gradient
         assert status(**bad) == B.DIPACO_EINVAL, bad
+    many = dict(out=(1 << 40,), numel=(1 << 21,))  # fewer values need no workspace
+    for bad in (dict(work=None), dict(work=p + 8), dict(size=64)):
+        assert status(**many, **bad) == B.DIPACO_EINVAL, bad
     assert status(numel=(1 << 45,)) == B.DIPACO_ELIMIT
     assert status(numel=(1 << 44,)) == B.DIPACO_ELIMIT  # more chunks than are counted
     size = ctypes.c_int64()
