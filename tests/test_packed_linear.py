@@ -330,8 +330,11 @@ def test_bad_arguments_are_refused():
         return lib.dipaco_packed_linear_pack(x, w, bias, bias_dtype, act, y, a, work, size, device, None)
 
     for bad in (dict(x=None), dict(y=None), dict(y=S(p, p, 4, 7, 16)), dict(a=S(p, p, 5, 6, 16)), dict(a=S(p, None, 4, 6, 16)),
-                dict(act=5), dict(bias=p + 1), dict(bias_dtype=-1), dict(work=None), dict(work=p + 4), dict(size=16), dict(device=-1)):
+                dict(act=5), dict(bias=p + 1), dict(bias_dtype=-1), dict(device=-1)):
         assert pack(**bad) == B.DIPACO_EINVAL, bad
+    nothing = dict(x=S(p, p, 4, 0, 16), w=S(p, p, 6, 0, 16))  # sums over nothing alone need a workspace
+    for bad in (dict(work=None), dict(work=p + 4), dict(size=16)):
+        assert pack(**nothing, **bad) == B.DIPACO_EINVAL, bad
     k = 65537
     assert pack(x=S(p, p, 4, k, k + 15), w=S(p, p, 6, k, k + 15)) == B.DIPACO_ELIMIT
     assert pack(x=S(p, p, 1 << 31, 8, 16), y=S(p, p, 1 << 31, 6, 16)) == B.DIPACO_ELIMIT
