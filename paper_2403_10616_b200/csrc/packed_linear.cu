@@ -1037,7 +1037,8 @@ int check_contraction(int64_t m, int64_t n, int64_t k)
 {
     if (k < 0) return DIPACO_EINVAL;
     if (const int rc = check_extents(m, n)) return rc;
-    return k > (int64_t)CHUNK_BF16 * STEP || ceil_div(m, PAIR_ROWS) * ceil_div(n, 128) > INT32_MAX ? DIPACO_ELIMIT : DIPACO_OK;
+    // tiles and the step to a pair's next one fit an int
+    return k > (int64_t)CHUNK_BF16 * STEP || ceil_div(m, PAIR_ROWS) * ceil_div(n, 128) > INT32_MAX - 65536 ? DIPACO_ELIMIT : DIPACO_OK;
 }
 
 int launch_few_pack(const FewPackArgs &p, int tokens, cudaStream_t stream)

@@ -406,9 +406,6 @@ enum : int { GATE_IN_COLUMNS, GATE_OF_ROW, GATE_OF_VALUES };
 
 constexpr int MAX_GROUP_COLS = 8192;  // 128 KB of parameters in shared memory
 
-// How many units of eight values a thread has: few for narrow rows, as many as the registers allow for wide ones.
-template <typename T> constexpr int ROW_UNITS = sizeof(T) == 2 ? 4 : 2;
-
 template <typename T, bool VEC, int GATE, int U>
 __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constant__ NormArgs a, int warps)
 {
@@ -1028,8 +1025,10 @@ template <typename T, bool VEC, int GATE, int U> int launch_groups(const NormArg
 template <typename T, bool VEC, int GATE> int launch_groups(const NormArgs &a, cudaStream_t stream)
 {
     if (a.cols <= 256) return launch_groups<T, VEC, GATE, 1>(a, stream);
-    if (a.cols <= 512 || ROW_UNITS<T> == 2) return launch_groups<T, VEC, GATE, 2>(a, stream);
-    return launch_groups<T, VEC, GATE, ROW_UNITS<T>>(a, stream);
+    if constexpr (sizeof(T) == 2 && VEC) {  // value by value four units spill registers (5662x3345 121 us)
+        if (a.cols > 512) return launch_groups<T, VEC, GATE, 4>(a, stream);
+    }
+    return launch_groups<T, VEC, GATE, 2>(a, stream);
 }
 
 template <typename T> int launch_rows(const NormArgs &a, cudaStream_t stream)
@@ -1085,13 +1084,13 @@ template <typename T, bool VEC, int GATE, int U, int THREADS> int launch_back_gr
     kernel<<<a.parts, groups * warps * 32, parameters + groups * stages * 4 * buffer, stream>>>(a, warps, stages, buffer);
     return launch_status();
 }
-// Narrow rows: one unit for a thread.  Wide ones: two in bf16, for which a thread takes 168 registers, three quarters
-// of the threads; from 6145 columns on these are too few for a row, and some registers are spilled.
+// One unit for a thread leaves registers for 16 warps, two in bf16 for 12, which have less to do for each value: they
+// are faster where rows fill them (16384x2048 122 us against 140) and not where a group of them is alone (8192x4096
+// 155 against 150) or where values come one by one (5662x3345 at odd addresses 197 against 128).
 template <typename T, bool VEC, int GATE> int launch_back_groups(NormArgs &a, cudaStream_t stream)
 {
-    if constexpr (sizeof(T) == 2) {
-        if (a.cols > 6144) return launch_back_groups<T, VEC, GATE, 2, 512>(a, stream);
-        if (a.cols > 256) return launch_back_groups<T, VEC, GATE, 2, 384>(a, stream);
+    if constexpr (sizeof(T) == 2 && VEC) {
+        if (a.cols > 256 && ceil_div(a.cols, 512) <= 6) return launch_back_groups<T, VEC, GATE, 2, 384>(a, stream);
     }
     if (a.cols > 4096) return launch_back_groups<T, VEC, GATE, 2, 512>(a, stream);
     return launch_back_groups<T, VEC, GATE, 1, 512>(a, stream);
