@@ -623,7 +623,7 @@ int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_pac
 
 /*
  * The norm of several gradients together, sqrt of the sum of all their squares, and the gradients times
- * min(1, max_norm / norm).  Squares are added in fp32 for at most 40 values and in fp64 beyond, or in fp64 where
+ * min(1, max_norm / norm).  Squares are added in fp32 for at most 80 values (in chains of 20) and in fp64 beyond, or in fp64 where
  * fp32 would overflow or lose them.  A norm that is not finite shows: with a NaN all results are NaN, with an infinity
  * they are zero, or NaN where the gradient is infinite.
  *   grads        HOST array [count] of device pointers, gradient i being numel[i] contiguous values of dtypes[i]

@@ -5,6 +5,9 @@
 // first, as those are the ones still in L2.  Few values take one launch of a cluster of blocks instead, whose sums
 // meet in distributed shared memory (cluster_kernel).  Tensors are listed in the kernels' arguments, so that a call
 // copies nothing and can be captured; longer lists take several launches.
+//
+// Bound by memory: gradients are read once for the norm and once more to be scaled.  144M in fp32, gathered: 286 us, 1.08
+// of what those bytes take at a copy's rate (the floor without the second reading is 176); 526,080 in two launches 6.7.
 #include "inner_common.cuh"
 
 #include <algorithm>
@@ -15,10 +18,13 @@ using namespace dipaco;
 
 namespace {
 
-constexpr int CHUNK = 8192;  // values
+constexpr int CHUNK = 8192, CLUSTER_CHUNK = 32768;  // values: the few blocks of a cluster need more on their way each
 constexpr int THREADS = 256;
 constexpr int CLUSTER = 8, CLUSTER_THREADS = 512;
-constexpr int CLUSTER_CHUNKS = 128;  // up to a million values: 2 MB take the eight SMs as long as a second launch
+// One launch instead of two and a workspace saves the host 6 us of a call; eight SMs take longer than all of them: 6.4 us
+// for 64,000 values (two launches 6.6), 8.8 for 256,000 (6.6), 15.1 for 512,000 (6.7).  It pays while they are done
+// before the host has made its next call, which takes it 17 us.
+constexpr int CLUSTER_VALUES = 600000;
 constexpr int FEW_TENSORS = 64, MANY_TENSORS = 640;  // 2 and 20 KB of arguments
 constexpr int MAX_BLOCKS = 148 * 8;
 constexpr int MAX_JOINED = 4096;  // sums that every block of scale_kernel joins by itself
@@ -37,7 +43,7 @@ template <int CAPACITY> struct Pieces {
 };
 
 // Chunk `chunk` is values [begin, end) of its piece, which is returned.
-template <int CAPACITY>
+template <int SIZE = CHUNK, int CAPACITY>
 __device__ __forceinline__ const Piece &find_chunk(const Pieces<CAPACITY> &t, unsigned chunk, long long &begin, long long &end)
 {
     int low = 0, high = t.count - 1;  // the last piece whose first chunk is not after this one (it has a chunk)
@@ -49,8 +55,8 @@ __device__ __forceinline__ const Piece &find_chunk(const Pieces<CAPACITY> &t, un
             high = mid - 1;
     }
     const Piece &p = t.piece[low];
-    begin = (long long)(chunk - p.first_chunk) * CHUNK;
-    end = min(p.numel, begin + CHUNK);
+    begin = (long long)(chunk - p.first_chunk) * SIZE;
+    end = min(p.numel, begin + SIZE);
     return p;
 }
 
@@ -94,15 +100,15 @@ template <typename T> __device__ __forceinline__ void add_squares(const uint4 &v
     for (int i = 0; i < Unit<T>::UE / 2; ++i) sum[i & 1] = fma2(w[i], w[i], sum[i & 1]);
 }
 
-// The sum of squares of this thread's values of a chunk.  Squares are added in fp32, at most 40 of them, and where that
-// overflows or loses small values, once more in fp64.
-template <typename T, int N> __device__ __forceinline__ double chunk_squares(const void *p, long long begin, long long end)
+// The sum of squares of this thread's values of a chunk.  Squares are added in fp32, at most 80 of them in four
+// chains, and where that overflows or loses small values, once more in fp64.
+template <typename T, int N, int SIZE> __device__ __forceinline__ double chunk_squares(const void *p, long long begin, long long end)
 {
-    constexpr int UE = Unit<T>::UE, EACH = CHUNK / UE / N;  // units of a thread
+    constexpr int UE = Unit<T>::UE, EACH = SIZE / UE / N;  // units of a thread
     const Units<T> units(p, begin, end);
     f32x2 sum[2] = {0ull, 0ull};
     unsigned bits = 0u;
-    if (units.lead == 0 && units.values == CHUNK) {  // all loads at once
+    if (units.lead == 0 && units.values == SIZE) {  // all loads at once
         uint4 v[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) v[i] = __ldg(units.first + threadIdx.x + i * N);
@@ -124,9 +130,9 @@ template <typename T, int N> __device__ __forceinline__ double chunk_squares(con
     }
     return exact;
 }
-template <int N> __device__ __forceinline__ double piece_squares(const Piece &p, long long begin, long long end)
+template <int N, int SIZE> __device__ __forceinline__ double piece_squares(const Piece &p, long long begin, long long end)
 {
-    return p.in_bf16 ? chunk_squares<__nv_bfloat16, N>(p.in, begin, end) : chunk_squares<float, N>(p.in, begin, end);
+    return p.in_bf16 ? chunk_squares<__nv_bfloat16, N, SIZE>(p.in, begin, end) : chunk_squares<float, N, SIZE>(p.in, begin, end);
 }
 
 // The sum over the block, on every thread.
@@ -150,7 +156,7 @@ __global__ void __launch_bounds__(THREADS) sums_kernel(const __grid_constant__ P
     for (unsigned c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, c, begin, end);
-        sum += piece_squares<THREADS>(p, begin, end);
+        sum += piece_squares<THREADS, CHUNK>(p, begin, end);
     }
     sum = block_sum(sum, shared);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -194,16 +200,16 @@ template <typename T, typename O> __device__ __forceinline__ void store_scaled(c
     }
 }
 
-template <typename T, typename O, int N>
+template <typename T, typename O, int N, int SIZE>
 __device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, long long end, float by)
 {
-    constexpr int UE = Unit<T>::UE, EACH = CHUNK / UE / N;
+    constexpr int UE = Unit<T>::UE, EACH = SIZE / UE / N;
     const T *in = static_cast<const T *>(p.in);
     O *out = static_cast<O *>(p.out);
     const Units<T> units(in, begin, end);
     O *const to = out + begin - units.lead;  // where the first unit's first value would go
     if (reinterpret_cast<uintptr_t>(to) % (UE * sizeof(O) < 16 ? UE * sizeof(O) : 16) == 0) {
-        if (units.lead == 0 && units.values == CHUNK) {
+        if (units.lead == 0 && units.values == SIZE) {
             uint4 v[EACH];
 #pragma unroll
             for (int i = 0; i < EACH; ++i) v[i] = __ldcs(units.first + threadIdx.x + i * N);
@@ -230,19 +236,19 @@ __device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, lon
 #pragma unroll 8
     for (long long i = begin + threadIdx.x; i < end; i += N) out[i] = narrow1<O>(widen1<T>(in[i]) * by);
 }
-template <int N> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, float by)
+template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, float by)
 {
     if (p.in == p.out && by == 1.0f) return;
     if (p.in_bf16) {
         if (p.out_bf16)
-            scale_chunk<__nv_bfloat16, __nv_bfloat16, N>(p, begin, end, by);
+            scale_chunk<__nv_bfloat16, __nv_bfloat16, N, SIZE>(p, begin, end, by);
         else
-            scale_chunk<__nv_bfloat16, float, N>(p, begin, end, by);
+            scale_chunk<__nv_bfloat16, float, N, SIZE>(p, begin, end, by);
     } else {
         if (p.out_bf16)
-            scale_chunk<float, __nv_bfloat16, N>(p, begin, end, by);
+            scale_chunk<float, __nv_bfloat16, N, SIZE>(p, begin, end, by);
         else
-            scale_chunk<float, float, N>(p, begin, end, by);
+            scale_chunk<float, float, N, SIZE>(p, begin, end, by);
     }
 }
 __device__ __forceinline__ float factor(double norm, double most)
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(THREADS)
     for (unsigned i = blockIdx.x; i < t.chunks; i += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, t.chunks - 1 - i, begin, end);
-        scale_piece<THREADS>(p, begin, end, by);
+        scale_piece<THREADS, CHUNK>(p, begin, end, by);
     }
 }
 
@@ -273,8 +279,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(CLUSTER_THREAD
     double sum = 0.0;
     for (unsigned c = blockIdx.x; c < t.chunks; c += CLUSTER) {
         long long begin, end;
-        const Piece &p = find_chunk(t, c, begin, end);
-        sum += piece_squares<CLUSTER_THREADS>(p, begin, end);
+        const Piece &p = find_chunk<CLUSTER_CHUNK>(t, c, begin, end);
+        sum += piece_squares<CLUSTER_THREADS, CLUSTER_CHUNK>(p, begin, end);
     }
     sum = block_sum<CLUSTER_THREADS>(sum, shared);
     if (threadIdx.x == 0) of_block = sum;
@@ -296,8 +302,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(CLUSTER_THREAD
         const float by = factor(of_all, most);
         for (unsigned c = blockIdx.x; c < t.chunks; c += CLUSTER) {
             long long begin, end;
-            const Piece &p = find_chunk(t, c, begin, end);
-            scale_piece<CLUSTER_THREADS>(p, begin, end, by);
+            const Piece &p = find_chunk<CLUSTER_CHUNK>(t, c, begin, end);
+            scale_piece<CLUSTER_THREADS, CLUSTER_CHUNK>(p, begin, end, by);
         }
     }
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -313,24 +319,25 @@ struct Launches {
     int64_t sums = 0;  // of the workspace
 };
 
-int64_t chunks_of(int64_t numel) { return ceil_div(numel, CHUNK); }
+int64_t chunks_of(int64_t numel, int size = CHUNK) { return ceil_div(numel, size); }
 
 int plan(const int64_t *numel, int32_t count, Launches &plan)
 {
     if (count < 0 || (count > 0 && !numel)) return DIPACO_EINVAL;
-    int64_t chunks = 0;
+    int64_t chunks = 0, values = 0;
     for (int i = 0; i < count; ++i) {
         if (numel[i] < 0) return DIPACO_EINVAL;
         if (numel[i] == 0) continue;
         if (numel[i] > ((int64_t)1 << 44)) return DIPACO_ELIMIT;
         plan.tensors.push_back(i);
         chunks += chunks_of(numel[i]);
+        values += numel[i];
         if (chunks > INT32_MAX) return DIPACO_ELIMIT;
     }
     const int tensors = (int)plan.tensors.size();
     plan.per_launch = tensors <= FEW_TENSORS ? FEW_TENSORS : MANY_TENSORS;
     plan.launches = (int)ceil_div(tensors, plan.per_launch);
-    plan.one_cluster = tensors <= FEW_TENSORS && chunks <= CLUSTER_CHUNKS;
+    plan.one_cluster = tensors <= FEW_TENSORS && values <= CLUSTER_VALUES;
     plan.sums = plan.one_cluster ? 0 : (int64_t)plan.launches * MAX_BLOCKS;
     return DIPACO_OK;
 }
@@ -374,7 +381,7 @@ int launch(const Launches &plan, const void *const *grads, void *const *out, con
             const int i = plan.tensors[k];
             t.piece[k - first] = {grads[i], out ? out[i] : nullptr, numel[i], t.chunks, dtypes[i] == DIPACO_BF16,
                                   (unsigned char)(out && out_dtypes[i] == DIPACO_BF16)};
-            t.chunks += (unsigned)chunks_of(numel[i]);
+            t.chunks += (unsigned)chunks_of(numel[i], plan.one_cluster ? CLUSTER_CHUNK : CHUNK);
         }
     };
     if constexpr (CAPACITY == FEW_TENSORS) {

@@ -1,7 +1,8 @@
 """The common norm of many gradients and their clipping against 64 bits.
 
-Squares are added in fp32 for at most 40 values, each addition off by u = 2^-24 of a sum of positive terms, and in
-fp64 beyond: the norm is off by at most 42 u / 2 + u of itself, and under 24 u.  The factor is rounded once more, and
+Squares are added in fp32 in chains of at most 20 values, four of them joined, each addition off by u = 2^-24 of a sum
+of positive terms, and in fp64 beyond: the sum is off by at most 23 u of itself, and the norm by half of that and its own
+rounding, under 24 u.  The factor is rounded once more, and
 so is each product: a result is off by 26 u of itself, and half a unit of bf16 where it is rounded to that.
 """
 from __future__ import annotations
