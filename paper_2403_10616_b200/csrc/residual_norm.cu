@@ -13,6 +13,12 @@
 //   rows_kernel       a block per row, which is read again for every sum: any width
 //   group_back_kernel every gradient in one pass, a row in the registers of a group: up to 8192 columns
 //   back_rows_kernel  as rows_kernel for dx, df and the two means that d needs; back_columns_kernel the sums over rows
+//
+// Measured: 16384x2048 in bf16 61 us (4.4 TB/s) and its gradient 115 (3.5 TB/s), 32768x896 49 and 121, with n and z
+// packed 64 (the packing kernel reads z from L2), 4999x2047 in fp32 49 and 67, 4096x8192 in bf16 92 and 205.
+// Two reads and two writes would take 41 us of the first, four and two 61 of its gradient.  The forward kernel is bound by
+// chains (each row's two sums, one after the other, in 16 warps; issue slots 50 % used), the gradient too: its sums over
+// rows take half of the registers, which leaves 12 warps (issue slots 45 %).
 #include "inner_common.cuh"
 
 #include <algorithm>
