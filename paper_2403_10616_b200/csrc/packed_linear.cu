@@ -14,7 +14,7 @@
 // Measured (one B200, short runs; the bare product of the same operands to bf16 takes 100 us for the first two and 176 for
 // the third): 32768x3584x896 packed with GELU and checkpoint 174 us, 164 without the checkpoint, 117 without either;
 // the gradient of the same extents through the GELU 195, 174 without the sums over rows, 115 without the slopes;
-// 16384x2048x8192 with bias and residual 188; one token through 3584x896, packed, 4.9 on the device.
+// 16384x2048x8192 with bias and residual 188; one token through 3584x896, packed, 5.8 on the device.
 // What bounds the packed forms is the epilogue: 11,300 clocks for a tile whose products take 3,600, of which activations
 // are 3,150 (two powers and one reciprocal for two values at 8 clocks each, all their unit gives).  Its warps wait for
 // their own chains: with 12 or 16 of them registers spill, and with twice the instructions in a loop they no longer stay

@@ -300,11 +300,20 @@ template <bool VEC> __device__ __forceinline__ int param_place(int col, int cols
 {
     return VEC ? ((col >> 2 & 1) * (cols >> 3) + (col >> 3)) * 4 + (col & 3) : col;
 }
+// Which of the row's units are the thread's (VEC); any that is there, where there is none.
+template <int U> struct Places {
+    int unit[U];
+    __device__ Places(const Group &g, int cols)
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) unit[u] = min(u * g.threads + g.thread, max((cols >> 3) - 1, 0));
+    }
+};
 template <bool VEC, int U>
-__device__ __forceinline__ void held_columns(const float *held, const Group &g, unsigned valid, int cols, int unit, f32x2 *v)
+__device__ __forceinline__ void held_columns(const float *held, const Group &g, const Places<U> &places, int cols, int unit, f32x2 *v)
 {
     if constexpr (VEC) {
-        const int at = min(unit * g.threads + g.thread, (cols >> 3) - 1);  // any that is there, where there is no value
+        const int at = places.unit[unit];
         const float4 *p = reinterpret_cast<const float4 *>(held);
         const float4 lo = p[at], hi = p[(cols >> 3) + at];
         v[0] = pair_of(lo.x, lo.y); v[1] = pair_of(lo.z, lo.w);
@@ -421,6 +430,7 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
     Group g = make_group<VEC, U>(warps, a.cols, slots, 1);
     const int groups = (int)(blockDim.x >> 5) / warps;
     const unsigned valid = valid_values<VEC, U>(g.threads, g.thread, a.cols);
+    const Places<U> places(g, a.cols);
     const int row_step = gridDim.x * groups;
     int row = blockIdx.x * groups + g.index;
     const T *f_row = static_cast<const T *>(a.f.dense) + row * a.f.stride, *x_row = static_cast<const T *>(a.x.dense) + row * a.x.stride;
@@ -460,8 +470,8 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             f32x2 factor[4], shift[4];
-            held_columns<VEC, U>(held, g, valid, a.cols, u, factor);
-            held_columns<VEC, U>(held + a.cols, g, valid, a.cols, u, shift);
+            held_columns<VEC, U>(held, g, places, a.cols, u, factor);
+            held_columns<VEC, U>(held + a.cols, g, places, a.cols, u, shift);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = 4 * u + i;
@@ -482,8 +492,8 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     f32x2 gamma[4], beta[4];
-                    held_columns<VEC, U>(held + 2 * a.cols, g, valid, a.cols, u, gamma);
-                    held_columns<VEC, U>(held + 3 * a.cols, g, valid, a.cols, u, beta);
+                    held_columns<VEC, U>(held + 2 * a.cols, g, places, a.cols, u, gamma);
+                    held_columns<VEC, U>(held + 3 * a.cols, g, places, a.cols, u, beta);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         v[4 * u + i] = fma2(mul2(add2(v[4 * u + i], pair_of(-of_z.x)), pair_of(of_z.y)), gamma[i], beta[i]);
@@ -614,14 +624,13 @@ template <typename T> __device__ __forceinline__ Feed make_feed(const Source &s,
 
 // A row's values in shared memory; where there are none, any of the row.
 template <typename T, bool VEC, int U>
-__device__ __forceinline__ void read_row(const uint8_t *at, const Group &g, int cols, f32x2 *v)
+__device__ __forceinline__ void read_row(const uint8_t *at, const Group &g, const Places<U> &places, int cols, f32x2 *v)
 {
     constexpr int UE = Unit<T>::UE;
     if constexpr (VEC) {
-        const int last = cols / 8 - 1;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint4 *p = reinterpret_cast<const uint4 *>(at) + min(u * g.threads + g.thread, last) * (8 / UE);
+            const uint4 *p = reinterpret_cast<const uint4 *>(at) + places.unit[u] * (8 / UE);
 #pragma unroll
             for (int i = 0; i < 8 / UE; ++i) widen_pairs<T>(p[i], v + 4 * u + i * UE / 2);
         }
@@ -634,17 +643,17 @@ __device__ __forceinline__ void read_row(const uint8_t *at, const Group &g, int 
     }
 }
 template <typename T, bool VEC, int U>
-__device__ __forceinline__ void read_source(const Source &s, int row, const uint8_t *at, const Group &g, int cols, f32x2 *v)
+__device__ __forceinline__ void read_source(const Source &s, int row, const uint8_t *at, const Group &g, const Places<U> &places, int cols, f32x2 *v)
 {
     if (s.dense) {
-        read_row<T, VEC, U>(at, g, cols, v);
+        read_row<T, VEC, U>(at, g, places, cols, v);
         return;
     }
     const uint8_t *scales = s.scales + (long long)(row / PACK_BLOCK) * s.scale_cols;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if constexpr (VEC) {
-            const int unit = min(u * g.threads + g.thread, cols / 8 - 1);
+            const int unit = places.unit[u];
             const uint2 w = reinterpret_cast<const uint2 *>(at)[unit];
             const f32x2 scale = pair_of(scale_value(scales[unit * 8 / PACK_BLOCK]));
             v[4 * u] = mul2(decode_pair(w.x), scale);
@@ -700,6 +709,7 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
     Group g = make_group<VEC, U>(warps, a.cols, slots, 2);
     const int groups = (int)(blockDim.x >> 5) / warps;
     const unsigned valid = valid_values<VEC, U>(g.threads, g.thread, a.cols);
+    const Places<U> places(g, a.cols);
     const int row_step = gridDim.x * groups;
     int row = blockIdx.x * groups + g.index;
     uint8_t *ring = reinterpret_cast<uint8_t *>(held) + (a.cols * 12 + 15) / 16 * 16 + g.index * stages * 4 * buffer;
@@ -752,24 +762,23 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             rstd_z = a.saved[3ll * a.rows + row];
         }
         const float of_row = GATE == GATE_OF_ROW ? load_param(a.gate, a.gate_bf16, row) : 1.0f;
-        if (ok) ok = bounded_wait(&arrived[stage], phase, &g_residual_norm_error, 1);
-        __syncwarp();
+        if (ok) ok = __all_sync(0xffffffffu, bounded_wait(&arrived[stage], phase, &g_residual_norm_error, 1));  // one answer for a warp
         f32x2 d[P], h[P];
         if (dz.bytes) {
-            read_row<T, VEC, U>(from + 2 * buffer + dz.ahead(row), g, a.cols, d);
+            read_row<T, VEC, U>(from + 2 * buffer + (VEC ? 0 : dz.ahead(row)), g, places, a.cols, d);
         } else {
 #pragma unroll
             for (int k = 0; k < P; ++k) d[k] = 0ull;
         }
         if (a.norm) {
             f32x2 y[P], all[2] = {0ull, 0ull};
-            read_row<T, VEC, U>(from + dn.ahead(row), g, a.cols, y);
-            read_source<T, VEC, U>(a.z, row, from + buffer + z.ahead(row), g, a.cols, h);
+            read_row<T, VEC, U>(from + (VEC ? 0 : dn.ahead(row)), g, places, a.cols, y);
+            read_source<T, VEC, U>(a.z, row, from + buffer + (VEC ? 0 : z.ahead(row)), g, places, a.cols, h);
             keep_valid_row<VEC, U>(valid, y);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 f32x2 gamma[4];
-                held_columns<VEC, U>(held, g, valid, a.cols, u, gamma);
+                held_columns<VEC, U>(held, g, places, a.cols, u, gamma);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int k = 4 * u + i;
@@ -796,7 +805,7 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             narrow_row<T, U>(out, raw);
             store_row<T, VEC, U>(static_cast<T *>(a.dx) + row * a.dx_stride, g, valid, raw);
         }
-        read_source<T, VEC, U>(a.f, row, from + 3 * buffer + f.ahead(row), g, a.cols, h);
+        read_source<T, VEC, U>(a.f, row, from + 3 * buffer + (VEC ? 0 : f.ahead(row)), g, places, a.cols, h);
         f32x2 gate[P], of_gate = 0ull, all[2] = {0ull, 0ull};
         if (GATE == GATE_OF_VALUES) {
             load_row<T, VEC, U>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);
@@ -805,8 +814,8 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             f32x2 factor[4], shift[4];
-            held_columns<VEC, U>(held + a.cols, g, valid, a.cols, u, factor);
-            if (GATE != GATE_IN_COLUMNS) held_columns<VEC, U>(held + 2 * a.cols, g, valid, a.cols, u, shift);
+            held_columns<VEC, U>(held + a.cols, g, places, a.cols, u, factor);
+            if (GATE != GATE_IN_COLUMNS) held_columns<VEC, U>(held + 2 * a.cols, g, places, a.cols, u, shift);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {  // d is zero outside the row
                 const int k = 4 * u + i;
@@ -841,7 +850,10 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
         }
         // every warp of the group is past its reads of this stage
         __syncwarp();
-        if (g.thread == 0 && ok && row + (long long)stages * row_step < a.rows) request(row + stages * row_step, stage);
+        if (g.warp == 0 && ok && row + (long long)stages * row_step < a.rows) {
+            if (elect_one()) request(row + stages * row_step, stage);
+            __syncwarp();
+        }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
         if (a.df) {
             if (a.post_norm) {
