@@ -14,8 +14,9 @@
 //   group_back_kernel every gradient in one pass, a row in the registers of a group: up to 8192 columns
 //   back_rows_kernel  as rows_kernel for dx, df and the two means that d needs; back_columns_kernel the sums over rows
 //
-// Measured: 16384x2048 in bf16 61 us (4.4 TB/s) and its gradient 115 (3.5 TB/s), 32768x896 49 and 121, with n and z
-// packed 64 (the packing kernel reads z from L2), 4999x2047 in fp32 49 and 67, 4096x8192 in bf16 92 and 205.
+// Measured: 16384x2048 in bf16 56 us (4.8 TB/s) and its gradient 101 (4.0 TB/s), 32768x896 48 and 99, with n and z
+// packed 64 (the packing kernel reads z from L2), 4999x2047 in fp32 44 and 67, 4096x8192 in bf16 70 and 171; a single row
+// of 896 4.4 and 10.
 // Two reads and two writes would take 41 us of the first, four and two 61 of its gradient.  The forward kernel is bound by
 // chains (each row's two sums, one after the other, in 16 warps; issue slots 50 % used), the gradient too: its sums over
 // rows take half of the registers, which leaves 12 warps (issue slots 45 %).
@@ -309,6 +310,45 @@ template <int U> struct Places {
         for (int u = 0; u < U; ++u) unit[u] = min(u * g.threads + g.thread, max((cols >> 3) - 1, 0));
     }
 };
+// Parameters to shared memory, some times the gate of columns.  The loads of four columns are all under way before the
+// first is used: one after another they were half of a call of few rows (40x6316 in fp32 19.7 us, now 10.2).
+struct HeldParam {
+    const void *p;
+    float otherwise;
+    bool gated;
+};
+template <bool VEC, int N>
+__device__ __forceinline__ void hold_params(const NormArgs &a, const HeldParam (&params)[N], float *held)
+{
+    const auto bits_at = [](const void *p, bool bf16, int c) -> unsigned {
+        if (!p) return 0u;
+        return bf16 ? __ldg(static_cast<const unsigned short *>(p) + c) : __ldg(static_cast<const unsigned *>(p) + c);
+    };
+    const auto value_of_bits = [](unsigned bits, bool bf16) { return __uint_as_float(bf16 ? bits << 16 : bits); };
+    const void *const gate = a.gate_kind == DIPACO_GATE_COLS ? a.gate : nullptr;
+    for (int first = threadIdx.x; first < a.cols; first += 4 * blockDim.x) {
+        unsigned bits[4][N], gate_bits[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = min(first + i * (int)blockDim.x, a.cols - 1);
+            gate_bits[i] = bits_at(gate, a.gate_bf16, c);
+#pragma unroll
+            for (int q = 0; q < N; ++q) bits[i][q] = bits_at(params[q].p, a.params_bf16, c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = first + i * (int)blockDim.x;
+            if (c >= a.cols) break;
+            const float by = gate ? value_of_bits(gate_bits[i], a.gate_bf16) : 1.0f;
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                float v = params[q].p ? value_of_bits(bits[i][q], a.params_bf16) : params[q].otherwise;
+                if (params[q].gated && (params[q].p || params[q].otherwise != 0.0f)) v *= by;  // no 0 times an infinite gate
+                held[q * a.cols + param_place<VEC>(c, a.cols)] = v;
+            }
+        }
+    }
+}
 template <bool VEC, int U>
 __device__ __forceinline__ void held_columns(const float *held, const Group &g, const Places<U> &places, int cols, int unit, f32x2 *v)
 {
@@ -440,14 +480,8 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
         load_row<T, VEC, U>(f_row, g, valid, next_f);
         load_row<T, VEC, U>(x_row, g, valid, next_x);
     }
-    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
-        const float gate = a.gate_kind == DIPACO_GATE_COLS ? load_param(a.gate, a.gate_bf16, c) : 1.0f;
-        const int at = param_place<VEC>(c, a.cols);
-        held[at] = gate * param_or(a.post_gamma, a.params_bf16, c, 1.0f);
-        held[a.cols + at] = gate * param_or(a.post_beta, a.params_bf16, c, 0.0f);
-        held[2 * a.cols + at] = param_or(a.gamma, a.params_bf16, c, 1.0f);
-        held[3 * a.cols + at] = param_or(a.beta, a.params_bf16, c, 0.0f);
-    }
+    const HeldParam params[4] = {{a.post_gamma, 1.0f, true}, {a.post_beta, 0.0f, true}, {a.gamma, 1.0f, false}, {a.beta, 0.0f, false}};
+    hold_params<VEC>(a, params, held);
     __syncthreads();
     for (; row < a.rows; row += row_step) {
         f32x2 v[P];
@@ -733,13 +767,8 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages && row + (long long)s * row_step < a.rows; ++s) request(row + s * row_step, s);
     }
-    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
-        const float gate = a.gate_kind == DIPACO_GATE_COLS ? load_param(a.gate, a.gate_bf16, c) : 1.0f;
-        const int at = param_place<VEC>(c, a.cols);
-        held[at] = param_or(a.gamma, a.params_bf16, c, 1.0f);
-        held[a.cols + at] = gate * param_or(a.post_gamma, a.params_bf16, c, 1.0f);
-        held[2 * a.cols + at] = param_or(a.post_beta, a.params_bf16, c, 0.0f);
-    }
+    const HeldParam params[3] = {{a.gamma, 1.0f, false}, {a.post_gamma, 1.0f, true}, {a.post_beta, 0.0f, false}};
+    hold_params<VEC>(a, params, held);
     __syncthreads();
     f32x2 sums[4][P];
 #pragma unroll
@@ -867,26 +896,49 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
     }
     if (!ok)  // a wait ran out: let the copies in flight land before the block ends
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    // the groups' sums, one group after another, in the place of the parameters
+    // the groups' sums, [group][4][cols] in the place of the rows, which everyone has read, then added in their order
+    __syncthreads();
+    float *const own = held + g.index * 4 * a.cols;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        __syncthreads();
-        for (int turn = 0; turn < groups; ++turn) {
-            if (g.index == turn) {
+        if constexpr (VEC) {
 #pragma unroll
-                for (int j = 0; j < 8 * U; ++j) {
-                    const float2 w = values_of(sums[q][j / 2]);
-                    const float own = j & 1 ? w.y : w.x;
-                    if (valid >> j & 1u) {
-                        float &at = held[param_place<VEC>(column<VEC>(g.threads, g.thread, j), a.cols)];
-                        at = turn ? at + own : own;
-                    }
+            for (int u = 0; u < U; ++u)
+                if (valid >> (8 * u) & 1u) {
+                    float4 *const to = reinterpret_cast<float4 *>(own + q * a.cols) + 2 * places.unit[u];
+                    const f32x2 *const w = &sums[q][4 * u];
+                    const float2 w0 = values_of(w[0]), w1 = values_of(w[1]), w2 = values_of(w[2]), w3 = values_of(w[3]);
+                    to[0] = make_float4(w0.x, w0.y, w1.x, w1.y);
+                    to[1] = make_float4(w2.x, w2.y, w3.x, w3.y);
                 }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8 * U; ++j) {
+                const float2 w = values_of(sums[q][j / 2]);
+                if (valid >> j & 1u) own[q * a.cols + column<false>(g.threads, g.thread, j)] = j & 1 ? w.y : w.x;
             }
-            __syncthreads();
         }
-        for (int c = threadIdx.x; c < a.cols; c += blockDim.x)
-            a.partial[((long long)blockIdx.x * 4 + q) * a.cols + c] = held[param_place<VEC>(c, a.cols)];
+    }
+    __syncthreads();
+    const int with_rows = min(groups, a.rows - (int)blockIdx.x * groups);
+    float *const part = a.partial + blockIdx.x * 4ll * a.cols;
+    if constexpr (VEC) {
+        for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+            const float4 *at = reinterpret_cast<const float4 *>(held) + c;
+            float4 sum = *at;
+            for (int i = 1; i < with_rows; ++i) {
+                at += a.cols;
+                const float4 w = *at;
+                sum = make_float4(sum.x + w.x, sum.y + w.y, sum.z + w.z, sum.w + w.w);
+            }
+            reinterpret_cast<float4 *>(part)[c] = sum;
+        }
+    } else {
+        for (int c = threadIdx.x; c < 4 * a.cols; c += blockDim.x) {
+            float sum = held[c];
+            for (int i = 1; i < with_rows; ++i) sum += held[i * 4 * a.cols + c];
+            part[c] = sum;
+        }
     }
 }
 
@@ -1099,18 +1151,19 @@ template <typename T, bool VEC, int GATE, int U, int THREADS> int launch_back_gr
     const int buffer = (a.cols * (int)sizeof(T) + 30) / 16 * 16, parameters = (a.cols * 12 + 15) / 16 * 16;
     const int stages = std::min(MAX_STAGES, (BACK_SMEM - parameters) / (groups * 4 * buffer));
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BACK_SMEM) != cudaSuccess) return launch_status();
-    kernel<<<a.parts, groups * warps * 32, parameters + groups * stages * 4 * buffer, stream>>>(a, warps, stages, buffer);
+    const int smem = std::max(parameters + groups * stages * 4 * buffer, groups * 16 * a.cols);  // rows, and at the end sums
+    kernel<<<a.parts, groups * warps * 32, smem, stream>>>(a, warps, stages, buffer);
     return launch_status();
 }
-// One unit for a thread leaves registers for 16 warps, two in bf16 for 12, which have less to do for each value: they
-// are faster where rows fill them (16384x2048 122 us against 140) and not where a group of them is alone (8192x4096
-// 155 against 150) or where values come one by one (5662x3345 at odd addresses 197 against 128).
+// One unit for a thread leaves registers for 16 warps, two for 12, which have less to do for each value: they are faster
+// (16384x2048 in bf16 101 us against 128, 8192x4096 128 against 134, 8192x2048 in fp32 87 against 95) but for a single
+// unit, which 4096x64 takes 19.5 against 21.5, and where values come one by one (16384x2048 at odd addresses 234 against
+// 146).  More than 4096 columns need two units all the same, and more than 6144 16 warps of them, whose registers do not
+// hold everything (3500x5120 in fp32 159 against 103, 3001x5555 218 against 161).
 template <typename T, bool VEC, int GATE> int launch_back_groups(NormArgs &a, cudaStream_t stream)
 {
-    if constexpr (sizeof(T) == 2 && VEC) {
-        if (a.cols > 256 && ceil_div(a.cols, 512) <= 6) return launch_back_groups<T, VEC, GATE, 2, 384>(a, stream);
-    }
-    if (a.cols > 4096) return launch_back_groups<T, VEC, GATE, 2, 512>(a, stream);
+    if (a.cols > 6144) return launch_back_groups<T, VEC, GATE, 2, 512>(a, stream);
+    if (a.cols > (VEC ? 256 : 4096)) return launch_back_groups<T, VEC, GATE, 2, 384>(a, stream);
     return launch_back_groups<T, VEC, GATE, 1, 512>(a, stream);
 }
 template <typename T, bool VEC> int launch_back_groups(NormArgs &a, cudaStream_t stream)

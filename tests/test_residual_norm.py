@@ -314,6 +314,27 @@ def test_infinities_and_nan_stay_in_their_rows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,pad", [(17, 255, 0), (300, 264, 0), (161, 512, 1), (5, 4096, 0), (5, 4097, 0), (4, 4104, 1), (3, 6144, 0),
+                                           (3, 6145, 0), (160, 6152, 0), (2, 8191, 1)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_widths_around_which_threads_take_other_shares(rows, cols, pad, dtype):
+    run_and_check(rows, cols, dtype, F32, "cols", pad=pad)
+    run_and_check(rows, cols, dtype, F32, "full", pad=pad)
+
+
+@pytest.mark.gpu
+def test_an_infinite_gate_meets_no_zero_that_nobody_gave():
+    for dtype in (F32, BF16):
+        f = torch.randn(3, 40, generator=gen(3)).to(dtype).to(DEV)
+        gate = torch.ones(40, device=DEV)
+        gate[5] = math.inf
+        z, _, _ = inner.residual_norm(torch.zeros_like(f), f, gate=gate, post_norm=False, norm=False)
+        assert torch.equal(z.float(), gate * f.float())
+        z, _, _ = inner.residual_norm(torch.zeros_like(f), f, post_gamma=torch.ones(40, device=DEV), gate=gate, norm=False)
+        assert bool((z[:, 5] == math.inf * torch.sign(f[:, 5].float() - f.float().mean(1))).all())
+
+
+@pytest.mark.gpu
 def test_no_rows_and_no_columns():
     for dtype in (F32, BF16):
         for rows, cols in ((0, 5), (4, 0), (0, 0)):
