@@ -18,12 +18,13 @@ using namespace dipaco;
 
 namespace {
 
-constexpr int CHUNK = 8192, CLUSTER_CHUNK = 32768;  // values: the few blocks of a cluster need more on their way each
+constexpr int CHUNK = 8192, WARP_CHUNK = 2048;  // values, of a block and of a warp
 constexpr int THREADS = 256;
-constexpr int CLUSTER = 8, CLUSTER_THREADS = 512;
-// One launch instead of two and a workspace saves the host 6 us of a call; eight SMs take longer than all of them: 6.4 us
-// for 64,000 values (two launches 6.6), 8.8 for 256,000 (6.6), 15.1 for 512,000 (6.7).  It pays while they are done
-// before the host has made its next call, which takes it 17 us.
+constexpr int CLUSTER = 8, CLUSTER_THREADS = 512, CLUSTER_WARPS = CLUSTER * CLUSTER_THREADS / 32;
+// One launch instead of two and a workspace saves the host 6 us of a call; eight SMs take longer than all of them: 5.4 us
+// for 64,000 values (two launches 6.6), 7.9 for 256,000 (6.6), 12.2 for 526,080 (6.7).  It pays while they are done
+// before the host has made its next call, which takes it 17 us.  A warp has a chunk to itself: tensors are small, and a
+// block to each chunk took 14 us for 64 of 1000 values, which take 6.6 now.
 constexpr int CLUSTER_VALUES = 600000;
 constexpr int FEW_TENSORS = 64, MANY_TENSORS = 640;  // 2 and 20 KB of arguments
 constexpr int MAX_BLOCKS = 148 * 8;
@@ -100,9 +101,9 @@ template <typename T> __device__ __forceinline__ void add_squares(const uint4 &v
     for (int i = 0; i < Unit<T>::UE / 2; ++i) sum[i & 1] = fma2(w[i], w[i], sum[i & 1]);
 }
 
-// The sum of squares of this thread's values of a chunk.  Squares are added in fp32, at most 80 of them in four
+// The sum of squares of thread me's values of a chunk, one of N.  Squares are added in fp32, at most 80 of them in four
 // chains, and where that overflows or loses small values, once more in fp64.
-template <typename T, int N, int SIZE> __device__ __forceinline__ double chunk_squares(const void *p, long long begin, long long end)
+template <typename T, int N, int SIZE> __device__ __forceinline__ double chunk_squares(const void *p, long long begin, long long end, int me)
 {
     constexpr int UE = Unit<T>::UE, EACH = SIZE / UE / N;  // units of a thread
     const Units<T> units(p, begin, end);
@@ -111,18 +112,18 @@ template <typename T, int N, int SIZE> __device__ __forceinline__ double chunk_s
     if (units.lead == 0 && units.values == SIZE) {  // all loads at once
         uint4 v[EACH];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) v[i] = __ldg(units.first + threadIdx.x + i * N);
+        for (int i = 0; i < EACH; ++i) v[i] = __ldg(units.first + me + i * N);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) add_squares<T>(v[i], sum, bits);
     } else {
 #pragma unroll 4
-        for (int u = threadIdx.x; u < units.count; u += N) add_squares<T>(load_masked(units, u), sum, bits);
+        for (int u = me; u < units.count; u += N) add_squares<T>(load_masked(units, u), sum, bits);
     }
     const float s = sum_of(add2(sum[0], sum[1]));
     const bool nothing = (bits & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu)) == 0u;
     if ((s >= 1e-28f && s <= 1e38f) || nothing) return s;
     double exact = 0.0;
-    for (int u = threadIdx.x; u < units.count; u += N) {
+    for (int u = me; u < units.count; u += N) {
         float f[UE];
         Unit<T>::widen(load_masked(units, u), f);
 #pragma unroll
@@ -130,9 +131,9 @@ template <typename T, int N, int SIZE> __device__ __forceinline__ double chunk_s
     }
     return exact;
 }
-template <int N, int SIZE> __device__ __forceinline__ double piece_squares(const Piece &p, long long begin, long long end)
+template <int N, int SIZE> __device__ __forceinline__ double piece_squares(const Piece &p, long long begin, long long end, int me)
 {
-    return p.in_bf16 ? chunk_squares<__nv_bfloat16, N, SIZE>(p.in, begin, end) : chunk_squares<float, N, SIZE>(p.in, begin, end);
+    return p.in_bf16 ? chunk_squares<__nv_bfloat16, N, SIZE>(p.in, begin, end, me) : chunk_squares<float, N, SIZE>(p.in, begin, end, me);
 }
 
 // The sum over the block, on every thread.
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(THREADS) sums_kernel(const __grid_constant__ P
     for (unsigned c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, c, begin, end);
-        sum += piece_squares<THREADS, CHUNK>(p, begin, end);
+        sum += piece_squares<THREADS, CHUNK>(p, begin, end, threadIdx.x);
     }
     sum = block_sum(sum, shared);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
@@ -201,54 +202,66 @@ template <typename T, typename O> __device__ __forceinline__ void store_scaled(c
 }
 
 template <typename T, typename O, int N, int SIZE>
-__device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, long long end, float by)
+__device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, long long end, float by, int me)
 {
     constexpr int UE = Unit<T>::UE, EACH = SIZE / UE / N;
-    const T *in = static_cast<const T *>(p.in);
-    O *out = static_cast<O *>(p.out);
-    const Units<T> units(in, begin, end);
-    O *const to = out + begin - units.lead;  // where the first unit's first value would go
+    constexpr int AT_ONCE = N == 32 ? 16 : 8;  // loads that wait for no store: the few warps of a cluster need more
+    const T *const in = static_cast<const T *>(p.in) + begin;
+    O *const out = static_cast<O *>(p.out) + begin;
+    const Units<T> units(in, 0, end - begin);
+    O *const to = out - units.lead;  // where the first unit's first value would go
+    int head = 0, tail = 0;          // values before the whole units; the first one after them
     if (reinterpret_cast<uintptr_t>(to) % (UE * sizeof(O) < 16 ? UE * sizeof(O) : 16) == 0) {
         if (units.lead == 0 && units.values == SIZE) {
             uint4 v[EACH];
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) v[i] = __ldcs(units.first + threadIdx.x + i * N);
+            for (int i = 0; i < EACH; ++i) v[i] = __ldcs(units.first + me + i * N);
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) store_scaled<T, O>(v[i], by, to + (threadIdx.x + i * N) * UE);
+            for (int i = 0; i < EACH; ++i) store_scaled<T, O>(v[i], by, to + (me + i * N) * UE);
             return;
         }
-        for (int u = threadIdx.x; u < units.count; u += N) {
-            const uint4 v = __ldcs(units.first + u);
-            O *q = to + (long long)u * UE;
-            if (units.whole(u)) {
-                store_scaled<T, O>(v, by, q);
-            } else {
-                float f[UE];
-                Unit<T>::widen(v, f);
+        const int whole = units.lead ? 1 : 0, last = (units.lead + units.values) / UE;
+        head = min(units.values, whole * UE - units.lead);
+        tail = max(head, last * UE - units.lead);
+        int u = whole + me;
+#pragma unroll 1
+        for (; u + (AT_ONCE / 4 - 1) * N < last; u += AT_ONCE / 4 * N) {
+            uint4 v[AT_ONCE / 4];
 #pragma unroll
-                for (int i = 0; i < UE; ++i)
-                    if (units.holds(u, i)) q[i] = narrow1<O>(f[i] * by);
-            }
+            for (int k = 0; k < AT_ONCE / 4; ++k) v[k] = __ldcs(units.first + u + k * N);
+#pragma unroll
+            for (int k = 0; k < AT_ONCE / 4; ++k) store_scaled<T, O>(v[k], by, to + (u + k * N) * UE);
         }
-        return;
+#pragma unroll 1
+        for (; u < last; u += N) store_scaled<T, O>(__ldcs(units.first + u), by, to + u * UE);
+        if (me < head) out[me] = narrow1<O>(widen1<T>(in[me]) * by);
     }
-    // results at another place within 16 bytes than the values: a value per thread
-#pragma unroll 8
-    for (long long i = begin + threadIdx.x; i < end; i += N) out[i] = narrow1<O>(widen1<T>(in[i]) * by);
+    // the rest, or all where results lie at another place within 16 bytes than the values: value by value
+    int i = tail + me;
+#pragma unroll 1
+    for (; i + (AT_ONCE - 1) * N < units.values; i += AT_ONCE * N) {
+        T v[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) v[k] = in[i + k * N];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) out[i + k * N] = narrow1<O>(widen1<T>(v[k]) * by);
+    }
+#pragma unroll 1
+    for (; i < units.values; i += N) out[i] = narrow1<O>(widen1<T>(in[i]) * by);
 }
-template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, float by)
+template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, float by, int me)
 {
     if (p.in == p.out && by == 1.0f) return;
     if (p.in_bf16) {
         if (p.out_bf16)
-            scale_chunk<__nv_bfloat16, __nv_bfloat16, N, SIZE>(p, begin, end, by);
+            scale_chunk<__nv_bfloat16, __nv_bfloat16, N, SIZE>(p, begin, end, by, me);
         else
-            scale_chunk<__nv_bfloat16, float, N, SIZE>(p, begin, end, by);
+            scale_chunk<__nv_bfloat16, float, N, SIZE>(p, begin, end, by, me);
     } else {
         if (p.out_bf16)
-            scale_chunk<float, __nv_bfloat16, N, SIZE>(p, begin, end, by);
+            scale_chunk<float, __nv_bfloat16, N, SIZE>(p, begin, end, by, me);
         else
-            scale_chunk<float, float, N, SIZE>(p, begin, end, by);
+            scale_chunk<float, float, N, SIZE>(p, begin, end, by, me);
     }
 }
 __device__ __forceinline__ float factor(double norm, double most)
@@ -267,7 +280,7 @@ __global__ void __launch_bounds__(THREADS)
     for (unsigned i = blockIdx.x; i < t.chunks; i += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, t.chunks - 1 - i, begin, end);
-        scale_piece<THREADS, CHUNK>(p, begin, end, by);
+        scale_piece<THREADS, CHUNK>(p, begin, end, by, threadIdx.x);
     }
 }
 
@@ -276,11 +289,13 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(CLUSTER_THREAD
     cluster_kernel(const __grid_constant__ Pieces<FEW_TENSORS> t, bool scale, double most, float *norm)
 {
     __shared__ double shared[CLUSTER_THREADS / 32], of_block;
+    const unsigned warp = threadIdx.x / 32 * CLUSTER + blockIdx.x;  // of the cluster
+    const int lane = threadIdx.x & 31;
     double sum = 0.0;
-    for (unsigned c = blockIdx.x; c < t.chunks; c += CLUSTER) {
+    for (unsigned c = warp; c < t.chunks; c += CLUSTER_WARPS) {
         long long begin, end;
-        const Piece &p = find_chunk<CLUSTER_CHUNK>(t, c, begin, end);
-        sum += piece_squares<CLUSTER_THREADS, CLUSTER_CHUNK>(p, begin, end);
+        const Piece &p = find_chunk<WARP_CHUNK>(t, c, begin, end);
+        sum += piece_squares<32, WARP_CHUNK>(p, begin, end, lane);
     }
     sum = block_sum<CLUSTER_THREADS>(sum, shared);
     if (threadIdx.x == 0) of_block = sum;
@@ -300,10 +315,10 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(CLUSTER_THREAD
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)of_all;
     if (scale) {
         const float by = factor(of_all, most);
-        for (unsigned c = blockIdx.x; c < t.chunks; c += CLUSTER) {
+        for (unsigned c = warp; c < t.chunks; c += CLUSTER_WARPS) {
             long long begin, end;
-            const Piece &p = find_chunk<CLUSTER_CHUNK>(t, c, begin, end);
-            scale_piece<CLUSTER_THREADS, CLUSTER_CHUNK>(p, begin, end, by);
+            const Piece &p = find_chunk<WARP_CHUNK>(t, c, begin, end);
+            scale_piece<32, WARP_CHUNK>(p, begin, end, by, lane);
         }
     }
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -381,7 +396,7 @@ int launch(const Launches &plan, const void *const *grads, void *const *out, con
             const int i = plan.tensors[k];
             t.piece[k - first] = {grads[i], out ? out[i] : nullptr, numel[i], t.chunks, dtypes[i] == DIPACO_BF16,
                                   (unsigned char)(out && out_dtypes[i] == DIPACO_BF16)};
-            t.chunks += (unsigned)chunks_of(numel[i], plan.one_cluster ? CLUSTER_CHUNK : CHUNK);
+            t.chunks += (unsigned)chunks_of(numel[i], plan.one_cluster ? WARP_CHUNK : CHUNK);
         }
     };
     if constexpr (CAPACITY == FEW_TENSORS) {
