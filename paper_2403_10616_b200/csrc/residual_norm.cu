@@ -303,12 +303,9 @@ template <bool VEC> __device__ __forceinline__ int param_place(int col, int cols
 }
 // Which of the row's units are the thread's (VEC); any that is there, where there is none.
 template <int U> struct Places {
-    int unit[U];
-    __device__ Places(const Group &g, int cols)
-    {
-#pragma unroll
-        for (int u = 0; u < U; ++u) unit[u] = min(u * g.threads + g.thread, max((cols >> 3) - 1, 0));
-    }
+    int thread, threads, last;
+    __device__ Places(const Group &g, int cols) : thread(g.thread), threads(g.threads), last(max((cols >> 3) - 1, 0)) {}
+    __device__ __forceinline__ int unit(int u) const { return min(u * threads + thread, last); }
 };
 // Parameters to shared memory, some times the gate of columns.  The loads of four columns are all under way before the
 // first is used: one after another they were half of a call of few rows (40x6316 in fp32 19.7 us, now 10.2).
@@ -353,7 +350,7 @@ template <bool VEC, int U>
 __device__ __forceinline__ void held_columns(const float *held, const Group &g, const Places<U> &places, int cols, int unit, f32x2 *v)
 {
     if constexpr (VEC) {
-        const int at = places.unit[unit];
+        const int at = places.unit(unit);
         const float4 *p = reinterpret_cast<const float4 *>(held);
         const float4 lo = p[at], hi = p[(cols >> 3) + at];
         v[0] = pair_of(lo.x, lo.y); v[1] = pair_of(lo.z, lo.w);
@@ -664,7 +661,7 @@ __device__ __forceinline__ void read_row(const uint8_t *at, const Group &g, cons
     if constexpr (VEC) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint4 *p = reinterpret_cast<const uint4 *>(at) + places.unit[u] * (8 / UE);
+            const uint4 *p = reinterpret_cast<const uint4 *>(at) + places.unit(u) * (8 / UE);
 #pragma unroll
             for (int i = 0; i < 8 / UE; ++i) widen_pairs<T>(p[i], v + 4 * u + i * UE / 2);
         }
@@ -687,7 +684,7 @@ __device__ __forceinline__ void read_source(const Source &s, int row, const uint
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if constexpr (VEC) {
-            const int unit = places.unit[u];
+            const int unit = places.unit(u);
             const uint2 w = reinterpret_cast<const uint2 *>(at)[unit];
             const f32x2 scale = pair_of(scale_value(scales[unit * 8 / PACK_BLOCK]));
             v[4 * u] = mul2(decode_pair(w.x), scale);
@@ -905,7 +902,7 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (valid >> (8 * u) & 1u) {
-                    float4 *const to = reinterpret_cast<float4 *>(own + q * a.cols) + 2 * places.unit[u];
+                    float4 *const to = reinterpret_cast<float4 *>(own + q * a.cols) + 2 * places.unit(u);
                     const f32x2 *const w = &sums[q][4 * u];
                     const float2 w0 = values_of(w[0]), w1 = values_of(w[1]), w2 = values_of(w[2]), w3 = values_of(w[3]);
                     to[0] = make_float4(w0.x, w0.y, w1.x, w1.y);
