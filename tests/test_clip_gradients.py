@@ -84,6 +84,24 @@ def test_norm_and_clipping(sizes, dtypes, offsets):
 
 
 @pytest.mark.gpu
+def test_a_tensor_whose_offsets_pass_32_bits():
+    """2^31 values and some, nearly all of them nothing: the others' squares are whole numbers."""
+    count = (1 << 31) + 8197
+    g = torch.zeros(count, dtype=BF16, device=DEV)
+    marks = {0: 3.0, 8191: -4.0, (1 << 30) + 5: 12.0, (1 << 31) - 1: 2.0, 1 << 31: 6.0, (1 << 31) + 1: -2.0, count - 1: 84.0}
+    for i, v in marks.items():
+        g[i] = v
+    norm = math.sqrt(sum(v * v for v in marks.values()))
+    assert abs(float(inner.gradient_norm([g])) - norm) <= NORM_OFF * norm
+    flat, got = inner.gather_gradients([torch.ones(1, dtype=BF16, device=DEV), g], dtype=BF16)  # at another place within 16 bytes
+    assert abs(float(got) - math.sqrt(norm * norm + 1)) <= NORM_OFF * norm
+    assert torch.equal(flat[1:], g)
+    del flat
+    inner.clip_gradients([g], norm / 2)  # halves, which bf16 holds; the factor is off by less than a quarter of its units
+    assert all(float(g[i]) == v / 2 for i, v in marks.items()) and int(torch.count_nonzero(g)) == len(marks)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("count", [64, 65, 640, 641, 1300])
 def test_many_tensors(count):
     sizes = [1 + (i * 37) % 501 for i in range(count)]

@@ -251,6 +251,39 @@ def test_results_stay_inside_a_slice_of_a_wider_buffer(m, n, first, stride):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m,stride", [(3, 1 << 31), (100, 1 << 26)])
+def test_rows_whose_offsets_pass_32_bits(m, stride):
+    """Operands, checkpoint and residual with rows far apart give what the same rows give side by side."""
+    n, k = 320, 256
+    x, w, back = (random_packed_on_device(i, *shape)[0] for i, shape in enumerate(((m, k), (n, k), (k, n))))
+    a = random_packed_on_device(3, m, n)[0]
+    residual = torch.randn(m, n, generator=gen(4)).to(BF16).to(DEV)
+    bias = vector(5, n).to(DEV)
+
+    def far(p):
+        hold = torch.empty((m - 1) * stride + p.shape[1], dtype=torch.uint8, device=DEV)
+        codes = hold.as_strided(p.shape, (stride, 1))
+        codes.copy_(p.codes.view(torch.uint8))
+        return inner.Packed(codes.view(torch.float8_e4m3fn), p.scales)
+
+    def far_dense(t):
+        hold = torch.empty((m - 1) * (stride // 2) + n, dtype=BF16, device=DEV)
+        view = hold.as_strided(t.shape, (stride // 2, 1))
+        return view.copy_(t)
+
+    def everything(x, a, residual):
+        dense = inner.packed_linear(x, w, bias, "gelu", residual)
+        y, kept = inner.packed_linear_pack(x, w, bias, "silu")
+        da, dbias = inner.packed_linear_pack_backward(x, back, a, "gelu")
+        return [t.view(torch.uint8) if t.element_size() == 1 else t
+                for t in (dense, y.codes, y.scales, kept.codes, kept.scales, da.codes, da.scales, dbias)]
+
+    near = everything(x, a, residual)
+    for got, want in zip(everything(far(x), far(a), far_dense(residual)), near):
+        assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
 def test_sums_over_nothing():
     dev = torch.device(DEV)
     bias = vector(1, 200)

@@ -335,6 +335,34 @@ def test_an_infinite_gate_meets_no_zero_that_nobody_gave():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cols,stride,at", [(896, 1 << 30, 0), (1001, (1 << 30) + 1, 3), (9000, 1 << 30, 0)])
+def test_rows_whose_offsets_pass_32_bits(cols, stride, at):
+    """Three rows of bf16 over 4 GB apart have the results of the same rows, placed the same way within 16 bytes, side by side."""
+    _, d = inputs(3, cols, BF16, F32, "full")
+
+    def far(t):
+        hold = torch.empty(2 * stride + at + cols, dtype=BF16, device=DEV)
+        view = hold.as_strided((3, cols), (stride, 1), at)
+        view.copy_(t)
+        return view
+
+    def near(t):
+        return place(t.cpu(), stride % 8 + 8 - cols % 8, at)
+
+    results = []
+    for put in (near, far):
+        x, f, gate = put(d["x"]), put(d["f"]), put(d["gate"])
+        z, n, stats = inner.residual_norm(x, f, *(d[k] for k in NAMES), gate, 0.5)
+        del x
+        z_far, dn, dz = put(z), put(d["dn"]), put(d["dz"])
+        back = inner.residual_norm_backward(dn, dz, f, z_far, stats, d["gamma"], d["post_gamma"], d["post_beta"], gate, 0.5)
+        results.append((z, n, stats, *back))
+        del f, gate, z_far, dn, dz
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
 def test_no_rows_and_no_columns():
     for dtype in (F32, BF16):
         for rows, cols in ((0, 5), (4, 0), (0, 0)):
