@@ -258,11 +258,13 @@ __device__ __forceinline__ void load_row(const void *row, const Group &g, unsign
     }
 }
 // A row of a gate of values that the next pass loads, into L2 (16384x2048 in bf16 76 us without it, 70 with it, the
-// gradient 131 and 123; 4999x2047 in fp32 56 and 57, 82 and 78).
+// gradient 131 and 123; 4999x2047 in fp32 56 and 57, 82 and 78).  Whole units of fp32 lose by it (8192x2048 64 and 65,
+// 109 and 113).
 template <typename T, bool VEC, int U>
 __device__ __forceinline__ void prefetch_row(const void *row, const Group &g, unsigned valid)
 {
     constexpr int EACH = VEC ? Unit<T>::UE : 1;  // values of a load
+    if (VEC && sizeof(T) == 4) return;
     if (g.lane % (128 / EACH / (int)sizeof(T)) != 0) return;  // a lane for each 128 bytes
 #pragma unroll
     for (int j = 0; j < 8 * U; j += EACH)
