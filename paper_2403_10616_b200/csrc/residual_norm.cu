@@ -430,12 +430,13 @@ template <int R> __device__ __forceinline__ const float2 *exchange(Group &g, con
 // Mean and 1 / sqrt(var + eps) of the group's row.  Differences are taken from the mean of the warp's first lane's
 // values: it is exact where all values are equal, and no farther from the warp's mean than the spread of the warp's
 // values times sqrt(32), so that the squares lose five bits at most.  The warps are joined about the first one's mean.
+// In units that are not the row's there may be anything (VEC; zeros otherwise): they are left out of every sum.
 template <bool VEC, int U>
 __device__ __forceinline__ float2 group_statistics(Group &g, const f32x2 *v, unsigned valid, float eps)
 {
-    f32x2 first = sum4(v);
+    f32x2 first = sum4(v);  // the first lane's first unit is the row's
 #pragma unroll
-    for (int u = 1; u < U; ++u) first = add2(first, sum4(v + 4 * u));
+    for (int u = 1; u < U; ++u) first = add2(first, if_valid<VEC>(valid, u, sum4(v + 4 * u)));
     const float centre = __shfl_sync(0xffffffffu, sum_of(first) * g.of_first, 0);
     f32x2 all = 0ull, squares = 0ull;
 #pragma unroll

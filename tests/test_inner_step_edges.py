@@ -1,0 +1,49 @@
+"""Edges of the operators around a block, the linear layers and clipping, against 64 bits.
+
+Tolerances are those of the operators' own tests (``check_norm``, ``product_tolerance``) unless stated.
+"""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2403_10616_b200 import inner
+from tests import inner_reference as ref
+from tests.test_inner_ops import BF16, DEV, F32, U, gen
+from tests.test_residual_norm import check_norm
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ norms around a block
+
+@pytest.mark.parametrize("cols", [264, 520, 640, 1280, 2560, 5000, 7176])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", [None, "cols", "rows", "full"])
+def test_a_partly_filled_unit_adds_nothing_to_the_second_norm(cols, dtype, kind):
+    """Units behind a row hold zeros, which the norm of f takes far away where its mean is large beside its spread."""
+    rows, eps = 6, 1e-5
+    f = torch.stack([100.0 + torch.randn(cols, generator=gen(1)), torch.full((cols,), 100.0), torch.full((cols,), 100.0),
+                     torch.full((cols,), -3.0e4), 1000.0 + 10 * torch.randn(cols, generator=gen(2)),
+                     torch.randn(cols, generator=gen(3))]).to(dtype)
+    x = torch.stack([torch.randn(cols, generator=gen(4)), torch.randn(cols, generator=gen(5)), torch.full((cols,), 4.0),
+                     torch.full((cols,), 1.5), 30.0 + torch.randn(cols, generator=gen(6)),
+                     torch.randn(cols, generator=gen(7))]).to(dtype)
+    gamma, beta = torch.randn(cols, generator=gen(8)) * 0.3 + 1.0, torch.randn(cols, generator=gen(9)) * 0.3
+    post, shift = torch.randn(cols, generator=gen(10)) * 0.3 + 1.0, torch.zeros(cols)
+    gate = None
+    if kind:
+        gate = (torch.rand({"cols": (cols,), "rows": (rows, 1), "full": (rows, cols)}[kind], generator=gen(11)) + 0.5).to(dtype)
+    on = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    given = (on(gamma), on(beta), on(post), on(shift), on(gate), 0.5)
+    z, n, stats = inner.residual_norm(on(x), on(f), *given)
+    st, held = stats.cpu(), z.cpu().double()
+    what = str((cols, dtype, kind))
+    check_norm(None, st[0], st[1], f.double(), None, None, eps, dtype, what + " f")
+    check_norm(n, st[2], st[3], held, gamma, beta, eps, dtype, what + " n")
+    z_too, n_too, kept, stats_too = inner.residual_norm_pack(on(x), on(f), *given)
+    assert torch.equal(z, z_too) and torch.equal(stats, stats_too)
+    mean, rstd = (s.double()[:, None] for s in st[2:])
+    want = (held - mean) * rstd * gamma.double() + beta.double()
+    ref.assert_packed_close(n_too.codes, n_too.scales, want,
+                            8 * U * (want.abs() + 2 * (1 + (held * rstd).abs()) * gamma.double().abs()), what + " packed")
