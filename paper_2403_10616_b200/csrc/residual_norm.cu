@@ -321,40 +321,41 @@ template <int U> struct Places {
     __device__ Places(const Group &g, int cols) : thread(g.thread), threads(g.threads), last(max((cols >> 3) - 1, 0)) {}
     __device__ __forceinline__ int unit(int u) const { return min(u * threads + thread, last); }
 };
-// Parameters to shared memory, some times the gate of columns.  The loads of four columns are all under way before the
-// first is used: one after another they were half of a call of few rows (40x6316 in fp32 19.7 us, now 10.2).
+// Parameters to shared memory, in the gradient some times the gate of columns.  The loads of four columns are all under
+// way before the first is used: one after another they were half of a call of few rows (40x6316 in fp32 19.7 us, now 10.2).
 struct HeldParam {
     const void *p;
+    bool bf16;
     float otherwise;
-    bool gated;
+    const void *gate;  // of columns, or NULL
 };
 template <bool VEC, int N>
-__device__ __forceinline__ void hold_params(const NormArgs &a, const HeldParam (&params)[N], float *held)
+__device__ __forceinline__ void hold_params(const NormArgs &a, const HeldParam *params, float *held)
 {
     const auto bits_at = [](const void *p, bool bf16, int c) -> unsigned {
         if (!p) return 0u;
         return bf16 ? __ldg(static_cast<const unsigned short *>(p) + c) : __ldg(static_cast<const unsigned *>(p) + c);
     };
     const auto value_of_bits = [](unsigned bits, bool bf16) { return __uint_as_float(bf16 ? bits << 16 : bits); };
-    const void *const gate = a.gate_kind == DIPACO_GATE_COLS ? a.gate : nullptr;
     for (int first = threadIdx.x; first < a.cols; first += 4 * blockDim.x) {
-        unsigned bits[4][N], gate_bits[4];
+        unsigned bits[4][N], gate_bits[4][N];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = min(first + i * (int)blockDim.x, a.cols - 1);
-            gate_bits[i] = bits_at(gate, a.gate_bf16, c);
 #pragma unroll
-            for (int q = 0; q < N; ++q) bits[i][q] = bits_at(params[q].p, a.params_bf16, c);
+            for (int q = 0; q < N; ++q) {
+                bits[i][q] = bits_at(params[q].p, params[q].bf16, c);
+                gate_bits[i][q] = bits_at(params[q].gate, a.gate_bf16, c);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int c = first + i * (int)blockDim.x;
             if (c >= a.cols) break;
-            const float by = gate ? value_of_bits(gate_bits[i], a.gate_bf16) : 1.0f;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                float v = params[q].p ? value_of_bits(bits[i][q], a.params_bf16) : params[q].otherwise;
-                if (params[q].gated && (params[q].p || params[q].otherwise != 0.0f)) v *= by;  // no 0 times an infinite gate
+                float v = params[q].p ? value_of_bits(bits[i][q], params[q].bf16) : params[q].otherwise;
+                if (params[q].gate) v *= value_of_bits(gate_bits[i][q], a.gate_bf16);
                 held[q * a.cols + param_place<VEC>(c, a.cols)] = v;
             }
         }
@@ -471,13 +472,17 @@ __device__ __forceinline__ float2 group_statistics(Group &g, const f32x2 *v, uns
 // GATE: what a thread needs for it.
 enum : int { GATE_IN_COLUMNS, GATE_OF_ROW, GATE_OF_VALUES };
 
-constexpr int MAX_GROUP_COLS = 8192;  // 128 KB of parameters in shared memory
+constexpr int MAX_GROUP_COLS = 8192;  // 160 KB of parameters in shared memory
+
+// Vectors that the threads of group_rows_kernel read from there.  A gate of columns is one of its own: multiplied into
+// the others it would turn gate (h post_gamma + 0) into NaN where it is infinite, and overflow where gate p does not.
+template <int GATE> constexpr int HELD_VECTORS = GATE == GATE_IN_COLUMNS ? 5 : 4;
 
 template <typename T, bool VEC, int GATE, int U>
 __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constant__ NormArgs a, int warps)
 {
     constexpr int P = 4 * U;
-    extern __shared__ __align__(16) float held[];  // [4][cols]: p = h factor + shift, a gate of columns in both; gamma, beta
+    extern __shared__ __align__(16) float held[];  // [HELD_VECTORS][cols]: p = h factor + shift; gamma, beta; gate
     __shared__ float2 slots[2 * 16];
     Group g = make_group<VEC, U>(warps, a.cols, slots, 1);
     const int groups = (int)(blockDim.x >> 5) / warps;
@@ -492,8 +497,11 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
         load_row<T, VEC, U>(f_row, g, valid, next_f);
         load_row<T, VEC, U>(x_row, g, valid, next_x);
     }
-    const HeldParam params[4] = {{a.post_gamma, 1.0f, true}, {a.post_beta, 0.0f, true}, {a.gamma, 1.0f, false}, {a.beta, 0.0f, false}};
-    hold_params<VEC>(a, params, held);
+    const bool bf16 = a.params_bf16;
+    const HeldParam params[5] = {{a.post_gamma, bf16, 1.0f, nullptr}, {a.post_beta, bf16, 0.0f, nullptr},
+                                 {a.gamma, bf16, 1.0f, nullptr}, {a.beta, bf16, 0.0f, nullptr},
+                                 {a.gate_kind == DIPACO_GATE_COLS ? a.gate : nullptr, a.gate_bf16, 1.0f, nullptr}};
+    hold_params<VEC, HELD_VECTORS<GATE>>(a, params, held);
     __syncthreads();
     for (; row < a.rows; row += row_step) {
         f32x2 v[P];
@@ -516,17 +524,16 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
         if (GATE == GATE_OF_VALUES) widen_row<T, U>(raw, gate);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            f32x2 factor[4], shift[4];
+            f32x2 factor[4], shift[4], by[4];
             held_columns<VEC, U>(held, g, places, a.cols, u, factor);
             held_columns<VEC, U>(held + a.cols, g, places, a.cols, u, shift);
+            if (GATE == GATE_IN_COLUMNS) held_columns<VEC, U>(held + 4 * a.cols, g, places, a.cols, u, by);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = 4 * u + i;
                 const f32x2 p = fma2(mul2(add2(v[k], pair_of(-of_f.x)), pair_of(of_f.y)), factor[i], shift[i]);
-                if (GATE == GATE_IN_COLUMNS)
-                    v[k] = fma2(stream[k], pair_of(a.scale), p);
-                else
-                    v[k] = fma2(GATE == GATE_OF_ROW ? of_row : gate[k], p, mul2(stream[k], pair_of(a.scale)));
+                v[k] = fma2(GATE == GATE_IN_COLUMNS ? by[i] : GATE == GATE_OF_ROW ? of_row : gate[k], p,
+                            mul2(stream[k], pair_of(a.scale)));
             }
             keep_valid<VEC>(valid, u, v + 4 * u);
         }
@@ -780,8 +787,11 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         for (int s = 0; s < stages && row + (long long)s * row_step < a.rows; ++s) request(row + s * row_step, s);
     }
-    const HeldParam params[3] = {{a.gamma, 1.0f, false}, {a.post_gamma, 1.0f, true}, {a.post_beta, 0.0f, false}};
-    hold_params<VEC>(a, params, held);
+    const bool bf16 = a.params_bf16;
+    const HeldParam params[3] = {{a.gamma, bf16, 1.0f, nullptr},
+                                 {a.post_gamma, bf16, 1.0f, a.gate_kind == DIPACO_GATE_COLS ? a.gate : nullptr},
+                                 {a.post_beta, bf16, 0.0f, nullptr}};
+    hold_params<VEC, 3>(a, params, held);
     __syncthreads();
     f32x2 sums[4][P];
 #pragma unroll
@@ -1101,10 +1111,11 @@ template <typename T, bool VEC, int GATE, int U> int launch_groups(const NormArg
 {
     const auto kernel = group_rows_kernel<T, VEC, GATE, U>;
     const int warps = (int)ceil_div(a.cols, 256 * U), groups = 16 / warps;
-    if (a.cols * 16 > 48 * 1024 &&
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_GROUP_COLS * 16) != cudaSuccess)
+    constexpr int held = HELD_VECTORS<GATE> * (int)sizeof(float);  // bytes of a column
+    if (a.cols * held > 48 * 1024 &&
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_GROUP_COLS * held) != cudaSuccess)
         return launch_status();
-    kernel<<<(unsigned)std::min<int64_t>(ceil_div(a.rows, groups), 148), groups * warps * 32, a.cols * 16, stream>>>(a, warps);
+    kernel<<<(unsigned)std::min<int64_t>(ceil_div(a.rows, groups), 148), groups * warps * 32, a.cols * held, stream>>>(a, warps);
     return launch_status();
 }
 template <typename T, bool VEC, int GATE> int launch_groups(const NormArgs &a, cudaStream_t stream)

@@ -4,6 +4,8 @@ Tolerances are those of the operators' own tests (``check_norm``, ``product_tole
 """
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
@@ -47,3 +49,23 @@ def test_a_partly_filled_unit_adds_nothing_to_the_second_norm(cols, dtype, kind)
     want = (held - mean) * rstd * gamma.double() + beta.double()
     ref.assert_packed_close(n_too.codes, n_too.scales, want,
                             8 * U * (want.abs() + 2 * (1 + (held * rstd).abs()) * gamma.double().abs()), what + " packed")
+
+
+@pytest.mark.parametrize("cols", [40, 37, 896, 9000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_gate_of_columns_multiplies_the_shifted_norm(cols, dtype):
+    """gate (LN(f) post_gamma + post_beta), of a gate that is infinite, or too large for its product with post_gamma."""
+    f = torch.randn(3, cols, generator=gen(1)).to(dtype)
+    f[1] = 0.0
+    f[1, 0], f[1, 1] = 1.0, -1.0                       # the mean is zero, and so is the norm of the others
+    post, shift, gate = torch.ones(cols), torch.zeros(cols), torch.ones(cols)
+    gate[5], gate[6] = math.inf, -math.inf
+    shift[6], post[7], gate[7], shift[7] = 1000.0, 1e25, 1e25, 2.0
+    on = lambda t: t.to(DEV)  # noqa: E731
+    z, _, stats = inner.residual_norm(torch.zeros_like(on(f)), on(f), None, None, on(post), on(shift), on(gate), norm=False)
+    z, mean = z.cpu().float(), stats[0].cpu()
+    for row in (0, 2):
+        assert float(z[row, 5]) == math.inf * (1 if f[row, 5] > mean[row] else -1)
+    assert bool((z[:, 6] == -math.inf).all())          # the shift is larger than any row's values
+    assert abs(float(z[1, 7]) / 2e25 - 1.0) <= (2.0 ** -8 if dtype == BF16 else 4 * U)
+    assert float(z[1, 8]) == 0.0 and bool(torch.isnan(z[1, 5]))  # an infinite gate times a norm of zero
