@@ -860,6 +860,8 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             store_row<T, VEC, U>(static_cast<T *>(a.dx) + row * a.dx_stride, g, valid, raw);
         }
         read_source<T, VEC, U>(a.f, row, from + 3 * buffer + (VEC ? 0 : f.ahead(row)), g, places, a.cols, h);
+        // d is zero outside the row, but its product with an infinite f is not (through the norm all of that row is NaN)
+        if (GATE == GATE_OF_ROW && !a.post_norm) keep_valid_row<VEC, U>(valid, h);
         f32x2 gate[P], of_gate = 0ull, all[2] = {0ull, 0ull};
         if (GATE == GATE_OF_VALUES) {
             load_row<T, VEC, U>(static_cast<const T *>(a.gate) + row * a.gate_stride, g, valid, raw);

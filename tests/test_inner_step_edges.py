@@ -11,7 +11,7 @@ import torch
 
 from paper_2403_10616_b200 import inner
 from tests import inner_reference as ref
-from tests.test_inner_ops import BF16, DEV, F32, U, gen
+from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, gen
 from tests.test_residual_norm import check_norm
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +69,21 @@ def test_a_gate_of_columns_multiplies_the_shifted_norm(cols, dtype):
     assert bool((z[:, 6] == -math.inf).all())          # the shift is larger than any row's values
     assert abs(float(z[1, 7]) / 2e25 - 1.0) <= (2.0 ** -8 if dtype == BF16 else 4 * U)
     assert float(z[1, 8]) == 0.0 and bool(torch.isnan(z[1, 5]))  # an infinite gate times a norm of zero
+
+
+@pytest.mark.parametrize("cols", [5, 33, 40, 264, 300, 2000, 9000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_an_infinity_at_a_row_s_end_counts_once_in_the_gradient_of_its_gate(cols, dtype):
+    """Without the norm after the block dgate = sum dz f, which is infinite where f is and dz is not zero."""
+    f, dz = torch.randn(4, cols, generator=gen(1)).to(dtype), torch.randn(4, cols, generator=gen(2)).to(dtype)
+    f[1, cols - 1], f[2, 0] = math.inf, -math.inf
+    dz[1, cols - 1], dz[2, 0] = 2.0, 3.0
+    stats = torch.stack([torch.zeros(4), torch.ones(4), torch.zeros(4), torch.ones(4)]).to(DEV)
+    got = inner.residual_norm_backward(None, dz.to(DEV), f.to(DEV), None, stats, gate=torch.ones(4, 1, device=DEV),
+                                       post_norm=False)
+    gate = got.gate.cpu().view(-1)
+    assert float(gate[1]) == math.inf and float(gate[2]) == -math.inf
+    each = dz.double() * f.double()
+    for row in (0, 3):
+        assert abs(float(gate[row]) - float(each[row].sum())) <= CHAIN * float(each[row].abs().sum())
+    assert torch.equal(got.f.cpu(), dz)
