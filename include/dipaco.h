@@ -624,12 +624,12 @@ int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_pac
 /*
  * The norm of several gradients together, sqrt of the sum of all their squares, and the gradients times
  * min(1, max_norm / norm).  Squares are added in fp32 for at most 80 values (in chains of 20) and in fp64 beyond, or in fp64 where
- * fp32 would overflow or lose them.  A norm that is not finite shows: with a NaN all results are NaN, with an infinity
- * they are zero, or NaN where the gradient is infinite.
+ * fp32 would overflow or lose them.  Under a limit a norm that is not finite shows: with a NaN all results are NaN, with
+ * an infinity they are zero, or NaN where the gradient is infinite.
  *   grads        HOST array [count] of device pointers, gradient i being numel[i] contiguous values of dtypes[i]
  *   out          HOST array of device pointers to as many values of out_dtypes[i]; a result is its own gradient's
  *                tensor (in place, of the same type) or overlaps nothing else; NULL = the norm alone
- *   max_norm     >= 0; infinity = no clipping (results are copies)
+ *   max_norm     >= 0; infinity = no clipping: results are copies, whatever the norm
  *   norm         fp32, before clipping; may be NULL
  *   workspace    16-byte aligned, at least the bytes that dipaco_clip_gradients_workspace reports (host only)
  * The arrays are read before the call returns.

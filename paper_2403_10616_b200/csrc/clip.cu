@@ -266,7 +266,7 @@ template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Pie
 }
 __device__ __forceinline__ float factor(double norm, double most)
 {
-    return norm <= most ? 1.0f : (float)(most / norm);  // a NaN makes all results NaN
+    return norm <= most || most == INFINITY ? 1.0f : (float)(most / norm);  // with a limit a NaN makes all results NaN
 }
 
 template <int CAPACITY>

@@ -87,3 +87,21 @@ def test_an_infinity_at_a_row_s_end_counts_once_in_the_gradient_of_its_gate(cols
     for row in (0, 3):
         assert abs(float(gate[row]) - float(each[row].sum())) <= CHAIN * float(each[row].abs().sum())
     assert torch.equal(got.f.cpu(), dz)
+
+
+# ------------------------------------------------------------------ clipping
+
+@pytest.mark.parametrize("sizes", [(100, 4), (300_000, 7, 500_000)])
+def test_without_a_limit_a_nan_stays_where_it_is(sizes):
+    g = [torch.randn(n, generator=gen(i)).to(BF16 if i == 1 else F32) for i, n in enumerate(sizes)]
+    g[0][5], g[1][0] = math.nan, math.inf
+    dev = [t.to(DEV) for t in g]
+    want = torch.cat([t.float() for t in g])
+    for call in (lambda: inner.gather_gradients(dev), lambda: inner.gather_gradients(dev, math.inf)):
+        flat, norm = call()
+        assert math.isnan(float(norm))
+        assert torch.equal(torch.isnan(flat.cpu()).nonzero(), torch.tensor([[5]]))
+        assert torch.equal(flat.cpu().nan_to_num(), want.nan_to_num())
+    assert math.isnan(float(inner.clip_gradients(dev, math.inf)))
+    for t, h in zip(dev, g):
+        assert torch.equal(t.cpu().nan_to_num(), h.nan_to_num())
