@@ -630,8 +630,9 @@ int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_pac
  *   out          HOST array of device pointers to as many values of out_dtypes[i]; a result is its own gradient's
  *                tensor (in place, of the same type) or overlaps nothing else; NULL = the norm alone
  *   max_norm     >= 0; infinity = no clipping: results are copies, whatever the norm
- *   norm         fp32, before clipping; may be NULL
- *   workspace    16-byte aligned, at least the bytes that dipaco_clip_gradients_workspace reports (host only)
+ *   norm         fp32, before clipping; may be NULL, and is then not computed for copies
+ *   workspace    16-byte aligned, at least the bytes that dipaco_clip_gradients_workspace reports (host only); not
+ *                needed for copies without the norm
  * The arrays are read before the call returns.
  */
 int dipaco_clip_gradients_workspace(const int64_t *numel, int32_t count, int64_t *bytes);

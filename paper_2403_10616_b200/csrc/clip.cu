@@ -4,7 +4,8 @@
 // squares for each block, scale_kernel joins them in every block and goes through the chunks again, the last
 // first, as those are the ones still in L2.  Few values take one launch of a cluster of blocks instead, whose sums
 // meet in distributed shared memory (cluster_kernel).  Tensors are listed in the kernels' arguments, so that a call
-// copies nothing and can be captured; longer lists take several launches.
+// copies nothing and can be captured; longer lists take several launches.  Where neither a limit nor the norm is asked
+// for, scale_kernel alone makes the copies.
 //
 // Bound by memory: gradients are read once for the norm and once more to be scaled.  144M in fp32, gathered: 286 us, 1.08
 // of what those bytes take at a copy's rate (the floor without the second reading is 176); 526,080 in two launches 6.7.
@@ -383,11 +384,15 @@ bool results_overlap(const Launches &plan, const void *const *grads, void *const
     return false;
 }
 
+// Neither a limit nor the norm is asked for: results are copies, and no square is added.
+bool are_copies(void *const *out, double most, const float *norm) { return out && most == INFINITY && !norm; }
+
 template <int CAPACITY>
 int launch(const Launches &plan, const void *const *grads, void *const *out, const int64_t *numel,
            const int32_t *dtypes, const int32_t *out_dtypes, double most, float *norm, double *sums, cudaStream_t stream)
 {
     Pieces<CAPACITY> t;
+    const bool copies = are_copies(out, most, norm), one_cluster = plan.one_cluster && !copies;
     const auto fill = [&](int launch) {
         const int first = launch * CAPACITY, last = std::min(first + CAPACITY, (int)plan.tensors.size());
         t.count = last - first;
@@ -396,18 +401,18 @@ int launch(const Launches &plan, const void *const *grads, void *const *out, con
             const int i = plan.tensors[k];
             t.piece[k - first] = {grads[i], out ? out[i] : nullptr, numel[i], t.chunks, dtypes[i] == DIPACO_BF16,
                                   (unsigned char)(out && out_dtypes[i] == DIPACO_BF16)};
-            t.chunks += (unsigned)chunks_of(numel[i], plan.one_cluster ? WARP_CHUNK : CHUNK);
+            t.chunks += (unsigned)chunks_of(numel[i], one_cluster ? WARP_CHUNK : CHUNK);
         }
     };
     if constexpr (CAPACITY == FEW_TENSORS) {
-        if (plan.one_cluster) {
+        if (one_cluster) {
             fill(0);
             cluster_kernel<<<CLUSTER, CLUSTER_THREADS, 0, stream>>>(t, out != nullptr, most, norm);
             return launch_status();
         }
     }
     int count = 0;
-    for (int l = 0; l < plan.launches; ++l) {
+    for (int l = 0; l < (copies ? 0 : plan.launches); ++l) {
         fill(l);
         const int blocks = (int)std::min<int64_t>(t.chunks, MAX_BLOCKS);
         sums_kernel<CAPACITY><<<blocks, THREADS, 0, stream>>>(t, sums + count);
@@ -422,7 +427,7 @@ int launch(const Launches &plan, const void *const *grads, void *const *out, con
         return launch_status();
     }
     for (int l = plan.launches - 1; l >= 0; --l) {
-        if (plan.launches > 1) fill(l);
+        if (plan.launches > 1 || copies) fill(l);
         const int blocks = (int)std::min<int64_t>(t.chunks, MAX_BLOCKS);
         scale_kernel<CAPACITY><<<blocks, THREADS, 0, stream>>>(t, sums, count, most, l == 0 ? norm : nullptr);
     }
@@ -460,7 +465,8 @@ int dipaco_clip_gradients(const void *const *grads, void *const *out, const int6
             if (out && (!is_dense_dtype(out_dtypes[i]) || !out[i] || !vector_ok(out[i], dense_size(out_dtypes[i])))) return DIPACO_EINVAL;
         }
         if (out && results_overlap(p, grads, out, numel, dtypes, out_dtypes)) return DIPACO_EINVAL;
-        if (p.sums > 0 && (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < p.sums * (int64_t)sizeof(double)))
+        if (p.sums > 0 && !are_copies(out, max_norm, norm) &&
+            (!workspace || (uintptr_t)workspace % 16 != 0 || workspace_bytes < p.sums * (int64_t)sizeof(double)))
             return DIPACO_EINVAL;
         DeviceScope scope(device);
         if (!scope.ok) return DIPACO_ECUDA;

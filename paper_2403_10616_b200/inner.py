@@ -543,7 +543,8 @@ def _gradients(grads: Sequence[torch.Tensor], any_order: bool):
     return grads, dev, [t.numel() for t in grads], [t.data_ptr() for t in grads], codes
 
 
-def _clip(like: torch.Tensor, dev, numels, ptrs, codes, out_ptrs, out_codes, max_norm: float) -> torch.Tensor:
+def _clip(like: torch.Tensor, dev, numels, ptrs, codes, out_ptrs, out_codes, max_norm: float,
+          keep: bool = True) -> Optional[torch.Tensor]:
     count = len(numels)
     words, longs = ctypes.c_int32 * count, ctypes.c_int64 * count
     numel, dtypes, grads = longs(*numels), words(*codes), longs(*ptrs)
@@ -551,10 +552,10 @@ def _clip(like: torch.Tensor, dev, numels, ptrs, codes, out_ptrs, out_codes, max
     if out_ptrs is not None:
         out = grads if out_ptrs is ptrs else longs(*out_ptrs)
         out_dtypes = dtypes if out_codes is codes else words(*out_codes)
-    norm = like.new_empty((), dtype=_F32)
-    need = B.dipaco_clip_gradients_workspace(numel, count)
-    work = norm.new_empty(need, dtype=torch.uint8) if need else None
-    B.dipaco_clip_gradients(grads, out, numel, dtypes, out_dtypes, count, max_norm, norm.data_ptr(),
+    norm = like.new_empty((), dtype=_F32) if keep else None
+    need = B.dipaco_clip_gradients_workspace(numel, count) if keep or max_norm < math.inf else 0
+    work = like.new_empty(need, dtype=torch.uint8) if need else None
+    B.dipaco_clip_gradients(grads, out, numel, dtypes, out_dtypes, count, max_norm, norm.data_ptr() if keep else None,
                             work.data_ptr() if need else None, need, dev, _stream(dev))
     return norm
 
@@ -579,10 +580,10 @@ def clip_gradients(grads: Sequence[torch.Tensor], max_norm: float) -> torch.Tens
     return _clip(grads[0], dev, numels, ptrs, codes, ptrs, codes, _most(max_norm))
 
 
-def gather_gradients(grads: Sequence[torch.Tensor], max_norm: Optional[float] = None,
-                     dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor]:
+def gather_gradients(grads: Sequence[torch.Tensor], max_norm: Optional[float] = None, dtype: torch.dtype = torch.float32,
+                     norm: bool = True) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """(flat, norm): the gradients one after another in a vector, as the modules lie in a path's copy, clipped to
-    ``max_norm`` unless it is None, and their norm before that."""
+    ``max_norm`` unless it is None, and their norm before that (None without ``norm``)."""
     if dtype not in _CODES:
         raise ValueError("dtype must be float32 or bfloat16")
     most = math.inf if max_norm is None else _most(max_norm)
@@ -592,7 +593,7 @@ def gather_gradients(grads: Sequence[torch.Tensor], max_norm: Optional[float] = 
     for n in numels:
         out.append(at)
         at += n * size
-    return flat, _clip(flat, dev, numels, ptrs, codes, out, [_CODES[dtype]] * len(out), most)
+    return flat, _clip(flat, dev, numels, ptrs, codes, out, [_CODES[dtype]] * len(out), most, norm)
 
 
 def inner_status(device=None) -> int:

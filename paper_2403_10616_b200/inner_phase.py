@@ -220,7 +220,7 @@ def inner_steps(copy: torch.Tensor, levels: int, width: int, x: torch.Tensor, ta
     for _ in range(steps):
         grads: list = []
         path_loss(copy, levels, width, x, target, grads, kind)
-        flat, _ = inner.gather_gradients([t for g in grads for t in g], clip)
+        flat, _ = inner.gather_gradients([t for g in grads for t in g], clip, norm=False)
         momentum.mul_(beta).add_(flat)
         master.sub_(momentum, alpha=lr)
         copy.copy_(master)

@@ -4,11 +4,13 @@ Tolerances are those of the operators' own tests (``check_norm``, ``product_tole
 """
 from __future__ import annotations
 
+import ctypes
 import math
 
 import pytest
 import torch
 
+from paper_2403_10616_b200 import binding as B
 from paper_2403_10616_b200 import inner
 from tests import inner_reference as ref
 from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, gen
@@ -105,3 +107,36 @@ def test_without_a_limit_a_nan_stays_where_it_is(sizes):
     assert math.isnan(float(inner.clip_gradients(dev, math.inf)))
     for t, h in zip(dev, g):
         assert torch.equal(t.cpu().nan_to_num(), h.nan_to_num())
+
+
+@pytest.mark.parametrize("sizes", [(0, 0), (7,), (100, 4, 0, 9000), (300_000, 7, 500_001), (9, 8200) * 700])
+def test_gathering_without_a_limit_or_the_norm_copies(sizes):
+    g = [torch.randn(n, generator=gen(i)).to(BF16 if i % 2 else F32) for i, n in enumerate(sizes)]
+    for t in g[:1]:
+        t[:1] = math.nan
+    dev = [t.to(DEV) for t in g]
+    for dtype in (F32, BF16):
+        flat, norm = inner.gather_gradients(dev, dtype=dtype, norm=False)
+        want = torch.cat([t.to(dtype) for t in g])
+        assert norm is None and torch.equal(torch.isnan(flat.cpu()), torch.isnan(want))
+        assert torch.equal(flat.cpu().nan_to_num(), want.nan_to_num())
+    dev = [t.nan_to_num() for t in dev]
+    with_norm, norm = inner.gather_gradients(dev, 0.5)
+    without, none = inner.gather_gradients(dev, 0.5, norm=False)
+    assert none is None and torch.equal(with_norm, without)
+
+
+def test_copies_need_no_workspace():
+    t = torch.randn(900_000, generator=gen(1)).to(DEV)
+    out, norm = torch.zeros_like(t), torch.zeros((), device=DEV)
+    longs, ints = ctypes.c_int64 * 1, ctypes.c_int32 * 1
+
+    def call(most, norm_ptr):
+        B.dipaco_clip_gradients(longs(t.data_ptr()), longs(out.data_ptr()), longs(t.numel()), ints(0), ints(0), 1, most,
+                                norm_ptr, None, 0, 0, torch.cuda.current_stream().cuda_stream)
+
+    call(math.inf, None)
+    assert torch.equal(out, t)
+    for most, norm_ptr in ((1.0, None), (math.inf, norm.data_ptr())):
+        with pytest.raises(B.DipacoError):
+            call(most, norm_ptr)
