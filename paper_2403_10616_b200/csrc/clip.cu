@@ -12,6 +12,7 @@
 #include "inner_common.cuh"
 
 #include <algorithm>
+#include <cfloat>
 #include <exception>
 #include <vector>
 
@@ -250,9 +251,31 @@ __device__ __forceinline__ void scale_chunk(const Piece &p, long long begin, lon
 #pragma unroll 1
     for (; i < units.values; i += N) out[i] = narrow1<O>(widen1<T>(in[i]) * by);
 }
-template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, float by, int me)
+// The same with a factor that fp32 holds to fewer bits than its own (gradients near the largest value): in fp64.
+template <typename T, typename O, int N>
+__device__ __noinline__ void scale_exactly(const Piece &p, long long begin, long long end, double by, int me)
 {
+    for (long long i = begin + me; i < end; i += N)
+        static_cast<O *>(p.out)[i] = narrow1<O>((float)((double)widen1<T>(static_cast<const T *>(p.in)[i]) * by));
+}
+template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Piece &p, long long begin, long long end, double factor, int me)
+{
+    const float by = (float)factor;
     if (p.in == p.out && by == 1.0f) return;
+    if (factor > 0.0 && factor < FLT_MIN) {
+        if (p.in_bf16) {
+            if (p.out_bf16)
+                scale_exactly<__nv_bfloat16, __nv_bfloat16, N>(p, begin, end, factor, me);
+            else
+                scale_exactly<__nv_bfloat16, float, N>(p, begin, end, factor, me);
+        } else {
+            if (p.out_bf16)
+                scale_exactly<float, __nv_bfloat16, N>(p, begin, end, factor, me);
+            else
+                scale_exactly<float, float, N>(p, begin, end, factor, me);
+        }
+        return;
+    }
     if (p.in_bf16) {
         if (p.out_bf16)
             scale_chunk<__nv_bfloat16, __nv_bfloat16, N, SIZE>(p, begin, end, by, me);
@@ -265,9 +288,9 @@ template <int N, int SIZE> __device__ __forceinline__ void scale_piece(const Pie
             scale_chunk<float, float, N, SIZE>(p, begin, end, by, me);
     }
 }
-__device__ __forceinline__ float factor(double norm, double most)
+__device__ __forceinline__ double factor(double norm, double most)
 {
-    return norm <= most || most == INFINITY ? 1.0f : (float)(most / norm);  // with a limit a NaN makes all results NaN
+    return norm <= most || most == INFINITY ? 1.0 : most / norm;  // with a limit a NaN makes all results NaN
 }
 
 template <int CAPACITY>
@@ -277,7 +300,7 @@ __global__ void __launch_bounds__(THREADS)
     __shared__ double shared[THREADS / 32];
     const double of_all = sqrt(joined(sums, count, shared));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)of_all;
-    const float by = factor(of_all, most);
+    const double by = factor(of_all, most);
     for (unsigned i = blockIdx.x; i < t.chunks; i += gridDim.x) {
         long long begin, end;
         const Piece &p = find_chunk(t, t.chunks - 1 - i, begin, end);
@@ -315,7 +338,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(CLUSTER_THREAD
     const double of_all = sqrt(sum);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)of_all;
     if (scale) {
-        const float by = factor(of_all, most);
+        const double by = factor(of_all, most);
         for (unsigned c = warp; c < t.chunks; c += CLUSTER_WARPS) {
             long long begin, end;
             const Piece &p = find_chunk<WARP_CHUNK>(t, c, begin, end);

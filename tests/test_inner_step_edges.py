@@ -13,7 +13,7 @@ import torch
 from paper_2403_10616_b200 import binding as B
 from paper_2403_10616_b200 import inner
 from tests import inner_reference as ref
-from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, gen
+from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, assert_within, gen
 from tests.test_residual_norm import check_norm
 
 pytestmark = pytest.mark.gpu
@@ -140,3 +140,20 @@ def test_copies_need_no_workspace():
     for most, norm_ptr in ((1.0, None), (math.inf, norm.data_ptr())):
         with pytest.raises(B.DipacoError):
             call(most, norm_ptr)
+
+
+@pytest.mark.parametrize("n", [1000, 900_000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_factor_that_fp32_hardly_holds(n, dtype):
+    """Gradients near the largest value, clipped to a norm whose share of theirs is subnormal in fp32."""
+    t = (torch.randn(n, generator=gen(1)).clamp(-3, 3) * 1e38).to(dtype)
+    total = float(t.double().square().sum().sqrt())
+    for most in (1.0, 1e-2, 1e-4):
+        want = t.double() * (most / total)
+        off = 26 * U * want.abs() + 2.0 ** -149
+        flat, norm = inner.gather_gradients([t.to(DEV)], most)
+        assert float(norm) == math.inf or abs(float(norm) - total) <= 24 * U * total
+        assert_within(flat, want, off, str(most))
+        own = t.to(DEV)
+        inner.clip_gradients([own], most)
+        assert_within(own, want, off, str(most), dtype)
