@@ -23,11 +23,12 @@ namespace {
 constexpr int CHUNK = 8192, WARP_CHUNK = 2048;  // values, of a block and of a warp
 constexpr int THREADS = 256;
 constexpr int CLUSTER = 8, CLUSTER_THREADS = 512, CLUSTER_WARPS = CLUSTER * CLUSTER_THREADS / 32;
-// One launch instead of two and a workspace saves the host 6 us of a call; eight SMs take longer than all of them: 5.4 us
-// for 64,000 values (two launches 6.6), 7.9 for 256,000 (6.6), 12.2 for 526,080 (6.7).  It pays while they are done
-// before the host has made its next call, which takes it 17 us.  A warp has a chunk to itself: tensors are small, and a
-// block to each chunk took 14 us for 64 of 1000 values, which take 6.6 now.
-constexpr int CLUSTER_VALUES = 600000;
+// One launch instead of two and a workspace, which saves the host 5.5 us of a call, while eight SMs take no longer than all
+// of them.  In a replayed graph, mean of 1, 6 and 60 tensors in fp32 and 6 in bf16: 4.8 us for 1000 values (two launches
+// 4.7), 6.5 for 64,000 (6.1), 6.6 for 96,000 (6.7), 7.4 for 128,000 (6.2), 9.2 for 256,000 (6.6), 13.8 for 526,080 (6.5).
+// A warp has a chunk to itself: tensors are small, and a block to each chunk took 14 us for 64 of 1000 values, which take
+// 6.6 now.
+constexpr int CLUSTER_VALUES = 100000;
 constexpr int FEW_TENSORS = 64, MANY_TENSORS = 640;  // 2 and 20 KB of arguments
 constexpr int MAX_BLOCKS = 148 * 8;
 constexpr int MAX_JOINED = 4096;  // sums that every block of scale_kernel joins by itself

@@ -142,6 +142,20 @@ def test_copies_need_no_workspace():
             call(most, norm_ptr)
 
 
+@pytest.mark.parametrize("sizes", [(99_999,), (100_000,), (100_001,), (60_000, 40_000, 1), (1600,) * 63, (526_080,)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_numbers_of_values_around_which_a_cluster_gives_way(sizes, dtype):
+    g = [torch.randn(n, generator=gen(i)).to(dtype) for i, n in enumerate(sizes)]
+    whole = torch.cat(g).double()
+    total = float(whole.norm())
+    flat, norm = inner.gather_gradients([t.to(DEV) for t in g], 0.25 * total)
+    assert abs(float(norm) - total) <= 24 * U * total
+    assert_within(flat, whole * 0.25, 26 * U * whole.abs() * 0.25, "gathered")
+    # in one launch by one cluster, without a workspace, while that takes no longer than all SMs
+    need = B.dipaco_clip_gradients_workspace((ctypes.c_int64 * len(sizes))(*sizes), len(sizes))
+    assert (need == 0) == (sum(sizes) <= 100_000)
+
+
 @pytest.mark.parametrize("n", [1000, 900_000])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_a_factor_that_fp32_hardly_holds(n, dtype):
