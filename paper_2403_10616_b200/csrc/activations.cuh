@@ -115,37 +115,16 @@ template <int ACTIVATION> __device__ __forceinline__ f32x2 slope(f32x2 a)
 }
 
 // The same with one reciprocal for two values, 1/x = y / (x y): where powers stay under 2^63, and no value is NaN.
-template <int ACTIVATION> __device__ __forceinline__ f32x2 share_in_pairs(f32x2 a, f32x2 square, f32x2 &d)
-{
-    constexpr float c1 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, c3 = c1 * 0.044715f;
-    const float2 e = values_of(ACTIVATION == DIPACO_ACTIVATION_GELU ? mul2(a, fma2(square, pair_of(c3), pair_of(c1)))
-                                                                    : mul2(a, pair_of(-1.4426950408889634f)));
-    d = pair_of(exp2_of(e.x), exp2_of(e.y));
-    const float2 t = values_of(add2(d, pair_of(1.0f)));
-    return mul2(pair_of(t.y, t.x), pair_of(reciprocal_of(t.x * t.y)));
-}
 template <int ACTIVATION> __device__ __forceinline__ f32x2 activate_in_pairs(f32x2 a)
 {
     if constexpr (ACTIVATION == DIPACO_ACTIVATION_GELU || ACTIVATION == DIPACO_ACTIVATION_SILU) {
-        f32x2 d;
-        return mul2(a, share_in_pairs<ACTIVATION>(a, mul2(a, a), d));
+        constexpr float c1 = -2.0f * 0.7978845608028654f * 1.4426950408889634f, c3 = c1 * 0.044715f;
+        const float2 e = values_of(ACTIVATION == DIPACO_ACTIVATION_GELU ? mul2(a, fma2(mul2(a, a), pair_of(c3), pair_of(c1)))
+                                                                        : mul2(a, pair_of(-1.4426950408889634f)));
+        const float2 t = values_of(add2(pair_of(exp2_of(e.x), exp2_of(e.y)), pair_of(1.0f)));
+        return mul2(a, mul2(pair_of(t.y, t.x), pair_of(reciprocal_of(t.x * t.y))));
     } else {
         return activate<ACTIVATION>(a);
-    }
-}
-template <int ACTIVATION> __device__ __forceinline__ f32x2 slope_in_pairs(f32x2 a)
-{
-    if constexpr (ACTIVATION == DIPACO_ACTIVATION_GELU) {
-        constexpr float k1 = 2.0f * 0.7978845608028654f, k3 = 3.0f * 0.044715f * k1;
-        f32x2 d;
-        const f32x2 square = mul2(a, a), s = share_in_pairs<ACTIVATION>(a, square, d);
-        return mul2(s, fma2(mul2(d, s), mul2(a, fma2(square, pair_of(k3), pair_of(k1))), pair_of(1.0f)));
-    } else if constexpr (ACTIVATION == DIPACO_ACTIVATION_SILU) {
-        f32x2 d;
-        const f32x2 s = share_in_pairs<ACTIVATION>(a, a, d);
-        return mul2(s, fma2(mul2(d, s), a, pair_of(1.0f)));
-    } else {
-        return slope<ACTIVATION>(a);
     }
 }
 // Up to which magnitude: -2u log2(e) is 54 at -7.2, -a log2(e) 58 at -40.

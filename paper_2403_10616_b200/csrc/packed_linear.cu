@@ -613,7 +613,7 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
                 if (inside) store_codes(p.first, row, col, left, w);
                 if (t + 1 < walk.own) {
                     tmem_wait(r);
-                    if (b.apart && t + 2 == walk.own) {
+                    if (b.apart && t + 2 == walk.own) {  // a warp has two groups or four
                         fence_before_sync();
                         if (lane == 0) arrive_remote(read_bars[sets & 1]);
                         __syncwarp();
@@ -626,11 +626,6 @@ __device__ __forceinline__ void pack_epilogue(const PackArgs &p, const PairBlock
             encode_tile(std::true_type());
         else
             encode_tile(std::false_type());
-        if (b.apart && walk.own == 1) {  // read at the start
-            fence_before_sync();
-            if (lane == 0) arrive_remote(read_bars[sets & 1]);
-            __syncwarp();
-        }
     }
 }
 
