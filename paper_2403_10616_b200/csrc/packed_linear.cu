@@ -291,7 +291,10 @@ __device__ __forceinline__ void linear_epilogue(const DenseArgs<Linear> &p, cons
         }
         for (int chunk = 0; chunk < chunks; ++chunk, ++sets) {
             walk.down = !(sets & 1);
-            if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
+            if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) {
+                ptx::bulk_wait_all();  // results on their way are read from this block's shared memory
+                return;
+            }
             fence_after_sync();
             const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
             const auto read_over = [&] {
