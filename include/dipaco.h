@@ -570,9 +570,11 @@ int dipaco_gelu_pack_backward(const void *dy, int64_t dy_stride, int32_t dtype, 
 
 /*
  * Product of two packed matrices on the tensor cores, C = op(A) op(B) with fp32 sums, rounded once to
- * dtype.  The tensor cores truncate when they add, 32 products at a time: a sum of one sign loses up to
- * 2^-24 of itself each time.  Sums are joined in fp32 from parts of 2048 values for results in fp32 (which
- * lose 2^-18 at most, under 1e-6 where signs mix) and of 65536 for results in bf16 (2^-13, beside 2^-9 of
+ * dtype.  The tensor cores truncate when they add, 32 products at a time: each product to 2^-25 of the sum
+ * so far, and the sum to 2^-23.  Where products are alike and of one sign that is 2^-24 of the sum each time;
+ * small products beside a large one may be lost whole.  Sums are joined in fp32 from parts of 2048 values for
+ * results in fp32 (which lose 2^-18 of alike products, under 1e-6 where signs mix, and never more than 2^-14 +
+ * 2^-17 of the magnitudes) and of 65536 for results in bf16 (2^-13, under 2^-9 + 2^-12 always, beside 2^-9 of
  * rounding).  op transposes its argument where the flag is nonzero.  For a layer y = x W^T with x
  * [tokens, in] and W [out, in]:
  *   forward          y  = x  W^T    transpose_b
@@ -601,7 +603,9 @@ int dipaco_packed_matmul(const dipaco_packed *a, const dipaco_packed *b, int32_t
  *                         workspace: of its query for m = tokens, n = in, k = out; only needed for dbias
  * Activations: relu(a) = max(a, 0); silu(a) = a / (1 + exp(-a)); gelu as above.  An infinity of a is NaN once it is
  * packed, and makes silu and gelu NaN or infinite; NaN stays NaN.  relu'(0) = 0.
- * The packed forms take their sums in one go: contractions over 65536 are refused (DIPACO_ELIMIT).
+ * The packed forms refuse contractions over 65536 (DIPACO_ELIMIT).  linear_pack takes its sums in one go, as results
+ * in bf16 do; linear_pack_backward those over up to 8192 values (2^-16 of alike products of one sign, which dbias then
+ * has lost too), and longer ones in parts of 2048, as results in fp32.
  */
 enum {
     DIPACO_ACTIVATION_NONE = 0,

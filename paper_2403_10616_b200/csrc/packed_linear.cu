@@ -703,7 +703,47 @@ struct BackShared {
 };
 static_assert(sizeof(BackShared) <= PAIR_EPILOGUE_WARPS * PAIR_STAGING * PAIR_STAGING_BYTES, "in the place of the buffers");
 
-template <int ACTIVATION>
+// Steps whose sums are taken in one go.  dbias is a result in fp32, whose sums would otherwise lose 1.3e-4 of themselves
+// over 65536 values of one sign (1.2e-6 in parts; over 8192 in one go 8e-6).  Parts cost the wide tiles: 16384x2048x8192
+// takes 197 us in one go and 289 in parts of 2048.  da goes with dbias and does not depend on whether that is wanted.
+constexpr int BACK_STEPS = 64;
+
+// The sums of a tile that are taken out of the products' sets a chunk at a time: added up in columns of tensor memory that
+// the sets leave free, each by the warp that reads it.  Counts the sets; false if a wait ran out.
+__device__ __forceinline__ bool add_chunks(const PackArgs &p, const PairBlock &b, const TileWalk &walk, const uint32_t *read_bars,
+                                           uint32_t totals, int &sets)
+{
+    const uint32_t rows = (uint32_t)(b.warp & 3) * 32 << 16;
+    for (int first = 0; first < p.steps; first += p.chunk, ++sets) {
+        if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return false;
+        fence_after_sync();
+        const uint32_t from = b.tmem + rows + ((sets & 1) ? b.second_set : 0);
+#pragma unroll 1
+        for (int s = 0; s < walk.own; ++s) {
+            uint32_t r[32], before[32];
+            f32x2 v[16];
+            tmem_load32(from + walk.column(s), r);
+            tmem_wait(r);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+            if (first > 0) {
+                tmem_load32(totals + walk.column(s), before);
+                tmem_wait(before);
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    v[j] = add2(pair_of(__uint_as_float(before[2 * j]), __uint_as_float(before[2 * j + 1])), v[j]);
+            }
+            tmem_store32(totals + walk.column(s), v);
+        }
+        tmem_stored();
+        fence_before_sync();
+        if (b.lane == 0) arrive_remote(read_bars[sets & 1]);
+        __syncwarp();
+    }
+    return true;
+}
+
+template <int ACTIVATION, bool CHUNKED>
 __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock &b, PackShared &shared)
 {
     BackShared &of_tiles = *reinterpret_cast<BackShared *>(b.aligned + PAIR_STAGING_AT);
@@ -739,7 +779,7 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
         of_tiles.slopes[set][0][code] = s.x;
         of_tiles.slopes[set][1][code] = s.y;
     };
-    int tile_m, tile_n, sets = 0;
+    int tile_m, tile_n, turn = 0, sets = 0;  // tiles, and sets of sums, so far
     PairWalk::place(p, b.pair, tile_m, tile_n);
     uint4 codes[2];
     float scales[2];
@@ -749,13 +789,20 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
     load_scales(tile_m, tile_n, scales);
     if (SLOPES) put_slopes(0, scales);
     if (!exchange.meet(0, most)) return;
-    for (int tile = b.pair; tile < p.whole_tiles; tile += p.pairs, ++sets) {  // as PairWalk takes them
+    for (int tile = b.pair; tile < p.whole_tiles; tile += p.pairs, ++turn) {  // as PairWalk takes them
         const int n0 = tile_n * p.tile_n, row0 = tile_m * PAIR_ROWS + (int)b.rank * 128;
         const int row = row0 + quarter * 32 + lane;
-        if (!warp_wait(&b.sums_full[sets & 1], (sets >> 1) & 1, 4)) return;
-        fence_after_sync();
-        const uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16) + ((sets & 1) ? b.second_set : 0);
-        walk.down = !(sets & 1);
+        uint32_t from = b.tmem + ((uint32_t)(quarter * 32) << 16);
+        const int set = turn & 1;  // of sums, unless they are chunks'
+        if constexpr (CHUNKED) {
+            from += p.tile_n;
+            if (!add_chunks(p, b, walk, read_bars, from, sets)) return;
+        } else {
+            if (!warp_wait(&b.sums_full[set], (turn >> 1) & 1, 4)) return;
+            fence_after_sync();
+            from += set ? b.second_set : 0;
+        }
+        walk.down = !(turn & 1);
         const bool more = tile + p.pairs < p.whole_tiles;
         if (more) {
             PairWalk::place(p, tile + p.pairs, tile_m, tile_n);
@@ -781,7 +828,7 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
             for (int j = 0; j < 16; ++j) v[j] = pair_of(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
             if (t + 1 < walk.own) tmem_load32(from + walk.column(walk.slot(t + 1)), r);
             if constexpr (SLOPES) {
-                const float *slopes = of_tiles.slopes[sets & 1][walk.block(t)];
+                const float *slopes = of_tiles.slopes[turn & 1][walk.block(t)];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const unsigned w = words[j / 2] >> 16 * (j & 1);
@@ -797,12 +844,12 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
             if (t > 0 || p.row_sums) tmem_store32(from + walk.column(slot), v);
             if (p.row_sums) {
                 tmem_stored();
-                of_tiles.sums[sets & 1][walk.group(t)][quarter][column_of_sum(lane)] = column_sums(from + walk.column(slot), lane);
+                of_tiles.sums[turn & 1][walk.group(t)][quarter][column_of_sum(lane)] = column_sums(from + walk.column(slot), lane);
             }
             if (t == 0) {
-                if (!b.apart) {
+                if (!CHUNKED && !b.apart) {
                     fence_before_sync();
-                    if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                    if (lane == 0) arrive_remote(read_bars[set]);
                     __syncwarp();
                 }
 #pragma unroll
@@ -814,10 +861,10 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
             }
         }
         tmem_stored();
-        if (SLOPES && more) put_slopes(~sets & 1, scales);
+        if (SLOPES && more) put_slopes(~turn & 1, scales);
         if (!exchange.meet(blocks, most)) return;
         if (p.row_sums && b.warp < p.tile_n / 32 && row0 < p.m && n0 + b.warp * 32 + lane < p.n) {
-            const float(*s)[32] = of_tiles.sums[sets & 1][b.warp];
+            const float(*s)[32] = of_tiles.sums[turn & 1][b.warp];
             p.row_sums[(long long)(row0 / 128) * p.n + n0 + b.warp * 32 + lane] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
         }
         // the results of the t-th group
@@ -855,9 +902,9 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
             for (int t = 0; t < walk.own; ++t) {
                 const int slot = walk.slot(t), col = n0 + walk.column(slot), left = p.n - col;
                 results(t);
-                if (b.apart && t + 1 == walk.own) {
+                if (!CHUNKED && b.apart && t + 1 == walk.own) {
                     fence_before_sync();
-                    if (lane == 0) arrive_remote(read_bars[sets & 1]);
+                    if (lane == 0) arrive_remote(read_bars[set]);
                     __syncwarp();
                 }
                 if (left <= 0) continue;
@@ -873,7 +920,7 @@ __device__ __forceinline__ void back_epilogue(const PackArgs &p, const PairBlock
     }
 }
 
-template <int ACTIVATION, bool BACK>
+template <int ACTIVATION, bool BACK, bool CHUNKED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGUE_WARPS), 1)
     packed_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                        const __grid_constant__ PackArgs p)
@@ -881,9 +928,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(EPILOGU
     __shared__ PackShared shared;
     __shared__ __align__(16) float columns[EPILOGUE_WARPS][GROUPS][32];  // biases of the warps' columns
     if (threadIdx.x == 64) ptx::mbar_init(&shared.exchanged, EPILOGUE_WARPS);  // seen after run_pair's first barrier
-    run_pair<false, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) {
+    run_pair<CHUNKED, EPILOGUE_WARPS>(a_map, b_map, p, [&](const PairBlock &b) {
         if constexpr (BACK)
-            back_epilogue<ACTIVATION>(p, b, shared);
+            back_epilogue<ACTIVATION, CHUNKED>(p, b, shared);
         else
             pack_epilogue<ACTIVATION>(p, b, shared, columns);
     });
@@ -1010,11 +1057,13 @@ PackedCodes packed_codes(const dipaco_packed *p)
 }
 
 // Tiles of whole blocks: 256 columns, or 128 where that takes less time by the estimate of plan_pairs (and some clocks
-// for a column's epilogue that the next products wait for).
-void plan_blocks(PackArgs &p)
+// for a column's epilogue that the next products wait for).  Sums taken in chunks are added up in the columns of tensor
+// memory that tiles of 128 leave free.
+void plan_blocks(PackArgs &p, bool chunked)
 {
     double best = 0.0;
     for (const int tile_n : {256, 128}) {
+        if (chunked && tile_n > 128) continue;
         const int64_t tiles = ceil_div(p.m, PAIR_ROWS) * ceil_div(p.n, tile_n);
         const double time = (double)ceil_div(tiles, PAIRS) * (p.steps * std::max(2.0 * tile_n, 64.0 * 4 + tile_n) + 12.0 * tile_n);
         if (best != 0.0 && time >= best) continue;
@@ -1025,15 +1074,16 @@ void plan_blocks(PackArgs &p)
         p.pairs = (int)std::min<int64_t>(PAIRS, tiles);
         p.whole_tiles = (int)tiles;
     }
-    p.chunk = CHUNK_BF16;
+    p.chunk = chunked ? CHUNK_F32 : CHUNK_BF16;
 }
 
-template <bool BACK> int launch_packed(const CUtensorMap &a_map, const CUtensorMap &b_map, const PackArgs &p, int activation, cudaStream_t stream)
+template <bool BACK, bool CHUNKED>
+int launch_packed(const CUtensorMap &a_map, const CUtensorMap &b_map, const PackArgs &p, int activation, cudaStream_t stream)
 {
-    const auto kernel = activation == DIPACO_ACTIVATION_RELU   ? packed_pair_kernel<DIPACO_ACTIVATION_RELU, BACK>
-                        : activation == DIPACO_ACTIVATION_SILU ? packed_pair_kernel<DIPACO_ACTIVATION_SILU, BACK>
-                        : activation == DIPACO_ACTIVATION_GELU ? packed_pair_kernel<DIPACO_ACTIVATION_GELU, BACK>
-                                                               : packed_pair_kernel<DIPACO_ACTIVATION_NONE, BACK>;
+    const auto kernel = activation == DIPACO_ACTIVATION_RELU   ? packed_pair_kernel<DIPACO_ACTIVATION_RELU, BACK, CHUNKED>
+                        : activation == DIPACO_ACTIVATION_SILU ? packed_pair_kernel<DIPACO_ACTIVATION_SILU, BACK, CHUNKED>
+                        : activation == DIPACO_ACTIVATION_GELU ? packed_pair_kernel<DIPACO_ACTIVATION_GELU, BACK, CHUNKED>
+                                                               : packed_pair_kernel<DIPACO_ACTIVATION_NONE, BACK, CHUNKED>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PAIR_SMEM) != cudaSuccess) return launch_status();
     kernel<<<2 * p.pairs, pair_threads(EPILOGUE_WARPS), PAIR_SMEM, stream>>>(a_map, b_map, p);
     return launch_status();
@@ -1156,14 +1206,14 @@ int dipaco_packed_linear_pack(const dipaco_packed *x, const dipaco_packed *w, co
     }
     PackArgs p = {};
     set_operands(p, x, w, false, true);
-    plan_blocks(p);
+    plan_blocks(p, false);
     p.first = packed_codes(y);
     p.second = packed_codes(a);
     p.bias = bias;
     p.bias_bf16 = bias_dtype == DIPACO_BF16;
     CUtensorMap a_map, b_map;
     if (!operand_map(&a_map, x, 128) || !operand_map(&b_map, w, p.tile_n / 2)) return DIPACO_ECUDA;
-    return launch_packed<false>(a_map, b_map, p, activation, stream);
+    return launch_packed<false, false>(a_map, b_map, p, activation, stream);
 }
 
 int dipaco_packed_linear_pack_backward_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes)
@@ -1202,7 +1252,8 @@ int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_pac
     }
     PackArgs p = {};
     set_operands(p, dy, w, false, false);
-    plan_blocks(p);
+    const bool chunked = p.steps > BACK_STEPS;
+    plan_blocks(p, chunked);
     p.first = packed_codes(da);
     p.a_codes = slopes ? static_cast<const uint8_t *>(a->codes) : nullptr;
     p.of_a_scales = slopes ? static_cast<const uint8_t *>(a->scales) : nullptr;
@@ -1210,7 +1261,9 @@ int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_pac
     p.row_sums = dbias ? static_cast<float *>(workspace) : nullptr;
     CUtensorMap a_map, b_map;
     if (!operand_map(&a_map, dy, 128) || !operand_map(&b_map, w, 128)) return DIPACO_ECUDA;
-    if (const int rc = launch_packed<true>(a_map, b_map, p, activation, stream)) return rc;
+    if (const int rc = chunked ? launch_packed<true, true>(a_map, b_map, p, activation, stream)
+                               : launch_packed<true, false>(a_map, b_map, p, activation, stream))
+        return rc;
     if (dbias)
         row_sums_kernel<<<(unsigned)ceil_div(n, 32), 32 * SLICES, 0, stream>>>(p.row_sums, (int)ceil_div(m, PACK_BLOCK), p.n, dbias);
     return launch_status();

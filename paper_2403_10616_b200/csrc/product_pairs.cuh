@@ -186,11 +186,12 @@ constexpr int SCALE_BYTES = 512;          // of shared memory for four columns: 
 // words are copied to tensor memory once for four steps.  Copies take the tensor cores' time: one for
 // each step cost 20 % (8192^3: 555 us, 445 without any copy).
 constexpr int QUAD = 4;
-// The tensor cores truncate when they add to an fp32 sum.  Every 32 contracted values lose up to 2^-24 of it
-// if all products have one sign, and less where signs mix (2.4e-5 over 65501).  Sums that are returned in fp32 are
-// therefore taken out of tensor memory every 16 steps, 2048 values, and added up in registers: under 1e-6.  A result
-// in bf16 has 2^-9 of rounding of its own: its sums are taken out every 512 steps, 65536 values, which lose less than
-// 2^-13.  (In one sum 2^21 positive products were off by a unit everywhere, 0.8 %.  Every 16 steps cost a product in
+// The tensor cores truncate when they add 32 products to an fp32 sum: each of them to a quarter of the sum's last place
+// (2^-25 of it) and the new sum to its own (2^-23).  Products that are alike lose 2^-24 of the sum so far, 2.4e-5 over
+// 65501 of them; small ones beside a large one are lost whole, 3.7e-5 of a sum of 2048 built for it, and 2^-14 + 2^-17
+// at most.  Sums that are returned in fp32 are therefore taken out of tensor memory every 16 steps, 2048 values, and added
+// up in registers: under 2^-18 where products are alike, under 1e-6 where signs mix.  A result in bf16 has 2^-9 of
+// rounding of its own: its sums are taken out every 512 steps, 65536 values, 2^-13 where products are alike.  (In one sum 2^21 positive products were off by a unit everywhere, 0.8 %.  Every 16 steps cost a product in
 // bf16 up to 8 %: 8192x2048x131072 1570 -> 1700 us.)
 constexpr int CHUNK_F32 = 16, CHUNK_BF16 = 512;  // powers of two
 

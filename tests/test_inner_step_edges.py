@@ -171,3 +171,31 @@ def test_a_factor_that_fp32_hardly_holds(n, dtype):
         own = t.to(DEV)
         inner.clip_gradients([own], most)
         assert_within(own, want, off, str(most), dtype)
+
+
+# ------------------------------------------------------------------ linear layers
+
+@pytest.mark.parametrize("name", [None, "relu", "gelu"])
+@pytest.mark.parametrize("m,n,k", [(100, 130, 8200), (300, 520, 8192), (70, 40, 65536), (300, 300, 65500), (9000, 1300, 10300)])
+def test_bias_gradients_over_long_sums_of_one_sign(m, n, k, name):
+    """Sums over up to 8192 values are taken in one go, longer ones in parts of 2048.  Of a part the tensor cores lose at most
+    2^-25 for each product and 2^-23 for every 32 of them; joining parts, u for each; the tokens' sums, under 100 additions
+    one after another."""
+    def positive(seed, rows, cols):
+        x = torch.exp(1.5 * torch.randn(rows, cols, generator=gen(seed))).to(DEV)  # sums with bits to lose
+        p = inner.pack(x)
+        return p, p.codes.double() * ref.spread(p.scales.double(), rows, cols)
+
+    dy, dyv = positive(1, m, k)
+    w, wv = positive(2, k, n)
+    a = inner.pack(torch.full((m, n), 30.0, device=DEV))  # slopes of one
+    da, dbias = inner.packed_linear_pack_backward(dy, w, None if name is None else a, name)
+    part, each = k if k <= 8192 else 2048, dyv @ wv
+    lost = part * 2.0 ** -25 + part / 32 * 2.0 ** -23 + k / 2048 * U
+    want = each.sum(0)
+    off = ((dbias.double() - want) / want).abs()
+    assert float(off.max()) <= lost + CHAIN, float(off.max())
+    ref.assert_packed_close(da.codes, da.scales, each.cpu(), (lost + 2 * U) * each.cpu())
+    again, _ = inner.packed_linear_pack_backward(dy, w, None if name is None else a, name, bias=False)
+    assert torch.equal(again.codes.view(torch.uint8), da.codes.view(torch.uint8))
+    assert inner.inner_status() == B.DIPACO_OK
