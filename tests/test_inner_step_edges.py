@@ -13,8 +13,9 @@ import torch
 from paper_2403_10616_b200 import binding as B
 from paper_2403_10616_b200 import inner
 from tests import inner_reference as ref
-from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, assert_within, gen
-from tests.test_residual_norm import check_norm
+from tests.test_inner_ops import BF16, CHAIN, DEV, F32, U, assert_within, gen, packed_operand, place, product_tolerance
+from tests.test_packed_linear import act
+from tests.test_residual_norm import NAMES, backward, check_norm, forward, inputs, or_one, or_zero, statistics
 
 pytestmark = pytest.mark.gpu
 
@@ -89,6 +90,41 @@ def test_an_infinity_at_a_row_s_end_counts_once_in_the_gradient_of_its_gate(cols
     for row in (0, 3):
         assert abs(float(gate[row]) - float(each[row].sum())) <= CHAIN * float(each[row].abs().sum())
     assert torch.equal(got.f.cpu(), dz)
+
+
+MATRICES = ("x", "f", "dn", "dz", "gate", "z")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 128), (6, 896), (4, 2048), (3, 8192), (3, 8200)])
+def test_matrices_of_one_call_at_different_alignments(rows, cols, dtype):
+    """One matrix at a time off the 16-byte boundaries that the others keep to: the results are those of the formula."""
+    host, dev = inputs(rows, cols, dtype, F32, "full")
+    ps, scale, eps = {k: dev[k] for k in NAMES}, 0.8, 1e-5
+    p = {k: host[k] for k in NAMES}
+    base = inner.residual_norm(dev["x"], dev["f"], **ps, gate=dev["gate"], residual_scale=scale)
+    held = base[0].cpu()
+    for odd in MATRICES:
+        at = {k: place(host[k] if k != "z" else held, 3, 1) if k == odd else (dev[k] if k != "z" else base[0]) for k in MATRICES}
+        z, n, stats = inner.residual_norm(at["x"], at["f"], **ps, gate=at["gate"], residual_scale=scale)
+        st, zv = stats.cpu(), z.cpu().double()
+        check_norm(None, st[0], st[1], host["f"].double(), None, None, eps, dtype, odd + " f")
+        check_norm(n, st[2], st[3], zv, p["gamma"], p["beta"], eps, dtype, odd + " n")
+        want, _ = forward(host["x"].double(), host["f"].double(), p, host["gate"].double(), scale, eps, True, False)
+        mean, rstd = statistics(host["f"].double(), eps)
+        hat, top = (host["f"].double() - mean) * rstd, host["f"].double().abs().amax(1, keepdim=True)
+        post, shift = or_one(p["post_gamma"], hat), or_zero(p["post_beta"], hat)
+        off = rstd * 6 * U * top + (CHAIN + 8 * U * top * rstd) * (1 + hat.abs())
+        tol = 4 * U * ((scale * host["x"].double()).abs() + (want - scale * host["x"].double()).abs())
+        tol = tol + host["gate"].double() * (off * post.abs() + 4 * U * ((hat * post).abs() + shift.abs()))
+        assert_within(z, want, tol, odd + " z", dtype)
+        stats = base[2]
+        got = inner.residual_norm_backward(at["dn"], at["dz"], at["f"], at["z"], stats, dev["gamma"], dev["post_gamma"],
+                                           dev["post_beta"], at["gate"], scale)
+        wanted = backward(host["dn"], host["dz"], host["f"].double(), held.double(), stats.cpu(), p, host["gate"], scale, True)
+        for name in got._fields:
+            v, tol = wanted[name]
+            assert_within(getattr(got, name), v, tol, odd + " d" + name, getattr(got, name).dtype)
 
 
 # ------------------------------------------------------------------ clipping
@@ -174,6 +210,32 @@ def test_a_factor_that_fp32_hardly_holds(n, dtype):
 
 
 # ------------------------------------------------------------------ linear layers
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+@pytest.mark.parametrize("shift", [-0.5, -2.0, -3.0, -5.0, -12.0, -30.0])
+@pytest.mark.parametrize("m", [3, 300])
+def test_tails_of_the_activations(name, shift, m):
+    """y = a s with s = 1 / (1 + 2^e): e is off by 4 u of itself, and with it 2^e by 4 u |e| ln 2 of itself; the power, the
+    sum, the reciprocal and the product by 8 u more.  What a is off counts by the slope there, which is at most
+    |y| (1 + k) for the exponent's slope k.  Powers over 2^126 leave nothing."""
+    n = 200
+    x, xv = packed_operand(1, m, 100, 0.02)
+    w, wv = packed_operand(2, n, 100, 0.02)
+    bias = torch.randn(n, generator=gen(3)) * 0.01 + shift
+    a = xv @ wv.t() + bias.double()
+    tol_a = product_tolerance(xv, wv.t(), 100) + 2 * U * (a.abs() + bias.double().abs())
+    if name == "gelu":
+        e, k = 2 * ref.ROOT * (a + ref.CUBIC * a ** 3), 2 * ref.ROOT * (1 + 3 * ref.CUBIC * a ** 2)
+    else:
+        e, k = a, torch.ones_like(a)
+    y = act(a, name).float().double()  # packed from its fp32 value, which may be nothing
+    over = y.abs() * (4 * U * e.abs() + 8 * U) + (y.abs() * (1 / a.abs() + 1.01 * k)) * tol_a + 40 * 2.0 ** -126
+    got, kept = inner.packed_linear_pack(x, w, bias.to(DEV), name)
+    ref.assert_packed_close(got.codes, got.scales, y, over, (name, shift))
+    ref.assert_packed_close(kept.codes, kept.scales, a, tol_a, (name, shift, "a"))
+    dense = inner.packed_linear(x, w, bias.to(DEV), name, out_dtype=F32)
+    assert_within(dense, y, over, (name, shift, "dense"))
+
 
 @pytest.mark.parametrize("name", [None, "relu", "gelu"])
 @pytest.mark.parametrize("m,n,k", [(100, 130, 8200), (300, 520, 8192), (70, 40, 65536), (300, 300, 65500), (9000, 1300, 10300)])
