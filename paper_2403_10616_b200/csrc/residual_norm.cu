@@ -257,14 +257,16 @@ __device__ __forceinline__ void load_row(const void *row, const Group &g, unsign
         }
     }
 }
-// A row of a gate of values that the next pass loads, into L2 (16384x2048 in bf16 76 us without it, 70 with it, the
-// gradient 131 and 123; 4999x2047 in fp32 56 and 57, 82 and 78).  Whole units of fp32 lose by it (8192x2048 64 and 65,
-// 109 and 113).
+// A row of a gate of values that the next pass loads, into L2.  Without and with it, us:
+//   forward    bf16 gains (16384x2048 76 and 70, 32768x896 66 and 60, 2048x8191 107 and 95), fp32 loses (8192x2048 65.5 and
+//              66.5, 4999x2047 57 and 60, 3001x5555 115 and 123)
+//   gradient   up to 6144 columns bf16 gains (133 and 121, 128 and 118, 4000x6144 116 and 104), and fp32 value by value in
+//              most (82 and 78, 175 and 158; 20000x333 67.6 and 69); whole units of fp32 lose (107.5 and 114.5), and more
+//              columns in either type (4096x8192 bf16 236 and 256, 2048x8191 fp32 226 and 250)
 template <typename T, bool VEC, int U>
 __device__ __forceinline__ void prefetch_row(const void *row, const Group &g, unsigned valid)
 {
     constexpr int EACH = VEC ? Unit<T>::UE : 1;  // values of a load
-    if (VEC && sizeof(T) == 4) return;
     if (g.lane % (128 / EACH / (int)sizeof(T)) != 0) return;  // a lane for each 128 bytes
 #pragma unroll
     for (int j = 0; j < 8 * U; j += EACH)
@@ -512,7 +514,7 @@ __global__ void __launch_bounds__(512, 1) group_rows_kernel(const __grid_constan
             x_row += x_step;
             load_row<T, VEC, U>(f_row, g, valid, next_f);
             load_row<T, VEC, U>(x_row, g, valid, next_x);
-            if (GATE == GATE_OF_VALUES) prefetch_row<T, VEC, U>(static_cast<const T *>(a.gate) + (row + row_step) * a.gate_stride, g, valid);
+            if (GATE == GATE_OF_VALUES && sizeof(T) == 2) prefetch_row<T, VEC, U>(static_cast<const T *>(a.gate) + (row + row_step) * a.gate_stride, g, valid);
         }
         float2 of_f = make_float2(0.0f, 1.0f), of_z = make_float2(0.0f, 1.0f);
         if (a.post_norm) of_f = group_statistics<VEC, U>(g, v, valid, a.eps);
@@ -814,7 +816,8 @@ __global__ void __launch_bounds__(THREADS, 1) group_back_kernel(const __grid_con
             rstd_z = a.saved[3ll * a.rows + row];
         }
         const float of_row = GATE == GATE_OF_ROW ? load_param(a.gate, a.gate_bf16, row) : 1.0f;
-        if (GATE == GATE_OF_VALUES && row < a.rows - row_step)
+        constexpr bool wide = U == 2 && THREADS == 512;  // over 6144 columns
+        if (GATE == GATE_OF_VALUES && !wide && (sizeof(T) == 2 || !VEC) && row < a.rows - row_step)
             prefetch_row<T, VEC, U>(static_cast<const T *>(a.gate) + (row + row_step) * a.gate_stride, g, valid);
         if (ok) ok = __all_sync(0xffffffffu, bounded_wait(&arrived[stage], phase, &g_residual_norm_error, 1));  // one answer for a warp
         f32x2 d[P], h[P];
