@@ -540,7 +540,8 @@ int dipaco_residual_norm(const dipaco_residual_norm_args *args, const void *x, i
  *   d = dz + rstd_z (u - mean(u) - h_z mean(u h_z)),  u = dn gamma;   dx = residual_scale d
  *   df = rstd_f (q - mean(q) - h_f mean(q h_f)),  q = d gate post_gamma   (q itself without post_norm)
  *   dgate = d p, summed over what shares a gate;  dpost_gamma = sum d gate h_f,  dpost_beta = sum d gate,
- *   dgamma = sum dn h_z,  dbeta = sum dn, over rows
+ *   dgamma = sum dn h_z,  dbeta = sum dn, over rows (a gate of columns is multiplied with post_gamma, and with the
+ *   sums, so that q and the sums overflow where those products do)
  *   f or f_packed, z or z_packed   exactly one of each: the forward call's, or 8-bit checkpoints of them (z with norm
  *                  only)
  *   dx, df         of dtype; NULL where not wanted, as the following
@@ -627,9 +628,9 @@ int dipaco_packed_linear_pack_backward(const dipaco_packed *dy, const dipaco_pac
 
 /*
  * The norm of several gradients together, sqrt of the sum of all their squares, and the gradients times
- * min(1, max_norm / norm).  Squares are added in fp32 for at most 80 values (in chains of 20) and in fp64 beyond, or in fp64 where
- * fp32 would overflow or lose them.  Under a limit a norm that is not finite shows: with a NaN all results are NaN, with
- * an infinity they are zero, or NaN where the gradient is infinite.
+ * min(1, max_norm / norm).  Squares are added in fp32 for at most 80 values (in chains of 20) and in fp64 beyond, or
+ * in fp64 where fp32 would overflow or lose them.  Under a limit a norm that is not finite shows: with a NaN all
+ * results are NaN, with an infinity they are zero, or NaN where the gradient is infinite.
  *   grads        HOST array [count] of device pointers, gradient i being numel[i] contiguous values of dtypes[i]
  *   out          HOST array of device pointers to as many values of out_dtypes[i]; a result is its own gradient's
  *                tensor (in place, of the same type) or overlaps nothing else; NULL = the norm alone
@@ -654,8 +655,9 @@ int dipaco_inner_status(int32_t device, void *cuda_stream);
 
 /*
  * Diagnostic: make a bounded wait of the norms (operators = 0; of the plain ones, then of those around a block), of
- * the packing kernels (1) or of the products and then the linear layers (2) run out on purpose, harmlessly: one warp waits at most limit_ns (1 .. 1e9) on a barrier that
- * nothing will complete; no copy is in flight and no buffer of the caller is involved.
+ * the packing kernels (1) or of the products and then the linear layers (2) run out on purpose, harmlessly: one warp
+ * waits at most limit_ns (1 .. 1e9) on a barrier that nothing will complete; no copy is in flight and no buffer of the
+ * caller is involved.
  */
 int dipaco_selftest_inner_wait_expiry(int32_t operators, int64_t limit_ns, int32_t device, void *cuda_stream);
 

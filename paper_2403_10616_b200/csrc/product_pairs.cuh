@@ -191,8 +191,9 @@ constexpr int QUAD = 4;
 // 65501 of them; small ones beside a large one are lost whole, 3.7e-5 of a sum of 2048 built for it, and 2^-14 + 2^-17
 // at most.  Sums that are returned in fp32 are therefore taken out of tensor memory every 16 steps, 2048 values, and added
 // up in registers: under 2^-18 where products are alike, under 1e-6 where signs mix.  A result in bf16 has 2^-9 of
-// rounding of its own: its sums are taken out every 512 steps, 65536 values, 2^-13 where products are alike.  (In one sum 2^21 positive products were off by a unit everywhere, 0.8 %.  Every 16 steps cost a product in
-// bf16 up to 8 %: 8192x2048x131072 1570 -> 1700 us.)
+// rounding of its own: its sums are taken out every 512 steps, 65536 values, 2^-13 where products are alike.  (In one
+// sum 2^21 positive products were off by a unit everywhere, 0.8 %.  Every 16 steps cost a product in bf16 up to 8 %:
+// 8192x2048x131072 1570 -> 1700 us.)
 constexpr int CHUNK_F32 = 16, CHUNK_BF16 = 512;  // powers of two
 
 struct ProductArgs {

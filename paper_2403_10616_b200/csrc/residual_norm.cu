@@ -14,11 +14,11 @@
 //   group_back_kernel every gradient in one pass, a row in the registers of a group: up to 8192 columns
 //   back_rows_kernel  as rows_kernel for dx, df and the two means that d needs; back_columns_kernel the sums over rows
 //
-// Measured: 16384x2048 in bf16 51 us (5.2 TB/s) and its gradient 100 (4.0 TB/s), 32768x896 47 and 98, with n and z
-// packed 62 (the packing kernel reads z from L2), 4999x2047 in fp32 42 and 66, 4096x8192 in bf16 69 and 171; a single row
-// of 896 4.4 and 10.
+// Measured: 16384x2048 in bf16 54 us (5.0 TB/s) and its gradient 97 (4.1 TB/s), 32768x896 49 and 98, with n and z
+// packed 64 (the packing kernel reads z from L2) and from such checkpoints 108, 4999x2047 in fp32 45 and 66, 4096x8192 in
+// bf16 77 and 171 (gates of columns); a single row of 896 4.5 and 10.
 // Two reads and two writes would take 41 us of the first, four and two 61 of its gradient.  The forward kernel is bound by
-// chains (each row's two sums, one after the other, in 16 warps; issue slots 57 % used), the gradient too: its sums over
+// chains (each row's two sums, one after the other, in 16 warps; issue slots 54 % used), the gradient too: its sums over
 // rows take half of the registers, which leaves 12 warps (issue slots 46 %).
 #include "inner_common.cuh"
 

@@ -2,8 +2,9 @@
 
 Layer norm with its gradient, matrices packed in 8 bits (activation checkpoints and the operands of
 the products), the GELU that writes and reads such checkpoints, the product of packed matrices on the
-tensor cores, linear layers with bias, activation and residual, the norms around a block with its gate and residual, and the clipping of gradients.  Each function allocates its results (and workspace) with torch, launches on the
-current stream of the tensors' device, and raises ``ValueError`` for shapes and dtypes that do not
+tensor cores, linear layers with bias, activation and residual, the norms around a block with its gate
+and residual, and the clipping of gradients.  Each function allocates its results (and workspace) with
+torch, launches on the current stream of the tensors' device, and raises ``ValueError`` for shapes and dtypes that do not
 fit together or ``binding.DipacoError`` with the library's status.  There is no CPU path.
 
 Autograd records nothing of these calls: the gradients are calls of their own.  A tensor that requires a
