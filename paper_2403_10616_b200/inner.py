@@ -385,8 +385,9 @@ def _gate(gate: Optional[torch.Tensor], rows: int, cols: int, dev: int, code: in
         if cols > 1 and gate.stride(0) != 1:
             raise ValueError("a gate of columns must be contiguous")
         return B.DIPACO_GATE_COLS, gate.data_ptr(), 0, own
-    if gate.shape == (rows, 1):
-        if rows > 1 and gate.stride(0) != 1:
+    in_steps = rows > 1 and gate.dim() == 2 and gate.stride(0) != 1
+    if gate.shape == (rows, 1) and not (in_steps and cols == 1):  # of one column: every value's, if rows are apart
+        if in_steps:
             raise ValueError("a gate of rows must be contiguous")
         return B.DIPACO_GATE_ROWS, gate.data_ptr(), 0, own
     if gate.shape == (rows, cols):

@@ -92,6 +92,24 @@ def test_an_infinity_at_a_row_s_end_counts_once_in_the_gradient_of_its_gate(cols
     assert torch.equal(got.f.cpu(), dz)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_gate_of_every_value_in_rows_of_one(dtype):
+    """It has the shape of a gate of rows, and is one where it lies like one."""
+    x, f, dn = (torch.randn(5, 1, generator=gen(i)).to(dtype).to(DEV) for i in range(3))
+    gate = (torch.rand(5, 1, generator=gen(3)) + 0.5).to(dtype)
+    together, apart = gate.to(DEV), place(gate, 3, 1)
+    results = []
+    for g in (together, apart):
+        z, n, stats = inner.residual_norm(x, f, gate=g, post_norm=False)
+        results.append((z, n, stats, *(t for t in inner.residual_norm_backward(dn, dn, f, z, stats, gate=g, post_norm=False)
+                                       if t is not None)))
+    assert results[0][5].dtype == F32 and results[1][5].dtype == dtype
+    for a, b in zip(*results):
+        assert torch.equal(a.to(b.dtype), b)
+    with pytest.raises(ValueError):
+        inner.residual_norm(x.expand(5, 2).contiguous(), f.expand(5, 2).contiguous(), gate=apart)
+
+
 MATRICES = ("x", "f", "dn", "dz", "gate", "z")
 
 
